@@ -95,7 +95,9 @@ enum {
   LBA_ERR_SCALE_LEN = -5, /* a scale length that is neither 1 nor the matching dimension     */
   LBA_ERR_CUDA = -6,      /* a CUDA call failed; see lba_last_cuda_error                     */
   LBA_ERR_WORKSPACE = -7, /* host-buffer entry points: workspace NULL, too small, misaligned */
-  LBA_ERR_STATIC_LIMIT = -8 /* lba_gemm_host_static: the problem needs more than LBA_STATIC_WORKSPACE_BYTES */
+  LBA_ERR_STATIC_LIMIT = -8, /* lba_gemm_host_static: the problem needs more than LBA_STATIC_WORKSPACE_BYTES */
+  LBA_ERR_LAYER = -9      /* lba_linear and its kin: an unknown activation or element type, a dropout outside [0, 1),
+                             or an option that the layer does not have                       */
 };
 
 /* GEMM  out[m][n] = epilogue( dot(A[m][:], B[n][:]) ), i.e. Y = X W^T with x_i = X_mi,
@@ -126,6 +128,46 @@ int lba_gemm_batched(const uint8_t* A, const uint8_t* B, const float* scale_a, i
                      int scale_b_len, const float* bias, int64_t batch, int64_t M, int64_t N, int64_t K,
                      int64_t stride_a, int64_t stride_b, int64_t stride_out, const lba_fmt* prod_fmt,
                      const lba_fmt* acc_fmt, int order, int chunk, float* out, void* stream);
+
+/* Layers: the same contraction with what a network does next in the kernel that forms it.  y is what lba_gemm computes, bit
+ * for bit, under the same formats, orders and loads; everything after it is binary32, one rounding per operation:
+ *     z = fl(fl(y*scale_a)*scale_b) (+ bias)
+ *     lba_linear   out = round( drop(act(z)) (+ residual) )
+ *     lba_gated    out = round( act(z_gate) * z_up )         two projections of the same rows
+ * drop: with dropout p > 0 an element is kept, times fl(1/(1-p)), where its 32-bit random word is at least floor(p 2^32 + 1/2),
+ * and is 0 elsewhere.  Words come from Philox4x32-10 (Salmon et al., SC 2011): row m, columns 4j..4j+3 take the four words of the
+ * counter (j, m, offset low, offset high) under the key (seed low, seed high); the mask is never stored, and the backward pass
+ * draws it again from the same two values.  A replayed graph draws the mask of the values that rng holds then. */
+enum { LBA_TYPE_F32 = 0, LBA_TYPE_BF16 = 1, LBA_TYPE_F16 = 2,
+       LBA_TYPE_CODES = 3 /* bytes of the call's own operand format, out / *out_scale to the nearest (ties to the even code,
+                             saturated; a NaN becomes the NaN code of E4M3 and the largest magnitude of M4E3) */ };
+enum { LBA_ACT_NONE = 0, LBA_ACT_RELU = 1, LBA_ACT_GELU = 2 /* z/2 (1 + erf(z/sqrt 2)) */,
+       LBA_ACT_GELU_TANH = 3 /* z/2 (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) */, LBA_ACT_SILU = 4 /* z / (1 + e^-z) */ };
+
+/* All zero: z itself, in binary32. */
+typedef struct {
+  int32_t activation;       /* LBA_ACT_*                                                              */
+  int32_t out_type;         /* LBA_TYPE_*: elements of out                                            */
+  const float* out_scale;   /* device, 1 value > 0, for LBA_TYPE_CODES                                */
+  void* preact;             /* device, or NULL: z for the backward pass, [M][N] (lba_gated: [2][M][N],
+                               the gate's first)                                                      */
+  const void* residual;     /* device, [M][N], or NULL (lba_linear only); may be out itself if the
+                               types are the same                                                     */
+  int32_t preact_type, residual_type;  /* LBA_TYPE_F32, BF16 or F16                                   */
+  double dropout;           /* p in [0, 1), lba_linear only; M is below 2^32 then                     */
+  const uint64_t* rng;      /* device, 2 values: seed, offset; needed for p > 0                       */
+} lba_layer;
+
+/* A, B, scales, bias, formats and order as for lba_gemm; layer: NULL means all zero; out: device, [M][N] of out_type. */
+int lba_linear(const uint8_t* A, const uint8_t* B, const float* scale_a, int scale_a_len, const float* scale_b,
+               int scale_b_len, const float* bias, int64_t M, int64_t N, int64_t K, const lba_fmt* prod_fmt,
+               const lba_fmt* acc_fmt, int order, int chunk, const lba_layer* layer, void* out, void* stream);
+
+/* B_gate, B_up [N][K] with scales of the same length (1 or N) each; both biases or neither (else LBA_ERR_NULL). */
+int lba_gated(const uint8_t* A, const uint8_t* B_gate, const uint8_t* B_up, const float* scale_a, int scale_a_len,
+              const float* scale_gate, const float* scale_up, int scale_b_len, const float* bias_gate,
+              const float* bias_up, int64_t M, int64_t N, int64_t K, const lba_fmt* prod_fmt, const lba_fmt* acc_fmt,
+              int order, int chunk, const lba_layer* layer, void* out, void* stream);
 
 /* Re-computation for the recursive overflow straight-through estimator (Sec. 4 and App. D): the forward pass is
  * deterministic, so the backward pass can replay it instead of storing one bit per FMAq.  For every output

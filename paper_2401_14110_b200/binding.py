@@ -23,7 +23,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblba.so")
 TORCH_LIB_PATH = os.path.join(_HERE, "lba_torch.so")
 
-EXPORTS = ["lba_gemm", "lba_gemm_batched", "lba_gemm_last_overflow", "lba_gemm_ste_mask", "lba_conv2d", "lba_gemm_host_workspace_bytes", "lba_gemm_host",
+EXPORTS = ["lba_gemm", "lba_gemm_batched", "lba_linear", "lba_gated", "lba_gemm_last_overflow", "lba_gemm_ste_mask", "lba_conv2d", "lba_gemm_host_workspace_bytes", "lba_gemm_host",
            "lba_conv2d_host_workspace_bytes", "lba_conv2d_host", "lba_gemm_host_static", "lba_count_nan_codes", "lba_describe_plan", "lba_describe_plan_batched",
            "lba_set_tile_override", "lba_status_string", "lba_last_cuda_error", "lba_version"]
 
@@ -38,6 +38,12 @@ class LbaError(RuntimeError):
 class _Fmt(C.Structure):
     _fields_ = [("man_bits", C.c_int32), ("exp_bits", C.c_int32), ("bias", C.c_int32), ("rounding", C.c_int32),
                 ("flags", C.c_int32)]
+
+
+class _Layer(C.Structure):
+    _fields_ = [("activation", C.c_int32), ("out_type", C.c_int32), ("out_scale", C.c_void_p), ("preact", C.c_void_p),
+                ("residual", C.c_void_p), ("preact_type", C.c_int32), ("residual_type", C.c_int32), ("dropout", C.c_double),
+                ("rng", C.c_void_p)]
 
 
 _lib = None
@@ -86,6 +92,9 @@ def load_library():
                                       C.c_void_p, C.c_void_p]
     lib.lba_gemm_batched.argtypes = gemm_args[:7] + [C.c_int64] * 7 + gemm_args[10:] + [C.c_void_p]
     lib.lba_gemm_host_static.argtypes = gemm_args + [C.c_void_p]
+    lib.lba_linear.argtypes = gemm_args[:14] + [C.POINTER(_Layer), C.c_void_p, C.c_void_p]
+    lib.lba_gated.argtypes = [C.c_void_p] * 4 + [C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p] + \
+        [C.c_int64] * 3 + gemm_args[10:14] + [C.POINTER(_Layer), C.c_void_p, C.c_void_p]
     conv_args = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_void_p] + [C.c_int] * 11 + \
         [C.POINTER(_Fmt), C.POINTER(_Fmt), C.c_int, C.c_int, C.c_void_p]
     lib.lba_conv2d.argtypes = conv_args + [C.c_void_p]
@@ -214,6 +223,126 @@ def lba_gemm_batched(A, B, scale_a, scale_b, bias, prod_fmt, acc_fmt, order=ORDE
                                 _dev(bias, torch.float32, "bias"), Z, M, N, K, M * K, stride_b, M * N, pf,
                                 af, order, chunk, _dev(out, torch.float32, "out"), _stream(stream)))
     return out
+
+
+_FLOAT_TYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+_OUT_TYPES = {**_FLOAT_TYPES, torch.uint8: 3}
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
+
+
+def _activation(name):
+    if name not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {', '.join(ACTIVATIONS)}, not {name!r}")
+    return ACTIVATIONS[name]
+
+
+def _typed(t, name):
+    """(data pointer, type number) of a contiguous CUDA tensor of 32- or 16-bit floats; (None, 0) for None."""
+    if t is None:
+        return None, 0
+    if not (isinstance(t, torch.Tensor) and t.dtype in _FLOAT_TYPES):
+        raise TypeError(f"{name} must be a float32, bfloat16 or float16 CUDA tensor")
+    return _dev(t, t.dtype, name), _FLOAT_TYPES[t.dtype]
+
+
+def _shaped(t, shape, name):
+    if t is not None and tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)}, not {tuple(t.shape)}")
+    return t
+
+
+def _same_device(first, *others):
+    if any(t is not None and t.device != first.device for t in others):
+        raise ValueError("all tensors of a call must be on one device")
+
+
+def _scale(t, name):
+    """(pointer, length) of a tensor of scales"""
+    ptr = _dev(t, torch.float32, name)
+    if ptr is None:
+        raise TypeError(f"{name} must be a contiguous CUDA tensor of dtype torch.float32")
+    return ptr, t.numel()
+
+
+def _rng(rng, dropout):
+    if not dropout:
+        return None
+    ptr = _dev(rng, torch.int64, "rng")
+    if ptr is None or rng.numel() != 2:
+        raise TypeError("rng must be a CUDA tensor of two int64 values (seed, offset) where dropout is not 0")
+    return ptr
+
+
+def _layer(out_shape, pre_shape, device, activation, out_dtype, out_scale, preact, out, residual=None, dropout=0.0, rng=None):
+    """The C struct of a layer's epilogue, and the output and pre-activation tensors that it points to."""
+    if out is None:
+        if out_dtype not in _OUT_TYPES:
+            raise TypeError("out_dtype must be torch.float32, bfloat16, float16, or uint8 for codes")
+        out = torch.empty(out_shape, dtype=out_dtype, device=device)
+    elif out.dtype not in _OUT_TYPES:
+        raise TypeError("out must be a float32, bfloat16, float16 or (codes) uint8 CUDA tensor")
+    _shaped(out, out_shape, "out")
+    if isinstance(preact, torch.dtype):
+        if preact not in _FLOAT_TYPES:
+            raise TypeError("preact must be torch.float32, bfloat16 or float16, a tensor of these, or None")
+        preact = torch.empty(pre_shape, dtype=preact, device=device)
+    pre, pre_type = _typed(_shaped(preact, pre_shape, "preact"), "preact")
+    res, res_type = _typed(_shaped(residual, out_shape, "residual"), "residual")
+    codes = out.dtype == torch.uint8
+    if codes and (out_scale is None or out_scale.numel() != 1):
+        raise TypeError("codes need out_scale, a CUDA tensor of one float32 value")
+    layer = _Layer(_activation(activation), _OUT_TYPES[out.dtype], _dev(out_scale, torch.float32, "out_scale") if codes else None, pre, res,
+                   pre_type, res_type, float(dropout), _rng(rng, dropout))
+    return layer, out, preact
+
+
+def lba_linear(A, B, scale_a, scale_b, bias, prod_fmt, acc_fmt, order=ORDER_CHUNKED, chunk=PAPER_CHUNK, activation="none",
+               residual=None, dropout=0.0, rng=None, out_dtype=torch.float32, out_scale=None, preact=None, out=None, stream=None):
+    """A linear layer: out[M][N] = round(drop(act(lba_gemm(A, B, ...))) + residual), in one kernel.  See ``lba_linear`` in lba.h.
+
+    ``activation``: "none", "relu", "gelu", "gelu_tanh" or "silu".  ``out_dtype``: float32, bfloat16, float16, or uint8 for codes
+    of the operands' own format, the output divided by ``out_scale`` (a tensor of one value).  ``dropout``: probability of
+    dropping an element, with ``rng`` an int64 CUDA tensor (seed, offset).  ``preact``: a float dtype, or a tensor to write: the
+    pre-activations that ``lba_linear_backward`` takes; the call then returns (out, preact)."""
+    lib = load_library()
+    M, K = A.shape
+    N, K2 = B.shape
+    if K != K2:
+        raise ValueError("A and B disagree on K")
+    _same_device(A, B, scale_a, scale_b, bias, residual, rng if dropout else None, out_scale, out, None if isinstance(preact, torch.dtype) else preact)
+    layer, out, pre = _layer((M, N), (M, N), A.device, activation, out_dtype, out_scale, preact, out, residual, dropout, rng)
+    sa, sa_len = _scale(scale_a, "scale_a")
+    sb, sb_len = _scale(scale_b, "scale_b")
+    _check(lib.lba_linear(_dev(A, torch.uint8, "A"), _dev(B, torch.uint8, "B"), sa, sa_len, sb, sb_len,
+                          _dev(_shaped(bias, (N,), "bias"), torch.float32, "bias"), M, N, K, _fmt_ref(prod_fmt), _fmt_ref(acc_fmt), order, chunk,
+                          C.byref(layer), _dev(out, out.dtype, "out"), _stream(stream)))
+    return out if pre is None else (out, pre)
+
+
+def lba_gated(A, B_gate, B_up, scale_a, scale_gate, scale_up, bias_gate, bias_up, prod_fmt, acc_fmt, order=ORDER_CHUNKED,
+              chunk=PAPER_CHUNK, activation="silu", out_dtype=torch.float32, out_scale=None, preact=None, out=None, stream=None):
+    """A gated feed-forward layer: out[M][N] = round(act(gate) * up) for the two projections gate = lba_gemm(A, B_gate, ...) and
+    up = lba_gemm(A, B_up, ...), in one kernel.  See ``lba_gated`` in lba.h.
+
+    ``preact``: a float dtype, or a tensor to write, [2][M][N]: both projections, as ``lba_gated_backward`` takes them; the call
+    then returns (out, preact).  The other arguments are those of ``lba_linear``."""
+    lib = load_library()
+    M, K = A.shape
+    N, K2 = B_gate.shape
+    if K != K2 or tuple(B_up.shape) != (N, K):
+        raise ValueError("A, B_gate and B_up disagree on K, or the two projections on N")
+    _same_device(A, B_gate, B_up, scale_a, scale_gate, scale_up, bias_gate, bias_up, out_scale, out, None if isinstance(preact, torch.dtype) else preact)
+    layer, out, pre = _layer((M, N), (2, M, N), A.device, activation, out_dtype, out_scale, preact, out)
+    sa, sa_len = _scale(scale_a, "scale_a")
+    sg, sg_len = _scale(scale_gate, "scale_gate")
+    su, su_len = _scale(scale_up, "scale_up")
+    if sg_len != su_len:
+        raise ValueError("scale_gate and scale_up must have the same length")
+    _check(lib.lba_gated(_dev(A, torch.uint8, "A"), _dev(B_gate, torch.uint8, "B_gate"), _dev(B_up, torch.uint8, "B_up"), sa, sa_len, sg, su,
+                         sg_len, _dev(_shaped(bias_gate, (N,), "bias_gate"), torch.float32, "bias_gate"),
+                         _dev(_shaped(bias_up, (N,), "bias_up"), torch.float32, "bias_up"), M, N, K, _fmt_ref(prod_fmt), _fmt_ref(acc_fmt), order,
+                         chunk, C.byref(layer), _dev(out, out.dtype, "out"), _stream(stream)))
+    return out if pre is None else (out, pre)
 
 
 def lba_gemm_last_overflow(A, B, prod_fmt, acc_fmt, out=None, stream=None):

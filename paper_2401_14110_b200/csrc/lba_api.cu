@@ -12,23 +12,29 @@
 
 namespace lba {
 
-// one definition per (QM, ORD), in the lba_fam_*.cu translation units
-#define LBA_DECL(QM, ORD) template <> cudaError_t launch_family<QM, ORD>(int, int, const Problem&, cudaStream_t);
+// one definition per (QM, ORD) and kind of problem, in the lba_fam_*.cu and lba_layer_*.cu translation units
+#define LBA_DECL(QM, ORD)                                                                          \
+  template <> cudaError_t launch_family<QM, ORD, Problem>(int, int, const Problem&, cudaStream_t); \
+  template <> cudaError_t launch_family<QM, ORD, LinearProblem>(int, int, const LinearProblem&, cudaStream_t);
 LBA_DECL(QM_FLOOR_FAST, ORD_SEQ) LBA_DECL(QM_FLOOR_FAST, ORD_CHUNK_SLAB) LBA_DECL(QM_FLOOR_FAST, ORD_CHUNK_ANY)
 LBA_DECL(QM_FLOOR_FAST, ORD_CHUNK16) LBA_DECL(QM_FLOOR_FULL, ORD_CHUNK16) LBA_DECL(QM_RNE_FULL, ORD_CHUNK16)
 LBA_DECL(QM_FLOOR_FULL, ORD_SEQ) LBA_DECL(QM_FLOOR_FULL, ORD_CHUNK_SLAB) LBA_DECL(QM_FLOOR_FULL, ORD_CHUNK_ANY)
 LBA_DECL(QM_RNE_FULL, ORD_SEQ) LBA_DECL(QM_RNE_FULL, ORD_CHUNK_SLAB) LBA_DECL(QM_RNE_FULL, ORD_CHUNK_ANY)
 LBA_DECL(QM_RNE_WIDE, ORD_SEQ) LBA_DECL(QM_RNE_WIDE, ORD_CHUNK_SLAB) LBA_DECL(QM_RNE_WIDE, ORD_CHUNK_ANY)
 #undef LBA_DECL
-template <> cudaError_t launch_small<0>(int, int, const Problem&, cudaStream_t);
-template <> cudaError_t launch_small<1>(int, int, const Problem&, cudaStream_t);
-template <> cudaError_t launch_small<2>(int, int, const Problem&, cudaStream_t);
+#define LBA_DECL(RNE)                                                                          \
+  template <> cudaError_t launch_small<RNE, Problem>(int, int, const Problem&, cudaStream_t); \
+  template <> cudaError_t launch_small<RNE, LinearProblem>(int, int, const LinearProblem&, cudaStream_t);
+LBA_DECL(0) LBA_DECL(1) LBA_DECL(2)
+#undef LBA_DECL
 
 cudaError_t launch_last_overflow(bool small, int qm, int load, const Problem& p, cudaStream_t stream);
 cudaError_t launch_ste_mask(bool small, int qm, int ord, int diff, int load, const Problem& p, cudaStream_t stream);
 cudaError_t launch_ste_packed(bool small, int pq, int chunk16, int load, const Problem& p, cudaStream_t stream);
 cudaError_t launch_fixed(int ord, int load, const Problem& p, cudaStream_t stream);
+cudaError_t launch_fixed(int ord, int load, const LinearProblem& p, cudaStream_t stream);
 cudaError_t launch_cluster_pair(int pq, int load, const Problem& p, cudaStream_t stream);
+cudaError_t launch_cluster_pair(int pq, int load, const LinearProblem& p, cudaStream_t stream);
 
 namespace {
 
@@ -40,17 +46,18 @@ int cuda_fail(cudaError_t e) {
   return LBA_ERR_CUDA;
 }
 
-const LaunchFn kLaunch[QM_COUNT][ORD_COUNT] = {
+template <class P>
+const LaunchFn<P> kLaunch[QM_COUNT][ORD_COUNT] = {
     // last column: chunk == 16 has a kernel of its own only for the floor quantisers (the plan never
     // selects it for the others; their entries repeat the general chunk-of-slabs family)
-    {launch_family<QM_FLOOR_FAST, ORD_SEQ>, launch_family<QM_FLOOR_FAST, ORD_CHUNK_SLAB>,
-     launch_family<QM_FLOOR_FAST, ORD_CHUNK_ANY>, launch_family<QM_FLOOR_FAST, ORD_CHUNK16>},
-    {launch_family<QM_FLOOR_FULL, ORD_SEQ>, launch_family<QM_FLOOR_FULL, ORD_CHUNK_SLAB>,
-     launch_family<QM_FLOOR_FULL, ORD_CHUNK_ANY>, launch_family<QM_FLOOR_FULL, ORD_CHUNK16>},
-    {launch_family<QM_RNE_FULL, ORD_SEQ>, launch_family<QM_RNE_FULL, ORD_CHUNK_SLAB>,
-     launch_family<QM_RNE_FULL, ORD_CHUNK_ANY>, launch_family<QM_RNE_FULL, ORD_CHUNK16>},
-    {launch_family<QM_RNE_WIDE, ORD_SEQ>, launch_family<QM_RNE_WIDE, ORD_CHUNK_SLAB>,
-     launch_family<QM_RNE_WIDE, ORD_CHUNK_ANY>, launch_family<QM_RNE_WIDE, ORD_CHUNK_SLAB>},
+    {launch_family<QM_FLOOR_FAST, ORD_SEQ, P>, launch_family<QM_FLOOR_FAST, ORD_CHUNK_SLAB, P>,
+     launch_family<QM_FLOOR_FAST, ORD_CHUNK_ANY, P>, launch_family<QM_FLOOR_FAST, ORD_CHUNK16, P>},
+    {launch_family<QM_FLOOR_FULL, ORD_SEQ, P>, launch_family<QM_FLOOR_FULL, ORD_CHUNK_SLAB, P>,
+     launch_family<QM_FLOOR_FULL, ORD_CHUNK_ANY, P>, launch_family<QM_FLOOR_FULL, ORD_CHUNK16, P>},
+    {launch_family<QM_RNE_FULL, ORD_SEQ, P>, launch_family<QM_RNE_FULL, ORD_CHUNK_SLAB, P>,
+     launch_family<QM_RNE_FULL, ORD_CHUNK_ANY, P>, launch_family<QM_RNE_FULL, ORD_CHUNK16, P>},
+    {launch_family<QM_RNE_WIDE, ORD_SEQ, P>, launch_family<QM_RNE_WIDE, ORD_CHUNK_SLAB, P>,
+     launch_family<QM_RNE_WIDE, ORD_CHUNK_ANY, P>, launch_family<QM_RNE_WIDE, ORD_CHUNK_SLAB, P>},
 };
 
 const char* const kQmName[QM_COUNT] = {"floor_fast", "floor_full", "rne_full", "rne_wide"};
@@ -577,7 +584,8 @@ void apply_plan(Problem* p, const Plan& pl) {
 
 bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15) == 0; }
 
-int run(const Problem& p, const Plan& pl, int load, cudaStream_t stream) {
+template <class P>
+int run(const P& p, const Plan& pl, int load, cudaStream_t stream) {
   if (p.M == 0 || p.N == 0 || p.batch == 0) return LBA_OK;
   if (p.batch > 65535) return LBA_ERR_SHAPE;
   if (pl.fixed) {  // Eq. 1: the integer kernel, one tile shape
@@ -599,14 +607,14 @@ int run(const Problem& p, const Plan& pl, int load, cudaStream_t stream) {
   const TileInfo ti = tile_info(tile);
   if (!grid_fits(p.M, p.N, ti.bm, ti.bn)) return LBA_ERR_SHAPE;
   if (pl.fused && pl.ord != ORD_CHUNK_ANY) {  // the plain packed tiles have the fused variant
-    Problem q = p;
+    P q = p;
     q.pq = PQ_FUSED;
     q.pk_b = pl.pk_b_fused;  // carries the accumulator's scaling in every step
     q.pk_a0 = pl.pk_a;
-    const cudaError_t e = kLaunch[pl.qm][pl.ord](tile, load, q, stream);
+    const cudaError_t e = kLaunch<P>[pl.qm][pl.ord](tile, load, q, stream);
     return e == cudaSuccess ? LBA_OK : cuda_fail(e);
   }
-  const cudaError_t e = kLaunch[pl.qm][pl.ord](tile, load, p, stream);
+  const cudaError_t e = kLaunch<P>[pl.qm][pl.ord](tile, load, p, stream);
   return e == cudaSuccess ? LBA_OK : cuda_fail(e);
 }
 
@@ -634,6 +642,46 @@ __global__ void count_nan_codes_kernel(const uint8_t* codes, int64_t n, unsigned
   for (int64_t i = (int64_t)blockIdx.x * blockDim.x + threadIdx.x; i < n; i += (int64_t)gridDim.x * blockDim.x)
     local += (codes[i] & 0x7F) == 0x7F;
   if (local) atomicAdd(count, local);
+}
+
+// ------------------------------------------------------------------ layers
+bool float_type(int t) { return t == LBA_TYPE_F32 || t == LBA_TYPE_BF16 || t == LBA_TYPE_F16; }
+
+int drop_constants(double p, const uint64_t* rng, int64_t M, uint32_t* below, float* scale) {
+  *below = 0;
+  *scale = 1.0f;
+  if (!(p >= 0.0 && p < 1.0)) return LBA_ERR_LAYER;
+  const uint64_t t = (uint64_t)(p * 4294967296.0 + 0.5);
+  if (t == 0) return LBA_OK;  // keeps everything
+  if (t > 0xFFFFFFFFull) return LBA_ERR_LAYER;
+  if (!rng) return LBA_ERR_NULL;
+  if (M > 0xFFFFFFFFLL) return LBA_ERR_SHAPE;  // a row's number is one word of the generator's counter
+  *below = (uint32_t)t;
+  *scale = (float)(1.0 / (1.0 - p));
+  return LBA_OK;
+}
+
+// the epilogue's fields; p->n, M and in_m4e3 are set
+int fill_layer(LinearProblem* p, const lba_layer* l, void* out) {
+  static const lba_layer kPlain = {};
+  if (!l) l = &kPlain;
+  if (l->activation < 0 || l->activation >= ACT_COUNT || l->out_type < 0 || l->out_type >= LT_COUNT) return LBA_ERR_LAYER;
+  if ((l->residual && !float_type(l->residual_type)) || (l->preact && !float_type(l->preact_type))) return LBA_ERR_LAYER;
+  if (l->out_type == LBA_TYPE_CODES && !l->out_scale) return LBA_ERR_NULL;
+  if (p->gated && (l->residual || l->dropout != 0.0)) return LBA_ERR_LAYER;
+  const int st = drop_constants(l->dropout, l->rng, p->M, &p->drop_below, &p->keep_scale);
+  if (st != LBA_OK) return st;
+  if (p->M > 0 && p->n > 0 && !out) return LBA_ERR_NULL;
+  p->act = l->activation;
+  p->residual = l->residual;
+  p->residual_type = l->residual_type;
+  p->dst = out;
+  p->dst_type = l->out_type;
+  p->pre = l->preact;
+  p->pre_type = l->preact_type;
+  p->out_scale = l->out_scale;
+  p->rng = l->rng;
+  return LBA_OK;
 }
 
 size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
@@ -672,6 +720,7 @@ const char* lba_status_string(int status) {
     case LBA_ERR_SCALE_LEN: return "scale length must be 1 or the matching dimension";
     case LBA_ERR_CUDA: return "a CUDA call failed (see lba_last_cuda_error)";
     case LBA_ERR_WORKSPACE: return "workspace missing, too small or misaligned";
+    case LBA_ERR_LAYER: return "unknown activation or element type, dropout outside [0, 1), or an option that a gated layer does not have";
     case LBA_ERR_STATIC_LIMIT: return "problem too large for the built-in workspace of lba_gemm_host_static (LBA_STATIC_WORKSPACE_BYTES)";
     default: return "unknown status";
   }
@@ -698,6 +747,58 @@ int lba_gemm(const uint8_t* A, const uint8_t* B, const float* scale_a, int scale
   p.out = out;
   apply_plan(&p, pl);
   const bool vec = K % BK == 0 && aligned16(A) && aligned16(B);
+  return run(p, pl, vec ? LD_GEMM_VEC : LD_GEMM_ROWS, (cudaStream_t)stream);
+}
+
+int lba_linear(const uint8_t* A, const uint8_t* B, const float* scale_a, int scale_a_len, const float* scale_b, int scale_b_len,
+               const float* bias, int64_t M, int64_t N, int64_t K, const lba_fmt* prod_fmt, const lba_fmt* acc_fmt, int order, int chunk,
+               const lba_layer* layer, void* out, void* stream) {
+  if (M < 0 || N < 0 || K < 0 || K > 2147483647LL) return LBA_ERR_SHAPE;
+  Plan pl;
+  int st = make_plan(prod_fmt, acc_fmt, order, chunk, K, &pl);
+  if (st != LBA_OK) return st;
+  LinearProblem p;
+  std::memset(&p, 0, sizeof(p));
+  p.M = M;
+  p.N = p.n = N;
+  p.K = K;
+  p.batch = 1;
+  if ((st = fill_scales(&p, scale_a, scale_a_len, scale_b, scale_b_len, bias)) != LBA_OK) return st;
+  if ((st = fill_layer(&p, layer, out)) != LBA_OK) return st;
+  if (K > 0 && ((M > 0 && !A) || (N > 0 && !B))) return LBA_ERR_NULL;
+  p.A = A;
+  p.B = B;
+  apply_plan(&p, pl);
+  const bool vec = K % BK == 0 && aligned16(A) && aligned16(B);
+  return run(p, pl, vec ? LD_GEMM_VEC : LD_GEMM_ROWS, (cudaStream_t)stream);
+}
+
+int lba_gated(const uint8_t* A, const uint8_t* B_gate, const uint8_t* B_up, const float* scale_a, int scale_a_len, const float* scale_gate,
+              const float* scale_up, int scale_b_len, const float* bias_gate, const float* bias_up, int64_t M, int64_t N, int64_t K,
+              const lba_fmt* prod_fmt, const lba_fmt* acc_fmt, int order, int chunk, const lba_layer* layer, void* out, void* stream) {
+  if (M < 0 || N < 0 || K < 0 || K > 2147483647LL || N > INT64_MAX / 2) return LBA_ERR_SHAPE;
+  Plan pl;
+  int st = make_plan(prod_fmt, acc_fmt, order, chunk, K, &pl);
+  if (st != LBA_OK) return st;
+  LinearProblem p;
+  std::memset(&p, 0, sizeof(p));
+  p.gated = 1;
+  p.M = M;
+  p.N = p.n = N;
+  p.K = K;
+  p.batch = 1;
+  if ((st = fill_scales(&p, scale_a, scale_a_len, scale_gate, scale_b_len, bias_gate)) != LBA_OK) return st;
+  if (!scale_up || !bias_gate != !bias_up) return LBA_ERR_NULL;  // both biases or neither
+  if ((st = fill_layer(&p, layer, out)) != LBA_OK) return st;
+  if (K > 0 && ((M > 0 && !A) || (N > 0 && (!B_gate || !B_up)))) return LBA_ERR_NULL;
+  p.A = A;
+  p.B = B_gate;
+  p.B2 = B_up;
+  p.sb2 = scale_up;
+  p.bias2 = bias_up;
+  p.N = 2 * N;  // columns of the contraction
+  apply_plan(&p, pl);
+  const bool vec = K % BK == 0 && aligned16(A) && aligned16(B_gate) && aligned16(B_up);
   return run(p, pl, vec ? LD_GEMM_VEC : LD_GEMM_ROWS, (cudaStream_t)stream);
 }
 

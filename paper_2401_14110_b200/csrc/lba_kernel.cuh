@@ -328,7 +328,8 @@ __device__ __forceinline__ u64 add2_rz_ftz(u64 a, u64 b) {
 __device__ __forceinline__ void after_previous() {
   asm volatile("griddepcontrol.wait;" ::: "memory");
 }
-inline cudaError_t launch_after(void (*kernel)(const Problem), dim3 grid, int threads, size_t smem, cudaStream_t stream, const Problem& p,
+template <class P>
+inline cudaError_t launch_after(void (*kernel)(const P), dim3 grid, int threads, size_t smem, cudaStream_t stream, const P& p,
                                 int cluster = 1) {
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = grid;
@@ -351,6 +352,17 @@ inline cudaError_t launch_after(void (*kernel)(const Problem), dim3 grid, int th
 }
 
 // ------------------------------------------------------------------ operand fetch
+// Row n of B, as the kernels count it: its operand's first row, its number there and how many rows that has (a gated layer has
+// two operands in turn; lba_layer.cuh)
+struct LinearProblem;
+template <int BM, int BN, int TM, int TN>
+__device__ __forceinline__ void layer_store_tile(const LinearProblem& p, int64_t m0, int64_t n0, int tx, int ty, const float (&s)[TM][TN]);
+template <int W>
+__device__ __forceinline__ void layer_store_sums(const LinearProblem& p, int64_t m, int64_t n, const float (&s)[W]);
+__device__ __forceinline__ const uint8_t* b_base(const Problem&, const uint8_t* b, int64_t) { return b; }
+__device__ __forceinline__ int64_t b_row(const Problem&, int64_t n) { return n; }
+__device__ __forceinline__ int64_t b_rows(const Problem& p) { return p.N; }
+
 // Each thread fetches, per slab, 16-byte pieces of the rows r = tid + l*NT of the CTA's A tile
 // (r < BM) and B tile (BM <= r < BM + BN).  Rows past the matrix edge and padded convolution taps
 // read as zero bytes, i.e. the value 0.
@@ -371,7 +383,8 @@ struct RowLoader {
   // bytes of the input row ih0 + kh; the cursor is (kh, offset inside that run) of the next slab's first k
   int any_kh = 0, any_off = 0;
 
-  __device__ __forceinline__ void init(const Problem& p, int tid, int64_t m0, int64_t n0) {
+  template <class P>
+  __device__ __forceinline__ void init(const P& p, int tid, int64_t m0, int64_t n0) {
     const uint8_t* const baseA = p.A + (int64_t)blockIdx.z * p.batch_a;
     const uint8_t* const baseB = p.B + (int64_t)blockIdx.z * p.batch_b;
 #pragma unroll
@@ -407,8 +420,8 @@ struct RowLoader {
         const int64_t n = n0 + (r - BM);
         if (n < p.N) {
           row_ok[l] = true;
-          if constexpr (LD == LD_GEMM_ROWS) init_row(p, l, baseB, n, p.N);
-          else row_ptr[l] = baseB + n * p.K;
+          if constexpr (LD == LD_GEMM_ROWS) init_row(p, l, b_base(p, baseB, n), b_row(p, n), b_rows(p));
+          else row_ptr[l] = b_base(p, baseB, n) + b_row(p, n) * p.K;
         }
       }
     }
@@ -576,8 +589,9 @@ struct RowLoader {
 // [M][ceil(chunks/32)][N] holds the bits of the folds T <- Q_acc(C + T), the chunk sum C in the product's place.
 enum { TRACK_NONE = 0, TRACK_LAST_OF = 1, TRACK_MASK_OF = 2, TRACK_MASK_DIFF = 3 };
 
-template <int BM, int BN, int TM, int TN, int QM, int ORD, int LD, int TRACK = TRACK_NONE>
-__global__ void __launch_bounds__((BM / TM) * (BN / TN), TRACK == TRACK_MASK_DIFF ? 2 : 1) lba_contract_kernel(const Problem p) {
+// P: Problem, or LinearProblem for the layers of lba_layer.cuh, whose epilogue replaces this kernel's.
+template <int BM, int BN, int TM, int TN, int QM, int ORD, int LD, int TRACK = TRACK_NONE, class P = Problem>
+__global__ void __launch_bounds__((BM / TM) * (BN / TN), TRACK == TRACK_MASK_DIFF ? 2 : 1) lba_contract_kernel(const P p) {
   static_assert(TRACK == TRACK_NONE || QM == QM_FLOOR_FULL || QM == QM_FLOOR_FAST, "tracking variants use the floor quantisers");
   static_assert(TRACK != TRACK_LAST_OF || ORD == ORD_SEQ, "last-overflow index: sequential order");
   static_assert(TRACK == TRACK_NONE || ORD != ORD_CHUNK16, "tracking variants: generic orders");
@@ -895,6 +909,16 @@ __global__ void __launch_bounds__((BM / TM) * (BN / TN), TRACK == TRACK_MASK_DIF
     return;
   }
 
+  if constexpr (std::is_same<P, LinearProblem>::value) {
+    float sums[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) sums[i][j] = CHUNKED ? acc2[CHUNKED ? i : 0][CHUNKED ? j : 0] : acc1[i][j];
+    layer_store_tile<BM, BN, TM, TN>(p, m0, n0, tx, ty, sums);
+    return;
+  }
+
   // ---- epilogue: back to real values, +0 for every zero, scales and bias in binary32
   float* const outz = p.out + (int64_t)blockIdx.z * p.batch_out;
   const bool vec_store = (p.N % 4 == 0) && ((reinterpret_cast<uintptr_t>(outz) & 15) == 0);
@@ -1085,13 +1109,13 @@ enum PackedProd { PQ_NONE = 0, PQ_MASK = 1, PQ_MASK_SAT = 2, PQ_FUSED = 3, PQ_CU
 // one cluster barrier per pair of chunks.  H16: the chunk sums travel as bfloat16 pairs, which a value with at most 7
 // mantissa bits is exactly (half the traffic, 2 % faster); otherwise as binary32 words.
 // This doubles the CTAs of a small problem without splitting any sequential chain, and both CTAs do the same work.
-template <int BM, int BN, int TM, int TN, int PQ, int RNE, int ORD, int LD, int STE = 0, int CL = 1, bool H16 = false>
+template <int BM, int BN, int TM, int TN, int PQ, int RNE, int ORD, int LD, int STE = 0, int CL = 1, bool H16 = false, class P = Problem>
 __global__ void __launch_bounds__((BM / TM) * (BN / TN),
                                   ((TM * TN == 64 && ORD != ORD_CHUNK_SLAB && !RNE) || (TM * TN == 32 && ORD == ORD_CHUNK16) ||
                                    (TM * TN == 32 && ORD == ORD_CHUNK_SLAB && LD == LD_CONV_ANY && (PQ == PQ_MASK || PQ == PQ_MASK_SAT || PQ == PQ_CUT_ANY) && !RNE) ||
                                    ((LD == LD_CONV_ANY || LD == LD_GEMM_ROWS || STE != 0) && !RNE && ORD != ORD_CHUNK_SLAB))
                                       ? 512 / ((BM / TM) * (BN / TN)) : 1)
-    lba_contract_packed_kernel(const Problem p) {
+    lba_contract_packed_kernel(const P p) {
   static_assert(STE == 0 || (!RNE && TM == 4 && (ORD == ORD_SEQ || ORD == ORD_CHUNK16)), "mask variant");
   static_assert(!RNE || PQ != PQ_CUT_ANY, "nearest-even has one cut");
   static_assert(CL == 1 || LD == LD_GEMM_VEC || LD == LD_CONV_VEC, "a CTA of the pair skips slabs");
@@ -1753,6 +1777,17 @@ __global__ void __launch_bounds__((BM / TM) * (BN / TN),
     }
 
     // ---- epilogue of the pair: this CTA's column half
+    if constexpr (std::is_same<P, LinearProblem>::value) {
+      float sums[TM][4];
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < HP; ++j) unpack2(T[i][j], sums[i][2 * j], sums[i][2 * j + 1]);
+#pragma unroll 1
+      for (int i = 0; i < TM; ++i)
+        if (m0 + ty * 4 + i < p.M) layer_store_sums<4>(p, m0 + ty * 4 + i, n0 + (int64_t)crank * (BN / 2) + tx * 4, sums[i]);
+      return;
+    }
     float* const outz = p.out + (int64_t)blockIdx.z * p.batch_out;
     const bool vec_store = (p.N % 4 == 0) && ((reinterpret_cast<uintptr_t>(outz) & 15) == 0);
     const int64_t n = n0 + (int64_t)crank * (BN / 2) + tx * 4;
@@ -1853,6 +1888,17 @@ __global__ void __launch_bounds__((BM / TM) * (BN / TN),
 
   if constexpr (STE != 0) return;  // the masks are the output
 
+  if constexpr (std::is_same<P, LinearProblem>::value) {
+    float sums[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < PN; ++j)
+        unpack2(T_IN_REGS ? acc2[T_IN_REGS ? i : 0][T_IN_REGS ? j : 0] : acc1[i][j], sums[i][2 * j], sums[i][2 * j + 1]);
+    layer_store_tile<BM, BN, TM, TN>(p, m0, n0, tx, ty, sums);
+    return;
+  }
+
   // ---- epilogue: back to real values, +0 for every zero, scales and bias in binary32
   float* const outz = p.out + (int64_t)blockIdx.z * p.batch_out;
   const bool vec_store = (p.N % 4 == 0) && ((reinterpret_cast<uintptr_t>(outz) & 15) == 0);
@@ -1929,9 +1975,10 @@ __host__ inline TileInfo tile_info(int t) {
   return tab[t];
 }
 
-typedef cudaError_t (*LaunchFn)(int tile, int load, const Problem& p, cudaStream_t stream);
+template <class P>
+using LaunchFn = cudaError_t (*)(int tile, int load, const P& p, cudaStream_t stream);
 
-template <int QM, int ORD>
-cudaError_t launch_family(int tile, int load, const Problem& p, cudaStream_t stream);
+template <int QM, int ORD, class P>
+cudaError_t launch_family(int tile, int load, const P& p, cudaStream_t stream);
 
 }  // namespace lba

@@ -15,6 +15,7 @@
 // lanes put two lanes of every quarter-warp on the same banks); orders and loaders as in the scalar kernel.
 #pragma once
 #include "lba_kernel.cuh"
+#include "lba_layer.cuh"
 
 namespace lba {
 
@@ -34,8 +35,8 @@ __device__ __forceinline__ int fx_sar(int v, int count) {
 
 // HOLD_P: 0 = the host proved that no product leaves the product format's range (Q_prod is the floor alone),
 // 1 = saturate, 2 = wrap around.
-template <int ORD, int LD, int HOLD_P, bool WRAP_A>
-__global__ void __launch_bounds__(256) lba_fixed_kernel(const Problem p) {
+template <int ORD, int LD, int HOLD_P, bool WRAP_A, class P = Problem>
+__global__ void __launch_bounds__(256) lba_fixed_kernel(const P p) {
   constexpr int BM = 64, BN = 64, TM = 4, TN = 4, NT = 256, TX = BN / TN;
   constexpr int ROWS = BM + BN;
   constexpr int LPT = (ROWS + NT - 1) / NT;
@@ -181,6 +182,18 @@ __global__ void __launch_bounds__(256) lba_fixed_kernel(const Problem p) {
   }
   if (ORD == ORD_CHUNK_SLAB && slabs_in_chunk > 0) close_chunk();
   if (ORD == ORD_CHUNK_ANY && k_in_chunk > 0) close_chunk();
+
+  if constexpr (std::is_same<P, LinearProblem>::value) {
+    float sums[TM][TN];
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) sums[i][j] = __fmul_rn(__int2float_rn(CHUNKED ? acc2[CHUNKED ? i : 0][CHUNKED ? j : 0] : acc1[i][j]), p.fx_unit);
+#pragma unroll 1
+    for (int i = 0; i < TM; ++i)
+      if (m0 + ty * 4 + i < p.M) layer_store<TN>(p, m0 + ty * 4 + i, n0 + tx * 4, sums[i]);
+    return;
+  }
 
   // ---- epilogue: integer -> binary32 (exact, B <= 24), * 2^-b_acc, scales and bias in binary32
   float* const outz = p.out + (int64_t)blockIdx.z * p.batch_out;

@@ -11,6 +11,7 @@
 // Results are those of the packed kernel bit for bit: the same steps, in the same order.
 #pragma once
 #include "lba_kernel.cuh"
+#include "lba_layer.cuh"
 
 namespace lba {
 
@@ -121,8 +122,8 @@ struct SplitShape {
   static constexpr size_t SMEM = G * (A_BYTES + B_BYTES) + sizeof(float) * 2 * G * BM * BN;
 };
 
-template <int BM, int BN, int TM, int TN, int G, bool SAT, int RNE, int LD>
-__global__ void __launch_bounds__(32 * G) lba_split_kernel(const Problem p) {
+template <int BM, int BN, int TM, int TN, int G, bool SAT, int RNE, int LD, class P = Problem>
+__global__ void __launch_bounds__(32 * G) lba_split_kernel(const P p) {
   typedef SplitShape<BM, BN, TM, TN, G> S;
   constexpr int TX = BN / TN, PN = TN / 2, OUTS = S::OUTS;
   typedef RowLoader<BM, BN, 32, LD> Loader;
@@ -230,6 +231,10 @@ __global__ void __launch_bounds__(32 * G) lba_split_kernel(const Problem p) {
   float o[OUTS];
 #pragma unroll
   for (int i = 0; i < OUTS / 2; ++i) unpack2(t2[i], o[2 * i], o[2 * i + 1]);
+  if constexpr (std::is_same<P, LinearProblem>::value) {
+    layer_store_sums<OUTS>(p, m, n, o);
+    return;
+  }
   const float sa = p.sa[p.sa_per_row ? m : 0];
   float* const dst = p.out + (int64_t)blockIdx.z * p.batch_out + m * p.N + n;
 #pragma unroll
@@ -255,8 +260,8 @@ __global__ void __launch_bounds__(32 * G) lba_split_kernel(const Problem p) {
 constexpr int CHAIN_SLABS = 4;
 constexpr int CHAIN_THREADS = 128 + 32 * CHAIN_SLABS;
 
-template <bool SAT, int RNE, int LD>
-__global__ void __launch_bounds__(CHAIN_THREADS) lba_chain_kernel(const Problem p) {
+template <bool SAT, int RNE, int LD, class P = Problem>
+__global__ void __launch_bounds__(CHAIN_THREADS) lba_chain_kernel(const P p) {
   constexpr int BM = 16, BN = 16, RING = 3 * CHAIN_SLABS;
   typedef RowLoader<BM, BN, 32, LD> Loader;
   static_assert(Loader::LPT == 1, "a lane decodes one row");
@@ -371,6 +376,10 @@ __global__ void __launch_bounds__(CHAIN_THREADS) lba_chain_kernel(const Problem 
   float* const dst = p.out + (int64_t)blockIdx.z * p.batch_out + m * p.N + n;
   float o[2];
   unpack2(acc, o[0], o[1]);
+  if constexpr (std::is_same<P, LinearProblem>::value) {
+    layer_store_sums<2>(p, m, n, o);
+    return;
+  }
   const bool both = n + 1 < p.N;
   if (n < p.N) o[0] = finish(p, o[0], sa, n);
   if (both) o[1] = finish(p, o[1], sa, n + 1);
@@ -382,7 +391,7 @@ __global__ void __launch_bounds__(CHAIN_THREADS) lba_chain_kernel(const Problem 
   }
 }
 
-template <int RNE>
-cudaError_t launch_small(int tile, int load, const Problem& p, cudaStream_t stream);
+template <int RNE, class P>
+cudaError_t launch_small(int tile, int load, const P& p, cudaStream_t stream);
 
 }  // namespace lba

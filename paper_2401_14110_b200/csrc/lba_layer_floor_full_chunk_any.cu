@@ -1,0 +1,4 @@
+#define LBA_PROBLEM LinearProblem
+#define LBA_QM lba::QM_FLOOR_FULL
+#define LBA_ORD lba::ORD_CHUNK_ANY
+#include "lba_family.inc"
