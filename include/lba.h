@@ -169,6 +169,45 @@ int lba_gated(const uint8_t* A, const uint8_t* B_gate, const uint8_t* B_up, cons
               const float* bias_up, int64_t M, int64_t N, int64_t K, const lba_fmt* prod_fmt, const lba_fmt* acc_fmt,
               int order, int chunk, const lba_layer* layer, void* out, void* stream);
 
+/* Backward pass of the two layers under the straight-through estimator of Sec. 3: the quantisers (Q_prod, Q_acc and those of the
+ * operands) pass the gradient.  With g = grad_out, z (and v, the up projection) the pre-activations that the forward call kept:
+ *     linear   dz = drop(g) act'(z)
+ *     gated    dz = g v act'(z) for the gate, g act(z) for the up projection
+ *     grad_a[m][k] = sum_n dz[m][n] scale_b[n] B[n][k]  (gated: over both projections): with respect to scale_a A
+ *     grad_b[n][k] = sum_m dz[m][n] scale_a[m] A[m][k]: with respect to scale_b B        grad_bias[n] = sum_m dz[m][n]
+ * act' of LBA_ACT_RELU is 0 at 0.  The residual's gradient is g itself.  Products run on the tensor cores with binary32 sums; the
+ * codes are exact there, dz is rounded to 8 significant bits for bfloat16 gradients, to 16 for binary16 ones and not at all for
+ * binary32 ones.  Sums are formed in a fixed order: a repeated call gives the same bits. */
+typedef struct {
+  int32_t activation;       /* LBA_ACT_*, as in the forward call                                      */
+  int32_t grad_type;        /* LBA_TYPE_F32, BF16 or F16: elements of grad_out                        */
+  int32_t out_type;         /* the same choice for grad_a and grad_b (grad_bias is binary32)          */
+  int32_t preact_type;      /* and for preact                                                         */
+  const void* preact;       /* device, as the forward call wrote it; may be NULL for lba_linear
+                               without an activation                                                  */
+  double dropout;           /* as in the forward call, with the same two values behind rng            */
+  const uint64_t* rng;
+  int32_t input_flags;      /* LBA_FLAG_INPUT_M4E3 or 0: the operands' byte format                    */
+} lba_backward;
+
+/* Device workspace, 256-byte aligned, of lba_backward_workspace_bytes bytes (0 for rejected arguments, and where none is needed);
+ * needs: which outputs the call asks for.  It holds nothing between calls; calls that may overlap need one each. */
+enum { LBA_NEEDS_A = 1, LBA_NEEDS_B = 2, LBA_NEEDS_BIAS = 4 };
+size_t lba_backward_workspace_bytes(int gated, int64_t M, int64_t N, int64_t K, int scale_a_len, int scale_b_len,
+                                    const lba_backward* how, int needs);
+
+/* grad_out [M][N]; outputs grad_a [M][K], grad_b [N][K], grad_bias [N], each NULL if it is not wanted (a gated layer's two
+ * projections: both or neither).  M and K are at most 2^31 - 1, N 2^30 - 1. */
+int lba_linear_backward(const void* grad_out, const uint8_t* A, const uint8_t* B, const float* scale_a, int scale_a_len,
+                        const float* scale_b, int scale_b_len, int64_t M, int64_t N, int64_t K, const lba_backward* how,
+                        void* grad_a, void* grad_b, float* grad_bias, void* workspace, size_t workspace_bytes,
+                        void* stream);
+int lba_gated_backward(const void* grad_out, const uint8_t* A, const uint8_t* B_gate, const uint8_t* B_up,
+                       const float* scale_a, int scale_a_len, const float* scale_gate, const float* scale_up,
+                       int scale_b_len, int64_t M, int64_t N, int64_t K, const lba_backward* how, void* grad_a,
+                       void* grad_gate, void* grad_up, float* grad_bias_gate, float* grad_bias_up, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
 /* Re-computation for the recursive overflow straight-through estimator (Sec. 4 and App. D): the forward pass is
  * deterministic, so the backward pass can replay it instead of storing one bit per FMAq.  For every output
  * (m, n), in SEQUENTIAL order, last[m][n] is the largest step index i with

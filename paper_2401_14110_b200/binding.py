@@ -17,13 +17,13 @@ import warnings
 import torch
 
 from .build import torch_tag
-from .formats import LbaFormat, ORDER_CHUNKED, PAPER_CHUNK
+from .formats import FLAG_INPUT_M4E3, LbaFormat, ORDER_CHUNKED, PAPER_CHUNK
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblba.so")
 TORCH_LIB_PATH = os.path.join(_HERE, "lba_torch.so")
 
-EXPORTS = ["lba_gemm", "lba_gemm_batched", "lba_linear", "lba_gated", "lba_gemm_last_overflow", "lba_gemm_ste_mask", "lba_conv2d", "lba_gemm_host_workspace_bytes", "lba_gemm_host",
+EXPORTS = ["lba_gemm", "lba_gemm_batched", "lba_linear", "lba_gated", "lba_linear_backward", "lba_gated_backward", "lba_backward_workspace_bytes", "lba_gemm_last_overflow", "lba_gemm_ste_mask", "lba_conv2d", "lba_gemm_host_workspace_bytes", "lba_gemm_host",
            "lba_conv2d_host_workspace_bytes", "lba_conv2d_host", "lba_gemm_host_static", "lba_count_nan_codes", "lba_describe_plan", "lba_describe_plan_batched",
            "lba_set_tile_override", "lba_status_string", "lba_last_cuda_error", "lba_version"]
 
@@ -44,6 +44,11 @@ class _Layer(C.Structure):
     _fields_ = [("activation", C.c_int32), ("out_type", C.c_int32), ("out_scale", C.c_void_p), ("preact", C.c_void_p),
                 ("residual", C.c_void_p), ("preact_type", C.c_int32), ("residual_type", C.c_int32), ("dropout", C.c_double),
                 ("rng", C.c_void_p)]
+
+
+class _Backward(C.Structure):
+    _fields_ = [("activation", C.c_int32), ("grad_type", C.c_int32), ("out_type", C.c_int32), ("preact_type", C.c_int32),
+                ("preact", C.c_void_p), ("dropout", C.c_double), ("rng", C.c_void_p), ("input_flags", C.c_int32)]
 
 
 _lib = None
@@ -95,6 +100,12 @@ def load_library():
     lib.lba_linear.argtypes = gemm_args[:14] + [C.POINTER(_Layer), C.c_void_p, C.c_void_p]
     lib.lba_gated.argtypes = [C.c_void_p] * 4 + [C.c_int, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_void_p] + \
         [C.c_int64] * 3 + gemm_args[10:14] + [C.POINTER(_Layer), C.c_void_p, C.c_void_p]
+    lib.lba_backward_workspace_bytes.restype = C.c_size_t
+    lib.lba_backward_workspace_bytes.argtypes = [C.c_int] + [C.c_int64] * 3 + [C.c_int, C.c_int, C.POINTER(_Backward), C.c_int]
+    lib.lba_linear_backward.argtypes = gemm_args[:2] + [C.c_void_p] + gemm_args[2:6] + [C.c_int64] * 3 + [C.POINTER(_Backward)] + \
+        [C.c_void_p] * 4 + [C.c_size_t, C.c_void_p]
+    lib.lba_gated_backward.argtypes = [C.c_void_p] * 5 + [C.c_int, C.c_void_p, C.c_void_p, C.c_int] + [C.c_int64] * 3 + \
+        [C.POINTER(_Backward)] + [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]
     conv_args = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_void_p] + [C.c_int] * 11 + \
         [C.POINTER(_Fmt), C.POINTER(_Fmt), C.c_int, C.c_int, C.c_void_p]
     lib.lba_conv2d.argtypes = conv_args + [C.c_void_p]
@@ -343,6 +354,90 @@ def lba_gated(A, B_gate, B_up, scale_a, scale_gate, scale_up, bias_gate, bias_up
                          _dev(_shaped(bias_up, (N,), "bias_up"), torch.float32, "bias_up"), M, N, K, _fmt_ref(prod_fmt), _fmt_ref(acc_fmt), order,
                          chunk, C.byref(layer), _dev(out, out.dtype, "out"), _stream(stream)))
     return out if pre is None else (out, pre)
+
+
+def _backward(gated, grad_out, shape, K, scale_a_len, scale_b_len, prod_fmt, preact, activation, dropout, rng, grad_dtype, needs, workspace,
+              device, stream):
+    """What both backward passes share: the C struct, the type of the gradients and the workspace."""
+    lib = load_library()
+    g, g_type = _typed(_shaped(grad_out, shape, "grad_out"), "grad_out")
+    if g is None:
+        raise TypeError("grad_out must be a float32, bfloat16 or float16 CUDA tensor")
+    pre, pre_type = _typed(_shaped(preact, (2, *shape) if gated else shape, "preact"), "preact")
+    grad_dtype = grad_out.dtype if grad_dtype is None else grad_dtype
+    if grad_dtype not in _FLOAT_TYPES:
+        raise TypeError("grad_dtype must be torch.float32, bfloat16 or float16")
+    flags = (prod_fmt.flags if isinstance(prod_fmt, LbaFormat) else int(tuple(prod_fmt)[4])) & FLAG_INPUT_M4E3
+    how = _Backward(_activation(activation), g_type, _FLOAT_TYPES[grad_dtype], pre_type, pre, float(dropout), _rng(rng, dropout), flags)
+    need = lib.lba_backward_workspace_bytes(gated, shape[0], shape[1], K, scale_a_len, scale_b_len, C.byref(how),
+                                            sum(1 << i for i, n in enumerate(needs) if n))
+    if workspace is None:
+        workspace = torch.empty(need, dtype=torch.uint8, device=device)
+        if stream is not None and need:   # memory that the caching allocator hands out again belongs to the current stream
+            workspace.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream), device))
+    return how, g, grad_dtype, workspace
+
+
+def lba_linear_backward(grad_out, A, B, scale_a, scale_b, prod_fmt, preact=None, activation="none", dropout=0.0, rng=None, grad_dtype=None,
+                        needs=(True, True, True), workspace=None, stream=None):
+    """(grad_a [M][K], grad_b [N][K], grad_bias [N]) of ``lba_linear`` under the straight-through estimator, None where ``needs`` says
+    so.  See ``lba_linear_backward`` in lba.h.
+
+    ``preact`` is what the forward call kept; ``activation``, ``dropout`` and ``rng`` are the forward call's (``rng`` holding the
+    same two values), and so is ``prod_fmt``, which says what the operands' bytes are.  ``grad_dtype``: of grad_a and grad_b,
+    grad_out's if None; grad_bias is float32.  ``workspace``: a CUDA uint8 tensor of ``backward_workspace_bytes``, or None."""
+    M, K = A.shape
+    N, K2 = B.shape
+    if K != K2:
+        raise ValueError("A and B disagree on K")
+    _same_device(A, B, scale_a, scale_b, grad_out, preact, rng if dropout else None, workspace)
+    sa, sa_len = _scale(scale_a, "scale_a")
+    sb, sb_len = _scale(scale_b, "scale_b")
+    how, g, dtype, ws = _backward(0, grad_out, (M, N), K, sa_len, sb_len, prod_fmt, preact, activation, dropout, rng, grad_dtype, needs,
+                                  workspace, A.device, stream)
+    ga = torch.empty((M, K), dtype=dtype, device=A.device) if needs[0] else None
+    gb = torch.empty((N, K), dtype=dtype, device=A.device) if needs[1] else None
+    gc = torch.empty((N,), dtype=torch.float32, device=A.device) if needs[2] else None
+    _check(load_library().lba_linear_backward(g, _dev(A, torch.uint8, "A"), _dev(B, torch.uint8, "B"), sa, sa_len, sb, sb_len, M, N, K,
+                                              C.byref(how), _typed(ga, "grad_a")[0], _typed(gb, "grad_b")[0],
+                                              _dev(gc, torch.float32, "grad_bias"), _dev(ws, torch.uint8, "workspace"), ws.numel(),
+                                              _stream(stream)))
+    return ga, gb, gc
+
+
+def lba_gated_backward(grad_out, A, B_gate, B_up, scale_a, scale_gate, scale_up, prod_fmt, preact, activation="silu", grad_dtype=None,
+                       needs=(True, True, True), workspace=None, stream=None):
+    """(grad_a, grad_gate, grad_up, grad_bias_gate, grad_bias_up) of ``lba_gated``; ``preact`` is the [2][M][N] that the forward call
+    kept, the other arguments are those of ``lba_linear_backward``.  See ``lba_gated_backward`` in lba.h."""
+    M, K = A.shape
+    N, K2 = B_gate.shape
+    if K != K2 or tuple(B_up.shape) != (N, K):
+        raise ValueError("A, B_gate and B_up disagree on K, or the two projections on N")
+    _same_device(A, B_gate, B_up, scale_a, scale_gate, scale_up, grad_out, preact, workspace)
+    sa, sa_len = _scale(scale_a, "scale_a")
+    sg, sg_len = _scale(scale_gate, "scale_gate")
+    su, su_len = _scale(scale_up, "scale_up")
+    if sg_len != su_len:
+        raise ValueError("scale_gate and scale_up must have the same length")
+    how, g, dtype, ws = _backward(1, grad_out, (M, N), K, sa_len, sg_len, prod_fmt, preact, activation, 0.0, None, grad_dtype, needs, workspace,
+                                  A.device, stream)
+    ga = torch.empty((M, K), dtype=dtype, device=A.device) if needs[0] else None
+    gg, gu = (torch.empty((N, K), dtype=dtype, device=A.device) if needs[1] else None for _ in range(2))
+    cg, cu = (torch.empty((N,), dtype=torch.float32, device=A.device) if needs[2] else None for _ in range(2))
+    _check(load_library().lba_gated_backward(g, _dev(A, torch.uint8, "A"), _dev(B_gate, torch.uint8, "B_gate"), _dev(B_up, torch.uint8, "B_up"),
+                                             sa, sa_len, sg, su, sg_len, M, N, K, C.byref(how), _typed(ga, "grad_a")[0],
+                                             _typed(gg, "grad_gate")[0], _typed(gu, "grad_up")[0], _dev(cg, torch.float32, "grad_bias_gate"),
+                                             _dev(cu, torch.float32, "grad_bias_up"), _dev(ws, torch.uint8, "workspace"), ws.numel(),
+                                             _stream(stream)))
+    return ga, gg, gu, cg, cu
+
+
+def backward_workspace_bytes(M, N, K, scale_a_len, scale_b_len, grad_dtype, activation="none", gated=False, grad_out_dtype=None,
+                             needs=(True, True, True)):
+    """Bytes of workspace of a backward call with gradients of ``grad_dtype``."""
+    how = _Backward(_activation(activation), _FLOAT_TYPES[grad_out_dtype or grad_dtype], _FLOAT_TYPES[grad_dtype], 0, None, 0.0, None, 0)
+    return load_library().lba_backward_workspace_bytes(int(gated), M, N, K, scale_a_len, scale_b_len, C.byref(how),
+                                                       sum(1 << i for i, n in enumerate(needs) if n))
 
 
 def lba_gemm_last_overflow(A, B, prod_fmt, acc_fmt, out=None, stream=None):

@@ -8,6 +8,7 @@
 #include <mutex>
 
 #include "../../include/lba.h"
+#include "lba_grad.cuh"
 #include "lba_kernel_small.cuh"
 
 namespace lba {
@@ -684,6 +685,43 @@ int fill_layer(LinearProblem* p, const lba_layer* l, void* out) {
   return LBA_OK;
 }
 
+// the backward pass' fields but for its outputs
+int fill_backward(GradCall* c, const lba_backward* h, int64_t M, int64_t N, int64_t K, int sa_len, int sb_len) {
+  if (M < 0 || N < 0 || K < 0 || M > 2147483647LL || N > 1073741823LL || K > 2147483647LL) return LBA_ERR_SHAPE;
+  if (!h) return LBA_ERR_NULL;
+  if (!(sa_len == 1 || (int64_t)sa_len == M) || !(sb_len == 1 || (int64_t)sb_len == N)) return LBA_ERR_SCALE_LEN;
+  if (h->activation < 0 || h->activation >= ACT_COUNT || !float_type(h->grad_type) || !float_type(h->out_type) || !float_type(h->preact_type) ||
+      (h->input_flags & ~LBA_FLAG_INPUT_M4E3))
+    return LBA_ERR_LAYER;
+  if (c->gated && h->dropout != 0.0) return LBA_ERR_LAYER;
+  c->M = M;
+  c->N = N;
+  c->K = K;
+  c->sa_per_row = sa_len != 1;
+  c->sb_per_col = sb_len != 1;
+  c->act = h->activation;
+  c->grad_type = h->grad_type;
+  c->out_type = h->out_type;
+  c->pre_type = h->preact_type;
+  c->in_m4e3 = (h->input_flags & LBA_FLAG_INPUT_M4E3) != 0;
+  c->rng = h->rng;
+  return LBA_OK;
+}
+
+int run_backward(GradCall* c, const lba_backward* h, void* workspace, size_t workspace_bytes, cudaStream_t stream) {
+  const int st = drop_constants(h->dropout, h->rng, c->M, &c->drop_below, &c->keep_scale);
+  if (st != LBA_OK) return st;
+  if (c->M > 0 && c->N > 0) {
+    if (!c->grad || ((c->gated || c->act != ACT_NONE) && !h->preact)) return LBA_ERR_NULL;
+    if (c->K > 0 && ((c->grad_a && (!c->B || (c->gated && !c->B2))) || (c->grad_b && !c->A))) return LBA_ERR_NULL;
+    const size_t need = backward_workspace(*c);
+    if (need > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need)) return LBA_ERR_WORKSPACE;
+  }
+  c->pre = h->preact;
+  const cudaError_t e = launch_backward(*c, workspace, stream);
+  return e == cudaSuccess ? LBA_OK : cuda_fail(e);
+}
+
 size_t round_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
 // Sizes of the host-buffer variants are formed in size_t; a shape whose operand or output byte count does not fit
@@ -800,6 +838,60 @@ int lba_gated(const uint8_t* A, const uint8_t* B_gate, const uint8_t* B_up, cons
   apply_plan(&p, pl);
   const bool vec = K % BK == 0 && aligned16(A) && aligned16(B_gate) && aligned16(B_up);
   return run(p, pl, vec ? LD_GEMM_VEC : LD_GEMM_ROWS, (cudaStream_t)stream);
+}
+
+size_t lba_backward_workspace_bytes(int gated, int64_t M, int64_t N, int64_t K, int scale_a_len, int scale_b_len, const lba_backward* how,
+                                    int needs) {
+  GradCall c = {};
+  c.gated = gated != 0;
+  if (fill_backward(&c, how, M, N, K, scale_a_len, scale_b_len) != LBA_OK) return 0;
+  static char some;  // an output that is wanted
+  c.grad_a = (needs & LBA_NEEDS_A) ? &some : nullptr;
+  c.grad_b = c.grad_b2 = (needs & LBA_NEEDS_B) ? &some : nullptr;
+  c.grad_bias = c.grad_bias2 = (needs & LBA_NEEDS_BIAS) ? reinterpret_cast<float*>(&some) : nullptr;
+  return backward_workspace(c);
+}
+
+int lba_linear_backward(const void* grad_out, const uint8_t* A, const uint8_t* B, const float* scale_a, int scale_a_len, const float* scale_b,
+                        int scale_b_len, int64_t M, int64_t N, int64_t K, const lba_backward* how, void* grad_a, void* grad_b, float* grad_bias,
+                        void* workspace, size_t workspace_bytes, void* stream) {
+  GradCall c = {};
+  const int st = fill_backward(&c, how, M, N, K, scale_a_len, scale_b_len);
+  if (st != LBA_OK) return st;
+  if (!scale_a || !scale_b) return LBA_ERR_NULL;
+  c.grad = grad_out;
+  c.A = A;
+  c.B = B;
+  c.sa = scale_a;
+  c.sb = scale_b;
+  c.grad_a = grad_a;
+  c.grad_b = grad_b;
+  c.grad_bias = grad_bias;
+  return run_backward(&c, how, workspace, workspace_bytes, (cudaStream_t)stream);
+}
+
+int lba_gated_backward(const void* grad_out, const uint8_t* A, const uint8_t* B_gate, const uint8_t* B_up, const float* scale_a,
+                       int scale_a_len, const float* scale_gate, const float* scale_up, int scale_b_len, int64_t M, int64_t N, int64_t K,
+                       const lba_backward* how, void* grad_a, void* grad_gate, void* grad_up, float* grad_bias_gate, float* grad_bias_up,
+                       void* workspace, size_t workspace_bytes, void* stream) {
+  GradCall c = {};
+  c.gated = 1;
+  const int st = fill_backward(&c, how, M, N, K, scale_a_len, scale_b_len);
+  if (st != LBA_OK) return st;
+  if (!scale_a || !scale_gate || !scale_up || !grad_gate != !grad_up || !grad_bias_gate != !grad_bias_up) return LBA_ERR_NULL;
+  c.grad = grad_out;
+  c.A = A;
+  c.B = B_gate;
+  c.B2 = B_up;
+  c.sa = scale_a;
+  c.sb = scale_gate;
+  c.sb2 = scale_up;
+  c.grad_a = grad_a;
+  c.grad_b = grad_gate;
+  c.grad_b2 = grad_up;
+  c.grad_bias = grad_bias_gate;
+  c.grad_bias2 = grad_bias_up;
+  return run_backward(&c, how, workspace, workspace_bytes, (cudaStream_t)stream);
 }
 
 int lba_gemm_batched(const uint8_t* A, const uint8_t* B, const float* scale_a, int scale_a_len, const float* scale_b,

@@ -70,3 +70,13 @@ def half_step(dtype, v):
     tiny = {torch.float32: 2.0 ** -150, torch.bfloat16: 2.0 ** -134, torch.float16: 2.0 ** -25, "e4m3": 2.0 ** -10, "m4e3": 2.0 ** -1 + 2.0 ** -5}[dtype]
     rel = {"e4m3": 2.0 ** -4, "m4e3": 2.0 ** -5}.get(dtype) or torch.finfo(dtype).eps / 2
     return v.abs() * rel + tiny
+
+# A binary32 slope is off by at most 2^-18: the worst is gelu_tanh's z/2 (1 - t^2) c (1 + 0.134 z^2), where 1 - t^2 is off by 2 x 2^-23
+# + 2^-24 and the factor stays below 6 where t is not 1 to the last bit (|z| <= 4.3); the others have factors below 2.
+SLOPE_ERR = 2.0 ** -18
+
+
+def piece_err(dtype):
+    """What is left of dz in the bfloat16 pieces that go with a result type: one rounding to 8 bits; a cut to 8 bits (remainder below
+    2^-7) and a rounding of that; two cuts and the last eight of 24 bits, exact."""
+    return {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -15, torch.float32: 0.0}[dtype]

@@ -93,3 +93,47 @@ def test_binding_refuses_on_the_host():
         lba.lba_gated(a, b, b[:4], s, s, s, None, None, PROD, ACC)
     with pytest.raises(ValueError):
         lba.lba_gated(a, b, b, s, s, s, None, None, PROD, ACC, preact=torch.zeros(4, 8))
+
+
+def _how(**kw):
+    h = lba._Backward()
+    h.activation, h.preact = 2, 256
+    for k, v in kw.items():
+        setattr(h, k, v)
+    return h
+
+
+def _backward(M=4, N=4, K=16, how=None, grad=FAKE, a=FAKE, ws=FAKE, ws_bytes=1 << 30, sa_len=1, sb_len=1, sa=FAKE):
+    return lba.load_library().lba_linear_backward(grad, a, FAKE, sa, sa_len, FAKE, sb_len, M, N, K, None if how is None else C.byref(how), FAKE, FAKE,
+                                                  FAKE, ws, ws_bytes, None)
+
+
+def _gated_backward(how, grads=(256, 256), biases=(256, 256), up=FAKE):
+    return lba.load_library().lba_gated_backward(FAKE, FAKE, FAKE, up, FAKE, 1, FAKE, FAKE, 1, 4, 4, 16, C.byref(how), FAKE, *grads, *biases, FAKE,
+                                                 1 << 30, None)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(activation=5), -9), (dict(grad_type=3), -9), (dict(out_type=3), -9), (dict(preact_type=3), -9), (dict(input_flags=1), -9),
+    (dict(dropout=1.0, rng=256), -9), (dict(dropout=0.5), -1), (dict(preact=None), -1),
+])
+def test_refused_backward_options(kw, status):
+    assert _backward(how=_how(**kw)) == status
+
+
+def test_refused_backward_arguments():
+    h = _how()
+    assert _backward(how=None) == -1 and _backward(how=h, grad=None) == -1 and _backward(how=h, a=None) == -1 and _backward(how=h, sa=None) == -1
+    assert _backward(M=-1, how=h) == -2 and _backward(N=1 << 30, how=h) == -2 and _backward(M=1 << 31, how=h) == -2
+    assert _backward(how=h, sa_len=3) == -5 and _backward(how=h, sb_len=3) == -5
+    assert _backward(how=h, ws=None) == -7 and _backward(how=h, ws=C.c_void_p(128)) == -7 and _backward(how=h, ws_bytes=256) == -7
+    assert _gated_backward(_how(dropout=0.5, rng=256)) == -9 and _gated_backward(_how(preact=None)) == -1
+    assert _gated_backward(h, grads=(256, None)) == -1 and _gated_backward(h, biases=(None, 256)) == -1 and _gated_backward(h, up=None) == -1
+
+
+def test_backward_workspace_grows_with_what_is_asked():
+    size = lambda **k: lba.backward_workspace_bytes(100, 50, 70, 1, k.pop("sb", 1), k.pop("dtype", torch.bfloat16), activation="gelu", **k)  # noqa: E731
+    full = size()
+    assert 0 < size(needs=(False, False, True)) < size(needs=(True, False, False)) < full
+    assert size(sb=50) > full and size(dtype=torch.float16) > full and size(gated=True) > full
+    assert size(needs=(False, False, False)) == 0 and lba.backward_workspace_bytes(0, 50, 70, 1, 1, torch.bfloat16) == 0
