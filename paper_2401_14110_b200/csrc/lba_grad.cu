@@ -17,6 +17,7 @@
 
 #include <cuda.h>
 
+#include "lba_async.cuh"
 #include "lba_layer.cuh"
 
 namespace lba {
@@ -257,27 +258,6 @@ struct ProductParams {
   int64_t row_blocks, N, np, nz;
 };
 
-__device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
-__device__ __forceinline__ void mbar_init(uint32_t bar, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
-__device__ __forceinline__ void mbar_expect(uint32_t bar, int bytes) {
-  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
-// Waits for the phase of the given parity, at most some seconds; then `dead` is set, no wait of the CTA takes long any more and
-// its outputs are NaN.
-__device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
-  for (uint32_t i = 0;; ++i) {
-    uint32_t done;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
-        : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    if (done) return;
-    if (i > (1u << 22) || (i > 1024 && *dead)) {
-      *dead = 1;
-      return;
-    }
-  }
-}
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
                "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
@@ -383,7 +363,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
       mbar_init(acc_free + 8 * i, 128);
     }
     *dead = 0;
-    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    mbar_init_fence();
   }
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(COLS) : "memory");
@@ -408,7 +388,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
             mbar_wait(empty + 8 * stage, phase ^ 1, dead);
             if (*dead) goto loaded;
             const uint32_t x = smem_u32(base + stage * STAGE), y = x + X_BYTES, bar = full + 8 * stage;
-            mbar_expect(bar, STAGE);
+            mbar_arrive_expect(bar, STAGE);
             if (j.x_mn) {
               tma_load(x, &p.x[v.job], r, b * BL, q, bar);
               tma_load(x + X_BYTES / 2, &p.x[v.job], r + 64, b * BL, q, bar);

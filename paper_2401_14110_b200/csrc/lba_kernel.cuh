@@ -1969,6 +1969,7 @@ struct TileInfo { int bm, bn, tm, tn; };
 constexpr int TILE_COUNT = 4;
 constexpr int TILE_PAIR = 5;  // 64x64 tile shared by a cluster of two CTAs (chunk-16 order, floor rounding)
 constexpr int TILE_SPLIT = 6;   // 6, 7: 16x16 and 32x32 with the chunk sums spread over the warps (lba_split_kernel)
+constexpr int TILE_ROWS = 11;   // layers on few rows (lba_rows_kernel)
 constexpr int TILE_CHAIN = 10;  // 16x16, one pair of chains per thread (lba_chain_kernel)
 __host__ inline TileInfo tile_info(int t) {
   const TileInfo tab[TILE_COUNT] = {{128, 128, 8, 8}, {128, 64, 4, 8}, {64, 64, 4, 8}, {32, 32, 4, 4}};

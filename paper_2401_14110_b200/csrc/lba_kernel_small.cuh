@@ -73,9 +73,11 @@ struct PairSteps {
   __device__ __forceinline__ u64 add(u64 pr, u64 s) const {
     return round<CLAMP>(RNE ? fma2_rn_ftz(cc, pr, s) : fma2_rz_ftz(cc, pr, s));
   }
-  __device__ __forceinline__ u64 fold(u64 c, u64 t) const {
-    return round<true>(RNE ? add2_rn_ftz(c, t) : add2_rz_ftz(c, t));
+  template <bool CLAMP>
+  __device__ __forceinline__ u64 fold_as(u64 c, u64 t) const {
+    return round<CLAMP>(RNE ? add2_rn_ftz(c, t) : add2_rz_ftz(c, t));
   }
+  __device__ __forceinline__ u64 fold(u64 c, u64 t) const { return fold_as<true>(c, t); }
 };
 
 // sixteen bytes of a row -> scaled binary32, k-major in shared memory, `stride` elements from one k to the next; returns the

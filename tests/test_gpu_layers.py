@@ -84,6 +84,25 @@ def test_every_tile(name, order, tiles):
             lba.set_tile_override(-1)
 
 
+@pytest.mark.parametrize("name", ["m7e4", "m7e4_paper", "m5e6", "m2e5", "m8e6", "m7e4_rne", "m10e6_rne", "m4e3_bytes"])
+def test_few_rows(name):
+    # the kernel for few rows against the tiles, bit for bit: several rounds of 512 k and trips around its rings, ragged ends of
+    # columns and rounds, one pair of columns and many; Gaussian operands, and codes whose sums saturate in both hierarchies
+    prod, acc = FORMATS[name]
+    for M, N, K in [(1, 1, 32), (1, 2, 512), (2, 3, 528), (1, 40, 5120), (3, 601, 1040), (5, 2048, 1536), (8, 77, 2064), (16, 330, 4096), (15, 4500, 544),
+                    (1, 9000, 1024), (16, 2, 16384), (17, 64, 512)]:
+        for wild in (False, True):
+            A, sa, B, sb, bias, B2, sb2, bias2 = inputs(M, N, K, 3 * M + N + K, prod, 2)
+            if wild:
+                A, B = (synth.random_codes(t.shape, 5 + i).to(DEV) for i, t in enumerate((A, B)))
+            z = lba.lba_gemm(A, B, sa, sb, bias, prod, acc)
+            v = lba.lba_gemm(A, B2, sa, sb2, bias2, prod, acc)
+            got = lba.lba_linear(A, B, sa, sb, bias, prod, acc)
+            assert torch.equal(bits(got), bits(z)), (M, N, K, wild)
+            out, pre = lba.lba_gated(A, B, B2, sa, sb, sb2, bias, bias2, prod, acc, activation="none", preact=torch.float32)
+            assert torch.equal(bits(pre), bits(torch.stack([z, v]))) and torch.equal(bits(out), bits(z * v)), (M, N, K, wild)
+
+
 def check(got, want, err, scale=None, m4e3=False):
     """got: a layer's output; want: what it should hold, in 64 bits, off by at most err before its last rounding"""
     if got.dtype == torch.uint8:
