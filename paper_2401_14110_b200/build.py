@@ -20,6 +20,7 @@ TORCH_SRC = os.path.join(CSRC, "lba_torch.cpp")
 TORCH_LIB = os.path.join(HERE, "lba_torch.so")
 NVCC = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
 FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC",
+         "--compress-mode=size",   # the kernels of all formats and tiles: 200 MB of device code otherwise
          "-I", os.path.join(ROOT, "include")]
 
 

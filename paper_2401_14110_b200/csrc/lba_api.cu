@@ -33,7 +33,6 @@ LBA_DECL(0) LBA_DECL(1) LBA_DECL(2)
 cudaError_t launch_last_overflow(bool small, int qm, int load, const Problem& p, cudaStream_t stream);
 cudaError_t launch_ste_mask(bool small, int qm, int ord, int diff, int load, const Problem& p, cudaStream_t stream);
 cudaError_t launch_ste_packed(bool small, int pq, int chunk16, int load, const Problem& p, cudaStream_t stream);
-cudaError_t launch_rows(int rne, const LinearProblem& p, int pairs, int stages, cudaStream_t stream);
 cudaError_t launch_fixed(int ord, int load, const Problem& p, cudaStream_t stream);
 cudaError_t launch_fixed(int ord, int load, const LinearProblem& p, cudaStream_t stream);
 cudaError_t launch_cluster_pair(int pq, int load, const Problem& p, cudaStream_t stream);
@@ -587,26 +586,26 @@ void apply_plan(Problem* p, const Plan& pl) {
 
 bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15) == 0; }
 
-// Few-row kernel: pairs of columns per CTA and stages, or no stages where it does not apply.  The fewest waves of CTAs in which
-// at least three stages fit; as many stages as do.
-struct RowsShape { int pairs, stages; };
+// Few-row kernel: the fewest waves of CTAs in which at least three stages and two rounds of sums fit; as many of either as do.
 RowsShape rows_shape(const LinearProblem& p, const Plan& pl, int load) {
   const bool packed = pl.qm == QM_FLOOR_FAST || pl.qm == QM_FLOOR_FULL || (pl.qm == QM_RNE_FULL && pl.rne_packed);
   const int forced = g_tile_override.load(std::memory_order_relaxed);
-  if (pl.fixed || !packed || pl.ord != ORD_CHUNK16 || load != LD_GEMM_VEC || p.M > ROWS_MAX || (forced >= 0 && forced != TILE_ROWS)) return {0, 0};
+  if (pl.fixed || !packed || pl.ord != ORD_CHUNK16 || load != LD_GEMM_VEC || p.M > ROWS_MAX || (forced >= 0 && forced != TILE_ROWS)) return {};
   const int64_t total = (p.N + 1) / 2;
-  const int rounds = (int)((p.K / BK + ROWS_CHUNKS - 1) / ROWS_CHUNKS), M = (int)p.M;
+  const int rounds = (int)((p.K / BK + ROWS_CHUNKS - 1) / ROWS_CHUNKS), M = (int)p.M, room = 227 * 1024;
   for (int64_t waves = 1; waves <= total; ++waves) {
     const int64_t pairs = (total + waves * sm_count() - 1) / (waves * sm_count());
-    if (pairs * M > 32 * ROWS_FOLD * ROWS_CHAINS || rows_smem(M, (int)pairs, 3) > 227 * 1024) continue;
-    int stages = 3;
-    while (stages < ROWS_MAX_STAGES && stages < rounds && rows_smem(M, (int)pairs, stages + 1) <= 227 * 1024) ++stages;
-    return {(int)pairs, stages};
+    RowsShape s = {(int)pairs, ROWS_MIN_STAGES, ROWS_SUM_RING};
+    if (pairs > 128 || 2 * pairs * M > 32 * ROWS_FOLD * ROWS_CHAINS) continue;
+    if (rows_smem(M, s.pairs, s.stages, s.ring) > room) s.ring = 2;
+    if (rows_smem(M, s.pairs, s.stages, s.ring) > room) continue;
+    while (s.stages < ROWS_MAX_STAGES && s.stages < rounds && rows_smem(M, s.pairs, s.stages + 1, s.ring) <= room) ++s.stages;
+    return s;
   }
-  return {0, 0};
+  return {};
 }
-RowsShape rows_shape(const Problem&, const Plan&, int) { return {0, 0}; }
-cudaError_t launch_rows(int, const Problem&, int, int, cudaStream_t) { return cudaErrorInvalidValue; }
+RowsShape rows_shape(const Problem&, const Plan&, int) { return {}; }
+cudaError_t launch_rows(int, const Problem&, const RowsShape&, cudaStream_t) { return cudaErrorInvalidValue; }
 
 template <class P>
 int run(const P& p, const Plan& pl, int load, cudaStream_t stream) {
@@ -614,7 +613,7 @@ int run(const P& p, const Plan& pl, int load, cudaStream_t stream) {
   if (p.batch > 65535) return LBA_ERR_SHAPE;
   const RowsShape rows = rows_shape(p, pl, load);
   if (rows.stages > 0) {
-    const cudaError_t e = launch_rows(pl.qm == QM_RNE_FULL ? pl.rne_packed : 0, p, rows.pairs, rows.stages, stream);
+    const cudaError_t e = launch_rows(pl.qm == QM_RNE_FULL ? pl.rne_packed : 0, p, rows, stream);
     return e == cudaSuccess ? LBA_OK : cuda_fail(e);
   }
   if (pl.fixed) {  // Eq. 1: the integer kernel, one tile shape

@@ -15,8 +15,6 @@
 //   grad_product_kernel   both products as one list of 128 x BN tiles (tcgen05, TMA), and the bias sums' last step.
 #include "lba_grad.cuh"
 
-#include <cuda.h>
-
 #include "lba_async.cuh"
 #include "lba_layer.cuh"
 
@@ -521,22 +519,9 @@ Layout layout(const GradCall& c) {
   return l;
 }
 
-typedef CUresult (*EncodeFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
-                             const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
-EncodeFn encoder() {
-  static const EncodeFn fn = [] {
-    void* f = nullptr;
-    cudaDriverEntryPointQueryResult found;
-    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &found) != cudaSuccess ||
-        found != cudaDriverEntryPointSuccess)
-      f = nullptr;
-    return (EncodeFn)f;
-  }();
-  return fn;
-}
 // planes x rows x cols of bfloat16, rows `pitch` elements apart; boxes of 64 columns and `box_rows` rows, 128-byte swizzle
 bool make_map(CUtensorMap* map, const void* base, int64_t cols, int64_t rows, int64_t planes, int64_t pitch, int64_t plane, int box_rows) {
-  const EncodeFn encode = encoder();
+  const EncodeTiled encode = tensor_map_encoder();
   if (!encode) return false;
   const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes}, strides[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)plane * 2};
   const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, step[3] = {1, 1, 1};

@@ -985,8 +985,8 @@ constexpr int KUNROLL = 16;  // k-steps unrolled in the packed slab body (the wh
 // holds its pipe for two clocks.  M4E3 bytes become halves by moving their seven magnitude bits under half precision's
 // exponent, for two bytes at a time, and adding 15 to it; the FMA's other factor is 0 for the code e = m = 0 and 1 for all others.
 template <bool M4E3>
-__device__ __forceinline__ void decode4(uint32_t w, u64& v01, u64& v23) {
-  uint32_t h[2], g[2] = {0x3C003C00u, 0x3C003C00u};
+__device__ __forceinline__ void decode4(uint32_t w, u64& v01, u64& v23, uint32_t factor = 0x3C003C00u) {  // factor: E4M3 only, two halves
+  uint32_t h[2], g[2] = {factor, factor};
   if (M4E3) {
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
