@@ -587,6 +587,9 @@ void apply_plan(Problem* p, const Plan& pl) {
 bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15) == 0; }
 
 // Few-row kernel: the fewest waves of CTAs in which at least three stages and two rounds of sums fit; as many of either as do.
+// Up to twelve rows it is ahead of the tiles everywhere (4096 x 4096, 1, 4, 8 and 12 rows: 9.5, 16.4, 24.5 and 34.2 us against 49.4,
+// 50.1, 50.9 and 52.0); behind that only where two waves do (sixteen rows: 50.1 against 53.0, gated 4096 x 1024 with four waves 35.2
+// against 28.3).
 RowsShape rows_shape(const LinearProblem& p, const Plan& pl, int load) {
   const bool packed = pl.qm == QM_FLOOR_FAST || pl.qm == QM_FLOOR_FULL || (pl.qm == QM_RNE_FULL && pl.rne_packed);
   const int forced = g_tile_override.load(std::memory_order_relaxed);
@@ -594,9 +597,10 @@ RowsShape rows_shape(const LinearProblem& p, const Plan& pl, int load) {
   const int64_t total = (p.N + 1) / 2;
   const int rounds = (int)((p.K / BK + ROWS_CHUNKS - 1) / ROWS_CHUNKS), M = (int)p.M, room = 227 * 1024;
   for (int64_t waves = 1; waves <= total; ++waves) {
+    if (M > 12 && waves > 2) break;
     const int64_t pairs = (total + waves * sm_count() - 1) / (waves * sm_count());
     RowsShape s = {(int)pairs, ROWS_MIN_STAGES, ROWS_SUM_RING};
-    if (pairs > 128 || 2 * pairs * M > 32 * ROWS_FOLD * ROWS_CHAINS) continue;
+    if (2 * pairs * M > 32 * ROWS_FOLD * (M == 1 ? 1 : ROWS_CHAINS)) continue;
     if (rows_smem(M, s.pairs, s.stages, s.ring) > room) s.ring = 2;
     if (rows_smem(M, s.pairs, s.stages, s.ring) > room) continue;
     while (s.stages < ROWS_MAX_STAGES && s.stages < rounds && rows_smem(M, s.pairs, s.stages + 1, s.ring) <= room) ++s.stages;

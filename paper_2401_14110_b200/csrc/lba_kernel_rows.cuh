@@ -28,7 +28,7 @@ constexpr int ROWS_FOLD = 4, ROWS_DECODE = 3, ROWS_COMPUTE = 12;  // warps, in t
 constexpr int ROWS_COPY_WARP = ROWS_FOLD + ROWS_DECODE, ROWS_FIRST_COMPUTE = ROWS_COPY_WARP + 1;
 constexpr int ROWS_WARPS = ROWS_FIRST_COMPUTE + ROWS_COMPUTE, ROWS_THREADS = 32 * ROWS_WARPS;
 constexpr int ROWS_MIN_STAGES = 3;           // at least as many as warps that take rounds in turn
-constexpr int ROWS_CHAINS = 4;               // (row, column) chains per lane of a fold warp, at most
+constexpr int ROWS_CHAINS = 4;               // (row, column) chains per lane of a fold warp, at most (one where there is one row)
 constexpr int ROWS_SUM_RING = 3;             // rounds of sums kept; two where a third would cost a wave of CTAs
 constexpr int ROWS_MAX_STAGES = 8;
 constexpr int ROWS_PITCH = ROWS_CHUNKS + 4;  // sums from one chain to the next: 16-byte aligned, lanes on different banks
@@ -306,19 +306,20 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) lba_rows_kernel(const __grid_
       stage += step_r;
     }
   } else if (warp < fold_warps) {
+    constexpr int CHAINS = ONE ? 1 : ROWS_CHAINS;
     const FoldStep<RNE> step(p);
     const int f = threadIdx.x, columns = 2 * mine;
     const int total = M * columns;  // chains of this CTA
-    float T[ROWS_CHAINS];
+    float T[CHAINS];
 #pragma unroll
-    for (int i = 0; i < ROWS_CHAINS; ++i) T[i] = 0.0f;
+    for (int i = 0; i < CHAINS; ++i) T[i] = 0.0f;
     int buf = 0;
     uint32_t phase = 0;
     for (int r = 0; r < rounds; ++r) {
       mbar_wait(sum_full + 8 * buf, phase, dead);
       const int have = chunks - r * ROWS_CHUNKS < ROWS_CHUNKS ? chunks - r * ROWS_CHUNKS : ROWS_CHUNKS;
 #pragma unroll
-      for (int i = 0; i < ROWS_CHAINS; ++i) {
+      for (int i = 0; i < CHAINS; ++i) {
         const int c = f + i * 32 * ROWS_FOLD;
         if (c >= total) break;
         const float* const s = reinterpret_cast<const float*>(sums + buf * s_bytes) + ((c / columns) * 2 * pairs + c % columns) * ROWS_PITCH;
@@ -342,7 +343,7 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) lba_rows_kernel(const __grid_
     }
     // a column's neighbour in its pair sits in the next lane
 #pragma unroll
-    for (int i = 0; i < ROWS_CHAINS; ++i) {
+    for (int i = 0; i < CHAINS; ++i) {
       const int c = f + i * 32 * ROWS_FOLD;
       float o[2] = {T[i], __shfl_down_sync(0xFFFFFFFFu, T[i], 1)};
       if (c >= total || (c & 1)) continue;
