@@ -48,6 +48,33 @@ __device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatil
     }
   }
 }
+// the same for a barrier that the other CTA of a cluster arrives at too
+__device__ __forceinline__ void mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* dead) {
+  for (uint32_t i = 0;; ++i) {
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
+        : "=r"(done) : "r"(bar), "r"(parity) : "memory");
+    if (done) return;
+    if (i > (1u << 22) || (i > 1024 && *dead)) {
+      *dead = 1;
+      return;
+    }
+  }
+}
+// a word in global memory that another CTA sets to 1
+__device__ __forceinline__ void wait_flag(const uint32_t* flag, volatile int* dead) {
+  for (uint32_t i = 0;; ++i) {
+    uint32_t v;
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(flag) : "memory");
+    if (v) return;
+    if (i > (1u << 22) || (i > 1024 && *dead)) {
+      *dead = 1;
+      return;
+    }
+    __nanosleep(64);
+  }
+}
 // one box of a two-dimensional tensor map
 __device__ __forceinline__ void tensor_load(uint32_t dst, const void* map, int x, int y, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.2d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];" ::"r"(dst),

@@ -9,10 +9,14 @@
 // gradients (a rounding of 2^-9 beside the result's own), two with binary16 ones (2^-15 at most), three with binary32 ones (dz exactly); fewer
 // where dz itself has no more bits (see pieces()).  Every piece costs one more pass of the matrix instruction.
 //
+// Scales that differ by row or column belong to the summed index of one of the products: dz is multiplied by both before it is
+// rounded, and the other product divides its rows by the one that it does not want.  So both read the same pieces.
+//
 // Two launches:
-//   grad_prepare_kernel   reads g and z once; writes the pieces of dz, dz sb where the scale differs by column, the sums of its rows
-//                         per column (for the bias), and both operands' codes as bfloat16.  Bound by memory.
-//   grad_product_kernel   both products as one list of 128 x BN tiles (tcgen05, TMA), and the bias sums' last step.
+//   grad_prepare_kernel   reads g and z once; writes the pieces of scaled dz, the sums of dz over blocks of rows (for the bias) and both
+//                         operands' codes as bfloat16.  Bound by memory.
+//   grad_product_kernel   both products as one list of 256 x 256 tiles, a pair of CTAs each (tcgen05, TMA), cut into equal shares of work;
+//                         and the bias sums' last step.
 #include "lba_grad.cuh"
 
 #include "lba_async.cuh"
@@ -21,40 +25,52 @@
 namespace lba {
 namespace {
 
-constexpr int PREP_ROWS = 32, PREP_COLS = 256, PREP_THREADS = 256;
+constexpr int PREP_ROWS = 32, PREP_COLS = 256, PREP_THREADS = 256, PREP_EACH = PREP_ROWS * PREP_COLS / (8 * PREP_THREADS);
 typedef __nv_bfloat16 bf16;
 
 struct PrepParams {
   const void *grad, *pre;
   const uint8_t *A, *B, *B2;
-  const float *sa, *sb, *sb2;
+  const float *sa, *sb, *sb2;  // factors of dz: by row; by column or by half (null: none)
   const uint64_t* rng;
-  bf16 *za, *zb, *aw, *bw;   // pieces of dz for grad_a and for grad_b (planes of `plane` elements), codes of A and B
+  bf16 *z, *aw, *bw;         // pieces of dz (planes of `plane` elements), codes of A and B
   float* partial;            // [row blocks][nz] sums of dz
+  uint32_t* flags;           // words that the second kernel wants at zero
   int64_t M, N, K, np, nz, kp, plane;
-  int pieces_a, pieces_b;    // 0: not wanted
-  int grad_type, pre_type, act, gated, in_m4e3, sa_per_row, sb_per_col;
+  int pieces;                // 0: no product is wanted
+  int act, in_m4e3, sb_per_col, flag_words;
   uint32_t drop_below;
-  int shared;                // grad_a reads grad_b's pieces
   int64_t z_blocks, col_blocks, a_blocks;  // blocks of dz, then of A's codes, then of B's
 };
 
+template <typename T> struct Raw8;  // eight elements as they lie in memory
+template <> struct Raw8<float> { float4 v[2]; };
+template <> struct Raw8<bf16> { uint4 v; };
+template <> struct Raw8<__half> { uint4 v; };
 // eight neighbouring elements from i on, `valid` of which exist
-__device__ __forceinline__ void load8(const void* base, int type, int64_t i, int valid, float (&v)[8]) {
-  if (type == LT_F32) {
-    float lo[4], hi[4];
-    load_some<float, 4>(base, i, valid < 4 ? valid : 4, lo);
-    load_some<float, 4>(base, i + 4, valid > 4 ? valid - 4 : 0, hi);
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      v[j] = lo[j];
-      v[4 + j] = hi[j];
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8(const void* base, int64_t i, int valid) {
+  Raw8<T> r;
+  const T* const src = static_cast<const T*>(base) + i;
+  if (valid == 8 && (reinterpret_cast<uintptr_t>(src) & 15) == 0) {
+    if constexpr (sizeof(T) == 4) {
+      r.v[0] = __ldcs(reinterpret_cast<const float4*>(src));
+      r.v[1] = __ldcs(reinterpret_cast<const float4*>(src) + 1);
+    } else {
+      r.v = __ldcs(reinterpret_cast<const uint4*>(src));
     }
-  } else if (type == LT_BF16) {
-    load_some<bf16, 8>(base, i, valid, v);
   } else {
-    load_some<__half, 8>(base, i, valid, v);
+    T* const e = reinterpret_cast<T*>(&r);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) e[j] = j < valid ? src[j] : from_f32<T>(0.0f);
   }
+  return r;
+}
+template <typename T>
+__device__ __forceinline__ void widen8(const Raw8<T>& r, float (&v)[8]) {
+  const T* const e = reinterpret_cast<const T*>(&r);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) v[j] = to_f32(e[j]);
 }
 
 // v as the sum of bfloat16 pieces, all but the last cut toward zero (which cannot overflow and leaves an exact remainder)
@@ -91,7 +107,7 @@ __device__ __forceinline__ void store_pieces(bf16* dst, int64_t plane, int piece
 __device__ __forceinline__ void expand_codes(const PrepParams& p, const uint8_t* row, bf16* dst, int64_t k) {
   uint4 out = make_uint4(0u, 0u, 0u, 0u);
   if (row) {
-    uint8_t c[8];
+    __align__(8) uint8_t c[8];
     const int valid = p.K - k < 8 ? (int)(p.K - k) : 8;
     const uint8_t* const src = row + k;
     if (valid == 8 && (reinterpret_cast<uintptr_t>(src) & 7) == 0) {
@@ -101,20 +117,31 @@ __device__ __forceinline__ void expand_codes(const PrepParams& p, const uint8_t*
       for (int j = 0; j < 8; ++j) c[j] = j < valid ? __ldg(src + j) : (uint8_t)0;
     }
     uint32_t* const w = &out.x;
+    const uint32_t* const c4 = reinterpret_cast<const uint32_t*>(c);
 #pragma unroll
-    for (int j = 0; j < 8; j += 2) {
-      const float lo = p.in_m4e3 ? decode_m4e3_top((uint32_t)c[j] << 24) : decode_e4m3_top((uint32_t)c[j] << 24, 0x1p120f);
-      const float hi = p.in_m4e3 ? decode_m4e3_top((uint32_t)c[j + 1] << 24) : decode_e4m3_top((uint32_t)c[j + 1] << 24, 0x1p120f);
-      w[j / 2] = (__float_as_uint(lo) >> 16) | (__float_as_uint(hi) & 0xFFFF0000u);  // exact
+    for (int q = 0; q < 2; ++q) {
+      u64 v[2];
+      if (p.in_m4e3) decode4<true>(c4[q], v[0], v[1]);
+      else decode4<false>(c4[q], v[0], v[1]);
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        float lo, hi;
+        unpack2(v[e], lo, hi);
+        w[2 * q + e] = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);  // exact: the low halves are zero
+      }
     }
   }
   *reinterpret_cast<uint4*>(dst + k) = out;
 }
 
+template <typename G, typename Z, bool GATED>
 __global__ void __launch_bounds__(PREP_THREADS) grad_prepare_kernel(const PrepParams p) {
+  constexpr int HALVES = GATED ? 2 : 1;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   after_previous();
   int64_t b = blockIdx.x;
+  if (b == 0)
+    for (int i = threadIdx.x; i < p.flag_words; i += PREP_THREADS) p.flags[i] = 0u;
   if (b >= p.z_blocks) {  // codes: a warp takes a row at a time
     b -= p.z_blocks;
     const bool is_a = b < p.a_blocks;
@@ -135,89 +162,93 @@ __global__ void __launch_bounds__(PREP_THREADS) grad_prepare_kernel(const PrepPa
     return;
   }
 
-  __shared__ float sums[2][PREP_THREADS / 32][PREP_COLS];
-  const int64_t n = (b % p.col_blocks) * PREP_COLS + lane * 8, m0 = (b / p.col_blocks) * PREP_ROWS;
+  __shared__ float sums[HALVES][PREP_THREADS / 32][PREP_COLS];
+  const int64_t n = (b % p.col_blocks) * PREP_COLS + lane * 8, m0 = (b / p.col_blocks) * PREP_ROWS + warp;
   const int valid = n >= p.N ? 0 : p.N - n < 8 ? (int)(p.N - n) : 8;
-  const int halves = p.gated ? 2 : 1;
-  float total[2][8];
+  float total[HALVES][8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) total[0][j] = total[1][j] = 0.0f;
+  for (int h = 0; h < HALVES; ++h)
+#pragma unroll
+    for (int j = 0; j < 8; ++j) total[h][j] = 0.0f;
   if (n < p.np) {
-    float scale[2][8];
+    // all of a thread's loads before its first store: four rows of sixteen bytes and more are on their way at a time
+    Raw8<G> g[PREP_EACH];
+    Raw8<Z> z[PREP_EACH][HALVES];
+    const bool reads_z = GATED || p.act != ACT_NONE;
+#pragma unroll
+    for (int i = 0; i < PREP_EACH; ++i) {
+      const int64_t m = m0 + i * (PREP_THREADS / 32);
+      if (m >= p.M) break;
+      g[i] = load8<G>(p.grad, m * p.N + n, valid);
+      if (reads_z) {
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) z[i][h] = load8<Z>(p.pre, (h * p.M + m) * p.N + n, valid);
+      }
+    }
+    float scale[HALVES][8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      // (a linear layer's common scale is applied to the finished product)
-      scale[0][j] = p.sb_per_col ? (j < valid ? p.sb[n + j] : 0.0f) : p.gated ? p.sb[0] : 1.0f;
-      scale[1][j] = !p.gated ? 0.0f : p.sb_per_col ? (j < valid ? p.sb2[n + j] : 0.0f) : p.sb2[0];
+      scale[0][j] = !p.sb ? 1.0f : p.sb_per_col ? (j < valid ? p.sb[n + j] : 0.0f) : p.sb[0];
+      if (GATED) scale[HALVES - 1][j] = p.sb_per_col ? (j < valid ? p.sb2[n + j] : 0.0f) : p.sb2[0];
     }
-#pragma unroll 1
-    for (int i = 0; i < PREP_ROWS / 8; ++i) {
-      const int64_t m = m0 + i * 8 + warp;
-      if (m >= p.M) break;
-      float g[8], z[8], d[2][8];
-      load8(p.grad, p.grad_type, m * p.N + n, valid, g);
-      if (p.drop_below) {
-        const uint64_t seed = p.rng[0], offset = p.rng[1];
+    with_act(p.act, [&](auto act_tag) {
+      constexpr int ACT = decltype(act_tag)::value;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const uint4 r = philox((uint32_t)(n >> 2) + h, (uint32_t)m, offset, seed);
-          const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+      for (int i = 0; i < PREP_EACH; ++i) {
+        const int64_t m = m0 + i * (PREP_THREADS / 32);
+        if (m >= p.M) break;
+        float gv[8], zv[8], d[HALVES][8];
+        widen8(g[i], gv);
+        if (GATED || ACT != ACT_NONE) widen8(z[i][0], zv);
+        if (!GATED && p.drop_below) {
+          const uint64_t seed = p.rng[0], offset = p.rng[1];
 #pragma unroll
-          for (int j = 0; j < 4; ++j)
-            if (w[j] < p.drop_below) g[4 * h + j] = 0.0f;
+          for (int h = 0; h < 2; ++h) {
+            const uint4 r = philox((uint32_t)(n >> 2) + h, (uint32_t)m, offset, seed);
+            const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (w[j] < p.drop_below) gv[4 * h + j] = 0.0f;
+          }
         }
-      }
-      if (p.gated) {
-        float v[8];
-        load8(p.pre, p.pre_type, m * p.N + n, valid, z);
-        load8(p.pre, p.pre_type, (p.M + m) * p.N + n, valid, v);
+        if constexpr (GATED) {
+          float v[8];
+          widen8(z[i][1], v);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          d[0][j] = g[j] * v[j] * act_slope(p.act, z[j]);
-          d[1][j] = g[j] * act_value(p.act, z[j]);
+          for (int j = 0; j < 8; ++j) {
+            d[0][j] = gv[j] * v[j] * act_slope_of<ACT>(zv[j]);
+            d[1][j] = gv[j] * act_value_of<ACT>(zv[j]);
+          }
+        } else {
+#pragma unroll
+          for (int j = 0; j < 8; ++j)
+            d[0][j] = ACT == ACT_NONE ? gv[j] : ACT == ACT_RELU ? (zv[j] > 0.0f ? gv[j] : 0.0f) : gv[j] * act_slope_of<ACT>(zv[j]);
         }
-      } else if (p.act == ACT_NONE) {
+        const float by = p.sa ? p.sa[m] : 1.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) d[0][j] = g[j];
-      } else {
-        load8(p.pre, p.pre_type, m * p.N + n, valid, z);
-#pragma unroll
-        for (int j = 0; j < 8; ++j) d[0][j] = p.act == ACT_RELU ? (z[j] > 0.0f ? g[j] : 0.0f) : g[j] * act_slope(p.act, z[j]);
-      }
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        if (h >= halves) break;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          d[h][j] = j < valid ? d[h][j] : 0.0f;  // the padding of a row
-          total[h][j] += d[h][j];
-        }
-        const int64_t at = m * p.nz + h * p.np + n;
-        if (p.pieces_b) {
-          float s[8];
-          const float by = p.sa_per_row ? p.sa[m] : 1.0f;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) s[j] = d[h][j] * by;
-          store_pieces(p.zb + at, p.plane, p.pieces_b, s);
-        }
-        if (p.pieces_a && !p.shared) {
+        for (int h = 0; h < HALVES; ++h) {
           float s[8];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) s[j] = d[h][j] * scale[h][j];
-          store_pieces(p.za + at, p.plane, p.pieces_a, s);
+          for (int j = 0; j < 8; ++j) {
+            d[h][j] = j < valid ? d[h][j] : 0.0f;  // the padding of a row
+            total[h][j] += d[h][j];
+            s[j] = d[h][j] * (scale[h][j] * by);
+          }
+          if (p.pieces) store_pieces(p.z + m * p.nz + h * p.np + n, p.plane, p.pieces, s);
         }
       }
-    }
+    });
   }
   if (!p.partial) return;
 #pragma unroll
-  for (int h = 0; h < 2; ++h)
+  for (int h = 0; h < HALVES; ++h)
 #pragma unroll
     for (int j = 0; j < 8; ++j) sums[h][warp][lane * 8 + j] = total[h][j];
   __syncthreads();
   const int64_t col = (b % p.col_blocks) * PREP_COLS + threadIdx.x;
   if (col >= p.np) return;
-  for (int h = 0; h < halves; ++h) {
+#pragma unroll
+  for (int h = 0; h < HALVES; ++h) {
     float s = 0.0f;
 #pragma unroll
     for (int w = 0; w < PREP_THREADS / 32; ++w) s += sums[h][w][threadIdx.x];
@@ -229,35 +260,53 @@ __global__ void __launch_bounds__(PREP_THREADS) grad_prepare_kernel(const PrepPa
 // out[r][s] = alpha sum_l X[r][l] Y[l][s] over the pieces of X.
 //   grad_a: r = m, l = n, s = k; X's rows are contiguous in l (K-major)
 //   grad_b: r = n, l = m, s = k; X is read from the same layout, contiguous in r (MN-major); so is Y, contiguous in s, in both
-// Persistent CTAs of six warps: one thread loads (TMA, 128-byte swizzle), one issues tcgen05.mma into one of two accumulators of
-// BN columns of tensor memory, four warps bring the other one out.
-constexpr int BM = 128, BL = 64, GRAD_THREADS = 192;
-constexpr int X_BYTES = BM * BL * 2;
-template <int BN> constexpr int STAGE_BYTES = X_BYTES + BN * BL * 2;
-template <int BN> constexpr int STAGE_COUNT = BN == 256 ? 4 : BN == 128 ? 6 : 8;
-template <int BN> constexpr size_t PRODUCT_SMEM = 1024 + (size_t)STAGE_BYTES<BN> * STAGE_COUNT<BN> + 256;
+// A cluster of two CTAs forms a 256 x 256 tile: each CTA holds 128 rows of X, half of Y's columns and the accumulators of its rows, and
+// one thread of the first issues the matrix instructions of both (cta_group::2).  What bounds such a product is what the L2 can
+// deliver: a CTA alone with 128 x 256 outputs fetched 48 KB per 64 l where this takes 32 (4096 x 4096 x 1024: 82 us alone).
+// Six warps a CTA: one thread loads, one multiplies into one of two accumulators of 256 columns of tensor memory, four bring the
+// other one out.
+//
+// Equal shares.  The tiles' steps of 64 l stand in one row, cut into shares of equal length; a cluster walks its own from the end.  A
+// tile that a border cuts is begun by lower shares, which leave binary32 sums in the workspace, and finished by the share with its last
+// step, which adds them in order.  A cluster takes the number of its share when it starts, from a counter, so it only ever waits for
+// clusters that run already or have ended, and what it waits for is the first thing that those do.  Where whole tiles divide as well, they stay whole.
+constexpr int BM = 128, BN = 256, BL = 64, GRAD_THREADS = 192;  // of a CTA: rows, columns, step
+constexpr int X_BYTES = BM * BL * 2, STAGE = 2 * X_BYTES, STAGES = 6;
+constexpr size_t PRODUCT_SMEM = 1024 + (size_t)STAGE * STAGES + 256;
+constexpr int PART_FLOATS = BM * BN;  // a CTA's part of a begun tile
 
 struct Job {
   int64_t rows, cols;       // of one half's output
   int64_t r_tiles, s_tiles; // r_tiles: of one half
   int64_t half;             // X's coordinate r of the second half
-  int x_mn, pieces, l_blocks, halves;
+  int x_mn, pieces, steps;  // steps: blocks of l times pieces
+  int div_stride;
   void* out[2];
-  const float *alpha[2];    // device factors of each half (null: 1)
+  const float *alpha[2], *div[2];  // factors of a half, divisors of its rows (or null)
 };
 struct ProductParams {
   CUtensorMap x[2], y[2];
   Job job[2];
   int64_t tiles0, tiles;    // of the first job, of both
+  int64_t units0, units;    // their steps
+  int64_t share;            // steps of a cluster; 0: whole tiles
   int out_type;
   float factor;
+  uint32_t* flags;          // shares: the counter, then a word per CTA's part
+  float* parts;
   const float* partial;     // bias: [row blocks][nz]
   float* bias[2];
   int64_t row_blocks, N, np, nz;
 };
 
+__device__ __forceinline__ uint32_t mapa(uint32_t addr, int rank) {
+  uint32_t d;
+  asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(d) : "r"(addr), "r"(rank));
+  return d;
+}
+// a box of a three-dimensional map into this CTA's memory, counted by a barrier of either CTA of the pair
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
+  asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
                "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
 }
 // Shared-memory operand of a matrix instruction, 128-byte swizzle: 1024-byte groups of eight 128-byte lines.  K-major: a line is
@@ -268,11 +317,20 @@ __device__ __forceinline__ uint64_t operand(uint32_t addr, int lead, int stride)
 }
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
   asm volatile(
-      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b),
+      "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b),
       "r"(idesc), "r"((uint32_t)add) : "memory");
 }
+// the barrier at this address in both CTAs
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
-  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+  asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3)
+               : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
+  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void cluster_sync() {
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
 }
 __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t (&r)[32]) {
   asm volatile(
@@ -286,22 +344,52 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t (&r)[32]) {
   tmem_wait_ld();
 }
 
-struct Tile {
-  int job, half;
-  int64_t r, s;  // first row (of the half) and column
+// a cluster's work, piece by piece: a tile and some of its steps
+struct Work {
+  int job, half, k0, k1;
+  int64_t r, s, start;  // first row (of the half) and column, the tile's first step among all
 };
-template <int BN>
-__device__ __forceinline__ Tile tile_of(const ProductParams& p, int64_t t) {
-  Tile v;
-  v.job = t >= p.tiles0;
-  const Job& j = p.job[v.job];
-  if (v.job) t -= p.tiles0;
-  v.s = (t % j.s_tiles) * BN;
-  t /= j.s_tiles;
-  v.half = t >= j.r_tiles;
-  v.r = (v.half ? t - j.r_tiles : t) * BM;
-  return v;
-}
+struct Walk {
+  int64_t at, end, by;  // shares: steps [end, at) are left; whole tiles: the next tile, their number
+  __device__ __forceinline__ Walk(const ProductParams& p, int64_t c, int64_t clusters) {
+    by = clusters;
+    if (p.share) {
+      end = c * p.share;
+      at = end + p.share < p.units ? end + p.share : p.units;
+    } else {
+      at = c;
+      end = p.tiles;
+    }
+  }
+  __device__ __forceinline__ bool next(const ProductParams& p, Work& w) {
+    int64_t t;
+    if (p.share) {
+      if (at <= end) return false;
+      w.job = at - 1 >= p.units0;
+      const int steps = p.job[w.job].steps;
+      const int64_t base = w.job ? p.units0 : 0;
+      t = (at - 1 - base) / steps;
+      w.start = base + t * steps;
+      w.k1 = (int)(at - w.start);
+      w.k0 = end > w.start ? (int)(end - w.start) : 0;
+      at = w.start + w.k0;
+    } else {
+      if (at >= end) return false;
+      w.job = at >= p.tiles0;
+      t = w.job ? at - p.tiles0 : at;
+      w.k0 = 0;
+      w.k1 = p.job[w.job].steps;
+      w.start = 0;
+      at += by;
+    }
+    const Job& j = p.job[w.job];
+    w.s = (t % j.s_tiles) * BN;
+    t /= j.s_tiles;
+    w.half = t >= j.r_tiles;
+    w.r = (w.half ? t - j.r_tiles : t) * (2 * BM);
+    return true;
+  }
+};
 
 // the bias' gradient: sums of the row blocks' sums, in their order; a warp adds every fourth of 32 columns
 __device__ __forceinline__ void bias_sums(const ProductParams& p, float (*part)[32], int warp, int lane) {
@@ -320,7 +408,7 @@ __device__ __forceinline__ void bias_sums(const ProductParams& p, float (*part)[
 }
 
 template <typename T>
-__device__ __forceinline__ void store32(T* dst, int64_t valid, const uint32_t (&r)[32], float alpha) {
+__device__ __forceinline__ void store32(T* dst, int64_t valid, const float (&r)[32], float alpha) {
   constexpr int W = 16 / (int)sizeof(T);
   if (valid >= 32 && (reinterpret_cast<uintptr_t>(dst) & 15) == 0) {
 #pragma unroll
@@ -328,101 +416,113 @@ __device__ __forceinline__ void store32(T* dst, int64_t valid, const uint32_t (&
       uint4 raw;
       T* const e = reinterpret_cast<T*>(&raw);
 #pragma unroll
-      for (int j = 0; j < W; ++j) e[j] = from_f32<T>(__uint_as_float(r[q * W + j]) * alpha);
+      for (int j = 0; j < W; ++j) e[j] = from_f32<T>(r[q * W + j] * alpha);
       *reinterpret_cast<uint4*>(dst + q * W) = raw;
     }
   } else {
 #pragma unroll
     for (int j = 0; j < 32; ++j)
-      if (j < valid) dst[j] = from_f32<T>(__uint_as_float(r[j]) * alpha);
+      if (j < valid) dst[j] = from_f32<T>(r[j] * alpha);
   }
 }
 
-template <int BN>
 __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __grid_constant__ ProductParams p) {
-  constexpr int STAGES = STAGE_COUNT<BN>, STAGE = STAGE_BYTES<BN>;
-  constexpr uint32_t COLS = 2 * BN;  // of tensor memory: 128, 256 or 512
-  extern __shared__ unsigned char smem_raw[];
-  unsigned char* const base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+  extern __shared__ unsigned char product_raw[];
+  unsigned char* const base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(product_raw) + 1023) & ~(uintptr_t)1023);
   uint64_t* const bars = reinterpret_cast<uint64_t*>(base + STAGES * STAGE);  // full, empty per stage; done, free per accumulator
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 4);
   volatile int* const dead = reinterpret_cast<volatile int*>(tmem_slot + 1);
+  uint32_t* const share_slot = tmem_slot + 2;
   __shared__ float part[4][32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = blockIdx.x & 1;  // in the cluster
   const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, acc_done = empty + 8 * STAGES, acc_free = acc_done + 16;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < STAGES; ++i) {
-      mbar_init(full + 8 * i, 1);
+      mbar_init(full + 8 * i, 1);   // the first CTA's counts both CTAs' bytes
       mbar_init(empty + 8 * i, 1);
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(acc_done + 8 * i, 1);
-      mbar_init(acc_free + 8 * i, 128);
+      mbar_init(acc_free + 8 * i, 256);  // the first CTA's: both CTAs' readers
     }
     *dead = 0;
     mbar_init_fence();
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(COLS) : "memory");
-    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(2 * BN) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
+  __syncwarp();
+  cluster_sync();  // the other CTA runs: its memory may be written
+  after_previous();
+  if (p.share && rank == 0 && threadIdx.x == 0) {
+    const uint32_t c = atomicAdd(p.flags, 1u);
+    *share_slot = c;
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(mapa(smem_u32(share_slot), 1)), "r"(c) : "memory");
+  }
+  __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-  __syncthreads();
+  cluster_sync();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = *tmem_slot;
-  after_previous();
+  const int64_t share = p.share ? *share_slot : blockIdx.x >> 1;
+  Walk walk(p, share, gridDim.x >> 1);
+  Work w;
 
   if (warp == 0) {
     if (lane == 0) {
       int stage = 0;
       uint32_t phase = 0;
-      for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x) {
-        const Tile v = tile_of<BN>(p, t);
-        const Job& j = p.job[v.job];
-        const int r = (int)(v.r + (v.half ? j.half : 0)), s = (int)v.s;
-        for (int b = 0; b < j.l_blocks; ++b)
-          for (int q = 0; q < j.pieces; ++q) {
-            mbar_wait(empty + 8 * stage, phase ^ 1, dead);
-            if (*dead) goto loaded;
-            const uint32_t x = smem_u32(base + stage * STAGE), y = x + X_BYTES, bar = full + 8 * stage;
-            mbar_arrive_expect(bar, STAGE);
-            if (j.x_mn) {
-              tma_load(x, &p.x[v.job], r, b * BL, q, bar);
-              tma_load(x + X_BYTES / 2, &p.x[v.job], r + 64, b * BL, q, bar);
-            } else {
-              tma_load(x, &p.x[v.job], b * BL, r, q, bar);
-            }
-#pragma unroll
-            for (int i = 0; i < BN / 64; ++i) tma_load(y + i * 64 * BL * 2, &p.y[v.job], s + 64 * i, b * BL, 0, bar);
-            if (++stage == STAGES) {
-              stage = 0;
-              phase ^= 1;
-            }
+      while (walk.next(p, w)) {
+        const Job& j = p.job[w.job];
+        const int r = (int)(w.r + (w.half ? j.half : 0)) + rank * BM, s = (int)w.s + rank * (BN / 2);
+        int l = w.k0 / j.pieces, q = w.k0 % j.pieces;
+        for (int k = w.k0; k < w.k1; ++k) {
+          mbar_wait(empty + 8 * stage, phase ^ 1, dead);
+          if (*dead) goto loaded;
+          const uint32_t x = smem_u32(base + stage * STAGE), y = x + X_BYTES, bar = mapa(full + 8 * stage, 0);
+          if (rank == 0) mbar_arrive_expect(full + 8 * stage, 2 * STAGE);
+          if (j.x_mn) {
+            tma_load(x, &p.x[w.job], r, l * BL, q, bar);
+            tma_load(x + X_BYTES / 2, &p.x[w.job], r + 64, l * BL, q, bar);
+          } else {
+            tma_load(x, &p.x[w.job], l * BL, r, q, bar);
           }
+          tma_load(y, &p.y[w.job], s, l * BL, 0, bar);
+          tma_load(y + X_BYTES / 2, &p.y[w.job], s + 64, l * BL, 0, bar);
+          if (++q == j.pieces) {
+            q = 0;
+            ++l;
+          }
+          if (++stage == STAGES) {
+            stage = 0;
+            phase ^= 1;
+          }
+        }
       }
     loaded:;
     }
   } else if (warp == 1) {
-    if (lane == 0) {
+    if (lane == 0 && rank == 0) {
       int stage = 0, acc = 0;
       uint32_t phase = 0, acc_phase = 0;
-      for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x) {
-        const Job& j = p.job[tile_of<BN>(p, t).job];
-        const int x_mn = j.x_mn, steps = j.l_blocks * j.pieces;
+      while (walk.next(p, w)) {
+        const int x_mn = p.job[w.job].x_mn;
         // binary32 sums of bfloat16 products; which operand is MN-major; sizes
-        const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)x_mn << 15) | (1u << 16) | ((BN / 8) << 17) | ((BM / 16) << 24);
-        mbar_wait(acc_free + 8 * acc, acc_phase ^ 1, dead);
+        const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)x_mn << 15) | (1u << 16) | ((BN / 8) << 17) | ((2 * BM / 16) << 24);
+        mbar_wait_cluster(acc_free + 8 * acc, acc_phase ^ 1, dead);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-        for (int b = 0; b < steps; ++b) {
-          mbar_wait(full + 8 * stage, phase, dead);
+        for (int b = w.k0; b < w.k1; ++b) {
+          mbar_wait_cluster(full + 8 * stage, phase, dead);
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t x = smem_u32(base + stage * STAGE), y = x + X_BYTES;
           if (!*dead) {
 #pragma unroll
             for (int k = 0; k < BL / 16; ++k)
               mma(tmem + acc * BN, x_mn ? operand(x + k * 2048, X_BYTES / 2, 1024) : operand(x + k * 32, 16, 1024),
-                  operand(y + k * 2048, 64 * BL * 2, 1024), idesc, b > 0 || k > 0);
+                  operand(y + k * 2048, X_BYTES / 2, 1024), idesc, b > w.k0 || k > 0);
           }
           mma_commit(empty + 8 * stage);
           if (++stage == STAGES) {
@@ -439,29 +539,63 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
     }
   } else {
     const int quarter = warp & 3;  // the lanes of tensor memory that this warp may read
+    const int row = quarter * 32 + lane;
     if (p.partial) bias_sums(p, part, quarter, lane);
     int acc = 0;
     uint32_t phase = 0;
-    for (int64_t t = blockIdx.x; t < p.tiles; t += gridDim.x) {
-      const Tile v = tile_of<BN>(p, t);
-      const Job& j = p.job[v.job];
+    while (walk.next(p, w)) {
+      const Job& j = p.job[w.job];
+      const bool begins = w.k1 < j.steps, ends = w.k0 > 0 && !begins;
+      const int64_t first = ends ? w.start / p.share : share;  // the shares that began this tile: first to share - 1
+      if (ends) {
+        if (row == 0)
+          for (int64_t c = first; c < share; ++c) wait_flag(p.flags + 1 + 2 * c + rank, dead);
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+      }
       mbar_wait(acc_done + 8 * acc, phase, dead);
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const int64_t r = v.r + quarter * 32 + lane;
-      const float alpha = *dead ? __uint_as_float(0x7FC00000u) : p.factor * (j.alpha[v.half] ? *j.alpha[v.half] : 1.0f);
+      const int64_t r = w.r + rank * BM + row;
+      float alpha = p.factor * (j.alpha[w.half] ? *j.alpha[w.half] : 1.0f);
+      if (j.div[w.half] && r < j.rows) alpha = __fdiv_rn(alpha, j.div[w.half][r * j.div_stride]);
+      if (*dead) alpha = __uint_as_float(0x7FC00000u);
+      float4* const mine = reinterpret_cast<float4*>(p.parts + (2 * share + rank) * PART_FLOATS) + row;  // [four columns][row]
 #pragma unroll 1
       for (int c = 0; c < BN; c += 32) {
-        uint32_t w[32];
-        tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + acc * BN + c, w);
-        const int64_t valid = j.cols - (v.s + c), at = r * j.cols + v.s + c;
+        uint32_t t[32];
+        float v[32];
+        tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + acc * BN + c, t);
+#pragma unroll
+        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(t[i]);
+        if (begins) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) mine[(c / 4 + i) * BM] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+          continue;
+        }
+        for (int64_t o = first; o < share; ++o) {
+          const float4* const theirs = reinterpret_cast<const float4*>(p.parts + (2 * o + rank) * PART_FLOATS) + row;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float4 f = __ldcg(theirs + (c / 4 + i) * BM);
+            v[4 * i] += f.x;
+            v[4 * i + 1] += f.y;
+            v[4 * i + 2] += f.z;
+            v[4 * i + 3] += f.w;
+          }
+        }
+        const int64_t valid = j.cols - (w.s + c), at = r * j.cols + w.s + c;
         if (r < j.rows && valid > 0) {
-          if (p.out_type == LT_F32) store32(static_cast<float*>(j.out[v.half]) + at, valid, w, alpha);
-          else if (p.out_type == LT_BF16) store32(static_cast<bf16*>(j.out[v.half]) + at, valid, w, alpha);
-          else store32(static_cast<__half*>(j.out[v.half]) + at, valid, w, alpha);
+          if (p.out_type == LT_F32) store32(static_cast<float*>(j.out[w.half]) + at, valid, v, alpha);
+          else if (p.out_type == LT_BF16) store32(static_cast<bf16*>(j.out[w.half]) + at, valid, v, alpha);
+          else store32(static_cast<__half*>(j.out[w.half]) + at, valid, v, alpha);
         }
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-      mbar_arrive(acc_free + 8 * acc);
+      mbar_arrive_cluster(mapa(acc_free + 8 * acc, 0));
+      if (begins) {
+        __threadfence();
+        asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (row == 0) asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(p.flags + 1 + 2 * share + rank), "r"(1u) : "memory");
+      }
       if (++acc == 2) {
         acc = 0;
         phase ^= 1;
@@ -470,8 +604,8 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
   }
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-  __syncthreads();
-  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(COLS) : "memory");
+  cluster_sync();  // nothing of the other CTA's is on its way here any more
+  if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * BN) : "memory");
 }
 
 // ------------------------------------------------------------------ host
@@ -480,41 +614,72 @@ size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 // bfloat16 pieces that dz takes beside a result of the given type; dz that is g itself or zero has no more bits than g, and a
 // common scale is applied to the finished product
-int pieces(const GradCall& c, bool scaled) {
+int pieces(const GradCall& c) {
   const auto of = [](int type) { return type == LT_BF16 ? 1 : type == LT_F16 ? 2 : 3; };
-  const bool plain = !c.gated && (c.act == ACT_NONE || c.act == ACT_RELU) && !scaled;
+  const bool plain = !c.gated && (c.act == ACT_NONE || c.act == ACT_RELU) && !c.sa_per_row && !c.sb_per_col;
   return plain && of(c.grad_type) < of(c.out_type) ? of(c.grad_type) : of(c.out_type);
+}
+
+int clusters_of_the_device() {
+  int dev = 0, n = 0;
+  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n < 2) return 74;
+  return n / 2;
 }
 
 struct Layout {
   int64_t np, nz, kp, row_blocks;
-  int pieces_a, pieces_b;
-  bool shared;  // both products read the same pieces of dz
-  size_t za, zb, aw, bw, partial, total;
+  int pieces, flag_words;
+  // tiles of the products and their division (see the product kernel)
+  int64_t tiles[2], units[2], share;
+  int steps[2], clusters;
+  size_t z, aw, bw, partial, flags, parts, total;
 };
 Layout layout(const GradCall& c) {
-  Layout l;
+  Layout l = {};
   const int halves = c.gated ? 2 : 1;
+  const bool a = c.grad_a && c.K > 0, b = c.grad_b && c.K > 0;
   l.np = up(c.N, 8);
   l.nz = l.np * halves;
   l.kp = up(c.K, 8);
   l.row_blocks = (c.M + PREP_ROWS - 1) / PREP_ROWS;
-  l.pieces_a = c.grad_a ? pieces(c, c.sb_per_col) : 0;
-  l.pieces_b = c.grad_b || c.grad_b2 ? pieces(c, c.sa_per_row) : 0;
-  // A gated layer's halves have scales of their own, so grad_a needs them inside dz
-  l.shared = l.pieces_a && l.pieces_b && l.pieces_a == l.pieces_b && !c.sb_per_col && !c.sa_per_row && !c.gated;
-  const size_t plane = (size_t)c.M * l.nz * 2;
+  l.pieces = a || b ? pieces(c) : 0;
+  const auto blocks = [](int64_t n, int64_t by) { return (n + by - 1) / by; };
+  if (a) {
+    l.steps[0] = (int)(blocks(l.nz, BL) * l.pieces);
+    l.tiles[0] = blocks(c.M, 2 * BM) * blocks(c.K, BN);
+  }
+  if (b) {
+    l.steps[1] = (int)(blocks(c.M, BL) * l.pieces);
+    l.tiles[1] = halves * blocks(c.N, 2 * BM) * blocks(c.K, BN);
+  }
+  for (int i = 0; i < 2; ++i) l.units[i] = l.tiles[i] * l.steps[i];
+  // Whole tiles, in turn, or equal shares: a cut costs about ten steps (a part written and read again), and a share has at least four
+  const int64_t all = l.tiles[0] + l.tiles[1], units = l.units[0] + l.units[1], most = clusters_of_the_device();
+  if (all > 0) {
+    const int64_t n = all < most ? all : most;
+    int64_t whole = 0;  // steps of the busiest cluster: cluster c takes the tiles c, c + n, ...
+    for (int64_t x = 0; x < n; ++x) {
+      const int64_t first = x < l.tiles[0] ? (l.tiles[0] - 1 - x) / n + 1 : 0, both = (all - 1 - x) / n + 1;
+      const int64_t load = first * l.steps[0] + (both - first) * l.steps[1];
+      whole = load > whole ? load : whole;
+    }
+    const int64_t even = blocks(units, most) < 4 ? 4 : blocks(units, most);
+    l.share = even + 10 < whole ? even : 0;
+    l.clusters = (int)(l.share ? blocks(units, l.share) : n);
+  }
+  l.flag_words = l.share ? 1 + 2 * l.clusters : 0;
   size_t at = 0;
   const auto take = [&at](size_t bytes) {
     const size_t was = at;
     at += up256(bytes);
     return was;
   };
-  l.zb = take(plane * l.pieces_b);
-  l.za = l.shared ? l.zb : take(plane * l.pieces_a);
-  l.aw = take(l.pieces_b ? (size_t)c.M * l.kp * 2 : 0);
-  l.bw = take(l.pieces_a ? (size_t)l.nz * l.kp * 2 : 0);
-  l.partial = take(c.grad_bias || c.grad_bias2 ? (size_t)l.row_blocks * l.nz * 4 : 0);
+  l.z = take((size_t)c.M * l.nz * 2 * l.pieces);
+  l.aw = take(b ? (size_t)c.M * l.kp * 2 : 0);
+  l.bw = take(a ? (size_t)l.nz * l.kp * 2 : 0);
+  l.partial = take(c.grad_bias ? (size_t)l.row_blocks * l.nz * 4 : 0);
+  l.flags = take((size_t)l.flag_words * 4);
+  l.parts = take(l.share ? (size_t)l.clusters * 2 * PART_FLOATS * 4 : 0);
   l.total = at;
   return l;
 }
@@ -529,22 +694,15 @@ bool make_map(CUtensorMap* map, const void* base, int64_t cols, int64_t rows, in
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-int multiprocessors() {
-  int dev = 0, n = 0;
-  if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess || n <= 0) return 148;
-  return n;
+template <typename G, typename Z>
+cudaError_t launch_prepare(const PrepParams& q, bool gated, unsigned blocks, cudaStream_t stream) {
+  return gated ? launch_after(grad_prepare_kernel<G, Z, true>, dim3(blocks), PREP_THREADS, 0, stream, q)
+               : launch_after(grad_prepare_kernel<G, Z, false>, dim3(blocks), PREP_THREADS, 0, stream, q);
 }
-
-template <int BN>
-cudaError_t launch_products(const ProductParams& p, int sms, cudaStream_t stream) {
-  auto kernel = grad_product_kernel<BN>;
-  constexpr size_t smem = PRODUCT_SMEM<BN>;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
-  if (e != cudaSuccess) return e;
-  int64_t grid = p.tiles;
-  if (p.partial && (p.nz + 31) / 32 > grid) grid = (p.nz + 31) / 32;
-  if (grid > sms) grid = sms;
-  return launch_after(kernel, dim3((unsigned)grid), GRAD_THREADS, smem, stream, p);
+template <typename G>
+cudaError_t launch_prepare(const PrepParams& q, const GradCall& c, unsigned blocks, cudaStream_t stream) {
+  return c.pre_type == LT_F32 ? launch_prepare<G, float>(q, c.gated, blocks, stream)
+         : c.pre_type == LT_BF16 ? launch_prepare<G, bf16>(q, c.gated, blocks, stream) : launch_prepare<G, __half>(q, c.gated, blocks, stream);
 }
 
 }  // namespace
@@ -565,93 +723,91 @@ cudaError_t launch_backward(const GradCall& c, void* workspace, cudaStream_t str
     zero(c.grad_bias2, c.N * 4);
     return e;
   }
-  GradCall w = c;
-  if (c.K == 0) w.grad_a = w.grad_b = w.grad_b2 = nullptr;  // nothing to write
-  const Layout l = layout(w);
-  if (!l.pieces_a && !l.pieces_b && !w.grad_bias && !w.grad_bias2) return cudaSuccess;
+  const Layout l = layout(c);
+  const bool a = l.tiles[0] > 0, b = l.tiles[1] > 0;
+  if (!a && !b && !c.grad_bias) return cudaSuccess;
   unsigned char* const ws = static_cast<unsigned char*>(workspace);
-  const int halves = c.gated ? 2 : 1;
 
   PrepParams q = {};
   q.grad = c.grad; q.pre = c.pre; q.A = c.A; q.B = c.B; q.B2 = c.B2;
-  q.sa = c.sa; q.sb = c.sb; q.sb2 = c.sb2; q.rng = c.rng;
-  q.za = reinterpret_cast<bf16*>(ws + l.za);
-  q.zb = reinterpret_cast<bf16*>(ws + l.zb);
+  q.sa = c.sa_per_row ? c.sa : nullptr;
+  q.sb = c.sb_per_col || c.gated ? c.sb : nullptr;
+  q.sb2 = c.sb2;
+  q.rng = c.rng;
+  q.z = reinterpret_cast<bf16*>(ws + l.z);
   q.aw = reinterpret_cast<bf16*>(ws + l.aw);
   q.bw = reinterpret_cast<bf16*>(ws + l.bw);
-  q.partial = w.grad_bias || w.grad_bias2 ? reinterpret_cast<float*>(ws + l.partial) : nullptr;
+  q.partial = c.grad_bias ? reinterpret_cast<float*>(ws + l.partial) : nullptr;
+  q.flags = reinterpret_cast<uint32_t*>(ws + l.flags);
+  q.flag_words = l.flag_words;
   q.M = c.M; q.N = c.N; q.K = c.K; q.np = l.np; q.nz = l.nz; q.kp = l.kp;
   q.plane = c.M * l.nz;
-  q.pieces_a = l.pieces_a; q.pieces_b = l.pieces_b; q.shared = l.shared;
-  q.grad_type = c.grad_type; q.pre_type = c.pre_type; q.act = c.act; q.gated = c.gated; q.in_m4e3 = c.in_m4e3;
-  q.sa_per_row = c.sa_per_row; q.sb_per_col = c.sb_per_col;
+  q.pieces = l.pieces;
+  q.act = c.act; q.in_m4e3 = c.in_m4e3; q.sb_per_col = c.sb_per_col;
   q.drop_below = c.drop_below;
   q.col_blocks = (l.np + PREP_COLS - 1) / PREP_COLS;
   q.z_blocks = q.col_blocks * l.row_blocks;
-  q.a_blocks = l.pieces_b ? (c.M + 7) / 8 : 0;
-  const int64_t b_blocks = l.pieces_a ? (l.nz + 7) / 8 : 0, blocks = q.z_blocks + q.a_blocks + b_blocks;
+  q.a_blocks = b ? (c.M + 7) / 8 : 0;
+  const int64_t b_blocks = a ? (l.nz + 7) / 8 : 0, blocks = q.z_blocks + q.a_blocks + b_blocks;
   if (blocks > 2147483647LL) return cudaErrorInvalidValue;
-  if ((e = launch_after(grad_prepare_kernel, dim3((unsigned)blocks), PREP_THREADS, 0, stream, q)) != cudaSuccess) return e;
+  e = c.grad_type == LT_F32 ? launch_prepare<float>(q, c, (unsigned)blocks, stream)
+      : c.grad_type == LT_BF16 ? launch_prepare<bf16>(q, c, (unsigned)blocks, stream) : launch_prepare<__half>(q, c, (unsigned)blocks, stream);
+  if (e != cudaSuccess) return e;
 
   ProductParams p = {};
   p.out_type = c.out_type;
   p.factor = c.keep_scale;
   p.partial = q.partial;
-  p.bias[0] = w.grad_bias; p.bias[1] = w.grad_bias2;
+  p.bias[0] = c.grad_bias; p.bias[1] = c.grad_bias2;
   p.row_blocks = l.row_blocks; p.N = c.N; p.np = l.np; p.nz = l.nz;
-  int jobs = 0;
-  const auto add = [&](const void* x, bool x_mn, int np, const void* y, int64_t y_rows, int64_t rows, int64_t length) -> Job& {
-    if (!make_map(&p.x[jobs], x, l.nz, c.M, np, l.nz, q.plane, x_mn ? BL : BM) || !make_map(&p.y[jobs], y, c.K, y_rows, 1, l.kp, y_rows * l.kp, BL))
+  p.flags = q.flags;
+  p.parts = reinterpret_cast<float*>(ws + l.parts);
+  p.share = l.share;
+  p.tiles0 = p.tiles = l.tiles[0];
+  p.units0 = p.units = l.units[0];
+  p.tiles += l.tiles[1];
+  p.units += l.units[1];
+  // (a job without tiles is never looked at: the first one's borders are both 0 then)
+  const auto add = [&](int i, bool x_mn, const void* y, int64_t y_rows, int64_t rows) -> Job& {
+    if (!make_map(&p.x[i], q.z, l.nz, c.M, l.pieces, l.nz, q.plane, x_mn ? BL : BM) ||
+        !make_map(&p.y[i], y, c.K, y_rows, 1, l.kp, y_rows * l.kp, BL))
       e = cudaErrorInvalidValue;
-    Job& j = p.job[jobs++];
+    Job& j = p.job[i];
     j.x_mn = x_mn;
-    j.pieces = np;
+    j.pieces = l.pieces;
+    j.steps = l.steps[i];
     j.rows = rows;
     j.cols = c.K;
-    j.l_blocks = (int)((length + BL - 1) / BL);
-    j.r_tiles = (rows + BM - 1) / BM;
-    j.halves = 1;
+    j.r_tiles = (rows + 2 * BM - 1) / (2 * BM);
+    j.s_tiles = (c.K + BN - 1) / BN;
     return j;
   };
-  if (l.pieces_a) {
-    Job& j = add(q.za, false, l.pieces_a, q.bw, l.nz, c.M, l.nz);
+  if (a) {
+    Job& j = add(0, false, q.bw, l.nz, c.M);
     j.out[0] = c.grad_a;
-    j.alpha[0] = c.sb_per_col || c.gated ? nullptr : c.sb;
+    j.alpha[0] = q.sb ? nullptr : c.sb;
+    j.div[0] = q.sa;
+    j.div_stride = 1;
   }
-  if (l.pieces_b) {
-    Job& j = add(q.zb, true, l.pieces_b, q.aw, c.M, c.N, c.M);
+  if (b) {
+    Job& j = add(1, true, q.aw, c.M, c.N);
     j.out[0] = c.grad_b;
     j.out[1] = c.grad_b2;
-    j.alpha[0] = j.alpha[1] = c.sa_per_row ? nullptr : c.sa;
-    j.halves = halves;
+    j.alpha[0] = j.alpha[1] = q.sa ? nullptr : c.sa;
+    j.div[0] = q.sb;
+    j.div[1] = c.sb2;
+    j.div_stride = c.sb_per_col;
     j.half = l.np;
   }
   if (e != cudaSuccess) return e;
-
-  // Tile width: the fewest rounds of tiles over the SMs, each round weighted by what a step of such a tile takes
-  const int sms = multiprocessors();
-  const auto tiles = [&](int bn) {
-    p.tiles = p.tiles0 = 0;
-    for (int i = 0; i < jobs; ++i) {
-      p.job[i].s_tiles = (c.K + bn - 1) / bn;
-      p.tiles += p.job[i].s_tiles * p.job[i].r_tiles * p.job[i].halves;
-      if (i == 0) p.tiles0 = p.tiles;
-    }
-    return p.tiles;
-  };
-  const int widths[3] = {256, 128, 64};
-  const double cost[3] = {1.0, 0.58, 0.4};
-  int best = 0;
-  double least = 1e300;
-  for (int i = 0; i < 3; ++i) {
-    const double t = (double)((tiles(widths[i]) + sms - 1) / sms) * cost[i];
-    if (t < least) {
-      least = t;
-      best = i;
-    }
+  e = cudaFuncSetAttribute(grad_product_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PRODUCT_SMEM);
+  if (e != cudaSuccess) return e;
+  int64_t clusters = l.clusters;
+  if (!p.share && c.grad_bias) {  // more CTAs for the bias: they find no tile
+    const int64_t wanted = (l.nz + 63) / 64, most = clusters_of_the_device();
+    if (clusters < wanted) clusters = wanted < most ? wanted : most;
   }
-  tiles(widths[best]);
-  return best == 0 ? launch_products<256>(p, sms, stream) : best == 1 ? launch_products<128>(p, sms, stream) : launch_products<64>(p, sms, stream);
+  return launch_after(grad_product_kernel, dim3((unsigned)(2 * clusters)), GRAD_THREADS, PRODUCT_SMEM, stream, p, 2);
 }
 
 }  // namespace lba

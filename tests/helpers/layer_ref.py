@@ -59,9 +59,10 @@ def slope(z, name):
     return torch.ones_like(z)
 
 
-# A binary32 activation is off by at most |z| 2^-21: the inner function (erff, tanhf: 2 ulp, below 2^-22 of 1; expf: 2 ulp) sees an
-# argument that is off by 4 roundings, 2^-22 relative, which moves it by less than 0.5 x 2^-22; the sum with 1 adds 2^-23; half of
-# these times |z| is below |z| 2^-22, and the remaining two products or the division add 2^-23 of a value that is at most |z|.
+# A binary32 activation is off by at most |z| 2^-21.  gelu: the approximation of P by 7.5e-8, its five-term sum and the product with the
+# density (at most 0.4) by 2^-23 together, 1 - q by 2^-25: 2.2e-7 < 2^-22, times |z|; two more products, 2^-23 of at most |z|.  The
+# logistic function: an exponential off by (2 + 1.2 |x|) 2^-24 relative, and the slope s (1 - s) that takes it to s has x s (1 - s) <=
+# 0.23 and s (1 - s) <= 1/4: below 2^-24 + 2^-25; the sum with 1 and the reciprocal (2 units) 2^-23.4 of s: below 2^-22 of 1.
 ACT_ERR = 2.0 ** -21
 
 
@@ -71,8 +72,8 @@ def half_step(dtype, v):
     rel = {"e4m3": 2.0 ** -4, "m4e3": 2.0 ** -5}.get(dtype) or torch.finfo(dtype).eps / 2
     return v.abs() * rel + tiny
 
-# A binary32 slope is off by at most 2^-18: the worst is gelu_tanh's z/2 (1 - t^2) c (1 + 0.134 z^2), where 1 - t^2 is off by 2 x 2^-23
-# + 2^-24 and the factor stays below 6 where t is not 1 to the last bit (|z| <= 4.3); the others have factors below 2.
+# A binary32 slope is off by at most 2^-18: a value as above (2^-21), and z times a density or s (1 - s) times a derivative that stays
+# below 6 where the other factor is not 0 to the last bit; these are off by (2 + 1.2 x 9) 2^-24 relative, and z s (1 - s) u' <= 1.2.
 SLOPE_ERR = 2.0 ** -18
 
 
