@@ -263,8 +263,8 @@ def _shaped(t, shape, name):
 
 
 def _same_device(first, *others):
-    if any(t is not None and t.device != first.device for t in others):
-        raise ValueError("all tensors of a call must be on one device")
+    if any(t is not None and t.device != first.device for t in others) or (first.is_cuda and first.device.index != torch.cuda.current_device()):
+        raise ValueError("all tensors of a call must be on the current CUDA device")
 
 
 def _scale(t, name):
@@ -316,6 +316,10 @@ def lba_linear(A, B, scale_a, scale_b, bias, prod_fmt, acc_fmt, order=ORDER_CHUN
     dropping an element, with ``rng`` an int64 CUDA tensor (seed, offset).  ``preact``: a float dtype, or a tensor to write: the
     pre-activations that ``lba_linear_backward`` takes; the call then returns (out, preact)."""
     lib = load_library()
+    done = _native and _native.linear(A, B, scale_a, scale_b, bias, prod_fmt, acc_fmt, order, chunk, activation, residual, dropout, rng, out_dtype,
+                                      out_scale, preact, out, stream)
+    if done is not None:
+        return _done(done)
     M, K = A.shape
     N, K2 = B.shape
     if K != K2:
@@ -338,6 +342,10 @@ def lba_gated(A, B_gate, B_up, scale_a, scale_gate, scale_up, bias_gate, bias_up
     ``preact``: a float dtype, or a tensor to write, [2][M][N]: both projections, as ``lba_gated_backward`` takes them; the call
     then returns (out, preact).  The other arguments are those of ``lba_linear``."""
     lib = load_library()
+    done = _native and _native.gated(A, B_gate, B_up, scale_a, scale_gate, scale_up, bias_gate, bias_up, prod_fmt, acc_fmt, order, chunk, activation,
+                                     out_dtype, out_scale, preact, out, stream)
+    if done is not None:
+        return _done(done)
     M, K = A.shape
     N, K2 = B_gate.shape
     if K != K2 or tuple(B_up.shape) != (N, K):
@@ -386,6 +394,11 @@ def lba_linear_backward(grad_out, A, B, scale_a, scale_b, prod_fmt, preact=None,
     ``preact`` is what the forward call kept; ``activation``, ``dropout`` and ``rng`` are the forward call's (``rng`` holding the
     same two values), and so is ``prod_fmt``, which says what the operands' bytes are.  ``grad_dtype``: of grad_a and grad_b,
     grad_out's if None; grad_bias is float32.  ``workspace``: a CUDA uint8 tensor of ``backward_workspace_bytes``, or None."""
+    lib = load_library()
+    done = _native and _native.linear_backward(grad_out, A, B, scale_a, scale_b, prod_fmt, preact, activation, dropout, rng, grad_dtype, needs,
+                                               workspace, stream)
+    if done is not None:
+        return _done(done)
     M, K = A.shape
     N, K2 = B.shape
     if K != K2:
@@ -398,7 +411,7 @@ def lba_linear_backward(grad_out, A, B, scale_a, scale_b, prod_fmt, preact=None,
     ga = torch.empty((M, K), dtype=dtype, device=A.device) if needs[0] else None
     gb = torch.empty((N, K), dtype=dtype, device=A.device) if needs[1] else None
     gc = torch.empty((N,), dtype=torch.float32, device=A.device) if needs[2] else None
-    _check(load_library().lba_linear_backward(g, _dev(A, torch.uint8, "A"), _dev(B, torch.uint8, "B"), sa, sa_len, sb, sb_len, M, N, K,
+    _check(lib.lba_linear_backward(g, _dev(A, torch.uint8, "A"), _dev(B, torch.uint8, "B"), sa, sa_len, sb, sb_len, M, N, K,
                                               C.byref(how), _typed(ga, "grad_a")[0], _typed(gb, "grad_b")[0],
                                               _dev(gc, torch.float32, "grad_bias"), _dev(ws, torch.uint8, "workspace"), ws.numel(),
                                               _stream(stream)))
@@ -409,6 +422,11 @@ def lba_gated_backward(grad_out, A, B_gate, B_up, scale_a, scale_gate, scale_up,
                        needs=(True, True, True), workspace=None, stream=None):
     """(grad_a, grad_gate, grad_up, grad_bias_gate, grad_bias_up) of ``lba_gated``; ``preact`` is the [2][M][N] that the forward call
     kept, the other arguments are those of ``lba_linear_backward``.  See ``lba_gated_backward`` in lba.h."""
+    lib = load_library()
+    done = _native and _native.gated_backward(grad_out, A, B_gate, B_up, scale_a, scale_gate, scale_up, prod_fmt, preact, activation, grad_dtype,
+                                              needs, workspace, stream)
+    if done is not None:
+        return _done(done)
     M, K = A.shape
     N, K2 = B_gate.shape
     if K != K2 or tuple(B_up.shape) != (N, K):
@@ -424,7 +442,7 @@ def lba_gated_backward(grad_out, A, B_gate, B_up, scale_a, scale_gate, scale_up,
     ga = torch.empty((M, K), dtype=dtype, device=A.device) if needs[0] else None
     gg, gu = (torch.empty((N, K), dtype=dtype, device=A.device) if needs[1] else None for _ in range(2))
     cg, cu = (torch.empty((N,), dtype=torch.float32, device=A.device) if needs[2] else None for _ in range(2))
-    _check(load_library().lba_gated_backward(g, _dev(A, torch.uint8, "A"), _dev(B_gate, torch.uint8, "B_gate"), _dev(B_up, torch.uint8, "B_up"),
+    _check(lib.lba_gated_backward(g, _dev(A, torch.uint8, "A"), _dev(B_gate, torch.uint8, "B_gate"), _dev(B_up, torch.uint8, "B_up"),
                                              sa, sa_len, sg, su, sg_len, M, N, K, C.byref(how), _typed(ga, "grad_a")[0],
                                              _typed(gg, "grad_gate")[0], _typed(gu, "grad_up")[0], _dev(cg, torch.float32, "grad_bias_gate"),
                                              _dev(cu, torch.float32, "grad_bias_up"), _dev(ws, torch.uint8, "workspace"), ws.numel(),

@@ -254,3 +254,59 @@ def test_two_layers_in_a_row_as_a_network_uses_them():
     assert torch.equal(synth.e4m3_encode(f / scale) & 0x7F, h & 0x7F)
     want = lba.lba_gemm(h, D, scale, sd, bias, prod, acc) + res.float()
     assert torch.equal(out, want.to(torch.bfloat16))
+
+
+def test_native_calls_are_those_of_the_ctypes_path(monkeypatch):
+    prod, acc = FORMATS["m7e4"]
+    A, sa, B, sb, bias, B2, sb2, bias2 = inputs(20, 40, 64, 12, prod, 2)
+    g, rng, scale = synth.gaussian((20, 40), 1).to(DEV), torch.tensor([3, 4], device=DEV), torch.tensor([0.1], device=DEV)
+    pre, buf = torch.empty(2, 20, 40, device=DEV), torch.empty(20, 40, dtype=torch.bfloat16, device=DEV)
+
+    def calls():
+        yield lba.lba_linear(A, B, sa, sb, bias, prod, acc)
+        yield from lba.lba_linear(A, B, sa, sb, bias, prod, acc, SEQ, 16, "gelu", g, 0.5, rng, torch.uint8, scale, torch.float16)
+        yield lba.lba_linear(A, B, sa, sb, torch.nn.Parameter(bias), prod.as_tuple(), acc.as_tuple(), out=buf).clone()
+        yield lba.lba_gated(A, B, B2, sa, sb, sb2, None, None, prod, acc, out_dtype=torch.bfloat16)
+        yield from (t.clone() for t in lba.lba_gated(A, B, B2, sa, sb, sb2, bias, bias2, prod, acc, activation="gelu_tanh", preact=pre, out=buf))
+        yield from lba.lba_linear_backward(g, A, B, sa, sb, prod, pre[0], "silu", 0.5, rng, torch.bfloat16)
+        yield from (t for t in lba.lba_linear_backward(g, A, B, sa, sb, prod, needs=(False, True, False)) if t is not None)
+        yield from lba.lba_gated_backward(g, A, B, B2, sa, sb, sb2, prod, pre)
+
+    assert lba._native
+    count = [0]
+    native = lba._native
+
+    class Counting:
+        def __getattr__(self, name):
+            def call(*args):
+                r = getattr(native, name)(*args)
+                count[0] += r is not None
+                return r
+            return call
+    monkeypatch.setattr(lba, "_native", Counting())
+    first = list(calls())
+    assert count[0] == 8                      # every one of them is regular
+    monkeypatch.setattr(lba, "_native", None)
+    assert all(torch.equal(x, y) for x, y in zip(first, list(calls()), strict=True))
+
+
+def test_what_is_refused_with_tensors_on_the_gpu():
+    prod, acc = FORMATS["m7e4"]
+    A, sa, B, sb, bias = inputs(4, 8, 16, 13, prod)
+    for kw in [dict(out=torch.empty(4, 9, device=DEV)), dict(residual=torch.empty(8, 4, device=DEV)), dict(preact=torch.empty(4, 9, device=DEV)),
+               dict(activation="swish"), dict(out=torch.empty(4, 8))]:
+        with pytest.raises((ValueError, TypeError)):
+            lba.lba_linear(A, B, sa, sb, bias, prod, acc, **kw)
+    for kw in [dict(out=torch.empty(8, 4, device=DEV).t()), dict(residual=torch.empty(8, 4, device=DEV).t()), dict(dropout=0.5),
+               dict(dropout=0.5, rng=torch.zeros(3, dtype=torch.int64, device=DEV)), dict(out_dtype=torch.uint8), dict(out_dtype=torch.float64)]:
+        with pytest.raises(TypeError):
+            lba.lba_linear(A, B, sa, sb, bias, prod, acc, **kw)
+    for p in (1.0, -0.5):
+        with pytest.raises(lba.LbaError):
+            lba.lba_linear(A, B, sa, sb, bias, prod, acc, dropout=p, rng=torch.zeros(2, dtype=torch.int64, device=DEV))
+    with pytest.raises(ValueError):
+        lba.lba_linear(A, B, sa, sb, bias[:7], prod, acc)
+    with pytest.raises(lba.LbaError):
+        lba.lba_linear(A, B, sa, sb[:7], bias, prod, acc)
+    with pytest.raises(lba.LbaError):
+        lba.lba_gated(A, B, B, sa, sb, sb, bias, None, prod, acc)
