@@ -25,6 +25,13 @@ inline EncodeTiled tensor_map_encoder() {
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ void mbar_init(uint32_t bar, int count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count)); }
 __device__ __forceinline__ void mbar_init_fence() { asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory"); }
+// true in one lane of a converged warp; the compiler then knows that operands of what follows are the same for all active lanes, where
+// a lane chosen by its number had each copy cost some hundred clocks of issue
+__device__ __forceinline__ bool elected() {
+  uint32_t d;
+  asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(d));
+  return d;
+}
 // announces bytes; the first form also arrives
 __device__ __forceinline__ void mbar_arrive_expect(uint32_t bar, int bytes) {
   asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
@@ -34,31 +41,31 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, int bytes) {
 }
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
 // Waits for the phase of the given parity, at most some seconds; then `dead` is set, no wait of the CTA takes long any more, and
-// its outputs become NaN.
-__device__ __forceinline__ void mbar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
+// its outputs become NaN.  Returns whether the phase ended.
+__device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
   for (uint32_t i = 0;; ++i) {
     uint32_t done;
     asm volatile(
         "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
         : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    if (done) return;
+    if (done) return true;
     if (i > (1u << 22) || (i > 1024 && *dead)) {
       *dead = 1;
-      return;
+      return false;
     }
   }
 }
 // the same for a barrier that the other CTA of a cluster arrives at too
-__device__ __forceinline__ void mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* dead) {
+__device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* dead) {
   for (uint32_t i = 0;; ++i) {
     uint32_t done;
     asm volatile(
         "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
         : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    if (done) return;
+    if (done) return true;
     if (i > (1u << 22) || (i > 1024 && *dead)) {
       *dead = 1;
-      return;
+      return false;
     }
   }
 }

@@ -19,13 +19,16 @@
 //                         and the bias sums' last step.
 #include "lba_grad.cuh"
 
+#include <cstring>
+
 #include "lba_async.cuh"
 #include "lba_layer.cuh"
 
 namespace lba {
 namespace {
 
-constexpr int PREP_ROWS = 32, PREP_COLS = 256, PREP_THREADS = 256, PREP_EACH = PREP_ROWS * PREP_COLS / (8 * PREP_THREADS);
+constexpr int PREP_COLS = 256, PREP_THREADS = 256, PREP_SIDE = 8 * PREP_THREADS / PREP_COLS;  // PREP_SIDE: rows beside each other in a block
+constexpr int PREP_EACH = 4;                  // rows of a thread where there are enough of them
 typedef __nv_bfloat16 bf16;
 
 struct PrepParams {
@@ -38,7 +41,7 @@ struct PrepParams {
   uint32_t* flags;           // words that the second kernel wants at zero
   int64_t M, N, K, np, nz, kp, plane;
   int pieces;                // 0: no product is wanted
-  int act, in_m4e3, sb_per_col, flag_words;
+  int act, in_m4e3, sb_per_col, flag_words, each;
   uint32_t drop_below;
   int64_t z_blocks, col_blocks, a_blocks;  // blocks of dz, then of A's codes, then of B's
 };
@@ -67,41 +70,56 @@ __device__ __forceinline__ Raw8<T> load8(const void* base, int64_t i, int valid)
   return r;
 }
 template <typename T>
-__device__ __forceinline__ void widen8(const Raw8<T>& r, float (&v)[8]) {
-  const T* const e = reinterpret_cast<const T*>(&r);
+__device__ __forceinline__ void widen8(const Raw8<T>& r, u64 (&v)[4]) {
+  if constexpr (std::is_same<T, bf16>::value) {
+    const uint32_t* const w = reinterpret_cast<const uint32_t*>(&r);
 #pragma unroll
-  for (int j = 0; j < 8; ++j) v[j] = to_f32(e[j]);
+    for (int j = 0; j < 4; ++j) v[j] = pack2u(w[j] << 16, w[j] & 0xFFFF0000u);
+  } else {
+    const T* const e = reinterpret_cast<const T*>(&r);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = pack2(to_f32(e[2 * j]), to_f32(e[2 * j + 1]));
+  }
 }
 
 // v as the sum of bfloat16 pieces, all but the last cut toward zero (which cannot overflow and leaves an exact remainder)
-__device__ __forceinline__ void store_pieces(bf16* dst, int64_t plane, int pieces, const float (&v)[8]) {
-  float rest[8];
+__device__ __forceinline__ void store_pieces(bf16* dst, int64_t plane, int pieces, const u64 (&v)[4]) {
+  uint4 out;
+  uint32_t* const w = &out.x;
+  if (pieces > 1) {
+    float rest[8];
 #pragma unroll
-  for (int j = 0; j < 8; ++j) rest[j] = v[j];
+    for (int j = 0; j < 4; ++j) unpack2(v[j], rest[2 * j], rest[2 * j + 1]);
 #pragma unroll 1
-  for (int q = 0; q < pieces; ++q) {
-    uint4 out;
-    uint32_t* const w = &out.x;
-    const bool last = q + 1 == pieces;
+    for (int q = 0; q + 1 < pieces; ++q) {
 #pragma unroll
-    for (int j = 0; j < 8; j += 2) {
-      uint32_t h[2];
+      for (int j = 0; j < 8; j += 2) {
+        uint32_t h[2];
 #pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        const float r = rest[j + e];
-        if (last) {
-          h[e] = (uint32_t)__bfloat16_as_ushort(__float2bfloat16_rn(r));
-        } else {
-          const float head = __uint_as_float(__float_as_uint(r) & 0xFFFF0000u);
-          h[e] = __float_as_uint(r) >> 16;
-          rest[j + e] = isfinite(r) ? r - head : 0.0f;
-          if (r != r) h[e] = 0x7FC0u;  // a NaN whose payload the cut would lose
+        for (int e = 0; e < 2; ++e) {
+          const float r = rest[j + e];
+          h[e] = r != r ? 0x7FC00000u : __float_as_uint(r) & 0xFFFF0000u;  // (a NaN's payload may lie in what is cut)
+          rest[j + e] = isfinite(r) ? r - __uint_as_float(h[e]) : 0.0f;
         }
+        w[j / 2] = __byte_perm(h[0], h[1], 0x7632);
       }
-      w[j / 2] = h[0] | (h[1] << 16);
+      *reinterpret_cast<uint4*>(dst + q * plane) = out;
     }
-    *reinterpret_cast<uint4*>(dst + q * plane) = out;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(rest[2 * j], rest[2 * j + 1]);
+      w[j] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      float lo, hi;
+      unpack2(v[j], lo, hi);
+      const __nv_bfloat162 b = __floats2bfloat162_rn(lo, hi);
+      w[j] = *reinterpret_cast<const uint32_t*>(&b);
+    }
   }
+  *reinterpret_cast<uint4*>(dst + (pieces - 1) * plane) = out;
 }
 
 __device__ __forceinline__ void expand_codes(const PrepParams& p, const uint8_t* row, bf16* dst, int64_t k) {
@@ -135,7 +153,7 @@ __device__ __forceinline__ void expand_codes(const PrepParams& p, const uint8_t*
 }
 
 template <typename G, typename Z, bool GATED>
-__global__ void __launch_bounds__(PREP_THREADS) grad_prepare_kernel(const PrepParams p) {
+__global__ void __launch_bounds__(PREP_THREADS, GATED ? 2 : 3) grad_prepare_kernel(const PrepParams p) {
   constexpr int HALVES = GATED ? 2 : 1;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   after_previous();
@@ -162,77 +180,94 @@ __global__ void __launch_bounds__(PREP_THREADS) grad_prepare_kernel(const PrepPa
     return;
   }
 
-  __shared__ float sums[HALVES][PREP_THREADS / 32][PREP_COLS];
-  const int64_t n = (b % p.col_blocks) * PREP_COLS + lane * 8, m0 = (b / p.col_blocks) * PREP_ROWS + warp;
+  __shared__ __align__(8) float sums[HALVES][PREP_THREADS / 32][PREP_COLS];
+  const int64_t n = (b % p.col_blocks) * PREP_COLS + lane * 8, m0 = (b / p.col_blocks) * (PREP_SIDE * p.each) + warp;
   const int valid = n >= p.N ? 0 : p.N - n < 8 ? (int)(p.N - n) : 8;
-  float total[HALVES][8];
+  u64 total[HALVES][4];
 #pragma unroll
   for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) total[h][j] = 0.0f;
-  if (n < p.np) {
-    // all of a thread's loads before its first store: four rows of sixteen bytes and more are on their way at a time
-    Raw8<G> g[PREP_EACH];
-    Raw8<Z> z[PREP_EACH][HALVES];
-    const bool reads_z = GATED || p.act != ACT_NONE;
+    for (int j = 0; j < 4; ++j) total[h][j] = 0ull;
+  if (n < p.np && m0 < p.M) {
+    u64 scale[HALVES][4];
 #pragma unroll
-    for (int i = 0; i < PREP_EACH; ++i) {
-      const int64_t m = m0 + i * (PREP_THREADS / 32);
-      if (m >= p.M) break;
-      g[i] = load8<G>(p.grad, m * p.N + n, valid);
-      if (reads_z) {
+    for (int h = 0; h < HALVES; ++h) {
+      const float* const sb = h ? p.sb2 : p.sb;
 #pragma unroll
-        for (int h = 0; h < HALVES; ++h) z[i][h] = load8<Z>(p.pre, (h * p.M + m) * p.N + n, valid);
-      }
-    }
-    float scale[HALVES][8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      scale[0][j] = !p.sb ? 1.0f : p.sb_per_col ? (j < valid ? p.sb[n + j] : 0.0f) : p.sb[0];
-      if (GATED) scale[HALVES - 1][j] = p.sb_per_col ? (j < valid ? p.sb2[n + j] : 0.0f) : p.sb2[0];
+      for (int j = 0; j < 4; ++j)
+        scale[h][j] = !sb ? both(1.0f) : !p.sb_per_col ? both(sb[0]) : pack2(2 * j < valid ? sb[n + 2 * j] : 0.0f, 2 * j + 1 < valid ? sb[n + 2 * j + 1] : 0.0f);
     }
     with_act(p.act, [&](auto act_tag) {
       constexpr int ACT = decltype(act_tag)::value;
+      constexpr bool READS_Z = GATED || ACT != ACT_NONE;
+      // the next row is on its way while one is computed; a rolled loop, because a straight run of four rows is 3000 instructions that
+      // each warp fetches once (32 x 512 took 18 us)
+      Raw8<G> g, g_next = load8<G>(p.grad, m0 * p.N + n, valid);
+      Raw8<Z> z[HALVES], z_next[HALVES];
+      if (READS_Z) {
 #pragma unroll
-      for (int i = 0; i < PREP_EACH; ++i) {
-        const int64_t m = m0 + i * (PREP_THREADS / 32);
+        for (int h = 0; h < HALVES; ++h) z_next[h] = load8<Z>(p.pre, (h * p.M + m0) * p.N + n, valid);
+      }
+#pragma unroll 1
+      for (int i = 0; i < p.each; ++i) {
+        const int64_t m = m0 + i * PREP_SIDE, after = m + PREP_SIDE;
         if (m >= p.M) break;
-        float gv[8], zv[8], d[HALVES][8];
-        widen8(g[i], gv);
-        if (GATED || ACT != ACT_NONE) widen8(z[i][0], zv);
+        g = g_next;
+#pragma unroll
+        for (int h = 0; h < HALVES; ++h) z[h] = z_next[h];
+        if (i + 1 < p.each && after < p.M) {
+          g_next = load8<G>(p.grad, after * p.N + n, valid);
+          if (READS_Z) {
+#pragma unroll
+            for (int h = 0; h < HALVES; ++h) z_next[h] = load8<Z>(p.pre, (h * p.M + after) * p.N + n, valid);
+          }
+        }
+        u64 gv[4], zv[4], d[HALVES][4];
+        widen8(g, gv);
+        if (READS_Z) widen8(z[0], zv);
         if (!GATED && p.drop_below) {
           const uint64_t seed = p.rng[0], offset = p.rng[1];
 #pragma unroll
           for (int h = 0; h < 2; ++h) {
             const uint4 r = philox((uint32_t)(n >> 2) + h, (uint32_t)m, offset, seed);
-            const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              if (w[j] < p.drop_below) gv[4 * h + j] = 0.0f;
+            float lo, hi;
+            unpack2(gv[2 * h], lo, hi);
+            gv[2 * h] = pack2(r.x < p.drop_below ? 0.0f : lo, r.y < p.drop_below ? 0.0f : hi);
+            unpack2(gv[2 * h + 1], lo, hi);
+            gv[2 * h + 1] = pack2(r.z < p.drop_below ? 0.0f : lo, r.w < p.drop_below ? 0.0f : hi);
           }
         }
-        if constexpr (GATED) {
-          float v[8];
-          widen8(z[i][1], v);
+        [[maybe_unused]] u64 other[4];
+        if constexpr (GATED) widen8(z[HALVES - 1], other);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            d[0][j] = gv[j] * v[j] * act_slope_of<ACT>(zv[j]);
-            d[1][j] = gv[j] * act_value_of<ACT>(zv[j]);
+        for (int j = 0; j < 4; ++j) {
+          u64 value, slope;
+          if (READS_Z) act_pair<ACT>(zv[j], value, slope);
+          if constexpr (GATED) {
+            d[0][j] = mul2_rn(mul2_rn(gv[j], other[j]), slope);
+            d[HALVES - 1][j] = mul2_rn(gv[j], value);
+          } else if (ACT == ACT_RELU) {  // (an infinite gradient stays out where the slope is 0)
+            float glo, ghi, slo, shi;
+            unpack2(gv[j], glo, ghi);
+            unpack2(slope, slo, shi);
+            d[0][j] = pack2(slo != 0.0f ? glo : 0.0f, shi != 0.0f ? ghi : 0.0f);
+          } else {
+            d[0][j] = ACT == ACT_NONE ? gv[j] : mul2_rn(gv[j], slope);
           }
-        } else {
-#pragma unroll
-          for (int j = 0; j < 8; ++j)
-            d[0][j] = ACT == ACT_NONE ? gv[j] : ACT == ACT_RELU ? (zv[j] > 0.0f ? gv[j] : 0.0f) : gv[j] * act_slope_of<ACT>(zv[j]);
         }
-        const float by = p.sa ? p.sa[m] : 1.0f;
+        // (the padding of a row: g is 0 there, z too, and every slope finite)
+        const u64 by = both(p.sa ? p.sa[m] : 1.0f);
 #pragma unroll
         for (int h = 0; h < HALVES; ++h) {
-          float s[8];
+          u64 s[4];
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            d[h][j] = j < valid ? d[h][j] : 0.0f;  // the padding of a row
-            total[h][j] += d[h][j];
-            s[j] = d[h][j] * (scale[h][j] * by);
+          for (int j = 0; j < 4; ++j) {
+            total[h][j] = add2_rn(total[h][j], d[h][j]);
+            s[j] = mul2_rn(d[h][j], scale[h][j]);
+          }
+          if (p.sa) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) s[j] = mul2_rn(s[j], by);
           }
           if (p.pieces) store_pieces(p.z + m * p.nz + h * p.np + n, p.plane, p.pieces, s);
         }
@@ -243,7 +278,7 @@ __global__ void __launch_bounds__(PREP_THREADS) grad_prepare_kernel(const PrepPa
 #pragma unroll
   for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sums[h][warp][lane * 8 + j] = total[h][j];
+    for (int j = 0; j < 4; ++j) *reinterpret_cast<u64*>(&sums[h][warp][lane * 8 + 2 * j]) = total[h][j];
   __syncthreads();
   const int64_t col = (b % p.col_blocks) * PREP_COLS + threadIdx.x;
   if (col >= p.np) return;
@@ -263,22 +298,26 @@ __global__ void __launch_bounds__(PREP_THREADS) grad_prepare_kernel(const PrepPa
 // A cluster of two CTAs forms a 256 x 256 tile: each CTA holds 128 rows of X, half of Y's columns and the accumulators of its rows, and
 // one thread of the first issues the matrix instructions of both (cta_group::2).  What bounds such a product is what the L2 can
 // deliver: a CTA alone with 128 x 256 outputs fetched 48 KB per 64 l where this takes 32 (4096 x 4096 x 1024: 82 us alone).
-// Six warps a CTA: one thread loads, one multiplies into one of two accumulators of 256 columns of tensor memory, four bring the
-// other one out.
+// Ten warps a CTA: one thread loads, one multiplies into one of two accumulators of 256 columns of tensor memory, eight warps bring the
+// other one out.  A step is 512 clocks of the tensor cores, so its loads must take the one thread less: two copies with three- and
+// four-dimensional boxes and no arithmetic but the coordinates' (three copies and 64-bit divisions in a lane chosen by its number had
+// taken 725).
 //
-// Equal shares.  The tiles' steps of 64 l stand in one row, cut into shares of equal length; a cluster walks its own from the end.  A
-// tile that a border cuts is begun by lower shares, which leave binary32 sums in the workspace, and finished by the share with its last
-// step, which adds them in order.  A cluster takes the number of its share when it starts, from a counter, so it only ever waits for
-// clusters that run already or have ended, and what it waits for is the first thing that those do.  Where whole tiles divide as well, they stay whole.
-constexpr int BM = 128, BN = 256, BL = 64, GRAD_THREADS = 192;  // of a CTA: rows, columns, step
-constexpr int X_BYTES = BM * BL * 2, STAGE = 2 * X_BYTES, STAGES = 6;
-constexpr size_t PRODUCT_SMEM = 1024 + (size_t)STAGE * STAGES + 256;
+// Clusters take whole tiles in turn, side by side in l, so that what one fetches its neighbours find in L2.  The tiles of a last, broken
+// round are divided instead: their steps of 64 l stand in one row, cut into equal shares, one per cluster.  A tile that a border
+// cuts is begun by lower shares, which leave binary32 sums in the workspace, and finished by the share with its last step, which
+// adds them in order.  A cluster walks its share from the end and before its whole tiles, and takes the share's number from a counter when it
+// starts: it only ever waits for clusters that run already or have ended, for the first thing that those do.
+constexpr int BM = 128, BN = 256, BL = 64, GRAD_THREADS = 320, OUT_THREADS = 256;  // of a CTA: rows, columns, step
+constexpr int X_BYTES = BM * BL * 2, STAGE = 2 * X_BYTES, STAGES = 5;
+constexpr int OUT_PITCH = 33;         // floats from row to row of a warp's 32 x 32 outputs in shared memory
+constexpr size_t PRODUCT_SMEM = 1024 + (size_t)STAGE * STAGES + 256 + OUT_THREADS * OUT_PITCH * 4;
 constexpr int PART_FLOATS = BM * BN;  // a CTA's part of a begun tile
 
 struct Job {
   int64_t rows, cols;       // of one half's output
-  int64_t r_tiles, s_tiles; // r_tiles: of one half
-  int64_t half;             // X's coordinate r of the second half
+  int r_tiles, s_tiles;     // r_tiles: of one half
+  int half;                 // blocks of 64 before the second half's first in X
   int x_mn, pieces, steps;  // steps: blocks of l times pieces
   int div_stride;
   void* out[2];
@@ -287,9 +326,10 @@ struct Job {
 struct ProductParams {
   CUtensorMap x[2], y[2];
   Job job[2];
-  int64_t tiles0, tiles;    // of the first job, of both
-  int64_t units0, units;    // their steps
-  int64_t share;            // steps of a cluster; 0: whole tiles
+  int tiles0, tiles;        // of the first job, of both
+  int whole;                // tiles that stay whole, the first ones
+  int units0, units, first; // with shares: steps of the first job, of both, those before the divided ones
+  int share;                // steps of a cluster's share; 0: there are none
   int out_type;
   float factor;
   uint32_t* flags;          // shares: the counter, then a word per CTA's part
@@ -304,10 +344,10 @@ __device__ __forceinline__ uint32_t mapa(uint32_t addr, int rank) {
   asm("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(d) : "r"(addr), "r"(rank));
   return d;
 }
-// a box of a three-dimensional map into this CTA's memory, counted by a barrier of either CTA of the pair
-__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar) {
-  asm volatile("cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst),
-               "l"(map), "r"(x), "r"(y), "r"(z), "r"(bar) : "memory");
+// a box of blocks of 64 columns: columns of block b, rows from y on, plane z; counted by a barrier of either CTA of the pair
+__device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, int y, int b, int z, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+               ::"r"(dst), "l"(map), "r"(0), "r"(y), "r"(b), "r"(z), "r"(bar) : "memory");
 }
 // Shared-memory operand of a matrix instruction, 128-byte swizzle: 1024-byte groups of eight 128-byte lines.  K-major: a line is
 // a row's 64 values of l, `stride` the step between groups of eight rows.  MN-major: a line is 64 rows at one l, `stride` the
@@ -347,46 +387,43 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t (&r)[32]) {
 // a cluster's work, piece by piece: a tile and some of its steps
 struct Work {
   int job, half, k0, k1;
-  int64_t r, s, start;  // first row (of the half) and column, the tile's first step among all
+  int r, s, start;  // first row tile (of the half) and column tile, the tile's first step among all
 };
 struct Walk {
-  int64_t at, end, by;  // shares: steps [end, at) are left; whole tiles: the next tile, their number
-  __device__ __forceinline__ Walk(const ProductParams& p, int64_t c, int64_t clusters) {
+  int at, end, tile, by;  // steps [end, at) of the share are left; the next whole tile, the number of clusters
+  __device__ __forceinline__ Walk(const ProductParams& p, int c, int clusters) {
+    tile = c;
     by = clusters;
+    end = at = 0;
     if (p.share) {
-      end = c * p.share;
+      end = p.first + c * p.share;
       at = end + p.share < p.units ? end + p.share : p.units;
-    } else {
-      at = c;
-      end = p.tiles;
     }
   }
   __device__ __forceinline__ bool next(const ProductParams& p, Work& w) {
-    int64_t t;
-    if (p.share) {
-      if (at <= end) return false;
+    int t;
+    if (at > end) {
       w.job = at - 1 >= p.units0;
-      const int steps = p.job[w.job].steps;
-      const int64_t base = w.job ? p.units0 : 0;
+      const int steps = p.job[w.job].steps, base = w.job ? p.units0 : 0;
       t = (at - 1 - base) / steps;
       w.start = base + t * steps;
-      w.k1 = (int)(at - w.start);
-      w.k0 = end > w.start ? (int)(end - w.start) : 0;
+      w.k1 = at - w.start;
+      w.k0 = end > w.start ? end - w.start : 0;
       at = w.start + w.k0;
     } else {
-      if (at >= end) return false;
-      w.job = at >= p.tiles0;
-      t = w.job ? at - p.tiles0 : at;
+      if (tile >= p.whole) return false;
+      w.job = tile >= p.tiles0;
+      t = w.job ? tile - p.tiles0 : tile;
       w.k0 = 0;
       w.k1 = p.job[w.job].steps;
       w.start = 0;
-      at += by;
+      tile += by;
     }
     const Job& j = p.job[w.job];
-    w.s = (t % j.s_tiles) * BN;
-    t /= j.s_tiles;
-    w.half = t >= j.r_tiles;
-    w.r = (w.half ? t - j.r_tiles : t) * (2 * BM);
+    const int row = t / j.s_tiles;
+    w.s = t - row * j.s_tiles;
+    w.half = row >= j.r_tiles;
+    w.r = w.half ? row - j.r_tiles : row;
     return true;
   }
 };
@@ -407,22 +444,33 @@ __device__ __forceinline__ void bias_sums(const ProductParams& p, float (*part)[
   }
 }
 
+// A warp's 32 x 32 outputs, a row per lane, to rows of `pitch` elements: through shared memory, W neighbouring columns of W rows at a
+// time.  (A row per lane straight to memory had each store touch 32 rows: with rows of 1203 floats, where nothing is aligned,
+// 1000 x 777 x 1203 took 42 us for its products.)
 template <typename T>
-__device__ __forceinline__ void store32(T* dst, int64_t valid, const float (&r)[32], float alpha) {
-  constexpr int W = 16 / (int)sizeof(T);
-  if (valid >= 32 && (reinterpret_cast<uintptr_t>(dst) & 15) == 0) {
+__device__ __forceinline__ void store_rows(void* base, int64_t at, int64_t pitch, int rows, int cols, const float* sm, int lane) {
+  T* const out = static_cast<T*>(base) + at;
+  if (pitch % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(T) - 1)) == 0 && cols == 32) {
+    const int c = lane % 8 * 4;
+    T* dst = out + (lane / 8) * pitch + c;
+    const float* src = sm + (lane / 8) * OUT_PITCH + c;
 #pragma unroll
-    for (int q = 0; q < 32 / W; ++q) {
-      uint4 raw;
-      T* const e = reinterpret_cast<T*>(&raw);
+    for (int i = 0; i < 8; ++i) {
+      T t[4];
 #pragma unroll
-      for (int j = 0; j < W; ++j) e[j] = from_f32<T>(r[q * W + j] * alpha);
-      *reinterpret_cast<uint4*>(dst + q * W) = raw;
+      for (int j = 0; j < 4; ++j) t[j] = from_f32<T>(src[i * 4 * OUT_PITCH + j]);
+      typename Bytes<4 * sizeof(T)>::type raw;
+      memcpy(&raw, t, sizeof(raw));
+      if (i * 4 + lane / 8 < rows) *reinterpret_cast<decltype(raw)*>(dst) = raw;
+      dst += 4 * pitch;
     }
-  } else {
-#pragma unroll
-    for (int j = 0; j < 32; ++j)
-      if (j < valid) dst[j] = from_f32<T>(r[j] * alpha);
+  } else if (lane < cols) {
+    T* dst = out + lane;
+#pragma unroll 8
+    for (int i = 0; i < rows; ++i) {
+      *dst = from_f32<T>(sm[i * OUT_PITCH + lane]);
+      dst += pitch;
+    }
   }
 }
 
@@ -433,6 +481,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
   uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 4);
   volatile int* const dead = reinterpret_cast<volatile int*>(tmem_slot + 1);
   uint32_t* const share_slot = tmem_slot + 2;
+  float* const outs = reinterpret_cast<float*>(base + STAGES * STAGE + 256);  // 32 x 32 of each warp that brings outputs out
   __shared__ float part[4][32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = blockIdx.x & 1;  // in the cluster
@@ -445,7 +494,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(acc_done + 8 * i, 1);
-      mbar_init(acc_free + 8 * i, 256);  // the first CTA's: both CTAs' readers
+      mbar_init(acc_free + 8 * i, 2 * OUT_THREADS);  // the first CTA's: both CTAs' readers
     }
     *dead = 0;
     mbar_init_fence();
@@ -455,7 +504,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
   }
   __syncwarp();
-  cluster_sync();  // the other CTA runs: its memory may be written
+  if (p.share) cluster_sync();  // the other CTA runs: its memory may be written
   after_previous();
   if (p.share && rank == 0 && threadIdx.x == 0) {
     const uint32_t c = atomicAdd(p.flags, 1u);
@@ -467,32 +516,34 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
   cluster_sync();
   asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
   const uint32_t tmem = *tmem_slot;
-  const int64_t share = p.share ? *share_slot : blockIdx.x >> 1;
+  const int share = p.share ? (int)*share_slot : blockIdx.x >> 1;
   Walk walk(p, share, gridDim.x >> 1);
   Work w;
 
   if (warp == 0) {
-    if (lane == 0) {
+    if (elected()) {
       int stage = 0;
-      uint32_t phase = 0;
-      while (walk.next(p, w)) {
+      uint32_t phase = 1;
+      bool alive = true;
+      const uint32_t stages = smem_u32(base), bars0 = mapa(full, 0);  // the first CTA's
+      while (alive && walk.next(p, w)) {
         const Job& j = p.job[w.job];
-        const int r = (int)(w.r + (w.half ? j.half : 0)) + rank * BM, s = (int)w.s + rank * (BN / 2);
-        int l = w.k0 / j.pieces, q = w.k0 % j.pieces;
+        const CUtensorMap *const xm = &p.x[w.job], *const ym = &p.y[w.job];
+        const int x_mn = j.x_mn, pieces = j.pieces;
+        const int r = w.r * (2 * BM) + rank * BM, rb = r / 64 + (w.half ? j.half : 0), sb = w.s * (BN / 64) + rank * (BN / 128);
+        int l = w.k0 / pieces, q = w.k0 - l * pieces;
+#pragma unroll 1
         for (int k = w.k0; k < w.k1; ++k) {
-          mbar_wait(empty + 8 * stage, phase ^ 1, dead);
-          if (*dead) goto loaded;
-          const uint32_t x = smem_u32(base + stage * STAGE), y = x + X_BYTES, bar = mapa(full + 8 * stage, 0);
-          if (rank == 0) mbar_arrive_expect(full + 8 * stage, 2 * STAGE);
-          if (j.x_mn) {
-            tma_load(x, &p.x[w.job], r, l * BL, q, bar);
-            tma_load(x + X_BYTES / 2, &p.x[w.job], r + 64, l * BL, q, bar);
-          } else {
-            tma_load(x, &p.x[w.job], l * BL, r, q, bar);
+          if (!mbar_wait(empty + 8 * stage, phase, dead)) {
+            alive = false;
+            break;
           }
-          tma_load(y, &p.y[w.job], s, l * BL, 0, bar);
-          tma_load(y + X_BYTES / 2, &p.y[w.job], s + 64, l * BL, 0, bar);
-          if (++q == j.pieces) {
+          const uint32_t x = stages + stage * STAGE, bar = bars0 + 8 * stage;
+          if (rank == 0) mbar_arrive_expect(full + 8 * stage, 2 * STAGE);
+          if (x_mn) tma_load(x, xm, l * BL, rb, q, bar);
+          else tma_load(x, xm, r, l, q, bar);
+          tma_load(x + X_BYTES, ym, l * BL, sb, 0, bar);
+          if (++q == pieces) {
             q = 0;
             ++l;
           }
@@ -502,27 +553,33 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
           }
         }
       }
-    loaded:;
     }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
+    if (rank == 0 && elected()) {
       int stage = 0, acc = 0;
-      uint32_t phase = 0, acc_phase = 0;
+      uint32_t phase = 0, acc_phase = 1;
+      const uint32_t stages = smem_u32(base);
       while (walk.next(p, w)) {
         const int x_mn = p.job[w.job].x_mn;
         // binary32 sums of bfloat16 products; which operand is MN-major; sizes
         const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)x_mn << 15) | (1u << 16) | ((BN / 8) << 17) | ((2 * BM / 16) << 24);
-        mbar_wait_cluster(acc_free + 8 * acc, acc_phase ^ 1, dead);
+        // operands of a stage at address 0; a step of 16 l is 2048 bytes on where l counts lines, 32 where it counts within one
+        const uint64_t x0 = x_mn ? operand(0, X_BYTES / 2, 1024) : operand(0, 16, 1024), y0 = operand(0, X_BYTES / 2, 1024);
+        const uint32_t xk = x_mn ? 2048 >> 4 : 32 >> 4;
+        mbar_wait_cluster(acc_free + 8 * acc, acc_phase, dead);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
+        bool add = false;
+#pragma unroll 1
         for (int b = w.k0; b < w.k1; ++b) {
-          mbar_wait_cluster(full + 8 * stage, phase, dead);
+          const bool there = mbar_wait_cluster(full + 8 * stage, phase, dead);
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-          const uint32_t x = smem_u32(base + stage * STAGE), y = x + X_BYTES;
-          if (!*dead) {
+          const uint32_t x = (stages + stage * STAGE) >> 4, y = x + (X_BYTES >> 4);
+          if (there) {
 #pragma unroll
-            for (int k = 0; k < BL / 16; ++k)
-              mma(tmem + acc * BN, x_mn ? operand(x + k * 2048, X_BYTES / 2, 1024) : operand(x + k * 32, 16, 1024),
-                  operand(y + k * 2048, X_BYTES / 2, 1024), idesc, b > w.k0 || k > 0);
+            for (int k = 0; k < BL / 16; ++k) {
+              mma(tmem + acc * BN, x0 + x + k * xk, y0 + y + k * (2048 >> 4), idesc, add);
+              add = true;
+            }
           }
           mma_commit(empty + 8 * stage);
           if (++stage == STAGES) {
@@ -539,28 +596,33 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
     }
   } else {
     const int quarter = warp & 3;  // the lanes of tensor memory that this warp may read
-    const int row = quarter * 32 + lane;
-    if (p.partial) bias_sums(p, part, quarter, lane);
+    const int row = quarter * 32 + lane, c_first = warp < 6 ? 0 : BN / 2;
+    const bool leader = threadIdx.x == 64;
+    float* const sm = outs + (warp - 2) * (32 * OUT_PITCH);
+    if (p.partial && warp < 6) bias_sums(p, part, quarter, lane);
     int acc = 0;
     uint32_t phase = 0;
     while (walk.next(p, w)) {
       const Job& j = p.job[w.job];
       const bool begins = w.k1 < j.steps, ends = w.k0 > 0 && !begins;
-      const int64_t first = ends ? w.start / p.share : share;  // the shares that began this tile: first to share - 1
+      const int first = ends ? (w.start - p.first) / p.share : share;  // the shares that began this tile: first to share - 1
       if (ends) {
-        if (row == 0)
-          for (int64_t c = first; c < share; ++c) wait_flag(p.flags + 1 + 2 * c + rank, dead);
-        asm volatile("bar.sync 1, 128;" ::: "memory");
+        if (leader)
+          for (int c = first; c < share; ++c) wait_flag(p.flags + 1 + 2 * c + rank, dead);
+        asm volatile("bar.sync 2, 256;" ::: "memory");
       }
-      mbar_wait(acc_done + 8 * acc, phase, dead);
-      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      const int64_t r = w.r + rank * BM + row;
+      const int64_t r0 = (int64_t)w.r * (2 * BM) + rank * BM + quarter * 32, r = r0 + lane;
       float alpha = p.factor * (j.alpha[w.half] ? *j.alpha[w.half] : 1.0f);
       if (j.div[w.half] && r < j.rows) alpha = __fdiv_rn(alpha, j.div[w.half][r * j.div_stride]);
+      mbar_wait(acc_done + 8 * acc, phase, dead);
+      asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       if (*dead) alpha = __uint_as_float(0x7FC00000u);
-      float4* const mine = reinterpret_cast<float4*>(p.parts + (2 * share + rank) * PART_FLOATS) + row;  // [four columns][row]
+      float4* const mine = reinterpret_cast<float4*>(p.parts + (2 * (int64_t)share + rank) * PART_FLOATS) + row;  // [four columns][row]
+      const int rows = j.rows - r0 < 32 ? (int)(j.rows - r0 > 0 ? j.rows - r0 : 0) : 32;
+      const int64_t s0 = (int64_t)w.s * BN;
 #pragma unroll 1
-      for (int c = 0; c < BN; c += 32) {
+      for (int c = c_first; c < c_first + BN / 2; c += 32) {
+        if (!begins && s0 + c >= j.cols) break;
         uint32_t t[32];
         float v[32];
         tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + acc * BN + c, t);
@@ -571,8 +633,9 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
           for (int i = 0; i < 8; ++i) mine[(c / 4 + i) * BM] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
           continue;
         }
-        for (int64_t o = first; o < share; ++o) {
-          const float4* const theirs = reinterpret_cast<const float4*>(p.parts + (2 * o + rank) * PART_FLOATS) + row;
+#pragma unroll 1
+        for (int o = first; o < share; ++o) {
+          const float4* const theirs = reinterpret_cast<const float4*>(p.parts + (2 * (int64_t)o + rank) * PART_FLOATS) + row;
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
             const float4 f = __ldcg(theirs + (c / 4 + i) * BM);
@@ -582,19 +645,22 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
             v[4 * i + 3] += f.w;
           }
         }
-        const int64_t valid = j.cols - (w.s + c), at = r * j.cols + w.s + c;
-        if (r < j.rows && valid > 0) {
-          if (p.out_type == LT_F32) store32(static_cast<float*>(j.out[w.half]) + at, valid, v, alpha);
-          else if (p.out_type == LT_BF16) store32(static_cast<bf16*>(j.out[w.half]) + at, valid, v, alpha);
-          else store32(static_cast<__half*>(j.out[w.half]) + at, valid, v, alpha);
-        }
+#pragma unroll
+        for (int i = 0; i < 32; ++i) sm[lane * OUT_PITCH + i] = v[i] * alpha;
+        __syncwarp();
+        const int cols = j.cols - (s0 + c) < 32 ? (int)(j.cols - (s0 + c)) : 32;
+        const int64_t at = r0 * j.cols + s0 + c;
+        if (p.out_type == LT_F32) store_rows<float>(j.out[w.half], at, j.cols, rows, cols, sm, lane);
+        else if (p.out_type == LT_BF16) store_rows<bf16>(j.out[w.half], at, j.cols, rows, cols, sm, lane);
+        else store_rows<__half>(j.out[w.half], at, j.cols, rows, cols, sm, lane);
+        __syncwarp();
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       mbar_arrive_cluster(mapa(acc_free + 8 * acc, 0));
       if (begins) {
         __threadfence();
-        asm volatile("bar.sync 1, 128;" ::: "memory");
-        if (row == 0) asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(p.flags + 1 + 2 * share + rank), "r"(1u) : "memory");
+        asm volatile("bar.sync 2, 256;" ::: "memory");
+        if (leader) asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(p.flags + 1 + 2 * share + rank), "r"(1u) : "memory");
       }
       if (++acc == 2) {
         acc = 0;
@@ -630,20 +696,22 @@ struct Layout {
   int64_t np, nz, kp, row_blocks;
   int pieces, flag_words;
   // tiles of the products and their division (see the product kernel)
-  int64_t tiles[2], units[2], share;
-  int steps[2], clusters;
+  int64_t tiles[2], units[2], whole, share, first;
+  int steps[2], clusters, each;
   size_t z, aw, bw, partial, flags, parts, total;
 };
 Layout layout(const GradCall& c) {
   Layout l = {};
   const int halves = c.gated ? 2 : 1;
   const bool a = c.grad_a && c.K > 0, b = c.grad_b && c.K > 0;
-  l.np = up(c.N, 8);
+  l.np = up(c.N, 64);  // whole blocks of the copies' 64 columns
   l.nz = l.np * halves;
-  l.kp = up(c.K, 8);
-  l.row_blocks = (c.M + PREP_ROWS - 1) / PREP_ROWS;
+  l.kp = up(c.K, 64);
   l.pieces = a || b ? pieces(c) : 0;
   const auto blocks = [](int64_t n, int64_t by) { return (n + by - 1) / by; };
+  const int64_t most = clusters_of_the_device();
+  l.each = blocks(c.M, PREP_SIDE * PREP_EACH) * blocks(l.np, PREP_COLS) >= 4 * most ? PREP_EACH : 1;
+  l.row_blocks = blocks(c.M, PREP_SIDE * l.each);
   if (a) {
     l.steps[0] = (int)(blocks(l.nz, BL) * l.pieces);
     l.tiles[0] = blocks(c.M, 2 * BM) * blocks(c.K, BN);
@@ -653,19 +721,21 @@ Layout layout(const GradCall& c) {
     l.tiles[1] = halves * blocks(c.N, 2 * BM) * blocks(c.K, BN);
   }
   for (int i = 0; i < 2; ++i) l.units[i] = l.tiles[i] * l.steps[i];
-  // Whole tiles, in turn, or equal shares: a cut costs about ten steps (a part written and read again), and a share has at least four
-  const int64_t all = l.tiles[0] + l.tiles[1], units = l.units[0] + l.units[1], most = clusters_of_the_device();
+  // The last, broken round of tiles: whole too, or in equal shares, which have at least eight steps.  A share costs what CUT steps do
+  // beside its own: sums of a begun tile written, waited for and read.
+  constexpr int64_t CUT = 16;
+  const int64_t all = l.tiles[0] + l.tiles[1], units = l.units[0] + l.units[1];
   if (all > 0) {
-    const int64_t n = all < most ? all : most;
-    int64_t whole = 0;  // steps of the busiest cluster: cluster c takes the tiles c, c + n, ...
-    for (int64_t x = 0; x < n; ++x) {
-      const int64_t first = x < l.tiles[0] ? (l.tiles[0] - 1 - x) / n + 1 : 0, both = (all - 1 - x) / n + 1;
-      const int64_t load = first * l.steps[0] + (both - first) * l.steps[1];
-      whole = load > whole ? load : whole;
-    }
-    const int64_t even = blocks(units, most) < 4 ? 4 : blocks(units, most);
-    l.share = even + 10 < whole ? even : 0;
-    l.clusters = (int)(l.share ? blocks(units, l.share) : n);
+    const int64_t rest = all % most;
+    l.whole = all - rest;
+    l.first = l.whole < l.tiles[0] ? l.whole * l.steps[0] : l.units[0] + (l.whole - l.tiles[0]) * l.steps[1];
+    const int64_t longest = l.whole < l.tiles[0] && (l.steps[0] > l.steps[1] || !b) ? l.steps[0] : b ? l.steps[1] : l.steps[0];
+    int64_t even = blocks(units - l.first, most);
+    even = even < 8 ? 8 : even;
+    if (rest > 0 && even + CUT < longest && units < (1ll << 31)) l.share = even;
+    else l.whole = all;
+    // every cluster has a share or a whole tile
+    l.clusters = (int)(l.whole == 0 ? blocks(units, l.share) : l.whole < most ? l.whole : most);
   }
   l.flag_words = l.share ? 1 + 2 * l.clusters : 0;
   size_t at = 0;
@@ -684,13 +754,14 @@ Layout layout(const GradCall& c) {
   return l;
 }
 
-// planes x rows x cols of bfloat16, rows `pitch` elements apart; boxes of 64 columns and `box_rows` rows, 128-byte swizzle
-bool make_map(CUtensorMap* map, const void* base, int64_t cols, int64_t rows, int64_t planes, int64_t pitch, int64_t plane, int box_rows) {
+// planes x rows x pitch / 64 blocks of 64 columns of bfloat16; boxes of `box_blocks` blocks of `box_rows` rows, 128-byte swizzle
+bool make_map(CUtensorMap* map, const void* base, int64_t rows, int64_t planes, int64_t pitch, int64_t plane, int box_rows, int box_blocks) {
   const EncodeTiled encode = tensor_map_encoder();
   if (!encode) return false;
-  const cuuint64_t dims[3] = {(cuuint64_t)cols, (cuuint64_t)rows, (cuuint64_t)planes}, strides[2] = {(cuuint64_t)pitch * 2, (cuuint64_t)plane * 2};
-  const cuuint32_t box[3] = {64, (cuuint32_t)box_rows, 1}, step[3] = {1, 1, 1};
-  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
+  const cuuint64_t dims[4] = {64, (cuuint64_t)rows, (cuuint64_t)pitch / 64, (cuuint64_t)planes};
+  const cuuint64_t strides[3] = {(cuuint64_t)pitch * 2, 128, (cuuint64_t)plane * 2};
+  const cuuint32_t box[4] = {64, (cuuint32_t)box_rows, (cuuint32_t)box_blocks, 1}, step[4] = {1, 1, 1, 1};
+  return encode(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE,
                 CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
@@ -726,6 +797,7 @@ cudaError_t launch_backward(const GradCall& c, void* workspace, cudaStream_t str
   const Layout l = layout(c);
   const bool a = l.tiles[0] > 0, b = l.tiles[1] > 0;
   if (!a && !b && !c.grad_bias) return cudaSuccess;
+  if (l.tiles[0] + l.tiles[1] > 2147483647LL) return cudaErrorInvalidValue;
   unsigned char* const ws = static_cast<unsigned char*>(workspace);
 
   PrepParams q = {};
@@ -740,6 +812,7 @@ cudaError_t launch_backward(const GradCall& c, void* workspace, cudaStream_t str
   q.partial = c.grad_bias ? reinterpret_cast<float*>(ws + l.partial) : nullptr;
   q.flags = reinterpret_cast<uint32_t*>(ws + l.flags);
   q.flag_words = l.flag_words;
+  q.each = l.each;
   q.M = c.M; q.N = c.N; q.K = c.K; q.np = l.np; q.nz = l.nz; q.kp = l.kp;
   q.plane = c.M * l.nz;
   q.pieces = l.pieces;
@@ -762,15 +835,17 @@ cudaError_t launch_backward(const GradCall& c, void* workspace, cudaStream_t str
   p.row_blocks = l.row_blocks; p.N = c.N; p.np = l.np; p.nz = l.nz;
   p.flags = q.flags;
   p.parts = reinterpret_cast<float*>(ws + l.parts);
-  p.share = l.share;
-  p.tiles0 = p.tiles = l.tiles[0];
-  p.units0 = p.units = l.units[0];
-  p.tiles += l.tiles[1];
-  p.units += l.units[1];
+  p.whole = (int)l.whole;
+  p.share = (int)l.share;
+  p.tiles0 = (int)l.tiles[0];
+  p.tiles = (int)(l.tiles[0] + l.tiles[1]);
+  p.units0 = (int)l.units[0];
+  p.units = (int)(l.units[0] + l.units[1]);
+  p.first = (int)l.first;
   // (a job without tiles is never looked at: the first one's borders are both 0 then)
   const auto add = [&](int i, bool x_mn, const void* y, int64_t y_rows, int64_t rows) -> Job& {
-    if (!make_map(&p.x[i], q.z, l.nz, c.M, l.pieces, l.nz, q.plane, x_mn ? BL : BM) ||
-        !make_map(&p.y[i], y, c.K, y_rows, 1, l.kp, y_rows * l.kp, BL))
+    if (!make_map(&p.x[i], q.z, c.M, l.pieces, l.nz, q.plane, x_mn ? BL : BM, x_mn ? BM / 64 : 1) ||
+        !make_map(&p.y[i], y, y_rows, 1, l.kp, y_rows * l.kp, BL, BN / 128))
       e = cudaErrorInvalidValue;
     Job& j = p.job[i];
     j.x_mn = x_mn;
@@ -778,8 +853,8 @@ cudaError_t launch_backward(const GradCall& c, void* workspace, cudaStream_t str
     j.steps = l.steps[i];
     j.rows = rows;
     j.cols = c.K;
-    j.r_tiles = (rows + 2 * BM - 1) / (2 * BM);
-    j.s_tiles = (c.K + BN - 1) / BN;
+    j.r_tiles = (int)((rows + 2 * BM - 1) / (2 * BM));
+    j.s_tiles = (int)((c.K + BN - 1) / BN);
     return j;
   };
   if (a) {
@@ -797,7 +872,7 @@ cudaError_t launch_backward(const GradCall& c, void* workspace, cudaStream_t str
     j.div[0] = q.sb;
     j.div[1] = c.sb2;
     j.div_stride = c.sb_per_col;
-    j.half = l.np;
+    j.half = (int)(l.np / 64);
   }
   if (e != cudaSuccess) return e;
   e = cudaFuncSetAttribute(grad_product_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PRODUCT_SMEM);

@@ -144,7 +144,8 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) lba_rows_kernel(const __grid_
   };
 
   // every warp helps with the first round's activations, for which there is nothing else to do yet
-  if (warp == ROWS_COPY_WARP && lane == 0) copy(0, 0);
+  if (warp == ROWS_COPY_WARP && elected()) copy(0, 0);
+  __syncwarp();
   for (int m = warp; m < M; m += ROWS_WARPS) decode(fetch(m, lane), smem_raw, m);
   __syncthreads();
 
@@ -266,7 +267,7 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) lba_rows_kernel(const __grid_
       }
     }
   } else if (warp == ROWS_COPY_WARP) {
-    if (lane == 0) {
+    if (elected()) {
       int stage = 1;
       uint32_t phase = 0;
       for (int r = 1; r < rounds; ++r) {
