@@ -28,7 +28,12 @@ namespace lba {
 namespace {
 
 constexpr int PREP_COLS = 256, PREP_THREADS = 256, PREP_SIDE = 8 * PREP_THREADS / PREP_COLS;  // PREP_SIDE: rows beside each other in a block
-constexpr int PREP_EACH = 4;                  // rows of a thread where there are enough of them
+// A thread takes eight columns of every eighth row of its block.  The bytes of its next rows are on their way to shared memory while it
+// computes one: under load a fetch takes 2000 clocks, so an SM wants 50 KB and more in flight (4096 x 4096 in bfloat16 took 21 us with a
+// row ahead in registers).  Blocks are as tall as makes them one wave, so that what a block does but once (indexes, scales, the sums'
+// last step, a third of all instructions with four rows a thread) weighs little.
+__host__ __device__ constexpr int prep_depth(int bytes) { return 4 * PREP_THREADS * bytes <= 48 * 1024 ? 4 : 2; }
+constexpr int PREP_RESIDENT = 4;  // blocks that an SM holds, as a rule
 typedef __nv_bfloat16 bf16;
 
 struct PrepParams {
@@ -43,30 +48,41 @@ struct PrepParams {
   int pieces;                // 0: no product is wanted
   int act, in_m4e3, sb_per_col, flag_words, each;
   uint32_t drop_below;
-  int64_t z_blocks, col_blocks, a_blocks;  // blocks of dz, then of A's codes, then of B's
+  int z_blocks, col_blocks, a_blocks;  // blocks of dz, then of A's codes, then of B's
 };
 
 template <typename T> struct Raw8;  // eight elements as they lie in memory
 template <> struct Raw8<float> { float4 v[2]; };
 template <> struct Raw8<bf16> { uint4 v; };
 template <> struct Raw8<__half> { uint4 v; };
-// eight neighbouring elements from i on, `valid` of which exist
+// sends for eight neighbouring elements, `valid` of which exist; they arrive in this thread's slot (one in every PREP_THREADS sixteen
+// bytes).  whole: all eight, at a 16-byte boundary
 template <typename T>
-__device__ __forceinline__ Raw8<T> load8(const void* base, int64_t i, int valid) {
-  Raw8<T> r;
-  const T* const src = static_cast<const T*>(base) + i;
-  if (valid == 8 && (reinterpret_cast<uintptr_t>(src) & 15) == 0) {
-    if constexpr (sizeof(T) == 4) {
-      r.v[0] = __ldcs(reinterpret_cast<const float4*>(src));
-      r.v[1] = __ldcs(reinterpret_cast<const float4*>(src) + 1);
-    } else {
-      r.v = __ldcs(reinterpret_cast<const uint4*>(src));
-    }
-  } else {
-    T* const e = reinterpret_cast<T*>(&r);
+__device__ __forceinline__ void send_for8(uint4* slot, const T* src, bool whole, int valid) {
+  if (whole) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) e[j] = j < valid ? src[j] : from_f32<T>(0.0f);
+    for (int q = 0; q < (int)sizeof(T) / 2; ++q)
+      asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(slot + q * PREP_THREADS)), "l"(reinterpret_cast<const uint4*>(src) + q) : "memory");
+  } else {
+    constexpr int PER = 16 / (int)sizeof(T);
+#pragma unroll
+    for (int q = 0; q < 8 / PER; ++q) {
+      T* const dst = reinterpret_cast<T*>(slot + q * PREP_THREADS);
+#pragma unroll
+      for (int j = 0; j < PER; ++j) dst[j] = q * PER + j < valid ? src[q * PER + j] : from_f32<T>(0.0f);
+    }
   }
+}
+template <typename T>
+__device__ __forceinline__ bool whole8(const void* base, int64_t pitch, int valid) {
+  return valid == 8 && ((reinterpret_cast<uintptr_t>(base) | (uintptr_t)(pitch * sizeof(T))) & 15) == 0;
+}
+template <typename T>
+__device__ __forceinline__ Raw8<T> arrived8(const uint4* slot) {
+  Raw8<T> r;
+  uint4* const v = reinterpret_cast<uint4*>(&r);
+#pragma unroll
+  for (int q = 0; q < (int)sizeof(T) / 2; ++q) v[q] = slot[q * PREP_THREADS];
   return r;
 }
 template <typename T>
@@ -153,17 +169,20 @@ __device__ __forceinline__ void expand_codes(const PrepParams& p, const uint8_t*
 }
 
 template <typename G, typename Z, bool GATED>
-__global__ void __launch_bounds__(PREP_THREADS, GATED ? 2 : 3) grad_prepare_kernel(const PrepParams p) {
+__global__ void __launch_bounds__(PREP_THREADS, GATED ? 3 : 4) grad_prepare_kernel(const PrepParams p) {
   constexpr int HALVES = GATED ? 2 : 1;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  // The second kernel's CTAs may be set up as SMs run out of these: they are let in when the last of these has started, and wait for
+  // the end of all (its shared memory does not fit beside these)
+  asm volatile("griddepcontrol.launch_dependents;" ::: "memory");
   after_previous();
-  int64_t b = blockIdx.x;
+  int b = blockIdx.x;
   if (b == 0)
     for (int i = threadIdx.x; i < p.flag_words; i += PREP_THREADS) p.flags[i] = 0u;
   if (b >= p.z_blocks) {  // codes: a warp takes a row at a time
     b -= p.z_blocks;
     const bool is_a = b < p.a_blocks;
-    const int64_t row = (is_a ? b : b - p.a_blocks) * 8 + warp;
+    const int64_t row = (int64_t)(is_a ? b : b - p.a_blocks) * 8 + warp;
     const uint8_t* src = nullptr;
     bf16* dst;
     if (is_a) {
@@ -180,8 +199,12 @@ __global__ void __launch_bounds__(PREP_THREADS, GATED ? 2 : 3) grad_prepare_kern
     return;
   }
 
-  __shared__ __align__(8) float sums[HALVES][PREP_THREADS / 32][PREP_COLS];
-  const int64_t n = (b % p.col_blocks) * PREP_COLS + lane * 8, m0 = (b / p.col_blocks) * (PREP_SIDE * p.each) + warp;
+  constexpr int G_SLOTS = sizeof(G) / 2, Z_SLOTS = sizeof(Z) / 2, ROW_SLOTS = (G_SLOTS + HALVES * Z_SLOTS) * PREP_THREADS;
+  constexpr int DEPTH = prep_depth(16 * ROW_SLOTS / PREP_THREADS);
+  __shared__ uint4 store[DEPTH * ROW_SLOTS];
+  static_assert(sizeof(store) >= HALVES * PREP_THREADS * 8 * 4 && sizeof(store) <= 48 * 1024, "the sums of the rows take its place");
+  const int row_block = b / p.col_blocks, col_block = b - row_block * p.col_blocks;  // (64-bit divisions here had been a third of all instructions)
+  const int64_t n = (int64_t)col_block * PREP_COLS + lane * 8, m0 = (int64_t)row_block * (PREP_SIDE * p.each) + warp;
   const int valid = n >= p.N ? 0 : p.N - n < 8 ? (int)(p.N - n) : 8;
   u64 total[HALVES][4];
 #pragma unroll
@@ -189,6 +212,29 @@ __global__ void __launch_bounds__(PREP_THREADS, GATED ? 2 : 3) grad_prepare_kern
 #pragma unroll
     for (int j = 0; j < 4; ++j) total[h][j] = 0ull;
   if (n < p.np && m0 < p.M) {
+    const bool reads_z = GATED || p.act != ACT_NONE;
+    const int64_t left = (p.M - m0 + PREP_SIDE - 1) / PREP_SIDE;
+    const int rows = left < p.each ? (int)left : p.each;
+    const int64_t pitch = PREP_SIDE * p.N;
+    const G* gp = static_cast<const G*>(p.grad) + m0 * p.N + n;
+    const Z* zp = static_cast<const Z*>(p.pre) + m0 * p.N + n;
+    const bool g_whole = whole8<G>(p.grad, p.N, valid), z_whole = whole8<Z>(p.pre, p.N, valid) && (!GATED || p.M * p.N * sizeof(Z) % 16 == 0);
+    uint4* slot = store + threadIdx.x;
+    const auto send = [&](bool there) {  // for the next row, into the current slot
+      if (there) {
+        send_for8(slot, gp, g_whole, valid);
+        if (reads_z) {
+#pragma unroll
+          for (int h = 0; h < HALVES; ++h) send_for8(slot + (G_SLOTS + h * Z_SLOTS) * PREP_THREADS, zp + h * p.M * p.N, z_whole, valid);
+        }
+        gp += pitch;
+        zp += pitch;
+      }
+      asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+#pragma unroll
+    for (int i = 0; i < DEPTH; ++i, slot += ROW_SLOTS) send(i < rows);
+    slot = store + threadIdx.x;
     u64 scale[HALVES][4];
 #pragma unroll
     for (int h = 0; h < HALVES; ++h) {
@@ -200,31 +246,15 @@ __global__ void __launch_bounds__(PREP_THREADS, GATED ? 2 : 3) grad_prepare_kern
     with_act(p.act, [&](auto act_tag) {
       constexpr int ACT = decltype(act_tag)::value;
       constexpr bool READS_Z = GATED || ACT != ACT_NONE;
-      // the next row is on its way while one is computed; a rolled loop, because a straight run of four rows is 3000 instructions that
-      // each warp fetches once (32 x 512 took 18 us)
-      Raw8<G> g, g_next = load8<G>(p.grad, m0 * p.N + n, valid);
-      Raw8<Z> z[HALVES], z_next[HALVES];
-      if (READS_Z) {
-#pragma unroll
-        for (int h = 0; h < HALVES; ++h) z_next[h] = load8<Z>(p.pre, (h * p.M + m0) * p.N + n, valid);
-      }
+      bf16* out = p.z + m0 * p.nz + n;
+      int64_t m = m0;
+      // (a rolled loop: a straight run of four rows is 3000 instructions that each warp fetches once; 32 x 512 took 18 us)
 #pragma unroll 1
-      for (int i = 0; i < p.each; ++i) {
-        const int64_t m = m0 + i * PREP_SIDE, after = m + PREP_SIDE;
-        if (m >= p.M) break;
-        g = g_next;
-#pragma unroll
-        for (int h = 0; h < HALVES; ++h) z[h] = z_next[h];
-        if (i + 1 < p.each && after < p.M) {
-          g_next = load8<G>(p.grad, after * p.N + n, valid);
-          if (READS_Z) {
-#pragma unroll
-            for (int h = 0; h < HALVES; ++h) z_next[h] = load8<Z>(p.pre, (h * p.M + after) * p.N + n, valid);
-          }
-        }
+      for (int i = 0; i < rows; ++i, m += PREP_SIDE, out += PREP_SIDE * p.nz) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(DEPTH - 1) : "memory");
         u64 gv[4], zv[4], d[HALVES][4];
-        widen8(g, gv);
-        if (READS_Z) widen8(z[0], zv);
+        widen8(arrived8<G>(slot), gv);
+        if (READS_Z) widen8(arrived8<Z>(slot + G_SLOTS * PREP_THREADS), zv);
         if (!GATED && p.drop_below) {
           const uint64_t seed = p.rng[0], offset = p.rng[1];
 #pragma unroll
@@ -238,7 +268,7 @@ __global__ void __launch_bounds__(PREP_THREADS, GATED ? 2 : 3) grad_prepare_kern
           }
         }
         [[maybe_unused]] u64 other[4];
-        if constexpr (GATED) widen8(z[HALVES - 1], other);
+        if constexpr (GATED) widen8(arrived8<Z>(slot + (G_SLOTS + Z_SLOTS) * PREP_THREADS), other);
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
           u64 value, slope;
@@ -269,25 +299,31 @@ __global__ void __launch_bounds__(PREP_THREADS, GATED ? 2 : 3) grad_prepare_kern
 #pragma unroll
             for (int j = 0; j < 4; ++j) s[j] = mul2_rn(s[j], by);
           }
-          if (p.pieces) store_pieces(p.z + m * p.nz + h * p.np + n, p.plane, p.pieces, s);
+          if (p.pieces) store_pieces(out + h * p.np, p.plane, p.pieces, s);
         }
+        send(i + DEPTH < rows);
+        slot += ROW_SLOTS;
+        if (slot >= store + DEPTH * ROW_SLOTS) slot -= DEPTH * ROW_SLOTS;
       }
     });
   }
   if (!p.partial) return;
+  __syncthreads();  // `store` is free
+  float* const sums = reinterpret_cast<float*>(store);  // [half][warp][column]
 #pragma unroll
   for (int h = 0; h < HALVES; ++h)
 #pragma unroll
-    for (int j = 0; j < 4; ++j) *reinterpret_cast<u64*>(&sums[h][warp][lane * 8 + 2 * j]) = total[h][j];
+    for (int j = 0; j < 4; j += 2)
+      *reinterpret_cast<ulonglong2*>(&sums[(h * (PREP_THREADS / 32) + warp) * PREP_COLS + lane * 8 + 2 * j]) = make_ulonglong2(total[h][j], total[h][j + 1]);
   __syncthreads();
-  const int64_t col = (b % p.col_blocks) * PREP_COLS + threadIdx.x;
+  const int64_t col = (int64_t)col_block * PREP_COLS + threadIdx.x;
   if (col >= p.np) return;
 #pragma unroll
   for (int h = 0; h < HALVES; ++h) {
     float s = 0.0f;
 #pragma unroll
-    for (int w = 0; w < PREP_THREADS / 32; ++w) s += sums[h][w][threadIdx.x];
-    p.partial[(b / p.col_blocks) * p.nz + h * p.np + col] = s;
+    for (int w = 0; w < PREP_THREADS / 32; ++w) s += sums[(h * (PREP_THREADS / 32) + w) * PREP_COLS + threadIdx.x];
+    p.partial[row_block * p.nz + h * p.np + col] = s;
   }
 }
 
@@ -310,7 +346,7 @@ __global__ void __launch_bounds__(PREP_THREADS, GATED ? 2 : 3) grad_prepare_kern
 // starts: it only ever waits for clusters that run already or have ended, for the first thing that those do.
 constexpr int BM = 128, BN = 256, BL = 64, GRAD_THREADS = 320, OUT_THREADS = 256;  // of a CTA: rows, columns, step
 constexpr int X_BYTES = BM * BL * 2, STAGE = 2 * X_BYTES, STAGES = 5;
-constexpr int OUT_PITCH = 33;         // floats from row to row of a warp's 32 x 32 outputs in shared memory
+constexpr int OUT_PITCH = 36;         // floats from row to row of a warp's 32 x 32 outputs in shared memory: 16-byte accesses on all banks
 constexpr size_t PRODUCT_SMEM = 1024 + (size_t)STAGE * STAGES + 256 + OUT_THREADS * OUT_PITCH * 4;
 constexpr int PART_FLOATS = BM * BN;  // a CTA's part of a begun tile
 
@@ -365,8 +401,10 @@ __device__ __forceinline__ void mma_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar), "h"((uint16_t)3)
                : "memory");
 }
+// (orders nothing but the arrival: what it follows, reads of tensor memory, has its own fence, and a release would wait for the
+// outputs' stores)
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
-  asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
 }
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -456,9 +494,8 @@ __device__ __forceinline__ void store_rows(void* base, int64_t at, int64_t pitch
     const float* src = sm + (lane / 8) * OUT_PITCH + c;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      T t[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) t[j] = from_f32<T>(src[i * 4 * OUT_PITCH + j]);
+      const float4 f = *reinterpret_cast<const float4*>(src + i * 4 * OUT_PITCH);
+      const T t[4] = {from_f32<T>(f.x), from_f32<T>(f.y), from_f32<T>(f.z), from_f32<T>(f.w)};
       typename Bytes<4 * sizeof(T)>::type raw;
       memcpy(&raw, t, sizeof(raw));
       if (i * 4 + lane / 8 < rows) *reinterpret_cast<decltype(raw)*>(dst) = raw;
@@ -494,7 +531,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
     }
     for (int i = 0; i < 2; ++i) {
       mbar_init(acc_done + 8 * i, 1);
-      mbar_init(acc_free + 8 * i, 2 * OUT_THREADS);  // the first CTA's: both CTAs' readers
+      mbar_init(acc_free + 8 * i, 2 * OUT_THREADS / 32);  // the first CTA's: both CTAs' reading warps
     }
     *dead = 0;
     mbar_init_fence();
@@ -502,6 +539,10 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)), "r"(2 * BN) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+  }
+  if (warp == 2 && lane < 4) {
+    const CUtensorMap* const map = lane < 2 ? &p.x[lane] : &p.y[lane - 2];
+    asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory");
   }
   __syncwarp();
   if (p.share) cluster_sync();  // the other CTA runs: its memory may be written
@@ -619,10 +660,12 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
       if (*dead) alpha = __uint_as_float(0x7FC00000u);
       float4* const mine = reinterpret_cast<float4*>(p.parts + (2 * (int64_t)share + rank) * PART_FLOATS) + row;  // [four columns][row]
       const int rows = j.rows - r0 < 32 ? (int)(j.rows - r0 > 0 ? j.rows - r0 : 0) : 32;
-      const int64_t s0 = (int64_t)w.s * BN;
+      const int64_t s0 = (int64_t)w.s * BN, pitch = j.cols;
+      void* const out = j.out[w.half];
+      const int type = p.out_type;
 #pragma unroll 1
       for (int c = c_first; c < c_first + BN / 2; c += 32) {
-        if (!begins && s0 + c >= j.cols) break;
+        if (!begins && s0 + c >= pitch) break;
         uint32_t t[32];
         float v[32];
         tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + acc * BN + c, t);
@@ -646,17 +689,20 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
           }
         }
 #pragma unroll
-        for (int i = 0; i < 32; ++i) sm[lane * OUT_PITCH + i] = v[i] * alpha;
+        for (int i = 0; i < 8; ++i)
+          *reinterpret_cast<float4*>(sm + lane * OUT_PITCH + 4 * i) =
+              make_float4(v[4 * i] * alpha, v[4 * i + 1] * alpha, v[4 * i + 2] * alpha, v[4 * i + 3] * alpha);
         __syncwarp();
-        const int cols = j.cols - (s0 + c) < 32 ? (int)(j.cols - (s0 + c)) : 32;
-        const int64_t at = r0 * j.cols + s0 + c;
-        if (p.out_type == LT_F32) store_rows<float>(j.out[w.half], at, j.cols, rows, cols, sm, lane);
-        else if (p.out_type == LT_BF16) store_rows<bf16>(j.out[w.half], at, j.cols, rows, cols, sm, lane);
-        else store_rows<__half>(j.out[w.half], at, j.cols, rows, cols, sm, lane);
+        const int cols = pitch - (s0 + c) < 32 ? (int)(pitch - (s0 + c)) : 32;
+        const int64_t at = r0 * pitch + s0 + c;
+        if (type == LT_F32) store_rows<float>(out, at, pitch, rows, cols, sm, lane);
+        else if (type == LT_BF16) store_rows<bf16>(out, at, pitch, rows, cols, sm, lane);
+        else store_rows<__half>(out, at, pitch, rows, cols, sm, lane);
         __syncwarp();
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
-      mbar_arrive_cluster(mapa(acc_free + 8 * acc, 0));
+      __syncwarp();
+      if (lane == 0) mbar_arrive_cluster(mapa(acc_free + 8 * acc, 0));
       if (begins) {
         __threadfence();
         asm volatile("bar.sync 2, 256;" ::: "memory");
@@ -710,7 +756,8 @@ Layout layout(const GradCall& c) {
   l.pieces = a || b ? pieces(c) : 0;
   const auto blocks = [](int64_t n, int64_t by) { return (n + by - 1) / by; };
   const int64_t most = clusters_of_the_device();
-  l.each = blocks(c.M, PREP_SIDE * PREP_EACH) * blocks(l.np, PREP_COLS) >= 4 * most ? PREP_EACH : 1;
+  l.each = (int)blocks(blocks(c.M, PREP_SIDE) * blocks(l.np, PREP_COLS), 2 * most * PREP_RESIDENT);
+  l.each = l.each < 1 ? 1 : l.each > 64 ? 64 : l.each;
   l.row_blocks = blocks(c.M, PREP_SIDE * l.each);
   if (a) {
     l.steps[0] = (int)(blocks(l.nz, BL) * l.pieces);
@@ -818,11 +865,12 @@ cudaError_t launch_backward(const GradCall& c, void* workspace, cudaStream_t str
   q.pieces = l.pieces;
   q.act = c.act; q.in_m4e3 = c.in_m4e3; q.sb_per_col = c.sb_per_col;
   q.drop_below = c.drop_below;
-  q.col_blocks = (l.np + PREP_COLS - 1) / PREP_COLS;
-  q.z_blocks = q.col_blocks * l.row_blocks;
-  q.a_blocks = b ? (c.M + 7) / 8 : 0;
-  const int64_t b_blocks = a ? (l.nz + 7) / 8 : 0, blocks = q.z_blocks + q.a_blocks + b_blocks;
+  const int64_t col_blocks = (l.np + PREP_COLS - 1) / PREP_COLS, z_blocks = col_blocks * l.row_blocks, a_blocks = b ? (c.M + 7) / 8 : 0;
+  const int64_t blocks = z_blocks + a_blocks + (a ? (l.nz + 7) / 8 : 0);
   if (blocks > 2147483647LL) return cudaErrorInvalidValue;
+  q.col_blocks = (int)col_blocks;
+  q.z_blocks = (int)z_blocks;
+  q.a_blocks = (int)a_blocks;
   e = c.grad_type == LT_F32 ? launch_prepare<float>(q, c, (unsigned)blocks, stream)
       : c.grad_type == LT_BF16 ? launch_prepare<bf16>(q, c, (unsigned)blocks, stream) : launch_prepare<__half>(q, c, (unsigned)blocks, stream);
   if (e != cudaSuccess) return e;
