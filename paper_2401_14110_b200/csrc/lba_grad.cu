@@ -342,7 +342,8 @@ __global__ void __launch_bounds__(PREP_THREADS, GATED ? 3 : 4) grad_prepare_kern
 // Clusters take whole tiles in turn, side by side in l, so that what one fetches its neighbours find in L2.  The tiles of a last, broken
 // round are divided instead: their steps of 64 l stand in one row, cut into equal shares, one per cluster.  A tile that a border
 // cuts is begun by lower shares, which leave binary32 sums in the workspace, and finished by the share with its last step, which
-// adds them in order.  A cluster walks its share from the end and before its whole tiles, and takes the share's number from a counter when it
+// adds them in order.  (`longest`: binary32 results of long sums would lose precision to the matrix instructions, which cut a sum at each
+// addition: 8192 terms were off by 2.8e-6, where 1500 are by 8e-7.  Their tiles are formed in stretches, added up in binary32.)  A cluster walks its share from the end and before its whole tiles, and takes the share's number from a counter when it
 // starts: it only ever waits for clusters that run already or have ended, for the first thing that those do.
 constexpr int BM = 128, BN = 256, BL = 64, GRAD_THREADS = 320, OUT_THREADS = 256;  // of a CTA: rows, columns, step
 constexpr int X_BYTES = BM * BL * 2, STAGE = 2 * X_BYTES, STAGES = 5;
@@ -354,7 +355,7 @@ struct Job {
   int64_t rows, cols;       // of one half's output
   int r_tiles, s_tiles;     // r_tiles: of one half
   int half;                 // blocks of 64 before the second half's first in X
-  int x_mn, pieces, steps;  // steps: blocks of l times pieces
+  int x_mn, pieces, blocks, steps;  // blocks of l, and these times pieces
   int div_stride;
   void* out[2];
   const float *alpha[2], *div[2];  // factors of a half, divisors of its rows (or null)
@@ -366,10 +367,11 @@ struct ProductParams {
   int whole;                // tiles that stay whole, the first ones
   int units0, units, first; // with shares: steps of the first job, of both, those before the divided ones
   int share;                // steps of a cluster's share; 0: there are none
+  int longest;              // steps that the matrix instructions add up before binary32 additions take over (all, if none is meant)
   int out_type;
   float factor;
   uint32_t* flags;          // shares: the counter, then a word per CTA's part
-  float* parts;
+  float *parts, *sums;      // parts of begun tiles, and sums of a CTA's steps so far: PART_FLOATS each per CTA
   const float* partial;     // bias: [row blocks][nz]
   float* bias[2];
   int64_t row_blocks, N, np, nz;
@@ -426,6 +428,8 @@ __device__ __forceinline__ void tmem_ld32(uint32_t addr, uint32_t (&r)[32]) {
 struct Work {
   int job, half, k0, k1;
   int r, s, start;  // first row tile (of the half) and column tile, the tile's first step among all
+  bool goes_on, last;  // k0 to k1 are not the first, are the last steps of this piece
+  int from, to;        // its steps
 };
 struct Walk {
   int at, end, tile, by;  // steps [end, at) of the share are left; the next whole tile, the number of clusters
@@ -438,22 +442,32 @@ struct Walk {
       at = end + p.share < p.units ? end + p.share : p.units;
     }
   }
+  __device__ __forceinline__ void stretch(const ProductParams& p, Work& w) {
+    w.last = w.to - w.k0 <= p.longest;
+    w.k1 = w.last ? w.to : w.k0 + p.longest;
+  }
   __device__ __forceinline__ bool next(const ProductParams& p, Work& w) {
+    if (!w.last) {  // more of the same piece
+      w.k0 = w.k1;
+      w.goes_on = true;
+      stretch(p, w);
+      return true;
+    }
     int t;
     if (at > end) {
       w.job = at - 1 >= p.units0;
       const int steps = p.job[w.job].steps, base = w.job ? p.units0 : 0;
       t = (at - 1 - base) / steps;
       w.start = base + t * steps;
-      w.k1 = at - w.start;
-      w.k0 = end > w.start ? end - w.start : 0;
-      at = w.start + w.k0;
+      w.to = at - w.start;
+      w.from = end > w.start ? end - w.start : 0;
+      at = w.start + w.from;
     } else {
       if (tile >= p.whole) return false;
       w.job = tile >= p.tiles0;
       t = w.job ? tile - p.tiles0 : tile;
-      w.k0 = 0;
-      w.k1 = p.job[w.job].steps;
+      w.from = 0;
+      w.to = p.job[w.job].steps;
       w.start = 0;
       tile += by;
     }
@@ -462,6 +476,9 @@ struct Walk {
     w.s = t - row * j.s_tiles;
     w.half = row >= j.r_tiles;
     w.r = w.half ? row - j.r_tiles : row;
+    w.k0 = w.from;
+    w.goes_on = false;
+    stretch(p, w);
     return true;
   }
 };
@@ -560,6 +577,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
   const int share = p.share ? (int)*share_slot : blockIdx.x >> 1;
   Walk walk(p, share, gridDim.x >> 1);
   Work w;
+  w.last = true;
 
   if (warp == 0) {
     if (elected()) {
@@ -570,9 +588,12 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
       while (alive && walk.next(p, w)) {
         const Job& j = p.job[w.job];
         const CUtensorMap *const xm = &p.x[w.job], *const ym = &p.y[w.job];
-        const int x_mn = j.x_mn, pieces = j.pieces;
+        const int x_mn = j.x_mn, blocks = j.blocks;
         const int r = w.r * (2 * BM) + rank * BM, rb = r / 64 + (w.half ? j.half : 0), sb = w.s * (BN / 64) + rank * (BN / 128);
-        int l = w.k0 / pieces, q = w.k0 - l * pieces;
+        // the last piece first: the matrix instructions cut their sums, so what is small is added up before what is large (all pieces of
+        // a step together had tripled the error of binary32 results)
+        int q = w.k0 / blocks, l = w.k0 - q * blocks;
+        q = j.pieces - 1 - q;
 #pragma unroll 1
         for (int k = w.k0; k < w.k1; ++k) {
           if (!mbar_wait(empty + 8 * stage, phase, dead)) {
@@ -584,9 +605,9 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
           if (x_mn) tma_load(x, xm, l * BL, rb, q, bar);
           else tma_load(x, xm, r, l, q, bar);
           tma_load(x + X_BYTES, ym, l * BL, sb, 0, bar);
-          if (++q == pieces) {
-            q = 0;
-            ++l;
+          if (++l == blocks) {
+            l = 0;
+            --q;
           }
           if (++stage == STAGES) {
             stage = 0;
@@ -645,7 +666,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
     uint32_t phase = 0;
     while (walk.next(p, w)) {
       const Job& j = p.job[w.job];
-      const bool begins = w.k1 < j.steps, ends = w.k0 > 0 && !begins;
+      const bool begins = w.last && w.to < j.steps, ends = w.last && w.from > 0 && !begins;
       const int first = ends ? (w.start - p.first) / p.share : share;  // the shares that began this tile: first to share - 1
       if (ends) {
         if (leader)
@@ -659,18 +680,34 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       if (*dead) alpha = __uint_as_float(0x7FC00000u);
       float4* const mine = reinterpret_cast<float4*>(p.parts + (2 * (int64_t)share + rank) * PART_FLOATS) + row;  // [four columns][row]
+      float4* const sums = reinterpret_cast<float4*>(p.sums + (int64_t)blockIdx.x * PART_FLOATS) + row;
       const int rows = j.rows - r0 < 32 ? (int)(j.rows - r0 > 0 ? j.rows - r0 : 0) : 32;
       const int64_t s0 = (int64_t)w.s * BN, pitch = j.cols;
       void* const out = j.out[w.half];
       const int type = p.out_type;
 #pragma unroll 1
       for (int c = c_first; c < c_first + BN / 2; c += 32) {
-        if (!begins && s0 + c >= pitch) break;
+        if (!begins && s0 + c >= pitch) break;  // (nothing of these is ever read)
         uint32_t t[32];
         float v[32];
         tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + acc * BN + c, t);
 #pragma unroll
         for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(t[i]);
+        if (w.goes_on) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            const float4 f = __ldcg(sums + (c / 4 + i) * BM);
+            v[4 * i] += f.x;
+            v[4 * i + 1] += f.y;
+            v[4 * i + 2] += f.z;
+            v[4 * i + 3] += f.w;
+          }
+        }
+        if (!w.last) {  // (read by this thread alone)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) __stcg(sums + (c / 4 + i) * BM, make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
+          continue;
+        }
         if (begins) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) mine[(c / 4 + i) * BM] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
@@ -743,8 +780,8 @@ struct Layout {
   int pieces, flag_words;
   // tiles of the products and their division (see the product kernel)
   int64_t tiles[2], units[2], whole, share, first;
-  int steps[2], clusters, each;
-  size_t z, aw, bw, partial, flags, parts, total;
+  int steps[2], clusters, each, longest;
+  size_t z, aw, bw, partial, flags, parts, sums, total;
 };
 Layout layout(const GradCall& c) {
   Layout l = {};
@@ -797,6 +834,10 @@ Layout layout(const GradCall& c) {
   l.partial = take(c.grad_bias ? (size_t)l.row_blocks * l.nz * 4 : 0);
   l.flags = take((size_t)l.flag_words * 4);
   l.parts = take(l.share ? (size_t)l.clusters * 2 * PART_FLOATS * 4 : 0);
+  const int most_steps = l.steps[0] > l.steps[1] ? l.steps[0] : l.steps[1];
+  constexpr int LONGEST = 24;
+  l.longest = c.out_type == LT_F32 && most_steps > LONGEST ? LONGEST : 2147483647;
+  l.sums = take(l.longest < most_steps ? (size_t)l.clusters * 2 * PART_FLOATS * 4 : 0);
   l.total = at;
   return l;
 }
@@ -883,6 +924,8 @@ cudaError_t launch_backward(const GradCall& c, void* workspace, cudaStream_t str
   p.row_blocks = l.row_blocks; p.N = c.N; p.np = l.np; p.nz = l.nz;
   p.flags = q.flags;
   p.parts = reinterpret_cast<float*>(ws + l.parts);
+  p.sums = reinterpret_cast<float*>(ws + l.sums);
+  p.longest = l.longest;
   p.whole = (int)l.whole;
   p.share = (int)l.share;
   p.tiles0 = (int)l.tiles[0];
@@ -898,6 +941,7 @@ cudaError_t launch_backward(const GradCall& c, void* workspace, cudaStream_t str
     Job& j = p.job[i];
     j.x_mn = x_mn;
     j.pieces = l.pieces;
+    j.blocks = l.steps[i] / l.pieces;
     j.steps = l.steps[i];
     j.rows = rows;
     j.cols = c.K;
