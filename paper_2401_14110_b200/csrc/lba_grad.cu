@@ -343,7 +343,7 @@ __global__ void __launch_bounds__(PREP_THREADS, GATED ? 3 : 4) grad_prepare_kern
 // round are divided instead: their steps of 64 l stand in one row, cut into equal shares, one per cluster.  A tile that a border
 // cuts is begun by lower shares, which leave binary32 sums in the workspace, and finished by the share with its last step, which
 // adds them in order.  (`longest`: binary32 results of long sums would lose precision to the matrix instructions, which cut a sum at each
-// addition: 8192 terms were off by 2.8e-6, where 1500 are by 8e-7.  Their tiles are formed in stretches, added up in binary32.)  A cluster walks its share from the end and before its whole tiles, and takes the share's number from a counter when it
+// addition: 8192 terms were off by 2.8e-6, where 1000 are by 8e-7.  Their tiles are formed in stretches, added up in binary32.)  A cluster walks its share from the end and before its whole tiles, and takes the share's number from a counter when it
 // starts: it only ever waits for clusters that run already or have ended, for the first thing that those do.
 constexpr int BM = 128, BN = 256, BL = 64, GRAD_THREADS = 320, OUT_THREADS = 256;  // of a CTA: rows, columns, step
 constexpr int X_BYTES = BM * BL * 2, STAGE = 2 * X_BYTES, STAGES = 5;
@@ -780,7 +780,7 @@ struct Layout {
   int pieces, flag_words;
   // tiles of the products and their division (see the product kernel)
   int64_t tiles[2], units[2], whole, share, first;
-  int steps[2], clusters, each, longest;
+  int steps[2], at_a, at_b, clusters, each, longest;  // at_a, at_b: each product's place in the list
   size_t z, aw, bw, partial, flags, parts, sums, total;
 };
 Layout layout(const GradCall& c) {
@@ -796,28 +796,52 @@ Layout layout(const GradCall& c) {
   l.each = (int)blocks(blocks(c.M, PREP_SIDE) * blocks(l.np, PREP_COLS), 2 * most * PREP_RESIDENT);
   l.each = l.each < 1 ? 1 : l.each > 64 ? 64 : l.each;
   l.row_blocks = blocks(c.M, PREP_SIDE * l.each);
+  // the product with shorter sums first: long tiles are the ones to divide
+  const int64_t steps_a = blocks(l.nz, BL) * l.pieces, steps_b = blocks(c.M, BL) * l.pieces;
+  l.at_a = !a ? -1 : b && steps_b < steps_a ? 1 : 0;
+  l.at_b = !b ? -1 : l.at_a == 0 ? 1 : 0;
   if (a) {
-    l.steps[0] = (int)(blocks(l.nz, BL) * l.pieces);
-    l.tiles[0] = blocks(c.M, 2 * BM) * blocks(c.K, BN);
+    l.steps[l.at_a] = (int)steps_a;
+    l.tiles[l.at_a] = blocks(c.M, 2 * BM) * blocks(c.K, BN);
   }
   if (b) {
-    l.steps[1] = (int)(blocks(c.M, BL) * l.pieces);
-    l.tiles[1] = halves * blocks(c.N, 2 * BM) * blocks(c.K, BN);
+    l.steps[l.at_b] = (int)steps_b;
+    l.tiles[l.at_b] = halves * blocks(c.N, 2 * BM) * blocks(c.K, BN);
   }
   for (int i = 0; i < 2; ++i) l.units[i] = l.tiles[i] * l.steps[i];
-  // The last, broken round of tiles: whole too, or in equal shares, which have at least eight steps.  A share costs what CUT steps do
-  // beside its own: sums of a begun tile written, waited for and read.
-  constexpr int64_t CUT = 16;
+  // How many tiles stay whole: all, or some full rounds of the clusters, the others in equal shares.  In steps, a share costs beside its
+  // own what its begun sums take to be written and waited for, less where whole tiles follow, and the finishing cluster JOIN for each share that it
+  // adds: a tile must not be cut too often.  All tiles whole and like this, us: 256 x 8192 x 512 gated 91.5 and 55.3 (94 with 26 shares a
+  // tile), 8192 x 512 x 512 51.2 and 35.8, 6000 x 4096 x 1024 106.7 and 98.6, 4096 x 4096 x 1024 71.2 and 70.9.
+  constexpr int64_t CUT = 30, CUT_BEFORE_WHOLE = 14, JOIN = 5;
   const int64_t all = l.tiles[0] + l.tiles[1], units = l.units[0] + l.units[1];
+  const auto steps_of = [&](int64_t tile) { return (int64_t)(tile < l.tiles[0] ? l.steps[0] : l.steps[1]); };
+  const auto steps_before = [&](int64_t tile) { return tile < l.tiles[0] ? tile * l.steps[0] : l.units[0] + (tile - l.tiles[0]) * l.steps[1]; };
   if (all > 0) {
-    const int64_t rest = all % most;
-    l.whole = all - rest;
-    l.first = l.whole < l.tiles[0] ? l.whole * l.steps[0] : l.units[0] + (l.whole - l.tiles[0]) * l.steps[1];
-    const int64_t longest = l.whole < l.tiles[0] && (l.steps[0] > l.steps[1] || !b) ? l.steps[0] : b ? l.steps[1] : l.steps[0];
-    int64_t even = blocks(units - l.first, most);
-    even = even < 8 ? 8 : even;
-    if (rest > 0 && even + CUT < longest && units < (1ll << 31)) l.share = even;
-    else l.whole = all;
+    // the busiest cluster, whose tile is the last of every round: rounds up to the last whole one
+    const auto load = [&](int64_t whole) {
+      int64_t sum = 0;
+      const int64_t rounds = blocks(whole, most), in_first = l.tiles[0] / most;  // full rounds of the first product
+      const int64_t first = rounds < in_first ? rounds : in_first;
+      sum = first * l.steps[0];
+      if (rounds > first) sum += (rounds - first - 1) * steps_of(all - 1) + steps_of(whole - 1);
+      return sum;
+    };
+    l.whole = all;
+    int64_t least = load(all);
+    for (int64_t whole = all / most * most, tries = 0; whole >= 0 && tries < 8 && units < (1ll << 31); whole -= most, ++tries) {
+      if (whole == all) continue;
+      const int64_t longest = steps_of(all - 1);
+      int64_t even = blocks(units - steps_before(whole), most);
+      while (even < 8 || even * even < JOIN * longest) ++even;
+      const int64_t time = load(whole) + even + (whole > 0 ? CUT_BEFORE_WHOLE : CUT) + JOIN * blocks(longest, even);
+      if (time < least) {
+        least = time;
+        l.whole = whole;
+        l.share = even;
+      }
+    }
+    l.first = steps_before(l.whole);
     // every cluster has a share or a whole tile
     l.clusters = (int)(l.whole == 0 ? blocks(units, l.share) : l.whole < most ? l.whole : most);
   }
@@ -835,7 +859,7 @@ Layout layout(const GradCall& c) {
   l.flags = take((size_t)l.flag_words * 4);
   l.parts = take(l.share ? (size_t)l.clusters * 2 * PART_FLOATS * 4 : 0);
   const int most_steps = l.steps[0] > l.steps[1] ? l.steps[0] : l.steps[1];
-  constexpr int LONGEST = 24;
+  constexpr int LONGEST = 16;
   l.longest = c.out_type == LT_F32 && most_steps > LONGEST ? LONGEST : 2147483647;
   l.sums = take(l.longest < most_steps ? (size_t)l.clusters * 2 * PART_FLOATS * 4 : 0);
   l.total = at;
@@ -883,7 +907,7 @@ cudaError_t launch_backward(const GradCall& c, void* workspace, cudaStream_t str
     return e;
   }
   const Layout l = layout(c);
-  const bool a = l.tiles[0] > 0, b = l.tiles[1] > 0;
+  const bool a = l.at_a >= 0, b = l.at_b >= 0;
   if (!a && !b && !c.grad_bias) return cudaSuccess;
   if (l.tiles[0] + l.tiles[1] > 2147483647LL) return cudaErrorInvalidValue;
   unsigned char* const ws = static_cast<unsigned char*>(workspace);
@@ -950,14 +974,14 @@ cudaError_t launch_backward(const GradCall& c, void* workspace, cudaStream_t str
     return j;
   };
   if (a) {
-    Job& j = add(0, false, q.bw, l.nz, c.M);
+    Job& j = add(l.at_a, false, q.bw, l.nz, c.M);
     j.out[0] = c.grad_a;
     j.alpha[0] = q.sb ? nullptr : c.sb;
     j.div[0] = q.sa;
     j.div_stride = 1;
   }
   if (b) {
-    Job& j = add(1, true, q.aw, c.M, c.N);
+    Job& j = add(l.at_b, true, q.aw, c.M, c.N);
     j.out[0] = c.grad_b;
     j.out[1] = c.grad_b2;
     j.alpha[0] = j.alpha[1] = q.sa ? nullptr : c.sa;
