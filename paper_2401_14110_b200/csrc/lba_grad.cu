@@ -713,7 +713,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
           for (int i = 0; i < 8; ++i) mine[(c / 4 + i) * BM] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
           continue;
         }
-#pragma unroll 1
+#pragma unroll 2  // (two shares' sums on their way at a time)
         for (int o = first; o < share; ++o) {
           const float4* const theirs = reinterpret_cast<const float4*>(p.parts + (2 * (int64_t)o + rank) * PART_FLOATS) + row;
 #pragma unroll
@@ -809,29 +809,28 @@ Layout layout(const GradCall& c) {
     l.tiles[l.at_b] = halves * blocks(c.N, 2 * BM) * blocks(c.K, BN);
   }
   for (int i = 0; i < 2; ++i) l.units[i] = l.tiles[i] * l.steps[i];
-  // How many tiles stay whole: all, or some full rounds of the clusters, the others in equal shares.  In steps, a share costs beside its
-  // own what its begun sums take to be written and waited for, less where whole tiles follow, and the finishing cluster JOIN for each share that it
-  // adds: a tile must not be cut too often.  All tiles whole and like this, us: 256 x 8192 x 512 gated 91.5 and 55.3 (94 with 26 shares a
-  // tile), 8192 x 512 x 512 51.2 and 35.8, 6000 x 4096 x 1024 106.7 and 98.6, 4096 x 4096 x 1024 71.2 and 70.9.
-  constexpr int64_t CUT = 30, CUT_BEFORE_WHOLE = 14, JOIN = 5;
+  // How many tiles stay whole: all, or some, the others in equal shares.  In steps, a tile takes at least EPILOGUE (bringing it out hides
+  // behind the next one's steps), so shorter tiles are never divided (1 x 4096 x 4096 89 us otherwise, 45 like this).  A share costs beside
+  // its own steps what its begun sums take to be written and waited for, less where whole tiles follow, and the finishing cluster
+  // JOIN for each share that it adds: a tile must not be cut too often.  All tiles whole and like this, us: 256 x 8192 x 512 gated
+  // 91.5 and 55.3 (94 with 26 shares a tile), 8192 x 512 x 512 51.2 and 35.8, 6000 x 4096 x 1024 106.7 and 98.6, 4096 x 4096 x 1024
+  // 71.2 and 70.9.
+  constexpr int64_t EPILOGUE = 16, CUT = 30, CUT_BEFORE_WHOLE = 14, JOIN = 5;
   const int64_t all = l.tiles[0] + l.tiles[1], units = l.units[0] + l.units[1];
   const auto steps_of = [&](int64_t tile) { return (int64_t)(tile < l.tiles[0] ? l.steps[0] : l.steps[1]); };
   const auto steps_before = [&](int64_t tile) { return tile < l.tiles[0] ? tile * l.steps[0] : l.units[0] + (tile - l.tiles[0]) * l.steps[1]; };
   if (all > 0) {
-    // the busiest cluster, whose tile is the last of every round: rounds up to the last whole one
-    const auto load = [&](int64_t whole) {
-      int64_t sum = 0;
-      const int64_t rounds = blocks(whole, most), in_first = l.tiles[0] / most;  // full rounds of the first product
-      const int64_t first = rounds < in_first ? rounds : in_first;
-      sum = first * l.steps[0];
-      if (rounds > first) sum += (rounds - first - 1) * steps_of(all - 1) + steps_of(whole - 1);
-      return sum;
+    const auto cost_of = [&](int64_t tile) { return steps_of(tile) > EPILOGUE ? steps_of(tile) : EPILOGUE; };
+    const auto load = [&](int64_t whole) {  // of the busiest cluster, whose tile is the last of every round
+      if (whole == 0) return (int64_t)0;
+      const int64_t rounds = blocks(whole, most), in_first = (whole < l.tiles[0] ? whole : l.tiles[0]) / most;
+      return in_first * cost_of(0) + (rounds > in_first ? (rounds - in_first - 1) * cost_of(all - 1) + cost_of(whole - 1) : 0);
     };
+    const int64_t longest = steps_of(all - 1), fewest = l.steps[0] < EPILOGUE ? l.tiles[0] : 0;  // whole tiles, at least
     l.whole = all;
     int64_t least = load(all);
-    for (int64_t whole = all / most * most, tries = 0; whole >= 0 && tries < 8 && units < (1ll << 31); whole -= most, ++tries) {
-      if (whole == all) continue;
-      const int64_t longest = steps_of(all - 1);
+    const auto consider = [&](int64_t whole) {
+      if (whole < fewest || whole >= all || longest < EPILOGUE || units >= (1ll << 31)) return;
       int64_t even = blocks(units - steps_before(whole), most);
       while (even < 8 || even * even < JOIN * longest) ++even;
       const int64_t time = load(whole) + even + (whole > 0 ? CUT_BEFORE_WHOLE : CUT) + JOIN * blocks(longest, even);
@@ -840,10 +839,13 @@ Layout layout(const GradCall& c) {
         l.whole = whole;
         l.share = even;
       }
-    }
+    };
+    for (int64_t whole = all / most * most, tries = 0; whole >= 0 && tries < 8; whole -= most, ++tries) consider(whole);
+    consider(fewest);
     l.first = steps_before(l.whole);
     // every cluster has a share or a whole tile
-    l.clusters = (int)(l.whole == 0 ? blocks(units, l.share) : l.whole < most ? l.whole : most);
+    const int64_t shares = l.share ? blocks(units - l.first, l.share) : 0, wholes = l.whole < most ? l.whole : most;
+    l.clusters = (int)(shares > wholes ? shares : wholes);
   }
   l.flag_words = l.share ? 1 + 2 * l.clusters : 0;
   size_t at = 0;
