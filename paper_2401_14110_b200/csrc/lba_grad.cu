@@ -347,7 +347,7 @@ __global__ void __launch_bounds__(PREP_THREADS, GATED ? 3 : 4) grad_prepare_kern
 // starts: it only ever waits for clusters that run already or have ended, for the first thing that those do.
 constexpr int BM = 128, BN = 256, BL = 64, GRAD_THREADS = 320, OUT_THREADS = 256;  // of a CTA: rows, columns, step
 constexpr int X_BYTES = BM * BL * 2, STAGE = 2 * X_BYTES, STAGES = 5;
-constexpr int OUT_PITCH = 36;         // floats from row to row of a warp's 32 x 32 outputs in shared memory: 16-byte accesses on all banks
+constexpr int OUT_PITCH = 36;         // floats from row to row of a warp's outputs in shared memory: 128 bytes, 16-byte accesses on all banks
 constexpr size_t PRODUCT_SMEM = 1024 + (size_t)STAGE * STAGES + 256 + OUT_THREADS * OUT_PITCH * 4;
 constexpr int PART_FLOATS = BM * BN;  // a CTA's part of a begun tile
 
@@ -499,31 +499,50 @@ __device__ __forceinline__ void bias_sums(const ProductParams& p, float (*part)[
   }
 }
 
-// A warp's 32 x 32 outputs, a row per lane, to rows of `pitch` elements: through shared memory, W neighbouring columns of W rows at a
-// time.  (A row per lane straight to memory had each store touch 32 rows: with rows of 1203 floats, where nothing is aligned,
-// 1000 x 777 x 1203 took 42 us for its products.)
+// Outputs leave through shared memory, 128 bytes of a row at a time: a warp's 32 rows, a row per lane there, four rows per store of
+// the warp to memory.  (A row per lane straight to memory had each store touch 32 rows: with rows of 1203 floats, where nothing is
+// aligned, 1000 x 777 x 1203 took 42 us for its products.)
+template <typename T> constexpr int OUT_COLS = 128 / (int)sizeof(T);
+// 32 columns of this lane's row, from column 32 `half` of the 128 bytes on
 template <typename T>
-__device__ __forceinline__ void store_rows(void* base, int64_t at, int64_t pitch, int rows, int cols, const float* sm, int lane) {
-  T* const out = static_cast<T*>(base) + at;
-  if (pitch % 4 == 0 && (reinterpret_cast<uintptr_t>(out) & (4 * sizeof(T) - 1)) == 0 && cols == 32) {
-    const int c = lane % 8 * 4;
-    T* dst = out + (lane / 8) * pitch + c;
-    const float* src = sm + (lane / 8) * OUT_PITCH + c;
+__device__ __forceinline__ void stage_row(float* row, int half, const float (&v)[32], float alpha) {
+  if constexpr (sizeof(T) == 4) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      reinterpret_cast<float4*>(row)[i] = make_float4(v[4 * i] * alpha, v[4 * i + 1] * alpha, v[4 * i + 2] * alpha, v[4 * i + 3] * alpha);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      T t[8];
+#pragma unroll
+      for (int q = 0; q < 8; ++q) t[q] = from_f32<T>(v[8 * i + q] * alpha);
+      uint4 raw;
+      memcpy(&raw, t, 16);
+      reinterpret_cast<uint4*>(row)[4 * half + i] = raw;
+    }
+  }
+}
+// `rows` and `cols` of them to rows of `pitch` elements
+template <typename T>
+__device__ __forceinline__ void store_rows(T* out, int64_t pitch, int rows, int cols, const float* sm, int lane) {
+  if (pitch * sizeof(T) % 16 == 0 && (reinterpret_cast<uintptr_t>(out) & 15) == 0 && cols == OUT_COLS<T>) {
+    uint4* dst = reinterpret_cast<uint4*>(out + (lane / 8) * pitch) + lane % 8;
+    const uint4* src = reinterpret_cast<const uint4*>(sm + (lane / 8) * OUT_PITCH) + lane % 8;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-      const float4 f = *reinterpret_cast<const float4*>(src + i * 4 * OUT_PITCH);
-      const T t[4] = {from_f32<T>(f.x), from_f32<T>(f.y), from_f32<T>(f.z), from_f32<T>(f.w)};
-      typename Bytes<4 * sizeof(T)>::type raw;
-      memcpy(&raw, t, sizeof(raw));
-      if (i * 4 + lane / 8 < rows) *reinterpret_cast<decltype(raw)*>(dst) = raw;
-      dst += 4 * pitch;
+      const uint4 raw = src[i * OUT_PITCH];  // four rows on: 4 OUT_PITCH floats
+      if (i * 4 + lane / 8 < rows) *dst = raw;
+      dst += pitch * sizeof(T) / 4;
     }
-  } else if (lane < cols) {
-    T* dst = out + lane;
+  } else {
+#pragma unroll 1
+    for (int c = lane; c < cols; c += 32) {
+      T* dst = out + c;
 #pragma unroll 8
-    for (int i = 0; i < rows; ++i) {
-      *dst = from_f32<T>(sm[i * OUT_PITCH + lane]);
-      dst += pitch;
+      for (int i = 0; i < rows; ++i) {
+        *dst = reinterpret_cast<const T*>(sm + i * OUT_PITCH)[c];
+        dst += pitch;
+      }
     }
   }
 }
@@ -684,58 +703,59 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
       const int rows = j.rows - r0 < 32 ? (int)(j.rows - r0 > 0 ? j.rows - r0 : 0) : 32;
       const int64_t s0 = (int64_t)w.s * BN, pitch = j.cols;
       void* const out = j.out[w.half];
-      const int type = p.out_type;
+      const bool mine_too = lane < rows;  // (rows behind the last one are never read)
+      const auto add = [&](float (&v)[32], const float4* from, int c) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const float4 f = __ldcg(from + (c / 4 + i) * BM);
+          v[4 * i] += f.x;
+          v[4 * i + 1] += f.y;
+          v[4 * i + 2] += f.z;
+          v[4 * i + 3] += f.w;
+        }
+      };
+      const auto keep = [&](const float (&v)[32], float4* to, int c) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) __stcg(to + (c / 4 + i) * BM, make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
+      };
+      const auto bring_out = [&](auto type_tag) {
+        typedef decltype(type_tag) T;
 #pragma unroll 1
-      for (int c = c_first; c < c_first + BN / 2; c += 32) {
-        if (!begins && s0 + c >= pitch) break;  // (nothing of these is ever read)
-        uint32_t t[32];
-        float v[32];
-        tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + acc * BN + c, t);
+        for (int c0 = c_first; c0 < c_first + BN / 2; c0 += OUT_COLS<T>) {
+          if (s0 + c0 >= pitch) break;
 #pragma unroll
-        for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(t[i]);
-        if (w.goes_on) {
+          for (int half = 0; half < OUT_COLS<T> / 32; ++half) {
+            const int c = c0 + 32 * half;
+            uint32_t t[32];
+            float v[32];
+            tmem_ld32(tmem + ((uint32_t)(quarter * 32) << 16) + acc * BN + c, t);
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float4 f = __ldcg(sums + (c / 4 + i) * BM);
-            v[4 * i] += f.x;
-            v[4 * i + 1] += f.y;
-            v[4 * i + 2] += f.z;
-            v[4 * i + 3] += f.w;
-          }
-        }
-        if (!w.last) {  // (read by this thread alone)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) __stcg(sums + (c / 4 + i) * BM, make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]));
-          continue;
-        }
-        if (begins) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) mine[(c / 4 + i) * BM] = make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
-          continue;
-        }
+            for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(t[i]);
+            if (w.goes_on && mine_too) add(v, sums, c);
+            if (!w.last) {  // (read by this thread alone)
+              if (mine_too) keep(v, sums, c);
+            } else if (begins) {
+              if (mine_too) keep(v, mine, c);
+            } else {
+              if (mine_too) {
 #pragma unroll 2  // (two shares' sums on their way at a time)
-        for (int o = first; o < share; ++o) {
-          const float4* const theirs = reinterpret_cast<const float4*>(p.parts + (2 * (int64_t)o + rank) * PART_FLOATS) + row;
-#pragma unroll
-          for (int i = 0; i < 8; ++i) {
-            const float4 f = __ldcg(theirs + (c / 4 + i) * BM);
-            v[4 * i] += f.x;
-            v[4 * i + 1] += f.y;
-            v[4 * i + 2] += f.z;
-            v[4 * i + 3] += f.w;
+                for (int o = first; o < share; ++o) add(v, reinterpret_cast<const float4*>(p.parts + (2 * (int64_t)o + rank) * PART_FLOATS) + row, c);
+              }
+              stage_row<T>(sm + lane * OUT_PITCH, half, v, alpha);
+            }
+          }
+          if (w.last && !begins) {
+            __syncwarp();
+            const int64_t left = pitch - (s0 + c0);
+            store_rows(static_cast<T*>(out) + r0 * pitch + s0 + c0, pitch, rows, left < OUT_COLS<T> ? (int)left : OUT_COLS<T>, sm, lane);
+            __syncwarp();
           }
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          *reinterpret_cast<float4*>(sm + lane * OUT_PITCH + 4 * i) =
-              make_float4(v[4 * i] * alpha, v[4 * i + 1] * alpha, v[4 * i + 2] * alpha, v[4 * i + 3] * alpha);
-        __syncwarp();
-        const int cols = pitch - (s0 + c) < 32 ? (int)(pitch - (s0 + c)) : 32;
-        const int64_t at = r0 * pitch + s0 + c;
-        if (type == LT_F32) store_rows<float>(out, at, pitch, rows, cols, sm, lane);
-        else if (type == LT_BF16) store_rows<bf16>(out, at, pitch, rows, cols, sm, lane);
-        else store_rows<__half>(out, at, pitch, rows, cols, sm, lane);
-        __syncwarp();
+      };
+      if (rows > 0) {
+        if (p.out_type == LT_F32) bring_out(float());
+        else if (p.out_type == LT_BF16) bring_out(bf16());
+        else bring_out(__half());
       }
       asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
       __syncwarp();
