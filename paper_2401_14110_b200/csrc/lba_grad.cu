@@ -9,8 +9,10 @@
 // gradients (a rounding of 2^-9 beside the result's own), two with binary16 ones (2^-15 at most), three with binary32 ones (dz exactly); fewer
 // where dz itself has no more bits (see pieces()).  Every piece costs one more pass of the matrix instruction.
 //
-// Scales that differ by row or column belong to the summed index of one of the products: dz is multiplied by both before it is
-// rounded, and the other product divides its rows by the one that it does not want.  So both read the same pieces.
+// Scales that differ by row or column belong to the summed index of one of the products: dz is multiplied by both scales' fractions
+// in [1, 2) before it is rounded, and the other product divides its rows by the one that it does not want.  So both read the same pieces.
+// The powers of two go into the codes' bfloat16 forms, which stay exact: dz keeps its range (the scale of a row of zeros is often the
+// smallest normal number, whose product with dz would have no bits left), and a scale of 0 gives zeros.
 //
 // Two launches:
 //   grad_prepare_kernel   reads g and z once; writes the pieces of scaled dz, the sums of dz over blocks of rows (for the bias) and both
@@ -39,7 +41,7 @@ typedef __nv_bfloat16 bf16;
 struct PrepParams {
   const void *grad, *pre;
   const uint8_t *A, *B, *B2;
-  const float *sa, *sb, *sb2;  // factors of dz: by row; by column or by half (null: none)
+  const float *sa, *sb, *sb2;  // scales in dz and the codes: by row; by column or by half (null: none)
   const uint64_t* rng;
   bf16 *z, *aw, *bw;         // pieces of dz (planes of `plane` elements), codes of A and B
   float* partial;            // [row blocks][nz] sums of dz
@@ -98,6 +100,10 @@ __device__ __forceinline__ void widen8(const Raw8<T>& r, u64 (&v)[4]) {
   }
 }
 
+// a scale s > 0 as 2^e f, 1 <= f < 2 (0 and subnormal numbers: 0 f)
+__device__ __forceinline__ float fraction_of(float s) { return __uint_as_float((__float_as_uint(s) & 0x007FFFFFu) | 0x3F800000u); }
+__device__ __forceinline__ float power_of(float s) { return __uint_as_float(__float_as_uint(s) & 0x7F800000u); }
+
 // v as the sum of bfloat16 pieces, all but the last cut toward zero (which cannot overflow and leaves an exact remainder)
 __device__ __forceinline__ void store_pieces(bf16* dst, int64_t plane, int pieces, const u64 (&v)[4]) {
   uint4 out;
@@ -138,7 +144,7 @@ __device__ __forceinline__ void store_pieces(bf16* dst, int64_t plane, int piece
   *reinterpret_cast<uint4*>(dst + (pieces - 1) * plane) = out;
 }
 
-__device__ __forceinline__ void expand_codes(const PrepParams& p, const uint8_t* row, bf16* dst, int64_t k) {
+__device__ __forceinline__ void expand_codes(const PrepParams& p, const uint8_t* row, bf16* dst, int64_t k, u64 power) {
   uint4 out = make_uint4(0u, 0u, 0u, 0u);
   if (row) {
     __align__(8) uint8_t c[8];
@@ -160,7 +166,7 @@ __device__ __forceinline__ void expand_codes(const PrepParams& p, const uint8_t*
 #pragma unroll
       for (int e = 0; e < 2; ++e) {
         float lo, hi;
-        unpack2(v[e], lo, hi);
+        unpack2(mul2_rn(v[e], power), lo, hi);
         w[2 * q + e] = __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632);  // exact: the low halves are zero
       }
     }
@@ -184,18 +190,25 @@ __global__ void __launch_bounds__(PREP_THREADS, GATED ? 3 : 4) grad_prepare_kern
     const bool is_a = b < p.a_blocks;
     const int64_t row = (int64_t)(is_a ? b : b - p.a_blocks) * 8 + warp;
     const uint8_t* src = nullptr;
+    const float* scale = nullptr;
     bf16* dst;
     if (is_a) {
       if (row >= p.M) return;
       src = p.A + row * p.K;
+      if (p.sa) scale = p.sa + row;
       dst = p.aw + row * p.kp;
     } else {
       if (row >= p.nz) return;
-      if (row < p.N) src = p.B + row * p.K;
-      else if (row >= p.np && row < p.np + p.N) src = p.B2 + (row - p.np) * p.K;
+      const int64_t n = row < p.np ? row : row - p.np;
+      if (n < p.N) {
+        src = (row < p.np ? p.B : p.B2) + n * p.K;
+        scale = row < p.np ? p.sb : p.sb2;
+        if (scale && p.sb_per_col) scale += n;
+      }
       dst = p.bw + row * p.kp;  // (rows of the padding: zeros)
     }
-    for (int64_t k = lane * 8; k < p.kp; k += 256) expand_codes(p, src, dst, k);
+    const u64 power = both(scale ? power_of(*scale) : 1.0f);
+    for (int64_t k = lane * 8; k < p.kp; k += 256) expand_codes(p, src, dst, k, power);
     return;
   }
 
@@ -241,7 +254,9 @@ __global__ void __launch_bounds__(PREP_THREADS, GATED ? 3 : 4) grad_prepare_kern
       const float* const sb = h ? p.sb2 : p.sb;
 #pragma unroll
       for (int j = 0; j < 4; ++j)
-        scale[h][j] = !sb ? both(1.0f) : !p.sb_per_col ? both(sb[0]) : pack2(2 * j < valid ? sb[n + 2 * j] : 0.0f, 2 * j + 1 < valid ? sb[n + 2 * j + 1] : 0.0f);
+        scale[h][j] = !sb ? both(1.0f)
+                      : !p.sb_per_col ? both(fraction_of(sb[0]))
+                                      : pack2(2 * j < valid ? fraction_of(sb[n + 2 * j]) : 0.0f, 2 * j + 1 < valid ? fraction_of(sb[n + 2 * j + 1]) : 0.0f);
     }
     with_act(p.act, [&](auto act_tag) {
       constexpr int ACT = decltype(act_tag)::value;
@@ -286,7 +301,7 @@ __global__ void __launch_bounds__(PREP_THREADS, GATED ? 3 : 4) grad_prepare_kern
           }
         }
         // (the padding of a row: g is 0 there, z too, and every slope finite)
-        const u64 by = both(p.sa ? p.sa[m] : 1.0f);
+        const u64 by = both(p.sa ? fraction_of(p.sa[m]) : 1.0f);
 #pragma unroll
         for (int h = 0; h < HALVES; ++h) {
           u64 s[4];
@@ -339,12 +354,13 @@ __global__ void __launch_bounds__(PREP_THREADS, GATED ? 3 : 4) grad_prepare_kern
 // four-dimensional boxes and no arithmetic but the coordinates' (three copies and 64-bit divisions in a lane chosen by its number had
 // taken 725).
 //
-// Clusters take whole tiles in turn, side by side in l, so that what one fetches its neighbours find in L2.  The tiles of a last, broken
-// round are divided instead: their steps of 64 l stand in one row, cut into equal shares, one per cluster.  A tile that a border
-// cuts is begun by lower shares, which leave binary32 sums in the workspace, and finished by the share with its last step, which
-// adds them in order.  (`longest`: binary32 results of long sums would lose precision to the matrix instructions, which cut a sum at each
-// addition: 8192 terms were off by 2.8e-6, where 1000 are by 8e-7.  Their tiles are formed in stretches, added up in binary32.)  A cluster walks its share from the end and before its whole tiles, and takes the share's number from a counter when it
-// starts: it only ever waits for clusters that run already or have ended, for the first thing that those do.
+// Clusters take whole tiles in turn, side by side in l, so that what one fetches its neighbours find in L2.  The last tiles of the list
+// are divided where that saves time (layout() says when): their steps of 64 l stand in one row, cut into equal shares, one per
+// cluster.  A tile that a border cuts is begun by lower shares, which leave binary32 sums in the workspace, and finished by the share with
+// its last step, which adds them in order.  A cluster walks its share from the end and before its whole tiles, and takes the share's number
+// from a counter when it starts: it only ever waits for clusters that run already or have ended, for the first thing that those do.
+// `longest`: binary32 results of long sums would lose precision to the matrix instructions, which cut a sum at each addition (8192
+// terms were off by 2.8e-6, where 1000 are by 8e-7).  Their tiles are formed in stretches, added up in binary32.
 constexpr int BM = 128, BN = 256, BL = 64, GRAD_THREADS = 320, OUT_THREADS = 256;  // of a CTA: rows, columns, step
 constexpr int X_BYTES = BM * BL * 2, STAGE = 2 * X_BYTES, STAGES = 5;
 constexpr int OUT_PITCH = 36;         // floats from row to row of a warp's outputs in shared memory: 128 bytes, 16-byte accesses on all banks
@@ -358,7 +374,7 @@ struct Job {
   int x_mn, pieces, blocks, steps;  // blocks of l, and these times pieces
   int div_stride;
   void* out[2];
-  const float *alpha[2], *div[2];  // factors of a half, divisors of its rows (or null)
+  const float *alpha[2], *div[2];  // factors of a half, scales whose fractions divide its rows (or null)
 };
 struct ProductParams {
   CUtensorMap x[2], y[2];
@@ -694,7 +710,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
       }
       const int64_t r0 = (int64_t)w.r * (2 * BM) + rank * BM + quarter * 32, r = r0 + lane;
       float alpha = p.factor * (j.alpha[w.half] ? *j.alpha[w.half] : 1.0f);
-      if (j.div[w.half] && r < j.rows) alpha = __fdiv_rn(alpha, j.div[w.half][r * j.div_stride]);
+      if (j.div[w.half] && r < j.rows) alpha = __fdiv_rn(alpha, fraction_of(j.div[w.half][r * j.div_stride]));
       mbar_wait(acc_done + 8 * acc, phase, dead);
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
       if (*dead) alpha = __uint_as_float(0x7FC00000u);

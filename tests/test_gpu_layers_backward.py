@@ -160,6 +160,33 @@ def test_empty_sums_are_zero():
         assert torch.equal(gc, torch.full((N,), float(M), device=DEV))
 
 
+@pytest.mark.parametrize("out", [F32, BF16, F16])
+def test_scales_of_empty_rows(out):
+    # rows and channels of zeros are quantised to the smallest normal scale; 2^-90 is as far from 1 as a user's may be, and scales of 0 stand
+    # for rows of zeros.  The codes' gradients do not depend on their own scales, however small
+    M, N, K = 70, 136, 96
+    A, sa, B, sb, B2, sb2 = case(M, N, K, 6, 2, per_row=True)
+    tiny = torch.finfo(F32).tiny
+    for s, codes, stride in ((sa, A, 9), (sb, B, 7), (sb2, B2, 5)):
+        s[::stride], s[1::2 * stride], s[2::2 * stride], s[3::4 * stride] = tiny, 0.0, 1.2345 * 2.0 ** -90, 1.2345 * 2.0 ** 6
+        codes[::stride] = 0
+    g = synth.gaussian((M, N), 1, 2.0 ** -8).to(BF16).to(DEV)
+    pre = synth.gaussian((2, M, N), 2).to(BF16).to(DEV)
+    dz = g.cpu().double()
+    for sx in (sa, torch.ones(1, device=DEV)):
+        ga, gb, _ = lba.lba_linear_backward(g, A, B, sx, sb, PROD, grad_dtype=out)
+        close(ga, dz, dz.abs() * 2.0 ** -21, dense(B, sb), rows, "a")
+        close(gb, dz, dz.abs() * 2.0 ** -21, dense(A, sx), cols, "b")
+        assert float(gb[::7].float().abs().max()) > 0
+    d1, d2 = dz * pre[1].cpu().double() * slope(pre[0].cpu(), "silu"), dz * act(pre[0].cpu(), "silu")
+    s1, s2 = (dz * pre[1].cpu().double()).abs() * SLOPE_ERR + d1.abs() * 2.0 ** -21, (dz * pre[0].cpu().double()).abs() * ACT_ERR + d2.abs() * 2.0 ** -21
+    for p, q in ((sb, sb2), (torch.full((1,), tiny, device=DEV), torch.full((1,), 0.75, device=DEV))):
+        ga, g1, g2, _, _ = lba.lba_gated_backward(g, A, B, B2, sa, p, q, PROD, pre, "silu", out)
+        close(ga, torch.cat([d1, d2], 1), torch.cat([s1, s2], 1), torch.cat([dense(B, p), dense(B2, q)]), rows, "a")
+        close(g1, d1, s1, dense(A, sa), cols, "gate")
+        close(g2, d2, s2, dense(A, sa), cols, "up")
+
+
 def test_special_values():
     # a NaN or an infinity reaches the sums it belongs to and no other; dropped elements reach none
     A, sa, B, sb = case(64, 64, 64, 5)
