@@ -928,7 +928,7 @@ cudaError_t launch_prepare(const PrepParams& q, const GradCall& c, unsigned bloc
 
 }  // namespace
 
-size_t backward_workspace(const GradCall& c) { return c.M > 0 && c.N > 0 ? layout(c).total : 0; }
+size_t backward_workspace(const GradCall& c) { return c.M > 0 && c.N > 0 && !few_rows(c, pieces(c)) ? layout(c).total : 0; }
 
 cudaError_t launch_backward(const GradCall& c, void* workspace, cudaStream_t stream) {
   const size_t size = c.out_type == LT_F32 ? 4 : 2;
@@ -944,6 +944,7 @@ cudaError_t launch_backward(const GradCall& c, void* workspace, cudaStream_t str
     zero(c.grad_bias2, c.N * 4);
     return e;
   }
+  if (few_rows(c, pieces(c))) return launch_backward_few(c, pieces(c), stream);
   const Layout l = layout(c);
   const bool a = l.at_a >= 0, b = l.at_b >= 0;
   if (!a && !b && !c.grad_bias) return cudaSuccess;

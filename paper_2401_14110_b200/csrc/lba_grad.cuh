@@ -1,4 +1,4 @@
-// Backward pass of the layers (lba_layer.cuh): host interface of lba_grad.cu.
+// Backward pass of the layers (lba_layer.cuh): host interface of lba_grad.cu and lba_grad_few.cu.
 #pragma once
 #include <cstddef>
 #include <cstdint>
@@ -22,5 +22,8 @@ struct GradCall {
 size_t backward_workspace(const GradCall& c);
 // M, N below 2^31 and K at most 2^31 - 1; workspace 256-byte aligned, backward_workspace(c) bytes
 cudaError_t launch_backward(const GradCall& c, void* workspace, cudaStream_t stream);
+// lba_grad_few.cu: the same for few rows, where few_rows() holds; needs no workspace
+bool few_rows(const GradCall& c, int pieces);
+cudaError_t launch_backward_few(const GradCall& c, int pieces, cudaStream_t stream);
 
 }  // namespace lba

@@ -52,7 +52,8 @@ def check_bias(got, dz, slack):
     assert bool(((got.cpu().double() - dz.sum(0)).abs() <= tol).all())
 
 
-SHAPES = [(1, 1, 1), (1, 130, 65), (2, 16, 16), (33, 40, 72), (64, 64, 64), (129, 257, 130), (300, 65, 511), (70, 520, 264)]
+SHAPES = [(1, 1, 1), (1, 130, 65), (2, 16, 16), (33, 40, 72), (64, 64, 64), (129, 257, 130), (300, 65, 511), (70, 520, 264),
+          (5, 1040, 48), (16, 300, 515), (17, 140, 1030), (32, 129, 144), (31, 1100, 70), (49, 260, 527)]
 
 
 @pytest.mark.parametrize("out", [F32, BF16, F16])
