@@ -552,8 +552,14 @@ size_t dz_bytes(const GradCall& c, int pieces) {
 
 }  // namespace
 
+// Every 16 rows bring the weights, and every 128 columns the elementwise work, once more, so the product of both is what this kernel's
+// time grows with.  Both gradients in bfloat16, us here and in two launches: 1 x 512 x 512 5.2 and 9.6, 16 x 8192 x 8192 104 and 135,
+// 32 x 2048 x 2048 17.7 and 18.9, 32 x 1024 x 4096 21.5 and 17.0, 48 x 4096 x 1024 22.3 and 27.8, 64 x 1024 x 1024 14.9 and 12.6,
+// 64 x 4096 x 1024 26.0 and 28.3, 64 x 4096 x 4096 82 and 45.
 bool few_rows(const GradCall& c, int pieces) {
   if (c.M <= 0 || c.M > FEW_ROWS || c.N <= 0 || c.K <= 0) return false;
+  const int64_t tiles = (c.M + 15) / 16;
+  if (tiles > 1 && tiles * c.K > 4096) return false;
   return c.grad_a ? dz_bytes(c, pieces) <= MOST_SMEM : c.grad_b != nullptr;
 }
 

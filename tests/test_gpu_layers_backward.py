@@ -53,7 +53,8 @@ def check_bias(got, dz, slack):
 
 
 SHAPES = [(1, 1, 1), (1, 130, 65), (2, 16, 16), (33, 40, 72), (64, 64, 64), (129, 257, 130), (300, 65, 511), (70, 520, 264),
-          (5, 1040, 48), (16, 300, 515), (17, 140, 1030), (32, 129, 144), (31, 1100, 70), (49, 260, 527)]
+          (5, 1040, 48), (16, 300, 515), (17, 140, 1030), (32, 129, 144), (31, 1100, 70), (49, 260, 527),
+          (50, 70, 1200)]
 
 
 @pytest.mark.parametrize("out", [F32, BF16, F16])
@@ -100,7 +101,7 @@ def test_gated_against_64_bits(name, out):
         check_bias(c2, d2, s2)
 
 
-@pytest.mark.parametrize("M,N,K", [(1500, 700, 1000), (5000, 256, 260), (260, 4000, 300), (2, 3000, 1100)])
+@pytest.mark.parametrize("M,N,K", [(1500, 700, 1000), (5000, 256, 260), (260, 4000, 300), (2, 3000, 1100), (20, 9000, 64), (3, 20000, 48)])
 def test_many_tiles(M, N, K):
     # several tiles per multiprocessor, long sums of either product
     A, sa, B, sb, B2, sb2 = case(M, N, K, M, 2)
@@ -149,6 +150,28 @@ def test_repeats_give_the_same_bits_and_subsets_the_same_values():
                         assert got[j] is None
                     else:
                         assert bool(((got[j] - full[j]).abs() <= 2.0 ** -7 * full[j].abs() + 2.0 ** -16 * full[j].abs().max()).all())
+
+
+def test_any_alignment():
+    # tensors that begin at any element give what their aligned copies give, up to the order of sums
+    def shifted(t, by):
+        room = torch.empty(t.numel() + by, dtype=t.dtype, device=DEV)
+        room[by:] = t.reshape(-1)
+        return room[by:].view(t.shape)
+
+    for M, N, K in [(5, 136, 80), (70, 136, 80), (20, 64, 1040)]:
+        A, sa, B, sb, B2, sb2 = case(M, N, K, 8, 2, per_row=True)
+        g, pre = synth.gaussian((M, N), 1).to(BF16).to(DEV), synth.gaussian((2, M, N), 2).to(DEV)
+        for by in (1, 3):
+            s = [shifted(t, by) for t in (g, A, B, B2, sa, sb, sb2, pre)]
+            got = lba.lba_gated_backward(*s[:7], PROD, s[7], "gelu", F32)
+            want = lba.lba_gated_backward(g, A, B, B2, sa, sb, sb2, PROD, pre, "gelu", F32)
+            for x, y in zip(got, want):
+                assert bool(((x - y).abs() <= 2.0 ** -16 * y.abs().max()).all())
+            got = lba.lba_linear_backward(s[0], s[1], s[2], s[4], s[5], PROD, s[7][1], "silu", grad_dtype=F16)
+            want = lba.lba_linear_backward(g, A, B, sa, sb, PROD, pre[1], "silu", grad_dtype=F16)
+            for x, y in zip(got, want):
+                assert bool(((x - y).abs() <= 2.0 ** -10 * y.abs() + 2.0 ** -14 * y.abs().max()).all())
 
 
 def test_empty_sums_are_zero():

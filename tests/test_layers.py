@@ -126,7 +126,7 @@ def test_refused_backward_arguments():
     assert _backward(how=None) == -1 and _backward(how=h, grad=None) == -1 and _backward(how=h, a=None) == -1 and _backward(how=h, sa=None) == -1
     assert _backward(M=-1, how=h) == -2 and _backward(N=1 << 30, how=h) == -2 and _backward(M=1 << 31, how=h) == -2
     assert _backward(how=h, sa_len=3) == -5 and _backward(how=h, sb_len=3) == -5
-    assert _backward(how=h, ws=None) == -7 and _backward(how=h, ws=C.c_void_p(128)) == -7 and _backward(how=h, ws_bytes=256) == -7
+    assert _backward(M=100, how=h, ws=None) == -7 and _backward(M=100, how=h, ws=C.c_void_p(128)) == -7 and _backward(M=100, how=h, ws_bytes=256) == -7
     assert _gated_backward(_how(dropout=0.5, rng=256)) == -9 and _gated_backward(_how(preact=None)) == -1
     assert _gated_backward(h, grads=(256, None)) == -1 and _gated_backward(h, biases=(None, 256)) == -1 and _gated_backward(h, up=None) == -1
 
@@ -136,4 +136,5 @@ def test_backward_workspace_grows_with_what_is_asked():
     full = size()
     assert 0 < size(needs=(False, False, True)) < size(needs=(True, False, False)) < full
     assert size(sb=50) == full and size(dtype=torch.float16) > full and size(gated=True) > full
+    assert lba.backward_workspace_bytes(16, 50, 70, 1, 1, torch.bfloat16, activation="gelu") == 0  # few rows need none
     assert size(needs=(False, False, False)) == 0 and lba.backward_workspace_bytes(0, 50, 70, 1, 1, torch.bfloat16) == 0
