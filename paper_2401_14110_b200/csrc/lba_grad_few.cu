@@ -71,13 +71,15 @@ __device__ __forceinline__ void load8(Raw& r, const void* base, int type, int64_
 }
 __device__ __forceinline__ void widen(const Raw& r, int type, u64 (&v)[4]) {
   const uint32_t* const w = &r.v[0].x;
+  if (type == LT_BF16) {
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
-    if (type == LT_F32) {
-      v[j] = pack2u(w[2 * j], w[2 * j + 1]);
-    } else if (type == LT_BF16) {
-      v[j] = pack2u(w[j] << 16, w[j] & 0xFFFF0000u);
-    } else {
+    for (int j = 0; j < 4; ++j) v[j] = pack2u(w[j] << 16, w[j] & 0xFFFF0000u);
+  } else if (type == LT_F32) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = pack2u(w[2 * j], w[2 * j + 1]);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
       const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&w[j]));
       v[j] = pack2(f.x, f.y);
     }
@@ -243,21 +245,24 @@ __device__ __forceinline__ float4 peer_float4(uint32_t addr, int rank) {
 
 // dz of `count` blocks, rows m from m0 on, into shared memory: pieces of it times the scales of n or m, or (for the bias) itself
 __device__ __forceinline__ void put_blocks(const FewParams& p, Kind kind, int block, int count, int m0, int rows, int pitch, int plane, unsigned char* dst) {
-  const int across = count * (BLOCK / 8), all = rows * across;
-  int o = threadIdx.x, row = o / across, at = o - row * across;
-  if (o >= all) return;
-  Inputs in = fetch(p, kind, block + at / (BLOCK / 8), m0 + row, at % (BLOCK / 8));
+  // (sixteen threads side by side; the others go down the rows of block after block, without a division per step)
+  const int n8 = threadIdx.x % (BLOCK / 8), first = threadIdx.x / (BLOCK / 8), by_blocks = 16 / rows, by_rows = 16 - by_blocks * rows;
+  static_assert(FEW_THREADS / (BLOCK / 8) == 16, "steps of 16 rows");
+  int b = first / rows, row = first - b * rows;
+  if (b >= count) return;
+  Inputs in = fetch(p, kind, block + b, m0 + row, n8);
 #pragma unroll 1
   while (true) {
-    const int here = row, col = at;
-    const bool more = o + FEW_THREADS < all;
-    Inputs next = in;
-    if (more) {
-      o += FEW_THREADS;
-      row = o / across;
-      at = o - row * across;
-      next = fetch(p, kind, block + at / (BLOCK / 8), m0 + row, at % (BLOCK / 8));
+    const int here = row, col = b * (BLOCK / 8) + n8;
+    b += by_blocks;
+    row += by_rows;
+    if (row >= rows) {
+      row -= rows;
+      ++b;
     }
+    const bool more = b < count;
+    Inputs next = in;
+    if (more) next = fetch(p, kind, block + b, m0 + row, n8);
     u64 d[4] = {0ull, 0ull, 0ull, 0ull};
     if (in.valid) {
       slopes(p, in, d);
@@ -475,6 +480,8 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) grad_few_kernel(const __grid_c
 #pragma unroll
     for (int i = 0; i < 4; ++i) now[i] = next[i];
     fetch_codes(c + 1);
+    uint32_t only[4];
+    load_fragment<false>(from, only);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const uint32_t r0 = (&now[0].x)[q], r1 = (&now[1].x)[q], r2 = (&now[2].x)[q], r3 = (&now[3].x)[q];
@@ -482,12 +489,17 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) grad_few_kernel(const __grid_c
                               decode_rows<M4E3, 3>(r0, r1)};
       const uint32_t b1[4] = {decode_rows<M4E3, 0>(r2, r3), decode_rows<M4E3, 1>(r2, r3), decode_rows<M4E3, 2>(r2, r3),
                               decode_rows<M4E3, 3>(r2, r3)};
-#pragma unroll 1
-      for (int piece = p.pieces - 1; piece >= 0; --piece) {
-        uint32_t a[4];
-        load_fragment<false>(from + 2 * piece * plane, a);
+      if (p.pieces == 1) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) mma16816(acc[4 * q + j], a, b0[j], b1[j]);
+        for (int j = 0; j < 4; ++j) mma16816(acc[4 * q + j], only, b0[j], b1[j]);
+      } else {
+#pragma unroll 1
+        for (int piece = p.pieces - 1; piece >= 0; --piece) {
+          uint32_t a[4];
+          load_fragment<false>(from + 2 * piece * plane, a);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) mma16816(acc[4 * q + j], a, b0[j], b1[j]);
+        }
       }
     }
   }
@@ -553,9 +565,9 @@ size_t dz_bytes(const GradCall& c, int pieces) {
 }  // namespace
 
 // Every 16 rows bring the weights, and every 128 columns the elementwise work, once more, so the product of both is what this kernel's
-// time grows with.  Both gradients in bfloat16, us here and in two launches: 1 x 512 x 512 5.2 and 9.6, 16 x 8192 x 8192 104 and 135,
-// 32 x 2048 x 2048 17.7 and 18.9, 32 x 1024 x 4096 21.5 and 17.0, 48 x 4096 x 1024 22.3 and 27.8, 64 x 1024 x 1024 14.9 and 12.6,
-// 64 x 4096 x 1024 26.0 and 28.3, 64 x 4096 x 4096 82 and 45.
+// time grows with.  Both gradients in bfloat16, us here and in two launches: 1 x 512 x 512 5.1 and 9.6, 16 x 8192 x 8192 102 and 135,
+// 32 x 2048 x 2048 17.2 and 18.9, 32 x 1024 x 4096 21.5 and 17.0, 48 x 4096 x 1024 21.8 and 27.8, 64 x 1024 x 1024 14.6 and 12.6,
+// 64 x 4096 x 1024 26.1 and 28.3, 64 x 4096 x 4096 82 and 45.
 bool few_rows(const GradCall& c, int pieces) {
   if (c.M <= 0 || c.M > FEW_ROWS || c.N <= 0 || c.K <= 0) return false;
   const int64_t tiles = (c.M + 15) / 16;
@@ -613,7 +625,8 @@ cudaError_t launch_backward_few(const GradCall& c, int pieces, cudaStream_t stre
   if (b_ctas) wants(tiles * 32 * ((size_t)pitch_of(BLOCK * (int)each) * pieces + pitch_of(width)) + FEW_THREADS / 32 * 16 * OUT_PITCH * 4);
   if (c.grad_bias) wants((size_t)tiles * 16 * RED_PITCH * 4);
   const auto launch = [&](auto kernel) {
-    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+    // (the same limit in every call: another thread's may lie between these two lines)
+    const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)MOST_SMEM);
     return e != cudaSuccess ? e : launch_after(kernel, dim3((unsigned)ctas), FEW_THREADS, smem, stream, p, CLUSTER);
   };
   if (c.in_m4e3) return k_whole ? launch(grad_few_kernel<true, true>) : launch(grad_few_kernel<true, false>);
