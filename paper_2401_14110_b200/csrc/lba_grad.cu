@@ -14,7 +14,7 @@
 // The powers of two go into the codes' bfloat16 forms, which stay exact: dz keeps its range (the scale of a row of zeros is often the
 // smallest normal number, whose product with dz would have no bits left), and a scale of 0 gives zeros.
 //
-// Two launches:
+// Two launches (few rows: one, in lba_grad_few.cu):
 //   grad_prepare_kernel   reads g and z once; writes the pieces of scaled dz, the sums of dz over blocks of rows (for the bias) and both
 //                         operands' codes as bfloat16.  Bound by memory.
 //   grad_product_kernel   both products as one list of 256 x 256 tiles, a pair of CTAs each (tcgen05, TMA), cut into equal shares of work;
