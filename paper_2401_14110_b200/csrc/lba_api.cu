@@ -593,9 +593,11 @@ bool aligned16(const void* ptr) { return (reinterpret_cast<uintptr_t>(ptr) & 15)
 RowsShape rows_shape(const LinearProblem& p, const Plan& pl, int load) {
   const bool packed = pl.qm == QM_FLOOR_FAST || pl.qm == QM_FLOOR_FULL || (pl.qm == QM_RNE_FULL && pl.rne_packed);
   const int forced = g_tile_override.load(std::memory_order_relaxed);
-  if (pl.fixed || !packed || pl.ord != ORD_CHUNK16 || load != LD_GEMM_VEC || p.M > ROWS_MAX || (forced >= 0 && forced != TILE_ROWS)) return {};
+  if (pl.fixed || !packed || pl.ord != ORD_CHUNK16 || load != LD_GEMM_VEC || p.M > ROWS_MAX || p.N > 2147483647LL ||
+      (forced >= 0 && forced != TILE_ROWS))
+    return {};
   const int64_t total = (p.N + 1) / 2;
-  const int rounds = (int)((p.K / BK + ROWS_CHUNKS - 1) / ROWS_CHUNKS), M = (int)p.M, room = 227 * 1024;
+  const int rounds = (int)((p.K / BK + ROWS_CHUNKS - 1) / ROWS_CHUNKS), M = (int)p.M, room = ROWS_ROOM;
   for (int64_t waves = 1; waves <= total; ++waves) {
     if (M > 12 && waves > 2) break;
     const int64_t pairs = (total + waves * sm_count() - 1) / (waves * sm_count());

@@ -6,7 +6,7 @@
 //
 // Nothing rounds between additions here, so the products run on the tensor cores.  Codes of either operand format have at most
 // five significant bits: bfloat16 holds them exactly, and only dz is rounded.  One bfloat16 piece of it goes with bfloat16
-// gradients (a rounding of 2^-9 beside the result's own), two with binary16 ones (2^-15 at most), three with binary32 ones (dz exactly); fewer
+// gradients (a rounding of 2^-9 beside the result's own; two where dz is small), two with binary16 ones (2^-15 at most), three with binary32 ones (dz exactly); fewer
 // where dz itself has no more bits (see pieces()).  Every piece costs one more pass of the matrix instruction.
 //
 // Scales that differ by row or column belong to the summed index of one of the products: dz is multiplied by both scales' fractions
@@ -798,11 +798,15 @@ int64_t up(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
 // bfloat16 pieces that dz takes beside a result of the given type; dz that is g itself or zero has no more bits than g, and a
-// common scale is applied to the finished product
+// common scale is applied to the finished product.  Two beside bfloat16 where dz has few elements: one piece is off by as much as the
+// result's own rounding, and only many of them even that out (1 x 50: results off by 1.6 times their rounding, else by 1.4 times); such
+// products wait for their launches anyway
 int pieces(const GradCall& c) {
+  constexpr int64_t FEW_ELEMENTS = 2048;
   const auto of = [](int type) { return type == LT_BF16 ? 1 : type == LT_F16 ? 2 : 3; };
   const bool plain = !c.gated && (c.act == ACT_NONE || c.act == ACT_RELU) && !c.sa_per_row && !c.sb_per_col;
-  return plain && of(c.grad_type) < of(c.out_type) ? of(c.grad_type) : of(c.out_type);
+  const int wanted = c.out_type == LT_BF16 && c.M * c.N <= FEW_ELEMENTS ? 2 : of(c.out_type);
+  return plain && of(c.grad_type) < wanted ? of(c.grad_type) : wanted;
 }
 
 int clusters_of_the_device() {

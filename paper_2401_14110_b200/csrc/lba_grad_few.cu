@@ -5,7 +5,7 @@
 // 4096 x 4096, bfloat16: 44 us in two launches).  Here a weight goes from memory to a register, becomes bfloat16 there and is an
 // operand of mma.m16n8k16, whose 16 rows are the activations'; dz is formed again by every CTA for the block of columns that it
 // needs, M elements per column, and kept in shared memory.  Three kinds of CTAs, by their number:
-//   A  grad_a: 16 rows m and 128 columns k; the eight CTAs of a cluster and their eight warps share out the sum over n, 16 at a time and
+//   A  grad_a: 16 rows m and 128 columns k, several times; the eight CTAs of a cluster and their eight warps share out the sum over n, 16 at a time and
 //      warp; the 64 sums are added in a fixed order, through shared memory and then through the cluster's.
 //   B  grad_b: 128 to 1024 rows n and 64 to 512 columns k, the activations' codes brought to bfloat16 in shared memory.
 //   C  grad_bias: 128 n.
@@ -23,10 +23,10 @@ namespace {
 typedef __nv_bfloat16 bf16;
 constexpr int FEW_THREADS = 256, BLOCK = 128, CLUSTER = 8, MOST_BLOCKS = 8;  // columns n of dz: in blocks; B: up to MOST_BLOCKS times tiles in a CTA
 constexpr int RED_PITCH = 132;                // floats from row to row of a warp's sums: 16-byte accesses on all banks
-constexpr int RED_FLOATS = 8 * 16 * RED_PITCH;
+constexpr int RED_FLOATS = 8 * 8 * RED_PITCH;  // eight warps' sums of eight rows
 constexpr int OUT_PITCH = 36;                 // of a warp's 16 x 32 outputs
 constexpr int FEW_ROWS = 64;
-constexpr size_t MOST_SMEM = 220 * 1024;
+constexpr size_t MOST_SMEM = 220 * 1024, SUMS_BYTES = (RED_FLOATS + 16 * 128) * 4;
 enum Kind { GRAD_A, GRAD_B, GRAD_BIAS };
 // elements from row to row of dz or of activations in shared memory: an odd number of 16-byte words
 __host__ __device__ constexpr int pitch_of(int cols) { return cols + 8; }
@@ -45,6 +45,7 @@ struct FewParams {
   float factor;
   int blocks, all, tiles;              // blocks of n in a half, in all; tiles of 16 rows
   int a_ctas, b_ctas, a_each, b_each;  // CTAs; blocks of n of a CTA (A: of a cluster's)
+  int a_times, red_at;                 // A: groups of 128 columns of a CTA, one after the other; where the warps' sums lie (bytes)
   int b_width, b_cols;                 // B: columns k of a CTA, CTAs side by side
   int n_whole;                         // eight elements of a row always lie whole at a 16-byte boundary
 };
@@ -365,7 +366,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) grad_few_kernel(const __grid_c
   int64_t k0 = 0;
   if (kind == GRAD_A) {
     const int cluster = blockIdx.x / CLUSTER, cols = p.a_ctas / (CLUSTER * p.tiles), tile = cluster / cols;
-    k0 = (int64_t)(cluster - tile * cols) * 128;
+    k0 = (int64_t)(cluster - tile * cols) * (128 * p.a_times);
     m0 = tile * 16;
     tiles = 1;
     c = rank * p.a_each;
@@ -443,7 +444,7 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) grad_few_kernel(const __grid_c
   }
 
   uint4 next[4];
-  const auto fetch_codes = [&](int block) {
+  const auto fetch_codes = [&](int block, int64_t k0) {
     const int half = block >= p.blocks;
     const int64_t n0 = (int64_t)(block - (half ? p.blocks : 0)) * BLOCK + 16 * warp + 2 * t;
     const uint8_t* const from = p.B[half] + n0 * p.K;
@@ -464,96 +465,102 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) grad_few_kernel(const __grid_c
       }
     }
   };
-  fetch_codes(c);
+  fetch_codes(c, k0);
   if (c < end) put_blocks(p, kind, c, end - c, m0, rows, pitch, plane, smem);  // (rows behind the last one: anything, they meet no other)
   __syncthreads();
-  float acc[16][4];
-#pragma unroll
-  for (int j = 0; j < 16; ++j)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) acc[j][e] = 0.0f;
-  // matrices of a fragment: rows m 0-7 and 8-15 at n 0-7, the same at n 8-15
-  uint32_t from = smem_u32(z) + 2 * (((lane & 7) + (lane & 8)) * pitch + 16 * warp + (lane >> 4) * 8);
+  float* const red = reinterpret_cast<float*>(smem + p.red_at);  // (in dz's place where no other group reads that)
+  float* const sums = red + RED_FLOATS;  // [16][128]
+  const float alpha = p.factor * (p.alpha_a ? *p.alpha_a : 1.0f);
 #pragma unroll 1
-  for (; c < end; ++c, from += 2 * BLOCK) {
-    uint4 now[4];
+  for (const int64_t k_end = k0 + 128 * p.a_times < p.K ? k0 + 128 * p.a_times : p.K; k0 < k_end; k0 += 128) {
+    float acc[16][4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) now[i] = next[i];
-    fetch_codes(c + 1);
-    uint32_t only[4];
-    load_fragment<false>(from, only);
+    for (int j = 0; j < 16; ++j)
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const uint32_t r0 = (&now[0].x)[q], r1 = (&now[1].x)[q], r2 = (&now[2].x)[q], r3 = (&now[3].x)[q];
-      const uint32_t b0[4] = {decode_rows<M4E3, 0>(r0, r1), decode_rows<M4E3, 1>(r0, r1), decode_rows<M4E3, 2>(r0, r1),
-                              decode_rows<M4E3, 3>(r0, r1)};
-      const uint32_t b1[4] = {decode_rows<M4E3, 0>(r2, r3), decode_rows<M4E3, 1>(r2, r3), decode_rows<M4E3, 2>(r2, r3),
-                              decode_rows<M4E3, 3>(r2, r3)};
-      if (p.pieces == 1) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) mma16816(acc[4 * q + j], only, b0[j], b1[j]);
-      } else {
+      for (int e = 0; e < 4; ++e) acc[j][e] = 0.0f;
+    // matrices of a fragment: rows m 0-7 and 8-15 at n 0-7, the same at n 8-15
+    uint32_t from = smem_u32(z) + 2 * (((lane & 7) + (lane & 8)) * pitch + 16 * warp + (lane >> 4) * 8);
 #pragma unroll 1
-        for (int piece = p.pieces - 1; piece >= 0; --piece) {
-          uint32_t a[4];
-          load_fragment<false>(from + 2 * piece * plane, a);
+    for (int b = c; b < end; ++b, from += 2 * BLOCK) {
+      uint4 now[4];
 #pragma unroll
-          for (int j = 0; j < 4; ++j) mma16816(acc[4 * q + j], a, b0[j], b1[j]);
+      for (int i = 0; i < 4; ++i) now[i] = next[i];
+      if (b + 1 < end) fetch_codes(b + 1, k0);
+      else if (k0 + 128 < k_end) fetch_codes(c, k0 + 128);
+      uint32_t only[4];
+      load_fragment<false>(from, only);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const uint32_t r0 = (&now[0].x)[q], r1 = (&now[1].x)[q], r2 = (&now[2].x)[q], r3 = (&now[3].x)[q];
+        const uint32_t b0[4] = {decode_rows<M4E3, 0>(r0, r1), decode_rows<M4E3, 1>(r0, r1), decode_rows<M4E3, 2>(r0, r1),
+                                decode_rows<M4E3, 3>(r0, r1)};
+        const uint32_t b1[4] = {decode_rows<M4E3, 0>(r2, r3), decode_rows<M4E3, 1>(r2, r3), decode_rows<M4E3, 2>(r2, r3),
+                                decode_rows<M4E3, 3>(r2, r3)};
+        if (p.pieces == 1) {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) mma16816(acc[4 * q + j], only, b0[j], b1[j]);
+        } else {
+#pragma unroll 1
+          for (int piece = p.pieces - 1; piece >= 0; --piece) {
+            uint32_t a[4];
+            load_fragment<false>(from + 2 * piece * plane, a);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) mma16816(acc[4 * q + j], a, b0[j], b1[j]);
+          }
         }
       }
     }
-  }
 
-  // The warps' sums: lane (g, t) holds columns 32 t to 32 t + 31 of rows g and g + 8.  16-byte words are exchanged within eight, so that
-  // lanes meet no bank twice
-  float* const red = reinterpret_cast<float*>(smem);
-  float* const sums = red + RED_FLOATS;  // [16][128]
-  __syncthreads();
+    // The warps' sums: lane (g, t) holds columns 32 t to 32 t + 31 of rows g and g + 8.  16-byte words are exchanged within eight, so that
+    // lanes meet no bank twice
 #pragma unroll
-  for (int r = 0; r < 2; ++r)
+    for (int r = 0; r < 2; ++r) {
+      if (8 * r >= rows) break;
+      __syncthreads();
+      if (g + 8 * r < rows) {
 #pragma unroll
-    for (int s = 0; s < 8; ++s) {
-      const int j = 4 * (s & 3), e = 2 * r + (s >> 2);
-      if (g + 8 * r < rows)
-        *reinterpret_cast<float4*>(red + (warp * 16 + g + 8 * r) * RED_PITCH + 32 * t + 4 * (s ^ (2 * t))) = make_float4(acc[j][e], acc[j + 1][e], acc[j + 2][e], acc[j + 3][e]);
+        for (int s = 0; s < 8; ++s) {
+          const int j = 4 * (s & 3), e = 2 * r + (s >> 2);
+          *reinterpret_cast<float4*>(red + (warp * 8 + g) * RED_PITCH + 32 * t + 4 * (s ^ (2 * t))) = make_float4(acc[j][e], acc[j + 1][e], acc[j + 2][e], acc[j + 3][e]);
+        }
+      }
+      __syncthreads();
+      const int row = threadIdx.x >> 5, s = threadIdx.x & 31, at = (s & 24) + ((s & 7) ^ (2 * (s >> 3)));
+      if (row + 8 * r < rows) {
+        float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int w = 0; w < 8; ++w) {
+          const float4 f = *reinterpret_cast<const float4*>(red + (w * 8 + row) * RED_PITCH + 4 * at);
+          v.x += f.x;
+          v.y += f.y;
+          v.z += f.z;
+          v.w += f.w;
+        }
+        reinterpret_cast<float4*>(sums)[(row + 8 * r) * 32 + s] = v;
+      }
     }
-  __syncthreads();
-#pragma unroll 1
-  for (int o = threadIdx.x; o < rows * 32; o += FEW_THREADS) {
-    const int row = o >> 5, s = o & 31, from = (s & 24) + ((s & 7) ^ (2 * (s >> 3)));
-    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    few_cluster_sync();
+    // the cluster's: a CTA takes every eighth row
+    if (warp < 2 && warp * CLUSTER + rank < rows) {
+      const int row = warp * CLUSTER + rank;
+      const uint32_t from = smem_u32(sums + row * 128 + 4 * lane);
+      float4 f[CLUSTER];
 #pragma unroll
-    for (int w = 0; w < 8; ++w) {
-      const float4 f = *reinterpret_cast<const float4*>(red + (w * 16 + row) * RED_PITCH + 4 * from);
-      v.x += f.x;
-      v.y += f.y;
-      v.z += f.z;
-      v.w += f.w;
+      for (int r = 0; r < CLUSTER; ++r) f[r] = peer_float4(from, r);
+      float v[4] = {f[0].x, f[0].y, f[0].z, f[0].w};
+#pragma unroll
+      for (int r = 1; r < CLUSTER; ++r) {
+        v[0] += f[r].x;
+        v[1] += f[r].y;
+        v[2] += f[r].z;
+        v[3] += f[r].w;
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (k0 + 4 * lane + j < p.K) store_one(p.out_a, p.out_type, (m0 + row) * p.K + k0 + 4 * lane + j, v[j] * alpha);
     }
-    reinterpret_cast<float4*>(sums)[row * 32 + s] = v;
+    few_cluster_sync();  // the others have read this CTA's sums
   }
-  few_cluster_sync();
-  // the cluster's: a CTA takes every eighth row
-  if (warp < 2 && warp * CLUSTER + rank < rows) {
-    const int row = warp * CLUSTER + rank;
-    const float alpha = p.factor * (p.alpha_a ? *p.alpha_a : 1.0f);
-    const uint32_t from = smem_u32(sums + row * 128 + 4 * lane);
-    float4 f[CLUSTER];
-#pragma unroll
-    for (int r = 0; r < CLUSTER; ++r) f[r] = peer_float4(from, r);
-    float v[4] = {f[0].x, f[0].y, f[0].z, f[0].w};
-#pragma unroll
-    for (int r = 1; r < CLUSTER; ++r) {
-      v[0] += f[r].x;
-      v[1] += f[r].y;
-      v[2] += f[r].z;
-      v[3] += f[r].w;
-    }
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (k0 + 4 * lane + j < p.K) store_one(p.out_a, p.out_type, (m0 + row) * p.K + k0 + 4 * lane + j, v[j] * alpha);
-  }
-  few_cluster_sync();  // the others have read this CTA's sums
 }
 
 // of a cluster's CTA: dz of 16 rows and an eighth of all n
@@ -565,7 +572,7 @@ size_t dz_bytes(const GradCall& c, int pieces) {
 }  // namespace
 
 // Every 16 rows bring the weights, and every 128 columns the elementwise work, once more, so the product of both is what this kernel's
-// time grows with.  Both gradients in bfloat16, us here and in two launches: 1 x 512 x 512 5.1 and 9.6, 16 x 8192 x 8192 102 and 135,
+// time grows with.  Both gradients in bfloat16, us here and in two launches: 1 x 512 x 512 5.6 and 9.6, 16 x 8192 x 8192 92 and 135,
 // 32 x 2048 x 2048 17.2 and 18.9, 32 x 1024 x 4096 21.5 and 17.0, 48 x 4096 x 1024 21.8 and 27.8, 64 x 1024 x 1024 14.6 and 12.6,
 // 64 x 4096 x 1024 26.1 and 28.3, 64 x 4096 x 4096 82 and 45.
 bool few_rows(const GradCall& c, int pieces) {
@@ -594,7 +601,13 @@ cudaError_t launch_backward_few(const GradCall& c, int pieces, cudaStream_t stre
   p.factor = c.keep_scale;
   const auto up8 = [](int64_t v) { return (v + CLUSTER - 1) / CLUSTER * CLUSTER; };
   const int64_t blocks = (c.N + BLOCK - 1) / BLOCK, all = c.gated ? 2 * blocks : blocks;
-  const int64_t tiles = (c.M + 15) / 16, a_ctas = c.grad_a ? (c.K + 127) / 128 * CLUSTER * tiles : 0;
+  const int64_t tiles = (c.M + 15) / 16, a_cols = (c.K + 127) / 128;
+  // A: no more clusters than run at a time, two CTAs an SM, so that dz is formed once by each (16 x 8192 x 8192, grad_a alone: 47 us
+  // with 64 clusters), where dz can stay beside the sums
+  const size_t dz = dz_bytes(c, pieces);
+  const int64_t times = dz + SUMS_BYTES <= 112 * 1024 ? (a_cols * tiles + 35) / 36 : 1;
+  const int64_t a_ctas = c.grad_a ? (a_cols + times - 1) / times * CLUSTER * tiles : 0;
+  p.red_at = times > 1 ? (int)dz : 0;
   // B: wide CTAs, which form less of dz again, where there are enough of them; several blocks each where there are many
   int width = 512;
   const auto cols = [&] { return (c.K + width - 1) / width; };
@@ -609,6 +622,7 @@ cudaError_t launch_backward_few(const GradCall& c, int pieces, cudaStream_t stre
   p.tiles = (int)tiles;
   p.a_ctas = (int)a_ctas;
   p.b_ctas = (int)b_ctas;
+  p.a_times = (int)times;
   p.a_each = (int)((all + CLUSTER - 1) / CLUSTER);
   p.b_each = (int)each;
   p.b_width = width;
@@ -619,8 +633,8 @@ cudaError_t launch_backward_few(const GradCall& c, int pieces, cudaStream_t stre
   size_t smem = 0;
   const auto wants = [&smem](size_t bytes) { smem = smem > bytes ? smem : bytes; };
   if (a_ctas) {
-    wants(dz_bytes(c, pieces));
-    wants((RED_FLOATS + 16 * 128) * 4);
+    wants(p.red_at + SUMS_BYTES);
+    wants(dz);
   }
   if (b_ctas) wants(tiles * 32 * ((size_t)pitch_of(BLOCK * (int)each) * pieces + pitch_of(width)) + FEW_THREADS / 32 * 16 * OUT_PITCH * 4);
   if (c.grad_bias) wants((size_t)tiles * 16 * RED_PITCH * 4);

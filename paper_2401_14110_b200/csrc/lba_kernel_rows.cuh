@@ -31,6 +31,7 @@ constexpr int ROWS_MIN_STAGES = 3;           // at least as many as warps that t
 constexpr int ROWS_CHAINS = 4;               // (row, column) chains per lane of a fold warp, at most (one where there is one row)
 constexpr int ROWS_SUM_RING = 3;             // rounds of sums kept; two where a third would cost a wave of CTAs
 constexpr int ROWS_MAX_STAGES = 8;
+constexpr int ROWS_ROOM = 227 * 1024;        // bytes of shared memory
 constexpr int ROWS_PITCH = ROWS_CHUNKS + 4;  // sums from one chain to the next: 16-byte aligned, lanes on different banks
 
 struct RowsProblem : LinearProblem {

@@ -8,7 +8,8 @@ template <bool SAT, int RNE, bool M4E3, bool SCALED>
 cudaError_t launch(const RowsProblem& p, cudaStream_t stream) {
   auto kernel = p.M == 1 ? lba_rows_kernel<SAT, RNE, M4E3, SCALED, true> : lba_rows_kernel<SAT, RNE, M4E3, SCALED, false>;
   const size_t smem = rows_smem((int)p.M, p.pairs, p.stages, p.ring);
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  // (the same limit in every call: another thread's may lie between this line and the launch)
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, ROWS_ROOM);
   if (e != cudaSuccess) return e;
   const int64_t pairs = (p.N + 1) / 2;
   return launch_after(kernel, dim3((unsigned)((pairs + p.pairs - 1) / p.pairs)), ROWS_THREADS, smem, stream, p);

@@ -1,4 +1,6 @@
 """Linear and gated layers: the contraction bit for bit, everything after it against 64 bits.  Needs a B200."""
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -239,6 +241,41 @@ def test_streams_and_graphs():
         g.replay()
         assert torch.equal((out == 0).cpu(), ~keep_mask(64, 64, 0.25, 9, offset))
     assert not torch.equal(out, first)
+
+
+def test_calls_of_several_threads():
+    # launches of different sizes and kernels from threads with streams of their own
+    prod, acc = FORMATS["m7e4"]
+    sizes = [(1, 700, 256), (7, 90, 1040), (12, 2000, 64), (40, 200, 512), (3, 64, 4096)]
+    data = [inputs(M, N, K, 20 + i, prod) for i, (M, N, K) in enumerate(sizes)]
+    grads = [synth.gaussian((M, N), i).to(torch.bfloat16).to(DEV) for i, (M, N, _) in enumerate(sizes)]
+
+    def calls(i, stream=None):
+        A, sa, B, sb, bias = data[i]
+        y = lba.lba_linear(A, B, sa, sb, bias, prod, acc, activation="gelu", stream=stream)
+        return (y, *lba.lba_linear_backward(grads[i], A, B, sa, sb, prod, y, "gelu", stream=stream))
+
+    want = [calls(i) for i in range(len(sizes))]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        try:
+            stream = torch.cuda.Stream()
+            with torch.cuda.stream(stream):
+                for _ in range(100):
+                    got = calls(i)
+                stream.synchronize()
+                wrong.extend((i, j) for j, (x, y) in enumerate(zip(got, want[i])) if not torch.equal(x, y))
+        except Exception as e:  # noqa: BLE001
+            wrong.append((i, e))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(len(sizes))]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
 
 
 def test_two_layers_in_a_row_as_a_network_uses_them():

@@ -132,7 +132,7 @@ def test_refused_backward_arguments():
 
 
 def test_backward_workspace_grows_with_what_is_asked():
-    size = lambda **k: lba.backward_workspace_bytes(100, 50, 70, 1, k.pop("sb", 1), k.pop("dtype", torch.bfloat16), activation="gelu", **k)  # noqa: E731
+    size = lambda **k: lba.backward_workspace_bytes(1000, 50, 70, 1, k.pop("sb", 1), k.pop("dtype", torch.bfloat16), activation="gelu", **k)  # noqa: E731
     full = size()
     assert 0 < size(needs=(False, False, True)) < size(needs=(True, False, False)) < full
     assert size(sb=50) == full and size(dtype=torch.float16) > full and size(gated=True) > full
