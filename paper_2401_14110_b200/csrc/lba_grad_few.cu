@@ -333,9 +333,17 @@ __device__ __forceinline__ void bring_out(T* out, const FewParams& p, int64_t n,
     if (whole) {
       constexpr int WORDS = (int)sizeof(T) / 2;
       uint4 raw[WORDS];
-      T* const e = reinterpret_cast<T*>(raw);
+      if constexpr (std::is_same<T, bf16>::value) {  // (two a conversion)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) e[j] = from_f32<T>(v[j]);
+        for (int j = 0; j < 4; ++j) {
+          const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+          (&raw[0].x)[j] = *reinterpret_cast<const uint32_t*>(&b);
+        }
+      } else {
+        T* const e = reinterpret_cast<T*>(raw);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) e[j] = from_f32<T>(v[j]);
+      }
       uint4* const dst = reinterpret_cast<uint4*>(out + (n + g + 8 * r) * p.K + k + 8 * t);
       if (n + g + 8 * r < p.N) {
 #pragma unroll
@@ -395,14 +403,15 @@ __global__ void __launch_bounds__(FEW_THREADS, 2) grad_few_kernel(const __grid_c
     put_blocks(p, kind, c, end - c, 0, rows, pitch, plane, smem);
     __syncthreads();
     const float alpha = p.factor * (p.alpha_b ? *p.alpha_b : 1.0f);
-    const int k_pitch = pitch_of(p.b_width), across = p.b_width / 32, units = (end - c) * (BLOCK / 16) * across;
+    const int k_pitch = pitch_of(p.b_width), across = p.b_width / 32, bits = __ffs(across) - 1;  // (a power of two)
+    const int units = (end - c) * (BLOCK / 16) << bits;
     float* const staged = reinterpret_cast<float*>(activations + tiles * 16 * k_pitch) + warp * 16 * OUT_PITCH;
     // matrices of a fragment, transposed: n 0-7 and 8-15 at m 0-7, the same at m 8-15; columns 0-7 at m 0-7 and 8-15, columns 8-15
     const uint32_t from = smem_u32(z) + 2 * (((lane & 7) + (lane >> 4) * 8) * pitch + (lane & 8));
     const uint32_t from_y = smem_u32(activations) + 2 * ((lane & 15) * k_pitch + (lane >> 4) * 8);
 #pragma unroll 1
     for (int o = warp; o < units; o += FEW_THREADS / 32) {  // 16 n and 32 k
-      const int s = o / across, j = o - s * across, block = c + s / (BLOCK / 16), half = block >= p.blocks;
+      const int s = o >> bits, j = o & (across - 1), block = c + s / (BLOCK / 16), half = block >= p.blocks;
       const int64_t n = (int64_t)(block - (half ? p.blocks : 0)) * BLOCK + s % (BLOCK / 16) * 16, k = k0 + 32 * j;
       if (n >= p.N || k >= p.K) continue;
       float sum[4][4];
@@ -572,8 +581,8 @@ size_t dz_bytes(const GradCall& c, int pieces) {
 }  // namespace
 
 // Every 16 rows bring the weights, and every 128 columns the elementwise work, once more, so the product of both is what this kernel's
-// time grows with.  Both gradients in bfloat16, us here and in two launches: 1 x 512 x 512 5.6 and 9.6, 16 x 8192 x 8192 92 and 135,
-// 32 x 2048 x 2048 17.2 and 18.9, 32 x 1024 x 4096 21.5 and 17.0, 48 x 4096 x 1024 21.8 and 27.8, 64 x 1024 x 1024 14.6 and 12.6,
+// time grows with.  Both gradients in bfloat16, us here and in two launches: 1 x 512 x 512 5.6 and 9.6, 4 x 8192 x 8192 74 and 140,
+// 32 x 2048 x 2048 17.0 and 18.9, 32 x 1024 x 4096 21.5 and 17.0, 48 x 4096 x 1024 21.8 and 27.8, 64 x 1024 x 1024 14.6 and 12.6,
 // 64 x 4096 x 1024 26.1 and 28.3, 64 x 4096 x 4096 82 and 45.
 bool few_rows(const GradCall& c, int pieces) {
   if (c.M <= 0 || c.M > FEW_ROWS || c.N <= 0 || c.K <= 0) return false;
