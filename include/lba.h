@@ -176,8 +176,8 @@ int lba_gated(const uint8_t* A, const uint8_t* B_gate, const uint8_t* B_up, cons
  *     grad_a[m][k] = sum_n dz[m][n] scale_b[n] B[n][k]  (gated: over both projections): with respect to scale_a A
  *     grad_b[n][k] = sum_m dz[m][n] scale_a[m] A[m][k]: with respect to scale_b B        grad_bias[n] = sum_m dz[m][n]
  * act' of LBA_ACT_RELU is 0 at 0.  The residual's gradient is g itself.  Products run on the tensor cores with binary32 sums; the
- * codes are exact there, dz is rounded to 8 significant bits for bfloat16 gradients (16 where it has at most 2048 elements), to 16 for
- * binary16 ones and not at all for binary32 ones.  Sums are formed in a fixed order: a repeated call gives the same bits. */
+ * codes are exact there, dz is held to 16 significant bits for bfloat16 gradients and not rounded at all for binary16 and binary32
+ * ones.  Sums are formed in a fixed order: a repeated call gives the same bits. */
 typedef struct {
   int32_t activation;       /* LBA_ACT_*, as in the forward call                                      */
   int32_t grad_type;        /* LBA_TYPE_F32, BF16 or F16: elements of grad_out                        */

@@ -5,8 +5,8 @@
 //   grad_a[m][k] = sum_n dz[m][n] sb[n] B[n][k]       grad_b[n][k] = sum_m dz[m][n] sa[m] A[m][k]       grad_bias[n] = sum_m dz[m][n]
 //
 // Nothing rounds between additions here, so the products run on the tensor cores.  Codes of either operand format have at most
-// five significant bits: bfloat16 holds them exactly, and only dz is rounded.  One bfloat16 piece of it goes with bfloat16
-// gradients (a rounding of 2^-9 beside the result's own; two where dz is small), two with binary16 ones (2^-15 at most), three with binary32 ones (dz exactly); fewer
+// five significant bits: bfloat16 holds them exactly, and only dz is rounded, to at least twice the result's significant bits: two
+// bfloat16 pieces beside bfloat16 gradients (off by 2^-15 of it at most), three beside binary16 and binary32 ones (dz exactly); fewer
 // where dz itself has no more bits (see pieces()).  Every piece costs one more pass of the matrix instruction.
 //
 // Scales that differ by row or column belong to the summed index of one of the products: dz is multiplied by both scales' fractions
@@ -797,16 +797,14 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
 int64_t up(int64_t v, int64_t a) { return (v + a - 1) / a * a; }
 size_t up256(size_t v) { return (v + 255) / 256 * 256; }
 
-// bfloat16 pieces that dz takes beside a result of the given type; dz that is g itself or zero has no more bits than g, and a
-// common scale is applied to the finished product.  Two beside bfloat16 where dz has few elements: one piece is off by as much as the
-// result's own rounding, and only many of them even that out (1 x 50: results off by 1.6 times their rounding, else by 1.4 times); such
-// products wait for their launches anyway
+// bfloat16 pieces that dz takes beside a result of the given type: at least twice the result's significant bits, 8 and 11, whatever the
+// sizes.  With as many bits as the result's own, dz's rounding is as large as the result's in sums of any length (terms of either sign grow
+// and their errors grow alike): gradients in bfloat16 were off by 1.41 times as much as with dz in binary32, single ones by twice.  dz that is
+// g itself or zero has no more bits than g, and a common scale is applied to the finished product.
 int pieces(const GradCall& c) {
-  constexpr int64_t FEW_ELEMENTS = 2048;
-  const auto of = [](int type) { return type == LT_BF16 ? 1 : type == LT_F16 ? 2 : 3; };
   const bool plain = !c.gated && (c.act == ACT_NONE || c.act == ACT_RELU) && !c.sa_per_row && !c.sb_per_col;
-  const int wanted = c.out_type == LT_BF16 && c.M * c.N <= FEW_ELEMENTS ? 2 : of(c.out_type);
-  return plain && of(c.grad_type) < wanted ? of(c.grad_type) : wanted;
+  const int wanted = c.out_type == LT_BF16 ? 2 : 3, held = c.grad_type == LT_BF16 ? 1 : c.grad_type == LT_F16 ? 2 : 3;
+  return plain && held < wanted ? held : wanted;
 }
 
 int clusters_of_the_device() {
