@@ -1,4 +1,6 @@
 """How exactly the layers' backward pass holds dz, and their activations the tails.  Needs a B200."""
+import math
+
 import pytest
 import torch
 
@@ -48,3 +50,24 @@ def test_dz_keeps_twice_the_results_bits(M, N, K, out):
     if out is BF16:  # the same sums with dz rounded once do not pass
         once = g.to(BF16).double()
         assert max(share_off((once @ w).to(out), dz, w, rows), share_off((once.T @ x).to(out), dz, x, cols)) > 0.05
+
+
+def test_gelu_keeps_its_tail():
+    # z P(z) and its slope are small below -3 and have all the bits of their type there.  Relative error: the sum of eight terms 28 roundings of
+    # 2^-24 at most, 1.7e-6, its own fit 2.6e-8 (1 + z^2), t 1.8e-7, the exponential 2.4e-7 and of its argument's three roundings 9e-8 z^2, two
+    # products 1.2e-7: below (5 + z^2 / 4) 2^-21.  Slopes: of both terms' magnitudes, with one more product and one more sum.
+    z = -torch.cat([torch.linspace(0.01, 12, 4001), torch.linspace(3, 6, 4000)])
+    N, z64 = z.numel(), z.double()
+    rel = (5 + z64 ** 2 / 4) * 2.0 ** -21
+    P, density = 0.5 * torch.special.erfc(-z64 / math.sqrt(2)), torch.exp(-z64 * z64 / 2) / math.sqrt(2 * math.pi)
+    one, codes = torch.ones(1, device=DEV), torch.zeros(N, 16, dtype=torch.uint8, device=DEV)
+    for out in (F32, BF16):
+        got = lba.lba_linear(codes[:1], codes, one, one, z.to(DEV), PROD, ACC, activation="gelu", out_dtype=out).cpu().double()[0]
+        want = z64 * P
+        assert bool(((got - want).abs() <= want.abs() * rel + half_step(out, want * (1 + rel))).all())
+    gated, pre = lba.lba_gated(codes[:1], codes, codes, one, one, one, z.to(DEV), torch.ones(N, device=DEV), PROD, ACC, activation="gelu", preact=F32)
+    assert torch.equal(pre[0, 0].cpu(), z) and bool(((gated.cpu().double()[0] - z64 * P).abs() <= (z64 * P).abs() * (rel + 2.0 ** -24) + 2.0 ** -126).all())
+    want, mass = P + z64 * density, P + z64.abs() * density
+    for needs in ((False, False, True), (True, True, True)):   # two launches, and the one of few rows
+        dz = lba.lba_linear_backward(torch.ones(1, N, device=DEV), codes[:1], codes, one, one, PROD, z[None].to(DEV), "gelu", needs=needs)[2]
+        assert bool(((dz.cpu().double() - want).abs() <= mass * (rel + 2.0 ** -22) + 2.0 ** -126).all())
