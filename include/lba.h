@@ -177,7 +177,8 @@ int lba_gated(const uint8_t* A, const uint8_t* B_gate, const uint8_t* B_up, cons
  *     grad_b[n][k] = sum_m dz[m][n] scale_a[m] A[m][k]: with respect to scale_b B        grad_bias[n] = sum_m dz[m][n]
  * act' of LBA_ACT_RELU is 0 at 0.  The residual's gradient is g itself.  Products run on the tensor cores with binary32 sums; the
  * codes are exact there, dz is held to 16 significant bits for bfloat16 gradients and not rounded at all for binary16 and binary32
- * ones.  Sums are formed in a fixed order: a repeated call gives the same bits. */
+ * ones.  Sums are formed in a fixed order: a repeated call gives the same bits.  Waits inside the kernels end after ten seconds (which
+ * nothing but a GPU that was taken away for as long should bring about); outputs that are not formed for it are NaN then. */
 typedef struct {
   int32_t activation;       /* LBA_ACT_*, as in the forward call                                      */
   int32_t grad_type;        /* LBA_TYPE_F32, BF16 or F16: elements of grad_out                        */
@@ -346,6 +347,11 @@ int lba_describe_plan_batched(int64_t batch, int64_t M, int64_t N, int64_t K, co
  * to every thread's later calls, and a caller that changes it while other threads are inside the library gets an
  * unspecified mix of old and new tiles, never a wrong result.  Returns LBA_OK, or LBA_ERR_SHAPE for an unknown tile. */
 int lba_set_tile_override(int tile);
+
+/* Testing hook, process-wide like the one above: lets waits inside the products of lba_linear_backward and lba_gated_backward (the
+ * form with a workspace) run out at once, as after their ten seconds: 0 = none, the default; 1 = those for another CTA's part of a
+ * tile, 2 = those for operands and 3 = those for finished sums, both in every third pair of CTAs.  Returns LBA_OK, or LBA_ERR_SHAPE for another number. */
+int lba_set_wait_override(int which);
 
 const char* lba_status_string(int status);
 int lba_last_cuda_error(void); /* cudaError_t of the most recent failed CUDA call in this thread, else 0 */

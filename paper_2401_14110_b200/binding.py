@@ -25,7 +25,7 @@ TORCH_LIB_PATH = os.path.join(_HERE, "lba_torch.so")
 
 EXPORTS = ["lba_gemm", "lba_gemm_batched", "lba_linear", "lba_gated", "lba_linear_backward", "lba_gated_backward", "lba_backward_workspace_bytes", "lba_gemm_last_overflow", "lba_gemm_ste_mask", "lba_conv2d", "lba_gemm_host_workspace_bytes", "lba_gemm_host",
            "lba_conv2d_host_workspace_bytes", "lba_conv2d_host", "lba_gemm_host_static", "lba_count_nan_codes", "lba_describe_plan", "lba_describe_plan_batched",
-           "lba_set_tile_override", "lba_status_string", "lba_last_cuda_error", "lba_version"]
+           "lba_set_tile_override", "lba_set_wait_override", "lba_status_string", "lba_last_cuda_error", "lba_version"]
 
 
 class LbaError(RuntimeError):
@@ -593,6 +593,11 @@ def set_tile_override(tile):
     """Force the CTA tile (0..3, 5 = cluster pair) or restore the automatic choice (-1).  A testing hook: process-wide.
     Speed only; results are unchanged."""
     _check(load_library().lba_set_tile_override(int(tile)))
+
+
+def set_wait_override(which):
+    """Let waits inside the layers' backward products run out at once (1 to 3, see lba.h), or restore them (0).  A testing hook: process-wide."""
+    _check(load_library().lba_set_wait_override(int(which)))
 
 
 def describe_plan(M, N, K, prod_fmt, acc_fmt, order=ORDER_CHUNKED, chunk=PAPER_CHUNK, is_conv=False, vec_ok=True, batch=1):

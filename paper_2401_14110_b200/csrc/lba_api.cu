@@ -42,6 +42,7 @@ namespace {
 
 thread_local int g_last_cuda_error = 0;
 std::atomic<int> g_tile_override{-1};  // testing and tuning hook (lba_set_tile_override)
+std::atomic<int> g_wait_override{0};   // testing hook (lba_set_wait_override)
 
 int cuda_fail(cudaError_t e) {
   g_last_cuda_error = (int)e;
@@ -751,6 +752,7 @@ int run_backward(GradCall* c, const lba_backward* h, void* workspace, size_t wor
     if (need > 0 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < need)) return LBA_ERR_WORKSPACE;
   }
   c->pre = h->preact;
+  c->wait_override = g_wait_override.load(std::memory_order_relaxed);
   const cudaError_t e = launch_backward(*c, workspace, stream);
   return e == cudaSuccess ? LBA_OK : cuda_fail(e);
 }
@@ -778,6 +780,12 @@ int lba_last_cuda_error(void) { return g_last_cuda_error; }
 int lba_set_tile_override(int tile) {
   if (tile < -1 || tile > TILE_ROWS || tile == TILE_COUNT || tile == 8 || tile == 9) return LBA_ERR_SHAPE;
   g_tile_override.store(tile, std::memory_order_relaxed);
+  return LBA_OK;
+}
+
+int lba_set_wait_override(int which) {
+  if (which < 0 || which > 3) return LBA_ERR_SHAPE;
+  g_wait_override.store(which, std::memory_order_relaxed);
   return LBA_OK;
 }
 

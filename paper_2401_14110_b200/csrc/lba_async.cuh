@@ -40,47 +40,54 @@ __device__ __forceinline__ void mbar_expect(uint32_t bar, int bytes) {
   asm volatile("mbarrier.expect_tx.relaxed.cta.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
 }
 __device__ __forceinline__ void mbar_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
-// Waits for the phase of the given parity, at most some seconds; then `dead` is set, no wait of the CTA takes long any more, and
-// its outputs become NaN.  Returns whether the phase ended.
+// Every wait ends: after WAIT_LIMIT, or soon where `dead` says that another of the CTA's has run out; then `dead` is set.  The clock is looked
+// at once in 64 tries, each of which may take its time.
+constexpr uint64_t WAIT_LIMIT = 10000000000ull;  // ns
+__device__ __forceinline__ uint64_t wall_ns() {
+  uint64_t t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  return t;
+}
+template <typename Try>
+__device__ __forceinline__ bool wait_until(Try there, volatile int* dead) {
+  uint64_t end = 0;
+  for (uint32_t i = 1;; ++i) {
+    if (there()) return true;
+    if (i & 63) continue;
+    const uint64_t now = wall_ns();
+    if (end == 0) end = now + WAIT_LIMIT;
+    if (*dead) return false;
+    if (now >= end) {
+      *dead = 1;
+      return false;
+    }
+  }
+}
+// Waits for the phase of the given parity.  Returns whether it ended.
 __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, volatile int* dead) {
-  for (uint32_t i = 0;; ++i) {
+  return wait_until([&] {
     uint32_t done;
     asm volatile(
         "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
         : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    if (done) return true;
-    if (i > (1u << 22) || (i > 1024 && *dead)) {
-      *dead = 1;
-      return false;
-    }
-  }
+    return done != 0;
+  }, dead);
 }
 // the same for a barrier that the other CTA of a cluster arrives at too
 __device__ __forceinline__ bool mbar_wait_cluster(uint32_t bar, uint32_t parity, volatile int* dead) {
-  for (uint32_t i = 0;; ++i) {
+  return wait_until([&] {
     uint32_t done;
     asm volatile(
         "{\n\t.reg .pred p;\n\tmbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\tselp.b32 %0, 1, 0, p;\n\t}"
         : "=r"(done) : "r"(bar), "r"(parity) : "memory");
-    if (done) return true;
-    if (i > (1u << 22) || (i > 1024 && *dead)) {
-      *dead = 1;
-      return false;
-    }
-  }
+    return done != 0;
+  }, dead);
 }
-// a word in global memory that another CTA sets to 1
-__device__ __forceinline__ void wait_flag(const uint32_t* flag, volatile int* dead) {
-  for (uint32_t i = 0;; ++i) {
-    uint32_t v;
-    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(flag) : "memory");
-    if (v) return;
-    if (i > (1u << 22) || (i > 1024 && *dead)) {
-      *dead = 1;
-      return;
-    }
-    __nanosleep(64);
-  }
+// Where a wait ran out, copies may still be on their way into the CTA's shared memory, which the next CTA on this SM gets: they land
+// within microseconds, and nothing counts them any more.
+__device__ __forceinline__ void let_copies_land() {
+#pragma unroll 1
+  for (int i = 0; i < 10000; ++i) __nanosleep(1000);
 }
 // one box of a two-dimensional tensor map
 __device__ __forceinline__ void tensor_load(uint32_t dst, const void* map, int x, int y, uint32_t bar) {

@@ -361,11 +361,16 @@ __global__ void __launch_bounds__(PREP_THREADS, GATED ? 3 : 4) grad_prepare_kern
 // from a counter when it starts: it only ever waits for clusters that run already or have ended, for the first thing that those do.
 // `longest`: binary32 results of long sums would lose precision to the matrix instructions, which cut a sum at each addition (8192
 // terms were off by 2.8e-6, where 1000 are by 8e-7).  Their tiles are formed in stretches, added up in binary32.
+// A wait that runs out ends in NaN, never in sums that miss a step.  Inside a pair it stops the copies and products of both CTAs (`dead`, set
+// in both): what either brings out from there on is NaN, and parts of tiles that it hands over are marked as lost.  A tile with a lost part, or
+// with one that was not handed over in time (`missed`), becomes NaN.
 constexpr int BM = 128, BN = 256, BL = 64, GRAD_THREADS = 320, OUT_THREADS = 256;  // of a CTA: rows, columns, step
 constexpr int X_BYTES = BM * BL * 2, STAGE = 2 * X_BYTES, STAGES = 5;
 constexpr int OUT_PITCH = 36;         // floats from row to row of a warp's outputs in shared memory: 128 bytes, 16-byte accesses on all banks
 constexpr size_t PRODUCT_SMEM = 1024 + (size_t)STAGE * STAGES + 256 + OUT_THREADS * OUT_PITCH * 4;
 constexpr int PART_FLOATS = BM * BN;  // a CTA's part of a begun tile
+enum PartFlag : uint32_t { PART_THERE = 1, PART_LOST = 2 };
+enum WaitOverride { WAIT_AS_IT_IS = 0, WAIT_NO_PART = 1, WAIT_NO_OPERANDS = 2, WAIT_NO_SUMS = 3 };  // lba_set_wait_override
 
 struct Job {
   int64_t rows, cols;       // of one half's output
@@ -385,6 +390,7 @@ struct ProductParams {
   int share;                // steps of a cluster's share; 0: there are none
   int longest;              // steps that the matrix instructions add up before binary32 additions take over (all, if none is meant)
   int out_type;
+  int wait_override;
   float factor;
   uint32_t* flags;          // shares: the counter, then a word per CTA's part
   float *parts, *sums;      // parts of begun tiles, and sums of a CTA's steps so far: PART_FLOATS each per CTA
@@ -423,6 +429,21 @@ __device__ __forceinline__ void mma_commit(uint32_t bar) {
 // outputs' stores)
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t bar) {
   asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(bar) : "memory");
+}
+// a wait of this pair ran out: both CTAs know
+__device__ __forceinline__ void give_up(volatile int* dead, int rank) {
+  *dead = 1;
+  asm volatile("st.relaxed.cluster.shared::cluster.u32 [%0], %1;" ::"r"(mapa(smem_u32(const_cast<int*>(dead)), rank ^ 1)), "r"(1) : "memory");
+}
+// waits for another CTA's part of a tile; false where it is lost, or not there in time
+__device__ __forceinline__ bool part_there(const uint32_t* flag, volatile int* missed) {
+  uint32_t v = 0;
+  wait_until([&] {
+    asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(v) : "l"(flag) : "memory");
+    if (!v) __nanosleep(64);
+    return v != 0;
+  }, missed);
+  return v == PART_THERE;
 }
 __device__ __forceinline__ void cluster_sync() {
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
@@ -566,15 +587,16 @@ __device__ __forceinline__ void store_rows(T* out, int64_t pitch, int rows, int 
 __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __grid_constant__ ProductParams p) {
   extern __shared__ unsigned char product_raw[];
   unsigned char* const base = reinterpret_cast<unsigned char*>((reinterpret_cast<uintptr_t>(product_raw) + 1023) & ~(uintptr_t)1023);
-  uint64_t* const bars = reinterpret_cast<uint64_t*>(base + STAGES * STAGE);  // full, empty per stage; done, free per accumulator
-  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 4);
-  volatile int* const dead = reinterpret_cast<volatile int*>(tmem_slot + 1);
-  uint32_t* const share_slot = tmem_slot + 2;
+  uint64_t* const bars = reinterpret_cast<uint64_t*>(base + STAGES * STAGE);  // full, empty per stage; done, free per accumulator; the last products
+  uint32_t* const tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * STAGES + 5);
+  volatile int *const dead = reinterpret_cast<volatile int*>(tmem_slot + 1), *const missed = dead + 1;
+  uint32_t* const share_slot = tmem_slot + 3;
   float* const outs = reinterpret_cast<float*>(base + STAGES * STAGE + 256);  // 32 x 32 of each warp that brings outputs out
   __shared__ float part[4][32];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int rank = blockIdx.x & 1;  // in the cluster
-  const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, acc_done = empty + 8 * STAGES, acc_free = acc_done + 16;
+  const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, acc_done = empty + 8 * STAGES, acc_free = acc_done + 16,
+                 last_done = acc_free + 16;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < STAGES; ++i) {
@@ -585,7 +607,8 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
       mbar_init(acc_done + 8 * i, 1);
       mbar_init(acc_free + 8 * i, 2 * OUT_THREADS / 32);  // the first CTA's: both CTAs' reading warps
     }
-    *dead = 0;
+    mbar_init(last_done, 1);
+    *dead = *missed = 0;
     mbar_init_fence();
   }
   if (warp == 1) {
@@ -611,6 +634,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
   const uint32_t tmem = *tmem_slot;
   const int share = p.share ? (int)*share_slot : blockIdx.x >> 1;
   Walk walk(p, share, gridDim.x >> 1);
+  const int runs_out = p.wait_override == WAIT_NO_PART || (blockIdx.x >> 1) % 3 == 1 ? p.wait_override : WAIT_AS_IT_IS;
   Work w;
   w.last = true;
 
@@ -632,6 +656,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
 #pragma unroll 1
         for (int k = w.k0; k < w.k1; ++k) {
           if (!mbar_wait(empty + 8 * stage, phase, dead)) {
+            give_up(dead, rank);
             alive = false;
             break;
           }
@@ -655,34 +680,40 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
     if (rank == 0 && elected()) {
       int stage = 0, acc = 0;
       uint32_t phase = 0, acc_phase = 1;
+      bool alive = true;
       const uint32_t stages = smem_u32(base);
-      while (walk.next(p, w)) {
+      while (alive && walk.next(p, w)) {
         const int x_mn = p.job[w.job].x_mn;
         // binary32 sums of bfloat16 products; which operand is MN-major; sizes
         const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)x_mn << 15) | (1u << 16) | ((BN / 8) << 17) | ((2 * BM / 16) << 24);
         // operands of a stage at address 0; a step of 16 l is 2048 bytes on where l counts lines, 32 where it counts within one
         const uint64_t x0 = x_mn ? operand(0, X_BYTES / 2, 1024) : operand(0, 16, 1024), y0 = operand(0, X_BYTES / 2, 1024);
         const uint32_t xk = x_mn ? 2048 >> 4 : 32 >> 4;
-        mbar_wait_cluster(acc_free + 8 * acc, acc_phase, dead);
+        alive = mbar_wait_cluster(acc_free + 8 * acc, acc_phase, dead);
         asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
         bool add = false;
 #pragma unroll 1
-        for (int b = w.k0; b < w.k1; ++b) {
-          const bool there = mbar_wait_cluster(full + 8 * stage, phase, dead);
+        for (int b = w.k0; alive && b < w.k1; ++b) {
+          if (!mbar_wait_cluster(full + 8 * stage, phase, dead) || runs_out == WAIT_NO_OPERANDS) {
+            alive = false;
+            break;
+          }
           asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
           const uint32_t x = (stages + stage * STAGE) >> 4, y = x + (X_BYTES >> 4);
-          if (there) {
 #pragma unroll
-            for (int k = 0; k < BL / 16; ++k) {
-              mma(tmem + acc * BN, x0 + x + k * xk, y0 + y + k * (2048 >> 4), idesc, add);
-              add = true;
-            }
+          for (int k = 0; k < BL / 16; ++k) {
+            mma(tmem + acc * BN, x0 + x + k * xk, y0 + y + k * (2048 >> 4), idesc, add);
+            add = true;
           }
           mma_commit(empty + 8 * stage);
           if (++stage == STAGES) {
             stage = 0;
             phase ^= 1;
           }
+        }
+        if (!alive) {  // (the sums never count as done: whoever waits for them gives up too)
+          give_up(dead, rank);
+          break;
         }
         mma_commit(acc_done + 8 * acc);
         if (++acc == 2) {
@@ -704,16 +735,18 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
       const bool begins = w.last && w.to < j.steps, ends = w.last && w.from > 0 && !begins;
       const int first = ends ? (w.start - p.first) / p.share : share;  // the shares that began this tile: first to share - 1
       if (ends) {
-        if (leader)
-          for (int c = first; c < share; ++c) wait_flag(p.flags + 1 + 2 * c + rank, dead);
+        if (leader)  // (one tile of a cluster's walk at most: `missed` is about that one)
+          for (int c = first; c < share; ++c)
+            if (runs_out == WAIT_NO_PART || !part_there(p.flags + 1 + 2 * c + rank, missed)) *missed = 1;
         asm volatile("bar.sync 2, 256;" ::: "memory");
       }
       const int64_t r0 = (int64_t)w.r * (2 * BM) + rank * BM + quarter * 32, r = r0 + lane;
       float alpha = p.factor * (j.alpha[w.half] ? *j.alpha[w.half] : 1.0f);
       if (j.div[w.half] && r < j.rows) alpha = __fdiv_rn(alpha, fraction_of(j.div[w.half][r * j.div_stride]));
-      mbar_wait(acc_done + 8 * acc, phase, dead);
+      if (runs_out == WAIT_NO_SUMS || !mbar_wait(acc_done + 8 * acc, phase, dead)) give_up(dead, rank);
+      __syncwarp();
       asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory");
-      if (*dead) alpha = __uint_as_float(0x7FC00000u);
+      if (*dead || (ends && *missed)) alpha = __uint_as_float(0x7FC00000u);
       float4* const mine = reinterpret_cast<float4*>(p.parts + (2 * (int64_t)share + rank) * PART_FLOATS) + row;  // [four columns][row]
       float4* const sums = reinterpret_cast<float4*>(p.sums + (int64_t)blockIdx.x * PART_FLOATS) + row;
       const int rows = j.rows - r0 < 32 ? (int)(j.rows - r0 > 0 ? j.rows - r0 : 0) : 32;
@@ -779,7 +812,8 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
       if (begins) {
         __threadfence();
         asm volatile("bar.sync 2, 256;" ::: "memory");
-        if (leader) asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(p.flags + 1 + 2 * share + rank), "r"(1u) : "memory");
+        if (leader)
+          asm volatile("st.release.gpu.global.u32 [%0], %1;" ::"l"(p.flags + 1 + 2 * share + rank), "r"((uint32_t)(*dead ? PART_LOST : PART_THERE)) : "memory");
       }
       if (++acc == 2) {
         acc = 0;
@@ -790,6 +824,16 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) grad_product_kernel(const __g
   __syncwarp();
   asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory");
   cluster_sync();  // nothing of the other CTA's is on its way here any more
+  if (*dead) {     // (the same in both CTAs) ... but what was sent before a wait ran out
+    if (warp == 1 && rank == 0 && elected()) {
+      asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(last_done) : "memory");
+      *missed = 0;
+      mbar_wait(last_done, 0, missed);
+    }
+    if (warp == 0) let_copies_land();
+    __syncwarp();
+    cluster_sync();
+  }
   if (warp == 1) asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(2 * BN) : "memory");
 }
 
@@ -983,6 +1027,7 @@ cudaError_t launch_backward(const GradCall& c, void* workspace, cudaStream_t str
 
   ProductParams p = {};
   p.out_type = c.out_type;
+  p.wait_override = c.wait_override;
   p.factor = c.keep_scale;
   p.partial = q.partial;
   p.bias[0] = c.grad_bias; p.bias[1] = c.grad_bias2;

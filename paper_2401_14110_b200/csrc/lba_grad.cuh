@@ -17,6 +17,7 @@ struct GradCall {
   int grad_type, pre_type, out_type, act, gated, in_m4e3, sa_per_row, sb_per_col;
   uint32_t drop_below;
   float keep_scale;
+  int wait_override;  // see lba_set_wait_override
 };
 
 size_t backward_workspace(const GradCall& c);

@@ -273,7 +273,7 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) lba_rows_kernel(const __grid_
       uint32_t phase = 0;
       for (int r = 1; r < rounds; ++r) {
         mbar_wait(empty + 8 * stage, phase ^ 1, dead);
-        if (*dead) break;
+        if (*dead) break;  // (the others' waits end for it)
         copy(r, stage);
         if (++stage == stages) {
           stage = 0;
@@ -353,6 +353,7 @@ __global__ void __launch_bounds__(ROWS_THREADS, 1) lba_rows_kernel(const __grid_
       layer_store_sums<2>(p, c / columns, n0 + c % columns, o);
     }
   }
+  if (*dead) let_copies_land();  // (a warp whose wait ran out sees it, and it was that warp's to wait for a copy)
 }
 
 struct RowsShape { int pairs, stages, ring; };  // no stages: the kernel does not apply
