@@ -9,6 +9,7 @@ Argument marshalling only: PyTorch supplies device memory and the current stream
 the computation runs in the CUDA kernels behind the C entry points.  There is no fallback: if the
 library is missing, or a call returns an error, an exception is raised.
 """
+import contextlib
 import ctypes as C
 import importlib.util
 import os
@@ -166,6 +167,26 @@ def _stream(stream):
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _torch_stream(stream, device):
+    """An explicit stream as PyTorch knows it (handles 0 and 1: the default stream)."""
+    if isinstance(stream, torch.cuda.Stream):
+        return stream
+    handle = _stream(stream)
+    return torch.cuda.default_stream(device) if handle in (0, 1) else torch.cuda.ExternalStream(handle, device)
+
+
+def _empty(shape, dtype, device, stream, returned=True):
+    """torch.empty for a kernel on ``stream``.  Memory belongs to the stream that it is allocated on: from the current one's, a kernel
+    elsewhere could be given what work that is still queued here reads.  What is returned is used here too, which the allocator is told."""
+    if stream is None or device.type != "cuda":
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(_torch_stream(stream, device)):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    if returned:
+        t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 def _dev(t, dtype, name):
     if t is None:
         return None
@@ -198,7 +219,7 @@ def lba_gemm(A, B, scale_a, scale_b, bias, prod_fmt, acc_fmt, order=ORDER_CHUNKE
     if K != K2:
         raise ValueError("A and B disagree on K")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.float32, device=A.device)
+        out = _empty((M, N), torch.float32, A.device, stream)
     pf, af = _fmt_ref(prod_fmt), _fmt_ref(acc_fmt)
     _check(lib.lba_gemm(_dev(A, torch.uint8, "A"), _dev(B, torch.uint8, "B"), _dev(scale_a, torch.float32, "scale_a"),
                         scale_a.numel(), _dev(scale_b, torch.float32, "scale_b"), scale_b.numel(),
@@ -226,7 +247,7 @@ def lba_gemm_batched(A, B, scale_a, scale_b, bias, prod_fmt, acc_fmt, order=ORDE
     if K != K2:
         raise ValueError("A and B disagree on K")
     if out is None:
-        out = torch.empty((Z, M, N), dtype=torch.float32, device=A.device)
+        out = _empty((Z, M, N), torch.float32, A.device, stream)
     pf, af = _fmt_ref(prod_fmt), _fmt_ref(acc_fmt)
     _check(lib.lba_gemm_batched(_dev(A, torch.uint8, "A"), _dev(B, torch.uint8, "B"),
                                 _dev(scale_a, torch.float32, "scale_a"), scale_a.numel(),
@@ -284,19 +305,19 @@ def _rng(rng, dropout):
     return ptr
 
 
-def _layer(out_shape, pre_shape, device, activation, out_dtype, out_scale, preact, out, residual=None, dropout=0.0, rng=None):
+def _layer(out_shape, pre_shape, device, stream, activation, out_dtype, out_scale, preact, out, residual=None, dropout=0.0, rng=None):
     """The C struct of a layer's epilogue, and the output and pre-activation tensors that it points to."""
     if out is None:
         if out_dtype not in _OUT_TYPES:
             raise TypeError("out_dtype must be torch.float32, bfloat16, float16, or uint8 for codes")
-        out = torch.empty(out_shape, dtype=out_dtype, device=device)
+        out = _empty(out_shape, out_dtype, device, stream)
     elif out.dtype not in _OUT_TYPES:
         raise TypeError("out must be a float32, bfloat16, float16 or (codes) uint8 CUDA tensor")
     _shaped(out, out_shape, "out")
     if isinstance(preact, torch.dtype):
         if preact not in _FLOAT_TYPES:
             raise TypeError("preact must be torch.float32, bfloat16 or float16, a tensor of these, or None")
-        preact = torch.empty(pre_shape, dtype=preact, device=device)
+        preact = _empty(pre_shape, preact, device, stream)
     pre, pre_type = _typed(_shaped(preact, pre_shape, "preact"), "preact")
     res, res_type = _typed(_shaped(residual, out_shape, "residual"), "residual")
     codes = out.dtype == torch.uint8
@@ -325,7 +346,7 @@ def lba_linear(A, B, scale_a, scale_b, bias, prod_fmt, acc_fmt, order=ORDER_CHUN
     if K != K2:
         raise ValueError("A and B disagree on K")
     _same_device(A, B, scale_a, scale_b, bias, residual, rng if dropout else None, out_scale, out, None if isinstance(preact, torch.dtype) else preact)
-    layer, out, pre = _layer((M, N), (M, N), A.device, activation, out_dtype, out_scale, preact, out, residual, dropout, rng)
+    layer, out, pre = _layer((M, N), (M, N), A.device, stream, activation, out_dtype, out_scale, preact, out, residual, dropout, rng)
     sa, sa_len = _scale(scale_a, "scale_a")
     sb, sb_len = _scale(scale_b, "scale_b")
     _check(lib.lba_linear(_dev(A, torch.uint8, "A"), _dev(B, torch.uint8, "B"), sa, sa_len, sb, sb_len,
@@ -351,7 +372,7 @@ def lba_gated(A, B_gate, B_up, scale_a, scale_gate, scale_up, bias_gate, bias_up
     if K != K2 or tuple(B_up.shape) != (N, K):
         raise ValueError("A, B_gate and B_up disagree on K, or the two projections on N")
     _same_device(A, B_gate, B_up, scale_a, scale_gate, scale_up, bias_gate, bias_up, out_scale, out, None if isinstance(preact, torch.dtype) else preact)
-    layer, out, pre = _layer((M, N), (2, M, N), A.device, activation, out_dtype, out_scale, preact, out)
+    layer, out, pre = _layer((M, N), (2, M, N), A.device, stream, activation, out_dtype, out_scale, preact, out)
     sa, sa_len = _scale(scale_a, "scale_a")
     sg, sg_len = _scale(scale_gate, "scale_gate")
     su, su_len = _scale(scale_up, "scale_up")
@@ -380,9 +401,7 @@ def _backward(gated, grad_out, shape, K, scale_a_len, scale_b_len, prod_fmt, pre
     need = lib.lba_backward_workspace_bytes(gated, shape[0], shape[1], K, scale_a_len, scale_b_len, C.byref(how),
                                             sum(1 << i for i, n in enumerate(needs) if n))
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=device)
-        if stream is not None and need:   # memory that the caching allocator hands out again belongs to the current stream
-            workspace.record_stream(stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream(stream), device))
+        workspace = _empty(need, torch.uint8, device, stream, returned=False)
     return how, g, grad_dtype, workspace
 
 
@@ -408,9 +427,9 @@ def lba_linear_backward(grad_out, A, B, scale_a, scale_b, prod_fmt, preact=None,
     sb, sb_len = _scale(scale_b, "scale_b")
     how, g, dtype, ws = _backward(0, grad_out, (M, N), K, sa_len, sb_len, prod_fmt, preact, activation, dropout, rng, grad_dtype, needs,
                                   workspace, A.device, stream)
-    ga = torch.empty((M, K), dtype=dtype, device=A.device) if needs[0] else None
-    gb = torch.empty((N, K), dtype=dtype, device=A.device) if needs[1] else None
-    gc = torch.empty((N,), dtype=torch.float32, device=A.device) if needs[2] else None
+    ga = _empty((M, K), dtype, A.device, stream) if needs[0] else None
+    gb = _empty((N, K), dtype, A.device, stream) if needs[1] else None
+    gc = _empty((N,), torch.float32, A.device, stream) if needs[2] else None
     _check(lib.lba_linear_backward(g, _dev(A, torch.uint8, "A"), _dev(B, torch.uint8, "B"), sa, sa_len, sb, sb_len, M, N, K,
                                               C.byref(how), _typed(ga, "grad_a")[0], _typed(gb, "grad_b")[0],
                                               _dev(gc, torch.float32, "grad_bias"), _dev(ws, torch.uint8, "workspace"), ws.numel(),
@@ -439,9 +458,9 @@ def lba_gated_backward(grad_out, A, B_gate, B_up, scale_a, scale_gate, scale_up,
         raise ValueError("scale_gate and scale_up must have the same length")
     how, g, dtype, ws = _backward(1, grad_out, (M, N), K, sa_len, sg_len, prod_fmt, preact, activation, 0.0, None, grad_dtype, needs, workspace,
                                   A.device, stream)
-    ga = torch.empty((M, K), dtype=dtype, device=A.device) if needs[0] else None
-    gg, gu = (torch.empty((N, K), dtype=dtype, device=A.device) if needs[1] else None for _ in range(2))
-    cg, cu = (torch.empty((N,), dtype=torch.float32, device=A.device) if needs[2] else None for _ in range(2))
+    ga = _empty((M, K), dtype, A.device, stream) if needs[0] else None
+    gg, gu = (_empty((N, K), dtype, A.device, stream) if needs[1] else None for _ in range(2))
+    cg, cu = (_empty((N,), torch.float32, A.device, stream) if needs[2] else None for _ in range(2))
     _check(lib.lba_gated_backward(g, _dev(A, torch.uint8, "A"), _dev(B_gate, torch.uint8, "B_gate"), _dev(B_up, torch.uint8, "B_up"),
                                              sa, sa_len, sg, su, sg_len, M, N, K, C.byref(how), _typed(ga, "grad_a")[0],
                                              _typed(gg, "grad_gate")[0], _typed(gu, "grad_up")[0], _dev(cg, torch.float32, "grad_bias_gate"),
@@ -466,7 +485,7 @@ def lba_gemm_last_overflow(A, B, prod_fmt, acc_fmt, out=None, stream=None):
     if K != K2:
         raise ValueError("A and B disagree on K")
     if out is None:
-        out = torch.empty((M, N), dtype=torch.int32, device=A.device)
+        out = _empty((M, N), torch.int32, A.device, stream)
     pf, af = _fmt_ref(prod_fmt), _fmt_ref(acc_fmt)
     _check(lib.lba_gemm_last_overflow(_dev(A, torch.uint8, "A"), _dev(B, torch.uint8, "B"), M, N, K, pf,
                                       af, _dev(out, torch.int32, "last"), _stream(stream)))
@@ -486,11 +505,11 @@ def lba_gemm_ste_mask(A, B, prod_fmt, acc_fmt, order=ORDER_CHUNKED, chunk=PAPER_
     if K != K2:
         raise ValueError("A and B disagree on K")
     if mask1 is None:
-        mask1 = torch.empty((M, (K + 31) // 32, N), dtype=torch.int32, device=A.device)
+        mask1 = _empty((M, (K + 31) // 32, N), torch.int32, A.device, stream)
     if order != ORDER_CHUNKED:
         mask2 = None
     elif mask2 is None:
-        mask2 = torch.empty((M, ((K + chunk - 1) // max(chunk, 1) + 31) // 32, N), dtype=torch.int32, device=A.device)
+        mask2 = _empty((M, ((K + chunk - 1) // max(chunk, 1) + 31) // 32, N), torch.int32, A.device, stream)
     pf, af = _fmt_ref(prod_fmt), _fmt_ref(acc_fmt)
     _check(lib.lba_gemm_ste_mask(_dev(A, torch.uint8, "A"), _dev(B, torch.uint8, "B"), M, N, K, pf, af,
                                  order, chunk, ste, C.c_float(eps1), C.c_float(eps2), _dev(mask1, torch.int32, "mask1"),
@@ -511,7 +530,7 @@ def lba_conv2d(x, w, scale_x, scale_w, bias, stride, pad, prod_fmt, acc_fmt, ord
         raise ValueError("x and w disagree on C_in")
     Hout, Wout = conv_out_hw(H, W, KH, KW, stride, pad)
     if out is None:
-        out = torch.empty((B, max(Hout, 0), max(Wout, 0), Cout), dtype=torch.float32, device=x.device)
+        out = _empty((B, max(Hout, 0), max(Wout, 0), Cout), torch.float32, x.device, stream)
     pf, af = _fmt_ref(prod_fmt), _fmt_ref(acc_fmt)
     _check(lib.lba_conv2d(_dev(x, torch.uint8, "x"), _dev(w, torch.uint8, "w"), _dev(scale_x, torch.float32, "scale_x"),
                           scale_x.numel(), _dev(scale_w, torch.float32, "scale_w"), scale_w.numel(),
@@ -583,10 +602,11 @@ def lba_conv2d_host(x, w, scale_x, scale_w, bias, stride, pad, prod_fmt, acc_fmt
 def count_nan_codes(codes, stream=None):
     """Number of E4M3 NaN codes (0x7F, 0xFF) in a CUDA uint8 tensor (synchronises)."""
     lib = load_library()
-    count = torch.zeros(1, dtype=torch.int64, device=codes.device)
-    _check(lib.lba_count_nan_codes(_dev(codes, torch.uint8, "codes"), codes.numel(), C.c_void_p(count.data_ptr()),
-                                   _stream(stream)))
-    return int(count.item())
+    data = _dev(codes, torch.uint8, "codes")
+    with contextlib.nullcontext() if stream is None else torch.cuda.stream(_torch_stream(stream, codes.device)):
+        count = torch.zeros(1, dtype=torch.int64, device=codes.device)
+        _check(lib.lba_count_nan_codes(data, codes.numel(), C.c_void_p(count.data_ptr()), _stream(stream)))
+        return int(count.item())
 
 
 def set_tile_override(tile):
