@@ -580,14 +580,17 @@ size_t dz_bytes(const GradCall& c, int pieces) {
 
 }  // namespace
 
-// Every 16 rows bring the weights, and every 128 columns the elementwise work, once more, so the product of both is what this kernel's
-// time grows with.  Both gradients in bfloat16, us here and in two launches: 1 x 512 x 512 5.6 and 9.6, 4 x 8192 x 8192 74 and 140,
-// 32 x 2048 x 2048 17.0 and 18.9, 32 x 1024 x 4096 21.5 and 17.0, 48 x 4096 x 1024 21.8 and 27.8, 64 x 1024 x 1024 14.6 and 12.6,
-// 64 x 4096 x 1024 26.1 and 28.3, 64 x 4096 x 4096 82 and 45.
+// Every 16 rows bring the weights and every 128 columns k the elementwise work of all rows once more, in more CTAs than run at a time where
+// there are many of both; and dz of many columns n leaves room for one group of 128 k a CTA.  Both sides on 305 sizes of 16 to 64 rows, 512 to
+// 8192 n and 256 to 4096 k, linear and gated, bfloat16 and binary32: the rule's choice takes 0.5 % more than the better side on
+// average, 35 % at most (48 x 8192 x 256, gated: 54 us instead of 40; without the limit on n it is 81 %).  All gradients in bfloat16, GELU, scales per channel, us
+// here and in two launches: 1 x 512 x 512 5.5 and 11.6, 4 x 8192 x 8192 89 and 153, 17 x 4096 x 4096 42 and 57, 32 x 2048 x 2048 18.8 and 27.7,
+// 32 x 1024 x 4096 20.2 and 26.1, 48 x 4096 x 1024 25.0 and 30.2, 64 x 1024 x 1024 16.2 and 17.0, 64 x 4096 x 1024 29.6 and 30.9,
+// 48 x 1024 x 2048 19.1 and 18.1, 64 x 2048 x 4096 46 and 32, 64 x 8192 x 1024 47.4 and 44.4, 64 x 4096 x 4096 130 and 55.
 bool few_rows(const GradCall& c, int pieces) {
   if (c.M <= 0 || c.M > FEW_ROWS || c.N <= 0 || c.K <= 0) return false;
   const int64_t tiles = (c.M + 15) / 16;
-  if (tiles > 1 && tiles * c.K > 4096) return false;
+  if (tiles > 1 && (tiles * tiles * c.K > 16384 || tiles * c.N * (c.gated ? 2 : 1) > 32768)) return false;
   return c.grad_a ? dz_bytes(c, pieces) <= MOST_SMEM : c.grad_b != nullptr;
 }
 

@@ -1,4 +1,6 @@
-"""The layers' testing hooks on the host."""
+"""The layers' testing hooks and choice of kernels, on the host."""
+import torch
+
 from paper_2401_14110_b200 import binding as lba
 
 
@@ -6,3 +8,10 @@ def test_wait_override_numbers():
     lib = lba.load_library()
     assert lib.lba_set_wait_override(4) == -2 and lib.lba_set_wait_override(-1) == -2
     assert lib.lba_set_wait_override(1) == 0 and lib.lba_set_wait_override(0) == 0
+
+
+def test_few_rows_take_the_faster_side():
+    # the kernel for few rows needs no workspace; sizes far on either side of its rule, where it took 0.4 to 0.8 and 1.4 to 2.3 times as long
+    size = lambda M, N, K, gated=False: lba.backward_workspace_bytes(M, N, K, 1, N, torch.bfloat16, activation="silu", gated=gated)  # noqa: E731
+    assert not any(size(*s) for s in [(1, 512, 512), (4, 8192, 8192), (17, 4096, 4096), (32, 2048, 2048), (48, 4096, 512), (64, 2048, 512)])
+    assert all(size(*s) for s in [(64, 2048, 4096), (64, 4096, 4096), (64, 8192, 2048), (64, 8192, 1024, True), (48, 8192, 1024, True), (64, 512, 4096), (65, 512, 512)])
