@@ -1,4 +1,6 @@
 """The layers' testing hooks and choice of kernels, on the host."""
+import ctypes as C
+
 import torch
 
 from paper_2401_14110_b200 import binding as lba
@@ -15,3 +17,15 @@ def test_few_rows_take_the_faster_side():
     size = lambda M, N, K, gated=False: lba.backward_workspace_bytes(M, N, K, 1, N, torch.bfloat16, activation="silu", gated=gated)  # noqa: E731
     assert not any(size(*s) for s in [(1, 512, 512), (4, 8192, 8192), (17, 4096, 4096), (32, 2048, 2048), (48, 4096, 512), (64, 2048, 512)])
     assert all(size(*s) for s in [(64, 2048, 4096), (64, 4096, 4096), (64, 8192, 2048), (64, 8192, 1024, True), (48, 8192, 1024, True), (64, 512, 4096), (65, 512, 512)])
+
+
+def test_sizes_whose_workspace_does_not_count_in_64_bits_are_refused():
+    lib = lba.load_library()
+    how = lba._Backward()
+    how.activation, how.preact = 4, 256
+    fake, most = C.c_void_p(256), (1 << 31) - 1
+    for M, N, K in [(most, most >> 1, 1), (most, most >> 1, most), (most, (1 << 29) + 100, 1)]:   # dz in three pieces: up to 2^64.6 bytes
+        assert lib.lba_gated_backward(fake, fake, fake, fake, fake, 1, fake, fake, 1, M, N, K, C.byref(how), fake, fake, fake, fake, fake, fake,
+                                      C.c_size_t(1 << 63), None) == -2
+        assert lib.lba_backward_workspace_bytes(1, M, N, K, 1, 1, C.byref(how), 7) == 0
+    assert lib.lba_backward_workspace_bytes(1, 1 << 24, 1 << 20, 64, 1, 1, C.byref(how), 7) > 6 << 45   # far more than a GPU holds, and countable
