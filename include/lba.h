@@ -154,7 +154,8 @@ typedef struct {
   const void* residual;     /* device, [M][N], or NULL (lba_linear only); may be out itself if the
                                types are the same                                                     */
   int32_t preact_type, residual_type;  /* LBA_TYPE_F32, BF16 or F16                                   */
-  double dropout;           /* p in [0, 1), lba_linear only; M is below 2^32 then                     */
+  double dropout;           /* p in [0, 1), p 2^32 + 1/2 below 2^32, lba_linear only; M is below 2^32
+                               then                                                                   */
   const uint64_t* rng;      /* device, 2 values: seed, offset; needed for p > 0                       */
 } lba_layer;
 
@@ -327,7 +328,8 @@ int lba_count_nan_codes(const uint8_t* codes, int64_t n, unsigned long long* cou
  * one that runs, with its micro-tile, grid and product mode: " by=split16x16(micro=2x4,grid=4x4,pq=none)" or
  * " by=split32x32(...)" (chunks of 16: the chunk sums of a tile spread over the warps of a CTA), " by=chain16x16(...)" (sequential).
  * is_conv selects the loader family; for a convolution pass M = B*H_out*W_out, N = C_out,
- * K = KH*KW*C_in and vec_ok = (C_in % 16 == 0 and pointers aligned).  Returns LBA_OK or the
+ * K = KH*KW*C_in and vec_ok = (C_in % 16 == 0 and pointers aligned).  lba_linear runs what lba_gemm runs and lba_gated what
+ * lba_gemm runs for 2 N columns, but for their kernel of few rows, which the text does not know.  Returns LBA_OK or the
  * error the real call would return; buf may be NULL. */
 int lba_describe_plan(int64_t M, int64_t N, int64_t K, const lba_fmt* prod_fmt, const lba_fmt* acc_fmt, int order,
                       int chunk, int is_conv, int vec_ok, char* buf, size_t buf_len);
@@ -340,7 +342,8 @@ int lba_describe_plan_batched(int64_t batch, int64_t M, int64_t N, int64_t K, co
 /* Testing and tuning hook: force the CTA tile (0 = 128x128, 1 = 128x64, 2 = 64x64, 3 = 32x32 outputs; 5 = the 64x64
  * tile shared by a cluster of two CTAs, each taking every second chunk, used only in chunk-16 order with floor
  * rounding and 16-byte loads, ignored otherwise; 6, 7 = the small-problem kernels of chunk-16 order on 16x16 and 32x32
- * tiles, 10 = that of sequential order, ignored where they do not apply; -1 = automatic choice, the default).  For lba_gemm_ste_mask, 3
+ * tiles, 10 = that of sequential order, ignored where they do not apply; 11 = the kernel for few rows of lba_linear and
+ * lba_gated, ignored where it does not apply, while 0 to 10 send such calls to the tiles; -1 = automatic choice, the default).  For lba_gemm_ste_mask, 3
  * selects the scalar tracking kernel where the packed one would run, and 2 and 7 force the 64x64 and the 32x32 tile of
  * the mask and last-overflow passes (difference masks in chunks that are a multiple of 16 have the 64x64 tile only).
  * Results never depend on the tile, only speed does.  The setting is one process-wide word (an atomic store): it is meant for tests and tuning runs, it applies

@@ -348,7 +348,8 @@ __global__ void __launch_bounds__(PREP_THREADS, GATED ? 3 : 4) grad_prepare_kern
 //   grad_b: r = n, l = m, s = k; X is read from the same layout, contiguous in r (MN-major); so is Y, contiguous in s, in both
 // A cluster of two CTAs forms a 256 x 256 tile: each CTA holds 128 rows of X, half of Y's columns and the accumulators of its rows, and
 // one thread of the first issues the matrix instructions of both (cta_group::2).  What bounds such a product is what the L2 can
-// deliver: a CTA alone with 128 x 256 outputs fetched 48 KB per 64 l where this takes 32 (4096 x 4096 x 1024: 82 us alone).
+// deliver: a CTA alone with 128 x 256 outputs fetched 48 KB per 64 l where this takes 32 (4096 x 4096 x 1024, one piece of dz: 82 us
+// alone against 53; two pieces 92, 87 % of the tensor pipe).
 // Ten warps a CTA: one thread loads, one multiplies into one of two accumulators of 256 columns of tensor memory, eight warps bring the
 // other one out.  A step is 512 clocks of the tensor cores, so its loads must take the one thread less: two copies with three- and
 // four-dimensional boxes and no arithmetic but the coordinates' (three copies and 64-bit divisions in a lane chosen by its number had
@@ -894,7 +895,7 @@ Layout layout(const GradCall& c) {
   // How many tiles stay whole: all, or some, the others in equal shares.  In steps, a tile takes at least EPILOGUE (bringing it out hides
   // behind the next one's steps), so shorter tiles are never divided (1 x 4096 x 4096 89 us otherwise, 45 like this).  A share costs beside
   // its own steps what its begun sums take to be written and waited for, less where whole tiles follow, and the finishing cluster
-  // JOIN for each share that it adds: a tile must not be cut too often.  All tiles whole and like this, us: 256 x 8192 x 512 gated
+  // JOIN for each share that it adds: a tile must not be cut too often.  All tiles whole and like this, us (dz in one piece): 256 x 8192 x 512 gated
   // 91.5 and 55.3 (94 with 26 shares a tile), 8192 x 512 x 512 51.2 and 35.8, 6000 x 4096 x 1024 106.7 and 98.6, 4096 x 4096 x 1024
   // 71.2 and 70.9.
   constexpr int64_t EPILOGUE = 16, CUT = 30, CUT_BEFORE_WHOLE = 14, JOIN = 5;
