@@ -199,7 +199,8 @@ size_t lba_backward_workspace_bytes(int gated, int64_t M, int64_t N, int64_t K, 
                                     const lba_backward* how, int needs);
 
 /* grad_out [M][N]; outputs grad_a [M][K], grad_b [N][K], grad_bias [N], each NULL if it is not wanted (a gated layer's two
- * projections: both or neither).  M and K are at most 2^31 - 1, N 2^30 - 1; sizes whose workspace would pass 2^62 bytes are refused. */
+ * projections: both or neither).  M and K are at most 2^31 - 1, N 2^30 - 1; sizes
+ * whose dz or codes would take 2^40 bytes as bfloat16 are refused. */
 int lba_linear_backward(const void* grad_out, const uint8_t* A, const uint8_t* B, const float* scale_a, int scale_a_len,
                         const float* scale_b, int scale_b_len, int64_t M, int64_t N, int64_t K, const lba_backward* how,
                         void* grad_a, void* grad_b, float* grad_bias, void* workspace, size_t workspace_bytes,

@@ -728,9 +728,10 @@ int fill_backward(GradCall* c, const lba_backward* h, int64_t M, int64_t N, int6
       (h->input_flags & ~LBA_FLAG_INPUT_M4E3))
     return LBA_ERR_LAYER;
   if (c->gated && h->dropout != 0.0) return LBA_ERR_LAYER;
-  // what the workspace may hold at most, pieces of dz and codes as bfloat16 in rows of whole 64s: its bytes are counted in 64 bits
-  const double n64 = (c->gated ? 2.0 : 1.0) * (double)(N + 63), k64 = (double)(K + 63);
-  if (6.0 * (double)M * n64 + 2.0 * ((double)M + n64) * k64 > 0x1p62) return LBA_ERR_SHAPE;
+  // a piece of dz and the codes as bfloat16, in rows of whole 64s: tensor copies know strides below 2^40 bytes, and the workspace's bytes
+  // are counted in 64 bits
+  const double n64 = (c->gated ? 2.0 : 1.0) * (double)((N + 63) / 64 * 64), k64 = (double)((K + 63) / 64 * 64);
+  if (M > 0 && N > 0 && std::fmax(2.0 * (double)M * n64, 2.0 * std::fmax((double)M, n64) * k64) >= 0x1p40) return LBA_ERR_SHAPE;
   c->M = M;
   c->N = N;
   c->K = K;

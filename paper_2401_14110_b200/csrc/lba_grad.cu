@@ -1022,9 +1022,6 @@ cudaError_t launch_backward(const GradCall& c, void* workspace, cudaStream_t str
   q.col_blocks = (int)col_blocks;
   q.z_blocks = (int)z_blocks;
   q.a_blocks = (int)a_blocks;
-  e = c.grad_type == LT_F32 ? launch_prepare<float>(q, c, (unsigned)blocks, stream)
-      : c.grad_type == LT_BF16 ? launch_prepare<bf16>(q, c, (unsigned)blocks, stream) : launch_prepare<__half>(q, c, (unsigned)blocks, stream);
-  if (e != cudaSuccess) return e;
 
   ProductParams p = {};
   p.out_type = c.out_type;
@@ -1079,6 +1076,9 @@ cudaError_t launch_backward(const GradCall& c, void* workspace, cudaStream_t str
   }
   if (e != cudaSuccess) return e;
   e = cudaFuncSetAttribute(grad_product_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)PRODUCT_SMEM);
+  if (e != cudaSuccess) return e;
+  e = c.grad_type == LT_F32 ? launch_prepare<float>(q, c, (unsigned)blocks, stream)
+      : c.grad_type == LT_BF16 ? launch_prepare<bf16>(q, c, (unsigned)blocks, stream) : launch_prepare<__half>(q, c, (unsigned)blocks, stream);
   if (e != cudaSuccess) return e;
   int64_t clusters = l.clusters;
   if (!p.share && c.grad_bias) {  // more CTAs for the bias: they find no tile
