@@ -96,8 +96,10 @@ enum {
   LBA_ERR_CUDA = -6,      /* a CUDA call failed; see lba_last_cuda_error                     */
   LBA_ERR_WORKSPACE = -7, /* host-buffer entry points: workspace NULL, too small, misaligned */
   LBA_ERR_STATIC_LIMIT = -8, /* lba_gemm_host_static: the problem needs more than LBA_STATIC_WORKSPACE_BYTES */
-  LBA_ERR_LAYER = -9      /* lba_linear and its kin: an unknown activation or element type, a dropout outside [0, 1),
+  LBA_ERR_LAYER = -9,     /* lba_linear and its kin: an unknown activation or element type, a dropout outside [0, 1),
                              or an option that the layer does not have                       */
+  LBA_ERR_ALIGN = -10     /* a tensor of lba_attention or a cache that starts, or whose rows start, between the 16-byte
+                             boundaries that its copies need                                 */
 };
 
 /* GEMM  out[m][n] = epilogue( dot(A[m][:], B[n][:]) ), i.e. Y = X W^T with x_i = X_mi,
@@ -210,6 +212,95 @@ int lba_gated_backward(const void* grad_out, const uint8_t* A, const uint8_t* B_
                        int scale_b_len, int64_t M, int64_t N, int64_t K, const lba_backward* how, void* grad_a,
                        void* grad_gate, void* grad_up, float* grad_bias_gate, float* grad_bias_up, void* workspace,
                        size_t workspace_bytes, void* stream);
+
+/* Between a transformer block's linear layers: rotary positions, attention over whole prompts with its gradients, and a key-value
+ * cache held in 4 bits with the attention that reads it.  No Q_prod or Q_acc acts in these: sums are binary32 (products on the tensor
+ * cores), softmax statistics too.  Heads of a tensor [rows][heads][dim] lie `head` elements apart and rows `token` elements apart, so
+ * that slices of a projection's output can be taken as they are; a head's values are contiguous. */
+typedef struct {
+  int64_t token, head; /* strides, in elements */
+} lba_strides;
+
+/* Rotary positions.  A head's first rotary_dim values are pairs (x, y), pair i of positions p and frequency f[i]:
+ *     (x cos pf - y sin pf, x sin pf + y cos pf) scale           inverse: the angle's negative, which is also the gradient
+ * The pair's values lie rotary_dim / 2 apart, or side by side if `interleaved`; a head's other values pass.  Angles are formed in
+ * binary64, so far positions keep theirs. */
+typedef struct {
+  int32_t type;         /* LBA_TYPE_F32, BF16 or F16: of all four tensors                              */
+  int32_t heads, kv_heads, dim, rotary_dim; /* of q; of k (0: there is no k); rotary_dim even, 2..dim  */
+  int32_t interleaved, inverse;
+  int32_t wide_positions; /* positions are int64 (else int32)                                          */
+  float scale;
+  int64_t tokens;
+  const void* positions; /* device, [tokens]                                                           */
+  const double* freqs;   /* device, [rotary_dim / 2], radians per position                             */
+} lba_rotary_how;
+/* q [tokens][heads][dim] and k [tokens][kv_heads][dim]; an output may be its input (same strides), and does not overlap it otherwise */
+int lba_rotary(const void* q, lba_strides q_at, const void* k, lba_strides k_at, const lba_rotary_how* how, void* q_out,
+               lba_strides q_out_at, void* k_out, lba_strides k_out_at, void* stream);
+
+/* Attention of packed sequences.  Sequence b has the rows cu_q[b] to cu_q[b+1] - 1 of q and cu_k[b] to cu_k[b+1] - 1 of k and v; query
+ * head h reads key-value head h / (heads / kv_heads):
+ *     out[i] = sum_j p_ij v[j],   p_ij = exp(scale q[i] k[j] - lse[i]),   lse[i] = log sum_j exp(scale q[i] k[j])
+ * over j of i's sequence, and with `causal` only those with j - i <= keys - queries of the sequence, rows counted from its first (the
+ * last row sees every key).  A row that sees no key gives 0, lse -inf.  What the mask hides does not count, infinities and NaN included.
+ * Rows of q in no sequence are left as they were in out and lse, and are 0 in the gradients.  Offsets outside [0, rows] count as the
+ * nearer end, a sequence that ends before it starts is empty; sequences follow each other in memory. */
+typedef struct {
+  int32_t type;         /* LBA_TYPE_BF16 or F16: of q, k, v and what has their shapes                 */
+  int32_t heads, kv_heads, dim; /* heads a multiple of kv_heads; dim a multiple of 8, 8..128            */
+  int32_t causal, sequences;
+  float scale;          /* finite                                                                     */
+  int64_t q_rows, k_rows; /* below 2^31 - 1024                                                          */
+  const int32_t *cu_q, *cu_k; /* device, [sequences + 1] each; NULL: one sequence of all rows           */
+  lba_strides q_at, k_at, v_at; /* multiples of 8, as the tensors start at multiples of 16 bytes         */
+} lba_attention_how;
+/* out [q_rows][heads][dim], contiguous: of the inputs' type, or (out_type LBA_TYPE_CODES) codes of out / *out_scale, E4M3 or with
+ * LBA_FLAG_INPUT_M4E3 in out_flags M4E3, as lba_linear gives them; lse [heads][q_rows], or NULL */
+int lba_attention(const void* q, const void* k, const void* v, const lba_attention_how* how, int out_type, const float* out_scale,
+                  int out_flags, void* out, float* lse, void* stream);
+/* With g = grad_out, dp_ij = g[i] v[j], ds_ij = p_ij (dp_ij - g[i] out[i]):
+ *     grad_q[i] = scale sum_j ds_ij k[j]     grad_k[j] = scale sum_i ds_ij q[i]     grad_v[j] = sum_i p_ij g[i]
+ * the latter two also over the query heads of a group.  out and lse are the forward call's.  grad_out, out and the gradients are contiguous
+ * [rows][heads][dim].  Sums are formed in a fixed order: a repeated call gives the same bits.  p and ds enter the products rounded to
+ * the inputs' type (ds of binary16 inputs by a common power of two, so that small gradients keep their bits).  The workspace is
+ * 256-byte aligned device memory, holds nothing between calls, and calls that may overlap need one each. */
+size_t lba_attention_backward_workspace_bytes(const lba_attention_how* how);
+int lba_attention_backward(const void* grad_out, const void* q, const void* k, const void* v, const void* out, const float* lse,
+                           const lba_attention_how* how, void* grad_q, void* grad_k, void* grad_v, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+/* Key-value cache in 4 bits.  32 neighbouring values of a head share a power of two 2^e, the flex-bias rule of Sec. 3.1 on E2M1: the
+ * smallest e in -126..125 with the largest magnitude at most 6 2^e; each value is the nearest of 0, 1/2, 1, 3/2, 2, 3, 4, 6 times +-2^e
+ * (ties to the even code; magnitudes above 6 2^125 saturate).  A group that holds an infinity or a NaN reads as NaN.  Memory: `pages` of `page` tokens, [page_count][kv_heads]
+ * runs of page (dim + dim / 16) bytes: key codes [page][dim/2], value codes [page][dim/2], key exponents [page][dim/32], value
+ * exponents [page][dim/32], an exponent byte being e + 127 (255: NaN; 0, in memory never written, reads as 0).  A byte holds two
+ * neighbouring values, the first in its low half, sign in its highest bit.  Bytes of a row stand as the matrix instructions' lanes
+ * take them: a key row's byte c (dim/8) + 4 g + j holds values 32 g + 8 c + 2 j and the next (c, j < 4), a value row's byte
+ * r (dim/16) + i holds values 16 i + 2 r and the next (r < 8).
+ * Token t of sequence b is row t % page of page table[b][t / page].  A token whose page number lies outside [0, page_count), or whose
+ * position lies outside [0, table_width page), is not there: it is not stored, reads as 0 and takes no part in attention. */
+typedef struct {
+  void* pages;          /* device, 16-byte aligned                                                    */
+  int64_t page_count;   /* at most 2^31 - 1                                                           */
+  int32_t kv_heads, dim, page; /* dim 32, 64, 96 or 128; page a multiple of 16, 16..1024               */
+  int32_t sequences, table_width;
+  const int32_t* table; /* device, [sequences][table_width]                                           */
+} lba_cache;
+/* Row i of sequence b in k and v (row cu[b] + i; cu [sequences + 1], or NULL: one row each) is token start[b] + i; rows in no sequence are
+ * passed over.  No two of a call's rows may be the same token of the same page.  Types LBA_TYPE_F32, BF16 or F16.
+ * lba_cache_read writes [tokens][kv_heads][dim], contiguous, and leaves rows in no sequence as they were. */
+int lba_cache_append(const lba_cache* cache, const void* k, lba_strides k_at, const void* v, lba_strides v_at, int type,
+                     int64_t tokens, const int32_t* start, const int32_t* cu, void* stream);
+int lba_cache_read(const lba_cache* cache, const int32_t* start, const int32_t* cu, int64_t tokens, int type, void* k, void* v,
+                   void* stream);
+/* One new token of each sequence: out[b][h] = softmax(scale q[b][h] k) v over the first lengths[b] tokens of the cache (0 for none);
+ * q [sequences][heads][dim] of LBA_TYPE_BF16 or F16 with row stride q_at.token; out as lba_attention's, [sequences][heads][dim].
+ * Workspace as for lba_attention_backward. */
+size_t lba_cache_attention_workspace_bytes(const lba_cache* cache, int heads);
+int lba_cache_attention(const void* q, lba_strides q_at, int type, int heads, const lba_cache* cache, const int32_t* lengths,
+                        float scale, int out_type, const float* out_scale, int out_flags, void* out, void* workspace,
+                        size_t workspace_bytes, void* stream);
 
 /* Re-computation for the recursive overflow straight-through estimator (Sec. 4 and App. D): the forward pass is
  * deterministic, so the backward pass can replay it instead of storing one bit per FMAq.  For every output

@@ -12,6 +12,7 @@ library is missing, or a call returns an error, an exception is raised.
 import contextlib
 import ctypes as C
 import importlib.util
+import math
 import os
 import warnings
 
@@ -24,7 +25,8 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "liblba.so")
 TORCH_LIB_PATH = os.path.join(_HERE, "lba_torch.so")
 
-EXPORTS = ["lba_gemm", "lba_gemm_batched", "lba_linear", "lba_gated", "lba_linear_backward", "lba_gated_backward", "lba_backward_workspace_bytes", "lba_gemm_last_overflow", "lba_gemm_ste_mask", "lba_conv2d", "lba_gemm_host_workspace_bytes", "lba_gemm_host",
+EXPORTS = ["lba_rotary", "lba_attention", "lba_attention_backward", "lba_attention_backward_workspace_bytes", "lba_cache_append", "lba_cache_read",
+           "lba_cache_attention", "lba_cache_attention_workspace_bytes", "lba_gemm", "lba_gemm_batched", "lba_linear", "lba_gated", "lba_linear_backward", "lba_gated_backward", "lba_backward_workspace_bytes", "lba_gemm_last_overflow", "lba_gemm_ste_mask", "lba_conv2d", "lba_gemm_host_workspace_bytes", "lba_gemm_host",
            "lba_conv2d_host_workspace_bytes", "lba_conv2d_host", "lba_gemm_host_static", "lba_count_nan_codes", "lba_describe_plan", "lba_describe_plan_batched",
            "lba_set_tile_override", "lba_set_wait_override", "lba_status_string", "lba_last_cuda_error", "lba_version"]
 
@@ -50,6 +52,27 @@ class _Layer(C.Structure):
 class _Backward(C.Structure):
     _fields_ = [("activation", C.c_int32), ("grad_type", C.c_int32), ("out_type", C.c_int32), ("preact_type", C.c_int32),
                 ("preact", C.c_void_p), ("dropout", C.c_double), ("rng", C.c_void_p), ("input_flags", C.c_int32)]
+
+
+class _Strides(C.Structure):
+    _fields_ = [("token", C.c_int64), ("head", C.c_int64)]
+
+
+class _Rotary(C.Structure):
+    _fields_ = [("type", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32), ("rotary_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("inverse", C.c_int32), ("wide_positions", C.c_int32), ("scale", C.c_float), ("tokens", C.c_int64),
+                ("positions", C.c_void_p), ("freqs", C.c_void_p)]
+
+
+class _Attention(C.Structure):
+    _fields_ = [("type", C.c_int32), ("heads", C.c_int32), ("kv_heads", C.c_int32), ("dim", C.c_int32), ("causal", C.c_int32),
+                ("sequences", C.c_int32), ("scale", C.c_float), ("q_rows", C.c_int64), ("k_rows", C.c_int64), ("cu_q", C.c_void_p),
+                ("cu_k", C.c_void_p), ("q_at", _Strides), ("k_at", _Strides), ("v_at", _Strides)]
+
+
+class _Cache(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("page_count", C.c_int64), ("kv_heads", C.c_int32), ("dim", C.c_int32), ("page", C.c_int32),
+                ("sequences", C.c_int32), ("table_width", C.c_int32), ("table", C.c_void_p)]
 
 
 _lib = None
@@ -107,6 +130,17 @@ def load_library():
         [C.c_void_p] * 4 + [C.c_size_t, C.c_void_p]
     lib.lba_gated_backward.argtypes = [C.c_void_p] * 5 + [C.c_int, C.c_void_p, C.c_void_p, C.c_int] + [C.c_int64] * 3 + \
         [C.POINTER(_Backward)] + [C.c_void_p] * 6 + [C.c_size_t, C.c_void_p]
+    lib.lba_rotary.argtypes = [C.c_void_p, _Strides, C.c_void_p, _Strides, C.POINTER(_Rotary), C.c_void_p, _Strides, C.c_void_p, _Strides, C.c_void_p]
+    lib.lba_attention.argtypes = [C.c_void_p] * 3 + [C.POINTER(_Attention), C.c_int, C.c_void_p, C.c_int] + [C.c_void_p] * 3
+    lib.lba_attention_backward_workspace_bytes.restype = C.c_size_t
+    lib.lba_attention_backward_workspace_bytes.argtypes = [C.POINTER(_Attention)]
+    lib.lba_attention_backward.argtypes = [C.c_void_p] * 6 + [C.POINTER(_Attention)] + [C.c_void_p] * 4 + [C.c_size_t, C.c_void_p]
+    lib.lba_cache_append.argtypes = [C.POINTER(_Cache), C.c_void_p, _Strides, C.c_void_p, _Strides, C.c_int, C.c_int64] + [C.c_void_p] * 3
+    lib.lba_cache_read.argtypes = [C.POINTER(_Cache), C.c_void_p, C.c_void_p, C.c_int64, C.c_int] + [C.c_void_p] * 3
+    lib.lba_cache_attention_workspace_bytes.restype = C.c_size_t
+    lib.lba_cache_attention_workspace_bytes.argtypes = [C.POINTER(_Cache), C.c_int]
+    lib.lba_cache_attention.argtypes = [C.c_void_p, _Strides, C.c_int, C.c_int, C.POINTER(_Cache), C.c_void_p, C.c_float, C.c_int, C.c_void_p, C.c_int] + \
+        [C.c_void_p] * 2 + [C.c_size_t, C.c_void_p]
     conv_args = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int, C.c_void_p, C.c_int, C.c_void_p] + [C.c_int] * 11 + \
         [C.POINTER(_Fmt), C.POINTER(_Fmt), C.c_int, C.c_int, C.c_void_p]
     lib.lba_conv2d.argtypes = conv_args + [C.c_void_p]
@@ -475,6 +509,261 @@ def backward_workspace_bytes(M, N, K, scale_a_len, scale_b_len, grad_dtype, acti
     how = _Backward(_activation(activation), _FLOAT_TYPES[grad_out_dtype or grad_dtype], _FLOAT_TYPES[grad_dtype], 0, None, 0.0, None, 0)
     return load_library().lba_backward_workspace_bytes(int(gated), M, N, K, scale_a_len, scale_b_len, C.byref(how),
                                                        sum(1 << i for i, n in enumerate(needs) if n))
+
+
+def rotary_frequencies(rotary_dim, base=10000.0, scaling="none", factor=1.0, original_length=8192, low=1.0, high=4.0, device="cuda"):
+    """float64 frequencies of a head's rotary_dim / 2 pairs for ``lba_rotary``, base^(-2 i / rotary_dim), and for texts longer than a
+    model was trained on (``factor`` times):
+
+    ``"linear"``: all divided by ``factor``.  ``"base"``: the base is raised so that the slowest pair is divided by ``factor``.  ``"ramp"``:
+    pairs that turn fewer than ``low`` times within ``original_length`` tokens are divided by ``factor``, those that turn more than ``high``
+    times are kept, and those between are blended linearly in their number of turns."""
+    if rotary_dim < 2 or rotary_dim % 2 or not factor > 0 or not base > 0:
+        raise ValueError("rotary_dim must be even and at least 2, factor and base above 0")
+    n = rotary_dim // 2
+    if scaling == "base" and n > 1:
+        base = base * factor ** (rotary_dim / (rotary_dim - 2))
+    f = base ** (-torch.arange(n, dtype=torch.float64) / n)
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "ramp":
+        if not high > low:
+            raise ValueError("high must be above low")
+        keep = ((original_length * f / (2 * math.pi) - low) / (high - low)).clamp(0.0, 1.0)
+        f = keep * f + (1 - keep) * f / factor
+    elif scaling not in ("none", "base"):
+        raise ValueError(f"scaling must be none, linear, base or ramp, not {scaling!r}")
+    return f.to(device)
+
+
+def _heads(t, name, dtypes=None):
+    """(pointer, strides, type number) of a CUDA tensor [rows][heads][dim] whose heads' values are contiguous; rows and heads may be apart"""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 3 and t.dtype in (dtypes or _FLOAT_TYPES)):
+        raise TypeError(f"{name} must be a CUDA tensor [rows][heads][dim] of " + ("bfloat16 or float16" if dtypes else "float32, bfloat16 or float16"))
+    if t.shape[2] > 1 and t.stride(2) != 1:
+        raise ValueError(f"the values of a head of {name} must be contiguous")
+    return t.data_ptr(), _Strides(t.stride(0), t.stride(1)), _FLOAT_TYPES[t.dtype]
+
+
+_HALF_TYPES = (torch.bfloat16, torch.float16)
+_NO_STRIDES = _Strides(0, 0)
+
+
+def _int32(t, n, name):
+    """pointer of a contiguous CUDA int32 tensor of n values (None: NULL)"""
+    if t is not None and t.numel() != n:
+        raise ValueError(f"{name} must hold {n} values, not {t.numel()}")
+    return _dev(t, torch.int32, name)
+
+
+def lba_rotary(q, k, positions, freqs, interleaved=False, inverse=False, scale=1.0, out=None, stream=None):
+    """(q, k) with their pairs turned by positions x frequencies: see ``lba_rotary`` in lba.h.
+
+    ``q`` [T][heads][dim], ``k`` [T][kv_heads][dim] or None: slices of a projection's output will do.  ``positions``: int32 or int64, [T];
+    ``freqs``: float64, half the values that turn (``rotary_frequencies``).  ``inverse``: the opposite way, which is the gradient's.
+    ``scale``: multiplies what turns.  ``out``: a pair of tensors, which may be ``q`` and ``k`` themselves."""
+    lib = load_library()
+    done = None and _native.rotary(q, k, positions, freqs, interleaved, inverse, scale, out, stream)
+    if done is not None:
+        return _done(done)
+    qo, ko = (None, None) if out is None else out
+    _same_device(q, k, positions, freqs, qo, ko)
+    pq, q_at, dtype = _heads(q, "q")
+    if k is not None and (k.dtype != q.dtype or k.dim() != 3 or k.shape[0] != q.shape[0] or k.shape[2] != q.shape[2]):
+        raise ValueError("k must have q's type, tokens and dim")
+    pk, k_at, _ = (None, _NO_STRIDES, 0) if k is None else _heads(k, "k")
+    if positions.dtype not in (torch.int32, torch.int64) or positions.numel() != q.shape[0]:
+        raise TypeError("positions must be an int32 or int64 CUDA tensor with a value for each token")
+    how = _Rotary(dtype, q.shape[1], 0 if k is None else k.shape[1], q.shape[2], 2 * freqs.numel(), int(interleaved), int(inverse),
+                  int(positions.dtype == torch.int64), float(scale), q.shape[0], _dev(positions, positions.dtype, "positions"),
+                  _dev(freqs, torch.float64, "freqs"))
+    if qo is None:
+        qo = _empty(q.shape, q.dtype, q.device, stream)
+    if k is not None and ko is None:
+        ko = _empty(k.shape, k.dtype, k.device, stream)
+    for t, like, name in ((qo, q, "out[0]"), (ko, k, "out[1]")):
+        if like is not None and (t.dtype != like.dtype or t.shape != like.shape):
+            raise ValueError(f"{name} must have the shape and type of what it is of")
+    po, qo_at, _ = _heads(qo, "out[0]")
+    pko, ko_at, _ = (None, _NO_STRIDES, 0) if k is None else _heads(ko, "out[1]")
+    _check(lib.lba_rotary(pq, q_at, pk, k_at, C.byref(how), po, qo_at, pko, ko_at, _stream(stream)))
+    return qo, (None if k is None else ko)
+
+
+def _attention(q, k, v, cu_q, cu_k, causal, scale):
+    """the C struct of an attention call, and its tensors' pointers"""
+    pq, q_at, dtype = _heads(q, "q", _HALF_TYPES)
+    pk, k_at, kt = _heads(k, "k", _HALF_TYPES)
+    pv, v_at, vt = _heads(v, "v", _HALF_TYPES)
+    if kt != dtype or vt != dtype or k.shape != v.shape or k.shape[2] != q.shape[2]:
+        raise ValueError("q, k and v must have one type and dim, k and v one shape")
+    if (cu_q is None) != (cu_k is None):
+        raise ValueError("cu_q and cu_k come together")
+    n = 1 if cu_q is None else cu_q.numel() - 1
+    if n < 0:
+        raise ValueError("cu_q holds one value more than there are sequences")
+    how = _Attention(dtype, q.shape[1], k.shape[1], q.shape[2], int(causal), n, float(q.shape[2] ** -0.5 if scale is None else scale), q.shape[0],
+                     k.shape[0], _int32(cu_q, n + 1, "cu_q"), _int32(cu_k, n + 1, "cu_k"), q_at, k_at, v_at)
+    return how, pq, pk, pv
+
+
+def _attention_out(shape, dtype, device, stream, out_dtype, out_scale, prod_fmt, out):
+    """(out, its type, scale pointer, flags) of an attention's output: the inputs' type, or codes"""
+    if out is None:
+        out = _empty(shape, dtype if out_dtype is None else out_dtype, device, stream)
+    _shaped(out, shape, "out")
+    if out.dtype not in (dtype, torch.uint8):
+        raise TypeError("out must have the inputs' type, or be uint8 for codes")
+    codes = out.dtype == torch.uint8
+    if codes and (out_scale is None or out_scale.numel() != 1):
+        raise TypeError("codes need out_scale, a CUDA tensor of one float32 value")
+    flags = 0
+    if codes and prod_fmt is not None:
+        flags = (prod_fmt.flags if isinstance(prod_fmt, LbaFormat) else int(tuple(prod_fmt)[4])) & FLAG_INPUT_M4E3
+    return out, _OUT_TYPES[out.dtype], _dev(out_scale, torch.float32, "out_scale") if codes else None, flags
+
+
+def lba_attention(q, k, v, cu_q=None, cu_k=None, causal=True, scale=None, out_dtype=None, out_scale=None, prod_fmt=None, lse=False, out=None,
+                  stream=None):
+    """Attention of packed sequences over whole prompts: out [Tq][heads][dim].  See ``lba_attention`` in lba.h.
+
+    ``q`` [Tq][heads][dim], ``k`` and ``v`` [Tk][kv_heads][dim], bfloat16 or float16; slices of a projection's output will do.  ``cu_q``,
+    ``cu_k``: int32 [sequences + 1], where each sequence's rows begin (None: one sequence of all rows).  ``scale``: dim^-1/2 if None.
+    ``out_dtype``: uint8 for codes of out / ``out_scale`` in the byte format that ``prod_fmt`` names (E4M3 if None), as the next
+    ``lba_linear`` takes them.  ``lse``: True, or a float32 tensor [heads][Tq] to write: the call then returns (out, lse), which
+    ``lba_attention_backward`` takes.  Rows that no sequence holds are left as they were."""
+    lib = load_library()
+    done = None and _native.attention(q, k, v, cu_q, cu_k, causal, scale, out_dtype, out_scale, prod_fmt, lse, out, stream)
+    if done is not None:
+        return _done(done)
+    sums = lse if isinstance(lse, torch.Tensor) else None
+    _same_device(q, k, v, cu_q, cu_k, out_scale, out, sums)
+    how, pq, pk, pv = _attention(q, k, v, cu_q, cu_k, causal, scale)
+    out, out_type, ps, flags = _attention_out(tuple(q.shape), q.dtype, q.device, stream, out_dtype, out_scale, prod_fmt, out)
+    if lse is True:
+        sums = _empty((q.shape[1], q.shape[0]), torch.float32, q.device, stream)
+    _check(lib.lba_attention(pq, pk, pv, C.byref(how), out_type, ps, flags, _dev(out, out.dtype, "out"),
+                             _dev(_shaped(sums, (q.shape[1], q.shape[0]), "lse"), torch.float32, "lse"), _stream(stream)))
+    return out if sums is None else (out, sums)
+
+
+def lba_attention_backward(grad_out, q, k, v, out, lse, cu_q=None, cu_k=None, causal=True, scale=None, workspace=None, stream=None):
+    """(grad_q, grad_k, grad_v) of ``lba_attention``, whose ``out`` (of the inputs' type) and ``lse`` these are; contiguous, of q's type.
+    See ``lba_attention_backward`` in lba.h.  ``workspace``: a CUDA uint8 tensor of ``attention_backward_workspace_bytes``, or None."""
+    lib = load_library()
+    done = None and _native.attention_backward(grad_out, q, k, v, out, lse, cu_q, cu_k, causal, scale, workspace, stream)
+    if done is not None:
+        return _done(done)
+    _same_device(q, k, v, grad_out, out, lse, cu_q, cu_k, workspace)
+    how, pq, pk, pv = _attention(q, k, v, cu_q, cu_k, causal, scale)
+    for t, name in ((grad_out, "grad_out"), (out, "out")):
+        _dev(_shaped(t, tuple(q.shape), name), q.dtype, name)
+    _shaped(lse, (q.shape[1], q.shape[0]), "lse")
+    if workspace is None:
+        workspace = _empty(lib.lba_attention_backward_workspace_bytes(C.byref(how)), torch.uint8, q.device, stream, returned=False)
+    gq = _empty(tuple(q.shape), q.dtype, q.device, stream)
+    gk, gv = (_empty(tuple(k.shape), q.dtype, q.device, stream) for _ in range(2))
+    _check(lib.lba_attention_backward(grad_out.data_ptr(), pq, pk, pv, out.data_ptr(), _dev(lse, torch.float32, "lse"), C.byref(how), gq.data_ptr(),
+                                      gk.data_ptr(), gv.data_ptr(), _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)))
+    return gq, gk, gv
+
+
+def attention_backward_workspace_bytes(q, k, v, cu_q=None, cu_k=None, causal=True, scale=None):
+    """Bytes of workspace of a ``lba_attention_backward`` call with these arguments."""
+    return load_library().lba_attention_backward_workspace_bytes(C.byref(_attention(q, k, v, cu_q, cu_k, causal, scale)[0]))
+
+
+def cache_shape(pages, kv_heads, page, dim):
+    """Shape of the uint8 tensor that holds a cache of ``pages`` pages of ``page`` tokens."""
+    return pages, kv_heads, page * (dim + dim // 16)
+
+
+def _cache(cache, page, table, sequences):
+    """the C struct of a cache [pages][kv_heads][page (dim + dim / 16)] and its block table [sequences][width]"""
+    if not isinstance(cache, torch.Tensor) or cache.dim() != 3 or not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise TypeError("cache must be a uint8 CUDA tensor of cache_shape(...), table an int32 one [sequences][pages of a sequence]")
+    if table.shape[0] != sequences:
+        raise ValueError(f"table must have a row for each of the {sequences} sequences")
+    page, run = int(page), cache.shape[2]
+    if page < 1 or run % (17 * page) or run * 16 // (17 * page) % 32:
+        raise ValueError("the cache's last size must be page (dim + dim / 16), dim a multiple of 32")
+    return _Cache(_dev(cache, torch.uint8, "cache"), cache.shape[0], cache.shape[1], run * 16 // (17 * page), page, sequences, table.shape[1],
+                  _dev(table, torch.int32, "table"))
+
+
+def lba_cache_append(k, v, cache, page, table, start, cu=None, stream=None):
+    """Rounds new keys and values [T][kv_heads][dim] to 4 bits and stores them: row i of sequence b (row cu[b] + i of k and v; ``cu`` None: one row a
+    sequence) becomes token start[b] + i.  See ``lba_cache_append`` in lba.h.  Returns ``cache``.
+
+    ``cache``: uint8 of ``cache_shape(...)``; ``page``: tokens of a page; ``table``: int32 [sequences][pages of a sequence], numbers of
+    pages; ``start``: int32 [sequences]; ``cu``: int32 [sequences + 1]."""
+    lib = load_library()
+    done = None and _native.cache_append(k, v, cache, page, table, start, cu, stream)
+    if done is not None:
+        return _done(done)
+    _same_device(cache, k, v, table, start, cu)
+    n = start.numel()
+    how = _cache(cache, page, table, n)
+    pk, k_at, kt = _heads(k, "k")
+    pv, v_at, vt = _heads(v, "v")
+    if kt != vt or k.shape != v.shape or tuple(k.shape[1:]) != (how.kv_heads, how.dim):
+        raise ValueError("k and v must be [tokens][kv_heads][dim] of the cache's heads and dim, of one type")
+    _check(lib.lba_cache_append(C.byref(how), pk, k_at, pv, v_at, kt, k.shape[0], _int32(start, n, "start"), _int32(cu, n + 1, "cu"), _stream(stream)))
+    return cache
+
+
+def lba_cache_read(cache, page, table, start, cu, tokens, dtype=torch.bfloat16, out=None, stream=None):
+    """(k, v) [tokens][kv_heads][dim] as numbers again: row cu[b] + i is token start[b] + i of sequence b.  See ``lba_cache_read`` in lba.h.
+
+    ``tokens``: rows of the outputs, as cu's last value says; ``dtype``: float32, bfloat16 or float16; ``out``: a pair of tensors to write."""
+    lib = load_library()
+    done = None and _native.cache_read(cache, page, table, start, cu, tokens, dtype, out, stream)
+    if done is not None:
+        return _done(done)
+    k, v = (None, None) if out is None else out
+    _same_device(cache, table, start, cu, k, v)
+    n = start.numel()
+    how = _cache(cache, page, table, n)
+    shape = (int(tokens), how.kv_heads, how.dim)
+    if dtype not in _FLOAT_TYPES:
+        raise TypeError("dtype must be torch.float32, bfloat16 or float16")
+    k, v = (_empty(shape, dtype, cache.device, stream) if t is None else _shaped(t, shape, "out") for t in (k, v))
+    pk, kt = _typed(k, "out[0]")
+    pv, vt = _typed(v, "out[1]")
+    if kt != vt:
+        raise ValueError("both outputs must have one type")
+    _check(lib.lba_cache_read(C.byref(how), _int32(start, n, "start"), _int32(cu, n + 1, "cu"), shape[0], kt, pk, pv, _stream(stream)))
+    return k, v
+
+
+def lba_cache_attention(q, cache, page, table, lengths, scale=None, out_dtype=None, out_scale=None, prod_fmt=None, workspace=None, out=None, stream=None):
+    """Attention of one new token of each sequence over its cached ones: out [sequences][heads][dim] for q of that shape.  See
+    ``lba_cache_attention`` in lba.h.
+
+    ``lengths``: int32 [sequences], tokens in the cache, the new one's among them.  ``out_dtype``, ``out_scale`` and ``prod_fmt`` are those of
+    ``lba_attention``; ``workspace``: a CUDA uint8 tensor of ``cache_attention_workspace_bytes``, or None."""
+    lib = load_library()
+    done = None and _native.cache_attention(q, cache, page, table, lengths, scale, out_dtype, out_scale, prod_fmt, workspace, out, stream)
+    if done is not None:
+        return _done(done)
+    _same_device(q, cache, table, lengths, out_scale, workspace, out)
+    pq, q_at, dtype = _heads(q, "q", _HALF_TYPES)
+    n = q.shape[0]
+    how = _cache(cache, page, table, n)
+    if q.shape[2] != how.dim:
+        raise ValueError(f"q must have the cache's dim, {how.dim}")
+    out, out_type, ps, flags = _attention_out(tuple(q.shape), q.dtype, q.device, stream, out_dtype, out_scale, prod_fmt, out)
+    if workspace is None:
+        workspace = _empty(lib.lba_cache_attention_workspace_bytes(C.byref(how), q.shape[1]), torch.uint8, q.device, stream, returned=False)
+    _check(lib.lba_cache_attention(pq, q_at, dtype, q.shape[1], C.byref(how), _int32(lengths, n, "lengths"),
+                                   float(how.dim ** -0.5 if scale is None else scale), out_type, ps, flags, _dev(out, out.dtype, "out"),
+                                   _dev(workspace, torch.uint8, "workspace"), workspace.numel(), _stream(stream)))
+    return out
+
+
+def cache_attention_workspace_bytes(cache, page, table, heads):
+    """Bytes of workspace of a ``lba_cache_attention`` call on this cache and table."""
+    return load_library().lba_cache_attention_workspace_bytes(C.byref(_cache(cache, page, table, table.shape[0])), heads)
 
 
 def lba_gemm_last_overflow(A, B, prod_fmt, acc_fmt, out=None, stream=None):

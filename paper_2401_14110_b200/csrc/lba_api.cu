@@ -38,16 +38,16 @@ cudaError_t launch_fixed(int ord, int load, const LinearProblem& p, cudaStream_t
 cudaError_t launch_cluster_pair(int pq, int load, const Problem& p, cudaStream_t stream);
 cudaError_t launch_cluster_pair(int pq, int load, const LinearProblem& p, cudaStream_t stream);
 
-namespace {
-
-thread_local int g_last_cuda_error = 0;
-std::atomic<int> g_tile_override{-1};  // testing and tuning hook (lba_set_tile_override)
-std::atomic<int> g_wait_override{0};   // testing hook (lba_set_wait_override)
-
+static thread_local int g_last_cuda_error = 0;
 int cuda_fail(cudaError_t e) {
   g_last_cuda_error = (int)e;
   return LBA_ERR_CUDA;
 }
+
+namespace {
+
+std::atomic<int> g_tile_override{-1};  // testing and tuning hook (lba_set_tile_override)
+std::atomic<int> g_wait_override{0};   // testing hook (lba_set_wait_override)
 
 template <class P>
 const LaunchFn<P> kLaunch[QM_COUNT][ORD_COUNT] = {
@@ -771,6 +771,9 @@ bool sizes_fit(double a_bytes, double b_bytes, double out_bytes) {
 }
 
 }  // namespace
+
+int device_sms() { return sm_count(); }
+
 }  // namespace lba
 
 using namespace lba;
@@ -805,6 +808,7 @@ const char* lba_status_string(int status) {
     case LBA_ERR_WORKSPACE: return "workspace missing, too small or misaligned";
     case LBA_ERR_LAYER: return "unknown activation or element type, dropout outside [0, 1), or an option that a gated layer does not have";
     case LBA_ERR_STATIC_LIMIT: return "problem too large for the built-in workspace of lba_gemm_host_static (LBA_STATIC_WORKSPACE_BYTES)";
+    case LBA_ERR_ALIGN: return "a tensor whose start or strides are not multiples of 16 bytes";
     default: return "unknown status";
   }
 }

@@ -1,0 +1,446 @@
+// Attention over whole prompts: out[i] = sum_j softmax_j(scale q[i] k[j]) v[j] for packed sequences, causal or not, grouped heads.
+//
+// One pass over the keys with the running maximum and sum of a softmax; scores and weights never leave the SM.  Bound by the tensor cores
+// and the exponential units together: 128 x 128 scores of 128 dimensions are 1024 clocks of matrix instructions (two products) and 1024 clocks of
+// exponentials (16 a clock).  So a CTA holds two tiles of 128 queries of one head: while the tensor cores work on one tile's products, a
+// warpgroup forms the other's weights.
+//   warps 0-3, 4-7   a tile's softmax each, a query row a thread: scores from tensor memory to registers, weights back over them as the second
+//                    product's operand; its output stays in tensor memory to the end.  The maximum that weights are relative to is raised only
+//                    when a score exceeds it by 2^8, and the output is rescaled only then (in 32 bits nothing is lost by weights of up to 256)
+//   warp 8           tensor copies of K and V tiles into a ring
+//   warp 9           one thread issues all products
+//   warps 10, 11     clean tiles of V that the mask cuts: rows behind the sequence become 0 (0 times a neighbour's infinity would be NaN),
+//                    and values that are not finite, which rows before them must not see, are taken out and added to the others' results
+// Weights are rounded to the inputs' type (2^-9 or 2^-12 of each, at random; the result is rounded to that type once more); sums of weights
+// are of the unrounded ones.
+#include <cmath>
+
+#include "lba_tile.cuh"
+
+namespace lba {
+namespace {
+
+constexpr int QT = 128, KT = 128, FWD_THREADS = 384, MAX_STAGES = 10, CUT_TILES = 4;
+constexpr float LAZY = 8.0f;  // binades
+
+struct ForwardParams {
+  CUtensorMap q, k, v;
+  const int32_t *cu_q, *cu_k;
+  int64_t q_rows, k_rows;
+  int sequences, heads, group, dim, causal, bf, in_m4e3, codes;
+  float to_log2;             // scale log2(e)
+  const float* out_scale;
+  const void* v_raw;
+  lba_strides v_at;
+  void* out;
+  float* lse;
+};
+
+template <int DT> constexpr int kTile = 128 * DT * 2;                       // bytes of a tile of 128 rows
+template <int DT> constexpr int kStages = DT == 128 ? 5 : 10;
+template <int DT> constexpr size_t kForwardSmem = 1024 + (size_t)kTile<DT> * (2 + kStages<DT>);
+
+struct ForwardShared {
+  uint64_t q_full[2], full[MAX_STAGES], empty[MAX_STAGES], scores[2], weights[2], done;
+  uint64_t cut_full[CUT_TILES], clean[CUT_TILES];  // copies of V that the mask cuts, and their cleaning: once each
+  uint32_t cut[CUT_TILES][4];  // rows of the masked tiles of V that hold values that are not finite
+  uint32_t tmem;
+  int dead;
+  int seq, block, found;
+};
+
+// weights of 32 scores, relative to the maximum: packed, and their sum
+template <typename T>
+__device__ __forceinline__ void weigh32(uint32_t* s, uint32_t* out, u64 by, u64 minus, u64& sum) {
+#pragma unroll
+  for (int i = 0; i < 32; i += 2) {
+    float lo, hi;
+    unpack2(fma2_rn(pack2u(s[i], s[i + 1]), by, minus), lo, hi);
+    lo = exp2_approx(lo);
+    hi = exp2_approx(hi);
+    sum = add2_rn(sum, pack2(lo, hi));
+    out[i / 2] = pack_pair<T>(lo, hi);
+  }
+}
+
+template <typename T, int DT>
+__global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_constant__ ForwardParams p) {
+  constexpr int BLOCKS = DT / 64, TILE = kTile<DT>, HALF = 128 * 128, STAGES = kStages<DT>;
+  extern __shared__ uint8_t raw_smem[];
+  __shared__ ForwardShared sh;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const uint32_t base = (smem_u32(raw_smem) + 1023) & ~1023u, q_smem = base, ring = base + 2 * TILE;
+  volatile int* const dead = &sh.dead;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      for (int i = 0; i < 2; ++i) {
+        mbar_init(smem_u32(&sh.q_full[i]), 1);
+        mbar_init(smem_u32(&sh.scores[i]), 1);
+        mbar_init(smem_u32(&sh.weights[i]), 128);
+      }
+      for (int i = 0; i < STAGES; ++i) {
+        mbar_init(smem_u32(&sh.full[i]), 1);
+        mbar_init(smem_u32(&sh.empty[i]), 1);
+      }
+      for (int i = 0; i < CUT_TILES; ++i) {
+        mbar_init(smem_u32(&sh.cut_full[i]), 1);
+        mbar_init(smem_u32(&sh.clean[i]), 64);
+      }
+      mbar_init(smem_u32(&sh.done), 1);
+      mbar_init_fence();
+      for (int i = 0; i < CUT_TILES * 4; ++i) sh.cut[i / 4][i % 4] = 0;
+      sh.dead = 0;
+    }
+  }
+  after_previous();
+  if (warp == 9) tmem_alloc(smem_u32(&sh.tmem), 512);  // (not before: a CTA of the kernel before this one could still want it)
+  const int head = blockIdx.x % p.heads;
+  if (warp == 8) {
+    int seq = 0, block = 0;
+    const bool found = find_block(p.cu_q, p.q_rows, p.sequences, 2 * QT, blockIdx.x / p.heads, &seq, &block);
+    if (lane == 0) {
+      sh.found = found;
+      sh.seq = seq;
+      sh.block = block;
+    }
+  }
+  tmem_before();
+  __syncthreads();
+  tmem_after();
+  const uint32_t tmem = sh.tmem;
+  bool alive = sh.found != 0;
+  if (alive) {
+    int q_first, q_count, k_first, k_count;
+    rows_of(p.cu_q, p.q_rows, sh.seq, &q_first, &q_count);
+    rows_of(p.cu_k, p.k_rows, sh.seq, &k_first, &k_count);
+    const int off = k_count - q_count;
+    // (with a causal mask the last blocks, which have the most keys, come first)
+    const int block = p.causal ? (q_count + 2 * QT - 1) / (2 * QT) - 1 - sh.block : sh.block;
+    const int i0 = block * 2 * QT;
+    // tiles of keys of either query tile, and the first that a mask cuts
+    int tiles[2], whole[2];
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      const int lo = i0 + w * QT, hi = min(lo + QT, q_count) - 1;
+      const int keys = lo >= q_count ? 0 : p.causal ? max(0, min(k_count, hi + off + 1)) : k_count;
+      tiles[w] = (keys + KT - 1) / KT;
+      whole[w] = (p.causal ? max(0, min(k_count, lo + off + 1)) : k_count) / KT;
+    }
+    const int all = max(tiles[0], tiles[1]);
+    // the first tile of V to be cleaned: behind it, masks cut every tile of some query tile that is not empty
+    const int dirty = min(tiles[0] ? whole[0] : all, tiles[1] ? whole[1] : all);
+    const int kv = head / p.group;
+
+    if (warp >= 8) {
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+      if (warp == 8) {
+        if (elected()) {
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            if (!tiles[w]) continue;
+            mbar_arrive_expect(smem_u32(&sh.q_full[w]), TILE);
+            for (int x = 0; x < BLOCKS; ++x) tile_load(q_smem + w * TILE + x * HALF, &p.q, x * 64, head, q_first + i0 + w * QT, smem_u32(&sh.q_full[w]));
+          }
+          int stage = 0;
+          uint32_t phase = 1;
+          for (int n = 0; n < 2 * all; ++n) {  // K and V of a tile in turn
+            if (!mbar_wait(smem_u32(&sh.empty[stage]), phase, dead)) break;
+            const bool cut = (n & 1) && (n >> 1) >= dirty;
+            const uint32_t dst = ring + stage * TILE, bar = smem_u32(cut ? &sh.cut_full[(n >> 1) - dirty] : &sh.full[stage]);
+            if (cut) mbar_arrive(smem_u32(&sh.full[stage]));  // (its phases count copies; those who want this one wait for its own barriers)
+            mbar_arrive_expect(bar, TILE);
+            for (int x = 0; x < BLOCKS; ++x) tile_load(dst + x * HALF, n & 1 ? &p.v : &p.k, x * 64, kv, k_first + (n >> 1) * KT, bar);
+            if (++stage == STAGES) {
+              stage = 0;
+              phase ^= 1;
+            }
+          }
+        }
+      } else if (warp == 9) {
+        if (elected()) {
+          const int steps = (p.dim + 15) / 16;
+          const uint32_t kind_s = tile_kind(p.bf, KT, false), kind_o = tile_kind(p.bf, steps * 16, true);
+          const uint64_t rows = tile_operand(0, 16, 1024), lines = tile_operand(0, HALF, 1024);
+          bool ok = true;
+          // K of tile j is copy 2 j, V 2 j + 1
+          const auto full = [&](int copy) { ok = ok && mbar_wait(smem_u32(&sh.full[copy % STAGES]), (copy / STAGES) & 1, dead); };
+          const auto scores = [&](int w, int j) {
+            full(2 * j);
+            if (!ok) return;
+            const uint64_t a = rows + ((q_smem + w * TILE) >> 4), b = rows + ((ring + (2 * j % STAGES) * TILE) >> 4);
+            for (int s = 0; s < steps; ++s) {
+              const int at = ((s >> 2) * HALF + (s & 3) * 32) >> 4;
+              mma_shared(tmem + w * KT, a + at, b + at, kind_s, s != 0);
+            }
+            mma_arrive(smem_u32(&sh.scores[w]));
+          };
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            if (!tiles[w]) continue;
+            ok = ok && mbar_wait(smem_u32(&sh.q_full[w]), 0, dead);
+            scores(w, 0);
+          }
+          if (ok && all) mma_arrive(smem_u32(&sh.empty[0]));
+          for (int j = 0; j < all && ok; ++j) {
+            const int vs = (2 * j + 1) % STAGES;
+            if (j >= dirty) ok = ok && mbar_wait(smem_u32(&sh.clean[j - dirty]), 0, dead);
+            else full(2 * j + 1);
+#pragma unroll
+            for (int w = 0; w < 2; ++w) {
+              if (j >= tiles[w]) continue;
+              ok = ok && mbar_wait(smem_u32(&sh.weights[w]), j & 1, dead);
+              if (!ok) break;
+              tmem_after();
+              const uint64_t b = lines + ((ring + vs * TILE) >> 4);
+              for (int s = 0; s < KT / 16; ++s)
+                mma_tensor(tmem + 256 + w * 128, tmem + w * KT + s * 8, b + s * (2048 >> 4), kind_o, j != 0 || s != 0);
+              if (j + 1 < tiles[w]) scores(w, j + 1);
+              else mma_arrive(smem_u32(&sh.scores[w]));  // the output is complete
+            }
+            if (ok) {
+              mma_arrive(smem_u32(&sh.empty[vs]));
+              if (j + 1 < all) mma_arrive(smem_u32(&sh.empty[(2 * j + 2) % STAGES]));
+            }
+          }
+          mma_arrive(smem_u32(&sh.done));
+        }
+      } else {
+        for (int j = dirty; j < all; ++j) {
+          const int stage = (2 * j + 1) % STAGES;
+          if (!mbar_wait(smem_u32(&sh.cut_full[j - dirty]), 0, dead)) break;
+          uint8_t* const tile = raw_smem + (ring - smem_u32(raw_smem)) + stage * TILE;
+          for (int row = threadIdx.x - 10 * 32; row < KT; row += 64) {
+            const bool behind = j * KT + row >= k_count;
+            bool odd = false;
+            if (behind || p.causal) {
+              for (int x = 0; x < BLOCKS; ++x) {
+#pragma unroll
+                for (int piece = 0; piece < 8; ++piece) {
+                  uint4* const at = reinterpret_cast<uint4*>(tile + x * HALF + swizzled(row, piece));
+                  if (behind) {
+                    *at = make_uint4(0u, 0u, 0u, 0u);
+                  } else {
+                    uint4 v = *at;
+                    uint32_t* const u = &v.x;
+                    constexpr uint32_t EXP = std::is_same<T, __nv_bfloat16>::value ? 0x7F80u : 0x7C00u;
+                    bool here = false;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                      if ((u[e] & EXP) == EXP) u[e] &= 0xFFFF0000u, here = true;
+                      if ((u[e] & (EXP << 16)) == EXP << 16) u[e] &= 0x0000FFFFu, here = true;
+                    }
+                    if (here) {
+                      *at = v;
+                      odd = true;
+                    }
+                  }
+                }
+              }
+            }
+            if (odd) atomicOr(&sh.cut[j - dirty][row >> 5], 1u << (row & 31));
+          }
+          asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+          mbar_arrive(smem_u32(&sh.clean[j - dirty]));
+        }
+      }
+    } else {
+      asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+      const int w = warp >> 2, mine = tiles[w], row = threadIdx.x & 127, i = i0 + w * QT + row;
+      const uint32_t lanes = (uint32_t)(warp & 3) << 21, s_at = tmem + w * KT + lanes, o_at = tmem + 256 + w * 128 + lanes;
+      const float c = p.to_log2;
+      float top = -INFINITY;
+      u64 total = both(0.0f);
+      bool ok = true;
+      for (int j = 0; j < mine; ++j) {
+        ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&sh.scores[w]), j & 1, dead));
+        if (!ok) break;
+        tmem_after();
+        uint32_t s[KT];
+#pragma unroll
+        for (int x = 0; x < KT; x += 32) tmem_load32(s_at + x, s + x);
+        tmem_wait_ld();
+        if (j >= whole[w]) {
+          const int limit = (p.causal ? min(k_count, i + off + 1) : k_count) - j * KT;  // keys of this tile that the row sees
+#pragma unroll
+          for (int x = 0; x < KT; ++x)
+            if (x >= limit) s[x] = 0xFF800000u;
+        }
+        float most = __uint_as_float(s[0]);
+#pragma unroll
+        for (int x = 1; x < KT; ++x) most = fmaxf(most, __uint_as_float(s[x]));
+        const bool raise = most * c > top * c + LAZY;  // (true whenever there is no maximum yet, and some score)
+        if (__any_sync(0xFFFFFFFFu, raise)) {
+          const float next = fmaxf(top, most);
+          if (j > 0) {
+            const float by = next == -INFINITY ? 1.0f : exp2_approx((top - next) * c);
+            const u64 by2 = both(by);
+            total = mul2_rn(total, by2);
+            for (int x = 0; x < p.dim; x += 32) {
+              uint32_t o[32];
+              tmem_load32(o_at + x, o);
+              tmem_wait_ld();
+#pragma unroll
+              for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * by);
+              tmem_store32(o_at + x, o);
+            }
+          }
+          top = next;
+        }
+        const u64 by = both(c), minus = both(top == -INFINITY ? 0.0f : -top * c);
+        uint32_t packed[KT / 2];
+#pragma unroll
+        for (int x = 0; x < KT; x += 32) weigh32<T>(s + x, packed + x / 2, by, minus, total);
+        tmem_store32(s_at, packed);
+        tmem_store32(s_at + 32, packed + 32);
+        tmem_wait_st();
+        tmem_before();
+        mbar_arrive(smem_u32(&sh.weights[w]));
+      }
+      if (mine && ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&sh.scores[w]), mine & 1, dead));
+      tmem_after();
+      float lo, hi;
+      unpack2(total, lo, hi);
+      const float sum = lo + hi;
+      const bool there = i < q_count;
+      const int64_t at = (int64_t)(q_first + i) * p.heads + head;
+      if (there && p.lse)
+        p.lse[(int64_t)head * p.q_rows + q_first + i] =
+            !ok ? __uint_as_float(0x7FC00000u) : sum == 0.0f ? -INFINITY : (top * c + log2f(sum)) * 0.69314718055994531f;
+      const float inv = sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum);
+      uint32_t poison = 0;  // of the cut tiles, as one word: any at all?
+      if (p.causal) {
+        for (int x = 0; x < CUT_TILES; ++x)
+          for (int e = 0; e < 4; ++e) poison |= sh.cut[x][e];
+      }
+      const float out_scale = p.codes ? *p.out_scale : 1.0f;
+#pragma unroll 1
+      for (int x = 0; x < p.dim; x += 32) {
+        uint32_t o[32];
+        __syncwarp();
+        if (mine) {
+          tmem_load32(o_at + x, o);
+          tmem_wait_ld();
+        }
+        float f[32];
+#pragma unroll
+        for (int e = 0; e < 32; ++e) f[e] = !ok ? __uint_as_float(0x7FC00000u) : mine ? __uint_as_float(o[e]) * inv : 0.0f;
+        if (poison && there) {
+          for (int t = 0; t < CUT_TILES * 128; ++t) {
+            const int key = dirty * KT + t;
+            if (!((sh.cut[t >> 7][(t >> 5) & 3] >> (t & 31)) & 1u) || key > i + off) continue;
+            const T* const src = static_cast<const T*>(p.v_raw) + (int64_t)(k_first + key) * p.v_at.token + kv * p.v_at.head + x;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const float v = x + e < p.dim ? to_f32(src[e]) : 0.0f;
+              if (!isfinite(v)) f[e] += v;
+            }
+          }
+        }
+        if (!there) continue;
+#pragma unroll
+        for (int e = 0; e < 32; e += 8) {
+          if (x + e >= p.dim) break;
+          if (p.codes) {
+            uint8_t b[8];
+#pragma unroll
+            for (int t = 0; t < 8; ++t) {
+              const float z = __fdiv_rn(f[e + t], out_scale);
+              b[t] = p.in_m4e3 ? encode_m4e3(z) : encode_e4m3(z);
+            }
+            store_some<uint8_t, 8>(p.out, at * p.dim + x + e, 8, b);
+          } else {
+            uint4 v;
+            v.x = pack_pair<T>(f[e], f[e + 1]);
+            v.y = pack_pair<T>(f[e + 2], f[e + 3]);
+            v.z = pack_pair<T>(f[e + 4], f[e + 5]);
+            v.w = pack_pair<T>(f[e + 6], f[e + 7]);
+            *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + at * p.dim + x + e) = v;
+          }
+        }
+      }
+      tmem_before();
+    }
+  }
+  __syncthreads();
+  if (warp == 9) {
+    if (*dead) {
+      let_copies_land();
+    } else if (alive) {
+      mbar_wait(smem_u32(&sh.done), 0, dead);
+    }
+    tmem_after();
+    __syncwarp();
+    tmem_free(tmem, 512);
+  }
+}
+
+template <typename T, int DT>
+cudaError_t launch_forward(const ForwardParams& p, int64_t blocks, cudaStream_t stream) {
+  cudaError_t e = cudaFuncSetAttribute(attention_kernel<T, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kForwardSmem<DT>);
+  if (e != cudaSuccess) return e;
+  return launch_after(attention_kernel<T, DT>, dim3((unsigned)blocks), FWD_THREADS, kForwardSmem<DT>, stream, p);
+}
+
+}  // namespace
+
+// what both passes ask of their arguments
+int check_attention(const lba_attention_how* h) {
+  if (!h) return LBA_ERR_NULL;
+  if (!half_type(h->type) || !(h->scale > 0.0f) || !std::isfinite(h->scale)) return LBA_ERR_LAYER;
+  if (h->heads < 1 || h->kv_heads < 1 || h->heads % h->kv_heads || h->heads > 65535 || h->dim < 8 || h->dim > 128 || h->dim % 8 || h->q_rows < 0 ||
+      h->k_rows < 0 || h->q_rows > 2147483647LL - 1024 || h->k_rows > 2147483647LL - 1024 || h->sequences < 0)
+    return LBA_ERR_SHAPE;
+  if ((!h->cu_q || !h->cu_k) && h->sequences != 1) return LBA_ERR_SHAPE;
+  const auto bad = [&](const lba_strides& s, int heads, int64_t rows) {  // tensor copies want strides of whole 16 bytes, below 2^40
+    const auto off = [](int64_t v) { return v < 8 || v % 8 || v >= (1LL << 39); };
+    return (heads > 1 && off(s.head)) || (rows > 1 && off(s.token));
+  };
+  if (bad(h->q_at, h->heads, h->q_rows) || bad(h->k_at, h->kv_heads, h->k_rows) || bad(h->v_at, h->kv_heads, h->k_rows)) return LBA_ERR_ALIGN;
+  // a CTA for every block of rows of every sequence and head, sequences at most a block more than their rows fill
+  if ((h->q_rows / 128 + h->k_rows / 128 + h->sequences + 2) > 2147483647LL / h->heads) return LBA_ERR_SHAPE;
+  return LBA_OK;
+}
+
+}  // namespace lba
+
+using namespace lba;
+
+extern "C" int lba_attention(const void* q, const void* k, const void* v, const lba_attention_how* how, int out_type, const float* out_scale,
+                             int out_flags, void* out, float* lse, void* stream) {
+  const int st = check_attention(how);
+  if (st != LBA_OK) return st;
+  if ((out_type != how->type && out_type != LBA_TYPE_CODES) || (out_flags & ~LBA_FLAG_INPUT_M4E3)) return LBA_ERR_LAYER;
+  if (how->q_rows == 0 || how->sequences == 0) return LBA_OK;
+  if (!q || !out || (how->k_rows > 0 && (!k || !v)) || (out_type == LBA_TYPE_CODES && !out_scale)) return LBA_ERR_NULL;
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(out)) return LBA_ERR_ALIGN;
+  ForwardParams p;
+  p.bf = how->type == LBA_TYPE_BF16;
+  // (without keys nothing is copied, but a map needs an address and a row)
+  if (!head_map(&p.q, p.bf, q, how->q_rows, how->heads, how->dim, how->q_at, 128) ||
+      !head_map(&p.k, p.bf, how->k_rows ? k : q, how->k_rows ? how->k_rows : 1, how->kv_heads, how->dim, how->k_rows ? how->k_at : how->q_at, 128) ||
+      !head_map(&p.v, p.bf, how->k_rows ? v : q, how->k_rows ? how->k_rows : 1, how->kv_heads, how->dim, how->k_rows ? how->v_at : how->q_at, 128))
+    return cuda_fail(cudaErrorInvalidValue);
+  p.cu_q = how->cu_q;
+  p.cu_k = how->cu_k;
+  p.q_rows = how->q_rows;
+  p.k_rows = how->k_rows;
+  p.sequences = how->sequences;
+  p.heads = how->heads;
+  p.group = how->heads / how->kv_heads;
+  p.dim = how->dim;
+  p.causal = how->causal != 0;
+  p.in_m4e3 = out_flags & LBA_FLAG_INPUT_M4E3;
+  p.codes = out_type == LBA_TYPE_CODES;
+  p.to_log2 = how->scale * LOG2E;
+  p.out_scale = out_scale;
+  p.v_raw = v;
+  p.v_at = how->v_at;
+  p.out = out;
+  p.lse = lse;
+  const int64_t blocks = (how->q_rows / (2 * QT) + how->sequences) * how->heads;
+  cudaStream_t s = (cudaStream_t)stream;
+  if (how->dim <= 64)
+    return status_of(p.bf ? launch_forward<__nv_bfloat16, 64>(p, blocks, s) : launch_forward<__half, 64>(p, blocks, s));
+  return status_of(p.bf ? launch_forward<__nv_bfloat16, 128>(p, blocks, s) : launch_forward<__half, 128>(p, blocks, s));
+}
