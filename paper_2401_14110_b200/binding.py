@@ -563,7 +563,7 @@ def lba_rotary(q, k, positions, freqs, interleaved=False, inverse=False, scale=1
     ``freqs``: float64, half the values that turn (``rotary_frequencies``).  ``inverse``: the opposite way, which is the gradient's.
     ``scale``: multiplies what turns.  ``out``: a pair of tensors, which may be ``q`` and ``k`` themselves."""
     lib = load_library()
-    done = None and _native.rotary(q, k, positions, freqs, interleaved, inverse, scale, out, stream)
+    done = _native and _native.rotary(q, k, positions, freqs, interleaved, inverse, scale, out, stream)
     if done is not None:
         return _done(done)
     qo, ko = (None, None) if out is None else out
@@ -633,7 +633,7 @@ def lba_attention(q, k, v, cu_q=None, cu_k=None, causal=True, scale=None, out_dt
     ``lba_linear`` takes them.  ``lse``: True, or a float32 tensor [heads][Tq] to write: the call then returns (out, lse), which
     ``lba_attention_backward`` takes.  Rows that no sequence holds are left as they were."""
     lib = load_library()
-    done = None and _native.attention(q, k, v, cu_q, cu_k, causal, scale, out_dtype, out_scale, prod_fmt, lse, out, stream)
+    done = _native and _native.attention(q, k, v, cu_q, cu_k, causal, scale, out_dtype, out_scale, prod_fmt, lse, out, stream)
     if done is not None:
         return _done(done)
     sums = lse if isinstance(lse, torch.Tensor) else None
@@ -651,7 +651,7 @@ def lba_attention_backward(grad_out, q, k, v, out, lse, cu_q=None, cu_k=None, ca
     """(grad_q, grad_k, grad_v) of ``lba_attention``, whose ``out`` (of the inputs' type) and ``lse`` these are; contiguous, of q's type.
     See ``lba_attention_backward`` in lba.h.  ``workspace``: a CUDA uint8 tensor of ``attention_backward_workspace_bytes``, or None."""
     lib = load_library()
-    done = None and _native.attention_backward(grad_out, q, k, v, out, lse, cu_q, cu_k, causal, scale, workspace, stream)
+    done = _native and _native.attention_backward(grad_out, q, k, v, out, lse, cu_q, cu_k, causal, scale, workspace, stream)
     if done is not None:
         return _done(done)
     _same_device(q, k, v, grad_out, out, lse, cu_q, cu_k, workspace)
@@ -698,7 +698,7 @@ def lba_cache_append(k, v, cache, page, table, start, cu=None, stream=None):
     ``cache``: uint8 of ``cache_shape(...)``; ``page``: tokens of a page; ``table``: int32 [sequences][pages of a sequence], numbers of
     pages; ``start``: int32 [sequences]; ``cu``: int32 [sequences + 1]."""
     lib = load_library()
-    done = None and _native.cache_append(k, v, cache, page, table, start, cu, stream)
+    done = _native and _native.cache_append(k, v, cache, page, table, start, cu, stream)
     if done is not None:
         return _done(done)
     _same_device(cache, k, v, table, start, cu)
@@ -717,7 +717,7 @@ def lba_cache_read(cache, page, table, start, cu, tokens, dtype=torch.bfloat16, 
 
     ``tokens``: rows of the outputs, as cu's last value says; ``dtype``: float32, bfloat16 or float16; ``out``: a pair of tensors to write."""
     lib = load_library()
-    done = None and _native.cache_read(cache, page, table, start, cu, tokens, dtype, out, stream)
+    done = _native and _native.cache_read(cache, page, table, start, cu, tokens, dtype, out, stream)
     if done is not None:
         return _done(done)
     k, v = (None, None) if out is None else out
@@ -743,7 +743,7 @@ def lba_cache_attention(q, cache, page, table, lengths, scale=None, out_dtype=No
     ``lengths``: int32 [sequences], tokens in the cache, the new one's among them.  ``out_dtype``, ``out_scale`` and ``prod_fmt`` are those of
     ``lba_attention``; ``workspace``: a CUDA uint8 tensor of ``cache_attention_workspace_bytes``, or None."""
     lib = load_library()
-    done = None and _native.cache_attention(q, cache, page, table, lengths, scale, out_dtype, out_scale, prod_fmt, workspace, out, stream)
+    done = _native and _native.cache_attention(q, cache, page, table, lengths, scale, out_dtype, out_scale, prod_fmt, workspace, out, stream)
     if done is not None:
         return _done(done)
     _same_device(q, cache, table, lengths, out_scale, workspace, out)

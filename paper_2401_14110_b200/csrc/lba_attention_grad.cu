@@ -8,13 +8,16 @@
 // the group), and walks over 64 rows of the others at a time:
 //   T1 = X1 Y1^T (scores), T2 = X2 Y2^T (dp)       X: q, g or k, v: shared memory for the whole CTA; Y: the other two, from a ring
 //   p and ds from T1 and T2, in registers          two warpgroups, each every second tile, a row a thread
-//   acc1 += ds Y1, and for keys acc2 += p Y2       p and ds lie in tensor memory over T1 and T2, sums in 256 more columns
+//   acc1 += ds Y1, and for keys acc2 += p Y2       p and ds lie in tensor memory over T1 and T2, sums in 128 more columns each
 // Scores and dp are so formed twice, seven products where five would do; in return every sum is formed by one CTA in a fixed order, and no
-// 32-bit gradient of q goes through memory or atomics.  Bound by the matrix instructions: 64 columns of scores want 192 bytes of shared
-// memory a clock where 128 are there, so a tile of a key block is 1280 clocks of tensor cores against 512 of exponentials.
+// 32-bit gradient of q goes through memory or atomics.
 //
-// p and ds are rounded to the inputs' type on their way into the products.  binary16 has few exponents: p is held times 2^8, and ds times a power
-// of two chosen from the largest |grad_out| and |v| so that it cannot overflow.
+// p is rounded to the inputs' type on its way into the product, and ds held as two pieces of it: delta comes from an output of 16 bits, and one
+// rounding more of ds would leave grad_q and grad_k off by 1.5 times what their own rounding costs (with two pieces by 1.1 times).  binary16
+// has few exponents: p is held times 2^8, and ds times a power of two chosen from the largest |grad_out| and |v| so that it cannot overflow.
+//
+// Bound by the matrix instructions.  128 x 64 scores with both operands in shared memory want 192 bytes a clock where 128 are there, 384 clocks
+// instead of 256, so a query block's X lies in tensor memory (1024 clocks a tile); a key block has no columns left for that (1536).
 #include <cmath>
 
 #include "lba_tile.cuh"
@@ -32,6 +35,8 @@ struct GradParams {
   int64_t q_rows, k_rows, key_blocks;
   int sequences, heads, kv_heads, group, dim, causal, bf;
   float to_log2, scale;
+  const void *q_raw, *g_raw; // contiguous grad_out
+  lba_strides q_at;
   const float2* stats;       // [heads][q_rows]: lse in powers of two, delta
   const uint32_t* most;      // largest |grad_out|, |v| as bits (binary16), or null
   void *grad_q, *grad_k, *grad_v;
@@ -121,7 +126,7 @@ template <int DT> constexpr int kY = YT * DT * 2;
 template <int DT> constexpr size_t kGradSmem = 1024 + 2 * (size_t)kX<DT> + 2 * (size_t)kY<DT> * GRAD_STAGES;
 
 struct GradShared {
-  uint64_t x_full, full[GRAD_STAGES], empty[GRAD_STAGES], cut_full[4], clean[4], products[2], weights[2], done;
+  uint64_t x_full, x_there, full[GRAD_STAGES], empty[GRAD_STAGES], cut_full[4], clean[4], products[2], weights[2], done;
   uint32_t tmem;
   int dead, seq, block, found;
   alignas(16) float2 stats[2][YT];
@@ -134,6 +139,12 @@ struct Walk {
   __device__ __forceinline__ int count() const { return heads * max(0, last - first); }
   __device__ __forceinline__ bool cut(int t) const { return t < low || t >= high; }
 };
+
+template <typename T>
+__device__ __forceinline__ float2 pair_values(uint32_t w) {
+  if constexpr (std::is_same<T, __nv_bfloat16>::value) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
+  return __half22float2(*reinterpret_cast<const __half2*>(&w));
+}
 
 template <typename T, int DT, bool KEYS>
 __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw_smem, uint32_t base, int head, uint32_t tmem) {
@@ -168,12 +179,13 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 8) {
       if (elected() && all) {
-        mbar_arrive_expect(smem_u32(&sh.x_full), 2 * X);
-        for (int i = 0; i < 2; ++i)
-          for (int x = 0; x < BLOCKS; ++x)
-            for (int r = 0; r < 2; ++r)
-              tile_load(base + i * X + x * X_BLOCK + r * Y_BLOCK, KEYS ? (i ? &p.v : &p.k) : (i ? &p.g : &p.q), x * 64, head, x_first + x0 + r * YT,
-                        smem_u32(&sh.x_full));
+        if (KEYS) {
+          mbar_arrive_expect(smem_u32(&sh.x_full), 2 * X);
+          for (int i = 0; i < 2; ++i)
+            for (int x = 0; x < BLOCKS; ++x)
+              for (int r = 0; r < 2; ++r)
+                tile_load(base + i * X + x * X_BLOCK + r * Y_BLOCK, i ? &p.v : &p.k, x * 64, head, x_first + x0 + r * YT, smem_u32(&sh.x_full));
+        }
         int cuts = 0;
         for (int n = 0; n < all; ++n) {
           const int stage = n % GRAD_STAGES, h = n / tiles, t = walk.first + n - h * tiles;
@@ -197,7 +209,8 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
         const int steps = (p.dim + 15) / 16;
         const uint32_t kind_t = tile_kind(p.bf, YT, false), kind_a = tile_kind(p.bf, steps * 16, true);
         const uint64_t rows = tile_operand(0, 16, 1024), lines = tile_operand(0, Y_BLOCK, 1024);
-        bool ok = all == 0 || mbar_wait(smem_u32(&sh.x_full), 0, dead);
+        bool ok = all == 0 || mbar_wait(smem_u32(KEYS ? &sh.x_full : &sh.x_there), 0, dead);
+        tmem_after();
         int cuts = 0;
         const auto products = [&](int n) {  // T1 and T2 of tile n
           const int stage = n % GRAD_STAGES, h = n / tiles, t = walk.first + n - h * tiles;
@@ -210,9 +223,12 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
           if (!ok) return;
           for (int i = 0; i < 2; ++i) {
             const uint64_t a = rows + ((base + i * X) >> 4), b = rows + ((ring + (stage * 2 + i) * Y) >> 4);
-            for (int s = 0; s < steps; ++s)
-              mma_shared(tmem + i * 128 + (n & 1) * YT, a + (((s >> 2) * X_BLOCK + (s & 3) * 32) >> 4), b + (((s >> 2) * Y_BLOCK + (s & 3) * 32) >> 4),
-                         kind_t, s != 0);
+            for (int s = 0; s < steps; ++s) {
+              const uint32_t d = tmem + i * 128 + (n & 1) * YT;
+              const uint64_t y = b + (((s >> 2) * Y_BLOCK + (s & 3) * 32) >> 4);
+              if (KEYS) mma_shared(d, a + (((s >> 2) * X_BLOCK + (s & 3) * 32) >> 4), y, kind_t, s != 0);
+              else mma_tensor(d, tmem + 384 + i * 64 + s * 8, y, kind_t, s != 0);
+            }
           }
           mma_arrive(smem_u32(&sh.products[n & 1]));
         };
@@ -223,8 +239,8 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
           tmem_after();
           const int stage = n % GRAD_STAGES;
           const uint64_t y1 = lines + ((ring + stage * 2 * Y) >> 4);
-          for (int s = 0; s < YT / 16; ++s)
-            mma_tensor(tmem + 256, tmem + 128 + (n & 1) * YT + s * 8, y1 + s * (2048 >> 4), kind_a, n != 0 || s != 0);
+          for (int s = 0; s < 2 * YT / 16; ++s)  // both pieces of ds
+            mma_tensor(tmem + 256, tmem + 128 + (n & 1) * YT + s * 8, y1 + (s % (YT / 16)) * (2048 >> 4), kind_a, n != 0 || s != 0);
           if (KEYS) {
             const uint64_t y2 = y1 + (Y >> 4);
             for (int s = 0; s < YT / 16; ++s) mma_tensor(tmem + 384, tmem + (n & 1) * YT + s * 8, y2 + s * (2048 >> 4), kind_a, n != 0 || s != 0);
@@ -287,6 +303,23 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
     mine = make_float2(0.0f, 0.0f);
     if (n < all && thread < YT && i < y_count) mine = __ldg(p.stats + (int64_t)(head * p.group + h) * p.q_rows + y_first + i);
   };
+  if (!KEYS) {  // this warpgroup's operand of all first products: a row a thread, in tensor memory beside the sums
+    const T* const row = w ? static_cast<const T*>(p.g_raw) + ((int64_t)(x_first + x) * p.heads + head) * p.dim
+                           : static_cast<const T*>(p.q_raw) + (int64_t)(x_first + x) * p.q_at.token + head * p.q_at.head;
+    for (int d = 0; d < p.dim; d += 32) {
+      uint32_t v[16];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const uint4 four = x < x_count && d + 8 * e < p.dim ? __ldg(reinterpret_cast<const uint4*>(row + d + 8 * e)) : make_uint4(0u, 0u, 0u, 0u);
+        v[4 * e] = four.x, v[4 * e + 1] = four.y, v[4 * e + 2] = four.z, v[4 * e + 3] = four.w;
+      }
+      __syncwarp();
+      tmem_st16(tmem + 384 + w * 64 + lanes + d / 2, v);
+    }
+    tmem_wait_st();
+    tmem_before();
+    mbar_arrive(smem_u32(&sh.x_there));
+  }
   if (KEYS) stats_of(w);
   else if (x < x_count) mine = __ldg(p.stats + (int64_t)head * p.q_rows + x_first + x);
   for (int n = w; n < all; n += 2) {
@@ -310,17 +343,21 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
       }
     }
     const bool masked = walk.cut(t);
+    uint32_t s[YT], dp[YT];
 #pragma unroll
     for (int half = 0; half < YT; half += 32) {
-      uint32_t s[32], dp[32], pw[16], dw[16];
-      tmem_load32(t1 + half, s);
-      tmem_load32(t2 + half, dp);
-      tmem_wait_ld();
+      tmem_load32(t1 + half, s + half);
+      tmem_load32(t2 + half, dp + half);
+    }
+    tmem_wait_ld();
 #pragma unroll
-      for (int e = 0; e < 32; e += 2) {
+    for (int half = 0; half < YT; half += 32) {
+      uint32_t pw[16], dw[16], low[16];
+#pragma unroll
+      for (int e = half; e < half + 32; e += 2) {
         u64 minus, delta;
         if (KEYS) {
-          const float4 st = *reinterpret_cast<const float4*>(&sh.stats[w][half + e]);
+          const float4 st = *reinterpret_cast<const float4*>(&sh.stats[w][e]);
           minus = pack2(-st.x, -st.z);
           delta = pack2(-st.y, -st.w);
         } else {
@@ -334,15 +371,19 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
         float d0, d1;
         unpack2(mul2_rn(mul2_rn(add2_rn(pack2u(dp[e], dp[e + 1]), delta), up), pack2(p0, p1)), d0, d1);
         if (masked) {
-          if (half + e < lo || half + e >= hi) p0 = d0 = 0.0f;
-          if (half + e + 1 < lo || half + e + 1 >= hi) p1 = d1 = 0.0f;
+          if (e < lo || e >= hi) p0 = d0 = 0.0f;
+          if (e + 1 < lo || e + 1 >= hi) p1 = d1 = 0.0f;
         }
-        if (KEYS) pw[e / 2] = pack_pair<T>(p0, p1);
-        dw[e / 2] = pack_pair<T>(d0, d1);
+        const int at = (e - half) / 2;
+        if (KEYS) pw[at] = pack_pair<T>(p0, p1);
+        dw[at] = pack_pair<T>(d0, d1);
+        const float2 held = pair_values<T>(dw[at]);
+        low[at] = pack_pair<T>(d0 - held.x, d1 - held.y);
       }
-      // A half's 16 columns of pairs go over columns that have been read: those of this half or of the first
-      if (KEYS) tmem_st16(t1 + half / 2, *reinterpret_cast<const uint32_t(*)[16]>(pw));
-      tmem_st16(t2 + half / 2, *reinterpret_cast<const uint32_t(*)[16]>(dw));
+      // over columns that have been read: p's 32, ds' first pieces' 32 and second pieces' 32
+      if (KEYS) tmem_st16(t1 + half / 2, pw);
+      tmem_st16(t2 + half / 2, dw);
+      tmem_st16(t2 + YT / 2 + half / 2, low);
     }
     tmem_wait_st();
     tmem_before();
@@ -393,6 +434,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) attention_grad_kernel(const _
   const uint32_t base = (smem_u32(raw_smem) + 1023) & ~1023u;
   if (threadIdx.x == 0) {
     mbar_init(smem_u32(&sh.x_full), 1);
+    mbar_init(smem_u32(&sh.x_there), 256);
     mbar_init(smem_u32(&sh.done), 1);
     for (int i = 0; i < GRAD_STAGES; ++i) {
       mbar_init(smem_u32(&sh.full[i]), 1);
@@ -480,6 +522,9 @@ int lba_attention_backward(const void* grad_out, const void* q, const void* k, c
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < lba_attention_backward_workspace_bytes(how)) return LBA_ERR_WORKSPACE;
   GradParams p;
   p.bf = how->type == LBA_TYPE_BF16;
+  p.q_raw = q;
+  p.g_raw = grad_out;
+  p.q_at = how->q_at;
   const lba_strides g_at = {(int64_t)how->heads * how->dim, how->dim};
   if (!head_map(&p.q, p.bf, q, how->q_rows, how->heads, how->dim, how->q_at, YT) || !head_map(&p.g, p.bf, grad_out, how->q_rows, how->heads, how->dim, g_at, YT) ||
       !head_map(&p.k, p.bf, k, how->k_rows, how->kv_heads, how->dim, how->k_at, YT) ||

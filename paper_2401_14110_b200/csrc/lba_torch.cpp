@@ -17,6 +17,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <climits>
+#include <cmath>
 #include <optional>
 
 #include "lba.h"
@@ -470,6 +471,266 @@ PyObject* gated_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
   });
 }
 
+// ------------------------------------------------------------------ between the linear layers
+bool as_bool(PyObject* o) {
+  if (!PyBool_Check(o)) not_regular();
+  return o == Py_True;
+}
+// a tensor [rows][heads][dim] of this type whose heads' values are contiguous
+struct Heads {
+  const at::Tensor& t;
+  lba_strides at;
+  void* data;
+  static const at::Tensor& checked(PyObject* o, const Call& call) {
+    if (Py_TYPE(o) != (PyTypeObject*)THPVariableClass && Py_TYPE(o) != (PyTypeObject*)g_parameter_type) not_regular();
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.defined() || !t.is_cuda() || t.get_device() != call.device || t.dim() != 3 || t.layout() != at::kStrided || (t.size(2) > 1 && t.stride(2) != 1))
+      not_regular();
+    return t;
+  }
+  Heads(PyObject* o, const Call& call) : t(checked(o, call)), at{t.stride(0), t.stride(1)}, data(t.data_ptr()) {}
+};
+// int32 values, n of them; None: null
+const int32_t* as_ints(PyObject* o, int64_t n, int device) {
+  if (o == Py_None) return nullptr;
+  const at::Tensor& t = as_tensor(o, at::kInt, -1, device);
+  if (t.numel() != n) not_regular();
+  return (const int32_t*)t.data_ptr();
+}
+int half_type(c10::ScalarType t) {
+  if (t != at::kBFloat16 && t != at::kHalf) not_regular();
+  return float_type(t);
+}
+int as_size(int64_t v) {
+  if (v > INT_MAX) not_regular();
+  return (int)v;
+}
+at::Tensor given_or_fresh(PyObject* o, const Call& call, at::IntArrayRef sizes, c10::ScalarType dtype) {
+  if (o == Py_None) return call.fresh(sizes, dtype);
+  const at::Tensor& t = as_tensor(o, dtype, -1, call.device);
+  if (t.sizes() != sizes) not_regular();
+  return t;
+}
+PyObject* wrapped(PyObject* given, const at::Tensor& t) { return given == Py_None ? THPVariable_Wrap(t) : Py_NewRef(given); }
+PyObject* both_of(PyObject* a, PyObject* b) {  // takes both references, which may be null with a Python error set
+  PyObject* const r = a && b ? PyTuple_Pack(2, a, b) : nullptr;
+  Py_XDECREF(a);
+  Py_XDECREF(b);
+  return r;
+}
+
+// q, k, positions, freqs, interleaved, inverse, scale, out, stream
+PyObject* rotary(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return regular_or_none(n, 9, [&]() -> PyObject* {
+    const Call call(a[8]);
+    const Heads q(a[0], call);
+    const bool has_k = a[1] != Py_None;
+    const std::optional<Heads> k = has_k ? std::optional<Heads>(std::in_place, a[1], call) : std::nullopt;
+    const c10::ScalarType dtype = q.t.scalar_type();
+    lba_rotary_how how = {};
+    how.type = float_type(dtype);
+    if (has_k && (k->t.scalar_type() != dtype || k->t.size(0) != q.t.size(0) || k->t.size(2) != q.t.size(2))) not_regular();
+    if (Py_TYPE(a[2]) != (PyTypeObject*)THPVariableClass) not_regular();
+    const c10::ScalarType pt = THPVariable_Unpack(a[2]).scalar_type();
+    if (pt != at::kInt && pt != at::kLong) not_regular();
+    const at::Tensor &pos = as_tensor(a[2], pt, -1, call.device), &freqs = as_tensor(a[3], at::kDouble, -1, call.device);
+    if (pos.numel() != q.t.size(0)) not_regular();
+    how.heads = as_size(q.t.size(1));
+    how.kv_heads = has_k ? as_size(k->t.size(1)) : 0;
+    how.dim = as_size(q.t.size(2));
+    how.rotary_dim = as_size(2 * freqs.numel());
+    how.interleaved = as_bool(a[4]);
+    how.inverse = as_bool(a[5]);
+    how.wide_positions = pt == at::kLong;
+    how.scale = (float)as_real(a[6]);
+    how.tokens = q.t.size(0);
+    how.positions = pos.data_ptr();
+    how.freqs = (const double*)freqs.data_ptr();
+    PyObject *go = Py_None, *gk = Py_None;
+    if (a[7] != Py_None) {
+      if (!PyTuple_CheckExact(a[7]) || PyTuple_GET_SIZE(a[7]) != 2) not_regular();
+      go = PyTuple_GET_ITEM(a[7], 0);
+      gk = PyTuple_GET_ITEM(a[7], 1);
+    }
+    const at::Tensor qo = go == Py_None ? call.fresh(q.t.sizes(), dtype) : Heads(go, call).t;
+    const at::Tensor ko = !has_k ? at::Tensor() : gk == Py_None ? call.fresh(k->t.sizes(), dtype) : Heads(gk, call).t;
+    if (qo.scalar_type() != dtype || qo.sizes() != q.t.sizes() || (has_k && (ko.scalar_type() != dtype || ko.sizes() != k->t.sizes()))) not_regular();
+    const lba_strides none = {0, 0}, qo_at = {qo.stride(0), qo.stride(1)}, ko_at = has_k ? lba_strides{ko.stride(0), ko.stride(1)} : none;
+    const lba_strides k_at = has_k ? k->at : none;
+    const void* const pk = has_k ? k->data : nullptr;
+    void *const po = qo.data_ptr(), *const pko = has_k ? ko.data_ptr() : nullptr;
+    const int status = without_gil([&] { return lba_rotary(q.data, q.at, pk, k_at, &how, po, qo_at, pko, ko_at, call.stream); });
+    if (status != 0) return PyLong_FromLong(status);
+    return both_of(wrapped(go, qo), has_k ? wrapped(gk, ko) : Py_NewRef(Py_None));
+  });
+}
+
+// what both passes share
+struct Attention {
+  Heads q, k, v;
+  lba_attention_how how = {};
+  Attention(const Call& call, PyObject* qo, PyObject* ko, PyObject* vo, PyObject* cu_q, PyObject* cu_k, PyObject* causal, PyObject* scale)
+      : q(qo, call), k(ko, call), v(vo, call) {
+    const c10::ScalarType dtype = q.t.scalar_type();
+    how.type = half_type(dtype);
+    if (k.t.scalar_type() != dtype || v.t.scalar_type() != dtype || k.t.sizes() != v.t.sizes() || k.t.size(2) != q.t.size(2) ||
+        (cu_q == Py_None) != (cu_k == Py_None))
+      not_regular();
+    how.sequences = 1;
+    if (cu_q != Py_None) {
+      const at::Tensor& t = as_tensor(cu_q, at::kInt, -1, call.device);
+      if (t.numel() < 1) not_regular();
+      how.sequences = as_size(t.numel() - 1);
+      how.cu_q = (const int32_t*)t.data_ptr();
+      how.cu_k = as_ints(cu_k, t.numel(), call.device);
+    }
+    how.heads = as_size(q.t.size(1));
+    how.kv_heads = as_size(k.t.size(1));
+    how.dim = as_size(q.t.size(2));
+    how.causal = as_bool(causal);
+    how.scale = (float)(scale == Py_None ? std::pow((double)how.dim, -0.5) : as_real(scale));
+    how.q_rows = q.t.size(0);
+    how.k_rows = k.t.size(0);
+    how.q_at = q.at;
+    how.k_at = k.at;
+    how.v_at = v.at;
+  }
+};
+// an attention's output: of the inputs' type, or codes
+struct Output {
+  at::Tensor out;
+  int type, flags = 0;
+  const float* scale = nullptr;
+  Output(const Call& call, at::IntArrayRef sizes, c10::ScalarType dtype, PyObject* out_dtype, PyObject* out_scale, PyObject* prod_fmt, PyObject* given) {
+    c10::ScalarType t = out_dtype == Py_None ? dtype : as_dtype(out_dtype);
+    if (given != Py_None) {
+      if (Py_TYPE(given) != (PyTypeObject*)THPVariableClass) not_regular();
+      t = THPVariable_Unpack(given).scalar_type();
+    }
+    if (t != dtype && t != at::kByte) not_regular();
+    type = t == at::kByte ? (int)LBA_TYPE_CODES : float_type(t);
+    if (t == at::kByte) {
+      const at::Tensor& s = as_tensor(out_scale, at::kFloat, -1, call.device);
+      if (s.numel() != 1) not_regular();
+      scale = (const float*)s.data_ptr();
+      if (prod_fmt != Py_None) flags = as_format(prod_fmt).flags & LBA_FLAG_INPUT_M4E3;
+    }
+    out = given_or_fresh(given, call, sizes, t);
+  }
+};
+
+// q, k, v, cu_q, cu_k, causal, scale, out_dtype, out_scale, prod_fmt, lse, out, stream
+PyObject* attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return regular_or_none(n, 13, [&]() -> PyObject* {
+    const Call call(a[12]);
+    const Attention x(call, a[0], a[1], a[2], a[3], a[4], a[5], a[6]);
+    const Output y(call, x.q.t.sizes(), x.q.t.scalar_type(), a[7], a[8], a[9], a[11]);
+    const bool fresh = a[10] == Py_True, wanted = fresh || (a[10] != Py_False && a[10] != Py_None);
+    at::Tensor lse;
+    if (wanted) lse = given_or_fresh(fresh ? Py_None : a[10], call, {x.q.t.size(1), x.q.t.size(0)}, at::kFloat);
+    float* const pl = wanted ? (float*)lse.data_ptr() : nullptr;
+    void* const po = y.out.data_ptr();
+    const int status =
+        without_gil([&] { return lba_attention(x.q.data, x.k.data, x.v.data, &x.how, y.type, y.scale, y.flags, po, pl, call.stream); });
+    if (status != 0) return PyLong_FromLong(status);
+    PyObject* const out = wrapped(a[11], y.out);
+    return wanted ? both_of(out, wrapped(fresh ? Py_None : a[10], lse)) : out;
+  });
+}
+
+// grad_out, q, k, v, out, lse, cu_q, cu_k, causal, scale, workspace, stream
+PyObject* attention_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return regular_or_none(n, 12, [&]() -> PyObject* {
+    const Call call(a[11]);
+    const Attention x(call, a[1], a[2], a[3], a[6], a[7], a[8], a[9]);
+    const c10::ScalarType dtype = x.q.t.scalar_type();
+    const at::Tensor &g = as_tensor(a[0], dtype, 3, call.device), &out = as_tensor(a[4], dtype, 3, call.device), &lse = as_tensor(a[5], at::kFloat, 2, call.device);
+    if (g.sizes() != x.q.t.sizes() || out.sizes() != x.q.t.sizes() || lse.size(0) != x.q.t.size(1) || lse.size(1) != x.q.t.size(0)) not_regular();
+    const at::Tensor ws = a[10] != Py_None ? as_tensor(a[10], at::kByte, -1, call.device)
+                                           : call.fresh({(int64_t)lba_attention_backward_workspace_bytes(&x.how)}, at::kByte);
+    const at::Tensor gq = call.fresh(x.q.t.sizes(), dtype), gk = call.fresh(x.k.t.sizes(), dtype), gv = call.fresh(x.k.t.sizes(), dtype);
+    const void *const pg = g.data_ptr(), *const po = out.data_ptr();
+    const float* const pl = (const float*)lse.data_ptr();
+    return results(without_gil([&] {
+                     return lba_attention_backward(pg, x.q.data, x.k.data, x.v.data, po, pl, &x.how, gq.data_ptr(), gk.data_ptr(), gv.data_ptr(),
+                                                   ws.data_ptr(), ws.numel(), call.stream);
+                   }), {gq, gk, gv});
+  });
+}
+
+// a cache [pages][heads][page (dim + dim / 16)] and its block table [sequences][width]
+lba_cache as_cache(PyObject* o, PyObject* page, PyObject* table, int64_t sequences, const Call& call) {
+  const at::Tensor &t = as_tensor(o, at::kByte, 3, call.device), &b = as_tensor(table, at::kInt, 2, call.device);
+  const int64_t p = as_int(page), run = t.size(2);
+  if (b.size(0) != sequences || p < 1 || run % (17 * p) || run * 16 / (17 * p) % 32) not_regular();
+  lba_cache c = {};
+  c.pages = t.data_ptr();
+  c.page_count = t.size(0);
+  c.kv_heads = as_size(t.size(1));
+  c.dim = as_size(run * 16 / (17 * p));
+  c.page = (int)p;
+  c.sequences = as_size(sequences);
+  c.table_width = as_size(b.size(1));
+  c.table = (const int32_t*)b.data_ptr();
+  return c;
+}
+
+// k, v, cache, page, table, start, cu, stream
+PyObject* cache_append(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return regular_or_none(n, 8, [&]() -> PyObject* {
+    const Call call(a[7]);
+    const Heads k(a[0], call), v(a[1], call);
+    const at::Tensor& start = as_tensor(a[5], at::kInt, -1, call.device);
+    const lba_cache c = as_cache(a[2], a[3], a[4], start.numel(), call);
+    if (k.t.scalar_type() != v.t.scalar_type() || k.t.sizes() != v.t.sizes() || k.t.size(1) != c.kv_heads || k.t.size(2) != c.dim) not_regular();
+    const int type = float_type(k.t.scalar_type());
+    const int32_t* const cu = as_ints(a[6], start.numel() + 1, call.device);
+    const int status = without_gil([&] {
+      return lba_cache_append(&c, k.data, k.at, v.data, v.at, type, k.t.size(0), (const int32_t*)start.data_ptr(), cu, call.stream);
+    });
+    return status != 0 ? PyLong_FromLong(status) : Py_NewRef(a[2]);
+  });
+}
+
+// cache, page, table, start, cu, tokens, dtype, out, stream
+PyObject* cache_read(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return regular_or_none(n, 9, [&]() -> PyObject* {
+    const Call call(a[8]);
+    const at::Tensor& start = as_tensor(a[3], at::kInt, -1, call.device);
+    const lba_cache c = as_cache(a[0], a[1], a[2], start.numel(), call);
+    const int32_t* const cu = as_ints(a[4], start.numel() + 1, call.device);
+    const int64_t tokens = as_int(a[5]);
+    const c10::ScalarType dtype = as_dtype(a[6]);
+    const int type = float_type(dtype);
+    if (tokens < 0 || a[7] != Py_None) not_regular();
+    const at::Tensor k = call.fresh({tokens, c.kv_heads, c.dim}, dtype), v = call.fresh({tokens, c.kv_heads, c.dim}, dtype);
+    return results(without_gil([&] {
+                     return lba_cache_read(&c, (const int32_t*)start.data_ptr(), cu, tokens, type, k.data_ptr(), v.data_ptr(), call.stream);
+                   }), {k, v});
+  });
+}
+
+// q, cache, page, table, lengths, scale, out_dtype, out_scale, prod_fmt, workspace, out, stream
+PyObject* cache_attention(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  return regular_or_none(n, 12, [&]() -> PyObject* {
+    const Call call(a[11]);
+    const Heads q(a[0], call);
+    const int type = half_type(q.t.scalar_type()), heads = as_size(q.t.size(1));
+    const lba_cache c = as_cache(a[1], a[2], a[3], q.t.size(0), call);
+    if (q.t.size(2) != c.dim || a[4] == Py_None) not_regular();
+    const int32_t* const lengths = as_ints(a[4], q.t.size(0), call.device);
+    const float scale = (float)(a[5] == Py_None ? std::pow((double)c.dim, -0.5) : as_real(a[5]));
+    const Output y(call, q.t.sizes(), q.t.scalar_type(), a[6], a[7], a[8], a[10]);
+    const at::Tensor ws = a[9] != Py_None ? as_tensor(a[9], at::kByte, -1, call.device)
+                                          : call.fresh({(int64_t)lba_cache_attention_workspace_bytes(&c, heads)}, at::kByte);
+    void* const po = y.out.data_ptr();
+    const int status = without_gil([&] {
+      return lba_cache_attention(q.data, q.at, type, heads, &c, lengths, scale, y.type, y.scale, y.flags, po, ws.data_ptr(), ws.numel(), call.stream);
+    });
+    return status != 0 ? PyLong_FromLong(status) : wrapped(a[10], y.out);
+  });
+}
+
 PyObject* init_module(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (n != 2) {
     PyErr_SetString(PyExc_TypeError, "init takes the format class and the parameter class");
@@ -492,6 +753,12 @@ PyMethodDef kMethods[] = {
     {"gated", (PyCFunction)(void (*)(void))gated, METH_FASTCALL, nullptr},
     {"linear_backward", (PyCFunction)(void (*)(void))linear_backward, METH_FASTCALL, nullptr},
     {"gated_backward", (PyCFunction)(void (*)(void))gated_backward, METH_FASTCALL, nullptr},
+    {"rotary", (PyCFunction)(void (*)(void))rotary, METH_FASTCALL, nullptr},
+    {"attention", (PyCFunction)(void (*)(void))attention, METH_FASTCALL, nullptr},
+    {"attention_backward", (PyCFunction)(void (*)(void))attention_backward, METH_FASTCALL, nullptr},
+    {"cache_append", (PyCFunction)(void (*)(void))cache_append, METH_FASTCALL, nullptr},
+    {"cache_read", (PyCFunction)(void (*)(void))cache_read, METH_FASTCALL, nullptr},
+    {"cache_attention", (PyCFunction)(void (*)(void))cache_attention, METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef kModule = {PyModuleDef_HEAD_INIT, "lba_torch", nullptr, -1, kMethods, nullptr, nullptr, nullptr, nullptr};
 
