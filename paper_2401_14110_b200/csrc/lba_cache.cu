@@ -17,6 +17,7 @@
 // Loads go straight to registers, two steps of 16 tokens ahead of the one computed; no shared memory, no barriers until the end.
 #include <cmath>
 
+#include "lba_async.cuh"
 #include "lba_entry.cuh"
 #include "lba_layer.cuh"
 
@@ -238,28 +239,43 @@ cudaError_t launch_rows(const RowsParams& p, int dim, int type, cudaStream_t str
 }
 
 // ------------------------------------------------------------------ attention of single tokens
-constexpr int DEC_WARPS = 8, DEC_THREADS = 32 * DEC_WARPS, STEP = 16;
+// Work is counted in units of 64 tokens of a line: a piece of up to HT query heads of a key-value head of a sequence.  All units of all
+// lines, sequence by sequence, stand in one row, cut into equal shares, one for each warp (a share may take in many lines, and a line
+// many shares), so no warp waits for another.  A warp leaves a part for every line that it meets: sums, maximum and outputs relative to
+// it.  Warp w's part of line i is number w + i: one of the two grows from each part to the next.  cache_combine_kernel adds up the parts
+// of each line.  (With CTAs that merged their eight warps' parts, each for a stretch of one line, 48 requests of up to 16384 tokens took
+// 135 us at the best length of a stretch: a CTA's start and end cost 5 us.)
+constexpr int UNIT = 64, STEP = 16, DEC_STAGES = 2, DEC_WARPS = 12, DEC_THREADS = 32 * DEC_WARPS;
+constexpr int KNOWN = 128, GROUPS = 65536 / KNOWN;  // sequences of which a warp knows the lengths at a time
 constexpr float HEADROOM = 5.0f;     // binades by which a score may exceed its head's running maximum
-constexpr float P_SCALE = 1024.0f;   // weights in binary16: at most 2^(10 + 5)
+constexpr float P_BITS = 10.0f;      // weights in binary16: at most 2^(10 + 5)
 constexpr float NO_MAX = -1e30f;
+constexpr uint32_t LEAST_REF = 0x10101010u;  // see `ref`
 
 struct DecodeParams {
   CacheView c;
   const void* q;
   lba_strides q_at;
   const int32_t* lengths;
-  int heads, group, blocks_of_heads;  // query heads; of a key-value head; pieces of 8 NT of a group
-  int chunk, chunks;                  // tokens of a CTA, most CTAs of a sequence's head
+  int heads, group, pieces;           // query heads; of a key-value head; pieces of a group
+  int warps;                          // that there are shares for, at most
   float scale;
   int out_type, in_m4e3;
   const float* out_scale;
   void* out;
-  float* parts;                       // [sequence][key-value head][piece][chunk][8 NT heads][D + 2]
+  int* before;                        // [sequences + 1]: units of a line in all sequences before
+  float* parts;                       // [warps + lines][HT][D + 2]
+  __host__ __device__ int lines() const { return c.heads * pieces; }  // of a sequence
 };
+__device__ __forceinline__ int share_of(const DecodeParams& p, int all_units) { return max((int)(((unsigned)(all_units * p.lines()) + p.warps - 1) / p.warps), 1); }
 
 __device__ __forceinline__ void mma16816(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma16816_first(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {  // sums from 0 on
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+      : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.0f));
 }
 __device__ __forceinline__ uint32_t transposed(uint32_t m) {
   uint32_t d;
@@ -279,58 +295,23 @@ __device__ __forceinline__ uint32_t max_bytes(uint32_t a, uint32_t b) {
   constexpr uint32_t EVEN = 0x00FF00FFu;
   return __vmaxu2(a & EVEN, b & EVEN) | (__vmaxu2((a >> 8) & EVEN, (b >> 8) & EVEN) << 8);
 }
-template <int N>
-__device__ __forceinline__ uint32_t load_exponents(const uint8_t* p) {
-  if constexpr (N == 4) return __ldg(reinterpret_cast<const uint32_t*>(p));
-  if constexpr (N == 2) return __ldg(reinterpret_cast<const uint16_t*>(p));
-  if constexpr (N == 1) return __ldg(p);
-  return (uint32_t)__ldg(p) | ((uint32_t)__ldg(p + 1) << 8) | ((uint32_t)__ldg(p + 2) << 16);
+__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, int bytes, uint32_t bar) {
+  asm volatile("cp.async.bulk.shared::cta.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
 }
 
-// what a lane needs of 16 tokens: rows r and r + 8 of the keys (r = lane / 4), tokens 2 c, 2 c + 1, 2 c + 8, 2 c + 9 of the values (c = lane % 4)
+// A unit in shared memory: the four planes of a run, 64 tokens of each
 template <int NG>
-struct Step16 {
-  uint32_t k[2][NG], ke[2], v[4][(NG + 1) / 2], ve[4];
-  __device__ __forceinline__ void load(const CacheView& cache, int64_t page, int head, int row, int r, int c) {
-    constexpr int D = 32 * NG;
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint8_t* const src = plane<D>(cache, page, head, 0) + (int64_t)(row + r + 8 * i) * (D / 2) + c * (D / 8);
-      if constexpr (NG == 4) {
-        const uint4 w = __ldg(reinterpret_cast<const uint4*>(src));
-        k[i][0] = w.x, k[i][1] = w.y, k[i][2] = w.z, k[i][3] = w.w;
-      } else if constexpr (NG == 2) {
-        const uint2 w = __ldg(reinterpret_cast<const uint2*>(src));
-        k[i][0] = w.x, k[i][1] = w.y;
-      } else {
-#pragma unroll
-        for (int g = 0; g < NG; ++g) k[i][g] = __ldg(reinterpret_cast<const uint32_t*>(src) + g);
-      }
-      ke[i] = load_exponents<NG>(plane<D>(cache, page, head, 2) + (int64_t)(row + r + 8 * i) * NG);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int t = row + 2 * c + (i & 1) + (i >> 1) * 8;
-      const uint8_t* const src = plane<D>(cache, page, head, 1) + (int64_t)t * (D / 2) + r * (D / 16);
-      if constexpr (NG == 4) {
-        const uint2 w = __ldg(reinterpret_cast<const uint2*>(src));
-        v[i][0] = w.x, v[i][1] = w.y;
-      } else if constexpr (NG == 2) {
-        v[i][0] = __ldg(reinterpret_cast<const uint32_t*>(src));
-      } else {
-        const uint16_t* const s = reinterpret_cast<const uint16_t*>(src);
-        v[i][0] = __ldg(s);
-        if constexpr (NG == 3) {
-          v[i][0] |= (uint32_t)__ldg(s + 1) << 16;
-          v[i][1] = __ldg(s + 2);
-        }
-      }
-      ve[i] = load_exponents<NG>(plane<D>(cache, page, head, 3) + (int64_t)t * NG);
-    }
-  }
+struct Unit {
+  static constexpr int D = 32 * NG, VALUES = UNIT * D / 2, KEY_EXP = UNIT * D, VALUE_EXP = UNIT * (D + NG), BYTES = UNIT * (D + 2 * NG);
 };
+template <int NG>
+__device__ __forceinline__ uint32_t exponents(const uint8_t* p) {
+  if constexpr (NG == 4) return *reinterpret_cast<const uint32_t*>(p);
+  if constexpr (NG == 2) return *reinterpret_cast<const uint16_t*>(p);
+  if constexpr (NG == 1) return *p;
+  return (uint32_t)p[0] | ((uint32_t)p[1] << 8) | ((uint32_t)p[2] << 16);
+}
 
-// Eight columns' worth of outputs of one head of the batch, from parts in turn: their maxima, sums and unscaled outputs
 template <int D>
 __device__ __forceinline__ void store_decoded(const DecodeParams& p, int64_t i, float v) {
   if (p.out_type == LBA_TYPE_CODES) {
@@ -343,329 +324,543 @@ __device__ __forceinline__ void store_decoded(const DecodeParams& p, int64_t i, 
   }
 }
 
-// of a sequence: what its length and its row of the table allow (below 2^31 - 2 chunk: view_of)
+// of a sequence: what its length and its row of the table allow (below 2^31 - 64: view_of)
 __device__ __forceinline__ int tokens_of(const DecodeParams& p, int b) { return max(0, min(p.lengths[b], p.c.width * p.c.page)); }
+__device__ __forceinline__ int units_of(int tokens) { return (tokens + UNIT - 1) / UNIT; }
 
-template <typename T, int NG, int NT>
-__global__ void __launch_bounds__(DEC_THREADS, NT == 1 ? 2 : 1) cache_attention_kernel(const DecodeParams p) {
-  constexpr int D = 32 * NG, COLS = 8 * NT, PART = D + 2;
-  extern __shared__ float merge[];  // [warp][COLS][D + 2]
+struct WarpState {  // what a warp needs from line to line
+  int before[KNOWN + 1], tokens[KNOWN];  // units of a line before each of the sequences that are known, and their tokens
+};
+template <int NG> constexpr size_t kDecodeSmem = (size_t)DEC_WARPS * (DEC_STAGES * (Unit<NG>::BYTES + 8) + sizeof(WarpState)) + 128;
+
+// HT: query heads of a line.  Columns of the scores are heads, eight at a time; with four heads they are there twice.
+template <typename T, int NG, int HT>
+__global__ void __launch_bounds__(DEC_THREADS, 1) cache_attention_kernel(const DecodeParams p) {
+  typedef Unit<NG> U;
+  constexpr int D = 32 * NG, NT = HT <= 8 ? 1 : HT / 8, OT = HT / 4, PART = D + 2;  // tiles of eight columns, of four heads' outputs
+  constexpr int BATCH = HT <= 8 ? 2 : 1;                                            // steps of 16 tokens side by side: independent chains
+  constexpr bool TWICE = HT == 4;
+  extern __shared__ __align__(128) uint8_t units[];  // [warp][stage], then each warp's barriers and state
+  __shared__ int groups[GROUPS + 1];                 // units of a line in all sequences before each KNOWN of them
+  __shared__ int dead_flag;
+  volatile int* const dead = &dead_flag;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane >> 2, c = lane & 3;
+  uint8_t* const mine = units + warp * (DEC_STAGES * U::BYTES);
+  uint64_t* const full = reinterpret_cast<uint64_t*>(units + DEC_WARPS * DEC_STAGES * U::BYTES) + warp * DEC_STAGES;
+  WarpState& state = reinterpret_cast<WarpState*>(units + DEC_WARPS * DEC_STAGES * (U::BYTES + 8))[warp];
+  if (threadIdx.x == 0) dead_flag = 0;
+  if (lane == 0) {
+    for (int i = 0; i < DEC_STAGES; ++i) mbar_init(smem_u32(full + i), 1);
+    mbar_init_fence();
+  }
   after_previous();
-  const int b = blockIdx.z, piece = blockIdx.y % p.blocks_of_heads, kvh = blockIdx.y / p.blocks_of_heads;
-  const int length = tokens_of(p, b), first = blockIdx.x * p.chunk;
-  if (first >= length && p.chunks != 1) return;  // (with a single chunk the outputs of empty sequences are written here)
-  const int tokens = min(p.chunk, length - first), steps = tokens > 0 ? (tokens + STEP - 1) / STEP : 0;  // 16-token steps, cut among the warps
-  const int s0 = steps * warp / DEC_WARPS, s1 = steps * (warp + 1) / DEC_WARPS;
-  const int32_t* const table = p.c.table + (int64_t)b * p.c.width;
-
-  const auto page_of = [&](int s) -> int {  // of step s of this CTA; -1: not there
-    if (s >= s1) return -1;
-    const int pg = __ldg(table + (first + s * STEP) / p.c.page);
-    return pg >= 0 && pg < p.c.page_count ? pg : -1;
-  };
-  // pages of the next 32 steps, one a lane
-  int window = s0, pages = page_of(s0 + lane);
-  const auto next_page = [&](int s) -> int {  // warp-uniform, s ascending
-    if (s - window >= 32) {
-      window = s;
-      pages = page_of(s + lane);
+  const int group_count = (p.c.sequences + KNOWN - 1) / KNOWN;
+  // the tokens of group g's sequences, four neighbours a lane; returns the group's units
+  const auto know = [&](int g, int units_before) -> int {
+    __syncwarp();  // (what was known is no longer read)
+    int n[4], sum = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int b = g * KNOWN + lane * 4 + i, t = b < p.c.sequences ? tokens_of(p, b) : 0;
+      state.tokens[lane * 4 + i] = t;
+      n[i] = sum;
+      sum += units_of(t);
     }
-    return __shfl_sync(0xFFFFFFFFu, pages, s - window);
-  };
-  Step16<NG> ahead[2];
-  int at[2], row = (first + s0 * STEP) % p.c.page;
-  const auto fetch = [&](int u, int s) {  // of one step after another
-    at[u] = s < s1 ? next_page(s) : -1;
-    if (at[u] >= 0) ahead[u].load(p.c, at[u], kvh, row, r, c);
-    row = row + STEP == p.c.page ? 0 : row + STEP;
-  };
-  fetch(0, s0);
-  fetch(1, s0 + 1);
-
-  // query heads: column r of a tile; values 32 g + 8 c to + 7
-  uint32_t q[NT][NG][4];
-  float to_log2[NT][2];  // of columns 2 c and 2 c + 1
+    int upto = sum;
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
-    const int h = piece * COLS + n * 8 + r;
-    float x[NG][8], top = 0.0f;
-    const bool there = h < p.group;
-    const T* const src = static_cast<const T*>(p.q) + (int64_t)b * p.q_at.token + (int64_t)(kvh * p.group + h) * p.q_at.head + c * 8;
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      load_some<T, 8>(src, g * 32, there ? 8 : 0, x[g]);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[g][j]));
+    for (int d = 1; d < 32; d *= 2) {
+      const int u = __shfl_up_sync(0xFFFFFFFFu, upto, d);
+      if (lane >= d) upto += u;
     }
-    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-    top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-    int e = (int)(__float_as_uint(top) >> 23) - 127;  // (infinities stay what they are under any factor)
-    e = e < -126 ? -126 : e > 126 ? 126 : e;
-    const float down = __uint_as_float((uint32_t)(127 - e) << 23), up = __uint_as_float((uint32_t)(127 + e) << 23) * (p.scale * LOG2E);
 #pragma unroll
-    for (int g = 0; g < NG; ++g)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) q[n][g][j] = half_pair(x[g][2 * j] * down, x[g][2 * j + 1] * down);
-#pragma unroll
-    for (int j = 0; j < 2; ++j) to_log2[n][j] = __shfl_sync(0xFFFFFFFFu, up, (2 * c + j) * 4);
+    for (int i = 0; i < 4; ++i) state.before[lane * 4 + i] = units_before + upto - sum + n[i];
+    const int all = __shfl_sync(0xFFFFFFFFu, upto, 31);
+    if (lane == 0) state.before[KNOWN] = units_before + all;
+    __syncwarp();
+    return all;
+  };
+  const int lines = p.lines();
+  int known = 0, all;
+  if (group_count <= 1) {
+    all = know(0, 0);
+    __syncthreads();  // (of what the first threads have set up)
+  } else {
+    for (int g = warp; g < group_count; g += DEC_WARPS) {
+      const int n = know(g, 0);
+      if (lane == 0) groups[g + 1] = n;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      int sum = 0;
+      groups[0] = 0;
+      for (int g = 1; g <= group_count; ++g) groups[g] = sum += groups[g];
+    }
+    __syncthreads();
+    all = groups[group_count];
   }
-
-  float o[NT][2 * NG][4], m[NT][2], l[NT][2];
-  uint32_t ref = 0;  // the largest exponent byte of each group so far
-#pragma unroll
-  for (int n = 0; n < NT; ++n) {
-#pragma unroll
-    for (int i = 0; i < 2 * NG; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) o[n][i][j] = 0.0f;
-    m[n][0] = m[n][1] = NO_MAX;
-    l[n][0] = l[n][1] = 0.0f;
+  if (blockIdx.x == 0) {  // for the second kernel
+    for (int g = warp; g < group_count; g += DEC_WARPS) {
+      if (group_count > 1) know(g, groups[g]);
+      for (int i = lane; i < KNOWN && g * KNOWN + i < p.c.sequences; i += 32) p.before[g * KNOWN + i] = state.before[i];
+      __syncwarp();
+    }
+    if (threadIdx.x == 0) p.before[p.c.sequences] = all;
   }
-
-  const auto compute = [&](Step16<NG>& w, int s) {
-    const int left = tokens - s * STEP;  // tokens of this step that exist
-    float z[NT][4];
+  const int share = share_of(p, all), total = all * lines;
+  int at = (int)min((unsigned)(blockIdx.x * DEC_WARPS + warp) * (unsigned)share, (unsigned)total);
+  const int end = (int)min((unsigned)at + (unsigned)share, (unsigned)total);
+  if (group_count > 1 && at < end) {  // the group of the first unit: the last that begins at or before it
+    int lo = 0, hi = group_count - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (groups[mid] <= at / lines) lo = mid;
+      else hi = mid - 1;
+    }
+    known = lo;
+    know(lo, groups[lo]);
+  }
+  int filled = 0;  // units that were sent for so far: their number says which stage and phase
+  bool ok = true;
+#pragma unroll 1
+  while (at < end) {
+    int seq;
+    while (true) {  // the last of the known sequences that begins at or before this unit, and is not empty
+      const int place = at / lines;
+      int n = 0;
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) z[n][j] = 0.0f;
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      uint32_t lo[4], hi[4];
-      decode8(w.k[0][g], lo);
-      decode8(w.k[1][g], hi);
-      const int up = 23 - 8 * g;
-      float by[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i) by[i] = __uint_as_float((up >= 0 ? w.ke[i] << (up & 31) : w.ke[i] >> (-up & 31)) & 0x7F800000u);
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        float sum[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-        const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
-        mma16816(sum, a0, q[n][g][0], q[n][g][1]);
-        mma16816(sum, a1, q[n][g][2], q[n][g][3]);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) z[n][j] = fmaf(sum[j], by[j >> 1], z[n][j]);
+      for (int i = 0; i < KNOWN; i += 32) n += __popc(__ballot_sync(0xFFFFFFFFu, state.before[i + lane] <= place));
+      if (place < state.before[KNOWN]) {  // (of several that begin there, all but the last are empty)
+        seq = n - 1;
+        break;
       }
+      ++known;
+      know(known, groups[known]);
     }
+    const int tokens = state.tokens[seq], n_units = units_of(tokens), inside = at - state.before[seq] * lines;
+    const int b = known * KNOWN + seq, line = inside / n_units, kvh = line / p.pieces, piece = line - kvh * p.pieces;
+    const int u0 = inside - line * n_units, u1 = min(n_units, u0 + end - at);
+    at += u1 - u0;
+
+    // A unit comes in runs of tokens that lie in one page: all 64, or 32 or 16 where pages are no multiples of 64.  The lanes hold the next 32 runs'
+    // pages (-1: not there) and first rows.  (The copies are an elected lane's with the same operands in every lane: where four lanes each
+    // sent for a run, a unit cost 200 instructions.)
+    const int run = p.c.page % 64 == 0 ? 64 : p.c.page % 32 == 0 ? 32 : 16, runs = UNIT / run;
+    int window = u0 * runs, pages, rows;
+    const auto look_up = [&] {
+      const int t = (window + lane) * run, number = t / p.c.page;
+      rows = t - number * p.c.page;
+      pages = t < tokens ? __ldg(p.c.table + (int64_t)b * p.c.width + number) : -1;
+      if (pages >= p.c.page_count) pages = -1;
+    };
+    look_up();
+    const auto fill = [&](int u, int stage) -> uint32_t {  // one unit after another; the mask says which of its four steps are there
+      if (u * runs - window >= 32) {
+        window = u * runs;
+        look_up();
+      }
+      uint32_t there = 0;
+      const int left = min(tokens - u * UNIT, UNIT);
+      const uint32_t bar = smem_u32(full + stage), dst = smem_u32(mine + stage * U::BYTES);
+      int page[4], row[4], up[4], bytes = 0;
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+      for (int i = 0; i < 4; ++i) {
+        if (i >= runs) break;
+        page[i] = __shfl_sync(0xFFFFFFFFu, pages, u * runs + i - window);
+        row[i] = __shfl_sync(0xFFFFFFFFu, rows, u * runs + i - window);
+        up[i] = page[i] < 0 ? 0 : (min(left - i * run, run) + STEP - 1) / STEP * STEP;  // whole steps: sizes are multiples of 16 bytes
+        there |= ((1u << (up[i] / STEP)) - 1u) << (i * run / STEP);
+        bytes += up[i] * (D + 2 * NG);
+      }
+      if (there && elected()) {
+        mbar_arrive_expect(bar, bytes);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) z[n][j] *= to_log2[n][j & 1];
-    if (left < STEP) {
-#pragma unroll
-      for (int n = 0; n < NT; ++n)
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (r + (j >> 1) * 8 >= left) z[n][j] = -INFINITY;
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (2 * c + (i & 1) + (i >> 1) * 8 >= left) w.ve[i] = 0;
-    }
-    uint32_t top = max_bytes(max_bytes(w.ve[0], w.ve[1]), max_bytes(w.ve[2], w.ve[3]));
-    bool raise = max_bytes(top, ref) != ref;
-#pragma unroll
-    for (int n = 0; n < NT; ++n)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) raise |= z[n][j] > m[n][j & 1] + HEADROOM;
-    if (__any_sync(0xFFFFFFFFu, raise)) {
-      top = max_bytes(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-      top = max_bytes(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-      const uint32_t old = ref;
-      ref = max_bytes(ref, top);
-      const uint32_t by = ref - old;
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        float a[2];
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          float t = fmaxf(fmaxf(z[n][j], z[n][j + 2]), m[n][j]);
-          t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 4));
-          t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 8));
-          t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 16));
-          a[j] = exp2_approx(m[n][j] - t);
-          m[n][j] = t;
-          l[n][j] *= a[j];
-        }
-#pragma unroll
-        for (int i = 0; i < 2 * NG; ++i) {
-          const int d = (by >> (8 * (i >> 1))) & 255;
-          const float down = d > 126 ? 0.0f : __uint_as_float((uint32_t)(127 - d) << 23);
-#pragma unroll
-          for (int j = 0; j < 4; ++j) o[n][i][j] *= a[j & 1] * down;
+        for (int i = 0; i < 4; ++i) {
+          if (i >= runs) break;
+          if (!up[i]) continue;
+          const uint8_t* const src = p.c.pages + ((int64_t)page[i] * p.c.heads + kvh) * p.c.run(D);
+          const int first = i * run;
+          bulk_load(dst + first * (D / 2), src + row[i] * (D / 2), up[i] * (D / 2), bar);
+          bulk_load(dst + U::VALUES + first * (D / 2), src + (p.c.page + row[i]) * (D / 2), up[i] * (D / 2), bar);
+          bulk_load(dst + U::KEY_EXP + first * NG, src + p.c.page * D + row[i] * NG, up[i] * NG, bar);
+          bulk_load(dst + U::VALUE_EXP + first * NG, src + p.c.page * (D + NG) + row[i] * NG, up[i] * NG, bar);
         }
       }
+      __syncwarp();
+      return there;
+    };
+    uint32_t there[DEC_STAGES];
+    int order[DEC_STAGES];  // of the fills: which stage and phase
+#pragma unroll
+    for (int i = 0; i < DEC_STAGES; ++i) {
+      there[i] = 0;
+      order[i] = filled;
+      if (u0 + i < u1) there[i] = fill(u0 + i, filled % DEC_STAGES);
+      if (there[i]) ++filled;
     }
-    // weights as operands: rows of the transposed 8 x 8 blocks are heads, columns tokens
-    uint32_t w0[NT], w1[NT];
+
+    // query heads: column r of a tile; values 32 g + 8 c to + 7
+    uint32_t q[NT][NG][4];
+    float to_log2[NT][2];  // of columns 2 c and 2 c + 1
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-      float e[4];
+      const int h = piece * HT + (TWICE ? r & 3 : n * 8 + r);
+      float x[NG][8], top = 0.0f;
+      const bool has = h < p.group;
+      const T* const src = static_cast<const T*>(p.q) + (int64_t)b * p.q_at.token + (int64_t)(kvh * p.group + h) * p.q_at.head + c * 8;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        e[j] = exp2_approx(z[n][j] - m[n][j & 1]);
-        l[n][j & 1] += e[j];
+      for (int g = 0; g < NG; ++g) {
+        load_some<T, 8>(src, g * 32, has ? 8 : 0, x[g]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) top = fmaxf(top, fabsf(x[g][j]));
       }
-      w0[n] = transposed(half_pair(e[0] * P_SCALE, e[1] * P_SCALE));
-      w1[n] = transposed(half_pair(e[2] * P_SCALE, e[3] * P_SCALE));
+      top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+      top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+      int e = (int)(__float_as_uint(top) >> 23) - 127;  // (infinities stay what they are under any factor)
+      e = e < -126 ? -126 : e > 126 ? 126 : e;
+      const float down = __uint_as_float((uint32_t)(127 - e) << 23), up = __uint_as_float((uint32_t)(127 + e) << 23) * (p.scale * LOG2E);
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) q[n][g][j] = half_pair(x[g][2 * j] * down, x[g][2 * j + 1] * down);
+#pragma unroll
+      for (int j = 0; j < 2; ++j) to_log2[n][j] = __shfl_sync(0xFFFFFFFFu, up, (2 * c + j) * 4);
     }
-    uint32_t below[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) below[i] = ref - w.ve[i];  // (no byte borrows)
-#pragma unroll
-    for (int g = 0; g < NG; ++g) {
-      // 2^-d of two tokens in binary16, 0 from d = 15 on
-      uint32_t f[2];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-        f[i] = 0x3C003C00u - (__vminu2(__byte_perm(below[2 * i], below[2 * i + 1], 0x0400 | (g << 8) | g) & 0x00FF00FFu, 0x000F000Fu) << 10);
-      uint32_t b0[NT], b1[NT];
-#pragma unroll
-      for (int n = 0; n < NT; ++n) {
-        b0[n] = mul_halves(w0[n], f[0]);
-        b1[n] = mul_halves(w1[n], f[1]);
-      }
-#pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        const int i = 2 * g + u;
-        uint32_t h[4];
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const uint32_t word = w.v[t][i / 4] >> (8 * (i % 4));
-          asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %1;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\t}" : "=r"(h[t]) : "r"(word));
-        }
-        const uint32_t a[4] = {__byte_perm(h[0], h[1], 0x5410), __byte_perm(h[0], h[1], 0x7632), __byte_perm(h[2], h[3], 0x5410),
-                               __byte_perm(h[2], h[3], 0x7632)};
-#pragma unroll
-        for (int n = 0; n < NT; ++n) mma16816(o[n][i], a, b0[n], b1[n]);
-      }
-    }
-  };
-#pragma unroll 1
-  for (int s = s0; s < s1; s += 2) {
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      Step16<NG> now = ahead[u];
-      const bool there = at[u] >= 0;
-      fetch(u, s + 2 + u);
-      if (there) compute(now, s + u);
-    }
-  }
 
-  // ---- the warps' sums together
-  float* const mine = merge + warp * COLS * PART;
+    // m: the maximum that weights are relative to, less 10 binades; limit: the score from which on it is raised.
+    // ref: for each group the exponent byte that weights are relative to, at least 16, so that the byte of ref - (an exponent) is in 0..15 only
+    // where the exponent is in ref - 15..ref (an exponent above ref gives 17 to 255 there, and borrows change no 0..15 to that).
+    float o[OT][NG][4], m[NT][2], limit[NT][2], l[NT][2];
+    constexpr uint32_t LEAST = LEAST_REF >> (8 * (4 - NG));
+    uint32_t ref = LEAST, base = 0x3C3C3C3Cu - 4u * LEAST;  // base + 4 e: bytes 0x3C - 4 (ref - e), the high byte of 2^-(ref - e) in binary16
 #pragma unroll
-  for (int n = 0; n < NT; ++n) {
+    for (int n = 0; n < NT; ++n) {
+      m[n][0] = m[n][1] = limit[n][0] = limit[n][1] = NO_MAX;
+      l[n][0] = l[n][1] = 0.0f;
+    }
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      float t = l[n][j];
-      t += __shfl_xor_sync(0xFFFFFFFFu, t, 4);
-      t += __shfl_xor_sync(0xFFFFFFFFu, t, 8);
-      t += __shfl_xor_sync(0xFFFFFFFFu, t, 16);
-      const int col = n * 8 + 2 * c + j;
-      if (r == 0) {
-        mine[col * PART + D] = m[n][j];
-        mine[col * PART + D + 1] = t;
+    for (int t = 0; t < OT; ++t)
+#pragma unroll
+      for (int g = 0; g < NG; ++g)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) o[t][g][j] = 0.0f;
+
+    // Bytes (0, 2^-d) as the half of a pair that a column's weights are in: of place g, by selector place_of + g place_step.  Values of tokens
+    // 2 c and 2 c + 1 (and 8 on) are taken in the other order where c is odd: so the four rows of a load lie in both halves of the banks.
+    const uint32_t place_of = r < 4 ? 0x4404u : 0x0444u, place_step = r < 4 ? 0x0010u : 0x1000u;
+    const int swap = c & 1;
+    const uint32_t pick0 = swap ? 0x3232u : 0x1010u, pick1 = swap ? 0x1010u : 0x3232u;
+
+    // BATCH steps from token `first` of a unit on, of which `left` tokens exist and `steps` (bits) are there
+    const auto compute = [&](const uint8_t* unit, int first, int left, uint32_t steps) {
+      float z[BATCH][NT][4];  // tokens r (0, 1) and r + 8 (2, 3); columns 2 c (0, 2) and 2 c + 1 (1, 3)
+      uint32_t ve[BATCH][4];
+      const uint8_t* const keys = unit + (first + r) * (D / 2) + c * (D / 8);
+      const uint8_t* const key_exps = unit + U::KEY_EXP + (first + r) * NG;
+      const uint8_t* const value_exps = unit + U::VALUE_EXP + (first + 2 * c) * NG;
+#pragma unroll
+      for (int x = 0; x < BATCH; ++x) {
+        uint32_t k[2][NG], ke[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint8_t* const src = keys + (x * STEP + 8 * i) * (D / 2);
+          if constexpr (NG == 4) {
+            const uint4 w = *reinterpret_cast<const uint4*>(src);
+            k[i][0] = w.x, k[i][1] = w.y, k[i][2] = w.z, k[i][3] = w.w;
+          } else if constexpr (NG == 2) {
+            const uint2 w = *reinterpret_cast<const uint2*>(src);
+            k[i][0] = w.x, k[i][1] = w.y;
+          } else {
+#pragma unroll
+            for (int g = 0; g < NG; ++g) k[i][g] = reinterpret_cast<const uint32_t*>(src)[g];
+          }
+          ke[i] = exponents<NG>(key_exps + (x * STEP + 8 * i) * NG);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) ve[x][i] = exponents<NG>(value_exps + (x * STEP + ((i & 1) ^ swap) + (i >> 1) * 8) * NG);
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          uint32_t lo[4], hi[4];
+          decode8(k[0][g], lo);
+          decode8(k[1][g], hi);
+          const int up = 23 - 8 * g;
+          float by[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) by[i] = __uint_as_float((up >= 0 ? ke[i] << (up & 31) : ke[i] >> (-up & 31)) & 0x7F800000u);
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            float sum[4];
+            const uint32_t a0[4] = {lo[0], hi[0], lo[1], hi[1]}, a1[4] = {lo[2], hi[2], lo[3], hi[3]};
+            mma16816_first(sum, a0, q[n][g][0], q[n][g][1]);
+            mma16816(sum, a1, q[n][g][2], q[n][g][3]);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) z[x][n][j] = g == 0 ? sum[j] * by[j >> 1] : fmaf(sum[j], by[j >> 1], z[x][n][j]);
+          }
+        }
+      }
+      if (left < BATCH * STEP || steps != (1u << BATCH) - 1u) {  // what does not exist, or was not copied, may be anything
+#pragma unroll
+        for (int x = 0; x < BATCH; ++x) {
+          const int here = (steps >> x) & 1 ? left - x * STEP : 0;
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              if (r + (j >> 1) * 8 >= here) z[x][n][j] = -INFINITY;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (2 * c + ((i & 1) ^ swap) + (i >> 1) * 8 >= here) ve[x][i] = ref;
+        }
+      }
+      uint32_t wide = 0;
+      bool raise = false;
+#pragma unroll
+      for (int x = 0; x < BATCH; ++x) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) wide |= ref - ve[x][i];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) raise |= z[x][n][j] > limit[n][j & 1];
+      }
+      raise |= (wide & 0xF0F0F0F0u) != 0;
+      uint32_t far[BATCH][4];  // groups whose values count as 0
+      bool any_far = false;
+      if (__any_sync(0xFFFFFFFFu, raise)) {
+        uint32_t top = ref;
+#pragma unroll
+        for (int x = 0; x < BATCH; ++x)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) top = max_bytes(top, ve[x][i]);
+        top = max_bytes(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        top = max_bytes(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+        const uint32_t by = top - ref;
+        ref = top;
+        base = 0x3C3C3C3Cu - 4u * ref;
+        float a[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            float t = fmaxf(z[0][n][j], z[0][n][j + 2]);
+            if (BATCH == 2) t = fmaxf(t, fmaxf(z[BATCH - 1][n][j], z[BATCH - 1][n][j + 2]));
+            t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 4));
+            t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 8));
+            t = fmaxf(t, __shfl_xor_sync(0xFFFFFFFFu, t, 16));
+            t = fmaxf(m[n][j], t * to_log2[n][j] - P_BITS);
+            a[n][j] = exp2_approx(m[n][j] - t);
+            m[n][j] = t;
+            limit[n][j] = t == NO_MAX ? NO_MAX : (t + P_BITS + HEADROOM) / to_log2[n][j];
+            l[n][j] *= a[n][j];
+          }
+#pragma unroll
+        for (int t = 0; t < OT; ++t) {
+          float f[2];  // of heads 4 t + 2 (c & 1) and the next
+#pragma unroll
+          for (int j = 0; j < 2; ++j) f[j] = TWICE ? a[0][j] : __shfl_sync(0xFFFFFFFFu, a[t / 2][j], (lane & 28) + 2 * (t & 1) + (c & 1));
+#pragma unroll
+          for (int g = 0; g < NG; ++g) {
+            const int d = (by >> (8 * g)) & 255;
+            const float down = d > 126 ? 0.0f : __uint_as_float((uint32_t)(127 - d) << 23);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[t][g][j] *= f[j & 1] * down;
+          }
+        }
+#pragma unroll
+        for (int x = 0; x < BATCH; ++x)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            far[x][i] = 0;
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+              const uint32_t byte = 255u << (8 * g);
+              if ((ref - ve[x][i]) & 0xF0F0F0F0u & byte) far[x][i] |= byte;
+            }
+            ve[x][i] = (ve[x][i] & ~far[x][i]) | (ref & far[x][i]);
+            any_far |= far[x][i] != 0;
+          }
+        any_far = __any_sync(0xFFFFFFFFu, any_far);
       }
 #pragma unroll
-      for (int i = 0; i < 2 * NG; ++i) {
-        const uint32_t e = (ref >> (8 * (i >> 1))) & 255u;
+      for (int x = 0; x < BATCH; ++x) {
+        // weights as operands: rows of the transposed 8 x 8 blocks are columns of the scores, columns tokens 2 c, 2 c + 1 and 2 c + 8, 2 c + 9
+        uint32_t both4[OT][4], high[4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+          float e[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            e[j] = exp2_approx(fmaf(z[x][n][j], to_log2[n][j & 1], -m[n][j & 1]));
+            l[n][j & 1] += e[j];
+          }
+          const uint32_t w0 = transposed(half_pair(e[0], e[1])), w1 = transposed(half_pair(e[2], e[3]));
+#pragma unroll
+          for (int t = n * OT / NT; t < (n + 1) * OT / NT; ++t) {
+            const int from_lane = (r & 3) * 4 + 16 * (t & 1) + c;
+            const uint32_t x0 = TWICE ? w0 : __shfl_sync(0xFFFFFFFFu, w0, from_lane), x1 = TWICE ? w1 : __shfl_sync(0xFFFFFFFFu, w1, from_lane);
+            both4[t][0] = __byte_perm(x0, x0, pick0);
+            both4[t][1] = __byte_perm(x0, x0, pick1);
+            both4[t][2] = __byte_perm(x1, x1, pick0);
+            both4[t][3] = __byte_perm(x1, x1, pick1);
+          }
+        }
+        uint32_t v[4][(NG + 1) / 2];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          high[i] = base + 4u * ve[x][i];
+          const uint8_t* const src = unit + U::VALUES + (first + x * STEP + 2 * c + ((i & 1) ^ swap) + (i >> 1) * 8) * (D / 2) + r * (D / 16);
+          if constexpr (NG == 4) {
+            const uint2 w = *reinterpret_cast<const uint2*>(src);
+            v[i][0] = w.x, v[i][1] = w.y;
+          } else if constexpr (NG == 2) {
+            v[i][0] = *reinterpret_cast<const uint32_t*>(src);
+          } else {
+            // (both halves of a word are filled: from a 16-bit load alone, nvcc 12.9 had the conversions of its bytes give 0)
+            const uint16_t* const h = reinterpret_cast<const uint16_t*>(src);
+            v[i][0] = h[0] | (uint32_t)h[NG == 3] << 16;
+            if constexpr (NG == 3) v[i][1] = h[2] | (uint32_t)h[2] << 16;
+          }
+        }
+        if (any_far) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+#pragma unroll
+            for (int g = 0; g < NG; ++g)
+              if ((far[x][i] >> (8 * g)) & 1u) v[i][g / 2] &= g & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+        }
+        // A byte's conversion gives two dimensions of a token.  They are two k-steps of the product, and its columns are four heads twice: the first
+        // four columns' weights are 0 for the second dimension, the others' for the first.  So are the factors that bring a weight to its group.
+#pragma unroll
+        for (int g = 0; g < NG; ++g) {
+          uint32_t h[4][2], f[4];  // [token][rows r and r + 8: bytes 16 g + r and 16 g + 8 + r]
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            f[i] = __byte_perm(high[i], 0u, place_of + g * place_step);
+            const uint32_t word = v[i][g / 2];
+            if (g & 1)
+              asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %2;\n\tcvt.rn.f16x2.e2m1x2 %0, c;\n\tcvt.rn.f16x2.e2m1x2 %1, d;\n\t}" : "=r"(h[i][0]), "=r"(h[i][1]) : "r"(word));
+            else
+              asm("{\n\t.reg .b8 a, b, c, d;\n\tmov.b32 {a, b, c, d}, %2;\n\tcvt.rn.f16x2.e2m1x2 %0, a;\n\tcvt.rn.f16x2.e2m1x2 %1, b;\n\t}" : "=r"(h[i][0]), "=r"(h[i][1]) : "r"(word));
+          }
+          const uint32_t a0[4] = {h[0][0], h[0][1], h[1][0], h[1][1]}, a1[4] = {h[2][0], h[2][1], h[3][0], h[3][1]};
+#pragma unroll
+          for (int t = 0; t < OT; ++t) {
+            mma16816(o[t][g], a0, mul_halves(both4[t][0], f[0]), mul_halves(both4[t][1], f[1]));
+            mma16816(o[t][g], a1, mul_halves(both4[t][2], f[2]), mul_halves(both4[t][3], f[3]));
+          }
+        }
+      }
+    };
+
+#pragma unroll 1
+    for (int u = u0; u < u1; u += DEC_STAGES) {
+#pragma unroll
+      for (int i = 0; i < DEC_STAGES; ++i) {
+        if (there[i]) {
+          const int stage = order[i] % DEC_STAGES;
+          ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(full + stage), (order[i] / DEC_STAGES) & 1, dead));
+          if (ok) {
+            const uint8_t* const unit = mine + stage * U::BYTES;
+            const int left = tokens - (u + i) * UNIT;
+#pragma unroll 1
+            for (int first = 0; first < UNIT; first += BATCH * STEP) {
+              const uint32_t steps = (there[i] >> (first / STEP)) & ((1u << BATCH) - 1u);
+              if (steps) compute(unit, first, left - first, steps);
+            }
+          }
+          __syncwarp();
+        }
+        const int next = u + i + DEC_STAGES;
+        order[i] = filled;
+        there[i] = ok && next < u1 ? fill(next, filled % DEC_STAGES) : 0;
+        if (there[i]) ++filled;
+      }
+    }
+
+    // the part
+    float* const part = p.parts + ((int64_t)blockIdx.x * DEC_WARPS + warp + (int64_t)b * lines + line) * (HT * PART);
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        float t = l[n][j];
+        t += __shfl_xor_sync(0xFFFFFFFFu, t, 4);
+        t += __shfl_xor_sync(0xFFFFFFFFu, t, 8);
+        t += __shfl_xor_sync(0xFFFFFFFFu, t, 16);
+        if (!ok) t = __uint_as_float(0x7FC00000u);
+        const int h = n * 8 + 2 * c + j;
+        if (r == 0 && h < HT) *reinterpret_cast<float2*>(part + h * PART + D) = make_float2(m[n][j], t);
+      }
+#pragma unroll
+    for (int t = 0; t < OT; ++t)
+#pragma unroll
+      for (int g = 0; g < NG; ++g) {
+        const uint32_t e = (ref >> (8 * g)) & 255u;
         const float by = e == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float(e << 23);
-        *reinterpret_cast<float2*>(mine + col * PART + 16 * i + 2 * r) =
-            make_float2(o[n][i][j] * (1.0f / P_SCALE) * by, o[n][i][2 + j] * (1.0f / P_SCALE) * by);
-      }
-    }
-  }
-  __syncthreads();
-  const int cols = p.group - piece * COLS < COLS ? p.group - piece * COLS : COLS;
-  float* const part = p.parts + ((((int64_t)b * gridDim.y + blockIdx.y) * p.chunks + blockIdx.x) * COLS) * PART;
-  for (int i = threadIdx.x; i < cols * D; i += DEC_THREADS) {
-    const int col = i / D, d = i - col * D;
-    float top = NO_MAX, sum = 0.0f, v = 0.0f;
 #pragma unroll
-    for (int w = 0; w < DEC_WARPS; ++w) top = fmaxf(top, merge[(w * COLS + col) * PART + D]);
-#pragma unroll
-    for (int w = 0; w < DEC_WARPS; ++w) {
-      const float* const src = merge + (w * COLS + col) * PART;
-      const float by = exp2_approx(src[D] - top);
-      sum = fmaf(src[D + 1], by, sum);
-      if (src[D + 1] != 0.0f) v = fmaf(src[d], by, v);  // (a warp without tokens has nothing to add)
-    }
-    if (p.chunks == 1) {
-      const int64_t at_out = ((int64_t)b * p.heads + kvh * p.group + piece * COLS + col) * D + d;
-      store_decoded<D>(p, at_out, sum == 0.0f ? 0.0f : __fdiv_rn(v, sum));
-    } else {
-      part[col * PART + d] = v;
-      if (d == 0) {
-        part[col * PART + D] = top;
-        part[col * PART + D + 1] = sum;
+        for (int j = 0; j < 4; ++j) part[(4 * t + 2 * (c & 1) + (j & 1)) * PART + 2 * (16 * g + r + 8 * (j >> 1)) + (c >> 1)] = o[t][g][j] * by;
       }
-    }
   }
+  if (!ok) let_copies_land();
 }
 
-// the chunks' sums together: a block per head
-template <int NG, int NT>
-__global__ void __launch_bounds__(128) cache_combine_kernel(const DecodeParams p) {
-  constexpr int D = 32 * NG, COLS = 8 * NT, PART = D + 2;
+// a line's parts together: a block per head
+template <int NG, int HT>
+__global__ void __launch_bounds__(32 * NG) cache_combine_kernel(const DecodeParams p) {
+  constexpr int D = 32 * NG, PART = D + 2;
   after_previous();
-  const int b = blockIdx.y, h = blockIdx.x, kvh = h / p.group, in_group = h - kvh * p.group, piece = in_group / COLS, col = in_group - piece * COLS;
-  const int d = threadIdx.x;
-  if (d >= D) return;
-  const int n = (tokens_of(p, b) + p.chunk - 1) / p.chunk;
-  const float* const part = p.parts + (((int64_t)b * p.c.heads * p.blocks_of_heads + kvh * p.blocks_of_heads + piece) * p.chunks) * COLS * PART + col * PART;
+  const int b = blockIdx.y, h = blockIdx.x, d = threadIdx.x, lines = p.lines();
+  const int kvh = h / p.group, in_group = h - kvh * p.group, piece = in_group / HT, line = kvh * p.pieces + piece, col = in_group - piece * HT;
+  const int begin = p.before[b], units = p.before[b + 1] - begin, share = share_of(p, p.before[p.c.sequences]), first = begin * lines + line * units;
   float top = NO_MAX, sum = 0.0f, v = 0.0f;
+  if (units > 0) {
+    const int w0 = first / share, n = (first + units - 1) / share - w0 + 1;
+    const float* const part = p.parts + (w0 + (int64_t)b * lines + line) * (HT * PART) + col * PART;
 #pragma unroll 4
-  for (int i = 0; i < n; ++i) {
-    const float* const src = part + (int64_t)i * COLS * PART;
-    const float mx = __ldg(src + D), li = __ldg(src + D + 1), vi = __ldg(src + d);
-    const float t = fmaxf(top, mx), was = exp2_approx(top - t), by = exp2_approx(mx - t);
-    sum = sum * was + li * by;
-    v = v * was;
-    if (li != 0.0f) v = fmaf(vi, by, v);
-    top = t;
+    for (int i = 0; i < n; ++i) {
+      const float* const src = part + (int64_t)i * HT * PART;
+      const float2 ml = __ldg(reinterpret_cast<const float2*>(src + D));
+      const float vi = __ldg(src + d);
+      const float t = fmaxf(top, ml.x), was = exp2_approx(top - t), by = exp2_approx(ml.x - t);
+      sum = sum * was + ml.y * by;
+      v = v * was;
+      if (ml.y != 0.0f) v = fmaf(vi, by, v);  // (tokens that are not there leave nothing)
+      top = t;
+    }
   }
   store_decoded<D>(p, ((int64_t)b * p.heads + h) * D + d, sum == 0.0f ? 0.0f : __fdiv_rn(v, sum));
 }
 
 struct DecodePlan {
-  int cols, pieces, chunk, chunks;
-  size_t bytes;
+  int cols, pieces, blocks;
+  size_t before_bytes, bytes;
 };
-// Tokens of a CTA: enough CTAs at full length for eight rounds over the SMs (lengths differ, and the host does not know them), 128 tokens at
-// least, a step of every warp, and 4096 at most.
-DecodePlan plan_decode(const CacheView& c, int dim, int heads) {
-  DecodePlan d = {};
+// A CTA on every SM, or as many as there can be units for.  Units are counted in 31 bits.
+bool plan_decode(const CacheView& c, int dim, int heads, DecodePlan* d) {
   const int group = heads / c.heads;
-  d.cols = group > 8 ? 16 : 8;
-  d.pieces = (group + d.cols - 1) / d.cols;
-  const int64_t most = (int64_t)c.width * c.page, lines = (int64_t)c.sequences * c.heads * d.pieces;
-  int64_t chunk = (int64_t)((double)most * (double)lines / (16.0 * device_sms()));
-  chunk = (chunk + 127) / 128 * 128;
-  chunk = chunk < 128 ? 128 : chunk > 4096 ? 4096 : chunk;
-  d.chunk = (int)chunk;
-  d.chunks = (int)(most <= chunk ? 1 : (most + chunk - 1) / chunk);
-  d.bytes = d.chunks == 1 ? 0 : (size_t)lines * d.chunks * d.cols * (dim + 2) * sizeof(float);
-  return d;
+  d->cols = group > 8 ? 16 : group > 4 ? 8 : 4;
+  d->pieces = (group + d->cols - 1) / d->cols;
+  const double lines = (double)c.sequences * c.heads * d->pieces, most = std::ceil((double)c.width * c.page / UNIT);
+  if (most * lines > 2147483647.0 - 65536.0) return false;
+  const int resident = device_sms(), useful = (int)std::ceil(most * lines / DEC_WARPS);
+  d->blocks = useful < 1 ? 1 : useful < resident ? useful : resident;
+  d->before_bytes = ((size_t)(c.sequences + 1) * sizeof(int) + 255) / 256 * 256;
+  d->bytes = d->before_bytes + ((size_t)d->blocks * DEC_WARPS + (size_t)lines) * d->cols * (dim + 2) * sizeof(float);
+  return true;
 }
 
-template <typename T, int NG, int NT>
+template <typename T, int NG, int HT>
 cudaError_t launch_decode(const DecodeParams& p, cudaStream_t stream) {
-  constexpr int D = 32 * NG;
-  constexpr size_t smem = (size_t)DEC_WARPS * 8 * NT * (D + 2) * sizeof(float);
-  cudaError_t e = cudaFuncSetAttribute(cache_attention_kernel<T, NG, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+  cudaError_t e = cudaFuncSetAttribute(cache_attention_kernel<T, NG, HT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kDecodeSmem<NG>);
   if (e != cudaSuccess) return e;
-  e = launch_after(cache_attention_kernel<T, NG, NT>, dim3((unsigned)p.chunks, (unsigned)(p.c.heads * p.blocks_of_heads), (unsigned)p.c.sequences),
-                   DEC_THREADS, smem, stream, p);
-  if (e != cudaSuccess || p.chunks == 1) return e;
-  return launch_after(cache_combine_kernel<NG, NT>, dim3((unsigned)p.heads, (unsigned)p.c.sequences), 128, 0, stream, p);
+  e = launch_after(cache_attention_kernel<T, NG, HT>, dim3((unsigned)(p.warps / DEC_WARPS)), DEC_THREADS, kDecodeSmem<NG>, stream, p);
+  if (e != cudaSuccess) return e;
+  return launch_after(cache_combine_kernel<NG, HT>, dim3((unsigned)p.heads, (unsigned)p.c.sequences), 32 * NG, 0, stream, p);
 }
 template <typename T>
 cudaError_t launch_decode(const DecodeParams& p, int dim, int cols, cudaStream_t stream) {
   const auto go = [&](auto ng) {
     constexpr int NG = decltype(ng)::value;
-    return cols == 8 ? launch_decode<T, NG, 1>(p, stream) : launch_decode<T, NG, 2>(p, stream);
+    return cols == 4 ? launch_decode<T, NG, 4>(p, stream) : cols == 8 ? launch_decode<T, NG, 8>(p, stream) : launch_decode<T, NG, 16>(p, stream);
   };
   switch (dim) {
     case 32: return go(std::integral_constant<int, 1>());
@@ -740,7 +935,8 @@ int lba_cache_read(const lba_cache* cache, const int32_t* start, const int32_t* 
 size_t lba_cache_attention_workspace_bytes(const lba_cache* cache, int heads) {
   CacheView c;
   if (view_of(cache, &c) != LBA_OK || heads < 1 || heads > 65535 || heads % c.heads) return 0;
-  return plan_decode(c, cache->dim, heads).bytes;
+  DecodePlan plan;
+  return plan_decode(c, cache->dim, heads, &plan) ? plan.bytes : 0;
 }
 
 int lba_cache_attention(const void* q, lba_strides q_at, int type, int heads, const lba_cache* cache, const int32_t* lengths, float scale,
@@ -753,22 +949,23 @@ int lba_cache_attention(const void* q, lba_strides q_at, int type, int heads, co
   if (cache->sequences == 0) return LBA_OK;
   if (!q || !out || !lengths || (cache->page_count > 0 && !cache->pages) || (cache->table_width > 0 && !cache->table)) return LBA_ERR_NULL;
   if (out_type == LBA_TYPE_CODES && !out_scale) return LBA_ERR_NULL;
-  const DecodePlan plan = plan_decode(p.c, cache->dim, heads);
-  if (plan.bytes && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < plan.bytes)) return LBA_ERR_WORKSPACE;
+  DecodePlan plan;
+  if (!plan_decode(p.c, cache->dim, heads, &plan)) return LBA_ERR_SHAPE;
+  if ((!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < plan.bytes)) return LBA_ERR_WORKSPACE;
   p.q = q;
   p.q_at = q_at;
   p.lengths = lengths;
   p.heads = heads;
   p.group = heads / cache->kv_heads;
-  p.blocks_of_heads = plan.pieces;
-  p.chunk = plan.chunk;
-  p.chunks = plan.chunks;
+  p.pieces = plan.pieces;
+  p.warps = plan.blocks * DEC_WARPS;
   p.scale = scale;
   p.out_type = out_type;
   p.in_m4e3 = out_flags & LBA_FLAG_INPUT_M4E3;
   p.out_scale = out_scale;
   p.out = out;
-  p.parts = static_cast<float*>(workspace);
+  p.before = static_cast<int*>(workspace);
+  p.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(workspace) + plan.before_bytes);
   return status_of(type == LBA_TYPE_BF16 ? launch_decode<__nv_bfloat16>(p, cache->dim, plan.cols, (cudaStream_t)stream)
                                          : launch_decode<__half>(p, cache->dim, plan.cols, (cudaStream_t)stream));
 }
