@@ -46,6 +46,7 @@ struct RowsParams {
   lba_strides k_at, v_at;
   int64_t tokens;
   const int32_t *start, *cu;
+  int block_heads;
 };
 
 // The (page, row) of token row t, or false.  `cu` was brought to shared memory where it fits.
@@ -78,9 +79,11 @@ __device__ __forceinline__ bool locate(const P& p, const int32_t* cu_shared, int
   return *page >= 0 && *page < p.c.page_count;
 }
 
-// A thread takes eight neighbouring values: a quarter of a group.  Blocks are rows (tokens) of one head's keys or values.
+// A lane takes eight neighbouring values, a quarter of a group; a warp a few tokens (those of 32 / (D / 8) rows), whose places it looks up once, and
+// walks over heads, a key and a value row of each token at a time and the next head's on their way.  Bound by memory; (with a block of 16
+// tokens for each head that looked up its own tokens, 12000 tokens of 8 heads took 41 us, three quarters of it issue slots).
 template <int D> constexpr int kRowSplit = D / 8;
-template <int D> constexpr int kBlockRows = ROW_THREADS / kRowSplit<D>;
+template <int D> constexpr int kWarpRows = 32 / kRowSplit<D>;
 
 __device__ __forceinline__ uint32_t encode8(const float (&x)[8]) {  // eight values as 4-bit codes, the first in the lowest bits
   uint32_t d;
@@ -122,108 +125,169 @@ __device__ __forceinline__ void store8(T* dst, const float (&x)[8]) {
   }
 }
 
+// what a lane reads and writes of one row, and their change from head to head
+template <typename T>
+struct Walk8 {
+  T* number;
+  uint8_t *codes, *exps;
+  __device__ __forceinline__ void next(int64_t stride, int64_t run) {
+    number += stride;
+    codes += run;
+    exps += run;
+  }
+};
+
+// 2^-e of a group from its largest magnitude's bits, and its exponent byte (255: not a number)
+__device__ __forceinline__ float group_scale(uint32_t top, int* byte) {
+  int e = (int)(top >> 23) - 129 + ((top & 0x7FFFFFu) > 0x400000u);  // 1.f 2^E <= 1.5 2^(e+2)
+  e = e < -126 ? -126 : e > 125 ? 125 : e;                            // (6 2^126 is no binary32 number)
+  *byte = top >= 0x7F800000u ? 255 : e + 127;
+  return __uint_as_float((uint32_t)(127 - e) << 23);
+}
+
 template <typename T, int D, bool READ>
 __global__ void __launch_bounds__(ROW_THREADS) cache_rows_kernel(const RowsParams p) {
-  constexpr int SPLIT = kRowSplit<D>, ROWS = kBlockRows<D>;
+  constexpr int SPLIT = kRowSplit<D>, ROWS = kWarpRows<D>;
   __shared__ int32_t cu[MAX_CU];
-  __shared__ __align__(16) uint8_t stage[ROWS * D / 2];
+  __shared__ __align__(16) uint8_t stage[ROW_THREADS / 32][ROWS * D / 2];
   after_previous();
-  const bool values = blockIdx.y >= (unsigned)p.c.heads;
-  const int head = blockIdx.y - (values ? p.c.heads : 0);
-  const int r = threadIdx.x / SPLIT, q = threadIdx.x % SPLIT;  // row of the block, eighth values q
-  const int64_t t = (int64_t)blockIdx.x * ROWS + r;
-  const bool there = r < ROWS && t < p.tokens;
-  const lba_strides at = values ? p.v_at : p.k_at;
-  T* const mine = static_cast<T*>(const_cast<void*>(values ? p.v : p.k)) + t * at.token + head * at.head + q * 8;
-  float x[8];
-  if (!READ && there) load8<T>(mine, x);   // on its way while the token's place is looked up
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, r = lane / SPLIT, q = lane % SPLIT;  // row of the warp, eighth values q
+  const int64_t t = ((int64_t)blockIdx.x * (ROW_THREADS / 32) + warp) * ROWS + r;
+  const int h0 = blockIdx.y * p.block_heads, h1 = min(h0 + p.block_heads, p.c.heads);
   if (p.cu && p.c.sequences < MAX_CU) {
     for (int i = threadIdx.x; i <= p.c.sequences; i += ROW_THREADS) cu[i] = p.cu[i];
     __syncthreads();
   }
+  const bool there = r < ROWS && t < p.tokens;
   int64_t page = -1;
   int row = 0;
-  bool in_sequence = there;
+  bool stored = there, in_sequence = there;  // stored: has a place in the cache
   if (there) {
-    const bool found = locate(p, cu, t, &page, &row);
-    if (!found) page = -1;
+    stored = locate(p, cu, t, &page, &row);
     if (READ && p.cu) {  // (a row of a sequence whose token is not there reads as 0; one of no sequence is left)
-      in_sequence = found || (t >= (p.c.sequences < MAX_CU ? cu[0] : p.cu[0]) && t < (p.c.sequences < MAX_CU ? cu[p.c.sequences] : p.cu[p.c.sequences]));
+      const int32_t* const all = p.c.sequences < MAX_CU ? cu : p.cu;
+      in_sequence = stored || (t >= all[0] && t < all[p.c.sequences]);
     } else if (READ) {
       in_sequence = t < p.c.sequences;
     }
   }
-  uint8_t* const codes = page < 0 ? nullptr : plane<D>(p.c, page, head, values ? 1 : 0) + (int64_t)row * (D / 2);
-  uint8_t* const exps = page < 0 ? nullptr : plane<D>(p.c, page, head, values ? 3 : 2) + (int64_t)row * (D / 32);
-  uint8_t* const line = stage + r * (D / 2);
+  const int64_t run = p.c.run(D);
   // a key row's eighth q = 4 g + c is the word at c D/8 + 4 g; a value row's q = 2 i + h are bytes (4 h + j) D/16 + i
-  const int word_at = (q & 3) * (D / 8) + (q >> 2) * 4;
+  Walk8<T> k, v;
+  k.number = static_cast<T*>(const_cast<void*>(p.k)) + t * p.k_at.token + h0 * p.k_at.head + q * 8;
+  v.number = static_cast<T*>(const_cast<void*>(p.v)) + t * p.v_at.token + h0 * p.v_at.head + q * 8;
+  if (!stored) page = 0;
+  k.codes = plane<D>(p.c, page, h0, 0) + row * (D / 2) + (q & 3) * (D / 8) + (q >> 2) * 4;
+  v.codes = plane<D>(p.c, page, h0, 1) + row * (D / 2) + 4 * q;
+  k.exps = plane<D>(p.c, page, h0, 2) + row * (D / 32) + (q >> 2);
+  v.exps = plane<D>(p.c, page, h0, 3) + row * (D / 32) + (q >> 2);
+  uint8_t* const line = stage[warp] + min(r, ROWS - 1) * (D / 2);
   if constexpr (!READ) {
-    uint32_t top = 0;
-    if (there) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+    float x[8], y[8];
+    if (there && h0 < h1) {
+      load8<T>(k.number, x);
+      load8<T>(v.number, y);
     }
-    // the four lanes of a group (SPLIT is a multiple of four; rows that are not there reduce zeros)
-    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-    const bool lost = top >= 0x7F800000u;
-    int e = (int)(top >> 23) - 129 + ((top & 0x7FFFFFu) > 0x400000u);  // 1.f 2^E <= 1.5 2^(e+2)
-    e = e < -126 ? -126 : e > 125 ? 125 : e;  // (6 2^126 is no binary32 number)
-    const float by = __uint_as_float((uint32_t)(127 - e) << 23);
-    if (there && page >= 0) {
-      uint32_t w = 0;
-      if (!lost) {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) x[j] *= by;
-        w = encode8(x);
-      }
-      if (values) {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) line[((q & 1) * 4 + j) * (D / 16) + (q >> 1)] = (uint8_t)(w >> (8 * j));
-      } else {
-        *reinterpret_cast<uint32_t*>(codes + word_at) = w;
-      }
-      if ((q & 3) == 0) exps[q >> 2] = lost ? 255 : (uint8_t)(e + 127);
-    }
-    if (!values) return;
-    __syncthreads();
-    if (there && page >= 0) *reinterpret_cast<uint32_t*>(codes + 4 * q) = *reinterpret_cast<const uint32_t*>(line + 4 * q);
-  } else {
-    uint32_t w = 0, exp = 0;
-    if (page >= 0) {
-      w = *reinterpret_cast<const uint32_t*>(codes + (values ? 4 * q : word_at));
-      exp = exps[q >> 2];
-    }
-    if (values) {
-      if (there) *reinterpret_cast<uint32_t*>(line + 4 * q) = w;
-      __syncthreads();
-      w = 0;
+#pragma unroll 1
+    for (int h = h0; h < h1; ++h) {
+      uint32_t top_x = 0, top_y = 0;
       if (there) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          top_x = max(top_x, __float_as_uint(x[j]) & 0x7FFFFFFFu);
+          top_y = max(top_y, __float_as_uint(y[j]) & 0x7FFFFFFFu);
+        }
+      }
+      // the four lanes of a group (lanes beyond the last row reduce zeros)
+#pragma unroll
+      for (int d = 1; d < 4; d *= 2) {
+        top_x = max(top_x, __shfl_xor_sync(0xFFFFFFFFu, top_x, d));
+        top_y = max(top_y, __shfl_xor_sync(0xFFFFFFFFu, top_y, d));
+      }
+      int byte_x, byte_y;
+      const float by_x = group_scale(top_x, &byte_x), by_y = group_scale(top_y, &byte_y);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        x[j] *= by_x;
+        y[j] *= by_y;
+      }
+      const uint32_t wx = byte_x == 255 ? 0u : encode8(x), wy = byte_y == 255 ? 0u : encode8(y);
+      Walk8<T> to_k = k, to_v = v;
+      k.next(p.k_at.head, run);
+      v.next(p.v_at.head, run);
+      if (there && h + 1 < h1) {
+        load8<T>(k.number, x);
+        load8<T>(v.number, y);
+      }
+      if (r < ROWS) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) line[((q & 1) * 4 + j) * (D / 16) + (q >> 1)] = (uint8_t)(wy >> (8 * j));
+      }
+      __syncwarp();
+      if (stored) {
+        *reinterpret_cast<uint32_t*>(to_k.codes) = wx;
+        *reinterpret_cast<uint32_t*>(to_v.codes) = *reinterpret_cast<const uint32_t*>(line + 4 * q);
+        if ((q & 3) == 0) {
+          *to_k.exps = (uint8_t)byte_x;
+          *to_v.exps = (uint8_t)byte_y;
+        }
+      }
+      __syncwarp();
+    }
+  } else {
+    uint32_t wk = 0, wv = 0, ek = 0, ev = 0;
+    const auto fetch = [&] {
+      if (stored) {
+        wk = *reinterpret_cast<const uint32_t*>(k.codes);
+        wv = *reinterpret_cast<const uint32_t*>(v.codes);
+        ek = *k.exps;
+        ev = *v.exps;
+      }
+    };
+    if (h0 < h1) fetch();
+#pragma unroll 1
+    for (int h = h0; h < h1; ++h) {
+      if (r < ROWS) *reinterpret_cast<uint32_t*>(line + 4 * q) = wv;
+      __syncwarp();
+      uint32_t w = 0;
+      if (r < ROWS) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) w |= (uint32_t)line[((q & 1) * 4 + j) * (D / 16) + (q >> 1)] << (8 * j);
       }
-    }
-    if (!in_sequence) return;
-    uint32_t h[4];
-    decode8(w, h);
-    const float by = exp == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float(exp << 23);
+      __syncwarp();
+      const auto write = [&](uint32_t word, uint32_t exp, T* to) {
+        uint32_t h2[4];
+        decode8(word, h2);
+        const float by = exp == 255 ? __uint_as_float(0x7FC00000u) : __uint_as_float(exp << 23);
+        float x[8];
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const float2 f = widen(h[j]);
-      x[2 * j] = f.x * by;
-      x[2 * j + 1] = f.y * by;
+        for (int j = 0; j < 4; ++j) {
+          const float2 f = widen(h2[j]);
+          x[2 * j] = f.x * by;
+          x[2 * j + 1] = f.y * by;
+        }
+        if (in_sequence) store8<T>(to, x);
+      };
+      const uint32_t word = wk, exp_k = ek, exp_v = ev;
+      T *const to_k = k.number, *const to_v = v.number;
+      k.next(p.k_at.head, run);
+      v.next(p.v_at.head, run);
+      if (h + 1 < h1) fetch();
+      write(word, exp_k, to_k);
+      write(w, exp_v, to_v);
     }
-    store8<T>(mine, x);
   }
 }
 
 template <bool READ, typename T>
-cudaError_t launch_rows(const RowsParams& p, int dim, cudaStream_t stream) {
+cudaError_t launch_rows(RowsParams p, int dim, cudaStream_t stream) {
   const auto go = [&](auto d) {
-    constexpr int D = decltype(d)::value;
-    return launch_after(cache_rows_kernel<T, D, READ>, dim3((unsigned)((p.tokens + kBlockRows<D> - 1) / kBlockRows<D>), (unsigned)(2 * p.c.heads)),
-                        ROW_THREADS, 0, stream, p);
+    constexpr int D = decltype(d)::value, ROWS = kWarpRows<D> * (ROW_THREADS / 32);
+    // heads of a block: all, or as few as bring eight blocks to every SM
+    const int64_t blocks = (p.tokens + ROWS - 1) / ROWS, parts = (8LL * device_sms() + blocks - 1) / blocks;
+    p.block_heads = (int)((p.c.heads + parts - 1) / parts);
+    return launch_after(cache_rows_kernel<T, D, READ>, dim3((unsigned)blocks, (unsigned)((p.c.heads + p.block_heads - 1) / p.block_heads)), ROW_THREADS, 0,
+                        stream, p);
   };
   switch (dim) {
     case 32: return go(std::integral_constant<int, 32>());

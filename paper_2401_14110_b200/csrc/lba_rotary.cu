@@ -1,9 +1,11 @@
 // Rotary positions: pair (x, y) of a head at position p and frequency f becomes (x cos pf - y sin pf, x sin pf + y cos pf) scale.
 //
-// Bound by memory: a value is read once and written once.  A block takes a few tokens: it forms their cosines and sines once in shared
-// memory, then all heads of q and k use them.  Angles are formed in binary64 and reduced to a quarter turn there, which costs some 60
-// instructions a pair of a token against 40 heads' loads and stores; in binary32 position 100000 would be off by 0.004.  A thread's first
-// values are on their way while the table is formed: for single tokens that is one trip to memory instead of two.
+// Bound by memory: a value is read once and written once.  A thread keeps a place in the row of a token, a head's pairs or some of its passing
+// values, and walks over the tokens of its block, the next one's values on their way; cosines and sines of the block's tokens come from a table in
+// shared memory that its threads form first, while the first values are on their way (for single tokens that is one trip to memory instead of
+// two).  Angles are formed in binary64 and reduced to a quarter turn there, some 50 instructions a pair of a token against 40 heads' loads
+// and stores; in binary32 position 100000 would be off by 0.004.  (With places and tokens found by division for every piece, 8191 tokens of
+// 40 heads took 46 us, 270 instructions a piece.)
 #include <cmath>
 
 #include "lba_entry.cuh"
@@ -12,7 +14,7 @@
 namespace lba {
 namespace {
 
-constexpr int ROT_THREADS = 256, ROT_AHEAD = 2, ROT_TABLE = 48 * 1024;
+constexpr int ROT_THREADS = 512, ROT_TABLE = 48 * 1024;
 
 struct RotaryParams {
   const void *q, *k;
@@ -23,91 +25,78 @@ struct RotaryParams {
   int64_t tokens;
   int heads, all_heads;       // of q; of both
   int pairs, rest;            // a head's pairs, and its values that pass
-  int items, rot_items;       // pieces of work of a head: PV pairs each, then 2 PV passing values each
-  int tile, block_heads;      // tokens and heads of a block
+  int items, rot_items;       // pieces of a head: PV pairs each, then 2 PV passing values each
+  int tile;                   // tokens of a block
   int wide_positions, inverse;
   float scale;
 };
 
 template <typename T, int N, int ALIGN> struct alignas(ALIGN) Few { T v[N]; };
 
-// one piece: where it comes from and goes to, and its values
 template <typename T, int PV, bool INTER>
-struct Piece {
-  T* to;
-  static constexpr int RUN = INTER ? 2 * PV : PV;
-  Few<T, RUN, PV == 1 ? sizeof(T) : RUN * sizeof(T)> a, b;  // half layout: two runs
-  int token, pair;                   // pair < 0: passes
-  __device__ __forceinline__ void load(const RotaryParams& p, int i, int64_t t0, int h0, int hs) {
-    const int c = i % p.items, r = i / p.items;
-    const int h = h0 + r % hs;
-    token = r / hs;
-    const bool is_q = h < p.heads;
-    const int head = is_q ? h : h - p.heads;
-    const lba_strides from_at = is_q ? p.q_at : p.k_at, to_at = is_q ? p.q_out_at : p.k_out_at;
-    const int64_t t = t0 + token;
-    pair = c < p.rot_items ? c * PV : -1;
-    const int first = c < p.rot_items ? (INTER ? 2 * c * PV : c * PV) : 2 * p.pairs + (c - p.rot_items) * 2 * PV;
-    const T* const from = static_cast<const T*>(is_q ? p.q : p.k) + t * from_at.token + head * from_at.head + first;
-    to = static_cast<T*>(is_q ? p.q_out : p.k_out) + t * to_at.token + head * to_at.head + first;
-    a = *reinterpret_cast<const decltype(a)*>(from);
-    if (!INTER) b = *reinterpret_cast<const decltype(b)*>(from + step(p));
-  }
-  __device__ __forceinline__ int step(const RotaryParams& p) const { return pair < 0 ? PV : p.pairs; }
-  __device__ __forceinline__ void turn(const RotaryParams& p, const float2* table) {
-    if (pair >= 0) {
-      const float2* const w = table + token * p.pairs + pair;
-#pragma unroll
-      for (int j = 0; j < PV; ++j) {
-        T& x = INTER ? a.v[2 * j] : a.v[j];
-        T& y = INTER ? a.v[INTER ? 2 * j + 1 : j] : b.v[j];
-        const float fx = to_f32(x), fy = to_f32(y), c = w[j].x, s = w[j].y;
-        x = from_f32<T>(fx * c - fy * s);
-        y = from_f32<T>(fx * s + fy * c);
-      }
-    }
-    *reinterpret_cast<decltype(a)*>(to) = a;
-    if (!INTER) *reinterpret_cast<decltype(b)*>(to + step(p)) = b;
-  }
-};
-
-template <typename T, int PV, bool INTER>
-__global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(const RotaryParams p) {
+__global__ void __launch_bounds__(ROT_THREADS, 3) rotary_kernel(const RotaryParams p) {
+  constexpr int RUN = INTER ? 2 * PV : PV;
+  typedef Few<T, RUN, PV == 1 ? sizeof(T) : RUN * sizeof(T)> Vec;
   extern __shared__ float2 table[];  // [tokens][pairs]: cosine, sine
   after_previous();
   const int64_t t0 = (int64_t)blockIdx.x * p.tile;
   const int tokens = p.tokens - t0 < p.tile ? (int)(p.tokens - t0) : p.tile;
-  const int h0 = blockIdx.y * p.block_heads, hs = p.all_heads - h0 < p.block_heads ? p.all_heads - h0 : p.block_heads;
-  const int total = tokens * hs * p.items;
-  Piece<T, PV, INTER> piece[ROT_AHEAD];
-#pragma unroll
-  for (int u = 0; u < ROT_AHEAD; ++u) {
-    const int i = threadIdx.x + u * ROT_THREADS;
-    if (i < total) piece[u].load(p, i, t0, h0, hs);
-  }
-  for (int i = threadIdx.x; i < tokens * p.pairs; i += ROT_THREADS) {
+  const int place = blockIdx.y * blockDim.x + threadIdx.x;
+  const bool mine = place < p.all_heads * p.items;
+  const int h = place / p.items, c = place - h * p.items;
+  const bool is_q = h < p.heads, turns = c < p.rot_items;
+  const int head = is_q ? h : h - p.heads;
+  const lba_strides from_at = is_q ? p.q_at : p.k_at, to_at = is_q ? p.q_out_at : p.k_out_at;
+  const int first = turns ? (INTER ? 2 * c * PV : c * PV) : 2 * p.pairs + (c - p.rot_items) * 2 * PV, step = turns ? p.pairs : PV;
+  const T* from = static_cast<const T*>(is_q ? p.q : p.k) + t0 * from_at.token + head * from_at.head + first;
+  T* to = static_cast<T*>(is_q ? p.q_out : p.k_out) + t0 * to_at.token + head * to_at.head + first;
+  Vec a, b;  // half layout, and what passes: two runs
+  const auto load = [&] {
+    a = *reinterpret_cast<const Vec*>(from);
+    if (!INTER) b = *reinterpret_cast<const Vec*>(from + step);
+    from += from_at.token;
+  };
+  if (mine) load();
+  for (int i = threadIdx.x; i < tokens * p.pairs; i += blockDim.x) {
     const int t = i / p.pairs, j = i - t * p.pairs;
     const int64_t at = t0 + t;
     const double pos = p.wide_positions ? (double)static_cast<const int64_t*>(p.positions)[at] : (double)static_cast<const int32_t*>(p.positions)[at];
     const double quarters = pos * p.freqs[j] * 0.63661977236758134308;  // 2 / pi
     const double whole = rint(quarters);
-    const int quadrant = (int)(whole - 4.0 * floor(whole * 0.25));
-    float s, c;
-    sincospif(0.5f * (float)(quarters - whole), &s, &c);
-    float2 w = quadrant == 0 ? make_float2(c, s) : quadrant == 1 ? make_float2(-s, c) : quadrant == 2 ? make_float2(-c, -s) : make_float2(s, -c);
+    const int quadrant = (int)__double2ll_rn(whole) & 3;
+    // sine and cosine of at most an eighth of a turn: their series, what is left out below 2^-28 of them
+    const float x = (float)(quarters - whole) * 1.57079632679f, x2 = x * x;
+    const float s = fmaf(x * x2, fmaf(x2, fmaf(x2, fmaf(x2, 1.0f / 362880, -1.0f / 5040), 1.0f / 120), -1.0f / 6), x);
+    const float c = fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, fmaf(x2, -1.0f / 3628800, 1.0f / 40320), -1.0f / 720), 1.0f / 24), -0.5f), 1.0f);
+    float2 w = quadrant & 1 ? make_float2(-s, c) : make_float2(c, s);
+    if (quadrant & 2) w = make_float2(-w.x, -w.y);
     if (p.inverse) w.y = -w.y;
-    table[i] = make_float2(w.x * p.scale, w.y * p.scale);
+    // (a thread's PV pairs lie a row of pieces apart, two and two, so that neighbouring threads' 16 bytes are neighbours)
+    const int piece = PV == 1 ? j : 2 * (((j % PV) / 2) * p.rot_items + j / PV) + j % 2;
+    table[t * p.pairs + piece] = make_float2(w.x * p.scale, w.y * p.scale);
   }
   __syncthreads();
-  for (int i0 = threadIdx.x; i0 < total; i0 += ROT_AHEAD * ROT_THREADS) {
+  if (!mine) return;
+  const float2* w = table + (turns ? (PV == 1 ? c : 2 * c) : 0);
+#pragma unroll 1
+  for (int t = 0; t < tokens; ++t) {
+    Vec x = a, y = b;
+    if (t + 1 < tokens) load();
+    if (turns) {
 #pragma unroll
-    for (int u = 0; u < ROT_AHEAD; ++u)
-      if (i0 + u * ROT_THREADS < total) piece[u].turn(p, table);
-#pragma unroll
-    for (int u = 0; u < ROT_AHEAD; ++u) {
-      const int i = i0 + (ROT_AHEAD + u) * ROT_THREADS;
-      if (i < total) piece[u].load(p, i, t0, h0, hs);
+      for (int j = 0; j < PV; ++j) {
+        T& first_of = INTER ? x.v[2 * j] : x.v[j];
+        T& second_of = INTER ? x.v[INTER ? 2 * j + 1 : j] : y.v[j];
+        const float2 cs = PV == 1 ? w[0] : w[2 * (j / 2) * p.rot_items + j % 2];
+        const float fx = to_f32(first_of), fy = to_f32(second_of);
+        first_of = from_f32<T>(fx * cs.x - fy * cs.y);
+        second_of = from_f32<T>(fx * cs.y + fy * cs.x);
+      }
     }
+    *reinterpret_cast<Vec*>(to) = x;
+    if (!INTER) *reinterpret_cast<Vec*>(to + step) = y;
+    to += to_at.token;
+    w += p.pairs;
   }
 }
 
@@ -125,17 +114,15 @@ cudaError_t run_rotary(RotaryParams p, cudaStream_t stream) {
   }
   p.rot_items = p.pairs / PV;
   p.items = p.rot_items + p.rest / (2 * PV);
-  // Tokens of a block: as many as leave four blocks an SM, eight at most; with few tokens the heads are divided too
-  const int sms = device_sms();
-  const int64_t fair = p.tokens / (4 * sms);
-  p.tile = (int)(fair < 1 ? 1 : fair > 8 ? 8 : fair);
+  // Places in equal blocks of whole warps.  Tokens of a block: five, or as many as leave four blocks an SM.  Blocks form their tables while others
+  // move values: 8191 tokens of 40 heads took 46 us with all blocks in one round of twelve tokens, 37 with eight tokens, 35 with five, 52 with one.
+  const int64_t places = (int64_t)p.all_heads * p.items;
+  const int64_t parts = (places + ROT_THREADS - 1) / ROT_THREADS, threads = ((places + parts - 1) / parts + 31) / 32 * 32;
+  const int64_t fair = p.tokens / (4 * device_sms());
+  p.tile = (int)(fair < 1 ? 1 : fair > 5 ? 5 : fair);
   while (p.tile > 1 && (size_t)p.tile * p.pairs * sizeof(float2) > ROT_TABLE) --p.tile;
-  const int64_t blocks = (p.tokens + p.tile - 1) / p.tile;
-  int64_t parts = blocks >= 2 * sms ? 1 : (2 * sms + blocks - 1) / blocks;
-  if (parts > p.all_heads) parts = p.all_heads;
-  p.block_heads = (int)((p.all_heads + parts - 1) / parts);
-  const dim3 grid((unsigned)blocks, (unsigned)((p.all_heads + p.block_heads - 1) / p.block_heads));
-  return launch_after(rotary_kernel<T, PV, INTER>, grid, ROT_THREADS, (size_t)p.tile * p.pairs * sizeof(float2), stream, p);
+  const dim3 grid((unsigned)((p.tokens + p.tile - 1) / p.tile), (unsigned)((places + threads - 1) / threads));
+  return launch_after(rotary_kernel<T, PV, INTER>, grid, (int)threads, (size_t)p.tile * p.pairs * sizeof(float2), stream, p);
 }
 template <typename T>
 cudaError_t run_rotary(const RotaryParams& p, bool interleaved, cudaStream_t stream) {
