@@ -169,7 +169,9 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
             full(2 * j);
             if (!ok) return;
             const uint64_t a = rows + ((q_smem + w * TILE) >> 4), b = rows + ((ring + (2 * j % STAGES) * TILE) >> 4);
-            for (int s = 0; s < steps; ++s) {
+#pragma unroll
+            for (int s = 0; s < DT / 16; ++s) {
+              if (s >= steps) break;
               const int at = ((s >> 2) * HALF + (s & 3) * 32) >> 4;
               mma_shared(tmem + w * KT, a + at, b + at, kind_s, s != 0);
             }
@@ -193,6 +195,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
               if (!ok) break;
               tmem_after();
               const uint64_t b = lines + ((ring + vs * TILE) >> 4);
+#pragma unroll
               for (int s = 0; s < KT / 16; ++s)
                 mma_tensor(tmem + 256 + w * 128, tmem + w * KT + s * 8, b + s * (2048 >> 4), kind_o, j != 0 || s != 0);
               if (j + 1 < tiles[w]) scores(w, j + 1);

@@ -5,19 +5,22 @@
 //
 // Two launches.  attention_delta_kernel forms delta and turns lse into powers of two, reading grad_out and out once.  Then
 // attention_grad_kernel: a CTA takes 128 rows that stay, of q (for grad_q) or of k and v (for grad_k and grad_v, over all query heads of
-// the group), and walks over 64 rows of the others at a time:
-//   T1 = X1 Y1^T (scores), T2 = X2 Y2^T (dp)       X: q, g or k, v: shared memory for the whole CTA; Y: the other two, from a ring
-//   p and ds from T1 and T2, in registers          two warpgroups, each every second tile, a row a thread
+// the group), and walks over 128 rows of the others at a time:
+//   T1 = X1 Y1^T (scores), T2 = X2 Y2^T (dp)       X: q, g or k, v: shared memory for the whole CTA; Y: the other two, from two rings
+//   p from T1, then ds from T2                     two warpgroups, 64 columns each, a row a thread
 //   acc1 += ds Y1, and for keys acc2 += p Y2       p and ds lie in tensor memory over T1 and T2, sums in 128 more columns each
 // Scores and dp are so formed twice, seven products where five would do; in return every sum is formed by one CTA in a fixed order, and no
 // 32-bit gradient of q goes through memory or atomics.
 //
-// p is rounded to the inputs' type on its way into the product, and ds held as two pieces of it: delta comes from an output of 16 bits, and one
-// rounding more of ds would leave grad_q and grad_k off by 1.5 times what their own rounding costs (with two pieces by 1.1 times).  binary16
-// has few exponents: p is held times 2^8, and ds times a power of two chosen from the largest |grad_out| and |v| so that it cannot overflow.
+// Bound by the matrix instructions, 512 clocks each.  They follow one another without a pause: for keys acc2(n), T1(n+1), acc1(n), T2(n+1), so that
+// p of tile n+1 is formed while acc1(n) and T2(n+1) run, and ds of tile n while acc2(n) and T1(n+1) do; for queries T1(n+1), acc1(n), T2(n+1).
+// (Tiles of 64 rows, two of them in flight, a warpgroup each: with 64 columns a product wants 192 bytes of shared memory a clock, or 128 of
+// tensor memory, and took 57 clocks a step instead of 32; 2 x 4096 tokens of 16 heads took 515 us.)
 //
-// Bound by the matrix instructions.  128 x 64 scores with both operands in shared memory want 192 bytes a clock where 128 are there, 384 clocks
-// instead of 256, so a query block's X lies in tensor memory (1024 clocks a tile); a key block has no columns left for that (1536).
+// p and ds are rounded to the inputs' type on their way into the products, which leaves gradients off by 1.4 times what their own rounding
+// costs.  delta comes from an output of 16 bits; where few keys are seen, that would add as much again (1.6 times with four keys), so rows
+// of up to 32 keys get theirs from p and dp.  binary16 has few exponents: p is held times 2^8, and ds times a power of two chosen from the
+// largest |grad_out| and |v| so that it cannot overflow.
 #include <cmath>
 
 #include "lba_tile.cuh"
@@ -25,29 +28,28 @@
 namespace lba {
 namespace {
 
-constexpr int XT = 128, YT = 64, GRAD_THREADS = 384, GRAD_STAGES = 4, DELTA_THREADS = 256;
+constexpr int XT = 128, YT = 128, YC = 64, GRAD_THREADS = 384, Y1_SLOTS = 3, Y2_SLOTS = 2, CUTS = 4, DELTA_THREADS = 256;  // YC: columns of a warpgroup
 constexpr float P_UP = 256.0f;
 constexpr int P_BITS = 8;
 
 struct GradParams {
-  CUtensorMap q, k, v, g;    // boxes of 64 rows
+  CUtensorMap q, k, v, g;    // boxes of 128 rows
   const int32_t *cu_q, *cu_k;
   int64_t q_rows, k_rows, key_blocks;
   int sequences, heads, kv_heads, group, dim, causal, bf;
   float to_log2, scale;
-  const void *q_raw, *g_raw; // contiguous grad_out
-  lba_strides q_at;
   const float2* stats;       // [heads][q_rows]: lse in powers of two, delta
   const uint32_t* most;      // largest |grad_out|, |v| as bits (binary16), or null
   void *grad_q, *grad_k, *grad_v;
 };
 struct DeltaParams {
-  const void *g, *out, *v;
-  lba_strides v_at;
+  const void *g, *out, *q, *k, *v;
+  lba_strides q_at, k_at, v_at;
   const float* lse;
   const int32_t *cu_q, *cu_k;
   int64_t q_rows, k_rows;
-  int sequences, heads, kv_heads, dim;
+  int sequences, heads, kv_heads, dim, causal;
+  float to_log2;
   float2* stats;
   uint32_t* most;
   void *grad_q, *grad_k, *grad_v;
@@ -55,6 +57,12 @@ struct DeltaParams {
 
 // ------------------------------------------------------------------ delta
 // A group of 16 lanes takes a row's head.  Rows of no sequence get gradients of 0.
+constexpr int FEW_KEYS = 32;
+__device__ __forceinline__ float sum16(float v, unsigned lanes) {
+#pragma unroll
+  for (int x = 8; x > 0; x /= 2) v += __shfl_xor_sync(lanes, v, x);
+  return v;
+}
 template <typename T>
 __global__ void __launch_bounds__(DELTA_THREADS) attention_delta_kernel(const DeltaParams p) {
   after_previous();
@@ -82,12 +90,54 @@ __global__ void __launch_bounds__(DELTA_THREADS) attention_delta_kernel(const De
         *reinterpret_cast<uint4*>(static_cast<T*>(p.grad_q) + i) = make_uint4(0u, 0u, 0u, 0u);
       }
     }
+    const unsigned lanes = 0xFFFFu << (threadIdx.x & 16);
+    sum = sum16(sum, lanes);
+    const float lse = inside ? p.lse[head * p.q_rows + row] : 0.0f;
+    if (inside) {
+      int b = 0;  // the last sequence that begins at or before the row
+      if (p.cu_q) {
+        int hi = p.sequences - 1;
+        while (b < hi) {
+          const int mid = (b + hi + 1) / 2;
+          if (p.cu_q[mid] <= row) b = mid;
+          else hi = mid - 1;
+        }
+      }
+      int q_first, q_count, k_first, k_count;
+      rows_of(p.cu_q, p.q_rows, b, &q_first, &q_count);
+      rows_of(p.cu_k, p.k_rows, b, &k_first, &k_count);
+      const int keys = p.causal ? min(k_count, (int)row - q_first + k_count - q_count + 1) : k_count;
+      if (keys > 0 && keys <= FEW_KEYS) {
+        const int kv = head / (p.heads / p.kv_heads);
+        float q[8], g[8], top = 0.0f;
+        sum = 0.0f;
 #pragma unroll
-    for (int x = 8; x > 0; x /= 2) sum += __shfl_xor_sync(0xFFFFu << (threadIdx.x & 16), sum, x);
-    if (sub == 0) {
-      const float lse = inside ? p.lse[head * p.q_rows + row] : 0.0f;
-      p.stats[head * p.q_rows + row] = make_float2(lse == -INFINITY ? INFINITY : lse * LOG2E, sum);
+        for (int e = 0; e < 8; ++e) q[e] = g[e] = 0.0f;
+        if (d < p.dim) {
+          load_some<T, 8>(static_cast<const T*>(p.q) + row * p.q_at.token + head * p.q_at.head, d, 8, q);
+          load_some<T, 8>(p.g, at * p.dim + d, 8, g);
+        }
+        for (int j = 0; j < keys; ++j) {
+          float s = 0.0f, dp = 0.0f, x[8], y[8];
+          if (d < p.dim) {
+            load_some<T, 8>(static_cast<const T*>(p.k) + (int64_t)(k_first + j) * p.k_at.token + kv * p.k_at.head, d, 8, x);
+            load_some<T, 8>(static_cast<const T*>(p.v) + (int64_t)(k_first + j) * p.v_at.token + kv * p.v_at.head, d, 8, y);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+              s = fmaf(q[e], x[e], s);
+              dp = fmaf(g[e], y[e], dp);
+            }
+          }
+          s = sum16(s, lanes);
+          dp = sum16(dp, lanes);
+          const float w = exp2_approx(fmaf(s, p.to_log2, -lse * LOG2E));
+          sum = fmaf(w, dp, sum);
+          top += w;
+        }
+        sum = __fdividef(sum, top);  // (1, but for rounding)
+      }
     }
+    if (sub == 0) p.stats[head * p.q_rows + row] = make_float2(lse == -INFINITY ? INFINITY : lse * LOG2E, sum);
   }
   if (at < m && d < p.dim) {
     const int64_t row = at / p.kv_heads;
@@ -121,15 +171,16 @@ __device__ __forceinline__ int ds_bits(const GradParams& p) {
 }
 
 // ------------------------------------------------------------------ gradients
-template <int DT> constexpr int kX = XT * DT * 2;  // bytes of a tile
-template <int DT> constexpr int kY = YT * DT * 2;
-template <int DT> constexpr size_t kGradSmem = 1024 + 2 * (size_t)kX<DT> + 2 * (size_t)kY<DT> * GRAD_STAGES;
+template <int DT> constexpr int kGradTile = 128 * DT * 2;  // bytes of 128 rows
+template <int DT> constexpr size_t kGradSmem = 1024 + (size_t)kGradTile<DT> * (2 + Y1_SLOTS + Y2_SLOTS);
 
 struct GradShared {
-  uint64_t x_full, x_there, full[GRAD_STAGES], empty[GRAD_STAGES], cut_full[4], clean[4], products[2], weights[2], done;
+  uint64_t x_full, full1[Y1_SLOTS], empty1[Y1_SLOTS], full2[Y2_SLOTS], empty2[Y2_SLOTS];
+  uint64_t cut1[CUTS], clean1[CUTS], cut2[CUTS], clean2[CUTS];  // copies that a mask cuts, and their cleaning
+  uint64_t t1, t2, p_there, ds_there, done;
   uint32_t tmem;
   int dead, seq, block, found;
-  alignas(16) float2 stats[2][YT];
+  alignas(16) float2 stats[2][YC];
 };
 
 // what a CTA walks over: tiles first..last - 1 of `heads` heads in turn
@@ -140,17 +191,11 @@ struct Walk {
   __device__ __forceinline__ bool cut(int t) const { return t < low || t >= high; }
 };
 
-template <typename T>
-__device__ __forceinline__ float2 pair_values(uint32_t w) {
-  if constexpr (std::is_same<T, __nv_bfloat16>::value) return make_float2(__uint_as_float(w << 16), __uint_as_float(w & 0xFFFF0000u));
-  return __half22float2(*reinterpret_cast<const __half2*>(&w));
-}
-
 template <typename T, int DT, bool KEYS>
 __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw_smem, uint32_t base, int head, uint32_t tmem) {
-  constexpr int BLOCKS = DT / 64, X = kX<DT>, Y = kY<DT>, X_BLOCK = XT * 128, Y_BLOCK = YT * 128;
+  constexpr int BLOCKS = DT / 64, TILE = kGradTile<DT>, BLOCK = 128 * 128;
   const int warp = threadIdx.x >> 5;
-  const uint32_t ring = base + 2 * X;
+  const uint32_t ring1 = base + 2 * TILE, ring2 = ring1 + Y1_SLOTS * TILE;
   volatile int* const dead = &sh.dead;
   int q_first, q_count, k_first, k_count;
   rows_of(p.cu_q, p.q_rows, sh.seq, &q_first, &q_count);
@@ -179,111 +224,138 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
     if (warp == 8) {
       if (elected() && all) {
-        if (KEYS) {
-          mbar_arrive_expect(smem_u32(&sh.x_full), 2 * X);
-          for (int i = 0; i < 2; ++i)
-            for (int x = 0; x < BLOCKS; ++x)
-              for (int r = 0; r < 2; ++r)
-                tile_load(base + i * X + x * X_BLOCK + r * Y_BLOCK, i ? &p.v : &p.k, x * 64, head, x_first + x0 + r * YT, smem_u32(&sh.x_full));
-        }
-        int cuts = 0;
+        const auto load = [&](uint32_t dst, const CUtensorMap* map, int h, int row, uint32_t bar) {
+          mbar_arrive_expect(bar, TILE);
+#pragma unroll
+          for (int x = 0; x < BLOCKS; ++x) tile_load(dst + x * BLOCK, map, x * 64, h, row, bar);
+        };
+        mbar_arrive_expect(smem_u32(&sh.x_full), 2 * TILE);
+        for (int i = 0; i < 2; ++i)
+          for (int x = 0; x < BLOCKS; ++x)
+            tile_load(base + i * TILE + x * BLOCK, KEYS ? (i ? &p.v : &p.k) : (i ? &p.g : &p.q), x * 64, head, x_first + x0, smem_u32(&sh.x_full));
+        int cuts = 0, h = 0, t = walk.first;
         for (int n = 0; n < all; ++n) {
-          const int stage = n % GRAD_STAGES, h = n / tiles, t = walk.first + n - h * tiles;
-          if (!mbar_wait(smem_u32(&sh.empty[stage]), ((n / GRAD_STAGES) & 1) ^ 1, dead)) break;
+          const int slot1 = n % Y1_SLOTS, slot2 = n % Y2_SLOTS, y_head = KEYS ? head * p.group + h : head / p.group, row = y_first + t * YT;
+          // (of a cut tile, those who want it wait for its own barriers; the slot's phases count copies.  Fewer tiles than there are cut barriers
+          // are under way, so the last use of each is over)
           const bool cut = walk.cut(t);
-          // (at most four tiles are under way, so the fourth cut tile before this one is done with)
-          const uint32_t bar = smem_u32(cut ? &sh.cut_full[cuts % 4] : &sh.full[stage]), dst = ring + stage * 2 * Y;
-          if (cut) {
-            mbar_arrive(smem_u32(&sh.full[stage]));
-            ++cuts;
+          if (!mbar_wait(smem_u32(&sh.empty1[slot1]), ((n / Y1_SLOTS) & 1) ^ 1, dead)) break;
+          if (cut) mbar_arrive(smem_u32(&sh.full1[slot1]));
+          load(ring1 + slot1 * TILE, KEYS ? &p.q : &p.k, y_head, row, smem_u32(cut ? &sh.cut1[cuts % CUTS] : &sh.full1[slot1]));
+          if (!mbar_wait(smem_u32(&sh.empty2[slot2]), ((n / Y2_SLOTS) & 1) ^ 1, dead)) break;
+          const bool cut2 = KEYS && cut;
+          if (cut2) mbar_arrive(smem_u32(&sh.full2[slot2]));
+          load(ring2 + slot2 * TILE, KEYS ? &p.g : &p.v, y_head, row, smem_u32(cut2 ? &sh.cut2[cuts % CUTS] : &sh.full2[slot2]));
+          cuts += cut;
+          if (++t == walk.last) {
+            t = walk.first;
+            ++h;
           }
-          mbar_arrive_expect(bar, 2 * Y);
-          const int y_head = KEYS ? head * p.group + h : head / p.group;
-          for (int i = 0; i < 2; ++i)
-            for (int x = 0; x < BLOCKS; ++x)
-              tile_load(dst + i * Y + x * Y_BLOCK, KEYS ? (i ? &p.g : &p.q) : (i ? &p.v : &p.k), x * 64, y_head, y_first + t * YT, bar);
         }
       }
     } else if (warp == 9) {
       if (elected()) {
         const int steps = (p.dim + 15) / 16;
         const uint32_t kind_t = tile_kind(p.bf, YT, false), kind_a = tile_kind(p.bf, steps * 16, true);
-        const uint64_t rows = tile_operand(0, 16, 1024), lines = tile_operand(0, Y_BLOCK, 1024);
-        bool ok = all == 0 || mbar_wait(smem_u32(KEYS ? &sh.x_full : &sh.x_there), 0, dead);
-        tmem_after();
-        int cuts = 0;
-        const auto products = [&](int n) {  // T1 and T2 of tile n
-          const int stage = n % GRAD_STAGES, h = n / tiles, t = walk.first + n - h * tiles;
-          if (walk.cut(t)) {
-            ok = ok && mbar_wait(smem_u32(&sh.clean[cuts % 4]), (cuts / 4) & 1, dead);
-            ++cuts;
-          } else {
-            ok = ok && mbar_wait(smem_u32(&sh.full[stage]), (n / GRAD_STAGES) & 1, dead);
+        const uint64_t rows = tile_operand(0, 16, 1024), lines = tile_operand(0, BLOCK, 1024);
+        bool ok = all == 0 || mbar_wait(smem_u32(&sh.x_full), 0, dead);
+        int cuts1 = 0, cuts2 = 0, t1 = walk.first, t2 = walk.first;  // of the next tile whose T1, T2 is formed
+        const auto product = [&](uint32_t d, uint32_t x, uint32_t y, uint64_t& bar) {
+          const uint64_t a = rows + (x >> 4), b = rows + (y >> 4);
+#pragma unroll
+          for (int s = 0; s < DT / 16; ++s) {
+            if (s >= steps) break;
+            const int at = ((s >> 2) * BLOCK + (s & 3) * 32) >> 4;
+            mma_shared(d, a + at, b + at, kind_t, s != 0);
           }
-          if (!ok) return;
-          for (int i = 0; i < 2; ++i) {
-            const uint64_t a = rows + ((base + i * X) >> 4), b = rows + ((ring + (stage * 2 + i) * Y) >> 4);
-            for (int s = 0; s < steps; ++s) {
-              const uint32_t d = tmem + i * 128 + (n & 1) * YT;
-              const uint64_t y = b + (((s >> 2) * Y_BLOCK + (s & 3) * 32) >> 4);
-              if (KEYS) mma_shared(d, a + (((s >> 2) * X_BLOCK + (s & 3) * 32) >> 4), y, kind_t, s != 0);
-              else mma_tensor(d, tmem + 384 + i * 64 + s * 8, y, kind_t, s != 0);
-            }
-          }
-          mma_arrive(smem_u32(&sh.products[n & 1]));
+          mma_arrive(smem_u32(&bar));
         };
-        for (int n = 0; n < 2 && n < all; ++n) products(n);
+        const auto form1 = [&](int n) {
+          if (walk.cut(t1)) {
+            ok = ok && mbar_wait(smem_u32(&sh.clean1[cuts1 % CUTS]), (cuts1 / CUTS) & 1, dead);
+            ++cuts1;
+          } else {
+            ok = ok && mbar_wait(smem_u32(&sh.full1[n % Y1_SLOTS]), (n / Y1_SLOTS) & 1, dead);
+          }
+          if (++t1 == walk.last) t1 = walk.first;
+          if (ok) product(tmem, base, ring1 + (n % Y1_SLOTS) * TILE, sh.t1);
+        };
+        const auto form2 = [&](int n) {
+          if (KEYS && walk.cut(t2)) {
+            ok = ok && mbar_wait(smem_u32(&sh.clean2[cuts2 % CUTS]), (cuts2 / CUTS) & 1, dead);
+            ++cuts2;
+          } else {
+            ok = ok && mbar_wait(smem_u32(&sh.full2[n % Y2_SLOTS]), (n / Y2_SLOTS) & 1, dead);
+          }
+          if (++t2 == walk.last) t2 = walk.first;
+          if (!ok) return;
+          product(tmem + 128, base + TILE, ring2 + (n % Y2_SLOTS) * TILE, sh.t2);
+          if (!KEYS) mma_arrive(smem_u32(&sh.empty2[n % Y2_SLOTS]));
+        };
+        const auto add = [&](uint32_t acc, uint32_t a, uint32_t y, bool more) {  // 64 columns' pairs from each warpgroup
+          const uint64_t b = lines + (y >> 4);
+#pragma unroll
+          for (int s = 0; s < YT / 16; ++s) mma_tensor(acc, a + (s >> 2) * YC + (s & 3) * 8, b + s * (2048 >> 4), kind_a, more || s != 0);
+        };
+        if (all && ok) {
+          form1(0);
+          form2(0);
+        }
         for (int n = 0; n < all && ok; ++n) {
-          ok = mbar_wait(smem_u32(&sh.weights[n & 1]), (n >> 1) & 1, dead);
+          ok = mbar_wait(smem_u32(&sh.p_there), n & 1, dead);
           if (!ok) break;
           tmem_after();
-          const int stage = n % GRAD_STAGES;
-          const uint64_t y1 = lines + ((ring + stage * 2 * Y) >> 4);
-          for (int s = 0; s < 2 * YT / 16; ++s)  // both pieces of ds
-            mma_tensor(tmem + 256, tmem + 128 + (n & 1) * YT + s * 8, y1 + (s % (YT / 16)) * (2048 >> 4), kind_a, n != 0 || s != 0);
           if (KEYS) {
-            const uint64_t y2 = y1 + (Y >> 4);
-            for (int s = 0; s < YT / 16; ++s) mma_tensor(tmem + 384, tmem + (n & 1) * YT + s * 8, y2 + s * (2048 >> 4), kind_a, n != 0 || s != 0);
+            add(tmem + 384, tmem, ring2 + (n % Y2_SLOTS) * TILE, n != 0);
+            mma_arrive(smem_u32(&sh.empty2[n % Y2_SLOTS]));
           }
-          mma_arrive(smem_u32(&sh.empty[stage]));
-          if (n + 2 < all) products(n + 2);
+          if (n + 1 < all) form1(n + 1);
+          ok = ok && mbar_wait(smem_u32(&sh.ds_there), n & 1, dead);
+          if (!ok) break;
+          tmem_after();
+          add(tmem + 256, tmem + 128, ring1 + (n % Y1_SLOTS) * TILE, n != 0);
+          mma_arrive(smem_u32(&sh.empty1[n % Y1_SLOTS]));
+          if (n + 1 < all) form2(n + 1);
         }
         mma_arrive(smem_u32(&sh.done));
       }
     } else {
-      // Cut tiles: a thread a row.  Rows behind the sequence become 0 where they are summed over (0 times a neighbour's infinity would be
+      // Cut tiles, Y1 one warp, Y2 the other.  Rows behind the sequence become 0 where they are summed over (0 times a neighbour's infinity would be
       // NaN), and so do values of Y1 that are not finite: rows that see them have an lse that is NaN.
-      const int row = threadIdx.x - 10 * 32;
-      int cuts = 0;
-      for (int n = 0; n < all; ++n) {
-        const int stage = n % GRAD_STAGES, h = n / tiles, t = walk.first + n - h * tiles;
-        if (!walk.cut(t)) continue;
-        if (!mbar_wait(smem_u32(&sh.cut_full[cuts % 4]), (cuts / 4) & 1, dead)) break;
-        uint8_t* const tile = raw_smem + (ring - smem_u32(raw_smem)) + stage * 2 * Y;
-        const bool behind = t * YT + row >= y_count;
-        for (int x = 0; x < BLOCKS; ++x) {
+      const bool second = warp == 11;
+      int cuts = 0, t = walk.first;
+      for (int n = 0; n < all && (KEYS || !second); ++n) {
+        const int at_t = t;
+        if (++t == walk.last) t = walk.first;
+        if (!walk.cut(at_t)) continue;
+        if (!mbar_wait(smem_u32(second ? &sh.cut2[cuts % CUTS] : &sh.cut1[cuts % CUTS]), (cuts / CUTS) & 1, dead)) break;
+        uint8_t* const tile = raw_smem + ((second ? ring2 + (n % Y2_SLOTS) * TILE : ring1 + (n % Y1_SLOTS) * TILE) - smem_u32(raw_smem));
+        for (int row = threadIdx.x & 31; row < YT; row += 32) {
+          const bool behind = at_t * YT + row >= y_count;
+          if (!behind && (second || !p.causal)) continue;
+          for (int x = 0; x < BLOCKS; ++x) {
 #pragma unroll
-          for (int piece = 0; piece < 8; ++piece) {
-            uint4* const at = reinterpret_cast<uint4*>(tile + x * Y_BLOCK + swizzled(row, piece));
-            if (behind) {
-              *at = make_uint4(0u, 0u, 0u, 0u);
-              if (KEYS) *reinterpret_cast<uint4*>(reinterpret_cast<uint8_t*>(at) + Y) = make_uint4(0u, 0u, 0u, 0u);
-            } else if (p.causal) {
-              uint4 v = *at;
-              uint32_t* const u = &v.x;
-              constexpr uint32_t EXP = std::is_same<T, __nv_bfloat16>::value ? 0x7F80u : 0x7C00u;
-              bool here = false;
+            for (int piece = 0; piece < 8; ++piece) {
+              uint4* const at = reinterpret_cast<uint4*>(tile + x * BLOCK + swizzled(row, piece));
+              if (behind) {
+                *at = make_uint4(0u, 0u, 0u, 0u);
+              } else {
+                uint4 v = *at;
+                uint32_t* const u = &v.x;
+                constexpr uint32_t EXP = std::is_same<T, __nv_bfloat16>::value ? 0x7F80u : 0x7C00u;
+                bool here = false;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                if ((u[e] & EXP) == EXP) u[e] &= 0xFFFF0000u, here = true;
-                if ((u[e] & (EXP << 16)) == EXP << 16) u[e] &= 0x0000FFFFu, here = true;
+                for (int e = 0; e < 4; ++e) {
+                  if ((u[e] & EXP) == EXP) u[e] &= 0xFFFF0000u, here = true;
+                  if ((u[e] & (EXP << 16)) == EXP << 16) u[e] &= 0x0000FFFFu, here = true;
+                }
+                if (here) *at = v;
               }
-              if (here) *at = v;
             }
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        mbar_arrive(smem_u32(&sh.clean[cuts % 4]));
+        mbar_arrive(smem_u32(second ? &sh.clean2[cuts % CUTS] : &sh.clean1[cuts % CUTS]));
         ++cuts;
       }
     }
@@ -292,102 +364,109 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
 
   asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
   const int w = warp >> 2, thread = threadIdx.x & 127, x = x0 + thread;  // the thread's row of X
-  const uint32_t lanes = (uint32_t)(warp & 3) << 21, t1 = tmem + w * YT + lanes, t2 = t1 + 128;
+  const uint32_t lanes = (uint32_t)(warp & 3) << 21, t1 = tmem + w * YC + lanes, t2 = t1 + 128;
   const u64 c = both(p.to_log2);
   const int bits = ds_bits(p);
-  const u64 up = both(power_of_two(bits - P_BITS));  // of ds, beside the 2^8 of p
+  const float up = power_of_two(bits - P_BITS);  // of ds, beside the 2^8 of p
+  const u64 up2 = both(up);
   bool ok = true;
   float2 mine = make_float2(0.0f, 0.0f);  // queries: this row's; keys: a column's of the next tile
   const auto stats_of = [&](int n) {
-    const int h = n / max(tiles, 1), i = (walk.first + n - h * tiles) * YT + thread;
+    const int h = n / max(tiles, 1), i = (walk.first + n - h * tiles) * YT + w * YC + thread;
     mine = make_float2(0.0f, 0.0f);
-    if (n < all && thread < YT && i < y_count) mine = __ldg(p.stats + (int64_t)(head * p.group + h) * p.q_rows + y_first + i);
+    if (n < all && thread < YC && i < y_count) mine = __ldg(p.stats + (int64_t)(head * p.group + h) * p.q_rows + y_first + i);
   };
-  if (!KEYS) {  // this warpgroup's operand of all first products: a row a thread, in tensor memory beside the sums
-    const T* const row = w ? static_cast<const T*>(p.g_raw) + ((int64_t)(x_first + x) * p.heads + head) * p.dim
-                           : static_cast<const T*>(p.q_raw) + (int64_t)(x_first + x) * p.q_at.token + head * p.q_at.head;
-    for (int d = 0; d < p.dim; d += 32) {
-      uint32_t v[16];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint4 four = x < x_count && d + 8 * e < p.dim ? __ldg(reinterpret_cast<const uint4*>(row + d + 8 * e)) : make_uint4(0u, 0u, 0u, 0u);
-        v[4 * e] = four.x, v[4 * e + 1] = four.y, v[4 * e + 2] = four.z, v[4 * e + 3] = four.w;
-      }
-      __syncwarp();
-      tmem_st16(tmem + 384 + w * 64 + lanes + d / 2, v);
-    }
-    tmem_wait_st();
-    tmem_before();
-    mbar_arrive(smem_u32(&sh.x_there));
-  }
-  if (KEYS) stats_of(w);
+  if (KEYS) stats_of(0);
   else if (x < x_count) mine = __ldg(p.stats + (int64_t)head * p.q_rows + x_first + x);
-  for (int n = w; n < all; n += 2) {
+  const u64 row_minus = both(P_BITS - mine.x), row_delta = both(-mine.y * up);
+  int t = walk.first;
+  for (int n = 0; n < all; ++n) {
     if (KEYS) {  // the columns' statistics; the warpgroup's own, so the barrier is its own too
       asm volatile("bar.sync %0, 128;" ::"r"(1 + w) : "memory");
-      if (thread < YT) sh.stats[w][thread] = make_float2(mine.x - P_BITS, mine.y);
+      if (thread < YC) sh.stats[w][thread] = make_float2(P_BITS - mine.x, -mine.y * up);
       asm volatile("bar.sync %0, 128;" ::"r"(1 + w) : "memory");
-      stats_of(n + 2);
+      stats_of(n + 1);
     }
-    ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&sh.products[w]), (n >> 1) & 1, dead));
+    const int at_t = t;
+    if (++t == walk.last) t = walk.first;
+    ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&sh.t1), n & 1, dead));
     if (!ok) continue;  // (the warpgroup's other warps wait at its barrier)
     tmem_after();
-    const int t = walk.first + n % tiles;
-    int lo = 0, hi = YT;  // columns that the row goes with
-    if (walk.cut(t)) {
+    int lo = 0, hi = YC;  // of the warpgroup's columns, those that the row goes with
+    const bool cut = walk.cut(at_t);
+    if (cut) {
+      const int first = at_t * YT + w * YC;
       if (KEYS) {
-        hi = y_count - t * YT;
-        if (p.causal) lo = x - off - t * YT;
+        hi = y_count - first;
+        if (p.causal) lo = x - off - first;
       } else {
-        hi = (p.causal ? min(y_count, x + off + 1) : y_count) - t * YT;
+        hi = (p.causal ? min(y_count, x + off + 1) : y_count) - first;
       }
     }
-    const bool masked = walk.cut(t);
-    uint32_t s[YT], dp[YT];
+    uint32_t s[YC];  // scores, then weights
 #pragma unroll
-    for (int half = 0; half < YT; half += 32) {
-      tmem_load32(t1 + half, s + half);
-      tmem_load32(t2 + half, dp + half);
-    }
+    for (int e = 0; e < YC; e += 32) tmem_load32(t1 + e, s + e);
     tmem_wait_ld();
+    const auto weights = [&](auto masked) {  // (a test per element, even of a value that is the same for all, doubled the instructions)
 #pragma unroll
-    for (int half = 0; half < YT; half += 32) {
-      uint32_t pw[16], dw[16], low[16];
+      for (int half = 0; half < YC; half += 32) {
+        uint32_t pw[16];
 #pragma unroll
-      for (int e = half; e < half + 32; e += 2) {
-        u64 minus, delta;
-        if (KEYS) {
-          const float4 st = *reinterpret_cast<const float4*>(&sh.stats[w][e]);
-          minus = pack2(-st.x, -st.z);
-          delta = pack2(-st.y, -st.w);
-        } else {
-          minus = both(P_BITS - mine.x);
-          delta = both(-mine.y);
+        for (int e = half; e < half + 32; e += 2) {
+          u64 minus = row_minus;
+          if (KEYS) minus = pack2(sh.stats[w][e].x, sh.stats[w][e + 1].x);
+          float p0, p1;
+          unpack2(fma2_rn(pack2u(s[e], s[e + 1]), c, minus), p0, p1);
+          p0 = exp2_approx(p0);
+          p1 = exp2_approx(p1);
+          if constexpr (decltype(masked)::value) {
+            if (e < lo || e >= hi) p0 = 0.0f;
+            if (e + 1 < lo || e + 1 >= hi) p1 = 0.0f;
+          }
+          s[e] = __float_as_uint(p0);
+          s[e + 1] = __float_as_uint(p1);
+          if (KEYS) pw[(e - half) / 2] = pack_pair<T>(p0, p1);
         }
-        float p0, p1;
-        unpack2(fma2_rn(pack2u(s[e], s[e + 1]), c, minus), p0, p1);
-        p0 = exp2_approx(p0);
-        p1 = exp2_approx(p1);
-        float d0, d1;
-        unpack2(mul2_rn(mul2_rn(add2_rn(pack2u(dp[e], dp[e + 1]), delta), up), pack2(p0, p1)), d0, d1);
-        if (masked) {
-          if (e < lo || e >= hi) p0 = d0 = 0.0f;
-          if (e + 1 < lo || e + 1 >= hi) p1 = d1 = 0.0f;
-        }
-        const int at = (e - half) / 2;
-        if (KEYS) pw[at] = pack_pair<T>(p0, p1);
-        dw[at] = pack_pair<T>(d0, d1);
-        const float2 held = pair_values<T>(dw[at]);
-        low[at] = pack_pair<T>(d0 - held.x, d1 - held.y);
+        if (KEYS) tmem_st16(t1 + half / 2, pw);  // over columns that have been read
       }
-      // over columns that have been read: p's 32, ds' first pieces' 32 and second pieces' 32
-      if (KEYS) tmem_st16(t1 + half / 2, pw);
-      tmem_st16(t2 + half / 2, dw);
-      tmem_st16(t2 + YT / 2 + half / 2, low);
-    }
+    };
+    if (cut) weights(std::true_type());
+    else weights(std::false_type());
+    if (KEYS) tmem_wait_st();
+    tmem_before();
+    mbar_arrive(smem_u32(&sh.p_there));
+
+    ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&sh.t2), n & 1, dead));
+    if (!ok) continue;
+    tmem_after();
+    uint32_t dp[YC];
+#pragma unroll
+    for (int e = 0; e < YC; e += 32) tmem_load32(t2 + e, dp + e);
+    tmem_wait_ld();
+    const auto slopes = [&](auto masked) {
+#pragma unroll
+      for (int half = 0; half < YC; half += 32) {
+        uint32_t dw[16];
+#pragma unroll
+        for (int e = half; e < half + 32; e += 2) {
+          u64 delta = row_delta;
+          if (KEYS) delta = pack2(sh.stats[w][e].y, sh.stats[w][e + 1].y);
+          float d0, d1;
+          unpack2(mul2_rn(fma2_rn(pack2u(dp[e], dp[e + 1]), up2, delta), pack2u(s[e], s[e + 1])), d0, d1);
+          if constexpr (decltype(masked)::value) {  // (0 times what a mask hides may be NaN)
+            if (e < lo || e >= hi) d0 = 0.0f;
+            if (e + 1 < lo || e + 1 >= hi) d1 = 0.0f;
+          }
+          dw[(e - half) / 2] = pack_pair<T>(d0, d1);
+        }
+        tmem_st16(t2 + half / 2, dw);
+      }
+    };
+    if (cut) slopes(std::true_type());
+    else slopes(std::false_type());
     tmem_wait_st();
     tmem_before();
-    mbar_arrive(smem_u32(&sh.weights[w]));
+    mbar_arrive(smem_u32(&sh.ds_there));
   }
   // both warpgroups bring the sums out, each half of the columns
   ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&sh.done), 0, dead)) && ok && !*dead;
@@ -434,20 +513,25 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) attention_grad_kernel(const _
   const uint32_t base = (smem_u32(raw_smem) + 1023) & ~1023u;
   if (threadIdx.x == 0) {
     mbar_init(smem_u32(&sh.x_full), 1);
-    mbar_init(smem_u32(&sh.x_there), 256);
     mbar_init(smem_u32(&sh.done), 1);
-    for (int i = 0; i < GRAD_STAGES; ++i) {
-      mbar_init(smem_u32(&sh.full[i]), 1);
-      mbar_init(smem_u32(&sh.empty[i]), 1);
+    for (int i = 0; i < Y1_SLOTS; ++i) {
+      mbar_init(smem_u32(&sh.full1[i]), 1);
+      mbar_init(smem_u32(&sh.empty1[i]), 1);
     }
-    for (int i = 0; i < 4; ++i) {
-      mbar_init(smem_u32(&sh.cut_full[i]), 1);
-      mbar_init(smem_u32(&sh.clean[i]), 64);
+    for (int i = 0; i < Y2_SLOTS; ++i) {
+      mbar_init(smem_u32(&sh.full2[i]), 1);
+      mbar_init(smem_u32(&sh.empty2[i]), 1);
     }
-    for (int i = 0; i < 2; ++i) {
-      mbar_init(smem_u32(&sh.products[i]), 1);
-      mbar_init(smem_u32(&sh.weights[i]), 128);
+    for (int i = 0; i < CUTS; ++i) {
+      mbar_init(smem_u32(&sh.cut1[i]), 1);
+      mbar_init(smem_u32(&sh.cut2[i]), 1);
+      mbar_init(smem_u32(&sh.clean1[i]), 32);
+      mbar_init(smem_u32(&sh.clean2[i]), 32);
     }
+    mbar_init(smem_u32(&sh.t1), 1);
+    mbar_init(smem_u32(&sh.t2), 1);
+    mbar_init(smem_u32(&sh.p_there), 256);
+    mbar_init(smem_u32(&sh.ds_there), 256);
     mbar_init_fence();
     sh.dead = 0;
   }
@@ -522,9 +606,6 @@ int lba_attention_backward(const void* grad_out, const void* q, const void* k, c
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255) || workspace_bytes < lba_attention_backward_workspace_bytes(how)) return LBA_ERR_WORKSPACE;
   GradParams p;
   p.bf = how->type == LBA_TYPE_BF16;
-  p.q_raw = q;
-  p.g_raw = grad_out;
-  p.q_at = how->q_at;
   const lba_strides g_at = {(int64_t)how->heads * how->dim, how->dim};
   if (!head_map(&p.q, p.bf, q, how->q_rows, how->heads, how->dim, how->q_at, YT) || !head_map(&p.g, p.bf, grad_out, how->q_rows, how->heads, how->dim, g_at, YT) ||
       !head_map(&p.k, p.bf, k, how->k_rows, how->kv_heads, how->dim, how->k_at, YT) ||
@@ -535,8 +616,14 @@ int lba_attention_backward(const void* grad_out, const void* q, const void* k, c
   DeltaParams d = {};
   d.g = grad_out;
   d.out = out;
+  d.q = q;
+  d.k = k;
   d.v = v;
+  d.q_at = how->q_at;
+  d.k_at = how->k_at;
   d.v_at = how->v_at;
+  d.causal = how->causal != 0;
+  d.to_log2 = how->scale * LOG2E;
   d.lse = lse;
   d.cu_q = p.cu_q = how->cu_q;
   d.cu_k = p.cu_k = how->cu_k;
