@@ -8,12 +8,14 @@
 // the group), and walks over 128 rows of the others at a time:
 //   T1 = X1 Y1^T (scores), T2 = X2 Y2^T (dp)       X: q, g or k, v: shared memory for the whole CTA; Y: the other two, from two rings
 //   p from T1, then ds from T2                     two warpgroups, 64 columns each, a row a thread
-//   acc1 += ds Y1, and for keys acc2 += p Y2       p and ds lie in tensor memory over T1 and T2, sums in 128 more columns each
+//   acc1 += ds Y1, and for keys acc2 += p Y2       p and ds lie in tensor memory over T2, sums in 128 more columns each
 // Scores and dp are so formed twice, seven products where five would do; in return every sum is formed by one CTA in a fixed order, and no
 // 32-bit gradient of q goes through memory or atomics.
 //
-// Bound by the matrix instructions, 512 clocks each.  They follow one another without a pause: for keys acc2(n), T1(n+1), acc1(n), T2(n+1), so that
-// p of tile n+1 is formed while acc1(n) and T2(n+1) run, and ds of tile n while acc2(n) and T1(n+1) do; for queries T1(n+1), acc1(n), T2(n+1).
+// Bound by the matrix instructions, 512 clocks each (four for keys, three for queries), and by the 1024 clocks of exponentials and what goes
+// with them.  p waits in registers until T2 has been read: so T1(n+1) is formed as soon as T1(n) is in registers, and scores are there before the
+// warpgroups want them; acc1(n), acc2(n) and T2(n+1) follow while they form p of tile n+1.  (With p over T1, T1(n+1) came after acc2(n): 3500
+// clocks a tile.  With p in shared memory there is room for two tiles of Y1 only, and their copies came late: 4200.)
 // (Tiles of 64 rows, two of them in flight, a warpgroup each: with 64 columns a product wants 192 bytes of shared memory a clock, or 128 of
 // tensor memory, and took 57 clocks a step instead of 32; 2 x 4096 tokens of 16 heads took 515 us.)
 //
@@ -177,10 +179,10 @@ template <int DT> constexpr size_t kGradSmem = 1024 + (size_t)kGradTile<DT> * (2
 struct GradShared {
   uint64_t x_full, full1[Y1_SLOTS], empty1[Y1_SLOTS], full2[Y2_SLOTS], empty2[Y2_SLOTS];
   uint64_t cut1[CUTS], clean1[CUTS], cut2[CUTS], clean2[CUTS];  // copies that a mask cuts, and their cleaning
-  uint64_t t1, t2, p_there, ds_there, done;
+  uint64_t t1, t1_read, t2, ds_there, done;
   uint32_t tmem;
   int dead, seq, block, found;
-  alignas(16) float2 stats[2][YC];
+  alignas(16) float minus[2][YC], delta[2][YC];
 };
 
 // what a CTA walks over: tiles first..last - 1 of `heads` heads in turn
@@ -292,29 +294,31 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
           product(tmem + 128, base + TILE, ring2 + (n % Y2_SLOTS) * TILE, sh.t2);
           if (!KEYS) mma_arrive(smem_u32(&sh.empty2[n % Y2_SLOTS]));
         };
-        const auto add = [&](uint32_t acc, uint32_t a, uint32_t y, bool more) {  // 64 columns' pairs from each warpgroup
-          const uint64_t b = lines + (y >> 4);
-#pragma unroll
-          for (int s = 0; s < YT / 16; ++s) mma_tensor(acc, a + (s >> 2) * YC + (s & 3) * 8, b + s * (2048 >> 4), kind_a, more || s != 0);
-        };
         if (all && ok) {
           form1(0);
           form2(0);
         }
         for (int n = 0; n < all && ok; ++n) {
-          ok = mbar_wait(smem_u32(&sh.p_there), n & 1, dead);
-          if (!ok) break;
-          tmem_after();
-          if (KEYS) {
-            add(tmem + 384, tmem, ring2 + (n % Y2_SLOTS) * TILE, n != 0);
-            mma_arrive(smem_u32(&sh.empty2[n % Y2_SLOTS]));
+          if (n + 1 < all) {
+            ok = mbar_wait(smem_u32(&sh.t1_read), n & 1, dead);
+            tmem_after();
+            form1(n + 1);
           }
-          if (n + 1 < all) form1(n + 1);
           ok = ok && mbar_wait(smem_u32(&sh.ds_there), n & 1, dead);
           if (!ok) break;
           tmem_after();
-          add(tmem + 256, tmem + 128, ring1 + (n % Y1_SLOTS) * TILE, n != 0);
+          // in T2, of each warpgroup's 64 columns: the pairs of ds, then those of p
+          const auto add = [&](uint32_t acc, uint32_t a, uint32_t y) {
+            const uint64_t b = lines + (y >> 4);
+#pragma unroll
+            for (int s = 0; s < YT / 16; ++s) mma_tensor(acc, a + (s >> 2) * YC + (s & 3) * 8, b + s * (2048 >> 4), kind_a, n != 0 || s != 0);
+          };
+          add(tmem + 256, tmem + 128, ring1 + (n % Y1_SLOTS) * TILE);
           mma_arrive(smem_u32(&sh.empty1[n % Y1_SLOTS]));
+          if (KEYS) {
+            add(tmem + 384, tmem + 128 + YC / 2, ring2 + (n % Y2_SLOTS) * TILE);
+            mma_arrive(smem_u32(&sh.empty2[n % Y2_SLOTS]));
+          }
           if (n + 1 < all) form2(n + 1);
         }
         mma_arrive(smem_u32(&sh.done));
@@ -383,7 +387,10 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
   for (int n = 0; n < all; ++n) {
     if (KEYS) {  // the columns' statistics; the warpgroup's own, so the barrier is its own too
       asm volatile("bar.sync %0, 128;" ::"r"(1 + w) : "memory");
-      if (thread < YC) sh.stats[w][thread] = make_float2(P_BITS - mine.x, -mine.y * up);
+      if (thread < YC) {
+        sh.minus[w][thread] = P_BITS - mine.x;
+        sh.delta[w][thread] = -mine.y * up;
+      }
       asm volatile("bar.sync %0, 128;" ::"r"(1 + w) : "memory");
       stats_of(n + 1);
     }
@@ -407,35 +414,31 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
 #pragma unroll
     for (int e = 0; e < YC; e += 32) tmem_load32(t1 + e, s + e);
     tmem_wait_ld();
+    tmem_before();
+    mbar_arrive(smem_u32(&sh.t1_read));
+    uint32_t pw[KEYS ? YC / 2 : 1];
     const auto weights = [&](auto masked) {  // (a test per element, even of a value that is the same for all, doubled the instructions)
 #pragma unroll
-      for (int half = 0; half < YC; half += 32) {
-        uint32_t pw[16];
+      for (int e = 0; e < YC; e += 4) {
+        const float4 m = KEYS ? *reinterpret_cast<const float4*>(&sh.minus[w][e]) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
-        for (int e = half; e < half + 32; e += 2) {
-          u64 minus = row_minus;
-          if (KEYS) minus = pack2(sh.stats[w][e].x, sh.stats[w][e + 1].x);
+        for (int f = 0; f < 4; f += 2) {
           float p0, p1;
-          unpack2(fma2_rn(pack2u(s[e], s[e + 1]), c, minus), p0, p1);
+          unpack2(fma2_rn(pack2u(s[e + f], s[e + f + 1]), c, KEYS ? (f ? pack2(m.z, m.w) : pack2(m.x, m.y)) : row_minus), p0, p1);
           p0 = exp2_approx(p0);
           p1 = exp2_approx(p1);
           if constexpr (decltype(masked)::value) {
-            if (e < lo || e >= hi) p0 = 0.0f;
-            if (e + 1 < lo || e + 1 >= hi) p1 = 0.0f;
+            if (e + f < lo || e + f >= hi) p0 = 0.0f;
+            if (e + f + 1 < lo || e + f + 1 >= hi) p1 = 0.0f;
           }
-          s[e] = __float_as_uint(p0);
-          s[e + 1] = __float_as_uint(p1);
-          if (KEYS) pw[(e - half) / 2] = pack_pair<T>(p0, p1);
+          s[e + f] = __float_as_uint(p0);
+          s[e + f + 1] = __float_as_uint(p1);
+          if (KEYS) pw[(e + f) / 2] = pack_pair<T>(p0, p1);
         }
-        if (KEYS) tmem_st16(t1 + half / 2, pw);  // over columns that have been read
       }
     };
     if (cut) weights(std::true_type());
     else weights(std::false_type());
-    if (KEYS) tmem_wait_st();
-    tmem_before();
-    mbar_arrive(smem_u32(&sh.p_there));
-
     ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&sh.t2), n & 1, dead));
     if (!ok) continue;
     tmem_after();
@@ -448,22 +451,26 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
       for (int half = 0; half < YC; half += 32) {
         uint32_t dw[16];
 #pragma unroll
-        for (int e = half; e < half + 32; e += 2) {
-          u64 delta = row_delta;
-          if (KEYS) delta = pack2(sh.stats[w][e].y, sh.stats[w][e + 1].y);
-          float d0, d1;
-          unpack2(mul2_rn(fma2_rn(pack2u(dp[e], dp[e + 1]), up2, delta), pack2u(s[e], s[e + 1])), d0, d1);
-          if constexpr (decltype(masked)::value) {  // (0 times what a mask hides may be NaN)
-            if (e < lo || e >= hi) d0 = 0.0f;
-            if (e + 1 < lo || e + 1 >= hi) d1 = 0.0f;
+        for (int e = half; e < half + 32; e += 4) {
+          const float4 m = KEYS ? *reinterpret_cast<const float4*>(&sh.delta[w][e]) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+          for (int f = 0; f < 4; f += 2) {
+            float d0, d1;
+            unpack2(mul2_rn(fma2_rn(pack2u(dp[e + f], dp[e + f + 1]), up2, KEYS ? (f ? pack2(m.z, m.w) : pack2(m.x, m.y)) : row_delta),
+                            pack2u(s[e + f], s[e + f + 1])), d0, d1);
+            if constexpr (decltype(masked)::value) {  // (0 times what a mask hides may be NaN)
+              if (e + f < lo || e + f >= hi) d0 = 0.0f;
+              if (e + f + 1 < lo || e + f + 1 >= hi) d1 = 0.0f;
+            }
+            dw[(e + f - half) / 2] = pack_pair<T>(d0, d1);
           }
-          dw[(e - half) / 2] = pack_pair<T>(d0, d1);
         }
         tmem_st16(t2 + half / 2, dw);
       }
     };
     if (cut) slopes(std::true_type());
     else slopes(std::false_type());
+    if constexpr (KEYS) tmem_store32(t2 + YC / 2, pw);
     tmem_wait_st();
     tmem_before();
     mbar_arrive(smem_u32(&sh.ds_there));
@@ -530,7 +537,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) attention_grad_kernel(const _
     }
     mbar_init(smem_u32(&sh.t1), 1);
     mbar_init(smem_u32(&sh.t2), 1);
-    mbar_init(smem_u32(&sh.p_there), 256);
+    mbar_init(smem_u32(&sh.t1_read), 256);
     mbar_init(smem_u32(&sh.ds_there), 256);
     mbar_init_fence();
     sh.dead = 0;
