@@ -46,7 +46,7 @@ struct ForwardShared {
   uint32_t cut[CUT_TILES][4];  // rows of the masked tiles of V that hold values that are not finite
   uint32_t tmem;
   int dead;
-  int seq, block, found;
+  Place place;
 };
 
 // weights of 32 scores, relative to the maximum: packed, and their sum
@@ -72,6 +72,12 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
   const uint32_t base = (smem_u32(raw_smem) + 1023) & ~1023u, q_smem = base, ring = base + 2 * TILE;
   volatile int* const dead = &sh.dead;
 
+  const int head = blockIdx.x % p.heads;
+  if (warp == 8 && lane == 0) {
+    map_ahead(&p.q);
+    map_ahead(&p.k);
+    map_ahead(&p.v);
+  }
   if (warp == 0) {
     if (lane == 0) {
       for (int i = 0; i < 2; ++i) {
@@ -95,28 +101,19 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
   }
   after_previous();
   if (warp == 9) tmem_alloc(smem_u32(&sh.tmem), 512);  // (not before: a CTA of the kernel before this one could still want it)
-  const int head = blockIdx.x % p.heads;
   if (warp == 8) {
-    int seq = 0, block = 0;
-    const bool found = find_block(p.cu_q, p.q_rows, p.sequences, 2 * QT, blockIdx.x / p.heads, &seq, &block);
-    if (lane == 0) {
-      sh.found = found;
-      sh.seq = seq;
-      sh.block = block;
-    }
+    const Place place = find_place(p.cu_q, p.q_rows, p.cu_k, p.k_rows, p.sequences, false, 2 * QT, blockIdx.x / p.heads);
+    if (lane == 0) sh.place = place;
   }
   tmem_before();
   __syncthreads();
   tmem_after();
   const uint32_t tmem = sh.tmem;
-  bool alive = sh.found != 0;
+  const Place place = sh.place;
+  const bool alive = place.found != 0;
   if (alive) {
-    int q_first, q_count, k_first, k_count;
-    rows_of(p.cu_q, p.q_rows, sh.seq, &q_first, &q_count);
-    rows_of(p.cu_k, p.k_rows, sh.seq, &k_first, &k_count);
-    const int off = k_count - q_count;
-    // (with a causal mask the last blocks, which have the most keys, come first)
-    const int block = p.causal ? (q_count + 2 * QT - 1) / (2 * QT) - 1 - sh.block : sh.block;
+    // (with a causal mask the last blocks, which have the most keys, are of the highest levels)
+    const int q_first = place.q_first, q_count = place.q_count, k_first = place.k_first, k_count = place.k_count, off = k_count - q_count, block = place.level;
     const int i0 = block * 2 * QT;
     // tiles of keys of either query tile, and the first that a mask cuts
     int tiles[2], whole[2];

@@ -49,7 +49,7 @@ struct DeltaParams {
   lba_strides q_at, k_at, v_at;
   const float* lse;
   const int32_t *cu_q, *cu_k;
-  int64_t q_rows, k_rows;
+  int64_t q_rows, k_rows, row_blocks;
   int sequences, heads, kv_heads, dim, causal;
   float to_log2;
   float2* stats;
@@ -58,106 +58,146 @@ struct DeltaParams {
 };
 
 // ------------------------------------------------------------------ delta
-// A group of 16 lanes takes a row's head.  Rows of no sequence get gradients of 0.
-constexpr int FEW_KEYS = 32;
-__device__ __forceinline__ float sum16(float v, unsigned lanes) {
+// A warp takes eight heads of a row, 16 lanes each, all on their way at once.  Rows of no sequence get gradients of 0.
+constexpr int FEW_KEYS = 32, DELTA_AHEAD = 4;
+template <typename T>
+__device__ __forceinline__ void widen8(const T* src, float (&v)[8]) {  // at a 16-byte boundary
+  const uint4 raw = *reinterpret_cast<const uint4*>(src);
+  const T* const e = reinterpret_cast<const T*>(&raw);
 #pragma unroll
-  for (int x = 8; x > 0; x /= 2) v += __shfl_xor_sync(lanes, v, x);
-  return v;
+  for (int j = 0; j < 8; ++j) v[j] = to_f32(e[j]);
 }
 template <typename T>
-__global__ void __launch_bounds__(DELTA_THREADS) attention_delta_kernel(const DeltaParams p) {
-  after_previous();
-  const int sub = threadIdx.x & 15, d = sub * 8;
-  const int64_t n = p.q_rows * p.heads, m = p.k_rows * p.kv_heads;
-  const int64_t at = (int64_t)blockIdx.x * (DELTA_THREADS / 16) + (threadIdx.x >> 4);
-  uint32_t most_g = 0, most_v = 0;
-  if (at < n) {
-    const int64_t row = at / p.heads;
-    const int head = (int)(at - row * p.heads);
-    const bool inside = !p.cu_q || (row >= p.cu_q[0] && row < p.cu_q[p.sequences]);
-    float sum = 0.0f;
-    if (d < p.dim) {
-      const int64_t i = at * p.dim + d;
-      if (inside) {
-        float g[8], o[8];
-        load_some<T, 8>(p.g, i, 8, g);
-        load_some<T, 8>(p.out, i, 8, o);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          sum = fmaf(g[e], o[e], sum);
-          most_g = max(most_g, __float_as_uint(g[e]) & 0x7FFFFFFFu);
-        }
-      } else {
-        *reinterpret_cast<uint4*>(static_cast<T*>(p.grad_q) + i) = make_uint4(0u, 0u, 0u, 0u);
-      }
-    }
-    const unsigned lanes = 0xFFFFu << (threadIdx.x & 16);
-    sum = sum16(sum, lanes);
-    const float lse = inside ? p.lse[head * p.q_rows + row] : 0.0f;
-    if (inside) {
-      int b = 0;  // the last sequence that begins at or before the row
-      if (p.cu_q) {
-        int hi = p.sequences - 1;
-        while (b < hi) {
-          const int mid = (b + hi + 1) / 2;
-          if (p.cu_q[mid] <= row) b = mid;
-          else hi = mid - 1;
-        }
-      }
-      int q_first, q_count, k_first, k_count;
-      rows_of(p.cu_q, p.q_rows, b, &q_first, &q_count);
-      rows_of(p.cu_k, p.k_rows, b, &k_first, &k_count);
-      const int keys = p.causal ? min(k_count, (int)row - q_first + k_count - q_count + 1) : k_count;
-      if (keys > 0 && keys <= FEW_KEYS) {
-        const int kv = head / (p.heads / p.kv_heads);
-        float q[8], g[8], top = 0.0f;
-        sum = 0.0f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) q[e] = g[e] = 0.0f;
-        if (d < p.dim) {
-          load_some<T, 8>(static_cast<const T*>(p.q) + row * p.q_at.token + head * p.q_at.head, d, 8, q);
-          load_some<T, 8>(p.g, at * p.dim + d, 8, g);
-        }
-        for (int j = 0; j < keys; ++j) {
-          float s = 0.0f, dp = 0.0f, x[8], y[8];
-          if (d < p.dim) {
-            load_some<T, 8>(static_cast<const T*>(p.k) + (int64_t)(k_first + j) * p.k_at.token + kv * p.k_at.head, d, 8, x);
-            load_some<T, 8>(static_cast<const T*>(p.v) + (int64_t)(k_first + j) * p.v_at.token + kv * p.v_at.head, d, 8, y);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-              s = fmaf(q[e], x[e], s);
-              dp = fmaf(g[e], y[e], dp);
-            }
-          }
-          s = sum16(s, lanes);
-          dp = sum16(dp, lanes);
-          const float w = exp2_approx(fmaf(s, p.to_log2, -lse * LOG2E));
-          sum = fmaf(w, dp, sum);
-          top += w;
-        }
-        sum = __fdividef(sum, top);  // (1, but for rounding)
-      }
-    }
-    if (sub == 0) p.stats[head * p.q_rows + row] = make_float2(lse == -INFINITY ? INFINITY : lse * LOG2E, sum);
+__device__ __forceinline__ void load_half8(const T* src, float (&v)[8]) {
+  const uint4 raw = __ldg(reinterpret_cast<const uint4*>(src));
+  widen8(reinterpret_cast<const T*>(&raw), v);
+}
+// The rows of a sequence that see few keys, for one head: sum p dp / sum p.  The keys and values lie in shared memory; a warp a row, a key a lane.
+template <typename T>
+__device__ void delta_of_few(const DeltaParams& p, int b, int h, uint4* shared) {
+  constexpr int PITCH = 128 / 8 + 1;  // pieces of 16 bytes from key to key: lanes' pieces lie in different banks
+  int q_first, q_count, k_first, k_count;
+  rows_of(p.cu_q, p.q_rows, b, &q_first, &q_count);
+  rows_of(p.cu_k, p.k_rows, b, &k_first, &k_count);
+  const int off = k_count - q_count, lane = threadIdx.x & 31, pieces = p.dim / 8;
+  const int first = p.causal ? max(0, -off) : 0, last = p.causal ? min(q_count, FEW_KEYS - off) : k_count <= FEW_KEYS ? q_count : 0;
+  const int most = min(k_count, FEW_KEYS);
+  if (first >= last || most == 0) return;
+  const int kv = h / (p.heads / p.kv_heads);
+  uint4 *const ks = shared, *const vs = shared + FEW_KEYS * PITCH;
+  for (int i = threadIdx.x; i < most * pieces; i += DELTA_THREADS) {
+    const int j = i / pieces, c = i - j * pieces;
+    ks[j * PITCH + c] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(p.k) + (int64_t)(k_first + j) * p.k_at.token + kv * p.k_at.head) + c);
+    vs[j * PITCH + c] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(p.v) + (int64_t)(k_first + j) * p.v_at.token + kv * p.v_at.head) + c);
   }
-  if (at < m && d < p.dim) {
-    const int64_t row = at / p.kv_heads;
-    const bool inside = !p.cu_k || (row >= p.cu_k[0] && row < p.cu_k[p.sequences]);
-    if (!inside) {
-      *reinterpret_cast<uint4*>(static_cast<T*>(p.grad_k) + at * p.dim + d) = make_uint4(0u, 0u, 0u, 0u);
-      *reinterpret_cast<uint4*>(static_cast<T*>(p.grad_v) + at * p.dim + d) = make_uint4(0u, 0u, 0u, 0u);
-    } else if (p.most) {
-      float v[8];
-      load_some<T, 8>(static_cast<const T*>(p.v) + row * p.v_at.token + (at - row * p.kv_heads) * p.v_at.head, d, 8, v);
+  __syncthreads();
+  for (int i = first + (threadIdx.x >> 5); i < last; i += DELTA_THREADS / 32) {
+    const int keys = p.causal ? min(k_count, i + off + 1) : k_count;
+    const int64_t row = q_first + i;
+    const T *const q = static_cast<const T*>(p.q) + row * p.q_at.token + h * p.q_at.head, *const g = static_cast<const T*>(p.g) + (row * p.heads + h) * p.dim;
+    const float lse = p.lse[h * p.q_rows + row];
+    const int mine = min(lane, most - 1) * PITCH;
+    float s = 0.0f, dp = 0.0f;
+#pragma unroll 4
+    for (int c = 0; c < pieces; ++c) {
+      float a[8], x[8];
+      load_half8(q + c * 8, a);
+      widen8(reinterpret_cast<const T*>(ks + mine + c), x);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) most_v = max(most_v, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+      for (int f = 0; f < 8; ++f) s = fmaf(a[f], x[f], s);
+      load_half8(g + c * 8, a);
+      widen8(reinterpret_cast<const T*>(vs + mine + c), x);
+#pragma unroll
+      for (int f = 0; f < 8; ++f) dp = fmaf(a[f], x[f], dp);
+    }
+    float weight = lane < keys ? exp2_approx(fmaf(s, p.to_log2, -lse * LOG2E)) : 0.0f, sum = lane < keys ? weight * dp : 0.0f;
+#pragma unroll
+    for (int x = 16; x > 0; x /= 2) {
+      sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
+      weight += __shfl_xor_sync(0xFFFFFFFFu, weight, x);
+    }
+    if (lane == 0) p.stats[h * p.q_rows + row] = make_float2(lse * LOG2E, __fdividef(sum, weight));  // (weights add up to 1, but for rounding)
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(DELTA_THREADS, 5) attention_delta_kernel(const DeltaParams p) {
+  __shared__ uint4 shared[2 * FEW_KEYS * (128 / 8 + 1)];
+  after_previous();
+  if ((int64_t)blockIdx.x >= p.row_blocks) {
+    const int64_t i = blockIdx.x - p.row_blocks;
+    if (blockIdx.y == 0) delta_of_few<T>(p, (int)(i / p.heads), (int)(i % p.heads), shared);
+    return;
+  }
+  const int lane = threadIdx.x & 31, d = (lane & 15) * 8;
+  const int64_t row = (int64_t)blockIdx.x * (DELTA_THREADS / 32) + (threadIdx.x >> 5);
+  uint32_t most_g = 0, most_v = 0;
+  const T* const g_row = static_cast<const T*>(p.g) + row * p.heads * p.dim;
+  if (row < p.q_rows && p.cu_q && (row < p.cu_q[0] || row >= p.cu_q[p.sequences])) {
+    for (int i = (blockIdx.y * 32 + lane) * 8; i < p.heads * p.dim; i += gridDim.y * 256) *reinterpret_cast<uint4*>(static_cast<T*>(p.grad_q) + row * p.heads * p.dim + i) = make_uint4(0u, 0u, 0u, 0u);
+  } else if (row < p.q_rows) {
+    const T* const o_row = static_cast<const T*>(p.out) + row * p.heads * p.dim;
+    uint4 g[DELTA_AHEAD], o[DELTA_AHEAD];
+    float lse[DELTA_AHEAD];
+#pragma unroll
+    for (int u = 0; u < DELTA_AHEAD; ++u) {
+      const int h = (blockIdx.y * DELTA_AHEAD + u) * 2 + (lane >> 4);
+      const bool there = h < p.heads && d < p.dim;
+      g[u] = there ? __ldg(reinterpret_cast<const uint4*>(g_row + h * p.dim + d)) : make_uint4(0u, 0u, 0u, 0u);
+      o[u] = there ? __ldg(reinterpret_cast<const uint4*>(o_row + h * p.dim + d)) : make_uint4(0u, 0u, 0u, 0u);
+      lse[u] = h < p.heads ? __ldg(p.lse + h * p.q_rows + row) : 0.0f;
+    }
+    int b = 0;  // the last sequence that begins at or before the row
+    if (p.cu_q) {
+      int hi = p.sequences - 1;
+      while (b < hi) {
+        const int mid = (b + hi + 1) / 2;
+        if (p.cu_q[mid] <= row) b = mid;
+        else hi = mid - 1;
+      }
+    }
+    int q_first, q_count, k_first, k_count;
+    rows_of(p.cu_q, p.q_rows, b, &q_first, &q_count);
+    rows_of(p.cu_k, p.k_rows, b, &k_first, &k_count);
+    const int keys = p.causal ? min(k_count, (int)row - q_first + k_count - q_count + 1) : k_count;
+#pragma unroll
+    for (int u = 0; u < DELTA_AHEAD; ++u) {
+      const int h = (blockIdx.y * DELTA_AHEAD + u) * 2 + (lane >> 4);
+      float x[8], y[8], sum = 0.0f;
+      widen8(reinterpret_cast<const T*>(&g[u]), x);
+      widen8(reinterpret_cast<const T*>(&o[u]), y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        sum = fmaf(x[e], y[e], sum);
+        most_g = max(most_g, __float_as_uint(x[e]) & 0x7FFFFFFFu);
+      }
+#pragma unroll
+      for (int e = 8; e > 0; e /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, e);
+      if ((lane & 15) == 0 && h < p.heads && !(keys > 0 && keys <= FEW_KEYS))
+        p.stats[h * p.q_rows + row] = make_float2(lse[u] == -INFINITY ? INFINITY : lse[u] * LOG2E, sum);
+    }
+  }
+  if (row < p.k_rows && blockIdx.y == 0) {
+    const int64_t n = (int64_t)p.kv_heads * p.dim;
+    if (p.cu_k && (row < p.cu_k[0] || row >= p.cu_k[p.sequences])) {
+      for (int64_t i = lane * 8; i < n; i += 256) {
+        *reinterpret_cast<uint4*>(static_cast<T*>(p.grad_k) + row * n + i) = make_uint4(0u, 0u, 0u, 0u);
+        *reinterpret_cast<uint4*>(static_cast<T*>(p.grad_v) + row * n + i) = make_uint4(0u, 0u, 0u, 0u);
+      }
+    } else if (p.most) {
+      for (int h = lane >> 4; h < p.kv_heads; h += 2) {
+        if (d >= p.dim) continue;
+        float v[8];
+        load_half8(static_cast<const T*>(p.v) + row * p.v_at.token + h * p.v_at.head + d, v);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) most_v = max(most_v, __float_as_uint(v[e]) & 0x7FFFFFFFu);
+      }
     }
   }
   if (p.most) {  // (a maximum does not depend on the order)
     most_g = __reduce_max_sync(0xFFFFFFFFu, most_g);
     most_v = __reduce_max_sync(0xFFFFFFFFu, most_v);
-    if ((threadIdx.x & 31) == 0) {
+    if (lane == 0) {
       if (most_g > __ldcg(p.most)) atomicMax(p.most, most_g);
       if (most_v > __ldcg(p.most + 1)) atomicMax(p.most + 1, most_v);
     }
@@ -181,7 +221,8 @@ struct GradShared {
   uint64_t cut1[CUTS], clean1[CUTS], cut2[CUTS], clean2[CUTS];  // copies that a mask cuts, and their cleaning
   uint64_t t1, t1_read, t2, ds_there, done;
   uint32_t tmem;
-  int dead, seq, block, found;
+  int dead;
+  Place place;
   alignas(16) float minus[2][YC], delta[2][YC];
 };
 
@@ -199,13 +240,11 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
   const int warp = threadIdx.x >> 5;
   const uint32_t ring1 = base + 2 * TILE, ring2 = ring1 + Y1_SLOTS * TILE;
   volatile int* const dead = &sh.dead;
-  int q_first, q_count, k_first, k_count;
-  rows_of(p.cu_q, p.q_rows, sh.seq, &q_first, &q_count);
-  rows_of(p.cu_k, p.k_rows, sh.seq, &k_first, &k_count);
+  const Place place = sh.place;
+  const int q_first = place.q_first, q_count = place.q_count, k_first = place.k_first, k_count = place.k_count;
   const int off = k_count - q_count;
   const int x_first = KEYS ? k_first : q_first, x_count = KEYS ? k_count : q_count, y_first = KEYS ? q_first : k_first, y_count = KEYS ? q_count : k_count;
-  // longest first: the last queries, the first keys
-  const int block = !KEYS && p.causal ? (x_count + XT - 1) / XT - 1 - sh.block : sh.block;
+  const int block = KEYS ? place.blocks - 1 - place.level : place.level;  // (with a causal mask the first keys and the last queries have most to do)
   const int x0 = block * XT;
   Walk walk;
   walk.heads = KEYS ? p.group : 1;
@@ -516,8 +555,14 @@ template <typename T, int DT>
 __global__ void __launch_bounds__(GRAD_THREADS, 1) attention_grad_kernel(const __grid_constant__ GradParams p) {
   extern __shared__ uint8_t raw_smem[];
   __shared__ GradShared sh;
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int warp = threadIdx.x >> 5;
   const uint32_t base = (smem_u32(raw_smem) + 1023) & ~1023u;
+  if (threadIdx.x == 8 * 32) {
+    map_ahead(&p.q);
+    map_ahead(&p.k);
+    map_ahead(&p.v);
+    map_ahead(&p.g);
+  }
   if (threadIdx.x == 0) {
     mbar_init(smem_u32(&sh.x_full), 1);
     mbar_init(smem_u32(&sh.done), 1);
@@ -548,19 +593,14 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) attention_grad_kernel(const _
   const int64_t index = keys ? blockIdx.x : blockIdx.x - p.key_blocks;
   const int heads = keys ? p.kv_heads : p.heads, head = (int)(index % heads);
   if (warp == 8) {
-    int seq = 0, block = 0;
-    const bool found = find_block(keys ? p.cu_k : p.cu_q, keys ? p.k_rows : p.q_rows, p.sequences, XT, index / heads, &seq, &block);
-    if (lane == 0) {
-      sh.found = found;
-      sh.seq = seq;
-      sh.block = block;
-    }
+    const Place place = find_place(p.cu_q, p.q_rows, p.cu_k, p.k_rows, p.sequences, keys, XT, index / heads);
+    if ((threadIdx.x & 31) == 0) sh.place = place;
   }
   tmem_before();
   __syncthreads();
   tmem_after();
   const uint32_t tmem = sh.tmem;
-  const bool found = sh.found != 0;
+  const bool found = sh.place.found != 0;
   if (found) {
     if (keys) attention_grad<T, DT, true>(p, sh, raw_smem, base, head, tmem);
     else attention_grad<T, DT, false>(p, sh, raw_smem, base, head, tmem);
@@ -653,13 +693,14 @@ int lba_attention_backward(const void* grad_out, const void* q, const void* k, c
   p.scale = how->scale;
   p.key_blocks = (how->k_rows / XT + how->sequences) * how->kv_heads;
   const int64_t blocks = p.key_blocks + (how->q_rows / XT + how->sequences) * how->heads;
-  const int64_t vectors = how->q_rows * how->heads > how->k_rows * how->kv_heads ? how->q_rows * how->heads : how->k_rows * how->kv_heads;
-  const int64_t delta_blocks = (vectors + DELTA_THREADS / 16 - 1) / (DELTA_THREADS / 16);
+  const int64_t most_rows = how->q_rows > how->k_rows ? how->q_rows : how->k_rows, row_blocks = (most_rows + DELTA_THREADS / 32 - 1) / (DELTA_THREADS / 32);
+  const int64_t delta_blocks = row_blocks + (int64_t)how->sequences * how->heads;
+  d.row_blocks = row_blocks;
   if (delta_blocks > 2147483647LL || blocks > 2147483647LL) return LBA_ERR_SHAPE;
   cudaError_t e = most ? cudaMemsetAsync(most, 0, 8, s) : cudaSuccess;
   if (e != cudaSuccess) return status_of(e);
-  e = p.bf ? launch_after(attention_delta_kernel<__nv_bfloat16>, dim3((unsigned)delta_blocks), DELTA_THREADS, 0, s, d)
-           : launch_after(attention_delta_kernel<__half>, dim3((unsigned)delta_blocks), DELTA_THREADS, 0, s, d);
+  e = p.bf ? launch_after(attention_delta_kernel<__nv_bfloat16>, dim3((unsigned)delta_blocks, (unsigned)((how->heads + 2 * DELTA_AHEAD - 1) / (2 * DELTA_AHEAD))), DELTA_THREADS, 0, s, d)
+           : launch_after(attention_delta_kernel<__half>, dim3((unsigned)delta_blocks, (unsigned)((how->heads + 2 * DELTA_AHEAD - 1) / (2 * DELTA_AHEAD))), DELTA_THREADS, 0, s, d);
   if (e != cudaSuccess) return status_of(e);
   if (how->dim <= 64) return status_of(p.bf ? launch_grad<__nv_bfloat16, 64>(p, blocks, s) : launch_grad<__half, 64>(p, blocks, s));
   return status_of(p.bf ? launch_grad<__nv_bfloat16, 128>(p, blocks, s) : launch_grad<__half, 128>(p, blocks, s));

@@ -65,6 +65,7 @@ __device__ __forceinline__ void mma_tensor(uint32_t d, uint32_t a, uint64_t b, u
 __device__ __forceinline__ void mma_arrive(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
 }
+__device__ __forceinline__ void map_ahead(const CUtensorMap* map) { asm volatile("prefetch.tensormap [%0];" ::"l"(map) : "memory"); }
 // rows y.. of head h, values x to x + 63, as a block of a tile
 __device__ __forceinline__ void tile_load(uint32_t dst, const CUtensorMap* map, int x, int h, int y, uint32_t bar) {
   asm volatile("cp.async.bulk.tensor.3d.shared::cta.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];" ::"r"(dst), "l"(map),
@@ -106,15 +107,70 @@ __device__ __forceinline__ void rows_of(const int32_t* cu, int64_t rows, int b, 
   *first = lo;
   *count = max(hi - lo, 0);
 }
-// Block `index` of all sequences' blocks of `size` rows: its sequence and its number there; false past the last.  A warp, every lane the same
-// arguments and results.  Sequences are counted 32 at a time.
-__device__ __forceinline__ bool find_block(const int32_t* cu, int64_t rows, int sequences, int size, int64_t index, int* seq, int* block) {
+// Where a block of `size` rows lies: of a sequence with `blocks` of them, the one with `level` blocks that have less to do (or as much).
+struct Place {
+  int found, level, blocks, q_first, q_count, k_first, k_count;
+};
+// Block `index` of all sequences' blocks of their rows of q, or of k; a warp, every lane the same arguments and results.  With up to 128
+// sequences, blocks of high levels come first, whatever their sequence: a launch ends with short ones (seven sequences of 1 to 2003 rows, the
+// longest one last, took 52 us in the sequences' order).  With more, sequence by sequence.  One trip to memory for both kinds of rows.
+__device__ __forceinline__ Place find_place(const int32_t* cu_q, int64_t q_rows, const int32_t* cu_k, int64_t k_rows, int sequences, bool by_keys, int size,
+                                            int64_t index) {
   const int lane = threadIdx.x & 31;
+  Place p = {};
+  const auto blocks_of = [&](int b, Place& x) -> int {
+    x.q_count = x.k_count = 0;
+    if (b >= sequences) return 0;
+    rows_of(cu_q, q_rows, b, &x.q_first, &x.q_count);
+    rows_of(cu_k, k_rows, b, &x.k_first, &x.k_count);
+    return ((by_keys ? x.k_count : x.q_count) + size - 1) / size;
+  };
+  const auto take = [&](const Place& x, int from) {
+    p.found = 1;
+    p.q_first = __shfl_sync(0xFFFFFFFFu, x.q_first, from);
+    p.q_count = __shfl_sync(0xFFFFFFFFu, x.q_count, from);
+    p.k_first = __shfl_sync(0xFFFFFFFFu, x.k_first, from);
+    p.k_count = __shfl_sync(0xFFFFFFFFu, x.k_count, from);
+    p.blocks = ((by_keys ? p.k_count : p.q_count) + size - 1) / size;
+  };
+  constexpr int MANY = 4;
+  if (sequences <= 32 * MANY) {
+    Place x[MANY];
+    int n[MANY], most = 0;
+#pragma unroll
+    for (int i = 0; i < MANY; ++i) n[i] = 32 * i < sequences ? blocks_of(32 * i + lane, x[i]) : 0;
+#pragma unroll
+    for (int i = 0; i < MANY; ++i) most = max(most, n[i]);
+    most = __reduce_max_sync(0xFFFFFFFFu, most);
+    const auto from_level = [&](int t) -> int64_t {  // blocks of level t and above
+      int64_t sum = 0;
+#pragma unroll
+      for (int i = 0; i < MANY; ++i)
+        if (32 * i < sequences) sum += __reduce_add_sync(0xFFFFFFFFu, max(0, n[i] - t));
+      return sum;
+    };
+    if (index >= from_level(0)) return p;
+    int lo = 0, hi = most - 1;  // the highest level that index has reached
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (from_level(mid) > index) lo = mid;
+      else hi = mid - 1;
+    }
+    int rank = (int)(index - from_level(lo + 1));
+#pragma unroll
+    for (int i = 0; i < MANY; ++i) {
+      if (32 * i >= sequences || p.found) continue;
+      const unsigned has = __ballot_sync(0xFFFFFFFFu, n[i] > lo);
+      if (rank < __popc(has)) take(x[i], __fns(has, 0, rank + 1));
+      else rank -= __popc(has);
+    }
+    p.level = lo;
+    return p;
+  }
   for (int b0 = 0; b0 < sequences; b0 += 32) {
-    int first, count = 0;
-    if (b0 + lane < sequences) rows_of(cu, rows, b0 + lane, &first, &count);
-    const int blocks = (count + size - 1) / size;
-    int upto = blocks;
+    Place x;
+    const int n = blocks_of(b0 + lane, x);
+    int upto = n;
 #pragma unroll
     for (int d = 1; d < 32; d *= 2) {
       const int v = __shfl_up_sync(0xFFFFFFFFu, upto, d);
@@ -123,13 +179,13 @@ __device__ __forceinline__ bool find_block(const int32_t* cu, int64_t rows, int 
     const unsigned hit = __ballot_sync(0xFFFFFFFFu, index < upto);
     if (hit) {
       const int l = __ffs(hit) - 1;
-      *seq = b0 + l;
-      *block = (int)(index - (__shfl_sync(0xFFFFFFFFu, upto, l) - __shfl_sync(0xFFFFFFFFu, blocks, l)));
-      return true;
+      take(x, l);
+      p.level = __shfl_sync(0xFFFFFFFFu, upto, l) - 1 - (int)index;
+      return p;
     }
     index -= __shfl_sync(0xFFFFFFFFu, upto, 31);
   }
-  return false;
+  return p;
 }
 
 int check_attention(const lba_attention_how* how);  // lba_attention.cu
