@@ -41,7 +41,7 @@ template <int DT> constexpr int kStages = DT == 128 ? 5 : 10;
 template <int DT> constexpr size_t kForwardSmem = 1024 + (size_t)kTile<DT> * (2 + kStages<DT>);
 
 struct ForwardShared {
-  uint64_t q_full[2], full[MAX_STAGES], empty[MAX_STAGES], scores[2], weights[2], done;
+  uint64_t q_full[2], full[MAX_STAGES], empty[MAX_STAGES], scores[2], weights[2][2], done;  // weights: of the first 96 keys of a tile, of the others
   uint64_t cut_full[CUT_TILES], clean[CUT_TILES];  // copies of V that the mask cuts, and their cleaning: once each
   uint32_t cut[CUT_TILES][4];  // rows of the masked tiles of V that hold values that are not finite
   uint32_t tmem;
@@ -49,19 +49,73 @@ struct ForwardShared {
   Place place;
 };
 
-// weights of 32 scores, relative to the maximum: packed, and their sum
-template <typename T>
-__device__ __forceinline__ void weigh32(uint32_t* s, uint32_t* out, u64 by, u64 minus, u64& sum) {
+// 2^x of a pair without the exponential units: the nearest whole number goes into the exponent, 2^f of what is left, |f| <= 1/2, is a polynomial of
+// the fourth degree (least maximum of the relative error by repeated least squares in 64 bits: 2.6e-6).  Below 2^-126 it is that; NaN stays.
+__device__ __forceinline__ void exp2_poly(u64 x, float& lo, float& hi) {
+  constexpr float WHOLE = 12582912.0f;  // 1.5 2^23: a sum with it has the nearest whole number in its lowest bits
+  unpack2(x, lo, hi);
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(lo) : "f"(lo), "f"(-126.0f));
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(hi) : "f"(hi), "f"(-126.0f));
+  const u64 y = pack2(lo, hi), t = add2_rn(y, both(WHOLE)), f = fma2_rn(add2_rn(t, both(-WHOLE)), both(-1.0f), y);
+  u64 v = fma2_rn(both(0.0095701f), f, both(0.05591786f));
+  v = fma2_rn(v, f, both(0.24024745f));
+  v = fma2_rn(v, f, both(0.69312181f));
+  v = fma2_rn(v, f, both(0.99999926f));
+  float t0, t1;
+  unpack2(t, t0, t1);
+  // (a product, not a sum of bits, which would make a number of a NaN)
+  unpack2(mul2_rn(v, pack2u((__float_as_uint(t0) << 23) + 0x3F800000u, (__float_as_uint(t1) << 23) + 0x3F800000u)), lo, hi);
+}
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
+}
+// weights of 32 scores, relative to the maximum: packed, and their sum.  SHARE: every fourth pair is left to the FMA units, which have less to do
+template <typename T, bool SHARE>
+__device__ __forceinline__ void weigh32(const uint32_t* s, uint32_t* out, u64 by, u64 minus, u64 (&sum)[4]) {
 #pragma unroll
   for (int i = 0; i < 32; i += 2) {
+    const u64 x = fma2_rn(pack2u(s[i], s[i + 1]), by, minus);
     float lo, hi;
-    unpack2(fma2_rn(pack2u(s[i], s[i + 1]), by, minus), lo, hi);
-    lo = exp2_approx(lo);
-    hi = exp2_approx(hi);
-    sum = add2_rn(sum, pack2(lo, hi));
+    if (SHARE && i % 8 == 6) {
+      exp2_poly(x, lo, hi);
+    } else {
+      unpack2(x, lo, hi);
+      lo = exp2_approx(lo);
+      hi = exp2_approx(hi);
+    }
+    sum[i / 2 % 4] = add2_rn(sum[i / 2 % 4], pack2(lo, hi));
     out[i / 2] = pack_pair<T>(lo, hi);
   }
 }
+
+// Codes of quotients, nearest and saturated as encode_e4m3 and encode_m4e3 of the rounded quotient.  Both ends of an interval around v times the
+// reciprocal that holds the quotient have the same code almost always, codes being monotone; only else is there a division (which branches, and
+// took 117 clocks an element).
+struct Quotients {
+  float scale, low, high;  // reciprocals less and plus 2^-21 of themselves; 0 where they have no such precision
+  __device__ __forceinline__ explicit Quotients(float s) : scale(s) {
+    const bool normal = s > 0x1p-100f && s < 0x1p100f;
+    const float r = normal ? 1.0f / s : 0.0f;
+    low = r * (1.0f - 0x1p-21f);
+    high = r * (1.0f + 0x1p-21f);
+  }
+  __device__ __forceinline__ static uint32_t four(float a, float b, float c, float d, bool m4e3) {
+    if (m4e3) return encode_m4e3(a) | (uint32_t)encode_m4e3(b) << 8 | (uint32_t)encode_m4e3(c) << 16 | (uint32_t)encode_m4e3(d) << 24;
+    uint32_t x;
+    asm("{\n\t.reg .b16 l, h;\n\tcvt.rn.satfinite.e4m3x2.f32 l, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 h, %4, %3;\n\tmov.b32 %0, {l, h};\n\t}"
+        : "=r"(x) : "f"(a), "f"(b), "f"(c), "f"(d));
+    return x;
+  }
+  __device__ __noinline__ static uint32_t divided(float a, float b, float c, float d, float s, bool m4e3) {
+    return four(__fdiv_rn(a, s), __fdiv_rn(b, s), __fdiv_rn(c, s), __fdiv_rn(d, s), m4e3);
+  }
+  __device__ __forceinline__ uint32_t codes(const float4& v, bool m4e3) const {
+    const uint32_t x = four(v.x * low, v.y * low, v.z * low, v.w * low, m4e3), y = four(v.x * high, v.y * high, v.z * high, v.w * high, m4e3);
+    return x == y && low != 0.0f ? x : divided(v.x, v.y, v.z, v.w, scale, m4e3);
+  }
+};
 
 template <typename T, int DT>
 __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_constant__ ForwardParams p) {
@@ -83,7 +137,8 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
       for (int i = 0; i < 2; ++i) {
         mbar_init(smem_u32(&sh.q_full[i]), 1);
         mbar_init(smem_u32(&sh.scores[i]), 1);
-        mbar_init(smem_u32(&sh.weights[i]), 128);
+        mbar_init(smem_u32(&sh.weights[i][0]), 128);
+        mbar_init(smem_u32(&sh.weights[i][1]), 128);
       }
       for (int i = 0; i < STAGES; ++i) {
         mbar_init(smem_u32(&sh.full[i]), 1);
@@ -188,13 +243,17 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
 #pragma unroll
             for (int w = 0; w < 2; ++w) {
               if (j >= tiles[w]) continue;
-              ok = ok && mbar_wait(smem_u32(&sh.weights[w]), j & 1, dead);
-              if (!ok) break;
-              tmem_after();
               const uint64_t b = lines + ((ring + vs * TILE) >> 4);
 #pragma unroll
-              for (int s = 0; s < KT / 16; ++s)
+              for (int s = 0; s < KT / 16; ++s) {
+                if (s == 0 || s == 6) {
+                  ok = ok && mbar_wait(smem_u32(&sh.weights[w][s / 6]), j & 1, dead);
+                  if (!ok) break;
+                  tmem_after();
+                }
                 mma_tensor(tmem + 256 + w * 128, tmem + w * KT + s * 8, b + s * (2048 >> 4), kind_o, j != 0 || s != 0);
+              }
+              if (!ok) break;
               if (j + 1 < tiles[w]) scores(w, j + 1);
               else mma_arrive(smem_u32(&sh.scores[w]));  // the output is complete
             }
@@ -250,7 +309,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
       const uint32_t lanes = (uint32_t)(warp & 3) << 21, s_at = tmem + w * KT + lanes, o_at = tmem + 256 + w * 128 + lanes;
       const float c = p.to_log2;
       float top = -INFINITY;
-      u64 total = both(0.0f);
+      u64 total[4] = {};  // chains of their own
       bool ok = true;
       for (int j = 0; j < mine; ++j) {
         ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&sh.scores[w]), j & 1, dead));
@@ -266,16 +325,24 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
           for (int x = 0; x < KT; ++x)
             if (x >= limit) s[x] = 0xFF800000u;
         }
-        float most = __uint_as_float(s[0]);
+        // (three operands an instruction, eight chains: one chain of 127 took 450 clocks)
+        float top8[8];
 #pragma unroll
-        for (int x = 1; x < KT; ++x) most = fmaxf(most, __uint_as_float(s[x]));
+        for (int x = 0; x < 8; ++x) top8[x] = __uint_as_float(s[x]);
+#pragma unroll
+        for (int x = 8; x < KT; x += 16) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) top8[e] = x + 8 + e < KT ? max3(top8[e], __uint_as_float(s[x + e]), __uint_as_float(s[x + 8 + e])) : fmaxf(top8[e], __uint_as_float(s[x + e]));
+        }
+        const float most = max3(max3(top8[0], top8[1], top8[2]), max3(top8[3], top8[4], top8[5]), fmaxf(top8[6], top8[7]));
         const bool raise = most * c > top * c + LAZY;  // (true whenever there is no maximum yet, and some score)
         if (__any_sync(0xFFFFFFFFu, raise)) {
           const float next = fmaxf(top, most);
           if (j > 0) {
             const float by = next == -INFINITY ? 1.0f : exp2_approx((top - next) * c);
             const u64 by2 = both(by);
-            total = mul2_rn(total, by2);
+#pragma unroll
+            for (int x = 0; x < 4; ++x) total[x] = mul2_rn(total[x], by2);
             for (int x = 0; x < p.dim; x += 32) {
               uint32_t o[32];
               tmem_load32(o_at + x, o);
@@ -289,75 +356,84 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
         }
         const u64 by = both(c), minus = both(top == -INFINITY ? 0.0f : -top * c);
         uint32_t packed[KT / 2];
+        const auto weigh = [&](auto share) {
+          // (the first products start while the last quarter is formed)
 #pragma unroll
-        for (int x = 0; x < KT; x += 32) weigh32<T>(s + x, packed + x / 2, by, minus, total);
-        tmem_store32(s_at, packed);
-        tmem_store32(s_at + 32, packed + 32);
-        tmem_wait_st();
-        tmem_before();
-        mbar_arrive(smem_u32(&sh.weights[w]));
+          for (int x = 0; x < 96; x += 32) weigh32<T, decltype(share)::value>(s + x, packed + x / 2, by, minus, total);
+          tmem_store32(s_at, packed);
+          tmem_st16(s_at + 32, *reinterpret_cast<const uint32_t(*)[16]>(packed + 32));
+          tmem_wait_st();
+          tmem_before();
+          mbar_arrive(smem_u32(&sh.weights[w][0]));
+          weigh32<T, decltype(share)::value>(s + 96, packed + 48, by, minus, total);
+          tmem_st16(s_at + 48, *reinterpret_cast<const uint32_t(*)[16]>(packed + 48));
+          tmem_wait_st();
+          tmem_before();
+          mbar_arrive(smem_u32(&sh.weights[w][1]));
+        };
+        if (j >= whole[w]) weigh(std::false_type());  // (a masked weight is 0, not 2^-126)
+        else weigh(std::true_type());
       }
       if (mine && ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&sh.scores[w]), mine & 1, dead));
       tmem_after();
       float lo, hi;
-      unpack2(total, lo, hi);
+      unpack2(add2_rn(add2_rn(total[0], total[1]), add2_rn(total[2], total[3])), lo, hi);
       const float sum = lo + hi;
       const bool there = i < q_count;
-      const int64_t at = (int64_t)(q_first + i) * p.heads + head;
       if (there && p.lse)
         p.lse[(int64_t)head * p.q_rows + q_first + i] =
             !ok ? __uint_as_float(0x7FC00000u) : sum == 0.0f ? -INFINITY : (top * c + log2f(sum)) * 0.69314718055994531f;
-      const float inv = sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum);
+      const float inv = !ok ? __uint_as_float(0x7FC00000u) : sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum);
       uint32_t poison = 0;  // of the cut tiles, as one word: any at all?
       if (p.causal) {
         for (int x = 0; x < CUT_TILES; ++x)
           for (int e = 0; e < 4; ++e) poison |= sh.cut[x][e];
       }
-      const float out_scale = p.codes ? *p.out_scale : 1.0f;
+      const Quotients quotients(p.codes ? *p.out_scale : 1.0f);
+      // 32 values a row at a time go out through shared memory (the tile of Q is no longer read), four lanes a row side by side.  The code is kept
+      // short: it runs once a CTA and is fetched as it runs (unrolled over a row's values, codes took 10000 clocks).
+      uint8_t* const stage = raw_smem + (q_smem - smem_u32(raw_smem)) + w * TILE + (warp & 3) * 4096;
+      const int rows = min(32, q_count - (i - lane));
 #pragma unroll 1
-      for (int x = 0; x < p.dim; x += 32) {
+      for (int x = 0; x < p.dim && rows > 0; x += 32) {
         uint32_t o[32];
-        __syncwarp();
         if (mine) {
           tmem_load32(o_at + x, o);
           tmem_wait_ld();
-        }
-        float f[32];
+        } else {
 #pragma unroll
-        for (int e = 0; e < 32; ++e) f[e] = !ok ? __uint_as_float(0x7FC00000u) : mine ? __uint_as_float(o[e]) * inv : 0.0f;
+          for (int e = 0; e < 32; ++e) o[e] = 0u;
+        }
+#pragma unroll
+        for (int e = 0; e < 32; e += 4)
+          *reinterpret_cast<float4*>(stage + swizzled(lane, e / 4)) =
+              make_float4(__uint_as_float(o[e]) * inv, __uint_as_float(o[e + 1]) * inv, __uint_as_float(o[e + 2]) * inv, __uint_as_float(o[e + 3]) * inv);
         if (poison && there) {
           for (int t = 0; t < CUT_TILES * 128; ++t) {
             const int key = dirty * KT + t;
             if (!((sh.cut[t >> 7][(t >> 5) & 3] >> (t & 31)) & 1u) || key > i + off) continue;
             const T* const src = static_cast<const T*>(p.v_raw) + (int64_t)(k_first + key) * p.v_at.token + kv * p.v_at.head + x;
-#pragma unroll
-            for (int e = 0; e < 32; ++e) {
-              const float v = x + e < p.dim ? to_f32(src[e]) : 0.0f;
-              if (!isfinite(v)) f[e] += v;
+#pragma unroll 1
+            for (int e = 0; e < 32 && x + e < p.dim; ++e) {
+              const float v = to_f32(src[e]);
+              if (!isfinite(v)) *reinterpret_cast<float*>(stage + swizzled(lane, e >> 2) + (e & 3) * 4) += v;
             }
           }
         }
-        if (!there) continue;
+        __syncwarp();
+        const int c = lane & 3, col = x + c * 8;
 #pragma unroll
-        for (int e = 0; e < 32; e += 8) {
-          if (x + e >= p.dim) break;
+        for (int r = lane >> 2; r < 32; r += 8) {
+          if (r >= rows || col >= p.dim) break;
+          const float4 a = *reinterpret_cast<const float4*>(stage + swizzled(r, 2 * c)), b = *reinterpret_cast<const float4*>(stage + swizzled(r, 2 * c + 1));
+          const int64_t at = ((int64_t)(q_first + i - lane + r) * p.heads + head) * p.dim + col;
           if (p.codes) {
-            uint8_t b[8];
-#pragma unroll
-            for (int t = 0; t < 8; ++t) {
-              const float z = __fdiv_rn(f[e + t], out_scale);
-              b[t] = p.in_m4e3 ? encode_m4e3(z) : encode_e4m3(z);
-            }
-            store_some<uint8_t, 8>(p.out, at * p.dim + x + e, 8, b);
+            *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.out) + at) = make_uint2(quotients.codes(a, p.in_m4e3), quotients.codes(b, p.in_m4e3));
           } else {
-            uint4 v;
-            v.x = pack_pair<T>(f[e], f[e + 1]);
-            v.y = pack_pair<T>(f[e + 2], f[e + 3]);
-            v.z = pack_pair<T>(f[e + 4], f[e + 5]);
-            v.w = pack_pair<T>(f[e + 6], f[e + 7]);
-            *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + at * p.dim + x + e) = v;
+            *reinterpret_cast<uint4*>(static_cast<T*>(p.out) + at) = make_uint4(pack_pair<T>(a.x, a.y), pack_pair<T>(a.z, a.w), pack_pair<T>(b.x, b.y), pack_pair<T>(b.z, b.w));
           }
         }
+        __syncwarp();
       }
       tmem_before();
     }
