@@ -49,42 +49,21 @@ struct ForwardShared {
   Place place;
 };
 
-// 2^x of a pair without the exponential units: the nearest whole number goes into the exponent, 2^f of what is left, |f| <= 1/2, is a polynomial of
-// the fourth degree (least maximum of the relative error by repeated least squares in 64 bits: 2.6e-6).  Below 2^-126 it is that; NaN stays.
-__device__ __forceinline__ void exp2_poly(u64 x, float& lo, float& hi) {
-  constexpr float WHOLE = 12582912.0f;  // 1.5 2^23: a sum with it has the nearest whole number in its lowest bits
-  unpack2(x, lo, hi);
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(lo) : "f"(lo), "f"(-126.0f));
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(hi) : "f"(hi), "f"(-126.0f));
-  const u64 y = pack2(lo, hi), t = add2_rn(y, both(WHOLE)), f = fma2_rn(add2_rn(t, both(-WHOLE)), both(-1.0f), y);
-  u64 v = fma2_rn(both(0.0095701f), f, both(0.05591786f));
-  v = fma2_rn(v, f, both(0.24024745f));
-  v = fma2_rn(v, f, both(0.69312181f));
-  v = fma2_rn(v, f, both(0.99999926f));
-  float t0, t1;
-  unpack2(t, t0, t1);
-  // (a product, not a sum of bits, which would make a number of a NaN)
-  unpack2(mul2_rn(v, pack2u((__float_as_uint(t0) << 23) + 0x3F800000u, (__float_as_uint(t1) << 23) + 0x3F800000u)), lo, hi);
-}
 __device__ __forceinline__ float max3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
   return d;
 }
-// weights of 32 scores, relative to the maximum: packed, and their sum.  SHARE: every fourth pair is left to the FMA units, which have less to do
-template <typename T, bool SHARE>
+// weights of 32 scores, relative to the maximum: packed, and their sum.  (A quarter of the exponentials as polynomials on the FMA units was slower:
+// a prompt of 8192 took 481 us instead of 461, and 540 instead of 520 at the power limit.)
+template <typename T>
 __device__ __forceinline__ void weigh32(const uint32_t* s, uint32_t* out, u64 by, u64 minus, u64 (&sum)[4]) {
 #pragma unroll
   for (int i = 0; i < 32; i += 2) {
-    const u64 x = fma2_rn(pack2u(s[i], s[i + 1]), by, minus);
     float lo, hi;
-    if (SHARE && i % 8 == 6) {
-      exp2_poly(x, lo, hi);
-    } else {
-      unpack2(x, lo, hi);
-      lo = exp2_approx(lo);
-      hi = exp2_approx(hi);
-    }
+    unpack2(fma2_rn(pack2u(s[i], s[i + 1]), by, minus), lo, hi);
+    lo = exp2_approx(lo);
+    hi = exp2_approx(hi);
     sum[i / 2 % 4] = add2_rn(sum[i / 2 % 4], pack2(lo, hi));
     out[i / 2] = pack_pair<T>(lo, hi);
   }
@@ -356,23 +335,19 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
         }
         const u64 by = both(c), minus = both(top == -INFINITY ? 0.0f : -top * c);
         uint32_t packed[KT / 2];
-        const auto weigh = [&](auto share) {
-          // (the first products start while the last quarter is formed)
+        // (the first products start while the last quarter is formed)
 #pragma unroll
-          for (int x = 0; x < 96; x += 32) weigh32<T, decltype(share)::value>(s + x, packed + x / 2, by, minus, total);
-          tmem_store32(s_at, packed);
-          tmem_st16(s_at + 32, *reinterpret_cast<const uint32_t(*)[16]>(packed + 32));
-          tmem_wait_st();
-          tmem_before();
-          mbar_arrive(smem_u32(&sh.weights[w][0]));
-          weigh32<T, decltype(share)::value>(s + 96, packed + 48, by, minus, total);
-          tmem_st16(s_at + 48, *reinterpret_cast<const uint32_t(*)[16]>(packed + 48));
-          tmem_wait_st();
-          tmem_before();
-          mbar_arrive(smem_u32(&sh.weights[w][1]));
-        };
-        if (j >= whole[w]) weigh(std::false_type());  // (a masked weight is 0, not 2^-126)
-        else weigh(std::true_type());
+        for (int x = 0; x < 96; x += 32) weigh32<T>(s + x, packed + x / 2, by, minus, total);
+        tmem_store32(s_at, packed);
+        tmem_st16(s_at + 32, *reinterpret_cast<const uint32_t(*)[16]>(packed + 32));
+        tmem_wait_st();
+        tmem_before();
+        mbar_arrive(smem_u32(&sh.weights[w][0]));
+        weigh32<T>(s + 96, packed + 48, by, minus, total);
+        tmem_st16(s_at + 48, *reinterpret_cast<const uint32_t(*)[16]>(packed + 48));
+        tmem_wait_st();
+        tmem_before();
+        mbar_arrive(smem_u32(&sh.weights[w][1]));
       }
       if (mine && ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&sh.scores[w]), mine & 1, dead));
       tmem_after();

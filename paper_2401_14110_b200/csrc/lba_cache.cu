@@ -868,28 +868,45 @@ __global__ void __launch_bounds__(DEC_THREADS, 1) cache_attention_kernel(const D
 }
 
 // a line's parts together: a block per head
+constexpr int PARTS_AT_ONCE = 256;
 template <int NG, int HT>
 __global__ void __launch_bounds__(32 * NG) cache_combine_kernel(const DecodeParams p) {
   constexpr int D = 32 * NG, PART = D + 2;
+  __shared__ float2 weight[PARTS_AT_ONCE];  // of a part: its maximum and sum; then the factor of its outputs, and its sum times that
+  __shared__ float tops[NG];
   after_previous();
   const int b = blockIdx.y, h = blockIdx.x, d = threadIdx.x, lines = p.lines();
   const int kvh = h / p.group, in_group = h - kvh * p.group, piece = in_group / HT, line = kvh * p.pieces + piece, col = in_group - piece * HT;
   const int begin = p.before[b], units = p.before[b + 1] - begin, share = share_of(p, p.before[p.c.sequences]), first = begin * lines + line * units;
+  const int w0 = first / share, n = units > 0 ? (first + units - 1) / share - w0 + 1 : 0;
+  const float* const part = p.parts + (w0 + (int64_t)b * lines + line) * (HT * PART) + col * PART;
   float top = NO_MAX, sum = 0.0f, v = 0.0f;
-  if (units > 0) {
-    const int w0 = first / share, n = (first + units - 1) / share - w0 + 1;
-    const float* const part = p.parts + (w0 + (int64_t)b * lines + line) * (HT * PART) + col * PART;
-#pragma unroll 4
-    for (int i = 0; i < n; ++i) {
-      const float* const src = part + (int64_t)i * HT * PART;
-      const float2 ml = __ldg(reinterpret_cast<const float2*>(src + D));
-      const float vi = __ldg(src + d);
-      const float t = fmaxf(top, ml.x), was = exp2_approx(top - t), by = exp2_approx(ml.x - t);
-      sum = sum * was + ml.y * by;
-      v = v * was;
-      if (ml.y != 0.0f) v = fmaf(vi, by, v);  // (tokens that are not there leave nothing)
-      top = t;
+  for (int i0 = 0; i0 < n; i0 += PARTS_AT_ONCE) {  // (two trips to memory for 256 parts; one after the other they cost one each four)
+    const int here = min(n - i0, PARTS_AT_ONCE);
+    float most = top;
+    for (int i = d; i < here; i += D) {
+      const float2 ml = __ldg(reinterpret_cast<const float2*>(part + (int64_t)(i0 + i) * HT * PART + D));
+      weight[i] = ml;
+      most = fmaxf(most, ml.x);
     }
+#pragma unroll
+    for (int x = 16; x > 0; x /= 2) most = fmaxf(most, __shfl_xor_sync(0xFFFFFFFFu, most, x));
+    if ((d & 31) == 0) tops[d >> 5] = most;
+    __syncthreads();
+#pragma unroll
+    for (int x = 0; x < NG; ++x) most = fmaxf(most, tops[x]);
+    const float was = exp2_approx(top - most);
+    top = most;
+    sum *= was;
+    v *= was;
+    const float* src = part + (int64_t)i0 * HT * PART + d;
+#pragma unroll 8
+    for (int i = 0; i < here; ++i, src += HT * PART) {
+      const float vi = __ldg(src), by = exp2_approx(weight[i].x - top);
+      sum = fmaf(weight[i].y, by, sum);
+      if (weight[i].y != 0.0f) v = fmaf(vi, by, v);  // (tokens that are not there leave nothing)
+    }
+    __syncthreads();
   }
   store_decoded<D>(p, ((int64_t)b * p.heads + h) * D + d, sum == 0.0f ? 0.0f : __fdiv_rn(v, sum));
 }
