@@ -250,7 +250,7 @@ typedef struct {
   int32_t type;         /* LBA_TYPE_BF16 or F16: of q, k, v and what has their shapes                 */
   int32_t heads, kv_heads, dim; /* heads a multiple of kv_heads; dim a multiple of 8, 8..128            */
   int32_t causal, sequences;
-  float scale;          /* finite                                                                     */
+  float scale;          /* finite and > 0                                                             */
   int64_t q_rows, k_rows; /* below 2^31 - 1024                                                          */
   const int32_t *cu_q, *cu_k; /* device, [sequences + 1] each; NULL: one sequence of all rows           */
   lba_strides q_at, k_at, v_at; /* multiples of 8, as the tensors start at multiples of 16 bytes         */
@@ -295,8 +295,8 @@ int lba_cache_append(const lba_cache* cache, const void* k, lba_strides k_at, co
 int lba_cache_read(const lba_cache* cache, const int32_t* start, const int32_t* cu, int64_t tokens, int type, void* k, void* v,
                    void* stream);
 /* One new token of each sequence: out[b][h] = softmax(scale q[b][h] k) v over the first lengths[b] tokens of the cache (0 for none);
- * q [sequences][heads][dim] of LBA_TYPE_BF16 or F16 with row stride q_at.token; out as lba_attention's, [sequences][heads][dim].
- * Workspace as for lba_attention_backward. */
+ * q [sequences][heads][dim] of LBA_TYPE_BF16 or F16 with row stride q_at.token; out as lba_attention's, [sequences][heads][dim];
+ * scale finite and > 0.  Workspace as for lba_attention_backward. */
 size_t lba_cache_attention_workspace_bytes(const lba_cache* cache, int heads);
 int lba_cache_attention(const void* q, lba_strides q_at, int type, int heads, const lba_cache* cache, const int32_t* lengths,
                         float scale, int out_type, const float* out_scale, int out_flags, void* out, void* workspace,

@@ -111,6 +111,11 @@ def test_refused_cache_arguments():
     assert _decode(sequences=65535, table_width=1 << 24, page=64, kv_heads=4, heads=4) == -2
 
 
+@pytest.mark.parametrize("scale", [0.0, -0.1, math.inf, math.nan])
+def test_refused_scales_of_cache_attention(scale):
+    assert _decode(scale=scale) == -9
+
+
 def test_binding_refuses_what_is_no_cuda_tensor():
     x, n = torch.zeros(4, 2, 64, dtype=torch.bfloat16), torch.zeros(4, dtype=torch.int32)
     cache, table = torch.zeros(lba.cache_shape(3, 2, 16, 64), dtype=torch.uint8), torch.zeros(4, 1, dtype=torch.int32)
