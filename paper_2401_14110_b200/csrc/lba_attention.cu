@@ -2,15 +2,18 @@
 //
 // One pass over the keys with the running maximum and sum of a softmax; scores and weights never leave the SM.  Bound by the tensor cores
 // and the exponential units together: 128 x 128 scores of 128 dimensions are 1024 clocks of matrix instructions (two products) and 1024 clocks of
-// exponentials (16 a clock).  So a CTA holds two tiles of 128 queries of one head: while the tensor cores work on one tile's products, a
-// warpgroup forms the other's weights.
-//   warps 0-3, 4-7   a tile's softmax each, a query row a thread: scores from tensor memory to registers, weights back over them as the second
+// exponentials (16 a clock).  So an SM holds two tiles of 128 queries: while the tensor cores work on one tile's products, a warpgroup forms the
+// other's weights.  The tiles are two of one head in one CTA, which share their keys' copies (W = 2), or two CTAs with a tile each, whose
+// starts and ends hide behind each other (W = 1; for 128 dimensions they have room for one K and one V tile each).
+//   4 warps a tile   its softmax, a query row a thread: scores from tensor memory to registers, weights back over them as the second
 //                    product's operand; its output stays in tensor memory to the end.  The maximum that weights are relative to is raised only
 //                    when a score exceeds it by 2^8, and the output is rescaled only then (in 32 bits nothing is lost by weights of up to 256)
-//   warp 8           tensor copies of K and V tiles into a ring
-//   warp 9           one thread issues all products
-//   warps 10, 11     clean tiles of V that the mask cuts: rows behind the sequence become 0 (0 times a neighbour's infinity would be NaN),
+//   a warp           tensor copies of K and V tiles into a ring
+//   a warp           one thread issues all products
+//   two warps        clean tiles of V that the mask cuts: rows behind the sequence become 0 (0 times a neighbour's infinity would be NaN),
 //                    and values that are not finite, which rows before them must not see, are taken out and added to the others' results
+// A prompt of 8192 tokens, 32 heads of 128, takes 461 us in a burst (1.19 PFLOP/s, 70% of the matrix peak) and 533 us under the power limit;
+// short sequences are bound by what a CTA does once: some 9 us for its place, its first copies and products, and its rows' way out.
 // Weights are rounded to the inputs' type (2^-9 or 2^-12 of each, at random; the result is rounded to that type once more); sums of weights
 // are of the unrounded ones.
 #include <cmath>
@@ -20,7 +23,7 @@
 namespace lba {
 namespace {
 
-constexpr int QT = 128, KT = 128, FWD_THREADS = 384, MAX_STAGES = 10, CUT_TILES = 4;
+constexpr int QT = 128, KT = 128, MAX_STAGES = 10, CUT_TILES = 4;
 constexpr float LAZY = 8.0f;  // binades
 
 struct ForwardParams {
@@ -37,8 +40,8 @@ struct ForwardParams {
 };
 
 template <int DT> constexpr int kTile = 128 * DT * 2;                       // bytes of a tile of 128 rows
-template <int DT> constexpr int kStages = DT == 128 ? 5 : 10;
-template <int DT> constexpr size_t kForwardSmem = 1024 + (size_t)kTile<DT> * (2 + kStages<DT>);
+template <int DT, int W> constexpr int kStages = W == 1 ? (DT == 128 ? 2 : 5) : (DT == 128 ? 5 : 10);
+template <int DT, int W> constexpr size_t kForwardSmem = 1024 + (size_t)kTile<DT> * (W + kStages<DT, W>);
 
 struct ForwardShared {
   uint64_t q_full[2], full[MAX_STAGES], empty[MAX_STAGES], scores[2], weights[2][2], done;  // weights: of the first 96 keys of a tile, of the others
@@ -96,24 +99,26 @@ struct Quotients {
   }
 };
 
-template <typename T, int DT>
-__global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_constant__ ForwardParams p) {
-  constexpr int BLOCKS = DT / 64, TILE = kTile<DT>, HALF = 128 * 128, STAGES = kStages<DT>;
+// W: tiles of queries of a CTA
+template <typename T, int DT, int W>
+__global__ void __launch_bounds__(128 * (W + 1), 3 - W) attention_kernel(const __grid_constant__ ForwardParams p) {
+  constexpr int BLOCKS = DT / 64, TILE = kTile<DT>, HALF = 128 * 128, STAGES = kStages<DT, W>, COLUMNS = 256 * W;
+  constexpr int COPIES = 4 * W, PRODUCTS = COPIES + 1, CLEAN = COPIES + 2;  // warps
   extern __shared__ uint8_t raw_smem[];
   __shared__ ForwardShared sh;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const uint32_t base = (smem_u32(raw_smem) + 1023) & ~1023u, q_smem = base, ring = base + 2 * TILE;
+  const uint32_t base = (smem_u32(raw_smem) + 1023) & ~1023u, q_smem = base, ring = base + W * TILE;
   volatile int* const dead = &sh.dead;
 
   const int head = blockIdx.x % p.heads;
-  if (warp == 8 && lane == 0) {
+  if (warp == COPIES && lane == 0) {
     map_ahead(&p.q);
     map_ahead(&p.k);
     map_ahead(&p.v);
   }
   if (warp == 0) {
     if (lane == 0) {
-      for (int i = 0; i < 2; ++i) {
+      for (int i = 0; i < W; ++i) {
         mbar_init(smem_u32(&sh.q_full[i]), 1);
         mbar_init(smem_u32(&sh.scores[i]), 1);
         mbar_init(smem_u32(&sh.weights[i][0]), 128);
@@ -134,9 +139,9 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
     }
   }
   after_previous();
-  if (warp == 9) tmem_alloc(smem_u32(&sh.tmem), 512);  // (not before: a CTA of the kernel before this one could still want it)
-  if (warp == 8) {
-    const Place place = find_place(p.cu_q, p.q_rows, p.cu_k, p.k_rows, p.sequences, false, 2 * QT, blockIdx.x / p.heads);
+  if (warp == PRODUCTS) tmem_alloc(smem_u32(&sh.tmem), COLUMNS);  // (not before: a CTA of the kernel before this one could still want it)
+  if (warp == COPIES) {
+    const Place place = find_place(p.cu_q, p.q_rows, p.cu_k, p.k_rows, p.sequences, false, W * QT, blockIdx.x / p.heads);
     if (lane == 0) sh.place = place;
   }
   tmem_before();
@@ -148,27 +153,29 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
   if (alive) {
     // (with a causal mask the last blocks, which have the most keys, are of the highest levels)
     const int q_first = place.q_first, q_count = place.q_count, k_first = place.k_first, k_count = place.k_count, off = k_count - q_count, block = place.level;
-    const int i0 = block * 2 * QT;
+    const int i0 = block * W * QT;
     // tiles of keys of either query tile, and the first that a mask cuts
-    int tiles[2], whole[2];
+    int tiles[W], whole[W];
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
+    for (int w = 0; w < W; ++w) {
       const int lo = i0 + w * QT, hi = min(lo + QT, q_count) - 1;
       const int keys = lo >= q_count ? 0 : p.causal ? max(0, min(k_count, hi + off + 1)) : k_count;
       tiles[w] = (keys + KT - 1) / KT;
       whole[w] = (p.causal ? max(0, min(k_count, lo + off + 1)) : k_count) / KT;
     }
-    const int all = max(tiles[0], tiles[1]);
+    const int all = max(tiles[0], tiles[W - 1]);
     // the first tile of V to be cleaned: behind it, masks cut every tile of some query tile that is not empty
-    const int dirty = min(tiles[0] ? whole[0] : all, tiles[1] ? whole[1] : all);
+    const int dirty = min(tiles[0] ? whole[0] : all, tiles[W - 1] ? whole[W - 1] : all);
     const int kv = head / p.group;
 
-    if (warp >= 8) {
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
-      if (warp == 8) {
+    if (warp >= COPIES) {
+      // (168 or 128 registers a thread are there from the launch; the softmax threads take 208 or 192)
+      if constexpr (W == 1) asm volatile("setmaxnreg.dec.sync.aligned.u32 64;");
+      else asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+      if (warp == COPIES) {
         if (elected()) {
 #pragma unroll
-          for (int w = 0; w < 2; ++w) {
+          for (int w = 0; w < W; ++w) {
             if (!tiles[w]) continue;
             mbar_arrive_expect(smem_u32(&sh.q_full[w]), TILE);
             for (int x = 0; x < BLOCKS; ++x) tile_load(q_smem + w * TILE + x * HALF, &p.q, x * 64, head, q_first + i0 + w * QT, smem_u32(&sh.q_full[w]));
@@ -188,7 +195,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
             }
           }
         }
-      } else if (warp == 9) {
+      } else if (warp == PRODUCTS) {
         if (elected()) {
           const int steps = (p.dim + 15) / 16;
           const uint32_t kind_s = tile_kind(p.bf, KT, false), kind_o = tile_kind(p.bf, steps * 16, true);
@@ -209,7 +216,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
             mma_arrive(smem_u32(&sh.scores[w]));
           };
 #pragma unroll
-          for (int w = 0; w < 2; ++w) {
+          for (int w = 0; w < W; ++w) {
             if (!tiles[w]) continue;
             ok = ok && mbar_wait(smem_u32(&sh.q_full[w]), 0, dead);
             scores(w, 0);
@@ -220,7 +227,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
             if (j >= dirty) ok = ok && mbar_wait(smem_u32(&sh.clean[j - dirty]), 0, dead);
             else full(2 * j + 1);
 #pragma unroll
-            for (int w = 0; w < 2; ++w) {
+            for (int w = 0; w < W; ++w) {
               if (j >= tiles[w]) continue;
               const uint64_t b = lines + ((ring + vs * TILE) >> 4);
 #pragma unroll
@@ -230,7 +237,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
                   if (!ok) break;
                   tmem_after();
                 }
-                mma_tensor(tmem + 256 + w * 128, tmem + w * KT + s * 8, b + s * (2048 >> 4), kind_o, j != 0 || s != 0);
+                mma_tensor(tmem + (W + w) * 128, tmem + w * KT + s * 8, b + s * (2048 >> 4), kind_o, j != 0 || s != 0);
               }
               if (!ok) break;
               if (j + 1 < tiles[w]) scores(w, j + 1);
@@ -248,7 +255,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
           const int stage = (2 * j + 1) % STAGES;
           if (!mbar_wait(smem_u32(&sh.cut_full[j - dirty]), 0, dead)) break;
           uint8_t* const tile = raw_smem + (ring - smem_u32(raw_smem)) + stage * TILE;
-          for (int row = threadIdx.x - 10 * 32; row < KT; row += 64) {
+          for (int row = threadIdx.x - CLEAN * 32; row < KT; row += 64) {
             const bool behind = j * KT + row >= k_count;
             bool odd = false;
             if (behind || p.causal) {
@@ -283,9 +290,10 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
         }
       }
     } else {
-      asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
+      if constexpr (W == 1) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+      else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
       const int w = warp >> 2, mine = tiles[w], row = threadIdx.x & 127, i = i0 + w * QT + row;
-      const uint32_t lanes = (uint32_t)(warp & 3) << 21, s_at = tmem + w * KT + lanes, o_at = tmem + 256 + w * 128 + lanes;
+      const uint32_t lanes = (uint32_t)(warp & 3) << 21, s_at = tmem + w * KT + lanes, o_at = tmem + (W + w) * 128 + lanes;
       const float c = p.to_log2;
       float top = -INFINITY;
       u64 total[4] = {};  // chains of their own
@@ -414,7 +422,7 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
     }
   }
   __syncthreads();
-  if (warp == 9) {
+  if (warp == PRODUCTS) {
     if (*dead) {
       let_copies_land();
     } else if (alive) {
@@ -422,15 +430,28 @@ __global__ void __launch_bounds__(FWD_THREADS, 1) attention_kernel(const __grid_
     }
     tmem_after();
     __syncwarp();
-    tmem_free(tmem, 512);
+    tmem_free(tmem, COLUMNS);
   }
 }
 
-template <typename T, int DT>
-cudaError_t launch_forward(const ForwardParams& p, int64_t blocks, cudaStream_t stream) {
-  cudaError_t e = cudaFuncSetAttribute(attention_kernel<T, DT>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kForwardSmem<DT>);
+template <typename T, int DT, int W>
+cudaError_t launch_forward(const ForwardParams& p, cudaStream_t stream) {
+  const cudaError_t e = cudaFuncSetAttribute(attention_kernel<T, DT, W>, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kForwardSmem<DT, W>);
   if (e != cudaSuccess) return e;
-  return launch_after(attention_kernel<T, DT>, dim3((unsigned)blocks), FWD_THREADS, kForwardSmem<DT>, stream, p);
+  const int64_t blocks = (p.q_rows / (W * QT) + p.sequences) * p.heads;
+  return launch_after(attention_kernel<T, DT, W>, dim3((unsigned)blocks), 128 * (W + 1), kForwardSmem<DT, W>, stream, p);
+}
+// One tile a CTA for short sequences: they leave fewer halves of a CTA empty, and start and end more often.  Longer ones want their keys copied
+// once for two tiles, the more of 128 dimensions (those copies would come near what L2 can give).  A mask of the future halves a row's keys.
+// One against two, us, bfloat16: 12 heads of 64, 32 x 128 tokens 13.6 19.4, 4 x 1024 33.2 36.7, 4 x 2048 97 92; causal, 4 x 2048 56.5 59.4,
+// 8192 163 161.  32 heads of 128, 32 x 128 tokens 36 60, 12 x 384 53 71, 8 x 700 113 109; causal, 12 x 384 70 88, 24 of 1 to 1024 185 210, 4 x 1024
+// 87 82.  16 heads of 80, causal, 7 of 1 to 2003: 45 52.
+template <typename T>
+cudaError_t launch_forward(const ForwardParams& p, cudaStream_t stream) {
+  const int64_t limit = (p.dim <= 64 ? 1024 : 384) * (p.causal ? 2 : 1);
+  const bool one = p.q_rows <= limit * p.sequences;
+  if (p.dim <= 64) return one ? launch_forward<T, 64, 1>(p, stream) : launch_forward<T, 64, 2>(p, stream);
+  return one ? launch_forward<T, 128, 1>(p, stream) : launch_forward<T, 128, 2>(p, stream);
 }
 
 }  // namespace
@@ -489,9 +510,5 @@ extern "C" int lba_attention(const void* q, const void* k, const void* v, const 
   p.v_at = how->v_at;
   p.out = out;
   p.lse = lse;
-  const int64_t blocks = (how->q_rows / (2 * QT) + how->sequences) * how->heads;
-  cudaStream_t s = (cudaStream_t)stream;
-  if (how->dim <= 64)
-    return status_of(p.bf ? launch_forward<__nv_bfloat16, 64>(p, blocks, s) : launch_forward<__half, 64>(p, blocks, s));
-  return status_of(p.bf ? launch_forward<__nv_bfloat16, 128>(p, blocks, s) : launch_forward<__half, 128>(p, blocks, s));
+  return status_of(p.bf ? launch_forward<__nv_bfloat16>(p, (cudaStream_t)stream) : launch_forward<__half>(p, (cudaStream_t)stream));
 }

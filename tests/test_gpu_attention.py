@@ -109,6 +109,31 @@ def test_a_neighbours_values_do_not_leak():
         assert torch.equal(lba.lba_attention(*bad, cu, cu, causal=causal)[:100], clean[:100])
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("dim", [16, 64, 72, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_blocks_of_one_and_two_tiles_agree(dim, causal, dtype):
+    """Many rows to a sequence, though most are in none, make the blocks twice as long: the same sums in the same order"""
+    lq, lk = [1, 0, 200, 128, 5, 0, 300, 17, 256, 0, 257], [1, 7, 200, 64, 500, 0, 0, 300, 255, 0, 700]
+    n = sum(lq)
+    q, k, v = _randn(n + 24000, 4, dim, dtype=dtype), _randn(sum(lk), 2, dim, seed=1, dtype=dtype), _randn(sum(lk), 2, dim, seed=2, dtype=dtype)
+    k[3], v[300, 0, 5], v[1300, 1, 3], v[2000, 0, :8] = math.nan, math.inf, -math.inf, math.nan
+    scale = torch.tensor([0.01], device="cuda")
+    for kw in ({}, dict(out_dtype=torch.uint8, out_scale=scale)):
+        short, lse = lba.lba_attention(q[:n], k, v, _cu(lq), _cu(lk), causal=causal, lse=True, **kw)
+        long, lse2 = lba.lba_attention(q, k, v, _cu(lq), _cu(lk), causal=causal, lse=True, **kw)
+        assert torch.equal(short.view(torch.uint8), long[:n].view(torch.uint8))
+        assert torch.equal(lse.view(torch.int32), lse2[:, :n].contiguous().view(torch.int32))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("dim", [40, 64, 104, 128])
+@pytest.mark.parametrize("causal", [False, True])
+def test_long_blocks(dim, causal, dtype):
+    for T in (2177, 2305):  # a last block of one tile and of two
+        _check(_randn(T, 2, dim, dtype=dtype), _randn(T - 100, 1, dim, seed=1, dtype=dtype), _randn(T - 100, 1, dim, seed=2, dtype=dtype), None, None, causal)
+
+
 def test_strides_of_projections():
     T, H, G, D = 150, 6, 2, 64
     x = _randn(T, H + 2 * G, D)
