@@ -219,7 +219,7 @@ template <int DT> constexpr size_t kGradSmem = 1024 + (size_t)kGradTile<DT> * (2
 struct GradShared {
   uint64_t x_full, full1[Y1_SLOTS], empty1[Y1_SLOTS], full2[Y2_SLOTS], empty2[Y2_SLOTS];
   uint64_t cut1[CUTS], clean1[CUTS], cut2[CUTS], clean2[CUTS];  // copies that a mask cuts, and their cleaning
-  uint64_t t1, t1_read, t2, ds_there, done;
+  uint64_t t1, t1_read, t2[2], ds_there, done;
   uint32_t tmem;
   int dead;
   Place place;
@@ -237,6 +237,9 @@ struct Walk {
 template <typename T, int DT, bool KEYS>
 __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw_smem, uint32_t base, int head, uint32_t tmem) {
   constexpr int BLOCKS = DT / 64, TILE = kGradTile<DT>, BLOCK = 128 * 128;
+  // Tensor memory: T1, T2, acc1, acc2, 128 columns each; where the sums leave room, a second T2, which every other tile has
+  constexpr bool TWO = !KEYS || DT == 64;
+  constexpr int ACC1 = 256, ACC2 = TWO ? 320 : 384, OTHER = TWO ? 256 : 0;
   const int warp = threadIdx.x >> 5;
   const uint32_t ring1 = base + 2 * TILE, ring2 = ring1 + Y1_SLOTS * TILE;
   volatile int* const dead = &sh.dead;
@@ -330,7 +333,7 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
           }
           if (++t2 == walk.last) t2 = walk.first;
           if (!ok) return;
-          product(tmem + 128, base + TILE, ring2 + (n % Y2_SLOTS) * TILE, sh.t2);
+          product(tmem + 128 + (n & 1) * OTHER, base + TILE, ring2 + (n % Y2_SLOTS) * TILE, sh.t2[n & 1]);
           if (!KEYS) mma_arrive(smem_u32(&sh.empty2[n % Y2_SLOTS]));
         };
         if (all && ok) {
@@ -342,6 +345,7 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
             ok = mbar_wait(smem_u32(&sh.t1_read), n & 1, dead);
             tmem_after();
             form1(n + 1);
+            if (TWO && ok) form2(n + 1);
           }
           ok = ok && mbar_wait(smem_u32(&sh.ds_there), n & 1, dead);
           if (!ok) break;
@@ -352,13 +356,14 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
 #pragma unroll
             for (int s = 0; s < YT / 16; ++s) mma_tensor(acc, a + (s >> 2) * YC + (s & 3) * 8, b + s * (2048 >> 4), kind_a, n != 0 || s != 0);
           };
-          add(tmem + 256, tmem + 128, ring1 + (n % Y1_SLOTS) * TILE);
+          const uint32_t of = tmem + 128 + (n & 1) * OTHER;
+          add(tmem + ACC1, of, ring1 + (n % Y1_SLOTS) * TILE);
           mma_arrive(smem_u32(&sh.empty1[n % Y1_SLOTS]));
           if (KEYS) {
-            add(tmem + 384, tmem + 128 + YC / 2, ring2 + (n % Y2_SLOTS) * TILE);
+            add(tmem + ACC2, of + YC / 2, ring2 + (n % Y2_SLOTS) * TILE);
             mma_arrive(smem_u32(&sh.empty2[n % Y2_SLOTS]));
           }
-          if (n + 1 < all) form2(n + 1);
+          if (!TWO && n + 1 < all) form2(n + 1);
         }
         mma_arrive(smem_u32(&sh.done));
       }
@@ -407,7 +412,7 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
 
   asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
   const int w = warp >> 2, thread = threadIdx.x & 127, x = x0 + thread;  // the thread's row of X
-  const uint32_t lanes = (uint32_t)(warp & 3) << 21, t1 = tmem + w * YC + lanes, t2 = t1 + 128;
+  const uint32_t lanes = (uint32_t)(warp & 3) << 21, t1 = tmem + w * YC + lanes;
   const u64 c = both(p.to_log2);
   const int bits = ds_bits(p);
   const float up = power_of_two(bits - P_BITS);  // of ds, beside the 2^8 of p
@@ -478,9 +483,10 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
     };
     if (cut) weights(std::true_type());
     else weights(std::false_type());
-    ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&sh.t2), n & 1, dead));
+    ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&sh.t2[n & 1]), (n >> 1) & 1, dead));
     if (!ok) continue;
     tmem_after();
+    const uint32_t t2 = t1 + 128 + (n & 1) * OTHER;
     uint32_t dp[YC];
 #pragma unroll
     for (int e = 0; e < YC; e += 32) tmem_load32(t2 + e, dp + e);
@@ -530,7 +536,7 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
       uint32_t o[32];
       __syncwarp();
       if (all) {
-        tmem_load32(tmem + 256 + which * 128 + lanes + d, o);
+        tmem_load32(tmem + (which ? ACC2 : ACC1) + lanes + d, o);
         tmem_wait_ld();
       }
       if (!there) continue;
@@ -581,7 +587,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) attention_grad_kernel(const _
       mbar_init(smem_u32(&sh.clean2[i]), 32);
     }
     mbar_init(smem_u32(&sh.t1), 1);
-    mbar_init(smem_u32(&sh.t2), 1);
+    for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&sh.t2[i]), 1);
     mbar_init(smem_u32(&sh.t1_read), 256);
     mbar_init(smem_u32(&sh.ds_there), 256);
     mbar_init_fence();
