@@ -256,33 +256,9 @@ __global__ void __launch_bounds__(128 * (W + 1), 3 - W) attention_kernel(const _
           if (!mbar_wait(smem_u32(&sh.cut_full[j - dirty]), 0, dead)) break;
           uint8_t* const tile = raw_smem + (ring - smem_u32(raw_smem)) + stage * TILE;
           for (int row = threadIdx.x - CLEAN * 32; row < KT; row += 64) {
-            const bool behind = j * KT + row >= k_count;
             bool odd = false;
-            if (behind || p.causal) {
-              for (int x = 0; x < BLOCKS; ++x) {
-#pragma unroll
-                for (int piece = 0; piece < 8; ++piece) {
-                  uint4* const at = reinterpret_cast<uint4*>(tile + x * HALF + swizzled(row, piece));
-                  if (behind) {
-                    *at = make_uint4(0u, 0u, 0u, 0u);
-                  } else {
-                    uint4 v = *at;
-                    uint32_t* const u = &v.x;
-                    constexpr uint32_t EXP = std::is_same<T, __nv_bfloat16>::value ? 0x7F80u : 0x7C00u;
-                    bool here = false;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                      if ((u[e] & EXP) == EXP) u[e] &= 0xFFFF0000u, here = true;
-                      if ((u[e] & (EXP << 16)) == EXP << 16) u[e] &= 0x0000FFFFu, here = true;
-                    }
-                    if (here) {
-                      *at = v;
-                      odd = true;
-                    }
-                  }
-                }
-              }
-            }
+            if (j * KT + row >= k_count) clear_row<BLOCKS>(tile, row);
+            else if (p.causal) odd = keep_finite<T, BLOCKS>(tile, row);
             if (odd) atomicOr(&sh.cut[j - dirty][row >> 5], 1u << (row & 31));
           }
           asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -408,7 +384,8 @@ __global__ void __launch_bounds__(128 * (W + 1), 3 - W) attention_kernel(const _
 #pragma unroll
         for (int r = lane >> 2; r < 32; r += 8) {
           if (r >= rows || col >= p.dim) break;
-          const float4 a = *reinterpret_cast<const float4*>(stage + swizzled(r, 2 * c)), b = *reinterpret_cast<const float4*>(stage + swizzled(r, 2 * c + 1));
+          float4 a = *reinterpret_cast<const float4*>(stage + swizzled(r, 2 * c)), b = *reinterpret_cast<const float4*>(stage + swizzled(r, 2 * c + 1));
+          if (!ok) a = b = make_float4(inv, inv, inv, inv);  // (a late copy of Q could still land here)
           const int64_t at = ((int64_t)(q_first + i - lane + r) * p.heads + head) * p.dim + col;
           if (p.codes) {
             *reinterpret_cast<uint2*>(static_cast<uint8_t*>(p.out) + at) = make_uint2(quotients.codes(a, p.in_m4e3), quotients.codes(b, p.in_m4e3));

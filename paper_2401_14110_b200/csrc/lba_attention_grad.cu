@@ -214,7 +214,6 @@ __device__ __forceinline__ int ds_bits(const GradParams& p) {
 
 // ------------------------------------------------------------------ gradients
 template <int DT> constexpr int kGradTile = 128 * DT * 2;  // bytes of 128 rows
-template <int DT> constexpr size_t kGradSmem = 1024 + (size_t)kGradTile<DT> * (2 + Y1_SLOTS + Y2_SLOTS);
 
 struct GradShared {
   uint64_t x_full, full1[Y1_SLOTS], empty1[Y1_SLOTS], full2[Y2_SLOTS], empty2[Y2_SLOTS];
@@ -223,8 +222,12 @@ struct GradShared {
   uint32_t tmem;
   int dead;
   Place place;
-  alignas(16) float minus[2][YC], delta[2][YC];
+  alignas(16) float minus[2][2][YC], delta[2][2][YC];  // [tile's parity][warpgroup]
 };
+
+template <int DT> constexpr size_t kGradTiles = (size_t)kGradTile<DT> * (2 + Y1_SLOTS + Y2_SLOTS);
+template <int DT> constexpr size_t kGradSmem = kGradTiles<DT> + sizeof(GradShared);
+static_assert(kGradSmem<128> <= 227 * 1024, "shared memory of a CTA");
 
 // what a CTA walks over: tiles first..last - 1 of `heads` heads in turn
 struct Walk {
@@ -368,42 +371,27 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
         mma_arrive(smem_u32(&sh.done));
       }
     } else {
-      // Cut tiles, Y1 one warp, Y2 the other.  Rows behind the sequence become 0 where they are summed over (0 times a neighbour's infinity would be
-      // NaN), and so do values of Y1 that are not finite: rows that see them have an lse that is NaN.
-      const bool second = warp == 11;
+      // Cut tiles.  Rows behind the sequence become 0 where they are summed over (0 times a neighbour's infinity would be NaN), and so do values of Y1
+      // that are not finite: rows that see them have an lse that is NaN.
       int cuts = 0, t = walk.first;
-      for (int n = 0; n < all && (KEYS || !second); ++n) {
+      bool ok = true;
+      const auto clean = [&](uint32_t tile_at, int at_t, bool values, uint64_t& there, uint64_t& clean) {
+        ok = ok && mbar_wait(smem_u32(&there), (cuts / CUTS) & 1, dead);
+        if (!ok) return;
+        uint8_t* const tile = raw_smem + (tile_at - smem_u32(raw_smem));
+        for (int row = threadIdx.x - 10 * 32; row < YT; row += 64) {
+          if (at_t * YT + row >= y_count) clear_row<BLOCKS>(tile, row);
+          else if (values) keep_finite<T, BLOCKS>(tile, row);
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        mbar_arrive(smem_u32(&clean));
+      };
+      for (int n = 0; n < all && ok; ++n) {
         const int at_t = t;
         if (++t == walk.last) t = walk.first;
         if (!walk.cut(at_t)) continue;
-        if (!mbar_wait(smem_u32(second ? &sh.cut2[cuts % CUTS] : &sh.cut1[cuts % CUTS]), (cuts / CUTS) & 1, dead)) break;
-        uint8_t* const tile = raw_smem + ((second ? ring2 + (n % Y2_SLOTS) * TILE : ring1 + (n % Y1_SLOTS) * TILE) - smem_u32(raw_smem));
-        for (int row = threadIdx.x & 31; row < YT; row += 32) {
-          const bool behind = at_t * YT + row >= y_count;
-          if (!behind && (second || !p.causal)) continue;
-          for (int x = 0; x < BLOCKS; ++x) {
-#pragma unroll
-            for (int piece = 0; piece < 8; ++piece) {
-              uint4* const at = reinterpret_cast<uint4*>(tile + x * BLOCK + swizzled(row, piece));
-              if (behind) {
-                *at = make_uint4(0u, 0u, 0u, 0u);
-              } else {
-                uint4 v = *at;
-                uint32_t* const u = &v.x;
-                constexpr uint32_t EXP = std::is_same<T, __nv_bfloat16>::value ? 0x7F80u : 0x7C00u;
-                bool here = false;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                  if ((u[e] & EXP) == EXP) u[e] &= 0xFFFF0000u, here = true;
-                  if ((u[e] & (EXP << 16)) == EXP << 16) u[e] &= 0x0000FFFFu, here = true;
-                }
-                if (here) *at = v;
-              }
-            }
-          }
-        }
-        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-        mbar_arrive(smem_u32(second ? &sh.clean2[cuts % CUTS] : &sh.clean1[cuts % CUTS]));
+        clean(ring1 + (n % Y1_SLOTS) * TILE, at_t, p.causal, sh.cut1[cuts % CUTS], sh.clean1[cuts % CUTS]);
+        if (KEYS) clean(ring2 + (n % Y2_SLOTS) * TILE, at_t, false, sh.cut2[cuts % CUTS], sh.clean2[cuts % CUTS]);
         ++cuts;
       }
     }
@@ -424,19 +412,25 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
     mine = make_float2(0.0f, 0.0f);
     if (n < all && thread < YC && i < y_count) mine = __ldg(p.stats + (int64_t)(head * p.group + h) * p.q_rows + y_first + i);
   };
-  if (KEYS) stats_of(0);
-  else if (x < x_count) mine = __ldg(p.stats + (int64_t)head * p.q_rows + x_first + x);
+  const auto hand_over = [&](int n) {
+    if (thread < YC) {
+      sh.minus[n & 1][w][thread] = P_BITS - mine.x;
+      sh.delta[n & 1][w][thread] = -mine.y * up;
+    }
+    stats_of(n + 1);
+  };
+  if (KEYS) {
+    stats_of(0);
+    hand_over(0);
+  } else if (x < x_count) {
+    mine = __ldg(p.stats + (int64_t)head * p.q_rows + x_first + x);
+  }
   const u64 row_minus = both(P_BITS - mine.x), row_delta = both(-mine.y * up);
   int t = walk.first;
   for (int n = 0; n < all; ++n) {
-    if (KEYS) {  // the columns' statistics; the warpgroup's own, so the barrier is its own too
+    if (KEYS) {  // the columns' statistics; the warpgroup's own, so the barrier is its own too.  Behind it the last tile's are read no more
       asm volatile("bar.sync %0, 128;" ::"r"(1 + w) : "memory");
-      if (thread < YC) {
-        sh.minus[w][thread] = P_BITS - mine.x;
-        sh.delta[w][thread] = -mine.y * up;
-      }
-      asm volatile("bar.sync %0, 128;" ::"r"(1 + w) : "memory");
-      stats_of(n + 1);
+      hand_over(n + 1);
     }
     const int at_t = t;
     if (++t == walk.last) t = walk.first;
@@ -464,7 +458,7 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
     const auto weights = [&](auto masked) {  // (a test per element, even of a value that is the same for all, doubled the instructions)
 #pragma unroll
       for (int e = 0; e < YC; e += 4) {
-        const float4 m = KEYS ? *reinterpret_cast<const float4*>(&sh.minus[w][e]) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        const float4 m = KEYS ? *reinterpret_cast<const float4*>(&sh.minus[n & 1][w][e]) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
 #pragma unroll
         for (int f = 0; f < 4; f += 2) {
           float p0, p1;
@@ -487,35 +481,37 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
     if (!ok) continue;
     tmem_after();
     const uint32_t t2 = t1 + 128 + (n & 1) * OTHER;
-    uint32_t dp[YC];
-#pragma unroll
-    for (int e = 0; e < YC; e += 32) tmem_load32(t2 + e, dp + e);
-    tmem_wait_ld();
+    // the upper half first: p goes over it while the lower one is formed
+    uint32_t dw[YC / 2];
     const auto slopes = [&](auto masked) {
 #pragma unroll
-      for (int half = 0; half < YC; half += 32) {
-        uint32_t dw[16];
+      for (int half = YC - 32; half >= 0; half -= 32) {
+        uint32_t dp[32];
+        tmem_load32(t2 + half, dp);
+        float4 m[KEYS ? 8 : 1];
+        if (KEYS) {
 #pragma unroll
-        for (int e = half; e < half + 32; e += 4) {
-          const float4 m = KEYS ? *reinterpret_cast<const float4*>(&sh.delta[w][e]) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-#pragma unroll
-          for (int f = 0; f < 4; f += 2) {
-            float d0, d1;
-            unpack2(mul2_rn(fma2_rn(pack2u(dp[e + f], dp[e + f + 1]), up2, KEYS ? (f ? pack2(m.z, m.w) : pack2(m.x, m.y)) : row_delta),
-                            pack2u(s[e + f], s[e + f + 1])), d0, d1);
-            if constexpr (decltype(masked)::value) {  // (0 times what a mask hides may be NaN)
-              if (e + f < lo || e + f >= hi) d0 = 0.0f;
-              if (e + f + 1 < lo || e + f + 1 >= hi) d1 = 0.0f;
-            }
-            dw[(e + f - half) / 2] = pack_pair<T>(d0, d1);
-          }
+          for (int e = 0; e < 8; ++e) m[e] = *reinterpret_cast<const float4*>(&sh.delta[n & 1][w][half + 4 * e]);
         }
-        tmem_st16(t2 + half / 2, dw);
+        tmem_wait_ld();
+        if (KEYS && half) tmem_store32(t2 + YC / 2, pw);
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+          const float4& four = m[KEYS ? e / 4 : 0];
+          float d0, d1;
+          unpack2(mul2_rn(fma2_rn(pack2u(dp[e], dp[e + 1]), up2, KEYS ? (e & 2 ? pack2(four.z, four.w) : pack2(four.x, four.y)) : row_delta),
+                          pack2u(s[half + e], s[half + e + 1])), d0, d1);
+          if constexpr (decltype(masked)::value) {  // (0 times what a mask hides may be NaN)
+            if (half + e < lo || half + e >= hi) d0 = 0.0f;
+            if (half + e + 1 < lo || half + e + 1 >= hi) d1 = 0.0f;
+          }
+          dw[(half + e) / 2] = pack_pair<T>(d0, d1);
+        }
       }
     };
     if (cut) slopes(std::true_type());
     else slopes(std::false_type());
-    if constexpr (KEYS) tmem_store32(t2 + YC / 2, pw);
+    tmem_store32(t2, dw);
     tmem_wait_st();
     tmem_before();
     mbar_arrive(smem_u32(&sh.ds_there));
@@ -523,35 +519,42 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
   // both warpgroups bring the sums out, each half of the columns
   ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&sh.done), 0, dead)) && ok && !*dead;
   tmem_after();
-  const bool there = x < x_count;
-  const int out_heads = KEYS ? p.kv_heads : p.heads;
-  const int64_t at = ((int64_t)(x_first + x) * out_heads + head) * p.dim;
+  const int lane = threadIdx.x & 31, out_heads = KEYS ? p.kv_heads : p.heads, there = min(32, x_count - (x - lane));  // rows of the warp
   const float by1 = p.scale * power_of_two(-bits), by2 = 1.0f / P_UP;
+  // 32 values a row at a time, through shared memory (X is no longer read), four lanes a row side by side
+  uint8_t* const stage = raw_smem + (base - smem_u32(raw_smem)) + warp * 2048;
+  const auto piece_of = [&](int r, int c) { return reinterpret_cast<uint4*>(stage + r * 64 + ((c ^ ((r >> 1) & 3)) << 4)); };
 #pragma unroll 1
   for (int which = 0; which < (KEYS ? 2 : 1); ++which) {
-    T* const dst = static_cast<T*>(KEYS ? (which ? p.grad_v : p.grad_k) : p.grad_q) + at;
+    T* const dst = static_cast<T*>(KEYS ? (which ? p.grad_v : p.grad_k) : p.grad_q);
     const float by = which ? by2 : by1;
 #pragma unroll 1
     for (int d = w * (DT / 2); d < (w + 1) * (DT / 2) && d < p.dim; d += 32) {
       uint32_t o[32];
-      __syncwarp();
       if (all) {
         tmem_load32(tmem + (which ? ACC2 : ACC1) + lanes + d, o);
         tmem_wait_ld();
-      }
-      if (!there) continue;
+      } else {
 #pragma unroll
-      for (int e = 0; e < 32; e += 8) {
-        if (d + e >= p.dim) break;
+        for (int e = 0; e < 32; ++e) o[e] = 0u;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
         uint32_t v[4];
 #pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          float lo = all ? __uint_as_float(o[e + 2 * u]) * by : 0.0f, hi = all ? __uint_as_float(o[e + 2 * u + 1]) * by : 0.0f;
-          if (!ok) lo = hi = __uint_as_float(0x7FC00000u);
-          v[u] = pack_pair<T>(lo, hi);
-        }
-        *reinterpret_cast<uint4*>(dst + d + e) = make_uint4(v[0], v[1], v[2], v[3]);
+        for (int u = 0; u < 4; ++u) v[u] = pack_pair<T>(__uint_as_float(o[8 * e + 2 * u]) * by, __uint_as_float(o[8 * e + 2 * u + 1]) * by);
+        *piece_of(lane, e) = make_uint4(v[0], v[1], v[2], v[3]);
       }
+      __syncwarp();
+      const int c = lane & 3;
+#pragma unroll
+      for (int r = lane >> 2; r < 32; r += 8) {
+        if (r >= there || d + c * 8 >= p.dim) break;
+        uint4 v = *piece_of(r, c);
+        if (!ok) v = make_uint4(0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu, 0x7FFF7FFFu);  // NaN
+        *reinterpret_cast<uint4*>(dst + ((int64_t)(x_first + x - lane + r) * out_heads + head) * p.dim + d + c * 8) = v;
+      }
+      __syncwarp();
     }
   }
   tmem_before();
@@ -559,10 +562,10 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
 
 template <typename T, int DT>
 __global__ void __launch_bounds__(GRAD_THREADS, 1) attention_grad_kernel(const __grid_constant__ GradParams p) {
-  extern __shared__ uint8_t raw_smem[];
-  __shared__ GradShared sh;
+  extern __shared__ __align__(1024) uint8_t raw_smem[];  // (1024: the swizzle's period.  There is no room to find a boundary in)
+  GradShared& sh = *reinterpret_cast<GradShared*>(raw_smem + kGradTiles<DT>);
   const int warp = threadIdx.x >> 5;
-  const uint32_t base = (smem_u32(raw_smem) + 1023) & ~1023u;
+  const uint32_t base = smem_u32(raw_smem);
   if (threadIdx.x == 8 * 32) {
     map_ahead(&p.q);
     map_ahead(&p.k);
@@ -583,8 +586,8 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) attention_grad_kernel(const _
     for (int i = 0; i < CUTS; ++i) {
       mbar_init(smem_u32(&sh.cut1[i]), 1);
       mbar_init(smem_u32(&sh.cut2[i]), 1);
-      mbar_init(smem_u32(&sh.clean1[i]), 32);
-      mbar_init(smem_u32(&sh.clean2[i]), 32);
+      mbar_init(smem_u32(&sh.clean1[i]), 64);
+      mbar_init(smem_u32(&sh.clean2[i]), 64);
     }
     mbar_init(smem_u32(&sh.t1), 1);
     for (int i = 0; i < 2; ++i) mbar_init(smem_u32(&sh.t2[i]), 1);

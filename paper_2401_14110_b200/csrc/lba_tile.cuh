@@ -95,6 +95,44 @@ inline bool head_map(CUtensorMap* map, bool bf, const void* base, int64_t rows, 
                 CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
+// A tile's row: to 0; or rid of values that are not finite, true if it had any.  (A line's eight loads come first, then a sum that carries into a sign
+// bit from exponents of ones only: with loads and tests in turn a tile took one warp 5000 clocks.)
+template <int BLOCKS>
+__device__ __forceinline__ void clear_row(uint8_t* tile, int row) {
+#pragma unroll
+  for (int x = 0; x < BLOCKS; ++x)
+#pragma unroll
+    for (int piece = 0; piece < 8; ++piece) *reinterpret_cast<uint4*>(tile + x * 128 * 128 + swizzled(row, piece)) = make_uint4(0u, 0u, 0u, 0u);
+}
+template <typename T, int BLOCKS>
+__device__ __forceinline__ bool keep_finite(uint8_t* tile, int row) {
+  constexpr uint32_t EXP = std::is_same<T, __nv_bfloat16>::value ? 0x7F807F80u : 0x7C007C00u, ONE = std::is_same<T, __nv_bfloat16>::value ? 0x00800080u : 0x04000400u;
+  constexpr uint32_t SIGNS = 0x80008000u;
+  bool any = false;
+#pragma unroll 1
+  for (int x = 0; x < BLOCKS; ++x) {
+    uint4 v[8];
+#pragma unroll
+    for (int piece = 0; piece < 8; ++piece) v[piece] = *reinterpret_cast<const uint4*>(tile + x * 128 * 128 + swizzled(row, piece));
+    uint32_t here = 0;
+#pragma unroll
+    for (int piece = 0; piece < 8; ++piece)
+      here |= ((v[piece].x & EXP) + ONE) | ((v[piece].y & EXP) + ONE) | ((v[piece].z & EXP) + ONE) | ((v[piece].w & EXP) + ONE);
+    if (!(here & SIGNS)) continue;
+    any = true;
+#pragma unroll 1
+    for (int piece = 0; piece < 8; ++piece) {
+      uint32_t* const u = reinterpret_cast<uint32_t*>(tile + x * 128 * 128 + swizzled(row, piece));
+#pragma unroll 1
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t bad = ((u[e] & EXP) + ONE) & SIGNS;  // a value's sign bit, where all of the value goes
+        u[e] &= ~(bad | (bad - (bad >> 15)));
+      }
+    }
+  }
+  return any;
+}
+
 // ------------------------------------------------------------------ packed sequences
 // the rows of sequence b: from first on, `count` of them
 __device__ __forceinline__ void rows_of(const int32_t* cu, int64_t rows, int b, int* first, int* count) {
