@@ -265,7 +265,7 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
     walk.last = (max(0, min(y_count, min(x0 + XT, x_count) + off)) + YT - 1) / YT;
     walk.high = min(walk.high, max(0, x0 + off + 1) / YT);
   }
-  const int tiles = max(0, walk.last - walk.first), all = walk.count();
+  const int all = walk.count();
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
@@ -407,20 +407,25 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
   const u64 up2 = both(up);
   bool ok = true;
   float2 mine = make_float2(0.0f, 0.0f);  // queries: this row's; keys: a column's of the next tile
-  const auto stats_of = [&](int n) {
-    const int h = n / max(tiles, 1), i = (walk.first + n - h * tiles) * YT + w * YC + thread;
+  int h_ahead = 0, t_ahead = walk.first;  // of the next tile whose statistics are fetched
+  const auto stats_ahead = [&] {
+    const int i = t_ahead * YT + w * YC + thread;
     mine = make_float2(0.0f, 0.0f);
-    if (n < all && thread < YC && i < y_count) mine = __ldg(p.stats + (int64_t)(head * p.group + h) * p.q_rows + y_first + i);
+    if (h_ahead < walk.heads && thread < YC && i < y_count) mine = __ldg(p.stats + (int64_t)(head * p.group + h_ahead) * p.q_rows + y_first + i);
+    if (++t_ahead >= walk.last) {
+      t_ahead = walk.first;
+      ++h_ahead;
+    }
   };
   const auto hand_over = [&](int n) {
     if (thread < YC) {
       sh.minus[n & 1][w][thread] = P_BITS - mine.x;
       sh.delta[n & 1][w][thread] = -mine.y * up;
     }
-    stats_of(n + 1);
+    stats_ahead();
   };
   if (KEYS) {
-    stats_of(0);
+    stats_ahead();
     hand_over(0);
   } else if (x < x_count) {
     mine = __ldg(p.stats + (int64_t)head * p.q_rows + x_first + x);
@@ -428,14 +433,9 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
   const u64 row_minus = both(P_BITS - mine.x), row_delta = both(-mine.y * up);
   int t = walk.first;
   for (int n = 0; n < all; ++n) {
-    if (KEYS) {  // the columns' statistics; the warpgroup's own, so the barrier is its own too.  Behind it the last tile's are read no more
-      asm volatile("bar.sync %0, 128;" ::"r"(1 + w) : "memory");
-      hand_over(n + 1);
-    }
     const int at_t = t;
     if (++t == walk.last) t = walk.first;
     ok = ok && __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&sh.t1), n & 1, dead));
-    if (!ok) continue;  // (the warpgroup's other warps wait at its barrier)
     tmem_after();
     int lo = 0, hi = YC;  // of the warpgroup's columns, those that the row goes with
     const bool cut = walk.cut(at_t);
@@ -449,11 +449,17 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
       }
     }
     uint32_t s[YC];  // scores, then weights
+    if (ok) {
 #pragma unroll
-    for (int e = 0; e < YC; e += 32) tmem_load32(t1 + e, s + e);
-    tmem_wait_ld();
-    tmem_before();
-    mbar_arrive(smem_u32(&sh.t1_read));
+      for (int e = 0; e < YC; e += 32) tmem_load32(t1 + e, s + e);
+      tmem_wait_ld();
+      tmem_before();
+      mbar_arrive(smem_u32(&sh.t1_read));
+    }
+    // The columns' statistics are there, and those of the last tile are read no more.  The warpgroup's own, so the barrier is its own too; warps whose
+    // wait ran out meet the others here all the same.
+    if (KEYS) asm volatile("bar.sync %0, 128;" ::"r"(1 + w) : "memory");
+    if (!ok) continue;
     uint32_t pw[KEYS ? YC / 2 : 1];
     const auto weights = [&](auto masked) {  // (a test per element, even of a value that is the same for all, doubled the instructions)
 #pragma unroll
@@ -477,6 +483,7 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
     };
     if (cut) weights(std::true_type());
     else weights(std::false_type());
+    if (KEYS) hand_over(n + 1);
     ok = __all_sync(0xFFFFFFFFu, mbar_wait(smem_u32(&sh.t2[n & 1]), (n >> 1) & 1, dead));
     if (!ok) continue;
     tmem_after();
