@@ -13,9 +13,11 @@
 // 32-bit gradient of q goes through memory or atomics.
 //
 // Bound by the matrix instructions, 512 clocks each (four for keys, three for queries), and by the 1024 clocks of exponentials and what goes
-// with them.  p waits in registers until T2 has been read: so T1(n+1) is formed as soon as T1(n) is in registers, and scores are there before the
-// warpgroups want them; acc1(n), acc2(n) and T2(n+1) follow while they form p of tile n+1.  (With p over T1, T1(n+1) came after acc2(n): 3500
-// clocks a tile.  With p in shared memory there is room for two tiles of Y1 only, and their copies came late: 4200.)
+// with them, which they hide only in part: 2600 clocks a tile for keys, 2100 for queries.  p waits in registers until T2 has been read: so T1(n+1) is formed
+// as soon as T1(n) is in registers, and scores are there before the warpgroups want them.  Where the sums leave room in tensor memory (queries; heads
+// of up to 64) there is a second T2, and T2(n+1) is formed ahead too; else it follows acc1(n) and acc2(n) while the warpgroups form p of tile n+1.  (With
+// p over T1, T1(n+1) came after acc2(n): 3500 clocks a tile.  With p in shared memory there is room for two tiles of Y1 only, and their copies came late: 4200.)
+// 2 x 4096 tokens, 16 heads and 4 key-value heads of 128, causal, both launches: 397 us, 0.87 PFLOP/s of the five products.
 // (Tiles of 64 rows, two of them in flight, a warpgroup each: with 64 columns a product wants 192 bytes of shared memory a clock, or 128 of
 // tensor memory, and took 57 clocks a step instead of 32; 2 x 4096 tokens of 16 heads took 515 us.)
 //
@@ -49,7 +51,8 @@ struct DeltaParams {
   lba_strides q_at, k_at, v_at;
   const float* lse;
   const int32_t *cu_q, *cu_k;
-  int64_t q_rows, k_rows, row_blocks;
+  int64_t q_rows, k_rows;
+  uint32_t few_blocks;       // of rows of few keys
   int sequences, heads, kv_heads, dim, causal;
   float to_log2;
   float2* stats;
@@ -58,7 +61,8 @@ struct DeltaParams {
 };
 
 // ------------------------------------------------------------------ delta
-// A warp takes eight heads of a row, 16 lanes each, all on their way at once.  Rows of no sequence get gradients of 0.
+// A warp takes 8 or 16 heads of a row, 16 lanes each, or 8 where a head has up to 64 values; they and the sequences' ends are on their way at once.  Rows
+// of no sequence get gradients of 0.
 constexpr int FEW_KEYS = 32, DELTA_AHEAD = 4;
 template <typename T>
 __device__ __forceinline__ void widen8(const T* src, float (&v)[8]) {  // at a 16-byte boundary
@@ -72,97 +76,136 @@ __device__ __forceinline__ void load_half8(const T* src, float (&v)[8]) {
   const uint4 raw = __ldg(reinterpret_cast<const uint4*>(src));
   widen8(reinterpret_cast<const T*>(&raw), v);
 }
-// The rows of a sequence that see few keys, for one head: sum p dp / sum p.  The keys and values lie in shared memory; a warp a row, a key a lane.
+// The rows of a sequence that see few keys, for one head: sum p dp / sum p.  Keys, values and 8 rows at a time lie in shared memory; a warp a row, a key
+// a lane.  Four blocks share the rows, and come before the others.  (One block behind them, with rows read as they were wanted, kept 2 x 4096 rows of
+// 16 heads at 31 us instead of 19.)
+constexpr int FEW_ROWS = DELTA_THREADS / 32, FEW_PARTS = 4, FEW_PITCH = 128 / 8 + 1;  // pieces of 16 bytes from row to row: lanes' pieces lie in different banks
+struct FewShared {
+  uint4 k[FEW_KEYS * FEW_PITCH], v[FEW_KEYS * FEW_PITCH], q[FEW_ROWS * FEW_PITCH], g[FEW_ROWS * FEW_PITCH];
+  float lse[FEW_ROWS];
+};
 template <typename T>
-__device__ void delta_of_few(const DeltaParams& p, int b, int h, uint4* shared) {
-  constexpr int PITCH = 128 / 8 + 1;  // pieces of 16 bytes from key to key: lanes' pieces lie in different banks
+__device__ void delta_of_few(const DeltaParams& p, int b, int h, int part, FewShared& sh) {
   int q_first, q_count, k_first, k_count;
   rows_of(p.cu_q, p.q_rows, b, &q_first, &q_count);
   rows_of(p.cu_k, p.k_rows, b, &k_first, &k_count);
   const int off = k_count - q_count, lane = threadIdx.x & 31, pieces = p.dim / 8;
-  const int first = p.causal ? max(0, -off) : 0, last = p.causal ? min(q_count, FEW_KEYS - off) : k_count <= FEW_KEYS ? q_count : 0;
+  const int first = (p.causal ? max(0, -off) : 0) + part * FEW_ROWS, last = p.causal ? min(q_count, FEW_KEYS - off) : k_count <= FEW_KEYS ? q_count : 0;
   const int most = min(k_count, FEW_KEYS);
   if (first >= last || most == 0) return;
   const int kv = h / (p.heads / p.kv_heads);
-  uint4 *const ks = shared, *const vs = shared + FEW_KEYS * PITCH;
-  for (int i = threadIdx.x; i < most * pieces; i += DELTA_THREADS) {
-    const int j = i / pieces, c = i - j * pieces;
-    ks[j * PITCH + c] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(p.k) + (int64_t)(k_first + j) * p.k_at.token + kv * p.k_at.head) + c);
-    vs[j * PITCH + c] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(p.v) + (int64_t)(k_first + j) * p.v_at.token + kv * p.v_at.head) + c);
-  }
-  __syncthreads();
-  for (int i = first + (threadIdx.x >> 5); i < last; i += DELTA_THREADS / 32) {
-    const int keys = p.causal ? min(k_count, i + off + 1) : k_count;
-    const int64_t row = q_first + i;
-    const T *const q = static_cast<const T*>(p.q) + row * p.q_at.token + h * p.q_at.head, *const g = static_cast<const T*>(p.g) + (row * p.heads + h) * p.dim;
-    const float lse = p.lse[h * p.q_rows + row];
-    const int mine = min(lane, most - 1) * PITCH;
-    float s = 0.0f, dp = 0.0f;
-#pragma unroll 4
-    for (int c = 0; c < pieces; ++c) {
-      float a[8], x[8];
-      load_half8(q + c * 8, a);
-      widen8(reinterpret_cast<const T*>(ks + mine + c), x);
-#pragma unroll
-      for (int f = 0; f < 8; ++f) s = fmaf(a[f], x[f], s);
-      load_half8(g + c * 8, a);
-      widen8(reinterpret_cast<const T*>(vs + mine + c), x);
-#pragma unroll
-      for (int f = 0; f < 8; ++f) dp = fmaf(a[f], x[f], dp);
+  const auto bring = [&](uint4* to, const void* from, int64_t row, int rows, int head, const lba_strides& at) {
+    for (int i = threadIdx.x; i < rows * pieces; i += DELTA_THREADS) {
+      const int j = i / pieces, c = i - j * pieces;
+      to[j * FEW_PITCH + c] = __ldg(reinterpret_cast<const uint4*>(static_cast<const T*>(from) + (row + j) * at.token + head * at.head) + c);
     }
-    float weight = lane < keys ? exp2_approx(fmaf(s, p.to_log2, -lse * LOG2E)) : 0.0f, sum = lane < keys ? weight * dp : 0.0f;
-#pragma unroll
-    for (int x = 16; x > 0; x /= 2) {
-      sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
-      weight += __shfl_xor_sync(0xFFFFFFFFu, weight, x);
+  };
+  const lba_strides g_at = {(int64_t)p.heads * p.dim, p.dim};
+  for (int i0 = first; i0 < last; i0 += FEW_PARTS * FEW_ROWS) {
+    const int rows = min(FEW_ROWS, last - i0), i = threadIdx.x >> 5;
+    const int64_t row0 = q_first + i0;
+    if (i0 == first) {
+      bring(sh.k, p.k, k_first, most, kv, p.k_at);
+      bring(sh.v, p.v, k_first, most, kv, p.v_at);
+    } else {
+      __syncthreads();  // (the rows before are no longer read)
     }
-    if (lane == 0) p.stats[h * p.q_rows + row] = make_float2(lse * LOG2E, __fdividef(sum, weight));  // (weights add up to 1, but for rounding)
+    bring(sh.q, p.q, row0, rows, h, p.q_at);
+    bring(sh.g, p.g, row0, rows, h, g_at);
+    if (threadIdx.x < rows) sh.lse[threadIdx.x] = __ldg(p.lse + h * p.q_rows + row0 + threadIdx.x);
+    __syncthreads();
+    if (i < rows) {
+      const int keys = p.causal ? min(k_count, i0 + i + off + 1) : k_count, mine = min(lane, most - 1) * FEW_PITCH;
+      const float lse = sh.lse[i];
+      float s = 0.0f, dp = 0.0f;
+#pragma unroll 2
+      for (int c = 0; c < pieces; ++c) {
+        float a[8], x[8];
+        widen8(reinterpret_cast<const T*>(sh.q + i * FEW_PITCH + c), a);
+        widen8(reinterpret_cast<const T*>(sh.k + mine + c), x);
+#pragma unroll
+        for (int f = 0; f < 8; ++f) s = fmaf(a[f], x[f], s);
+        widen8(reinterpret_cast<const T*>(sh.g + i * FEW_PITCH + c), a);
+        widen8(reinterpret_cast<const T*>(sh.v + mine + c), x);
+#pragma unroll
+        for (int f = 0; f < 8; ++f) dp = fmaf(a[f], x[f], dp);
+      }
+      float weight = lane < keys ? exp2_approx(fmaf(s, p.to_log2, -lse * LOG2E)) : 0.0f, sum = lane < keys ? weight * dp : 0.0f;
+#pragma unroll
+      for (int x = 16; x > 0; x /= 2) {
+        sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
+        weight += __shfl_xor_sync(0xFFFFFFFFu, weight, x);
+      }
+      if (lane == 0) p.stats[h * p.q_rows + row0 + i] = make_float2(lse * LOG2E, __fdividef(sum, weight));  // (weights add up to 1, but for rounding)
+    }
   }
 }
 
-template <typename T>
+// Of `row`'s sequence, the last that begins at or before it, the first row in q and the counts; false for rows of no sequence
+__device__ __forceinline__ bool ends_of(const DeltaParams& p, int64_t row, int lane, int* q_first, int* q_count, int* k_count) {
+  int b = 0, k_first;
+  if (p.cu_q && p.sequences < 32) {  // one trip to memory
+    const int at = min(lane, p.sequences), q = __ldg(p.cu_q + at), k = p.cu_k ? __ldg(p.cu_k + at) : 0;
+    b = __popc(__ballot_sync(0xFFFFFFFFu, lane < p.sequences && q <= row)) - 1;
+    const bool inside = b >= 0 && row < __shfl_sync(0xFFFFFFFFu, q, p.sequences);
+    b = max(b, 0);
+    const int q_top = (int)p.q_rows, k_top = (int)p.k_rows;
+    *q_first = min(max(__shfl_sync(0xFFFFFFFFu, q, b), 0), q_top);
+    *q_count = max(min(max(__shfl_sync(0xFFFFFFFFu, q, b + 1), 0), q_top) - *q_first, 0);
+    const int lo = min(max(__shfl_sync(0xFFFFFFFFu, k, b), 0), k_top), hi = min(max(__shfl_sync(0xFFFFFFFFu, k, b + 1), 0), k_top);
+    *k_count = p.cu_k ? max(hi - lo, 0) : k_top;
+    return inside;
+  }
+  bool inside = true;
+  if (p.cu_q) {
+    inside = row >= p.cu_q[0] && row < p.cu_q[p.sequences];
+    int hi = p.sequences - 1;
+    while (b < hi) {
+      const int mid = (b + hi + 1) / 2;
+      if (p.cu_q[mid] <= row) b = mid;
+      else hi = mid - 1;
+    }
+  }
+  rows_of(p.cu_q, p.q_rows, b, q_first, q_count);
+  rows_of(p.cu_k, p.k_rows, b, &k_first, k_count);
+  return inside;
+}
+
+template <typename T, int LANES>  // of a head
 __global__ void __launch_bounds__(DELTA_THREADS, 5) attention_delta_kernel(const DeltaParams p) {
-  __shared__ uint4 shared[2 * FEW_KEYS * (128 / 8 + 1)];
+  constexpr int HEADS = 32 / LANES;  // at a time
+  __shared__ FewShared few;
   after_previous();
-  if ((int64_t)blockIdx.x >= p.row_blocks) {
-    const int64_t i = blockIdx.x - p.row_blocks;
-    if (blockIdx.y == 0) delta_of_few<T>(p, (int)(i / p.heads), (int)(i % p.heads), shared);
+  if (blockIdx.x < p.few_blocks) {
+    const uint32_t line = blockIdx.x / FEW_PARTS;
+    if (blockIdx.y == 0) delta_of_few<T>(p, (int)(line / p.heads), (int)(line % p.heads), blockIdx.x % FEW_PARTS, few);
     return;
   }
-  const int lane = threadIdx.x & 31, d = (lane & 15) * 8;
-  const int64_t row = (int64_t)blockIdx.x * (DELTA_THREADS / 32) + (threadIdx.x >> 5);
+  const int lane = threadIdx.x & 31, d = lane % LANES * 8, h0 = blockIdx.y * DELTA_AHEAD * HEADS + lane / LANES;
+  const int64_t row = (int64_t)(blockIdx.x - p.few_blocks) * (DELTA_THREADS / 32) + (threadIdx.x >> 5);
   uint32_t most_g = 0, most_v = 0;
-  const T* const g_row = static_cast<const T*>(p.g) + row * p.heads * p.dim;
-  if (row < p.q_rows && p.cu_q && (row < p.cu_q[0] || row >= p.cu_q[p.sequences])) {
-    for (int i = (blockIdx.y * 32 + lane) * 8; i < p.heads * p.dim; i += gridDim.y * 256) *reinterpret_cast<uint4*>(static_cast<T*>(p.grad_q) + row * p.heads * p.dim + i) = make_uint4(0u, 0u, 0u, 0u);
-  } else if (row < p.q_rows) {
-    const T* const o_row = static_cast<const T*>(p.out) + row * p.heads * p.dim;
+  if (row < p.q_rows) {
+    const T *const g_row = static_cast<const T*>(p.g) + row * p.heads * p.dim, *const o_row = static_cast<const T*>(p.out) + row * p.heads * p.dim;
     uint4 g[DELTA_AHEAD], o[DELTA_AHEAD];
     float lse[DELTA_AHEAD];
 #pragma unroll
     for (int u = 0; u < DELTA_AHEAD; ++u) {
-      const int h = (blockIdx.y * DELTA_AHEAD + u) * 2 + (lane >> 4);
+      const int h = h0 + u * HEADS;
       const bool there = h < p.heads && d < p.dim;
       g[u] = there ? __ldg(reinterpret_cast<const uint4*>(g_row + h * p.dim + d)) : make_uint4(0u, 0u, 0u, 0u);
       o[u] = there ? __ldg(reinterpret_cast<const uint4*>(o_row + h * p.dim + d)) : make_uint4(0u, 0u, 0u, 0u);
       lse[u] = h < p.heads ? __ldg(p.lse + h * p.q_rows + row) : 0.0f;
     }
-    int b = 0;  // the last sequence that begins at or before the row
-    if (p.cu_q) {
-      int hi = p.sequences - 1;
-      while (b < hi) {
-        const int mid = (b + hi + 1) / 2;
-        if (p.cu_q[mid] <= row) b = mid;
-        else hi = mid - 1;
-      }
-    }
-    int q_first, q_count, k_first, k_count;
-    rows_of(p.cu_q, p.q_rows, b, &q_first, &q_count);
-    rows_of(p.cu_k, p.k_rows, b, &k_first, &k_count);
+    int q_first, q_count, k_count;
+    const bool inside = ends_of(p, row, lane, &q_first, &q_count, &k_count);
     const int keys = p.causal ? min(k_count, (int)row - q_first + k_count - q_count + 1) : k_count;
 #pragma unroll
     for (int u = 0; u < DELTA_AHEAD; ++u) {
-      const int h = (blockIdx.y * DELTA_AHEAD + u) * 2 + (lane >> 4);
+      const int h = h0 + u * HEADS;
+      if (!inside) {
+        if (h < p.heads && d < p.dim) *reinterpret_cast<uint4*>(static_cast<T*>(p.grad_q) + (row * p.heads + h) * p.dim + d) = make_uint4(0u, 0u, 0u, 0u);
+        continue;
+      }
       float x[8], y[8], sum = 0.0f;
       widen8(reinterpret_cast<const T*>(&g[u]), x);
       widen8(reinterpret_cast<const T*>(&o[u]), y);
@@ -172,8 +215,8 @@ __global__ void __launch_bounds__(DELTA_THREADS, 5) attention_delta_kernel(const
         most_g = max(most_g, __float_as_uint(x[e]) & 0x7FFFFFFFu);
       }
 #pragma unroll
-      for (int e = 8; e > 0; e /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, e);
-      if ((lane & 15) == 0 && h < p.heads && !(keys > 0 && keys <= FEW_KEYS))
+      for (int e = LANES / 2; e > 0; e /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, e);
+      if (d == 0 && h < p.heads && !(keys > 0 && keys <= FEW_KEYS))
         p.stats[h * p.q_rows + row] = make_float2(lse[u] == -INFINITY ? INFINITY : lse[u] * LOG2E, sum);
     }
   }
@@ -185,7 +228,7 @@ __global__ void __launch_bounds__(DELTA_THREADS, 5) attention_delta_kernel(const
         *reinterpret_cast<uint4*>(static_cast<T*>(p.grad_v) + row * n + i) = make_uint4(0u, 0u, 0u, 0u);
       }
     } else if (p.most) {
-      for (int h = lane >> 4; h < p.kv_heads; h += 2) {
+      for (int h = lane / LANES; h < p.kv_heads; h += HEADS) {
         if (d >= p.dim) continue;
         float v[8];
         load_half8(static_cast<const T*>(p.v) + row * p.v_at.token + h * p.v_at.head + d, v);
@@ -638,6 +681,12 @@ cudaError_t launch_grad(const GradParams& p, int64_t blocks, cudaStream_t stream
   return launch_after(attention_grad_kernel<T, DT>, dim3((unsigned)blocks), GRAD_THREADS, kGradSmem<DT>, stream, p);
 }
 
+template <typename T, int LANES>
+cudaError_t launch_delta(const DeltaParams& d, int64_t blocks, cudaStream_t stream) {
+  constexpr int HEADS = DELTA_AHEAD * 32 / LANES;
+  return launch_after(attention_delta_kernel<T, LANES>, dim3((unsigned)blocks, (unsigned)((d.heads + HEADS - 1) / HEADS)), DELTA_THREADS, 0, stream, d);
+}
+
 size_t stats_bytes(const lba_attention_how* h) { return (size_t)h->heads * h->q_rows * sizeof(float2); }
 
 }  // namespace
@@ -710,13 +759,13 @@ int lba_attention_backward(const void* grad_out, const void* q, const void* k, c
   p.key_blocks = (how->k_rows / XT + how->sequences) * how->kv_heads;
   const int64_t blocks = p.key_blocks + (how->q_rows / XT + how->sequences) * how->heads;
   const int64_t most_rows = how->q_rows > how->k_rows ? how->q_rows : how->k_rows, row_blocks = (most_rows + DELTA_THREADS / 32 - 1) / (DELTA_THREADS / 32);
-  const int64_t delta_blocks = row_blocks + (int64_t)how->sequences * how->heads;
-  d.row_blocks = row_blocks;
+  const int64_t few_blocks = (int64_t)how->sequences * how->heads * FEW_PARTS, delta_blocks = row_blocks + few_blocks;
   if (delta_blocks > 2147483647LL || blocks > 2147483647LL) return LBA_ERR_SHAPE;
+  d.few_blocks = (uint32_t)few_blocks;
   cudaError_t e = most ? cudaMemsetAsync(most, 0, 8, s) : cudaSuccess;
   if (e != cudaSuccess) return status_of(e);
-  e = p.bf ? launch_after(attention_delta_kernel<__nv_bfloat16>, dim3((unsigned)delta_blocks, (unsigned)((how->heads + 2 * DELTA_AHEAD - 1) / (2 * DELTA_AHEAD))), DELTA_THREADS, 0, s, d)
-           : launch_after(attention_delta_kernel<__half>, dim3((unsigned)delta_blocks, (unsigned)((how->heads + 2 * DELTA_AHEAD - 1) / (2 * DELTA_AHEAD))), DELTA_THREADS, 0, s, d);
+  e = how->dim <= 64 ? (p.bf ? launch_delta<__nv_bfloat16, 8>(d, delta_blocks, s) : launch_delta<__half, 8>(d, delta_blocks, s))
+                     : (p.bf ? launch_delta<__nv_bfloat16, 16>(d, delta_blocks, s) : launch_delta<__half, 16>(d, delta_blocks, s));
   if (e != cudaSuccess) return status_of(e);
   if (how->dim <= 64) return status_of(p.bf ? launch_grad<__nv_bfloat16, 64>(p, blocks, s) : launch_grad<__half, 64>(p, blocks, s));
   return status_of(p.bf ? launch_grad<__nv_bfloat16, 128>(p, blocks, s) : launch_grad<__half, 128>(p, blocks, s));
