@@ -263,7 +263,8 @@ int lba_attention(const void* q, const void* k, const void* v, const lba_attenti
  *     grad_q[i] = scale sum_j ds_ij k[j]     grad_k[j] = scale sum_i ds_ij q[i]     grad_v[j] = sum_i p_ij g[i]
  * the latter two also over the query heads of a group.  out and lse are the forward call's.  grad_out, out and the gradients are contiguous
  * [rows][heads][dim].  Sums are formed in a fixed order: a repeated call gives the same bits.  p and ds enter the products rounded to
- * the inputs' type (ds of binary16 inputs by a common power of two, so that small gradients keep their bits).  The workspace is
+ * the inputs' type (ds of binary16 inputs by a common power of two, so that small gradients keep their bits), in two pieces where
+ * a sequence's other side has at most 256 rows.  What infinities of grad_out reach is infinite or NaN.  The workspace is
  * 256-byte aligned device memory, holds nothing between calls, and calls that may overlap need one each. */
 size_t lba_attention_backward_workspace_bytes(const lba_attention_how* how);
 int lba_attention_backward(const void* grad_out, const void* q, const void* k, const void* v, const void* out, const float* lse,

@@ -22,7 +22,7 @@
 // tensor memory, and took 57 clocks a step instead of 32; 2 x 4096 tokens of 16 heads took 515 us.)
 //
 // p and ds are rounded to the inputs' type on their way into the products, which leaves gradients off by 1.4 times what their own rounding
-// costs.  delta comes from an output of 16 bits; where few keys are seen, that would add as much again (1.6 times with four keys), so rows
+// costs; where a CTA walks over one or two tiles of a head, and a few terms may cancel, they have a second piece (over T1, which is then formed late).  delta comes from an output of 16 bits; where few keys are seen, that would add as much again (1.6 times with four keys), so rows
 // of up to 32 keys get theirs from p and dp.  binary16 has few exponents: p is held times 2^8, and ds times a power of two chosen from the
 // largest |grad_out| and |v| so that it cannot overflow.
 #include <cmath>
@@ -33,6 +33,7 @@ namespace lba {
 namespace {
 
 constexpr int XT = 128, YT = 128, YC = 64, GRAD_THREADS = 384, Y1_SLOTS = 3, Y2_SLOTS = 2, CUTS = 4, DELTA_THREADS = 256;  // YC: columns of a warpgroup
+constexpr int FINE_TILES = 2;  // of a head: walks in which p and ds have two pieces
 constexpr float P_UP = 256.0f;
 constexpr int P_BITS = 8;
 
@@ -247,6 +248,12 @@ __global__ void __launch_bounds__(DELTA_THREADS, 5) attention_delta_kernel(const
   }
 }
 __device__ __forceinline__ float power_of_two(int e) { return __uint_as_float((uint32_t)(127 + e) << 23); }
+// what the rounding of a pair has cut off, rounded itself
+template <typename T>
+__device__ __forceinline__ uint32_t rest_of(float lo, float hi, uint32_t pair) {
+  const T* const t = reinterpret_cast<const T*>(&pair);
+  return pack_pair<T>(lo - to_f32(t[0]), hi - to_f32(t[1]));
+}
 // the power of two that ds is multiplied by: |ds| <= 2 dim |g| |v| stays below 2^15
 __device__ __forceinline__ int ds_bits(const GradParams& p) {
   if (!p.most) return 0;
@@ -309,6 +316,7 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
     walk.high = min(walk.high, max(0, x0 + off + 1) / YT);
   }
   const int all = walk.count();
+  const bool fine = walk.last - walk.first <= FINE_TILES;
 
   if (warp >= 8) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
@@ -387,7 +395,7 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
           form2(0);
         }
         for (int n = 0; n < all && ok; ++n) {
-          if (n + 1 < all) {
+          if (n + 1 < all && !fine) {
             ok = mbar_wait(smem_u32(&sh.t1_read), n & 1, dead);
             tmem_after();
             form1(n + 1);
@@ -396,20 +404,23 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
           ok = ok && mbar_wait(smem_u32(&sh.ds_there), n & 1, dead);
           if (!ok) break;
           tmem_after();
-          // in T2, of each warpgroup's 64 columns: the pairs of ds, then those of p
-          const auto add = [&](uint32_t acc, uint32_t a, uint32_t y) {
+          // in T2, of each warpgroup's 64 columns: the pairs of ds, then those of p; in T1 their second pieces
+          const auto add = [&](uint32_t acc, uint32_t a, uint32_t y, bool more) {
             const uint64_t b = lines + (y >> 4);
 #pragma unroll
-            for (int s = 0; s < YT / 16; ++s) mma_tensor(acc, a + (s >> 2) * YC + (s & 3) * 8, b + s * (2048 >> 4), kind_a, n != 0 || s != 0);
+            for (int s = 0; s < YT / 16; ++s) mma_tensor(acc, a + (s >> 2) * YC + (s & 3) * 8, b + s * (2048 >> 4), kind_a, more || s != 0);
           };
           const uint32_t of = tmem + 128 + (n & 1) * OTHER;
-          add(tmem + ACC1, of, ring1 + (n % Y1_SLOTS) * TILE);
+          add(tmem + ACC1, of, ring1 + (n % Y1_SLOTS) * TILE, n != 0);
+          if (fine) add(tmem + ACC1, tmem, ring1 + (n % Y1_SLOTS) * TILE, true);
           mma_arrive(smem_u32(&sh.empty1[n % Y1_SLOTS]));
           if (KEYS) {
-            add(tmem + ACC2, of + YC / 2, ring2 + (n % Y2_SLOTS) * TILE);
+            add(tmem + ACC2, of + YC / 2, ring2 + (n % Y2_SLOTS) * TILE, n != 0);
+            if (fine) add(tmem + ACC2, tmem + YC / 2, ring2 + (n % Y2_SLOTS) * TILE, true);
             mma_arrive(smem_u32(&sh.empty2[n % Y2_SLOTS]));
           }
-          if (!TWO && n + 1 < all) form2(n + 1);
+          if (n + 1 < all && fine) form1(n + 1);
+          if (n + 1 < all && (fine || !TWO)) form2(n + 1);
         }
         mma_arrive(smem_u32(&sh.done));
       }
@@ -533,7 +544,7 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
     const uint32_t t2 = t1 + 128 + (n & 1) * OTHER;
     // the upper half first: p goes over it while the lower one is formed
     uint32_t dw[YC / 2];
-    const auto slopes = [&](auto masked) {
+    const auto slopes = [&](auto masked, auto two) {
 #pragma unroll
       for (int half = YC - 32; half >= 0; half -= 32) {
         uint32_t dp[32];
@@ -545,6 +556,7 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
         }
         tmem_wait_ld();
         if (KEYS && half) tmem_store32(t2 + YC / 2, pw);
+        uint32_t rest[16];
 #pragma unroll
         for (int e = 0; e < 32; e += 2) {
           const float4& four = m[KEYS ? e / 4 : 0];
@@ -556,11 +568,21 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
             if (half + e + 1 < lo || half + e + 1 >= hi) d1 = 0.0f;
           }
           dw[(half + e) / 2] = pack_pair<T>(d0, d1);
+          if constexpr (decltype(two)::value) rest[e / 2] = rest_of<T>(d0, d1, dw[(half + e) / 2]);
+        }
+        if constexpr (decltype(two)::value) {
+          tmem_st16(t1 + half / 2, rest);
+          if constexpr (KEYS) {
+#pragma unroll
+            for (int e = 0; e < 32; e += 2) rest[e / 2] = rest_of<T>(__uint_as_float(s[half + e]), __uint_as_float(s[half + e + 1]), pw[(half + e) / 2]);
+            tmem_st16(t1 + YC / 2 + half / 2, rest);
+          }
         }
       }
     };
-    if (cut) slopes(std::true_type());
-    else slopes(std::false_type());
+    if (fine) slopes(std::true_type(), std::true_type());
+    else if (cut) slopes(std::true_type(), std::false_type());
+    else slopes(std::false_type(), std::false_type());
     tmem_store32(t2, dw);
     tmem_wait_st();
     tmem_before();
