@@ -662,7 +662,7 @@ PyObject* attention_backward(PyObject*, PyObject* const* a, Py_ssize_t n) {
 lba_cache as_cache(PyObject* o, PyObject* page, PyObject* table, int64_t sequences, const Call& call) {
   const at::Tensor &t = as_tensor(o, at::kByte, 3, call.device), &b = as_tensor(table, at::kInt, 2, call.device);
   const int64_t p = as_int(page), run = t.size(2);
-  if (b.size(0) != sequences || p < 1 || run % (17 * p) || run * 16 / (17 * p) % 32) not_regular();
+  if (b.size(0) != sequences || p < 1 || p > INT_MAX || run % (17 * p) || run * 16 / (17 * p) % 32) not_regular();
   lba_cache c = {};
   c.pages = t.data_ptr();
   c.page_count = t.size(0);
