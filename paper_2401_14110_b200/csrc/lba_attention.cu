@@ -270,7 +270,7 @@ __global__ void __launch_bounds__(128 * (W + 1), 3 - W) attention_kernel(const _
       else asm volatile("setmaxnreg.inc.sync.aligned.u32 208;");
       const int w = warp >> 2, mine = tiles[w], row = threadIdx.x & 127, i = i0 + w * QT + row;
       const uint32_t lanes = (uint32_t)(warp & 3) << 21, s_at = tmem + w * KT + lanes, o_at = tmem + (W + w) * 128 + lanes;
-      const float c = p.to_log2;
+      const float c = p.to_log2, out_scale = p.codes ? __ldg(p.out_scale) : 1.0f;  // (fetched here: at the end every block would wait for it)
       float top = -INFINITY;
       u64 total[4] = {};  // chains of their own
       bool ok = true;
@@ -348,7 +348,7 @@ __global__ void __launch_bounds__(128 * (W + 1), 3 - W) attention_kernel(const _
         for (int x = 0; x < CUT_TILES; ++x)
           for (int e = 0; e < 4; ++e) poison |= sh.cut[x][e];
       }
-      const Quotients quotients(p.codes ? *p.out_scale : 1.0f);
+      const Quotients quotients(out_scale);
       // 32 values a row at a time go out through shared memory (the tile of Q is no longer read), four lanes a row side by side.  The code is kept
       // short: it runs once a CTA and is fetched as it runs (unrolled over a row's values, codes took 10000 clocks).
       uint8_t* const stage = raw_smem + (q_smem - smem_u32(raw_smem)) + w * TILE + (warp & 3) * 4096;

@@ -884,8 +884,11 @@ __global__ void __launch_bounds__(32 * NG) cache_combine_kernel(const DecodePara
   const int begin = p.before[b], units = p.before[b + 1] - begin, share = share_of(p, p.before[p.c.sequences]), first = begin * lines + line * units;
   const int w0 = first / share, n = units > 0 ? (first + units - 1) / share - w0 + 1 : 0;
   const float* const part = p.parts + (w0 + (int64_t)b * lines + line) * (HT * PART) + col * PART;
-  float top = NO_MAX, sum = 0.0f, v = 0.0f;
-  for (int i0 = 0; i0 < n; i0 += PARTS_AT_ONCE) {  // (two trips to memory for 256 parts; one after the other they cost one each four)
+  constexpr int AHEAD = 8;
+  float top = NO_MAX, sum = 0.0f, v = 0.0f, ahead[AHEAD];  // ahead: of the first parts, beside their weights
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) ahead[i] = i < n ? __ldg(part + (int64_t)i * HT * PART + d) : 0.0f;
+  for (int i0 = 0; i0 < n; i0 += PARTS_AT_ONCE) {  // (two trips to memory for 256 parts, one for the first eight; one after the other they cost one each four)
     const int here = min(n - i0, PARTS_AT_ONCE);
     float most = top;
     for (int i = d; i < here; i += D) {
@@ -903,13 +906,18 @@ __global__ void __launch_bounds__(32 * NG) cache_combine_kernel(const DecodePara
     top = most;
     sum *= was;
     v *= was;
-    const float* src = part + (int64_t)i0 * HT * PART + d;
-#pragma unroll 8
-    for (int i = 0; i < here; ++i, src += HT * PART) {
-      const float vi = __ldg(src), by = exp2_approx(weight[i].x - top);
+    const auto add = [&](int i, float vi) {
+      const float by = exp2_approx(weight[i].x - top);
       sum = fmaf(weight[i].y, by, sum);
       if (weight[i].y != 0.0f) v = fmaf(vi, by, v);  // (tokens that are not there leave nothing)
+    };
+    if (i0 == 0) {
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+        if (i < here) add(i, ahead[i]);
     }
+#pragma unroll 8
+    for (int i = i0 == 0 ? AHEAD : 0; i < here; ++i) add(i, __ldg(part + (int64_t)(i0 + i) * HT * PART + d));
     __syncthreads();
   }
   store_decoded<D>(p, ((int64_t)b * p.heads + h) * D + d, sum == 0.0f ? 0.0f : __fdiv_rn(v, sum));
