@@ -475,7 +475,9 @@ __global__ void __launch_bounds__(DEC_THREADS, 1) cache_attention_kernel(const D
     if (threadIdx.x == 0) p.before[p.c.sequences] = all;
   }
   const int share = share_of(p, all), total = all * lines;
-  int at = (int)min((unsigned)(blockIdx.x * DEC_WARPS + warp) * (unsigned)share, (unsigned)total);
+  // (first the first warp of every CTA: few units spread over the SMs)
+  const int me = warp * (int)gridDim.x + (int)blockIdx.x;
+  int at = (int)min((unsigned)me * (unsigned)share, (unsigned)total);
   const int end = (int)min((unsigned)at + (unsigned)share, (unsigned)total);
   if (group_count > 1 && at < end) {  // the group of the first unit: the last that begins at or before it
     int lo = 0, hi = group_count - 1;
@@ -845,7 +847,7 @@ __global__ void __launch_bounds__(DEC_THREADS, 1) cache_attention_kernel(const D
     }
 
     // the part
-    float* const part = p.parts + ((int64_t)blockIdx.x * DEC_WARPS + warp + (int64_t)b * lines + line) * (HT * PART);
+    float* const part = p.parts + (me + (int64_t)b * lines + line) * (HT * PART);
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -884,11 +886,11 @@ __global__ void __launch_bounds__(32 * NG) cache_combine_kernel(const DecodePara
   const int begin = p.before[b], units = p.before[b + 1] - begin, share = share_of(p, p.before[p.c.sequences]), first = begin * lines + line * units;
   const int w0 = first / share, n = units > 0 ? (first + units - 1) / share - w0 + 1 : 0;
   const float* const part = p.parts + (w0 + (int64_t)b * lines + line) * (HT * PART) + col * PART;
-  constexpr int AHEAD = 8;
+  constexpr int AHEAD = 16;
   float top = NO_MAX, sum = 0.0f, v = 0.0f, ahead[AHEAD];  // ahead: of the first parts, beside their weights
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i) ahead[i] = i < n ? __ldg(part + (int64_t)i * HT * PART + d) : 0.0f;
-  for (int i0 = 0; i0 < n; i0 += PARTS_AT_ONCE) {  // (two trips to memory for 256 parts, one for the first eight; one after the other they cost one each four)
+  for (int i0 = 0; i0 < n; i0 += PARTS_AT_ONCE) {  // (two trips to memory for 256 parts, one for the first sixteen; one after the other they cost one each four)
     const int here = min(n - i0, PARTS_AT_ONCE);
     float most = top;
     for (int i = d; i < here; i += D) {
@@ -934,8 +936,8 @@ bool plan_decode(const CacheView& c, int dim, int heads, DecodePlan* d) {
   d->pieces = (group + d->cols - 1) / d->cols;
   const double lines = (double)c.sequences * c.heads * d->pieces, most = std::ceil((double)c.width * c.page / UNIT);
   if (most * lines > 2147483647.0 - 65536.0) return false;
-  const int resident = device_sms(), useful = (int)std::ceil(most * lines / DEC_WARPS);
-  d->blocks = useful < 1 ? 1 : useful < resident ? useful : resident;
+  const double resident = device_sms(), useful = most * lines;
+  d->blocks = useful < 1 ? 1 : (int)(useful < resident ? useful : resident);
   d->before_bytes = ((size_t)(c.sequences + 1) * sizeof(int) + 255) / 256 * 256;
   d->bytes = d->before_bytes + ((size_t)d->blocks * DEC_WARPS + (size_t)lines) * d->cols * (dim + 2) * sizeof(float);
   return true;
