@@ -191,3 +191,31 @@ def test_native_calls_are_regular_and_agree_with_ctypes(monkeypatch):
     monkeypatch.setattr(lba, "_native", None)
     for x, y in zip(a, all_calls()):
         assert torch.equal(x, y)
+
+
+def test_calls_on_three_streams_at_once():
+    """blocks of one and of two tiles, a backward pass and a cache's reader meet on the same SMs; every result is what the call alone gives"""
+    g = torch.Generator("cuda").manual_seed(5)
+    randn = lambda *s: torch.randn(*s, generator=g, device="cuda").to(torch.bfloat16)  # noqa: E731
+    cu = torch.arange(0, 25 * 100, 100, dtype=torch.int32, device="cuda")
+    q, k, v = randn(2400, 8, 64), randn(2400, 4, 64), randn(2400, 4, 64)
+    long_q, long_k, long_v, grad = randn(3000, 4, 128), randn(3000, 2, 128), randn(3000, 2, 128), randn(3000, 4, 128)
+    out, lse = lba.lba_attention(long_q, long_k, long_v, lse=True)
+    cache = torch.zeros(lba.cache_shape(40, 2, 64, 128), dtype=torch.uint8, device="cuda")
+    table = torch.randperm(40, generator=g, device="cuda").to(torch.int32).view(2, 20)
+    ends = torch.tensor([0, 1270, 1300], dtype=torch.int32, device="cuda")
+    lba.lba_cache_append(long_k[:1300], long_v[:1300], cache, 64, table, torch.zeros(2, dtype=torch.int32, device="cuda"), ends)
+    calls = [lambda s: (lba.lba_attention(q, k, v, cu, cu, stream=s),),
+             lambda s: (lba.lba_attention(long_q, long_k, long_v, stream=s),),
+             lambda s: lba.lba_attention_backward(grad, long_q, long_k, long_v, out, lse, stream=s),
+             lambda s: (lba.lba_cache_attention(long_q[:2], cache, 64, table, torch.tensor([1270, 30], dtype=torch.int32, device="cuda"), stream=s),)]
+    want = [call(torch.cuda.current_stream()) for call in calls]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(3)]
+    got = []
+    for i in range(24):
+        with torch.cuda.stream(streams[i % 3]):
+            got.append((i % 4, calls[i % 4](streams[i % 3])))
+    torch.cuda.synchronize()
+    for which, result in got:
+        assert all(torch.equal(a, b) for a, b in zip(result, want[which]))
