@@ -297,7 +297,10 @@ int lba_cache_read(const lba_cache* cache, const int32_t* start, const int32_t* 
                    void* stream);
 /* One new token of each sequence: out[b][h] = softmax(scale q[b][h] k) v over the first lengths[b] tokens of the cache (0 for none);
  * q [sequences][heads][dim] of LBA_TYPE_BF16 or F16 with row stride q_at.token; out as lba_attention's, [sequences][heads][dim];
- * scale finite and > 0.  Workspace as for lba_attention_backward. */
+ * scale finite and > 0.  Scores, weights and sums are binary32.  A weight p enters the second product rounded to 11 bits, or by 2^-20 of
+ * the largest weight times the largest value beside it (of its group of 32): each token adds at most (2^-11 p) |v| and that much to an error.
+ * Values may be of any sizes: tokens whose powers of two lie outside 16 binades are weighed in binary32, at some seven times the time for
+ * their sequence's head, and count down to 2^-126 of the largest.  Workspace as for lba_attention_backward. */
 size_t lba_cache_attention_workspace_bytes(const lba_cache* cache, int heads);
 int lba_cache_attention(const void* q, lba_strides q_at, int type, int heads, const lba_cache* cache, const int32_t* lengths,
                         float scale, int out_type, const float* out_scale, int out_flags, void* out, void* workspace,

@@ -10,9 +10,10 @@
 //               finished 32-term sum, in binary32
 //   softmax     one pass; a running maximum per head that is raised only when a score exceeds it by 2^5, so that a vote replaces the
 //               reduction of most steps
-//   O = V^T P   P goes from accumulator to operand layout by the matrix transpose, with 10 bits of headroom below; the values' powers of two
-//               differ by token and group, so P is multiplied by them, relative to the largest that the warp has met in the group (15 and
-//               more binades below it they count as 0: 2^-15 of the largest value).  binary16: 2^-12 of a weight
+//   O = V^T P   P goes from accumulator to operand layout by the matrix transpose, with 9 bits of headroom below; the values' powers of two
+//               differ by token and group, so P is multiplied by them, relative to one that the warp's first steps with a line have set.  16
+//               binades around it are binary16's to tell apart (2^-12 of a weight); once any token's power of two lies outside, weights
+//               and values of that line are multiplied in binary32, token by token (740 us instead of 109 for the 48 requests below)
 // A query head is brought to [1, 2) by a power of two first and is then exact in binary16 but for what lies 2^-14 below its largest value.
 // A warp has two units of 64 tokens in shared memory, one that it computes and one on its way by bulk copies, and meets no other warp.  What
 // bounds it now is the widening: some 290 instructions for 16 tokens of 128 dimensions and four heads, half of them conversions and byte moves on
@@ -316,9 +317,9 @@ cudaError_t launch_rows(const RowsParams& p, int dim, int type, cudaStream_t str
 constexpr int UNIT = 64, STEP = 16, DEC_STAGES = 2, DEC_WARPS = 12, DEC_THREADS = 32 * DEC_WARPS;
 constexpr int KNOWN = 128, GROUPS = 65536 / KNOWN;  // sequences of which a warp knows the lengths at a time
 constexpr float HEADROOM = 5.0f;     // binades by which a score may exceed its head's running maximum
-constexpr float P_BITS = 10.0f;      // weights in binary16: at most 2^(10 + 5)
+constexpr float P_BITS = 9.0f;       // weights in binary16: at most 2^(9 + 5), and twice that times the power of two of their values
 constexpr float NO_MAX = -1e30f;
-constexpr uint32_t LEAST_REF = 0x10101010u;  // see `ref`
+constexpr int EDGE_ABOVE = 3;        // binades that a line's values may grow by above its first ones' largest; 12 are left below
 
 struct DecodeParams {
   CacheView c;
@@ -596,12 +597,13 @@ __global__ void __launch_bounds__(DEC_THREADS, 1) cache_attention_kernel(const D
       for (int j = 0; j < 2; ++j) to_log2[n][j] = __shfl_sync(0xFFFFFFFFu, up, (2 * c + j) * 4);
     }
 
-    // m: the maximum that weights are relative to, less 10 binades; limit: the score from which on it is raised.
-    // ref: for each group the exponent byte that weights are relative to, at least 16, so that the byte of ref - (an exponent) is in 0..15 only
-    // where the exponent is in ref - 15..ref (an exponent above ref gives 17 to 255 there, and borrows change no 0..15 to that).
+    // m: the maximum that weights are relative to, less 9 binades; limit: the score from which on it is raised.
+    // edge: for each group the highest exponent byte of the 16 that weights can be brought to, in 16..254 (0: no token yet): outputs are relative to
+    // the power of two below it.  A byte of edge - (exponents) is in 0..15 where the exponent is among the 16; an exponent above gives 17 to 255
+    // there, and a borrow only comes from such a byte: no high half of a byte set means that all are among them.
     float o[OT][NG][4], m[NT][2], limit[NT][2], l[NT][2];
-    constexpr uint32_t LEAST = LEAST_REF >> (8 * (4 - NG));
-    uint32_t ref = LEAST, base = 0x3C3C3C3Cu - 4u * LEAST;  // base + 4 e: bytes 0x3C - 4 (ref - e), the high byte of 2^-(ref - e) in binary16
+    uint32_t edge = 0, base = 0;  // base + 4 e: bytes 0x40 - 4 (edge - e), the high byte of 2^(1 - (edge - e)) in binary16
+    bool by_token = false;        // some token was outside: from then on products are formed in binary32
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
       m[n][0] = m[n][1] = limit[n][0] = limit[n][1] = NO_MAX;
@@ -619,6 +621,52 @@ __global__ void __launch_bounds__(DEC_THREADS, 1) cache_attention_kernel(const D
     const uint32_t place_of = r < 4 ? 0x4404u : 0x0444u, place_step = r < 4 ? 0x0010u : 0x1000u;
     const int swap = c & 1;
     const uint32_t pick0 = swap ? 0x3232u : 0x1010u, pick1 = swap ? 0x1010u : 0x3232u;
+
+    // The same sums token by token in binary32: a weight comes from the lane that holds it, a lane's outputs are those of the matrix instructions
+    const auto add_by_token = [&](const uint8_t* unit, int first, int left, uint32_t steps, const float (&z)[BATCH][NT][4]) {
+#pragma unroll
+      for (int x = 0; x < BATCH; ++x) {
+        const int here = (steps >> x) & 1 ? left - x * STEP : 0;
+        float e[NT][4];
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            e[n][j] = exp2_approx(fmaf(z[x][n][j], to_log2[n][j & 1], -m[n][j & 1]));
+            l[n][j & 1] += e[n][j];
+          }
+#pragma unroll
+        for (int half = 0; half < 2; ++half)
+#pragma unroll 1
+          for (int i = 0; i < 8 && half * 8 + i < here; ++i) {
+            float w[OT][2];  // of heads 4 t + 2 (c & 1) and the next
+#pragma unroll
+            for (int t = 0; t < OT; ++t)
+#pragma unroll
+              for (int j = 0; j < 2; ++j)
+                w[t][j] = __shfl_sync(0xFFFFFFFFu, e[t * NT / OT][2 * half + j], i * 4 + (TWICE ? 0 : 2 * (t & 1)) + (c & 1));
+            const int row = first + x * STEP + half * 8 + i;
+            const uint32_t exps = exponents<NG>(unit + U::VALUE_EXP + row * NG);
+            const uint8_t* const codes = unit + U::VALUES + row * (D / 2) + r * (D / 16);
+#pragma unroll
+            for (int g = 0; g < NG; ++g) {
+              // (an exponent byte of 0 holds nothing but zeros; 2^-126 below the outputs' power of two values count as 0)
+              const int power = (int)((exps >> (8 * g)) & 255u), d = power - (int)((edge >> (8 * g)) & 255u) + 1;
+              const float by = power == 255 ? __uint_as_float(0x7FC00000u) : power == 0 || d < -126 ? 0.0f : __uint_as_float((uint32_t)(127 + d) << 23);
+#pragma unroll
+              for (int k = 0; k < 2; ++k) {
+                const uint32_t code = codes[2 * g + k] >> (c >> 1) * 4;
+                // as a binary32 number 2^126 below, 1/2 among those without a leading 1
+                const float v = __uint_as_float((code & 8u) << 28 | (code & 7u) << 22) * 0x1p126f * by;
+#pragma unroll
+                for (int t = 0; t < OT; ++t)
+#pragma unroll
+                  for (int j = 0; j < 2; ++j) o[t][g][2 * k + j] = fmaf(w[t][j], v, o[t][g][2 * k + j]);
+              }
+            }
+          }
+      }
+    };
 
     // BATCH steps from token `first` of a unit on, of which `left` tokens exist and `steps` (bits) are there
     const auto compute = [&](const uint8_t* unit, int first, int left, uint32_t steps) {
@@ -678,7 +726,7 @@ __global__ void __launch_bounds__(DEC_THREADS, 1) cache_attention_kernel(const D
               if (r + (j >> 1) * 8 >= here) z[x][n][j] = -INFINITY;
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (2 * c + ((i & 1) ^ swap) + (i >> 1) * 8 >= here) ve[x][i] = ref;
+            if (2 * c + ((i & 1) ^ swap) + (i >> 1) * 8 >= here) ve[x][i] = edge;
         }
       }
       uint32_t wide = 0;
@@ -686,26 +734,43 @@ __global__ void __launch_bounds__(DEC_THREADS, 1) cache_attention_kernel(const D
 #pragma unroll
       for (int x = 0; x < BATCH; ++x) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) wide |= ref - ve[x][i];
+        for (int i = 0; i < 4; ++i) wide |= edge - ve[x][i];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int j = 0; j < 4; ++j) raise |= z[x][n][j] > limit[n][j & 1];
       }
-      raise |= (wide & 0xF0F0F0F0u) != 0;
-      uint32_t far[BATCH][4];  // groups whose values count as 0
-      bool any_far = false;
+      raise |= edge == 0 || (wide & 0xF0F0F0F0u) != 0;
       if (__any_sync(0xFFFFFFFFu, raise)) {
-        uint32_t top = ref;
+        // (a byte of 255, no number, has no binade.  Tokens that are not there have bytes of edge: 0 before there is one)
+        uint32_t top = 0;
 #pragma unroll
         for (int x = 0; x < BATCH; ++x)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) top = max_bytes(top, ve[x][i]);
+          for (int i = 0; i < 4; ++i) top = max_bytes(top, ve[x][i] & ~__vcmpeq4(ve[x][i], 0xFFFFFFFFu));
         top = max_bytes(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
         top = max_bytes(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-        const uint32_t by = top - ref;
-        ref = top;
-        base = 0x3C3C3C3Cu - 4u * ref;
+        uint32_t by = 0;  // binades by which the edge rises, and outputs with it
+        if (edge == 0) {
+          constexpr uint32_t GROUP_BYTES = 0xFFFFFFFFu >> (8 * (4 - NG));
+          edge = __vminu4(__vmaxu4(__vaddus4(top, 0x01010101u * EDGE_ABOVE), 0x10101010u), 0xFEFEFEFEu) & GROUP_BYTES;
+          base = (0x40404040u & GROUP_BYTES) - 4u * edge;
+          wide = 0;
+#pragma unroll
+          for (int x = 0; x < BATCH; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const int here = (steps >> x) & 1 ? left - x * STEP : 0;
+              if (2 * c + ((i & 1) ^ swap) + (i >> 1) * 8 >= here) ve[x][i] = edge;
+              wide |= edge - ve[x][i];
+            }
+        }
+        by_token = by_token || __any_sync(0xFFFFFFFFu, (wide & 0xF0F0F0F0u) != 0);
+        if (by_token) {
+          top = max_bytes(top, edge);
+          by = top - edge;
+          edge = top;
+        }
         float a[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -735,20 +800,10 @@ __global__ void __launch_bounds__(DEC_THREADS, 1) cache_attention_kernel(const D
             for (int j = 0; j < 4; ++j) o[t][g][j] *= f[j & 1] * down;
           }
         }
-#pragma unroll
-        for (int x = 0; x < BATCH; ++x)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            far[x][i] = 0;
-#pragma unroll
-            for (int g = 0; g < NG; ++g) {
-              const uint32_t byte = 255u << (8 * g);
-              if ((ref - ve[x][i]) & 0xF0F0F0F0u & byte) far[x][i] |= byte;
-            }
-            ve[x][i] = (ve[x][i] & ~far[x][i]) | (ref & far[x][i]);
-            any_far |= far[x][i] != 0;
-          }
-        any_far = __any_sync(0xFFFFFFFFu, any_far);
+      }
+      if (by_token) {
+        add_by_token(unit, first, left, steps, z);
+        return;
       }
 #pragma unroll
       for (int x = 0; x < BATCH; ++x) {
@@ -789,13 +844,6 @@ __global__ void __launch_bounds__(DEC_THREADS, 1) cache_attention_kernel(const D
             v[i][0] = h[0] | (uint32_t)h[NG == 3] << 16;
             if constexpr (NG == 3) v[i][1] = h[2] | (uint32_t)h[2] << 16;
           }
-        }
-        if (any_far) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-#pragma unroll
-            for (int g = 0; g < NG; ++g)
-              if ((far[x][i] >> (8 * g)) & 1u) v[i][g / 2] &= g & 1 ? 0x0000FFFFu : 0xFFFF0000u;
         }
         // A byte's conversion gives two dimensions of a token.  They are two k-steps of the product, and its columns are four heads twice: the first
         // four columns' weights are 0 for the second dimension, the others' for the first.  So are the factors that bring a weight to its group.
@@ -864,8 +912,8 @@ __global__ void __launch_bounds__(DEC_THREADS, 1) cache_attention_kernel(const D
     for (int t = 0; t < OT; ++t)
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
-        const uint32_t e = (ref >> (8 * g)) & 255u;
-        const float by = e == 255u ? __uint_as_float(0x7FC00000u) : __uint_as_float(e << 23);
+        const uint32_t e = (edge >> (8 * g)) & 255u;
+        const float by = __uint_as_float((e == 0 ? 0u : e - 1) << 23);  // (0: no token was there)
 #pragma unroll
         for (int j = 0; j < 4; ++j) part[(4 * t + 2 * (c & 1) + (j & 1)) * PART + 2 * (16 * g + r + 8 * (j >> 1)) + (c >> 1)] = o[t][g][j] * by;
       }
