@@ -894,8 +894,9 @@ __global__ void __launch_bounds__(DEC_THREADS, 1) cache_attention_kernel(const D
       }
     }
 
-    // the part
+    // The part.  It is brought to a sum of weights in 1/4..1/2, so that its outputs, which are at most that times the largest value, are in range.
     float* const part = p.parts + (me + (int64_t)b * lines + line) * (HT * PART);
+    float to_range[NT][2];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -905,18 +906,24 @@ __global__ void __launch_bounds__(DEC_THREADS, 1) cache_attention_kernel(const D
         t += __shfl_xor_sync(0xFFFFFFFFu, t, 8);
         t += __shfl_xor_sync(0xFFFFFFFFu, t, 16);
         if (!ok) t = __uint_as_float(0x7FC00000u);
+        const int e = t > 0.0f && t < INFINITY ? (int)(__float_as_uint(t) >> 23) - 125 : 0;  // (a sum that is not 0 is 2^-126 or more)
+        to_range[n][j] = __uint_as_float((uint32_t)(127 - e) << 23);
         const int h = n * 8 + 2 * c + j;
-        if (r == 0 && h < HT) *reinterpret_cast<float2*>(part + h * PART + D) = make_float2(m[n][j], t);
+        if (r == 0 && h < HT) *reinterpret_cast<float2*>(part + h * PART + D) = make_float2(m[n][j] + (float)e, t * to_range[n][j]);
       }
 #pragma unroll
-    for (int t = 0; t < OT; ++t)
+    for (int t = 0; t < OT; ++t) {
+      float f[2];  // of heads 4 t + 2 (c & 1) and the next
+#pragma unroll
+      for (int j = 0; j < 2; ++j) f[j] = TWICE ? to_range[0][j] : __shfl_sync(0xFFFFFFFFu, to_range[t / 2][j], (lane & 28) + 2 * (t & 1) + (c & 1));
 #pragma unroll
       for (int g = 0; g < NG; ++g) {
         const uint32_t e = (edge >> (8 * g)) & 255u;
         const float by = __uint_as_float((e == 0 ? 0u : e - 1) << 23);  // (0: no token was there)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) part[(4 * t + 2 * (c & 1) + (j & 1)) * PART + 2 * (16 * g + r + 8 * (j >> 1)) + (c >> 1)] = o[t][g][j] * by;
+        for (int j = 0; j < 4; ++j) part[(4 * t + 2 * (c & 1) + (j & 1)) * PART + 2 * (16 * g + r + 8 * (j >> 1)) + (c >> 1)] = o[t][g][j] * f[j & 1] * by;
       }
+    }
   }
   if (!ok) let_copies_land();
 }
@@ -935,6 +942,7 @@ __global__ void __launch_bounds__(32 * NG) cache_combine_kernel(const DecodePara
   const int w0 = first / share, n = units > 0 ? (first + units - 1) / share - w0 + 1 : 0;
   const float* const part = p.parts + (w0 + (int64_t)b * lines + line) * (HT * PART) + col * PART;
   constexpr int AHEAD = 16;
+  const float down = n > 1 ? (float)(32 - __clz(n - 1)) : 0.0f;  // binades that n parts' sums may be above one's
   float top = NO_MAX, sum = 0.0f, v = 0.0f, ahead[AHEAD];  // ahead: of the first parts, beside their weights
 #pragma unroll
   for (int i = 0; i < AHEAD; ++i) ahead[i] = i < n ? __ldg(part + (int64_t)i * HT * PART + d) : 0.0f;
@@ -957,7 +965,7 @@ __global__ void __launch_bounds__(32 * NG) cache_combine_kernel(const DecodePara
     sum *= was;
     v *= was;
     const auto add = [&](int i, float vi) {
-      const float by = exp2_approx(weight[i].x - top);
+      const float by = exp2_approx(weight[i].x - top - down);
       sum = fmaf(weight[i].y, by, sum);
       if (weight[i].y != 0.0f) v = fmaf(vi, by, v);  // (tokens that are not there leave nothing)
     };

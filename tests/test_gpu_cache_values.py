@@ -108,3 +108,15 @@ def test_a_group_that_is_no_number_among_small_and_large_ones():
     v[3, 0, 40], v[5] = math.nan, v[5] * 2.0 ** 30
     got = _check(_first_value(4, 64), [k], [v])
     assert torch.isnan(got[..., 32:]).all() and torch.isfinite(got[..., :32]).all()
+
+
+@pytest.mark.parametrize("tokens", [1, 3, 100, 5000])
+@pytest.mark.parametrize("size", [2.0 ** 127, 2.0 ** 100, 2.0 ** -120])
+def test_values_at_the_ends_of_the_range(size, tokens):
+    """an output lies between its values, however large they are"""
+    k, v = _randn(tokens, 1, 64, seed=1), (_randn(tokens, 1, 64, seed=2).abs() * 0.25 + 0.5).clamp_max(1.4) * size
+    cache, table, lengths = _cache([k], [v])
+    q = _randn(1, 4, 64, seed=3, dtype=torch.bfloat16)
+    got = lba.lba_cache_attention(q, cache, PAGE, table, _ints(lengths), scale=0.5)
+    want, bound = attention(q, cache, PAGE, table, lengths, 0.5)
+    close(got, want, bound + 2.0 ** -140)   # (parts of what is below 2^-126 are held to 2^-149, and a sum of parts to their number of times that)
