@@ -588,7 +588,8 @@ __global__ void __launch_bounds__(DEC_THREADS, 1) cache_attention_kernel(const D
       top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
       int e = (int)(__float_as_uint(top) >> 23) - 127;  // (infinities stay what they are under any factor)
       e = e < -126 ? -126 : e > 126 ? 126 : e;
-      const float down = __uint_as_float((uint32_t)(127 - e) << 23), up = __uint_as_float((uint32_t)(127 + e) << 23) * (p.scale * LOG2E);
+      const float down = __uint_as_float((uint32_t)(127 - e) << 23);
+      const float up = fmaxf(__uint_as_float((uint32_t)(127 + e) << 23) * (p.scale * LOG2E), 0x1p-149f);  // (0 times the -inf of what is not there is no number)
 #pragma unroll
       for (int g = 0; g < NG; ++g)
 #pragma unroll

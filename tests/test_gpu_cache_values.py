@@ -120,3 +120,18 @@ def test_values_at_the_ends_of_the_range(size, tokens):
     got = lba.lba_cache_attention(q, cache, PAGE, table, _ints(lengths), scale=0.5)
     want, bound = attention(q, cache, PAGE, table, lengths, 0.5)
     close(got, want, bound + 2.0 ** -140)   # (parts of what is below 2^-126 are held to 2^-149, and a sum of parts to their number of times that)
+
+
+@pytest.mark.parametrize("scale", [1e-38, 1e-20, 1.0])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_a_query_of_zeros_and_a_small_scale(dtype, scale):
+    """weights are all the same: the mean of the values, whatever stands behind the last token"""
+    k, v = (torch.randn(21, 1, 32, generator=torch.Generator("cuda").manual_seed(s), device="cuda") for s in (1, 2))
+    cache = torch.full(lba.cache_shape(2, 1, 16, 32), 0xFF, dtype=torch.uint8, device="cuda")
+    table = torch.tensor([[1, 0]], dtype=torch.int32, device="cuda")
+    ends = torch.tensor([0, 21], dtype=torch.int32, device="cuda")
+    lba.lba_cache_append(k, v, cache, 16, table, ends[:1], ends)
+    q = torch.zeros(1, 2, 32, dtype=dtype, device="cuda")
+    q[0, 1, 5] = 2.0 ** -24
+    got = lba.lba_cache_attention(q, cache, 16, table, ends[1:], scale=scale)
+    close(got, *attention(q, cache, 16, table, [21], scale))
