@@ -245,7 +245,9 @@ int lba_rotary(const void* q, lba_strides q_at, const void* k, lba_strides k_at,
  * over j of i's sequence, and with `causal` only those with j - i <= keys - queries of the sequence, rows counted from its first (the
  * last row sees every key).  A row that sees no key gives 0, lse -inf.  What the mask hides does not count, infinities and NaN included.
  * Rows of q in no sequence are left as they were in out and lse, and are 0 in the gradients.  Offsets outside [0, rows] count as the
- * nearer end, a sequence that ends before it starts is empty; sequences follow each other in memory. */
+ * nearer end, a sequence that ends before it starts is empty; sequences follow each other in memory.
+ * Scores, weights and sums are binary32; in the second product a weight is rounded to the inputs' type, 8 or 11 bits (binary16: those below
+ * 2^-21 of the row's largest to 2^-32 of that). */
 typedef struct {
   int32_t type;         /* LBA_TYPE_BF16 or F16: of q, k, v and what has their shapes                 */
   int32_t heads, kv_heads, dim; /* heads a multiple of kv_heads; dim a multiple of 8, 8..128            */

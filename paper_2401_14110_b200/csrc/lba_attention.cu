@@ -15,7 +15,8 @@
 // A prompt of 8192 tokens, 32 heads of 128, takes 461 us in a burst (1.19 PFLOP/s, 70% of the matrix peak) and 533 us under the power limit;
 // short sequences are bound by what a CTA does once: some 9 us for its place, its first copies and products, and its rows' way out.
 // Weights are rounded to the inputs' type (2^-9 or 2^-12 of each, at random; the result is rounded to that type once more); sums of weights
-// are of the unrounded ones.
+// are of the unrounded ones.  binary16 has few exponents: weights are held 2^7 above the maximum's, so that with the 2^8 by which a score may exceed it
+// they end at 2^15, and those below 2^-21 of the maximum's have fewer bits, those below 2^-32 none.
 #include <cmath>
 
 #include "lba_tile.cuh"
@@ -25,6 +26,7 @@ namespace {
 
 constexpr int QT = 128, KT = 128, MAX_STAGES = 10, CUT_TILES = 4;
 constexpr float LAZY = 8.0f;  // binades
+template <typename T> constexpr float kUp = std::is_same<T, __half>::value ? 7.0f : 0.0f;  // binades that weights are held above the maximum's
 
 struct ForwardParams {
   CUtensorMap q, k, v;
@@ -317,7 +319,7 @@ __global__ void __launch_bounds__(128 * (W + 1), 3 - W) attention_kernel(const _
           }
           top = next;
         }
-        const u64 by = both(c), minus = both(top == -INFINITY ? 0.0f : -top * c);
+        const u64 by = both(c), minus = both(top == -INFINITY ? 0.0f : kUp<T> - top * c);
         uint32_t packed[KT / 2];
         // (the first products start while the last quarter is formed)
 #pragma unroll
@@ -341,7 +343,7 @@ __global__ void __launch_bounds__(128 * (W + 1), 3 - W) attention_kernel(const _
       const bool there = i < q_count;
       if (there && p.lse)
         p.lse[(int64_t)head * p.q_rows + q_first + i] =
-            !ok ? __uint_as_float(0x7FC00000u) : sum == 0.0f ? -INFINITY : (top * c + log2f(sum)) * 0.69314718055994531f;
+            !ok ? __uint_as_float(0x7FC00000u) : sum == 0.0f ? -INFINITY : (top * c + (log2f(sum) - kUp<T>)) * 0.69314718055994531f;
       const float inv = !ok ? __uint_as_float(0x7FC00000u) : sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum);
       uint32_t poison = 0;  // of the cut tiles, as one word: any at all?
       if (p.causal) {
