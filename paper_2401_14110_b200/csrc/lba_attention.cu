@@ -273,6 +273,7 @@ __global__ void __launch_bounds__(128 * (W + 1), 3 - W) attention_kernel(const _
       const int w = warp >> 2, mine = tiles[w], row = threadIdx.x & 127, i = i0 + w * QT + row;
       const uint32_t lanes = (uint32_t)(warp & 3) << 21, s_at = tmem + w * KT + lanes, o_at = tmem + (W + w) * 128 + lanes;
       const float c = p.to_log2, out_scale = p.codes ? __ldg(p.out_scale) : 1.0f;  // (fetched here: at the end every block would wait for it)
+      const bool there = i < q_count;
       float top = -INFINITY;
       u64 total[4] = {};  // chains of their own
       bool ok = true;
@@ -300,7 +301,9 @@ __global__ void __launch_bounds__(128 * (W + 1), 3 - W) attention_kernel(const _
           for (int e = 0; e < 8; ++e) top8[e] = x + 8 + e < KT ? max3(top8[e], __uint_as_float(s[x + e]), __uint_as_float(s[x + 8 + e])) : fmaxf(top8[e], __uint_as_float(s[x + e]));
         }
         const float most = max3(max3(top8[0], top8[1], top8[2]), max3(top8[3], top8[4], top8[5]), fmaxf(top8[6], top8[7]));
-        const bool raise = most * c > top * c + LAZY;  // (true whenever there is no maximum yet, and some score)
+        // (True whenever there is no maximum yet, and some score.  Rows behind the sequence, the next one's, have no say: a sequence's bits do not depend
+        // on what is packed beside it.)
+        const bool raise = there && most * c > top * c + LAZY;
         if (__any_sync(0xFFFFFFFFu, raise)) {
           const float next = fmaxf(top, most);
           if (j > 0) {
@@ -340,7 +343,6 @@ __global__ void __launch_bounds__(128 * (W + 1), 3 - W) attention_kernel(const _
       float lo, hi;
       unpack2(add2_rn(add2_rn(total[0], total[1]), add2_rn(total[2], total[3])), lo, hi);
       const float sum = lo + hi;
-      const bool there = i < q_count;
       if (there && p.lse)
         p.lse[(int64_t)head * p.q_rows + q_first + i] =
             !ok ? __uint_as_float(0x7FC00000u) : sum == 0.0f ? -INFINITY : (top * c + (log2f(sum) - kUp<T>)) * 0.69314718055994531f;

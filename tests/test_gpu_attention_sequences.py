@@ -1,4 +1,4 @@
-"""Attention, its gradients and the cache over many sequences: each way of finding a row's sequence."""
+"""Attention, its gradients and the cache over many sequences: each way of finding a row's sequence, and neighbours."""
 import numpy as np
 import pytest
 import torch
@@ -98,3 +98,35 @@ def test_one_line_in_very_many_parts(tokens):
     for heads in (1, 12):
         q = _randn(1, heads, D, seed=3)
         close(lba.lba_cache_attention(q, cache, page, table, _ints([tokens])), *cache_ref.attention(q, cache, page, table, [tokens], D ** -0.5))
+
+
+def _alone_and_packed(call, n, heads, D, dtype):
+    """what a call gives of a sequence of n rows alone, and of the same rows with others in front and behind whose scores are far larger"""
+    x = [_randn(n, h, D, seed=s, dtype=dtype) for s, h in enumerate(heads)]
+    for before, behind in ((0, 40), (77, 200), (130, 0)):
+        others = [_randn(before + behind, h, D, seed=9 + i, dtype=dtype) * 8 for i, h in enumerate(heads)]
+        packed = [torch.cat([o[:before], t, o[before:]]) for o, t in zip(others, x)]
+        got = call(packed, _ints([0, before, before + n, before + n + behind]))
+        yield call(x, _ints([0, n])), [t[before:before + n] for t in got]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("n", [1, 31, 100, 129, 300])
+def test_bits_do_not_depend_on_neighbours(n, causal, dtype):
+    def call(x, cu):
+        out, lse = lba.lba_attention(*x, cu, cu, causal=causal, lse=True)
+        return out, lse.T
+    for alone, packed in _alone_and_packed(call, n, (4, 2, 2), 64, dtype):
+        assert all(torch.equal(a, b) for a, b in zip(alone, packed))
+
+
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("n", [1, 31, 100, 129, 300])
+def test_bits_of_gradients_do_not_depend_on_neighbours(n, causal, dtype=torch.bfloat16):
+    def call(x, cu):
+        q, k, v, g = x
+        out, lse = lba.lba_attention(q, k, v, cu, cu, causal=causal, lse=True)
+        return lba.lba_attention_backward(g, q, k, v, out, lse, cu, cu, causal=causal)
+    for alone, packed in _alone_and_packed(call, n, (4, 2, 2, 4), 64, dtype):
+        assert all(torch.equal(a, b) for a, b in zip(alone, packed))
