@@ -142,29 +142,35 @@ __device__ void delta_of_few(const DeltaParams& p, int b, int h, int part, FewSh
   }
 }
 
-// Of `row`'s sequence, the last that begins at or before it, the first row in q and the counts; false for rows of no sequence
+// Of `row`'s sequence the first row in q and the counts; false for rows of no sequence.  A warp, every lane the same arguments and results.
 __device__ __forceinline__ bool ends_of(const DeltaParams& p, int64_t row, int lane, int* q_first, int* q_count, int* k_count) {
-  int b = 0, k_first;
   if (p.cu_q && p.sequences < 32) {  // one trip to memory
-    const int at = min(lane, p.sequences), q = __ldg(p.cu_q + at), k = p.cu_k ? __ldg(p.cu_k + at) : 0;
-    b = __popc(__ballot_sync(0xFFFFFFFFu, lane < p.sequences && q <= row)) - 1;
-    const bool inside = b >= 0 && row < __shfl_sync(0xFFFFFFFFu, q, p.sequences);
-    b = max(b, 0);
+    const int at = min(lane, p.sequences), q = __ldg(p.cu_q + at), k = p.cu_k ? __ldg(p.cu_k + at) : 0, q_next = __shfl_down_sync(0xFFFFFFFFu, q, 1);
+    const unsigned has = __ballot_sync(0xFFFFFFFFu, lane < p.sequences && q <= row && row < q_next);
+    const int b = max(__ffs(has) - 1, 0);
     const int q_top = (int)p.q_rows, k_top = (int)p.k_rows;
     *q_first = min(max(__shfl_sync(0xFFFFFFFFu, q, b), 0), q_top);
     *q_count = max(min(max(__shfl_sync(0xFFFFFFFFu, q, b + 1), 0), q_top) - *q_first, 0);
     const int lo = min(max(__shfl_sync(0xFFFFFFFFu, k, b), 0), k_top), hi = min(max(__shfl_sync(0xFFFFFFFFu, k, b + 1), 0), k_top);
     *k_count = p.cu_k ? max(hi - lo, 0) : k_top;
-    return inside;
+    return has != 0;
   }
   bool inside = true;
+  int b = 0, k_first;
   if (p.cu_q) {
-    inside = row >= p.cu_q[0] && row < p.cu_q[p.sequences];
-    int hi = p.sequences - 1;
+    const auto holds = [&](int x) { return p.cu_q[x] <= row && row < p.cu_q[x + 1]; };
+    int hi = p.sequences - 1;  // the last sequence that begins at or before the row
     while (b < hi) {
       const int mid = (b + hi + 1) / 2;
       if (p.cu_q[mid] <= row) b = mid;
       else hi = mid - 1;
+    }
+    inside = holds(b);
+    // (that is another one where offsets descend: a sequence that ends before it starts)
+    for (int b0 = 0; !inside && b0 < p.sequences; b0 += 32) {
+      const unsigned has = __ballot_sync(0xFFFFFFFFu, b0 + lane < p.sequences && holds(b0 + lane));
+      inside = has != 0;
+      if (inside) b = b0 + __ffs(has) - 1;
     }
   }
   rows_of(p.cu_q, p.q_rows, b, q_first, q_count);

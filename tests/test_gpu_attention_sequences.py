@@ -1,4 +1,4 @@
-"""Attention, its gradients and the cache over many sequences: each way of finding a row's sequence, and neighbours."""
+"""Attention, its gradients and the cache over many sequences: each way of finding a row's sequence, offsets that descend, and neighbours."""
 import numpy as np
 import pytest
 import torch
@@ -44,6 +44,15 @@ def test_attention_and_gradients_of_many_sequences(sequences, causal):
     lq[sequences // 2], lk[sequences // 2] = 150, 300
     cu_q, cu_k = (_ints((np.cumsum([0] + list(n)) + 2).tolist()) for n in (lq, lk))
     _both_directions(lq, lk, cu_q, cu_k, causal, dtype=torch.float16 if sequences % 2 else torch.bfloat16)
+
+
+@pytest.mark.parametrize("many", [0, 40, 200])
+@pytest.mark.parametrize("ends_q,ends_k", [([0, 100, 50], [0, 90, 90]), ([0, 100, 50], [0, 100, 30]), ([40, 140, 20, 20], [7, 60, 0, 0]),
+                                           ([60, 30, 90], [60, 10, 80]), ([0, 100, -5], [0, 100, 70])])
+def test_a_sequence_that_ends_before_it_starts_is_empty(ends_q, ends_k, many):
+    """the others are what they are without it, and rows of none get no gradient, however many (here empty) sequences there are"""
+    ends_q, ends_k = ends_q + [ends_q[-1]] * many, ends_k + [ends_k[-1]] * many
+    _both_directions([140], [140], _ints(ends_q), _ints(ends_k))
 
 
 @pytest.mark.parametrize("requests", [127, 128, 129, 400])
