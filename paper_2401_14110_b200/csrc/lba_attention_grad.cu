@@ -24,7 +24,8 @@
 // p and ds are rounded to the inputs' type on their way into the products, which leaves gradients off by 1.4 times what their own rounding
 // costs; where a CTA walks over one or two tiles of a head, and a few terms may cancel, they have a second piece (over T1, which is then formed late).  delta comes from an output of 16 bits; where few keys are seen, that would add as much again (1.6 times with four keys), so rows
 // of up to 32 keys get theirs from p and dp.  binary16 has few exponents: p is held times 2^8, and ds times a power of two chosen from the
-// largest |grad_out| and |v| so that it cannot overflow.
+// largest finite |grad_out| and |v| so that it cannot overflow: for grad_q of the row's own g and the values up to its block's last key, for the
+// others of the rows from the block's first on that go with its keys.  So neither other sequences nor rows and keys that a mask hides cost it bits.
 #include <cmath>
 
 #include "lba_tile.cuh"
@@ -44,7 +45,8 @@ struct GradParams {
   int sequences, heads, kv_heads, group, dim, causal, bf;
   float to_log2, scale;
   const float2* stats;       // [heads][q_rows]: lse in powers of two, delta
-  const uint32_t* most;      // largest |grad_out|, |v| as bits (binary16), or null
+  const uint32_t *most_g, *most_v;  // see DeltaParams
+  const uint8_t* row_most;
   void *grad_q, *grad_k, *grad_v;
 };
 struct DeltaParams {
@@ -53,13 +55,17 @@ struct DeltaParams {
   const float* lse;
   const int32_t *cu_q, *cu_k;
   int64_t q_rows, k_rows;
-  uint32_t few_blocks;       // of rows of few keys
+  uint32_t few_blocks, value_blocks;  // of rows of few keys; of 128 rows of v in one head (binary16)
   int sequences, heads, kv_heads, dim, causal;
   float to_log2;
   float2* stats;
-  uint32_t* most;
+  // binary16 only: largest finite |grad_out|, |v| of blocks of 128 rows as bits, [block_at][kv_heads]; the exponent byte of a row's |grad_out|, [heads][q_rows]
+  uint32_t *most_g, *most_v;
+  uint8_t* row_most;
   void *grad_q, *grad_k, *grad_v;
 };
+// the place of block t of sequence b, which begins at row `first`, among all sequences' blocks of 128 rows: sequences leave one free at most
+__device__ __forceinline__ int64_t block_at(int first, int b, int t) { return (int64_t)(first / XT) + b + t; }
 
 // ------------------------------------------------------------------ delta
 // A warp takes 8 or 16 heads of a row, 16 lanes each, or 8 where a head has up to 64 values; they and the sequences' ends are on their way at once.  Rows
@@ -142,8 +148,28 @@ __device__ void delta_of_few(const DeltaParams& p, int b, int h, int part, FewSh
   }
 }
 
-// Of `row`'s sequence the first row in q and the counts; false for rows of no sequence.  A warp, every lane the same arguments and results.
-__device__ __forceinline__ bool ends_of(const DeltaParams& p, int64_t row, int lane, int* q_first, int* q_count, int* k_count) {
+// The sequence of a row, or -1.  A warp, every lane the same arguments and results, here and in ends_of.
+__device__ __forceinline__ int sequence_of(const int32_t* cu, int sequences, int64_t row, int lane) {
+  if (!cu) return 0;
+  const auto holds = [&](int x) { return cu[x] <= row && row < cu[x + 1]; };
+  if (sequences >= 32) {
+    int b = 0, hi = sequences - 1;  // the last sequence that begins at or before the row
+    while (b < hi) {
+      const int mid = (b + hi + 1) / 2;
+      if (cu[mid] <= row) b = mid;
+      else hi = mid - 1;
+    }
+    if (holds(b)) return b;
+  }
+  // (that is another one where offsets descend: a sequence that ends before it starts)
+  for (int b0 = 0; b0 < sequences; b0 += 32) {
+    const unsigned has = __ballot_sync(0xFFFFFFFFu, b0 + lane < sequences && holds(b0 + lane));
+    if (has) return b0 + __ffs(has) - 1;
+  }
+  return -1;
+}
+// Of `row`'s sequence, which is returned (-1: none), the first row in q and the counts
+__device__ __forceinline__ int ends_of(const DeltaParams& p, int64_t row, int lane, int* q_first, int* q_count, int* k_count) {
   if (p.cu_q && p.sequences < 32) {  // one trip to memory
     const int at = min(lane, p.sequences), q = __ldg(p.cu_q + at), k = p.cu_k ? __ldg(p.cu_k + at) : 0, q_next = __shfl_down_sync(0xFFFFFFFFu, q, 1);
     const unsigned has = __ballot_sync(0xFFFFFFFFu, lane < p.sequences && q <= row && row < q_next);
@@ -153,44 +179,65 @@ __device__ __forceinline__ bool ends_of(const DeltaParams& p, int64_t row, int l
     *q_count = max(min(max(__shfl_sync(0xFFFFFFFFu, q, b + 1), 0), q_top) - *q_first, 0);
     const int lo = min(max(__shfl_sync(0xFFFFFFFFu, k, b), 0), k_top), hi = min(max(__shfl_sync(0xFFFFFFFFu, k, b + 1), 0), k_top);
     *k_count = p.cu_k ? max(hi - lo, 0) : k_top;
-    return has != 0;
+    return has ? b : -1;
   }
-  bool inside = true;
-  int b = 0, k_first;
-  if (p.cu_q) {
-    const auto holds = [&](int x) { return p.cu_q[x] <= row && row < p.cu_q[x + 1]; };
-    int hi = p.sequences - 1;  // the last sequence that begins at or before the row
-    while (b < hi) {
-      const int mid = (b + hi + 1) / 2;
-      if (p.cu_q[mid] <= row) b = mid;
-      else hi = mid - 1;
-    }
-    inside = holds(b);
-    // (that is another one where offsets descend: a sequence that ends before it starts)
-    for (int b0 = 0; !inside && b0 < p.sequences; b0 += 32) {
-      const unsigned has = __ballot_sync(0xFFFFFFFFu, b0 + lane < p.sequences && holds(b0 + lane));
-      inside = has != 0;
-      if (inside) b = b0 + __ffs(has) - 1;
-    }
+  const int b = sequence_of(p.cu_q, p.sequences, row, lane);
+  int k_first;
+  rows_of(p.cu_q, p.q_rows, max(b, 0), q_first, q_count);
+  rows_of(p.cu_k, p.k_rows, max(b, 0), &k_first, k_count);
+  return b;
+}
+
+// the largest finite magnitude of eight values, as bits
+__device__ __forceinline__ uint32_t largest(const float (&x)[8], uint32_t most) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) most = fabsf(x[e]) < INFINITY ? max(most, __float_as_uint(fabsf(x[e]))) : most;
+  return most;
+}
+// 128 rows of v in one head
+template <typename T>
+__device__ void most_of_values(const DeltaParams& p, uint32_t block) {
+  __shared__ uint32_t warps[DELTA_THREADS / 32];
+  const int h = (int)(block % p.kv_heads), pieces = p.dim / 8;
+  const Place place = find_place(p.cu_q, p.q_rows, p.cu_k, p.k_rows, p.sequences, true, XT, block / p.kv_heads);
+  if (!place.found) return;
+  const int first = place.level * XT, rows = min(XT, place.k_count - first);
+  const T* const src = static_cast<const T*>(p.v) + (int64_t)(place.k_first + first) * p.v_at.token + h * p.v_at.head;
+  uint32_t most = 0;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < rows * pieces; i += DELTA_THREADS) {
+    float v[8];
+    load_half8(src + i / pieces * p.v_at.token + i % pieces * 8, v);
+    most = largest(v, most);
   }
-  rows_of(p.cu_q, p.q_rows, b, q_first, q_count);
-  rows_of(p.cu_k, p.k_rows, b, &k_first, k_count);
-  return inside;
+  most = __reduce_max_sync(0xFFFFFFFFu, most);
+  if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = most;
+  __syncthreads();
+  if (threadIdx.x == 0) {
+    for (int i = 1; i < DELTA_THREADS / 32; ++i) most = max(most, warps[i]);
+    p.most_v[block_at(place.k_first, place.sequence, place.level) * p.kv_heads + h] = most;
+  }
 }
 
 template <typename T, int LANES>  // of a head
 __global__ void __launch_bounds__(DELTA_THREADS, 5) attention_delta_kernel(const DeltaParams p) {
-  constexpr int HEADS = 32 / LANES;  // at a time
+  constexpr int HEADS = 32 / LANES, SLOTS = DELTA_AHEAD * HEADS;  // heads at a time, of a block
+  constexpr bool HALF = std::is_same<T, __half>::value;
   __shared__ FewShared few;
+  __shared__ uint32_t most[DELTA_THREADS / 32][HALF ? SLOTS : 1];
+  __shared__ int64_t most_at[DELTA_THREADS / 32];
   after_previous();
   if (blockIdx.x < p.few_blocks) {
     const uint32_t line = blockIdx.x / FEW_PARTS;
     if (blockIdx.y == 0) delta_of_few<T>(p, (int)(line / p.heads), (int)(line % p.heads), blockIdx.x % FEW_PARTS, few);
     return;
   }
+  if (HALF && blockIdx.x < p.few_blocks + p.value_blocks) {
+    if (blockIdx.y == 0) most_of_values<T>(p, blockIdx.x - p.few_blocks);
+    return;
+  }
   const int lane = threadIdx.x & 31, d = lane % LANES * 8, h0 = blockIdx.y * DELTA_AHEAD * HEADS + lane / LANES;
-  const int64_t row = (int64_t)(blockIdx.x - p.few_blocks) * (DELTA_THREADS / 32) + (threadIdx.x >> 5);
-  uint32_t most_g = 0, most_v = 0;
+  const int64_t row = (int64_t)(blockIdx.x - p.few_blocks - p.value_blocks) * (DELTA_THREADS / 32) + (threadIdx.x >> 5);
   if (row < p.q_rows) {
     const T *const g_row = static_cast<const T*>(p.g) + row * p.heads * p.dim, *const o_row = static_cast<const T*>(p.out) + row * p.heads * p.dim;
     uint4 g[DELTA_AHEAD], o[DELTA_AHEAD];
@@ -204,7 +251,9 @@ __global__ void __launch_bounds__(DELTA_THREADS, 5) attention_delta_kernel(const
       lse[u] = h < p.heads ? __ldg(p.lse + h * p.q_rows + row) : 0.0f;
     }
     int q_first, q_count, k_count;
-    const bool inside = ends_of(p, row, lane, &q_first, &q_count, &k_count);
+    const int b = ends_of(p, row, lane, &q_first, &q_count, &k_count);
+    const bool inside = b >= 0;
+    if (HALF && lane == 0) most_at[threadIdx.x >> 5] = inside ? block_at(q_first, b, ((int)row - q_first) / XT) : -1;
     const int keys = p.causal ? min(k_count, (int)row - q_first + k_count - q_count + 1) : k_count;
 #pragma unroll
     for (int u = 0; u < DELTA_AHEAD; ++u) {
@@ -217,9 +266,13 @@ __global__ void __launch_bounds__(DELTA_THREADS, 5) attention_delta_kernel(const
       widen8(reinterpret_cast<const T*>(&g[u]), x);
       widen8(reinterpret_cast<const T*>(&o[u]), y);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        sum = fmaf(x[e], y[e], sum);
-        most_g = max(most_g, __float_as_uint(x[e]) & 0x7FFFFFFFu);
+      for (int e = 0; e < 8; ++e) sum = fmaf(x[e], y[e], sum);
+      if constexpr (HALF) {
+        uint32_t m = largest(x, 0);
+#pragma unroll
+        for (int e = LANES / 2; e > 0; e /= 2) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, e));
+        if (d == 0) most[threadIdx.x >> 5][u * HEADS + lane / LANES] = m;
+        if (d == 0 && h < p.heads) p.row_most[h * p.q_rows + row] = (uint8_t)(m >> 23);
       }
 #pragma unroll
       for (int e = LANES / 2; e > 0; e /= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, e);
@@ -234,22 +287,23 @@ __global__ void __launch_bounds__(DELTA_THREADS, 5) attention_delta_kernel(const
         *reinterpret_cast<uint4*>(static_cast<T*>(p.grad_k) + row * n + i) = make_uint4(0u, 0u, 0u, 0u);
         *reinterpret_cast<uint4*>(static_cast<T*>(p.grad_v) + row * n + i) = make_uint4(0u, 0u, 0u, 0u);
       }
-    } else if (p.most) {
-      for (int h = lane / LANES; h < p.kv_heads; h += HEADS) {
-        if (d >= p.dim) continue;
-        float v[8];
-        load_half8(static_cast<const T*>(p.v) + row * p.v_at.token + h * p.v_at.head + d, v);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) most_v = max(most_v, __float_as_uint(v[e]) & 0x7FFFFFFFu);
-      }
     }
   }
-  if (p.most) {  // (a maximum does not depend on the order)
-    most_g = __reduce_max_sync(0xFFFFFFFFu, most_g);
-    most_v = __reduce_max_sync(0xFFFFFFFFu, most_v);
-    if (lane == 0) {
-      if (most_g > __ldcg(p.most)) atomicMax(p.most, most_g);
-      if (most_v > __ldcg(p.most + 1)) atomicMax(p.most + 1, most_v);
+  if constexpr (HALF) {  // the rows' largest together, head by head of the key-value heads (a maximum does not depend on the order)
+    if (row >= p.q_rows && lane == 0) most_at[threadIdx.x >> 5] = -1;
+    __syncthreads();
+    const int slot = threadIdx.x, h = blockIdx.y * SLOTS + slot, group = p.heads / p.kv_heads;
+    if (slot < SLOTS && h < p.heads && (slot == 0 || h % group == 0)) {
+      const int heads = min(min(group - h % group, SLOTS - slot), p.heads - h);
+      uint32_t m = 0;
+      for (int w = 0; w < DELTA_THREADS / 32; ++w) {
+        if (most_at[w] < 0) continue;
+        for (int i = 0; i < heads; ++i) m = max(m, most[w][slot + i]);
+        if (w + 1 < DELTA_THREADS / 32 && most_at[w + 1] == most_at[w]) continue;
+        uint32_t* const to = p.most_g + most_at[w] * p.kv_heads + h / group;
+        if (m > __ldcg(to)) atomicMax(to, m);
+        m = 0;
+      }
     }
   }
 }
@@ -260,12 +314,10 @@ __device__ __forceinline__ uint32_t rest_of(float lo, float hi, uint32_t pair) {
   const T* const t = reinterpret_cast<const T*>(&pair);
   return pack_pair<T>(lo - to_f32(t[0]), hi - to_f32(t[1]));
 }
-// the power of two that ds is multiplied by: |ds| <= 2 dim |g| |v| stays below 2^15
-__device__ __forceinline__ int ds_bits(const GradParams& p) {
-  if (!p.most) return 0;
-  const uint32_t g = p.most[0], v = p.most[1];
-  if (g >= 0x7F800000u || v >= 0x7F800000u || g == 0 || v == 0) return 0;
-  return 15 - ((int)(g >> 23) - 126) - ((int)(v >> 23) - 126) - (33 - __clz(p.dim - 1));
+// the power of two that ds is multiplied by, from the exponent bytes of the largest |g| and |v|: |ds| <= 2 dim |g| |v| stays below 2^15
+__device__ __forceinline__ int ds_bits(uint32_t g, uint32_t v, int dim) {
+  if (g == 0 || v == 0) return 0;
+  return 15 - ((int)g - 126) - ((int)v - 126) - (33 - __clz(dim - 1));
 }
 
 // ------------------------------------------------------------------ gradients
@@ -462,10 +514,22 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
   const int w = warp >> 2, thread = threadIdx.x & 127, x = x0 + thread;  // the thread's row of X
   const uint32_t lanes = (uint32_t)(warp & 3) << 21, t1 = tmem + w * YC + lanes;
   const u64 c = both(p.to_log2);
-  const int bits = ds_bits(p);
+  bool ok = true;
+  int bits = 0;
+  if constexpr (std::is_same<T, __half>::value) {
+    const int kv = KEYS ? head : head / p.group;
+    const auto most_of = [&](const uint32_t* most, int first, int from, int to) {
+      uint32_t x = 0;
+      for (int t = from + (threadIdx.x & 31); t < to; t += 32) x = max(x, __ldg(most + block_at(first, place.sequence, t) * p.kv_heads + kv));
+      return __reduce_max_sync(0xFFFFFFFFu, x) >> 23;
+    };
+    // (rows from walk.first on see the keys up to the last)
+    const uint32_t v = most_of(p.most_v, k_first, 0, KEYS ? (k_count + YT - 1) / YT : walk.last);
+    const uint32_t g = KEYS ? most_of(p.most_g, q_first, walk.first, walk.last) : x < x_count ? __ldg(p.row_most + (int64_t)head * p.q_rows + x_first + x) : 0u;
+    bits = ds_bits(g, v, p.dim);
+  }
   const float up = power_of_two(bits - P_BITS);  // of ds, beside the 2^8 of p
   const u64 up2 = both(up);
-  bool ok = true;
   float2 mine = make_float2(0.0f, 0.0f);  // queries: this row's; keys: a column's of the next tile
   int h_ahead = 0, t_ahead = walk.first;  // of the next tile whose statistics are fetched
   const auto stats_ahead = [&] {
@@ -716,6 +780,13 @@ cudaError_t launch_delta(const DeltaParams& d, int64_t blocks, cudaStream_t stre
 }
 
 size_t stats_bytes(const lba_attention_how* h) { return (size_t)h->heads * h->q_rows * sizeof(float2); }
+// blocks of 128 rows as block_at counts them, and bytes of the largest magnitudes of q's and k's
+int64_t blocks_of(const lba_attention_how* h, int64_t rows) { return rows / XT + h->sequences; }
+size_t most_bytes(const lba_attention_how* h) {
+  return h->type == LBA_TYPE_BF16 ? 0 : (size_t)(blocks_of(h, h->q_rows) + blocks_of(h, h->k_rows)) * h->kv_heads * sizeof(uint32_t);
+}
+size_t stats_offset(const lba_attention_how* h) { return (most_bytes(h) + 255) / 256 * 256; }
+size_t row_bytes(const lba_attention_how* h) { return h->type == LBA_TYPE_BF16 ? 0 : (size_t)h->heads * h->q_rows; }
 
 }  // namespace
 }  // namespace lba
@@ -725,7 +796,7 @@ using namespace lba;
 extern "C" {
 
 size_t lba_attention_backward_workspace_bytes(const lba_attention_how* how) {
-  return check_attention(how) == LBA_OK && how->sequences ? 256 + stats_bytes(how) : 0;
+  return check_attention(how) == LBA_OK && how->sequences ? stats_offset(how) + stats_bytes(how) + row_bytes(how) : 0;
 }
 
 int lba_attention_backward(const void* grad_out, const void* q, const void* k, const void* v, const void* out, const float* lse,
@@ -751,8 +822,8 @@ int lba_attention_backward(const void* grad_out, const void* q, const void* k, c
       !head_map(&p.k, p.bf, k, how->k_rows, how->kv_heads, how->dim, how->k_at, YT) ||
       !head_map(&p.v, p.bf, v, how->k_rows, how->kv_heads, how->dim, how->v_at, YT))
     return cuda_fail(cudaErrorInvalidValue);
-  uint32_t* const most = p.bf ? nullptr : static_cast<uint32_t*>(workspace);
-  float2* const stats = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + 256);
+  uint32_t *const most_g = p.bf ? nullptr : static_cast<uint32_t*>(workspace), *const most_v = p.bf ? nullptr : most_g + blocks_of(how, how->q_rows) * how->kv_heads;
+  float2* const stats = reinterpret_cast<float2*>(static_cast<uint8_t*>(workspace) + stats_offset(how));
   DeltaParams d = {};
   d.g = grad_out;
   d.out = out;
@@ -774,12 +845,16 @@ int lba_attention_backward(const void* grad_out, const void* q, const void* k, c
   d.kv_heads = p.kv_heads = how->kv_heads;
   d.dim = p.dim = how->dim;
   d.stats = stats;
-  d.most = most;
+  d.most_g = most_g;
+  d.most_v = most_v;
+  d.row_most = reinterpret_cast<uint8_t*>(stats) + stats_bytes(how);
+  p.row_most = d.row_most;
   d.grad_q = p.grad_q = grad_q;
   d.grad_k = p.grad_k = grad_k;
   d.grad_v = p.grad_v = grad_v;
   p.stats = stats;
-  p.most = most;
+  p.most_g = most_g;
+  p.most_v = most_v;
   p.group = how->heads / how->kv_heads;
   p.causal = how->causal != 0;
   p.to_log2 = how->scale * LOG2E;
@@ -787,10 +862,12 @@ int lba_attention_backward(const void* grad_out, const void* q, const void* k, c
   p.key_blocks = (how->k_rows / XT + how->sequences) * how->kv_heads;
   const int64_t blocks = p.key_blocks + (how->q_rows / XT + how->sequences) * how->heads;
   const int64_t most_rows = how->q_rows > how->k_rows ? how->q_rows : how->k_rows, row_blocks = (most_rows + DELTA_THREADS / 32 - 1) / (DELTA_THREADS / 32);
-  const int64_t few_blocks = (int64_t)how->sequences * how->heads * FEW_PARTS, delta_blocks = row_blocks + few_blocks;
+  const int64_t few_blocks = (int64_t)how->sequences * how->heads * FEW_PARTS, value_blocks = p.bf ? 0 : blocks_of(how, how->k_rows) * how->kv_heads;
+  const int64_t delta_blocks = row_blocks + few_blocks + value_blocks;
   if (delta_blocks > 2147483647LL || blocks > 2147483647LL) return LBA_ERR_SHAPE;
   d.few_blocks = (uint32_t)few_blocks;
-  cudaError_t e = most ? cudaMemsetAsync(most, 0, 8, s) : cudaSuccess;
+  d.value_blocks = (uint32_t)value_blocks;
+  cudaError_t e = most_g ? cudaMemsetAsync(most_g, 0, blocks_of(how, how->q_rows) * how->kv_heads * sizeof(uint32_t), s) : cudaSuccess;
   if (e != cudaSuccess) return status_of(e);
   e = how->dim <= 64 ? (p.bf ? launch_delta<__nv_bfloat16, 8>(d, delta_blocks, s) : launch_delta<__half, 8>(d, delta_blocks, s))
                      : (p.bf ? launch_delta<__nv_bfloat16, 16>(d, delta_blocks, s) : launch_delta<__half, 16>(d, delta_blocks, s));

@@ -147,7 +147,7 @@ __device__ __forceinline__ void rows_of(const int32_t* cu, int64_t rows, int b, 
 }
 // Where a block of `size` rows lies: of a sequence with `blocks` of them, the one with `level` blocks that have less to do (or as much).
 struct Place {
-  int found, level, blocks, q_first, q_count, k_first, k_count;
+  int found, sequence, level, blocks, q_first, q_count, k_first, k_count;
 };
 // Block `index` of all sequences' blocks of their rows of q, or of k; a warp, every lane the same arguments and results.  With up to 128
 // sequences, blocks of high levels come first, whatever their sequence: a launch ends with short ones (seven sequences of 1 to 2003 rows, the
@@ -199,8 +199,13 @@ __device__ __forceinline__ Place find_place(const int32_t* cu_q, int64_t q_rows,
     for (int i = 0; i < MANY; ++i) {
       if (32 * i >= sequences || p.found) continue;
       const unsigned has = __ballot_sync(0xFFFFFFFFu, n[i] > lo);
-      if (rank < __popc(has)) take(x[i], __fns(has, 0, rank + 1));
-      else rank -= __popc(has);
+      if (rank < __popc(has)) {
+        const int l = __fns(has, 0, rank + 1);
+        take(x[i], l);
+        p.sequence = 32 * i + l;
+      } else {
+        rank -= __popc(has);
+      }
     }
     p.level = lo;
     return p;
@@ -218,6 +223,7 @@ __device__ __forceinline__ Place find_place(const int32_t* cu_q, int64_t q_rows,
     if (hit) {
       const int l = __ffs(hit) - 1;
       take(x, l);
+      p.sequence = b0 + l;
       p.level = __shfl_sync(0xFFFFFFFFu, upto, l) - 1 - (int)index;
       return p;
     }
