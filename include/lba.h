@@ -267,7 +267,7 @@ int lba_attention(const void* q, const void* k, const void* v, const lba_attenti
  * [rows][heads][dim].  Sums are formed in a fixed order: a repeated call gives the same bits.  p and ds enter the products rounded to
  * the inputs' type, in two pieces where a sequence's other side has at most 256 rows.  ds of binary16 inputs is multiplied by a power of
  * two on the way, so that small gradients keep their bits: one for each row of grad_q, and for grad_k one for each block of 128 keys of a sequence, from
- * the finite values of the rows and keys that go with them, in blocks of 128.  What infinities of grad_out reach is infinite or NaN.  The workspace is
+ * the finite values of the rows and keys that go with them, in blocks of 128.  What infinities of grad_out reach by these sums is infinite or NaN, and nothing else.  The workspace is
  * 256-byte aligned device memory, holds nothing between calls, and calls that may overlap need one each. */
 size_t lba_attention_backward_workspace_bytes(const lba_attention_how* how);
 int lba_attention_backward(const void* grad_out, const void* q, const void* k, const void* v, const void* out, const float* lse,

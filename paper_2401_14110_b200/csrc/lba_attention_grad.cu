@@ -47,6 +47,7 @@ struct GradParams {
   const float2* stats;       // [heads][q_rows]: lse in powers of two, delta
   const uint32_t *most_g, *most_v;  // see DeltaParams
   const uint8_t* row_most;
+  const void* g_raw;
   void *grad_q, *grad_k, *grad_v;
 };
 struct DeltaParams {
@@ -329,6 +330,7 @@ struct GradShared {
   uint64_t t1, t1_read, t2[2], ds_there, done;
   uint32_t tmem;
   int dead;
+  int odd;                   // values of g that are not finite were taken out of a cut tile
   Place place;
   alignas(16) float minus[2][2][YC], delta[2][2][YC];  // [tile's parity][warpgroup]
 };
@@ -484,26 +486,42 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
       }
     } else {
       // Cut tiles.  Rows behind the sequence become 0 where they are summed over (0 times a neighbour's infinity would be NaN), and so do values of Y1
-      // that are not finite: rows that see them have an lse that is NaN.
-      int cuts = 0, t = walk.first;
+      // that are not finite: rows that see them have an lse that is NaN.  Rows of g that hold such values have a delta that is not finite; where a tile is
+      // cut by the causal mask they are taken out too, and added to the sums of the keys that the row sees at the end.
+      int cuts = 0, t = walk.first, h = 0;
       bool ok = true;
-      const auto clean = [&](uint32_t tile_at, int at_t, bool values, uint64_t& there, uint64_t& clean) {
+      const auto clean = [&](uint32_t tile_at, int at_t, const bool (&values)[YT / 64], uint64_t& there, uint64_t& clean) {
+        bool odd = false;
         ok = ok && mbar_wait(smem_u32(&there), (cuts / CUTS) & 1, dead);
         if (!ok) return;
         uint8_t* const tile = raw_smem + (tile_at - smem_u32(raw_smem));
-        for (int row = threadIdx.x - 10 * 32; row < YT; row += 64) {
+#pragma unroll
+        for (int i = 0; i < YT / 64; ++i) {
+          const int row = threadIdx.x - 10 * 32 + 64 * i;
           if (at_t * YT + row >= y_count) clear_row<BLOCKS>(tile, row);
-          else if (values) keep_finite<T, BLOCKS>(tile, row);
+          else if (values[i]) odd |= keep_finite<T, BLOCKS>(tile, row);
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        if (KEYS && odd) sh.odd = 1;
         mbar_arrive(smem_u32(&clean));
       };
       for (int n = 0; n < all && ok; ++n) {
-        const int at_t = t;
-        if (++t == walk.last) t = walk.first;
+        const int at_t = t, at_h = h;
+        if (++t == walk.last) {
+          t = walk.first;
+          ++h;
+        }
         if (!walk.cut(at_t)) continue;
-        clean(ring1 + (n % Y1_SLOTS) * TILE, at_t, p.causal, sh.cut1[cuts % CUTS], sh.clean1[cuts % CUTS]);
-        if (KEYS) clean(ring2 + (n % Y2_SLOTS) * TILE, at_t, false, sh.cut2[cuts % CUTS], sh.clean2[cuts % CUTS]);
+        bool values[YT / 64], bad_g[YT / 64];
+#pragma unroll
+        for (int i = 0; i < YT / 64; ++i) {
+          const int row = at_t * YT + threadIdx.x - 10 * 32 + 64 * i;
+          values[i] = p.causal;
+          bad_g[i] = KEYS && at_t < walk.low && row < y_count &&
+                     !isfinite(__ldg(p.stats + (int64_t)(head * p.group + at_h) * p.q_rows + y_first + row).y);
+        }
+        clean(ring1 + (n % Y1_SLOTS) * TILE, at_t, values, sh.cut1[cuts % CUTS], sh.clean1[cuts % CUTS]);
+        if (KEYS) clean(ring2 + (n % Y2_SLOTS) * TILE, at_t, bad_g, sh.cut2[cuts % CUTS], sh.clean2[cuts % CUTS]);
         ++cuts;
       }
     }
@@ -680,6 +698,20 @@ __device__ void attention_grad(const GradParams& p, GradShared& sh, uint8_t* raw
 #pragma unroll
         for (int e = 0; e < 32; ++e) o[e] = 0u;
       }
+      if (KEYS && which && sh.odd && x < x_count) {  // what was taken out of g
+        for (int h = 0; h < walk.heads; ++h) {
+          for (int i = max(walk.first * YT, x - off); i < min(walk.low * YT, y_count); ++i) {
+            const int64_t h_at = head * p.group + h;
+            if (isfinite(__ldg(p.stats + h_at * p.q_rows + y_first + i).y)) continue;
+            const T* const src = static_cast<const T*>(p.g_raw) + ((int64_t)(y_first + i) * p.heads + h_at) * p.dim + d;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+              const float v = d + e < p.dim ? to_f32(src[e]) : 0.0f;
+              if (!isfinite(v)) o[e] = __float_as_uint(__uint_as_float(o[e]) + v);
+            }
+          }
+        }
+      }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         uint32_t v[4];
@@ -737,6 +769,7 @@ __global__ void __launch_bounds__(GRAD_THREADS, 1) attention_grad_kernel(const _
     mbar_init(smem_u32(&sh.ds_there), 256);
     mbar_init_fence();
     sh.dead = 0;
+    sh.odd = 0;
   }
   after_previous();
   if (warp == 9) tmem_alloc(smem_u32(&sh.tmem), 512);
@@ -853,6 +886,7 @@ int lba_attention_backward(const void* grad_out, const void* q, const void* k, c
   d.grad_k = p.grad_k = grad_k;
   d.grad_v = p.grad_v = grad_v;
   p.stats = stats;
+  p.g_raw = grad_out;
   p.most_g = most_g;
   p.most_v = most_v;
   p.group = how->heads / how->kv_heads;
