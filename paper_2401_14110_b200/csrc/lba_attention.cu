@@ -26,7 +26,9 @@ namespace {
 
 constexpr int QT = 128, KT = 128, MAX_STAGES = 10, CUT_TILES = 4;
 constexpr float LAZY = 8.0f;  // binades
-template <typename T> constexpr float kUp = std::is_same<T, __half>::value ? 7.0f : 0.0f;  // binades that weights are held above the maximum's
+// binades that weights are held above the maximum's, and what takes them from their sum
+template <typename T> constexpr float kUp = std::is_same<T, __half>::value ? 7.0f : 0.0f;
+template <typename T> constexpr float kDown = std::is_same<T, __half>::value ? 0x1p-7f : 1.0f;
 
 struct ForwardParams {
   CUtensorMap q, k, v;
@@ -345,7 +347,7 @@ __global__ void __launch_bounds__(128 * (W + 1), 3 - W) attention_kernel(const _
       const float sum = lo + hi;
       if (there && p.lse)
         p.lse[(int64_t)head * p.q_rows + q_first + i] =
-            !ok ? __uint_as_float(0x7FC00000u) : sum == 0.0f ? -INFINITY : (top * c + (log2f(sum) - kUp<T>)) * 0.69314718055994531f;
+            !ok ? __uint_as_float(0x7FC00000u) : sum == 0.0f ? -INFINITY : (top * c + log2f(sum * kDown<T>)) * 0.69314718055994531f;
       const float inv = !ok ? __uint_as_float(0x7FC00000u) : sum == 0.0f ? 0.0f : __fdiv_rn(1.0f, sum);
       uint32_t poison = 0;  // of the cut tiles, as one word: any at all?
       if (p.causal) {
