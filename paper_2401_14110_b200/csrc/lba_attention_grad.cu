@@ -26,6 +26,7 @@
 // of up to 32 keys get theirs from p and dp.  binary16 has few exponents: p is held times 2^8, and ds times a power of two chosen from the
 // largest finite |grad_out| and |v| so that it cannot overflow: for grad_q of the row's own g and the values up to its block's last key, for the
 // others of the rows from the block's first on that go with its keys.  So neither other sequences nor rows and keys that a mask hides cost it bits.
+#include <algorithm>
 #include <cmath>
 
 #include "lba_tile.cuh"
@@ -56,6 +57,7 @@ struct DeltaParams {
   const float* lse;
   const int32_t *cu_q, *cu_k;
   int64_t q_rows, k_rows;
+  int few_parts;             // blocks that share a sequence's rows of few keys in one head
   uint32_t few_blocks, value_blocks;  // of rows of few keys; of 128 rows of v in one head (binary16)
   int sequences, heads, kv_heads, dim, causal;
   float to_log2;
@@ -85,9 +87,11 @@ __device__ __forceinline__ void load_half8(const T* src, float (&v)[8]) {
   widen8(reinterpret_cast<const T*>(&raw), v);
 }
 // The rows of a sequence that see few keys, for one head: sum p dp / sum p.  Keys, values and 8 rows at a time lie in shared memory; a warp a row, a key
-// a lane.  Four blocks share the rows, and come before the others.  (One block behind them, with rows read as they were wanted, kept 2 x 4096 rows of
-// 16 heads at 31 us instead of 19.)
-constexpr int FEW_ROWS = DELTA_THREADS / 32, FEW_PARTS = 4, FEW_PITCH = 128 / 8 + 1;  // pieces of 16 bytes from row to row: lanes' pieces lie in different banks
+// a lane.  Four blocks share the rows, which are 32 at most under a causal mask, and come before the others.  (One block behind them, with rows read as they
+// were wanted, kept 2 x 4096 rows of 16 heads at 31 us instead of 19.)  Without a mask they are all rows of a sequence of few keys: so there are as many
+// blocks as leave one eight turns of eight rows, where sequences are of one length, and 64 at most (with four, 8192 rows of 16 heads over 32 keys
+// took 627 us instead of 218, and 65536 took 6800 instead of 1760; over 33 keys, which have none of these blocks, 110 and 820).
+constexpr int FEW_ROWS = DELTA_THREADS / 32, FEW_PARTS = 4, FEW_PARTS_MOST = 64, FEW_TURNS = 8, FEW_PITCH = 128 / 8 + 1;  // pieces of 16 bytes from row to row: lanes' pieces lie in different banks
 struct FewShared {
   uint4 k[FEW_KEYS * FEW_PITCH], v[FEW_KEYS * FEW_PITCH], q[FEW_ROWS * FEW_PITCH], g[FEW_ROWS * FEW_PITCH];
   float lse[FEW_ROWS];
@@ -109,7 +113,7 @@ __device__ void delta_of_few(const DeltaParams& p, int b, int h, int part, FewSh
     }
   };
   const lba_strides g_at = {(int64_t)p.heads * p.dim, p.dim};
-  for (int i0 = first; i0 < last; i0 += FEW_PARTS * FEW_ROWS) {
+  for (int i0 = first; i0 < last; i0 += p.few_parts * FEW_ROWS) {
     const int rows = min(FEW_ROWS, last - i0), i = threadIdx.x >> 5;
     const int64_t row0 = q_first + i0;
     if (i0 == first) {
@@ -229,8 +233,8 @@ __global__ void __launch_bounds__(DELTA_THREADS, 5) attention_delta_kernel(const
   __shared__ int64_t most_at[DELTA_THREADS / 32];
   after_previous();
   if (blockIdx.x < p.few_blocks) {
-    const uint32_t line = blockIdx.x / FEW_PARTS;
-    if (blockIdx.y == 0) delta_of_few<T>(p, (int)(line / p.heads), (int)(line % p.heads), blockIdx.x % FEW_PARTS, few);
+    const uint32_t line = blockIdx.x / p.few_parts;
+    if (blockIdx.y == 0) delta_of_few<T>(p, (int)(line / p.heads), (int)(line % p.heads), blockIdx.x % p.few_parts, few);
     return;
   }
   if (HALF && blockIdx.x < p.few_blocks + p.value_blocks) {
@@ -896,7 +900,9 @@ int lba_attention_backward(const void* grad_out, const void* q, const void* k, c
   p.key_blocks = (how->k_rows / XT + how->sequences) * how->kv_heads;
   const int64_t blocks = p.key_blocks + (how->q_rows / XT + how->sequences) * how->heads;
   const int64_t most_rows = how->q_rows > how->k_rows ? how->q_rows : how->k_rows, row_blocks = (most_rows + DELTA_THREADS / 32 - 1) / (DELTA_THREADS / 32);
-  const int64_t few_blocks = (int64_t)how->sequences * how->heads * FEW_PARTS, value_blocks = p.bf ? 0 : blocks_of(how, how->k_rows) * how->kv_heads;
+  const int64_t turns = how->causal ? 0 : how->q_rows / how->sequences / FEW_ROWS;
+  d.few_parts = (int)std::min<int64_t>(std::max<int64_t>(turns / FEW_TURNS, FEW_PARTS), FEW_PARTS_MOST);
+  const int64_t few_blocks = (int64_t)how->sequences * how->heads * d.few_parts, value_blocks = p.bf ? 0 : blocks_of(how, how->k_rows) * how->kv_heads;
   const int64_t delta_blocks = row_blocks + few_blocks + value_blocks;
   if (delta_blocks > 2147483647LL || blocks > 2147483647LL) return LBA_ERR_SHAPE;
   d.few_blocks = (uint32_t)few_blocks;

@@ -55,6 +55,13 @@ def test_a_sequence_that_ends_before_it_starts_is_empty(ends_q, ends_k, many):
     _both_directions([140], [140], _ints(ends_q), _ints(ends_k))
 
 
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("lq,lk", [([5000], [32]), ([5000], [33]), ([2000, 3, 700], [31, 9, 40]), ([4100], [1])])
+def test_many_queries_over_few_keys(lq, lk, dtype):
+    cu_q, cu_k = (_ints(np.cumsum([0] + n).tolist()) for n in (lq, lk))
+    _both_directions(lq, lk, cu_q, cu_k, causal=False, H=3, G=1, D=64, dtype=dtype)
+
+
 @pytest.mark.parametrize("requests", [127, 128, 129, 400])
 def test_cache_attention_of_many_requests(requests):
     """lengths of 0 at the borders of what a warp knows at a time, at the start and at the end"""
