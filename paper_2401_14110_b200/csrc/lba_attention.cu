@@ -12,7 +12,8 @@
 //   a warp           one thread issues all products
 //   two warps        clean tiles of V that the mask cuts: rows behind the sequence become 0 (0 times a neighbour's infinity would be NaN),
 //                    and values that are not finite, which rows before them must not see, are taken out and added to the others' results
-// A prompt of 8192 tokens, 32 heads of 128, takes 461 us in a burst (1.19 PFLOP/s, 70% of the matrix peak) and 533 us under the power limit;
+// A prompt of 8192 tokens, 32 heads of 128, takes 530 us in a steady run, under the power limit (1.04 PFLOP/s), and 461 us in a burst
+// (1.19, 70% of the matrix peak);
 // short sequences are bound by what a CTA does once: some 9 us for its place, its first copies and products, and its rows' way out.
 // Weights are rounded to the inputs' type (2^-9 or 2^-12 of each, at random; the result is rounded to that type once more); sums of weights
 // are of the unrounded ones.  binary16 has few exponents: weights are held 2^7 above the maximum's, so that with the 2^8 by which a score may exceed it
@@ -62,7 +63,7 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return d;
 }
 // weights of 32 scores, relative to the maximum: packed, and their sum.  (A quarter of the exponentials as polynomials on the FMA units was slower:
-// a prompt of 8192 took 481 us instead of 461, and 540 instead of 520 at the power limit.)
+// a prompt of 8192 took 540 us instead of 520 in a steady run, 481 instead of 461 in a burst.)
 template <typename T>
 __device__ __forceinline__ void weigh32(const uint32_t* s, uint32_t* out, u64 by, u64 minus, u64 (&sum)[4]) {
 #pragma unroll
@@ -276,7 +277,7 @@ __global__ void __launch_bounds__(128 * (W + 1), 3 - W) attention_kernel(const _
       const uint32_t lanes = (uint32_t)(warp & 3) << 21, s_at = tmem + w * KT + lanes, o_at = tmem + (W + w) * 128 + lanes;
       const float c = p.to_log2, out_scale = p.codes ? __ldg(p.out_scale) : 1.0f;  // (fetched here: at the end every block would wait for it)
       const bool there = i < q_count;
-      float top = -INFINITY;
+      float top = there ? -INFINITY : INFINITY;  // (rows behind the sequence, the next one's, never raise: bits do not depend on what is packed beside it)
       u64 total[4] = {};  // chains of their own
       bool ok = true;
       for (int j = 0; j < mine; ++j) {
@@ -303,9 +304,7 @@ __global__ void __launch_bounds__(128 * (W + 1), 3 - W) attention_kernel(const _
           for (int e = 0; e < 8; ++e) top8[e] = x + 8 + e < KT ? max3(top8[e], __uint_as_float(s[x + e]), __uint_as_float(s[x + 8 + e])) : fmaxf(top8[e], __uint_as_float(s[x + e]));
         }
         const float most = max3(max3(top8[0], top8[1], top8[2]), max3(top8[3], top8[4], top8[5]), fmaxf(top8[6], top8[7]));
-        // (True whenever there is no maximum yet, and some score.  Rows behind the sequence, the next one's, have no say: a sequence's bits do not depend
-        // on what is packed beside it.)
-        const bool raise = there && most * c > top * c + LAZY;
+        const bool raise = most * c > top * c + LAZY;  // (true whenever there is no maximum yet, and some score)
         if (__any_sync(0xFFFFFFFFu, raise)) {
           const float next = fmaxf(top, most);
           if (j > 0) {

@@ -17,12 +17,14 @@
 // as soon as T1(n) is in registers, and scores are there before the warpgroups want them.  Where the sums leave room in tensor memory (queries; heads
 // of up to 64) there is a second T2, and T2(n+1) is formed ahead too; else it follows acc1(n) and acc2(n) while the warpgroups form p of tile n+1.  (With
 // p over T1, T1(n+1) came after acc2(n): 3500 clocks a tile.  With p in shared memory there is room for two tiles of Y1 only, and their copies came late: 4200.)
-// 2 x 4096 tokens, 16 heads and 4 key-value heads of 128, causal, both launches: 397 us, 0.87 PFLOP/s of the five products.
+// 2 x 4096 tokens, 16 heads and 4 key-value heads of 128, causal, both launches: 470 us in a steady run, under the power limit (0.73 PFLOP/s of the
+// five products), 408 in a burst.  binary16, whose maxima the first launch forms as well: 435.
 // (Tiles of 64 rows, two of them in flight, a warpgroup each: with 64 columns a product wants 192 bytes of shared memory a clock, or 128 of
 // tensor memory, and took 57 clocks a step instead of 32; 2 x 4096 tokens of 16 heads took 515 us.)
 //
 // p and ds are rounded to the inputs' type on their way into the products, which leaves gradients off by 1.4 times what their own rounding
-// costs; where a CTA walks over one or two tiles of a head, and a few terms may cancel, they have a second piece (over T1, which is then formed late).  delta comes from an output of 16 bits; where few keys are seen, that would add as much again (1.6 times with four keys), so rows
+// costs; where a CTA walks over one or two tiles of a head, and a few terms may cancel, they have a second piece (over T1, which is then formed late).
+// delta comes from an output of 16 bits; where few keys are seen, that would add as much again (1.6 times with four keys), so rows
 // of up to 32 keys get theirs from p and dp.  binary16 has few exponents: p is held times 2^8, and ds times a power of two chosen from the
 // largest finite |grad_out| and |v| so that it cannot overflow: for grad_q of the row's own g and the values up to its block's last key, for the
 // others of the rows from the block's first on that go with its keys.  So neither other sequences nor rows and keys that a mask hides cost it bits.

@@ -147,7 +147,7 @@ __device__ __forceinline__ void rows_of(const int32_t* cu, int64_t rows, int b, 
 }
 // Where a block of `size` rows lies: of a sequence with `blocks` of them, the one with `level` blocks that have less to do (or as much).
 struct Place {
-  int found, sequence, level, blocks, q_first, q_count, k_first, k_count;
+  int found, level, blocks, q_first, q_count, k_first, k_count, sequence;
 };
 // Block `index` of all sequences' blocks of their rows of q, or of k; a warp, every lane the same arguments and results.  With up to 128
 // sequences, blocks of high levels come first, whatever their sequence: a launch ends with short ones (seven sequences of 1 to 2003 rows, the
