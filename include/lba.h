@@ -247,7 +247,8 @@ int lba_rotary(const void* q, lba_strides q_at, const void* k, lba_strides k_at,
  * Rows of q in no sequence are left as they were in out and lse, and are 0 in the gradients.  Offsets outside [0, rows] count as the
  * nearer end, a sequence that ends before it starts is empty; sequences follow each other in memory.
  * Scores, weights and sums are binary32; in the second product a weight is rounded to the inputs' type, 8 or 11 bits (binary16: those below
- * 2^-21 of the row's largest to 2^-32 of that). */
+ * 2^-21 of the row's largest to 2^-32 of that).  Weights of up to 2^8 are summed before they are divided by their sum, so values above
+ * 2^119 / keys may overflow.  A sequence's bits do not depend on the others of a call. */
 typedef struct {
   int32_t type;         /* LBA_TYPE_BF16 or F16: of q, k, v and what has their shapes                 */
   int32_t heads, kv_heads, dim; /* heads a multiple of kv_heads; dim a multiple of 8, 8..128            */
@@ -255,7 +256,7 @@ typedef struct {
   float scale;          /* finite and > 0                                                             */
   int64_t q_rows, k_rows; /* below 2^31 - 1024                                                          */
   const int32_t *cu_q, *cu_k; /* device, [sequences + 1] each; NULL: one sequence of all rows           */
-  lba_strides q_at, k_at, v_at; /* multiples of 8, as the tensors start at multiples of 16 bytes         */
+  lba_strides q_at, k_at, v_at; /* multiples of 8 above 0 wherever there are two heads or rows, as the tensors start at multiples of 16 bytes */
 } lba_attention_how;
 /* out [q_rows][heads][dim], contiguous: of the inputs' type, or (out_type LBA_TYPE_CODES) codes of out / *out_scale, E4M3 or with
  * LBA_FLAG_INPUT_M4E3 in out_flags M4E3, as lba_linear gives them; lse [heads][q_rows], or NULL */
@@ -265,10 +266,11 @@ int lba_attention(const void* q, const void* k, const void* v, const lba_attenti
  *     grad_q[i] = scale sum_j ds_ij k[j]     grad_k[j] = scale sum_i ds_ij q[i]     grad_v[j] = sum_i p_ij g[i]
  * the latter two also over the query heads of a group.  out and lse are the forward call's.  grad_out, out and the gradients are contiguous
  * [rows][heads][dim].  Sums are formed in a fixed order: a repeated call gives the same bits.  p and ds enter the products rounded to
- * the inputs' type, in two pieces where a sequence's other side has at most 256 rows.  ds of binary16 inputs is multiplied by a power of
- * two on the way, so that small gradients keep their bits: one for each row of grad_q, and for grad_k one for each block of 128 keys of a sequence, from
- * the finite values of the rows and keys that go with them, in blocks of 128.  What infinities of grad_out reach by these sums is infinite or NaN, and nothing else.  The workspace is
- * 256-byte aligned device memory, holds nothing between calls, and calls that may overlap need one each. */
+ * the inputs' type (p of binary16 inputs to 2^-33 at least), in two pieces where a sequence's other side has at most 256 rows.  ds of
+ * binary16 inputs is multiplied by a power of two on the way, so that small gradients keep their bits: one for each row of grad_q, and for
+ * grad_k one for each block of 128 keys of a sequence, from the finite values of the rows and keys that go with them, in blocks of 128.
+ * What infinities of grad_out reach by these sums is infinite or NaN, and nothing else.  The workspace is 256-byte aligned device memory,
+ * holds nothing between calls, and calls that may overlap need one each. */
 size_t lba_attention_backward_workspace_bytes(const lba_attention_how* how);
 int lba_attention_backward(const void* grad_out, const void* q, const void* k, const void* v, const void* out, const float* lse,
                            const lba_attention_how* how, void* grad_q, void* grad_k, void* grad_v, void* workspace,
@@ -292,7 +294,7 @@ typedef struct {
   const int32_t* table; /* device, [sequences][table_width]                                           */
 } lba_cache;
 /* Row i of sequence b in k and v (row cu[b] + i; cu [sequences + 1], or NULL: one row each) is token start[b] + i; rows in no sequence are
- * passed over.  No two of a call's rows may be the same token of the same page.  Types LBA_TYPE_F32, BF16 or F16.
+ * passed over.  cu does not descend.  No two of a call's rows may be the same token of the same page.  Types LBA_TYPE_F32, BF16 or F16.
  * lba_cache_read writes [tokens][kv_heads][dim], contiguous, and leaves rows in no sequence as they were. */
 int lba_cache_append(const lba_cache* cache, const void* k, lba_strides k_at, const void* v, lba_strides v_at, int type,
                      int64_t tokens, const int32_t* start, const int32_t* cu, void* stream);
@@ -300,10 +302,13 @@ int lba_cache_read(const lba_cache* cache, const int32_t* start, const int32_t* 
                    void* stream);
 /* One new token of each sequence: out[b][h] = softmax(scale q[b][h] k) v over the first lengths[b] tokens of the cache (0 for none);
  * q [sequences][heads][dim] of LBA_TYPE_BF16 or F16 with row stride q_at.token; out as lba_attention's, [sequences][heads][dim];
- * scale finite and > 0.  Scores, weights and sums are binary32.  A weight p enters the second product rounded to 11 bits, or by 2^-20 of
- * the largest weight times the largest value beside it (of its group of 32): each token adds at most (2^-11 p) |v| and that much to an error.
- * Values may be of any sizes: tokens whose powers of two lie outside 16 binades are weighed in binary32, at some seven times the time for
- * their sequence's head, and count down to 2^-126 of the largest.  Workspace as for lba_attention_backward. */
+ * scale finite and > 0.  A query head enters the first product in binary16, held relative to its largest value: values below 2^-17 of that
+ * lose bits, those below 2^-25 count as 0.  Scores, weights and sums are binary32.  A weight p enters the second product rounded to 11
+ * bits, or by 2^-20 of the largest weight times the largest value beside it (of its group of 32): each token adds at most (2^-11 p) |v| and
+ * that much to an error.  Values may be of any sizes: tokens whose powers of two lie outside 16 binades are weighed in binary32, at some
+ * seven times the time for their sequence's head, and count down to 2^-126 of the largest.  A sequence's sum is formed in parts that the
+ * lengths of all sequences of the call decide, so its last bits may depend on them; a repeated call gives the same bits.  Workspace as for
+ * lba_attention_backward. */
 size_t lba_cache_attention_workspace_bytes(const lba_cache* cache, int heads);
 int lba_cache_attention(const void* q, lba_strides q_at, int type, int heads, const lba_cache* cache, const int32_t* lengths,
                         float scale, int out_type, const float* out_scale, int out_flags, void* out, void* workspace,

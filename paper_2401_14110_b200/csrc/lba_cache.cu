@@ -1,8 +1,8 @@
 // A key-value cache in 4 bits: what is appended is rounded to E2M1 values under a power of two per 32 (include/lba.h has the layout), and
 // the attention of single tokens reads it as it lies.
 //
-// Attention wants 136 bytes of memory and 512 g multiply-adds for a (token, head) of 128 dimensions, g being the query heads that share it.
-// Eight heads together are 190 TFLOP/s at 6.4 TB/s, out of reach of the CUDA cores, so both products run on the tensor cores, and a warp
+// Attention wants 136 bytes of memory and 256 g multiply-adds, 512 g operations, for a (token, head) of 128 dimensions, g being the query heads that
+// share it.  Eight heads together are 190 TFLOP/s at 6.4 TB/s, out of reach of the CUDA cores, so both products run on the tensor cores, and a warp
 // feeds them from registers: m16n8k16 with 16 tokens (keys) or 16 dimensions (values) as rows and eight query heads as columns.  tcgen05
 // would have a tile of 128 rows and operands in shared memory, where 4-bit values would have to be widened first.
 //   S = K Q^T   E2M1 values are exact in binary16 (one conversion instruction for two).  The bytes of a key row stand so that a lane's 16
@@ -14,12 +14,13 @@
 //               differ by token and group, so P is multiplied by them, relative to one that the warp's first steps with a line have set.  16
 //               binades around it are binary16's to tell apart (2^-12 of a weight); once any token's power of two lies outside, weights
 //               and values of that line are multiplied in binary32, token by token (740 us instead of 109 for the 48 requests below)
-// A query head is brought to [1, 2) by a power of two first and is then exact in binary16 but for what lies 2^-14 below its largest value.
+// A query head is brought to [1, 2) by a power of two first and is then exact in binary16 but for what lies 2^-17 (binary16 queries: 2^-14) below
+// its largest value.
 // A warp has two units of 64 tokens in shared memory, one that it computes and one on its way by bulk copies, and meets no other warp.  What
-// bounds it now is the widening: some 290 instructions for 16 tokens of 128 dimensions and four heads, half of them conversions and byte moves on
-// one pipe, while the copies are waited for in 4% of the time.  48 requests of up to 16384 tokens, 8 heads of 128, 4 query heads each: 107 us,
-// 4.0 TB/s.  (With loads straight to registers, two steps ahead, 140 us; 8 or 16 warps instead of 12, units of 32 tokens, three units or steps
-// one by one: 109 to 130 us.)
+// bounds it now is the latency of a warp's own chain from load to second product, with three warps a scheduler to hide it: some 290 instructions for
+// 16 tokens of 128 dimensions and four heads, issue slots 55% busy, the busiest pipe 51% (conversions, byte moves), while the copies are waited for
+// in 4% of the time.  48 requests of up to 16384 tokens, 8 heads of 128, 4 query heads each: 106 us, 4.0 TB/s.  (With loads straight to registers, two
+// steps ahead, 140 us; 8 or 16 warps instead of 12, units of 32 tokens, three units or steps one by one: 109 to 130 us.)
 #include <cmath>
 
 #include "lba_async.cuh"
@@ -85,8 +86,9 @@ __device__ __forceinline__ bool locate(const P& p, const int32_t* cu_shared, int
 }
 
 // A lane takes eight neighbouring values, a quarter of a group; a warp a few tokens (those of 32 / (D / 8) rows), whose places it looks up once, and
-// walks over heads, a key and a value row of each token at a time and the next head's on their way.  Bound by memory: 12000 tokens of 8 heads of
-// 128 are appended and read back, 111 MB, in 34 us.  (With a block of 16 tokens for each head that looked up its own tokens 41 us, three quarters of it issue slots.)
+// walks over heads, a key and a value row of each token at a time and the next head's on their way.  Bound by rounding's instructions (issue
+// slots 74% busy): 12000 tokens of 8 heads of 128 are appended and read back, 111 MB, in 34 us, half the memory's rate.  (With a block of 16
+// tokens for each head that looked up its own tokens 41 us, three quarters of it issue slots.)
 template <int D> constexpr int kRowSplit = D / 8;
 template <int D> constexpr int kWarpRows = 32 / kRowSplit<D>;
 
