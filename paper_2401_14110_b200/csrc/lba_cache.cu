@@ -754,8 +754,8 @@ __global__ void __launch_bounds__(DEC_THREADS, 1) cache_attention_kernel(const D
         top = max_bytes(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
         top = max_bytes(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
         uint32_t by = 0;  // binades by which the edge rises, and outputs with it
+        constexpr uint32_t GROUP_BYTES = 0xFFFFFFFFu >> (8 * (4 - NG));
         if (edge == 0) {
-          constexpr uint32_t GROUP_BYTES = 0xFFFFFFFFu >> (8 * (4 - NG));
           edge = __vminu4(__vmaxu4(__vaddus4(top, 0x01010101u * EDGE_ABOVE), 0x10101010u), 0xFEFEFEFEu) & GROUP_BYTES;
           base = (0x40404040u & GROUP_BYTES) - 4u * edge;
           wide = 0;
@@ -768,7 +768,26 @@ __global__ void __launch_bounds__(DEC_THREADS, 1) cache_attention_kernel(const D
               wide |= edge - ve[x][i];
             }
         }
-        by_token = by_token || __any_sync(0xFFFFFFFFu, (wide & 0xF0F0F0F0u) != 0);
+        if (!by_token && __any_sync(0xFFFFFFFFu, (wide & 0xF0F0F0F0u) != 0)) {
+          // groups of zeros (exponent byte 1, or 0 where nothing was written) go with any power of two
+          wide = 0;
+#pragma unroll
+          for (int x = 0; x < BATCH; ++x)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const uint8_t* const codes = unit + U::VALUES + (first + x * STEP + 2 * c + ((i & 1) ^ swap) + (i >> 1) * 8) * (D / 2) + r * (D / 16);
+              uint32_t used = 0;
+#pragma unroll
+              for (int g = 0; g < NG; ++g)
+                if ((codes[2 * g] | codes[2 * g + 1]) & 0x77u) used |= 255u << (8 * g);
+#pragma unroll
+              for (int d = 4; d < 32; d *= 2) used |= __shfl_xor_sync(0xFFFFFFFFu, used, d);
+              const uint32_t zero = __vcmpleu4(ve[x][i], 0x01010101u) & ~used & GROUP_BYTES;
+              ve[x][i] = (ve[x][i] & ~zero) | (edge & zero);
+              wide |= edge - ve[x][i];
+            }
+          by_token = __any_sync(0xFFFFFFFFu, (wide & 0xF0F0F0F0u) != 0);
+        }
         if (by_token) {
           top = max_bytes(top, edge);
           by = top - edge;

@@ -88,6 +88,18 @@ def test_sizes_and_weights_at_random(spread, dim, heads, kv):
         _check((_randn(3, heads, dim, seed=5) * size).to(torch.bfloat16), ks, vs, scale=1.0)
 
 
+@pytest.mark.parametrize("dim", [32, 64, 96, 128])
+@pytest.mark.parametrize("heads", [1, 8, 16])
+@pytest.mark.parametrize("size", [1.0, 2.0 ** -124])
+def test_groups_of_zeros_among_others(size, heads, dim):
+    """a first token of zeros, others here and there and single groups, -0 among them; beside values of any size, and of a size that has the exponent byte of zeros"""
+    n = 700
+    k, v = _randn(n, 1, dim, seed=1), _randn(n, 1, dim, seed=2) * size
+    k[0], v[0] = 0.0, 0.0
+    v[200], v[333], v[96:130], v[5::50, :, :32], v[400] = 0.0, -0.0, 0.0, 0.0, 6 * 2.0 ** -127
+    _check(_randn(1, heads, dim, seed=3, dtype=torch.bfloat16), [k], [v], scale=0.5)
+
+
 def test_other_requests_do_not_matter():
     """a request with large values of small weight, alone and among others that change the warps' shares"""
     n, dim = 500, 64
