@@ -12,8 +12,9 @@
 //               reduction of most steps
 //   O = V^T P   P goes from accumulator to operand layout by the matrix transpose, with 9 bits of headroom below; the values' powers of two
 //               differ by token and group, so P is multiplied by them, relative to one that the warp's first steps with a line have set.  16
-//               binades around it are binary16's to tell apart (2^-12 of a weight); once any token's power of two lies outside, weights
-//               and values of that line are multiplied in binary32, token by token (740 us instead of 109 for the 48 requests below)
+//               binades around it are binary16's to tell apart (2^-12 of a weight); once any token's power of two lies outside (of a
+//               group that is not all zeros), weights and values of that line are multiplied in binary32, token by token (740 us instead
+//               of 107 for the 48 requests below)
 // A query head is brought to [1, 2) by a power of two first and is then exact in binary16 but for what lies 2^-17 (binary16 queries: 2^-14) below
 // its largest value.
 // A warp has two units of 64 tokens in shared memory, one that it computes and one on its way by bulk copies, and meets no other warp.  What
