@@ -304,9 +304,9 @@ int lba_cache_read(const lba_cache* cache, const int32_t* start, const int32_t* 
  * q [sequences][heads][dim] of LBA_TYPE_BF16 or F16 with row stride q_at.token; out as lba_attention's, [sequences][heads][dim];
  * scale finite and > 0.  A query head enters the first product in binary16, held relative to its largest value: values below 2^-17 of that
  * lose bits, those below 2^-25 count as 0.  Scores, weights and sums are binary32.  A weight p enters the second product rounded to 11
- * bits, or by 2^-19 of the largest weight times the largest value beside it (of its group of 32): each token adds at most (2^-11 p) |v| and
- * that much to an error.  Values may be of any sizes: tokens whose powers of two lie outside 16 binades are weighed in binary32, at some
- * seven times the time for their sequence's head, and count down to 2^-126 of the largest.  A sequence's sum is formed in parts that the
+ * bits; where that is more, a token's p v is off by up to 2^-19 of the largest weight times the smallest group's maximum of |v| (of 32
+ * values, zeros apart).  Values may be of any sizes: tokens whose powers of two lie outside 16 binades are weighed in binary32, at
+ * some seven times the time for their sequence's head, and count down to 2^-126 of the largest.  A sequence's sum is formed in parts that the
  * lengths of all sequences of the call decide, so its last bits may depend on them; a repeated call gives the same bits.  Workspace as for
  * lba_attention_backward. */
 size_t lba_cache_attention_workspace_bytes(const lba_cache* cache, int heads);

@@ -7,8 +7,9 @@ from .block_ref import HALF, LEAST, cache_values
 def attention(q, cache, page, table, lengths, scale):
     """(out, bound).  Keys and values are exact, and so are scores but for binary32: D products and their sum, by instructions that cut (2^-23 each), and
     queries in binary16 beside their head's largest value.  A weight and its sum are off by that twice; the weight is then rounded to binary16 (2^-11), or
-    where its product with the power of two of the value's group falls below binary16's normal numbers by 2^-25 of 2^9 of the largest weight: the groups
-    that are treated so span 16 binades, so that is 2^-34 of the largest weight times 2^15 of its value's group, 1.5 times for 6 beside 4."""
+    where its product with the power of two of the value's group falls below binary16's normal numbers by 2^-25 of 2^9 of the largest weight, relative to a
+    power of two 2^14 above that of the least group that is not all zeros: with codes of up to 6, where that group's largest is 3 or more, 2^-25 2^-9 2^14 6/3
+    = 2^-19 of the largest weight times that largest value, or of what the token with the largest weight has, for each token."""
     B, H, D = q.shape
     keys, values = (t.cuda() for t in cache_values(cache.cpu(), page, D))
     out = torch.zeros(B, H, D, dtype=torch.float64, device="cuda")
@@ -30,7 +31,8 @@ def attention(q, cache, page, table, lengths, scale):
             p = torch.softmax(s, 0)
             v = V[:, g]
             largest = v.abs().view(len(pos), D // 32, 32).amax(2)
-            floor = len(pos) * 1.5 * 2.0 ** -20 * (p @ largest).repeat_interleave(32)
+            least = torch.where(largest > 0, largest, torch.inf).amin(0).nan_to_num(posinf=0.0)
+            floor = len(pos) * 2.0 ** -19 * torch.maximum(p @ largest, p.max() * least).repeat_interleave(32)
             out[b, h] = p @ v
             bound[b, h] = HALF[q.dtype] * out[b, h].abs() + (2.0 ** -11 + 2 * off + (len(pos) + 64) * 2.0 ** -23) * (p @ v.abs()) + LEAST[q.dtype] + floor
     return out, bound
